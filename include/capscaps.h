@@ -1,5 +1,6 @@
 /*
- * capscaps -- capsule convolution (forward and backward pass) on AMD MI355X (gfx950).  C ABI.
+ * capscaps -- capsule convolution (forward and backward pass), and what trains and serves a stack of such layers
+ * around it (block norms, gradient norm, AdamW), on AMD MI355X (gfx950).  C ABI.
  *
  * The operator (paper Sec. 1.2 and Algorithm 2, "General capsule convolution"; 3-D capsules
  * as in Fig. 2): for every image n, output pixel (x, y), output channel m and leading capsule
@@ -274,6 +275,160 @@ int capscaps_scheme2_fwd(const void* input, const void* kernel, void* out, const
                          size_t index_bytes, int N, int H, int W, int C, int M, int kh, int kw,
                          int stride, int pad, int D0, int D1, int D2, int D3, int dtype,
                          void* stream);
+
+/*
+ * Around a block of layers: the norm before it, the norm after it, its gate and the residual stream it is added
+ * to, in one pass.  Rows of `width` consecutive values are normalised by their root mean square; a row is whatever
+ * the caller makes one: all capsules of a pixel (width = C*D0*D1*D2) or one capsule (width = D0*D1*D2).
+ * With x the residual stream and b the block's result, for every row:
+ *
+ *     u = b * rstd_post * post_weight          rstd_post = 1 / sqrt(mean(b^2) + eps)   (post_norm = 0: u = b)
+ *     y = residual_scale * x + branch_scale * act(gate) * u                            (the residual stream after the block)
+ *     h = y * rstd_pre * pre_weight            rstd_pre = 1 / sqrt(mean(y^2) + eps)    (the next block's input)
+ *
+ * Everything is computed in fp32; y and h are rounded to nearest even once, at the store, and h is computed from the
+ * unrounded y.  Weights are fp32 vectors of `width` values (NULL = ones).
+ *
+ * Element types: `dtype` is that of the layers around (h, dh, dbranch, a full gate and its gradient);
+ * `stream_dtype` (x, y, dy, dx) and `branch_dtype` (b) are each fp32 or `dtype`.
+ * Pointers are device pointers, aligned to their elements (whole 16-byte vectors are fastest); row r of a tensor with
+ * stride s begins at element r*s.  Strides of inputs are >= 0, of outputs >= width where there is more than one row.
+ * Outputs do not overlap inputs or each other, with one exception: y may be x (same pointer and stride).  Stream and
+ * error rules as for the calls above; what a row's infinities, NaN, or squares past the largest float make of it (NaN, or
+ * zeros) stays in that row, but for sums over rows.
+ */
+#define CAPSCAPS_GATE_NONE 0
+#define CAPSCAPS_GATE_SHARED 1 /* one fp32 vector of `width` values for all rows (a learned scale) */
+#define CAPSCAPS_GATE_FULL 2   /* a value of type `dtype` for every value of b */
+#define CAPSCAPS_ACT_LINEAR 0  /* act(g) = g */
+#define CAPSCAPS_ACT_SIGMOID 1 /* 1 / (1 + exp(-g)) */
+#define CAPSCAPS_ACT_SILU 2    /* g / (1 + exp(-g)) */
+typedef struct capscaps_block {
+    long long rows;
+    int width;
+    int dtype, stream_dtype, branch_dtype;
+    int post_norm;      /* 0 or 1 */
+    int gate, gate_act; /* CAPSCAPS_GATE_*, CAPSCAPS_ACT_* */
+    float residual_scale, branch_scale;
+    float eps; /* > 0 */
+} capscaps_block;
+
+/*
+ * Forward.  branch = NULL: there is no block before (the first norm of a network); y = x then, h comes from it, and
+ * post_norm, gate and the scales are not used (gate must be CAPSCAPS_GATE_NONE).  y = NULL or h = NULL: not
+ * wanted (one of them must be; y needs a branch).  rstd_pre, rstd_post: `rows` floats each for the backward pass,
+ * or NULL.  One row is as good as many.  No workspace, one launch.
+ */
+typedef struct capscaps_block_fwd_args {
+    const void *x, *branch, *gate;
+    const float *pre_weight, *post_weight;
+    void *y, *h;
+    float *rstd_pre, *rstd_post;
+    long long x_stride, branch_stride, gate_stride, y_stride, h_stride;
+} capscaps_block_fwd_args;
+int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fwd_args* args, void* stream);
+
+/*
+ * Backward.  Given the y that the forward pass stored, its statistics, and the gradients dh and dy of h and y (either
+ * may be NULL = zero, not both):
+ *
+ *     d       = dy + rstd_pre * (dh * pre_weight - yn * mean(dh * pre_weight * yn))      yn = y * rstd_pre
+ *     dx      = residual_scale * d                    dpre_weight  = sum over rows of dh * yn
+ *     t       = branch_scale * d                      dgate        = t * u * act'(gate)        (SHARED: summed over rows)
+ *     e       = t * act(gate) * post_weight           dpost_weight = sum over rows of t * act(gate) * bn
+ *     dbranch = rstd_post * (e - bn * mean(e * bn))   bn = b * rstd_post
+ *
+ * dx has the stream's type, dbranch and a full gate's gradient have `dtype`, the others are fp32 vectors of `width`
+ * values.  All are overwritten; sums over rows are taken in an order that depends on the sizes alone, so runs repeat
+ * bit for bit.  Each output may be NULL = not wanted (one must be).  Without a branch the call is that of a norm
+ * by itself: dx = d, residual_scale is not used, and only dpre_weight may be asked for besides.
+ * y (and rstd_pre) may be NULL without dh, rstd_post without post_norm or where only dx and dpre_weight are wanted.
+ * The workspace holds partial sums over rows: capscaps_block_norm_bwd_workspace_bytes(block) bytes (host-only; 0 also for
+ * an invalid block).  It may be NULL where no sum over rows is wanted.
+ */
+typedef struct capscaps_block_bwd_args {
+    const void *y, *branch, *gate;
+    const float *pre_weight, *post_weight, *rstd_pre, *rstd_post;
+    const void *dh, *dy;
+    void *dx, *dbranch, *dgate;
+    float *dpre_weight, *dpost_weight;
+    long long y_stride, branch_stride, gate_stride, dh_stride, dy_stride, dx_stride, dbranch_stride, dgate_stride;
+} capscaps_block_bwd_args;
+size_t capscaps_block_norm_bwd_workspace_bytes(const capscaps_block* block);
+int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bwd_args* args, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * The norm of all gradients of a step, and what an optimizer step makes of it.  `control` (device memory, 16-byte
+ * aligned) is written so:
+ *
+ *     norm  = |grad_scale| * sqrt(sum over all values of all tensors of g^2)
+ *     scale = grad_scale * min(1, max_norm / norm)     (max_norm <= 0: no clipping, scale = grad_scale)
+ *     skip  = norm is infinite or NaN                  (scale = 0 then)
+ *     step  = step + 1 unless skipped                  (the only field that is read: zero it once, before training)
+ *
+ * grad_scale is what gradients are to be multiplied by before use (one over a loss scale, or 1); max_norm must not be NaN.
+ * Squares are summed in fp64 in a fixed order.  `grads` is an array in HOST memory, read during the call; a
+ * tensor's `dtype` is its element type, its values lie next to each other, n = 0 is allowed.  `workspace`:
+ * CAPSCAPS_GRAD_NORM_WORKSPACE_BYTES bytes of device memory.
+ */
+#define CAPSCAPS_GRAD_NORM_WORKSPACE_BYTES (65536u)
+typedef struct capscaps_grad_control {
+    float norm, scale;
+    int skip, step;
+} capscaps_grad_control;
+typedef struct capscaps_grad_tensor {
+    const void* grad;
+    long long n;
+    int dtype;
+} capscaps_grad_tensor;
+int capscaps_grad_norm(const capscaps_grad_tensor* grads, int count, float grad_scale, float max_norm,
+                       capscaps_grad_control* control, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * AdamW over many tensors (fp32 parameters): with g' = scale * g,
+ *
+ *     m = beta1 * m + (1 - beta1) * g'        v = beta2 * v + (1 - beta2) * g'^2
+ *     p = p * (1 - lr * weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *
+ * and, where a tensor has a `copy`, p rounded to nearest even to that 16-bit type (the kernel that the next forward
+ * pass reads).  `tensors` is an array in HOST memory, read during the call; 44 tensors are one launch.  n = 0 is allowed.
+ * Pointers are device pointers aligned to their elements; no two tensors overlap.
+ *
+ * `control`: NULL, or what capscaps_grad_norm wrote on the same stream: `scale` comes from there then, `skip` leaves
+ * every buffer as it is, and with step = 0 the step count t does too (so a graph replay counts its steps; a count
+ * of 0 is as `skip`).  With control = NULL, scale is 1.  t is `step` where that is > 0.
+ *
+ * state_bits = 32: m and v are fp32.  state_bits = 8: m and v are one byte a value, and each 256 consecutive values of a
+ * tensor share an exponent byte (m_exp, v_exp: (n + 255) / 256 bytes each).  With E that byte, the byte c of v
+ * stands for 0 where c = 0, else for the fp32 value with the bits (c + 8 (E - 31)) << 20: three bits of mantissa, 31 octaves
+ * below the block's largest value.  m has a sign bit and c in seven bits, with E - 15: 15 octaves.  E = 255 marks a
+ * block that holds an infinity or NaN, and every value of it reads as NaN.  A zeroed state (bytes and exponents) is a state of zeros.
+ * New values are rounded to a neighbouring code at random, up with the probability that makes the expected value
+ * exact (values of m below the smallest code become 0, such of v the smallest code): rounded to nearest, a v that
+ * changes by a thousandth a step would never move.  The random bits are a hash of `seed`, t, the tensor's index in
+ * `tensors` and the value's index in the tensor, so a step repeats bit for bit.  The parameters' update uses the unrounded m and v.
+ */
+typedef struct capscaps_adamw_tensor {
+    float* param;
+    const void* grad;
+    void *m, *v;
+    unsigned char *m_exp, *v_exp; /* state_bits = 8 only */
+    void* copy;                   /* or NULL */
+    long long n;
+    float weight_decay;
+    int grad_dtype;
+    int copy_dtype; /* CAPSCAPS_BF16 or CAPSCAPS_FP16 */
+} capscaps_adamw_tensor;
+int capscaps_adamw_step(const capscaps_adamw_tensor* tensors, int count, int state_bits, double lr, double beta1,
+                        double beta2, double eps, long long step, unsigned seed, const capscaps_grad_control* control,
+                        void* stream);
+/*
+ * The values that 8-bit moments stand for, in bfloat16, which holds each of them exactly: for tensor i, n values to m_out[i] and to
+ * v_out[i] (device pointers in HOST arrays).  Of `tensors` the fields m, v, m_exp, v_exp and n are used.
+ */
+int capscaps_adamw_state_values(const capscaps_adamw_tensor* tensors, int count, void* const* m_out,
+                                void* const* v_out, void* stream);
 
 /*
  * Measurement aid, not part of the operator: `blocks` workgroups of 4 waves each execute

@@ -8,7 +8,9 @@ library is missing or no GPU is present, calls fail.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
+from collections import namedtuple
 from pathlib import Path
 
 FP32, BF16, FP16 = 0, 1, 2
@@ -17,11 +19,50 @@ PATH_MFMA_TUNED32 = 5
 PATH_MFMA_SMALL = 6
 OK, EINVAL, EWORKSPACE, EUNSUPPORTED, EHIP, ESCRATCH = 0, -1, -2, -3, -4, -5
 STATIC_SCRATCH_BYTES = 80 << 20
+GATE_NONE, GATE_SHARED, GATE_FULL = 0, 1, 2
+ACT_LINEAR, ACT_SIGMOID, ACT_SILU = 0, 1, 2
+GRAD_NORM_WORKSPACE_BYTES = 65536
 
 # CAPSCAPS_SANITIZE=1 selects the build whose host code is instrumented (see build.py)
 _LIB_PATH = Path(__file__).resolve().parent / (
     "libcapscaps.san.so" if os.environ.get("CAPSCAPS_SANITIZE") == "1" else "libcapscaps.so")
 _lib = None
+
+
+def _fields(names, ctype):
+    return [(name, ctype) for name in names.split()]
+
+
+class BlockArgs(ctypes.Structure):
+    """capscaps_block"""
+    _fields_ = (_fields("rows", ctypes.c_longlong)
+                + _fields("width dtype stream_dtype branch_dtype post_norm gate gate_act", ctypes.c_int)
+                + _fields("residual_scale branch_scale eps", ctypes.c_float))
+
+
+class BlockFwdArgs(ctypes.Structure):
+    """capscaps_block_fwd_args"""
+    _fields_ = (_fields("x branch gate pre_weight post_weight y h rstd_pre rstd_post", ctypes.c_void_p)
+                + _fields("x_stride branch_stride gate_stride y_stride h_stride", ctypes.c_longlong))
+
+
+class BlockBwdArgs(ctypes.Structure):
+    """capscaps_block_bwd_args"""
+    _fields_ = (_fields("y branch gate pre_weight post_weight rstd_pre rstd_post dh dy dx dbranch dgate "
+                        "dpre_weight dpost_weight", ctypes.c_void_p)
+                + _fields("y_stride branch_stride gate_stride dh_stride dy_stride dx_stride dbranch_stride "
+                          "dgate_stride", ctypes.c_longlong))
+
+
+class GradTensor(ctypes.Structure):
+    """capscaps_grad_tensor"""
+    _fields_ = [("grad", ctypes.c_void_p), ("n", ctypes.c_longlong), ("dtype", ctypes.c_int)]
+
+
+class AdamwTensor(ctypes.Structure):
+    """capscaps_adamw_tensor"""
+    _fields_ = (_fields("param grad m v m_exp v_exp copy", ctypes.c_void_p) + [("n", ctypes.c_longlong)]
+                + [("weight_decay", ctypes.c_float)] + _fields("grad_dtype copy_dtype", ctypes.c_int))
 
 
 class CapscapsError(RuntimeError):
@@ -85,6 +126,19 @@ def _load():
     lib.capscaps_scheme2_build_index.restype = i
     lib.capscaps_scheme2_fwd.argtypes = [p, p, p, p, sz] + [i] * 14 + [p]
     lib.capscaps_scheme2_fwd.restype = i
+    ll, f, d = ctypes.c_longlong, ctypes.c_float, ctypes.c_double
+    lib.capscaps_block_norm_fwd.argtypes = [p, p, p]
+    lib.capscaps_block_norm_fwd.restype = i
+    lib.capscaps_block_norm_bwd_workspace_bytes.argtypes = [p]
+    lib.capscaps_block_norm_bwd_workspace_bytes.restype = sz
+    lib.capscaps_block_norm_bwd.argtypes = [p, p, p, sz, p]
+    lib.capscaps_block_norm_bwd.restype = i
+    lib.capscaps_grad_norm.argtypes = [p, i, f, f, p, p, sz, p]
+    lib.capscaps_grad_norm.restype = i
+    lib.capscaps_adamw_step.argtypes = [p, i, i, d, d, d, d, ll, ctypes.c_uint, p, p]
+    lib.capscaps_adamw_step.restype = i
+    lib.capscaps_adamw_state_values.argtypes = [p, i, p, p, p]
+    lib.capscaps_adamw_state_values.restype = i
     lib.capscaps_mfma_yardstick.argtypes = [p, p, i, i, i, p]
     lib.capscaps_mfma_yardstick.restype = i
     lib.capscaps_mfma_yardstick_flops.argtypes = [i, i, i]
@@ -219,6 +273,39 @@ def capscaps_scheme2_fwd(input, kernel, out, index, index_bytes, N, H, W, C, M, 
                                         kw, stride, pad, D0, D1, D2, D3, dtype, stream)
 
 
+def capscaps_block_norm_fwd(block, args, stream=None) -> int:
+    """`block`, `args`: BlockArgs and BlockFwdArgs."""
+    return _load().capscaps_block_norm_fwd(_ref(block), _ref(args), stream)
+
+
+def capscaps_block_norm_bwd_workspace_bytes(block) -> int:
+    return int(_load().capscaps_block_norm_bwd_workspace_bytes(_ref(block)))
+
+
+def capscaps_block_norm_bwd(block, args, workspace, workspace_bytes, stream=None) -> int:
+    """`block`, `args`: BlockArgs and BlockBwdArgs."""
+    return _load().capscaps_block_norm_bwd(_ref(block), _ref(args), workspace, workspace_bytes, stream)
+
+
+def capscaps_grad_norm(grads, count, grad_scale, max_norm, control, workspace, workspace_bytes, stream=None) -> int:
+    """`grads`: an array of GradTensor."""
+    return _load().capscaps_grad_norm(grads, count, grad_scale, max_norm, control, workspace, workspace_bytes, stream)
+
+
+def capscaps_adamw_step(tensors, count, state_bits, lr, beta1, beta2, eps, step, seed, control, stream=None) -> int:
+    """`tensors`: an array of AdamwTensor."""
+    return _load().capscaps_adamw_step(tensors, count, state_bits, lr, beta1, beta2, eps, step, seed, control, stream)
+
+
+def capscaps_adamw_state_values(tensors, count, m_out, v_out, stream=None) -> int:
+    """`tensors`: an array of AdamwTensor; `m_out`, `v_out`: arrays of device pointers (c_void_p)."""
+    return _load().capscaps_adamw_state_values(tensors, count, m_out, v_out, stream)
+
+
+def _ref(structure):
+    return None if structure is None else ctypes.addressof(structure)
+
+
 def capscaps_mfma_yardstick(seed, sink, dtype, blocks, iters, stream=None) -> int:
     return _load().capscaps_mfma_yardstick(seed, sink, dtype, blocks, iters, stream)
 
@@ -339,3 +426,319 @@ def conv_bwd_kernel(input, dout, kernel_hw, stride=1, pad=0):
     if rc != OK:
         raise CapscapsError(rc)
     return dk
+
+
+# ------------------------------------------------------------------ norms around a block
+BlockNorm = namedtuple("BlockNorm", "y h rstd_pre rstd_post")
+BlockNormGrads = namedtuple("BlockNormGrads", "dx dbranch dpre_weight dpost_weight dgate")
+_ACTS = {"linear": ACT_LINEAR, "sigmoid": ACT_SIGMOID, "silu": ACT_SILU}
+_codes = None
+
+
+def _code(dtype):
+    """The library's code of a torch dtype."""
+    global _codes
+    if _codes is None:
+        import torch
+        _codes = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16}
+    try:
+        return _codes[dtype]
+    except KeyError:
+        raise ValueError(f"{dtype}: float32, bfloat16 and float16 are supported") from None
+
+
+def _row_stride(t, shape, width, norm_dims, name):
+    """Distance between the rows of `t`, whose last `norm_dims` axes are one dense row and whose other axes follow
+    each other at equal distances."""
+    if not t.is_cuda:
+        raise ValueError("capscaps runs on the GPU only: pass device tensors")
+    if t.shape != shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
+    if t.is_contiguous():
+        return width
+    strides, dense = t.stride(), 1
+    for k in range(len(shape) - 1, len(shape) - 1 - norm_dims, -1):
+        if shape[k] != 1 and strides[k] != dense:
+            raise ValueError(f"{name}: a row's values must lie next to each other")
+        dense *= shape[k]
+    row, expect = None, None
+    for k in range(len(shape) - 1 - norm_dims, -1, -1):
+        if shape[k] == 1:
+            continue
+        if row is None:
+            row = expect = strides[k]
+        if strides[k] != expect:
+            raise ValueError(f"{name}: its rows must lie at equal distances")
+        expect *= shape[k]
+    return width if row is None else row
+
+
+def _vector(t, width, device, name):
+    if t is None:
+        return None
+    if _code(t.dtype) != FP32 or t.numel() != width or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be {width} contiguous float32 values on {device}")
+    return t.data_ptr()
+
+
+def _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scale, branch_scale, eps):
+    """(BlockArgs, pointers and strides of branch and gate): what both directions check."""
+    shape = x.shape
+    if not 1 <= norm_dims <= len(shape) or x.numel() == 0:
+        raise ValueError(f"{norm_dims} axes of a tensor of shape {tuple(shape)} are no rows")
+    width = math.prod(shape[len(shape) - norm_dims:])
+    layer, stream = _code(dtype), _code(x.dtype)
+    kind, gate_ptr, gate_stride = GATE_NONE, None, 0
+    if gate is not None:
+        if gate.shape == shape and gate.dim() > norm_dims:
+            if gate.dtype != dtype:
+                raise ValueError(f"a gate for every value must be {dtype}")
+            kind, gate_stride = GATE_FULL, _row_stride(gate, shape, width, norm_dims, "gate")
+            gate_ptr = gate.data_ptr()
+        else:
+            kind, gate_ptr = GATE_SHARED, _vector(gate, width, x.device, "gate")
+    if gate_act not in _ACTS:
+        raise ValueError(f"gate_act is one of {', '.join(_ACTS)}")
+    branch_ptr, branch_stride, branch_code = None, 0, FP32
+    if branch is not None:
+        branch_stride = _row_stride(branch, shape, width, norm_dims, "branch")
+        branch_ptr, branch_code = branch.data_ptr(), _code(branch.dtype)
+    elif gate is not None:
+        raise ValueError("a gate needs a branch")
+    if stream not in (FP32, layer) or branch_code not in (FP32, layer):
+        raise ValueError(f"x and branch must be float32 or {dtype}")
+    block = BlockArgs(x.numel() // width, width, layer, stream, branch_code, 1 if post_norm else 0, kind,
+                      _ACTS[gate_act], residual_scale, branch_scale, eps)
+    return block, branch_ptr, branch_stride, gate_ptr, gate_stride
+
+
+def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=None, gate_act="linear",
+                   post_norm=True, residual_scale=1.0, branch_scale=1.0, eps=1e-6, norm_dims=1, dtype=None,
+                   save=False, want_y=True, want_h=True, y=None, h=None):
+    """Between two blocks of layers, in one launch: the norm after the block, its gate, the residual sum, the norm
+    before the next block.
+
+        u = branch / rms(branch) * post_weight            (post_norm=False: u = branch)
+        y = residual_scale * x + branch_scale * act(gate) * u
+        h = y / rms(y) * pre_weight
+
+    The last `norm_dims` axes of x [N, ...] are a row: of an activation [N,H,W,C,D0,D1,D2], 4 normalises all
+    capsules of a pixel together, 3 every capsule by itself.  `dtype` is the layers' element type (that of h; default: x's): x, the
+    residual stream, and branch, a layer's output, are each float32 or `dtype`.  Weights are float32 of a row's
+    size; the gate is such a vector, or a tensor of x's shape and `dtype`.  Without a branch only h is computed.
+    Returns BlockNorm(y, h, rstd_pre, rstd_post); the statistics only with `save`, for block_norm_bwd.  `y` and `h`
+    may be given to write to; y may be x.  Enqueues on torch's current stream; does not synchronise."""
+    import torch
+    dtype = x.dtype if dtype is None else dtype
+    block, bp, bs, gp, gs = _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scale,
+                                   branch_scale, eps)
+    shape, width, device = x.shape, block.width, x.device
+    xs = _row_stride(x, shape, width, norm_dims, "x")
+    if branch is None:
+        if y is not None:
+            raise ValueError("without a branch there is no y")
+    elif y is None and want_y:
+        y = torch.empty(shape, dtype=x.dtype, device=device)
+    if h is None and want_h:
+        h = torch.empty(shape, dtype=dtype, device=device)
+    if y is not None and y.dtype != x.dtype or h is not None and h.dtype != dtype:
+        raise ValueError("y has x's type, h has `dtype`")
+    rpre = rpost = None
+    if save:
+        if h is not None:
+            rpre = torch.empty(shape[:len(shape) - norm_dims], dtype=torch.float32, device=device)
+        if branch is not None and post_norm:
+            rpost = torch.empty(shape[:len(shape) - norm_dims], dtype=torch.float32, device=device)
+    args = BlockFwdArgs(
+        x.data_ptr(), bp, gp, _vector(pre_weight, width, device, "pre_weight"),
+        _vector(post_weight, width, device, "post_weight"), None if y is None else y.data_ptr(),
+        None if h is None else h.data_ptr(), None if rpre is None else rpre.data_ptr(),
+        None if rpost is None else rpost.data_ptr(), xs, bs, gs,
+        0 if y is None else _row_stride(y, shape, width, norm_dims, "y"),
+        0 if h is None else _row_stride(h, shape, width, norm_dims, "h"))
+    rc = capscaps_block_norm_fwd(block, args, torch.cuda.current_stream(device).cuda_stream)
+    if rc != OK:
+        raise CapscapsError(rc)
+    return BlockNorm(y, h, rpre, rpost)
+
+
+def block_norm_bwd(y, branch, rstd_pre, rstd_post, dh, dy, *, pre_weight=None, post_weight=None, gate=None,
+                   gate_act="linear", post_norm=True, residual_scale=1.0, branch_scale=1.0, norm_dims=1, dtype=None):
+    """The gradients of block_norm_fwd, from what it returned with `save` and the gradients of h and y (`dh` of the
+    layers' type `dtype`, `dy` of the stream's; either may be None = zero).  `y` is the stream after the
+    block (without a branch: x).  Returns BlockNormGrads(dx, dbranch, dpre_weight, dpost_weight, dgate): dx in
+    the stream's type, dbranch and the gradient of a gate for every value in `dtype`, the other gates' and the weights' float32 sums over
+    rows; None where there is no such operand."""
+    import torch
+    if dh is None and dy is None:
+        raise ValueError("block_norm_bwd needs dh or dy")
+    if dtype is None:
+        dtype = y.dtype if dh is None else dh.dtype
+    block, bp, bs, gp, gs = _block(y, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scale,
+                                   branch_scale, 1.0)
+    shape, width, device = y.shape, block.width, y.device
+    if dh is not None and dh.dtype != dtype or dy is not None and dy.dtype != y.dtype:
+        raise ValueError("dh has `dtype`, dy has y's type")
+    post = branch is not None and post_norm
+
+    def vector():
+        return torch.empty(width, dtype=torch.float32, device=device)
+
+    dx = torch.empty(shape, dtype=y.dtype, device=device)
+    db = torch.empty(shape, dtype=dtype, device=device) if branch is not None else None
+    dpre = vector() if dh is not None and pre_weight is not None else None
+    dpost = vector() if post and post_weight is not None else None
+    dgate = None
+    if gate is not None:
+        dgate = vector().view(gate.shape) if block.gate == GATE_SHARED else torch.empty(shape, dtype=dtype, device=device)
+    need = capscaps_block_norm_bwd_workspace_bytes(block)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+    args = BlockBwdArgs(
+        y.data_ptr(), bp, gp, _vector(pre_weight, width, device, "pre_weight"),
+        _vector(post_weight, width, device, "post_weight"),
+        _vector(rstd_pre, block.rows, device, "rstd_pre") if dh is not None else None,
+        _vector(rstd_post, block.rows, device, "rstd_post") if post else None,
+        None if dh is None else dh.data_ptr(), None if dy is None else dy.data_ptr(), dx.data_ptr(),
+        None if db is None else db.data_ptr(), None if dgate is None else dgate.data_ptr(),
+        None if dpre is None else dpre.data_ptr(), None if dpost is None else dpost.data_ptr(),
+        _row_stride(y, shape, width, norm_dims, "y"), bs, gs,
+        0 if dh is None else _row_stride(dh, shape, width, norm_dims, "dh"),
+        0 if dy is None else _row_stride(dy, shape, width, norm_dims, "dy"), width, width, width)
+    rc = capscaps_block_norm_bwd(block, args, ws.data_ptr(), need, torch.cuda.current_stream(device).cuda_stream)
+    if rc != OK:
+        raise CapscapsError(rc)
+    return BlockNormGrads(dx, db, dpre, dpost, dgate)
+
+
+# ------------------------------------------------------------------ gradient norm, AdamW
+def _dense(t, what):
+    if not (t.is_cuda and t.is_contiguous()):
+        raise ValueError(f"{what} must be contiguous device tensors")
+    return t.data_ptr()
+
+
+def _control_ptr(control):
+    if control is None:
+        return None
+    if control.element_size() * control.numel() != 16:
+        raise ValueError("control is 16 bytes: norm, scale (float32), skip, step (int32)")
+    return _dense(control, "control")
+
+
+def grad_norm(grads, max_norm=None, grad_scale=1.0, control=None, workspace=None):
+    """The 2-norm of all gradients together, on the device: writes `control`, four values of 4 bytes that AdamW.step
+    reads: the norm (of grad_scale * gradients), the factor that scales and clips the gradients to `max_norm`
+    (None: no clipping), whether the step is to be skipped because the norm is not finite (int32), and the number of steps
+    not skipped so far (int32, counted up here; make `control` of zeros).  Returns it."""
+    import torch
+    if not grads and control is None:
+        raise ValueError("grad_norm of no tensors needs a control to write to")
+    device = control.device if control is not None else grads[0].device
+    if control is None:
+        control = torch.zeros(4, dtype=torch.float32, device=device)
+    if workspace is None:
+        workspace = torch.empty(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+    items = (GradTensor * max(1, len(grads)))(*[(_dense(g, "gradients"), g.numel(), _code(g.dtype)) for g in grads])
+    rc = capscaps_grad_norm(items, len(grads), grad_scale, 0.0 if max_norm is None else max_norm,
+                            _control_ptr(control), workspace.data_ptr(), workspace.numel(),
+                            torch.cuda.current_stream(device).cuda_stream)
+    if rc != OK:
+        raise CapscapsError(rc)
+    return control
+
+
+class AdamW:
+    """AdamW over a list of float32 device tensors, all in one launch (44 tensors a launch).
+
+    `weight_decay`: a number, or one for each tensor.  `copies`: None, a 16-bit dtype (copies of that type are made), or
+    a list of 16-bit tensors (None where there is none) of the parameters' sizes; each step writes the rounded
+    parameters there, for the layers to read.  `state_bits`: 32 (float32 moments) or 8 (a byte for each, and a
+    byte for each 256 values that share an exponent; rounded at random by a hash of `seed`, the step and the
+    position).  `state`: moments to go on from, (m, v) or (m, v, m_exp, v_exp), lists of tensors in that format; kept, not
+    copied."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, state_bits=32, copies=None,
+                 seed=0, state=None):
+        import torch
+        if state_bits not in (32, 8):
+            raise ValueError("state_bits is 32 or 8")
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("AdamW needs parameters")
+        count, eight = len(self.params), state_bits == 8
+        self.lr, self.betas, self.eps, self.state_bits, self.seed = lr, betas, eps, state_bits, seed
+        self.steps = 0
+        for p in self.params:
+            if p.dtype != torch.float32:
+                raise ValueError("parameters are float32")
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
+        if isinstance(copies, torch.dtype):
+            copies = [p.detach().to(copies) for p in self.params]
+        self.copies = [None] * count if copies is None else list(copies)
+        if state is None:
+            kind = torch.uint8 if eight else torch.float32
+            self.m, self.v = ([torch.zeros(p.shape, dtype=kind, device=p.device) for p in self.params]
+                              for _ in range(2))
+            self.m_exp, self.v_exp = ([torch.zeros((p.numel() + 255) // 256, dtype=torch.uint8, device=p.device)
+                                       for p in self.params] if eight else [None] * count for _ in range(2))
+        else:
+            if len(state) != (4 if eight else 2):
+                raise ValueError("state is (m, v), or (m, v, m_exp, v_exp) in 8 bits")
+            self.m, self.v, self.m_exp, self.v_exp = [list(s) for s in state] + (
+                [] if eight else [[None] * count, [None] * count])
+        if any(len(s) != count for s in (decay, self.copies, self.m, self.v, self.m_exp, self.v_exp)):
+            raise ValueError(f"{count} parameters need as many copies, moments and decays")
+        self._items = (AdamwTensor * count)()
+        self._sizes = [p.numel() for p in self.params]
+        for t, p, m, v, me, ve, c, d in zip(self._items, self.params, self.m, self.v, self.m_exp, self.v_exp,
+                                            self.copies, decay):
+            kind, n = (torch.uint8 if eight else torch.float32), p.numel()
+            if m.dtype != kind or v.dtype != kind or m.numel() != n or v.numel() != n:
+                raise ValueError(f"moments are {kind} of the parameters' sizes")
+            if eight and any(e.dtype != torch.uint8 or e.numel() != (n + 255) // 256 for e in (me, ve)):
+                raise ValueError("exponents are bytes, one for each 256 values")
+            if c is not None and (c.numel() != n or _code(c.dtype) == FP32):
+                raise ValueError("copies are 16-bit tensors of the parameters' sizes")
+            t.param, t.m, t.v, t.n, t.weight_decay = _dense(p, "parameters"), _dense(m, "moments"), _dense(v, "moments"), n, d
+            t.m_exp, t.v_exp = (_dense(me, "exponents"), _dense(ve, "exponents")) if eight else (None, None)
+            t.copy, t.copy_dtype = (None, BF16) if c is None else (_dense(c, "copies"), _code(c.dtype))
+
+    def step(self, grads, control=None, lr=None):
+        """One step with these gradients (float32, bfloat16 or float16, contiguous).  With `control`, what
+        grad_norm returned: their scale, the number of the step and whether it is skipped come from there;
+        without, steps are counted here.  Enqueues on torch's current stream."""
+        import torch
+        if len(grads) != len(self._items):
+            raise ValueError(f"{len(self._items)} parameters need as many gradients")
+        for t, g, n in zip(self._items, grads, self._sizes):
+            if g.numel() != n:
+                raise ValueError("gradients have the parameters' sizes")
+            t.grad, t.grad_dtype = _dense(g, "gradients"), _code(g.dtype)
+        step = 0 if control is not None else self.steps + 1
+        rc = capscaps_adamw_step(self._items, len(self._items), self.state_bits, self.lr if lr is None else lr,
+                                 self.betas[0], self.betas[1], self.eps, step, self.seed & 0xFFFFFFFF,
+                                 _control_ptr(control), torch.cuda.current_stream(self.params[0].device).cuda_stream)
+        if rc != OK:
+            raise CapscapsError(rc)
+        if control is None:
+            self.steps = step
+
+    def state_values(self, out=None):
+        """The moments (m, v) as lists of tensors; in 8 bits, the values their codes stand for, in bfloat16, which
+        holds them exactly (written to `out`, two lists of tensors, if given)."""
+        import torch
+        if self.state_bits == 32:
+            return self.m, self.v
+        if out is None:
+            out = [[torch.empty(p.shape, dtype=torch.bfloat16, device=p.device) for p in self.params]
+                   for _ in range(2)]
+        for t, n in zip(out[0] + out[1], self._sizes + self._sizes):
+            if t.dtype != torch.bfloat16 or t.numel() != n:
+                raise ValueError("moments' values are bfloat16 of the parameters' sizes")
+        count = len(self._items)
+        pointers = [(ctypes.c_void_p * count)(*[_dense(t, "values") for t in o]) for o in out]
+        rc = capscaps_adamw_state_values(self._items, count, pointers[0], pointers[1],
+                                         torch.cuda.current_stream(self.params[0].device).cuda_stream)
+        if rc != OK:
+            raise CapscapsError(rc)
+        return out[0], out[1]

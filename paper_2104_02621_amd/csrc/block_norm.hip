@@ -1,0 +1,324 @@
+// The norms around a block of layers with its gate and residual stream, forward and backward.
+// Formulas and contracts: include/capscaps.h.
+//
+// This file's kernels take rows of any width: a workgroup per row, which reads the row once for each mean it needs
+// and once more to write (the second and third time from the caches), and for the sums over rows a thread per
+// column.  Bounded by memory and, on short rows, by the idle threads of a row's workgroup.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/capscaps.h"
+#include "conv_shape.h"
+#include "element.h"
+
+namespace capscaps {
+namespace {
+
+constexpr int THREADS = 256;
+
+// act(g) and its derivative
+__device__ __forceinline__ float gate_value(int act, float g)
+{
+    if (act == CAPSCAPS_ACT_LINEAR) return g;
+    const float q = 1.0f / (1.0f + __expf(-g));
+    return act == CAPSCAPS_ACT_SIGMOID ? q : g * q;
+}
+__device__ __forceinline__ float gate_slope(int act, float g)
+{
+    if (act == CAPSCAPS_ACT_LINEAR) return 1.0f;
+    const float q = 1.0f / (1.0f + __expf(-g));
+    return act == CAPSCAPS_ACT_SIGMOID ? q * (1.0f - q) : q * (1.0f + g * (1.0f - q));
+}
+
+// sum over the workgroup, in every thread
+__device__ __forceinline__ float block_sum(float v, float* lds)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.0f;
+    for (int w = 0; w < THREADS / 64; ++w) v += lds[w];
+    __syncthreads();
+    return v;
+}
+
+__device__ __forceinline__ float gate_at(const capscaps_block& B, const void* gate, long long row, long long stride,
+                                         int c)
+{
+    return B.gate == CAPSCAPS_GATE_SHARED ? static_cast<const float*>(gate)[c]
+                                          : load_element(gate, row * stride + c, B.dtype);
+}
+
+__global__ void __launch_bounds__(THREADS) block_fwd_any_kernel(capscaps_block B, capscaps_block_fwd_args A)
+{
+    __shared__ float lds[THREADS / 64];
+    for (long long r = blockIdx.x; r < B.rows; r += gridDim.x) {
+        float rpost = 1.0f;
+        if (A.branch != nullptr && B.post_norm) {
+            float s = 0.0f;
+            for (int c = threadIdx.x; c < B.width; c += THREADS) {
+                const float b = load_element(A.branch, r * A.branch_stride + c, B.branch_dtype);
+                s += b * b;
+            }
+            rpost = 1.0f / sqrtf(block_sum(s, lds) / (float)B.width + B.eps);
+            if (A.rstd_post != nullptr && threadIdx.x == 0) A.rstd_post[r] = rpost;
+        }
+        auto value = [&](int c) {
+            const float x = load_element(A.x, r * A.x_stride + c, B.stream_dtype);
+            if (A.branch == nullptr) return x;
+            float u = load_element(A.branch, r * A.branch_stride + c, B.branch_dtype) * rpost;
+            if (B.post_norm && A.post_weight != nullptr) u *= A.post_weight[c];
+            if (B.gate != CAPSCAPS_GATE_NONE) u *= gate_value(B.gate_act, gate_at(B, A.gate, r, A.gate_stride, c));
+            return B.residual_scale * x + B.branch_scale * u;
+        };
+        float rpre = 1.0f;
+        if (A.h != nullptr) {
+            float s = 0.0f;
+            for (int c = threadIdx.x; c < B.width; c += THREADS) {
+                const float y = value(c);
+                s += y * y;
+            }
+            rpre = 1.0f / sqrtf(block_sum(s, lds) / (float)B.width + B.eps);
+            if (A.rstd_pre != nullptr && threadIdx.x == 0) A.rstd_pre[r] = rpre;
+        }
+        for (int c = threadIdx.x; c < B.width; c += THREADS) {
+            const float y = value(c);
+            if (A.y != nullptr) store_element(A.y, r * A.y_stride + c, y, B.stream_dtype);
+            if (A.h != nullptr)
+                store_element(A.h, r * A.h_stride + c, y * rpre * (A.pre_weight != nullptr ? A.pre_weight[c] : 1.0f),
+                              B.dtype);
+        }
+    }
+}
+
+// One element of the way back, given the row's mean of dh * pre_weight * yn
+struct Back {
+    float yn, dh, d;        // d: the gradient that reaches y
+    float t, bn, u, a, g;   // of the branch
+};
+__device__ __forceinline__ Back back_at(const capscaps_block& B, const capscaps_block_bwd_args& A, long long r, int c,
+                                        float mean_pre, float rpre, float rpost)
+{
+    Back k{};
+    k.d = A.dy != nullptr ? load_element(A.dy, r * A.dy_stride + c, B.stream_dtype) : 0.0f;
+    if (A.dh != nullptr) {
+        k.yn = load_element(A.y, r * A.y_stride + c, B.stream_dtype) * rpre;
+        k.dh = load_element(A.dh, r * A.dh_stride + c, B.dtype);
+        k.d += rpre * (k.dh * (A.pre_weight != nullptr ? A.pre_weight[c] : 1.0f) - k.yn * mean_pre);
+    }
+    if (A.branch != nullptr) {
+        k.t = B.branch_scale * k.d;
+        k.bn = load_element(A.branch, r * A.branch_stride + c, B.branch_dtype) * rpost;
+        k.u = B.post_norm && A.post_weight != nullptr ? k.bn * A.post_weight[c] : k.bn;
+        k.a = 1.0f;
+        if (B.gate != CAPSCAPS_GATE_NONE) {
+            k.g = gate_at(B, A.gate, r, A.gate_stride, c);
+            k.a = gate_value(B.gate_act, k.g);
+        }
+    }
+    return k;
+}
+
+// dx, dbranch, a full gate's gradient; the rows' means of dh * pre_weight * yn go to `mean`
+__global__ void __launch_bounds__(THREADS)
+    block_bwd_rows_kernel(capscaps_block B, capscaps_block_bwd_args A, float* mean)
+{
+    __shared__ float lds[THREADS / 64];
+    for (long long r = blockIdx.x; r < B.rows; r += gridDim.x) {
+        const float rpre = A.dh != nullptr ? A.rstd_pre[r] : 1.0f;
+        const float rpost = A.branch != nullptr && B.post_norm && A.rstd_post != nullptr ? A.rstd_post[r] : 1.0f;
+        float mean_pre = 0.0f;
+        if (A.dh != nullptr) {
+            float s = 0.0f;
+            for (int c = threadIdx.x; c < B.width; c += THREADS) {
+                float n = load_element(A.dh, r * A.dh_stride + c, B.dtype);
+                if (A.pre_weight != nullptr) n *= A.pre_weight[c];
+                s += n * (load_element(A.y, r * A.y_stride + c, B.stream_dtype) * rpre);
+            }
+            mean_pre = block_sum(s, lds) / (float)B.width;
+            if (mean != nullptr && threadIdx.x == 0) mean[r] = mean_pre;
+        }
+        auto e_of = [&](const Back& k, int c) {
+            return k.t * k.a * (B.post_norm && A.post_weight != nullptr ? A.post_weight[c] : 1.0f);
+        };
+        float mean_post = 0.0f;
+        if (A.dbranch != nullptr && B.post_norm) {
+            float s = 0.0f;
+            for (int c = threadIdx.x; c < B.width; c += THREADS) {
+                const Back k = back_at(B, A, r, c, mean_pre, rpre, rpost);
+                s += e_of(k, c) * k.bn;
+            }
+            mean_post = block_sum(s, lds) / (float)B.width;
+        }
+        for (int c = threadIdx.x; c < B.width; c += THREADS) {
+            const Back k = back_at(B, A, r, c, mean_pre, rpre, rpost);
+            if (A.dx != nullptr)
+                store_element(A.dx, r * A.dx_stride + c, A.branch != nullptr ? B.residual_scale * k.d : k.d,
+                              B.stream_dtype);
+            if (A.dgate != nullptr && B.gate == CAPSCAPS_GATE_FULL)
+                store_element(A.dgate, r * A.dgate_stride + c, k.t * k.u * gate_slope(B.gate_act, k.g), B.dtype);
+            if (A.dbranch != nullptr)
+                store_element(A.dbranch, r * A.dbranch_stride + c, rpost * (e_of(k, c) - k.bn * mean_post), B.dtype);
+        }
+    }
+}
+
+// Sums over a share of the rows, a thread per column: partial[share][3][width] = dpre_weight, dpost_weight, dgate
+__global__ void __launch_bounds__(THREADS)
+    block_bwd_columns_kernel(capscaps_block B, capscaps_block_bwd_args A, const float* mean, float* partial,
+                             long long rows_per_share)
+{
+    const int c = blockIdx.x * THREADS + threadIdx.x;
+    if (c >= B.width) return;
+    const long long r0 = blockIdx.y * rows_per_share;
+    const long long r1 = r0 + rows_per_share < B.rows ? r0 + rows_per_share : B.rows;
+    float pre = 0.0f, post = 0.0f, gate = 0.0f;
+    for (long long r = r0; r < r1; ++r) {
+        const float rpre = A.dh != nullptr ? A.rstd_pre[r] : 1.0f;
+        const float rpost = A.branch != nullptr && B.post_norm && A.rstd_post != nullptr ? A.rstd_post[r] : 1.0f;
+        const Back k = back_at(B, A, r, c, A.dh != nullptr ? mean[r] : 0.0f, rpre, rpost);
+        pre += k.dh * k.yn;
+        post += k.t * k.a * k.bn;
+        if (B.gate == CAPSCAPS_GATE_SHARED) gate += k.t * k.u * gate_slope(B.gate_act, k.g);
+    }
+    float* p = partial + (long long)blockIdx.y * 3 * B.width + c;
+    p[0] = pre;
+    p[B.width] = post;
+    p[2LL * B.width] = gate;
+}
+
+__global__ void __launch_bounds__(THREADS)
+    block_bwd_sum_kernel(const float* partial, int shares, int width, float* pre, float* post, float* gate)
+{
+    const int c = blockIdx.x * THREADS + threadIdx.x;
+    float* out = blockIdx.y == 0 ? pre : blockIdx.y == 1 ? post : gate;
+    if (c >= width || out == nullptr) return;
+    float s = 0.0f;
+    for (int k = 0; k < shares; ++k) s += partial[((long long)k * 3 + blockIdx.y) * width + c];
+    out[c] = s;
+}
+
+int row_shares(long long rows) { return rows < 256 ? (int)rows : 256; }
+
+bool misaligned(const void* p, int dtype)
+{
+    return (reinterpret_cast<uintptr_t>(p) & (element_bytes(dtype) - 1)) != 0;
+}
+
+// a tensor that the call reads or writes: aligned to its elements, rows within reach of 62 bits
+bool bad_rows(const capscaps_block& B, const void* p, long long stride, int dtype, bool output)
+{
+    if (p == nullptr) return false;
+    if (misaligned(p, dtype) || stride < 0) return true;
+    if (output && B.rows > 1 && stride < B.width) return true;
+    return (long double)B.rows * (long double)stride > 1e17L;
+}
+
+int check_block(const capscaps_block* B)
+{
+    if (B == nullptr || B->rows <= 0 || B->width <= 0 || !known_dtype(B->dtype)) return CAPSCAPS_EINVAL;
+    if (B->stream_dtype != CAPSCAPS_FP32 && B->stream_dtype != B->dtype) return CAPSCAPS_EINVAL;
+    if (B->branch_dtype != CAPSCAPS_FP32 && B->branch_dtype != B->dtype) return CAPSCAPS_EINVAL;
+    if ((unsigned)B->post_norm > 1 || (unsigned)B->gate > 2 || (unsigned)B->gate_act > 2) return CAPSCAPS_EINVAL;
+    if (!isfinite(B->residual_scale) || !isfinite(B->branch_scale)) return CAPSCAPS_EINVAL;
+    if (!(B->eps > 0.0f) || !isfinite(B->eps)) return CAPSCAPS_EINVAL;
+    if ((long double)B->rows * B->width > 1e17L) return CAPSCAPS_EINVAL;
+    return CAPSCAPS_OK;
+}
+
+unsigned row_blocks(const capscaps_block& B) { return (unsigned)(B.rows < (1 << 20) ? B.rows : (1 << 20)); }
+
+}  // namespace
+}  // namespace capscaps
+
+using namespace capscaps;
+
+extern "C" {
+
+int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fwd_args* args, void* stream)
+{
+    const int rc = check_block(block);
+    if (rc != CAPSCAPS_OK) return rc;
+    if (args == nullptr) return CAPSCAPS_EINVAL;
+    const capscaps_block& B = *block;
+    const capscaps_block_fwd_args& A = *args;
+    if (A.x == nullptr || (A.y == nullptr && A.h == nullptr)) return CAPSCAPS_EINVAL;
+    if (A.branch == nullptr && (A.y != nullptr || B.gate != CAPSCAPS_GATE_NONE)) return CAPSCAPS_EINVAL;
+    if ((A.gate != nullptr) != (B.gate != CAPSCAPS_GATE_NONE)) return CAPSCAPS_EINVAL;
+    const bool full = B.gate == CAPSCAPS_GATE_FULL;
+    if (bad_rows(B, A.x, A.x_stride, B.stream_dtype, false) ||
+        bad_rows(B, A.branch, A.branch_stride, B.branch_dtype, false) ||
+        bad_rows(B, A.gate, full ? A.gate_stride : 0, full ? B.dtype : CAPSCAPS_FP32, false) ||
+        bad_rows(B, A.y, A.y_stride, B.stream_dtype, true) || bad_rows(B, A.h, A.h_stride, B.dtype, true))
+        return CAPSCAPS_EINVAL;
+    for (const float* p : {A.pre_weight, A.post_weight, (const float*)A.rstd_pre, (const float*)A.rstd_post})
+        if (misaligned(p, CAPSCAPS_FP32)) return CAPSCAPS_EINVAL;
+    if (A.y == A.x && A.y_stride != A.x_stride) return CAPSCAPS_EINVAL;
+    block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, static_cast<hipStream_t>(stream)>>>(B, A);
+    return status_from_hip(hipGetLastError());
+}
+
+size_t capscaps_block_norm_bwd_workspace_bytes(const capscaps_block* block)
+{
+    if (check_block(block) != CAPSCAPS_OK) return 0;
+    const size_t means = (size_t)block->rows * 4, sums = (size_t)row_shares(block->rows) * 3 * block->width * 4;
+    return (means + 255) / 256 * 256 + sums;
+}
+
+int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bwd_args* args, void* workspace,
+                            size_t workspace_bytes, void* stream)
+{
+    const int rc = check_block(block);
+    if (rc != CAPSCAPS_OK) return rc;
+    if (args == nullptr) return CAPSCAPS_EINVAL;
+    const capscaps_block& B = *block;
+    const capscaps_block_bwd_args& A = *args;
+    const bool full = B.gate == CAPSCAPS_GATE_FULL;
+    if (A.dh == nullptr && A.dy == nullptr) return CAPSCAPS_EINVAL;
+    if (A.dh != nullptr && (A.y == nullptr || A.rstd_pre == nullptr)) return CAPSCAPS_EINVAL;
+    if (!A.dx && !A.dbranch && !A.dgate && !A.dpre_weight && !A.dpost_weight) return CAPSCAPS_EINVAL;
+    if ((A.gate != nullptr) != (B.gate != CAPSCAPS_GATE_NONE)) return CAPSCAPS_EINVAL;
+    const bool branch_wanted = A.dbranch || A.dgate || A.dpost_weight;
+    if (A.branch == nullptr && (branch_wanted || B.gate != CAPSCAPS_GATE_NONE)) return CAPSCAPS_EINVAL;
+    if (branch_wanted && B.post_norm && A.rstd_post == nullptr) return CAPSCAPS_EINVAL;
+    if (A.dgate != nullptr && B.gate == CAPSCAPS_GATE_NONE) return CAPSCAPS_EINVAL;
+    if (A.dpre_weight != nullptr && A.dh == nullptr) return CAPSCAPS_EINVAL;
+    if (A.dpost_weight != nullptr && !B.post_norm) return CAPSCAPS_EINVAL;
+    if (bad_rows(B, A.y, A.y_stride, B.stream_dtype, false) ||
+        bad_rows(B, A.branch, A.branch_stride, B.branch_dtype, false) ||
+        bad_rows(B, A.gate, full ? A.gate_stride : 0, full ? B.dtype : CAPSCAPS_FP32, false) ||
+        bad_rows(B, A.dh, A.dh_stride, B.dtype, false) || bad_rows(B, A.dy, A.dy_stride, B.stream_dtype, false) ||
+        bad_rows(B, A.dx, A.dx_stride, B.stream_dtype, true) ||
+        bad_rows(B, A.dbranch, A.dbranch_stride, B.dtype, true) ||
+        bad_rows(B, A.dgate, full ? A.dgate_stride : B.width, full ? B.dtype : CAPSCAPS_FP32, full))
+        return CAPSCAPS_EINVAL;
+    for (const float* p : {A.pre_weight, A.post_weight, A.rstd_pre, A.rstd_post, (const float*)A.dpre_weight,
+                           (const float*)A.dpost_weight})
+        if (misaligned(p, CAPSCAPS_FP32)) return CAPSCAPS_EINVAL;
+    float* dgate_sum = B.gate == CAPSCAPS_GATE_SHARED ? static_cast<float*>(A.dgate) : nullptr;
+    const bool sums = A.dpre_weight || A.dpost_weight || dgate_sum;
+    if (sums) {
+        if (workspace == nullptr || workspace_bytes < capscaps_block_norm_bwd_workspace_bytes(block))
+            return CAPSCAPS_EWORKSPACE;
+        if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CAPSCAPS_EINVAL;
+    }
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    float* mean = sums ? static_cast<float*>(workspace) : nullptr;
+    block_bwd_rows_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A, mean);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess || !sums) return status_from_hip(err);
+    float* partial = mean + ((size_t)B.rows + 63) / 64 * 64;
+    const int shares = row_shares(B.rows);
+    const long long per = (B.rows + shares - 1) / shares;
+    const unsigned columns = (unsigned)((B.width + THREADS - 1) / THREADS);
+    block_bwd_columns_kernel<<<dim3(columns, shares), dim3(THREADS), 0, st>>>(B, A, mean, partial, per);
+    err = hipGetLastError();
+    if (err != hipSuccess) return status_from_hip(err);
+    block_bwd_sum_kernel<<<dim3(columns, 3), dim3(THREADS), 0, st>>>(partial, shares, B.width, A.dpre_weight,
+                                                                     A.dpost_weight, dgate_sum);
+    return status_from_hip(hipGetLastError());
+}
+
+}  // extern "C"
