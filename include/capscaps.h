@@ -310,7 +310,7 @@ typedef struct capscaps_block {
     int post_norm;      /* 0 or 1 */
     int gate, gate_act; /* CAPSCAPS_GATE_*, CAPSCAPS_ACT_* */
     float residual_scale, branch_scale;
-    float eps; /* > 0 */
+    float eps; /* > 0, a normal number */
 } capscaps_block;
 
 /*

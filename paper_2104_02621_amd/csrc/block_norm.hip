@@ -1,21 +1,25 @@
 // The norms around a block of layers with its gate and residual stream, forward and backward.
 // Formulas and contracts: include/capscaps.h.
 //
-// This file's kernels take rows of any width: a workgroup per row, which reads the row once for each mean it needs
-// and once more to write (the second and third time from the caches), and for the sums over rows a thread per
-// column.  Bounded by memory and, on short rows, by the idle threads of a row's workgroup.
+// All of it is bounded by memory: some ten to thirty operations for every value moved.  So each value is read once and
+// each result written once, with the row in registers between: a group of lanes holds a row, eight values a
+// lane and vector (row_vectors.h), and the means are sums over the group.  Groups of up to 64 lanes share a wave and need
+// no barrier; wider rows take a workgroup.  Rows that no group holds (over 16384 values) take the kernels at the end.
 #include <hip/hip_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
 #include "../../include/capscaps.h"
 #include "conv_shape.h"
 #include "element.h"
+#include "row_vectors.h"
 
 namespace capscaps {
 namespace {
 
 constexpr int THREADS = 256;
+constexpr int CUS = 256;
 
 // act(g) and its derivative
 __device__ __forceinline__ float gate_value(int act, float g)
@@ -44,6 +48,150 @@ __device__ __forceinline__ float block_sum(float v, float* lds)
     return v;
 }
 
+
+// ------------------------------------------------------------------------------------ rows in registers
+// How rows lie on lanes: `group` lanes (a power of two) hold a row, lane l the vectors l, l + group, ... of `vectors`
+// a lane; `per_block` rows at a time in a workgroup of `threads`.
+struct RowPlan {
+    int group, vectors, threads, per_block;
+    unsigned blocks;
+    int full, tail;  // whole vectors in a row, and the values after them
+};
+
+constexpr int WIDEST = 16384;
+
+// Sum over a row's lanes.  Rows of more than one wave go through LDS: two buffers in turn, so that one barrier is
+// enough (a wave writes a buffer again only after the barrier of the other one, which every wave reaches after it has read).
+struct RowSum {
+    float* lds;  // [2][16]
+    int group, turn;
+    __device__ __forceinline__ float operator()(float v)
+    {
+        if (group <= 64) return lanes_sum(v, group);
+        v = lanes_sum(v, 64);
+        float* buffer = lds + 16 * turn;
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) buffer[threadIdx.x >> 6] = v;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        const int wave = threadIdx.x & 15;  // (every 16 lanes add up the same sums)
+        v = wave < group >> 6 ? buffer[wave] : 0.0f;
+        return lanes_sum(v, 16);
+    }
+};
+
+template <int DT, bool S16, bool B16, int I>
+struct FwdRow {
+    static constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
+    Raw<SD> x[I];
+    Raw<BD> b[I];
+    Raw<DT> g[I];
+};
+
+template <int DT, bool S16, bool B16, int I, bool TAIL>
+__global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capscaps_block_fwd_args A, RowPlan P)
+{
+    typedef FwdRow<DT, S16, B16, I> Row;
+    constexpr int SD = Row::SD, BD = Row::BD;
+    constexpr long long SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
+    __shared__ float lds[32];
+    RowSum sum{lds, P.group, 0};
+    const int lane = threadIdx.x & (P.group - 1);
+    const bool branch = A.branch != nullptr, gate = B.gate == CAPSCAPS_GATE_FULL;
+    const bool post = branch && B.post_norm, pre = A.h != nullptr;
+    const float inv_width = 1.0f / (float)B.width;
+    bool full[I], part[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        full[i] = lane + i * P.group < P.full;
+        part[i] = TAIL && lane + i * P.group == P.full;
+    }
+    // of a column: what multiplies b, apart from its statistic and a gate for every value; and h's weight
+    float cb[I][VEC], wh[I][VEC];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int v = lane + i * P.group;
+        load_column<TAIL>(cb[i], post ? A.post_weight : nullptr, v, full[i], part[i], P.tail, 1.0f);
+        load_column<TAIL>(wh[i], A.pre_weight, v, full[i], part[i], P.tail, 1.0f);
+        float g[VEC];
+        const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
+        load_column<TAIL>(g, shared ? static_cast<const float*>(A.gate) : nullptr, v, full[i], part[i], P.tail, 1.0f);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) cb[i][k] *= B.branch_scale * (shared ? gate_value(B.gate_act, g[k]) : 1.0f);
+    }
+    const long long first = (long long)blockIdx.x * P.per_block + threadIdx.x / P.group;
+    const long long step = (long long)gridDim.x * P.per_block;
+    const char* px = static_cast<const char*>(A.x) + (first * A.x_stride + lane * VEC) * SB;
+    const char* pb = static_cast<const char*>(A.branch) + (first * A.branch_stride + lane * VEC) * BB;
+    const char* pg = static_cast<const char*>(A.gate) + (first * A.gate_stride + lane * VEC) * LB;
+    char* py = static_cast<char*>(A.y) + (first * A.y_stride + lane * VEC) * SB;
+    char* ph = static_cast<char*>(A.h) + (first * A.h_stride + lane * VEC) * LB;
+    auto fetch = [&](Row& R) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            clear(R.x[i]);
+            clear(R.b[i]);
+            clear(R.g[i]);
+            load<SD, TAIL>(R.x[i], px + (long long)i * P.group * VEC * SB, full[i], part[i], P.tail);
+            if (branch) load<BD, TAIL>(R.b[i], pb + (long long)i * P.group * VEC * BB, full[i], part[i], P.tail);
+            if (gate) load<DT, TAIL>(R.g[i], pg + (long long)i * P.group * VEC * LB, full[i], part[i], P.tail);
+        }
+        px += step * A.x_stride * SB;
+        pb += step * A.branch_stride * BB;
+        pg += step * A.gate_stride * LB;
+    };
+    Row R;
+    if (first < B.rows) fetch(R);
+    for (long long r = first; r < B.rows; r += step) {
+        float rpost = 1.0f;
+        if (post) {
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) s += value<BD>(R.b[i], k) * value<BD>(R.b[i], k);
+            rpost = __builtin_amdgcn_rsqf(sum(s) * inv_width + B.eps);
+            if (A.rstd_post != nullptr && lane == 0) A.rstd_post[r] = rpost;
+        }
+        float y[I][VEC];
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                y[i][k] = value<SD>(R.x[i], k);
+                if (branch) {
+                    float u = value<BD>(R.b[i], k) * rpost * cb[i][k];
+                    if (gate) u *= gate_value(B.gate_act, value<DT>(R.g[i], k));
+                    y[i][k] = B.residual_scale * y[i][k] + u;
+                }
+                s += y[i][k] * y[i][k];
+            }
+        // the next row's values are under way while this one's are summed and written
+        if (r + step < B.rows) fetch(R);
+        if (A.y != nullptr) {
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+                store<SD, TAIL>(py + (long long)i * P.group * VEC * SB, y[i], full[i], part[i], P.tail);
+        }
+        if (pre) {
+            const float rpre = __builtin_amdgcn_rsqf(sum(s) * inv_width + B.eps);
+            if (A.rstd_pre != nullptr && lane == 0) A.rstd_pre[r] = rpre;
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                float h[VEC];
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) h[k] = y[i][k] * rpre * wh[i][k];
+                store<DT, TAIL>(ph + (long long)i * P.group * VEC * LB, h, full[i], part[i], P.tail);
+            }
+        }
+        py += step * A.y_stride * SB;
+        ph += step * A.h_stride * LB;
+    }
+}
+
+// ------------------------------------------------------------------------------------ rows of any width
 __device__ __forceinline__ float gate_at(const capscaps_block& B, const void* gate, long long row, long long stride,
                                          int c)
 {
@@ -223,9 +371,58 @@ int check_block(const capscaps_block* B)
     if (B->branch_dtype != CAPSCAPS_FP32 && B->branch_dtype != B->dtype) return CAPSCAPS_EINVAL;
     if ((unsigned)B->post_norm > 1 || (unsigned)B->gate > 2 || (unsigned)B->gate_act > 2) return CAPSCAPS_EINVAL;
     if (!isfinite(B->residual_scale) || !isfinite(B->branch_scale)) return CAPSCAPS_EINVAL;
-    if (!(B->eps > 0.0f) || !isfinite(B->eps)) return CAPSCAPS_EINVAL;
+    if (!(B->eps >= FLT_MIN) || !isfinite(B->eps)) return CAPSCAPS_EINVAL;  // (a normal number, for v_rsq_f32)
     if ((long double)B->rows * B->width > 1e17L) return CAPSCAPS_EINVAL;
     return CAPSCAPS_OK;
+}
+
+// The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024; two vectors each for rows of
+// more than 8192 values.
+RowPlan row_plan(const capscaps_block& B)
+{
+    RowPlan P;
+    const int vectors = (B.width + VEC - 1) / VEC;
+    P.group = 1;
+    while (P.group < vectors && P.group < 1024) P.group *= 2;
+    P.vectors = (vectors + P.group - 1) / P.group;
+    P.threads = P.group <= 64 ? 256 : P.group;
+    P.per_block = P.threads / P.group;
+    const long long blocks = (B.rows + P.per_block - 1) / P.per_block, most = CUS * 2048 / P.threads;
+    P.blocks = (unsigned)(blocks < most ? blocks : most);
+    P.full = B.width / VEC;
+    P.tail = B.width % VEC;
+    return P;
+}
+
+template <int DT, bool S16, bool B16>
+void launch_fwd(const capscaps_block& B, const capscaps_block_fwd_args& A, const RowPlan& P, hipStream_t st)
+{
+    const dim3 grid(P.blocks), threads(P.threads);
+    if (P.vectors == 1) {
+        if (P.tail)
+            block_fwd_kernel<DT, S16, B16, 1, true><<<grid, threads, 0, st>>>(B, A, P);
+        else
+            block_fwd_kernel<DT, S16, B16, 1, false><<<grid, threads, 0, st>>>(B, A, P);
+    } else {
+        if (P.tail)
+            block_fwd_kernel<DT, S16, B16, 2, true><<<grid, threads, 0, st>>>(B, A, P);
+        else
+            block_fwd_kernel<DT, S16, B16, 2, false><<<grid, threads, 0, st>>>(B, A, P);
+    }
+}
+
+template <int DT>
+void launch_fwd(const capscaps_block& B, const capscaps_block_fwd_args& A, const RowPlan& P, hipStream_t st)
+{
+    if constexpr (DT == CAPSCAPS_FP32) {
+        launch_fwd<DT, false, false>(B, A, P, st);
+    } else {
+        const bool s16 = B.stream_dtype == DT, b16 = B.branch_dtype == DT || A.branch == nullptr;
+        if (s16)
+            b16 ? launch_fwd<DT, true, true>(B, A, P, st) : launch_fwd<DT, true, false>(B, A, P, st);
+        else
+            b16 ? launch_fwd<DT, false, true>(B, A, P, st) : launch_fwd<DT, false, false>(B, A, P, st);
+    }
 }
 
 unsigned row_blocks(const capscaps_block& B) { return (unsigned)(B.rows < (1 << 20) ? B.rows : (1 << 20)); }
@@ -256,7 +453,15 @@ int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fw
     for (const float* p : {A.pre_weight, A.post_weight, (const float*)A.rstd_pre, (const float*)A.rstd_post})
         if (misaligned(p, CAPSCAPS_FP32)) return CAPSCAPS_EINVAL;
     if (A.y == A.x && A.y_stride != A.x_stride) return CAPSCAPS_EINVAL;
-    block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, static_cast<hipStream_t>(stream)>>>(B, A);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (B.width > WIDEST)
+        block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A);
+    else if (B.dtype == CAPSCAPS_FP32)
+        launch_fwd<CAPSCAPS_FP32>(B, A, row_plan(B), st);
+    else if (B.dtype == CAPSCAPS_BF16)
+        launch_fwd<CAPSCAPS_BF16>(B, A, row_plan(B), st);
+    else
+        launch_fwd<CAPSCAPS_FP16>(B, A, row_plan(B), st);
     return status_from_hip(hipGetLastError());
 }
 
