@@ -59,6 +59,8 @@ struct RowPlan {
 };
 
 constexpr int WIDEST = 16384;
+// threads of a compute unit that a launch counts on: further rows are the same threads' next ones
+constexpr int FWD_THREADS = 2048, BWD_THREADS = 1024;
 
 // Sum over a row's lanes.  Rows of more than one wave go through LDS: two buffers in turn, so that one barrier is
 // enough (a wave writes a buffer again only after the barrier of the other one, which every wave reaches after it has read).
@@ -189,6 +191,225 @@ __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capsc
         py += step * A.y_stride * SB;
         ph += step * A.h_stride * LB;
     }
+}
+
+// The way back.  Of the two sums over a row, the first (of dh * pre_weight * yn) needs y and dh, the second dy and b: each
+// pair is fetched while the other is worked on.  Sums over rows stay in registers, two for each column:
+// of dh * yn, and of d * act * bn, from which both dpost_weight and a shared gate's gradient follow, since all their other
+// factors are the column's.  A workgroup's sums go to `partial` [block][2][columns], columns in the order of lanes' places.
+template <int DT, bool S16, bool B16, int I, bool TAIL>
+__global__ void __launch_bounds__(1024)
+    block_bwd_kernel(capscaps_block B, capscaps_block_bwd_args A, RowPlan P, float* partial)
+{
+    constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
+    constexpr long long SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
+    __shared__ float lds[32];
+    RowSum sum{lds, P.group, 0};
+    const int lane = threadIdx.x & (P.group - 1);
+    const bool branch = A.branch != nullptr, gate = B.gate == CAPSCAPS_GATE_FULL, has_h = A.dh != nullptr;
+    const bool post = branch && B.post_norm && A.rstd_post != nullptr;
+    const float inv_width = 1.0f / (float)B.width;
+    const float to_x = branch ? B.residual_scale : 1.0f;
+    bool full[I], part[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        full[i] = lane + i * P.group < P.full;
+        part[i] = TAIL && lane + i * P.group == P.full;
+    }
+    // of a column: what leads from d to e, apart from a gate for every value; h's weight; the sums
+    float ce[I][VEC], wh[I][VEC], sum_h[I][VEC], sum_b[I][VEC];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        const int v = lane + i * P.group;
+        load_column<TAIL>(ce[i], post ? A.post_weight : nullptr, v, full[i], part[i], P.tail, 1.0f);
+        load_column<TAIL>(wh[i], A.pre_weight, v, full[i], part[i], P.tail, 1.0f);
+        float g[VEC];
+        const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
+        load_column<TAIL>(g, shared ? static_cast<const float*>(A.gate) : nullptr, v, full[i], part[i], P.tail, 1.0f);
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+            ce[i][k] *= B.branch_scale * (shared ? gate_value(B.gate_act, g[k]) : 1.0f);
+            sum_h[i][k] = sum_b[i][k] = 0.0f;
+        }
+    }
+    const long long first = (long long)blockIdx.x * P.per_block + threadIdx.x / P.group;
+    const long long step = (long long)gridDim.x * P.per_block;
+    const char* py = static_cast<const char*>(A.y) + (first * A.y_stride + lane * VEC) * SB;
+    const char* pdh = static_cast<const char*>(A.dh) + (first * A.dh_stride + lane * VEC) * LB;
+    const char* pdy = static_cast<const char*>(A.dy) + (first * A.dy_stride + lane * VEC) * SB;
+    const char* pb = static_cast<const char*>(A.branch) + (first * A.branch_stride + lane * VEC) * BB;
+    const char* pg = static_cast<const char*>(A.gate) + (first * A.gate_stride + lane * VEC) * LB;
+    char* pdx = static_cast<char*>(A.dx) + (first * A.dx_stride + lane * VEC) * SB;
+    char* pdb = static_cast<char*>(A.dbranch) + (first * A.dbranch_stride + lane * VEC) * LB;
+    char* pdg = static_cast<char*>(A.dgate) + (first * A.dgate_stride + lane * VEC) * LB;
+    Raw<SD> y[I], dy[I];
+    Raw<DT> dh[I], g[I];
+    Raw<BD> b[I];
+    float rpre = 1.0f, rpost = 1.0f;
+    auto fetch_h = [&](long long r) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            clear(y[i]);
+            clear(dh[i]);
+            if (has_h) {
+                load<SD, TAIL>(y[i], py + (long long)i * P.group * VEC * SB, full[i], part[i], P.tail);
+                load<DT, TAIL>(dh[i], pdh + (long long)i * P.group * VEC * LB, full[i], part[i], P.tail);
+            }
+        }
+        if (has_h) rpre = A.rstd_pre[r];
+        py += step * A.y_stride * SB;
+        pdh += step * A.dh_stride * LB;
+    };
+    auto fetch_b = [&](long long r) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            clear(dy[i]);
+            clear(b[i]);
+            clear(g[i]);
+            if (A.dy != nullptr) load<SD, TAIL>(dy[i], pdy + (long long)i * P.group * VEC * SB, full[i], part[i], P.tail);
+            if (branch) load<BD, TAIL>(b[i], pb + (long long)i * P.group * VEC * BB, full[i], part[i], P.tail);
+            if (gate) load<DT, TAIL>(g[i], pg + (long long)i * P.group * VEC * LB, full[i], part[i], P.tail);
+        }
+        if (post) rpost = A.rstd_post[r];
+        pdy += step * A.dy_stride * SB;
+        pb += step * A.branch_stride * BB;
+        pg += step * A.gate_stride * LB;
+    };
+    if (first < B.rows) fetch_h(first);
+    for (long long r = first; r < B.rows; r += step) {
+        fetch_b(r);
+        float s = 0.0f, mean = 0.0f;
+        if (has_h) {
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k)
+                    s += value<DT>(dh[i], k) * wh[i][k] * (value<SD>(y[i], k) * rpre);
+            mean = sum(s) * inv_width;
+        }
+        float e[I][VEC];
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            float dx[VEC], dg[VEC];
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) {
+                const float yn = value<SD>(y[i], k) * rpre, h = value<DT>(dh[i], k);
+                sum_h[i][k] += h * yn;
+                float d = value<SD>(dy[i], k);
+                if (has_h) d += rpre * (h * wh[i][k] - yn * mean);
+                dx[k] = to_x * d;
+                const float bn = value<BD>(b[i], k) * rpost;
+                if (gate) {
+                    const float gk = value<DT>(g[i], k);
+                    dg[k] = d * ce[i][k] * bn * gate_slope(B.gate_act, gk);
+                    d *= gate_value(B.gate_act, gk);
+                }
+                sum_b[i][k] += d * bn;
+                e[i][k] = d * ce[i][k];
+                s += e[i][k] * bn;
+            }
+            if (A.dx != nullptr)
+                store<SD, TAIL>(pdx + (long long)i * P.group * VEC * SB, dx, full[i], part[i], P.tail);
+            if (gate && A.dgate != nullptr)
+                store<DT, TAIL>(pdg + (long long)i * P.group * VEC * LB, dg, full[i], part[i], P.tail);
+        }
+        if (r + step < B.rows) fetch_h(r + step);
+        if (A.dbranch != nullptr) {
+            mean = post ? sum(s) * inv_width : 0.0f;
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                float db[VEC];
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) db[k] = rpost * (e[i][k] - value<BD>(b[i], k) * rpost * mean);
+                store<DT, TAIL>(pdb + (long long)i * P.group * VEC * LB, db, full[i], part[i], P.tail);
+            }
+        }
+        pdx += step * A.dx_stride * SB;
+        pdb += step * A.dbranch_stride * LB;
+        pdg += step * A.dgate_stride * LB;
+    }
+    if (partial == nullptr) return;
+    const int columns = P.vectors * P.group * VEC;
+    float* out = partial + (long long)blockIdx.x * 2 * columns;
+    if (P.group >= 64) {
+        // (one row at a time in a wave; waves that share columns are of different rows only where group = 64)
+        if (P.group > 64) {
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    out[(lane + i * P.group) * VEC + k] = sum_h[i][k];
+                    out[columns + (lane + i * P.group) * VEC + k] = sum_b[i][k];
+                }
+            return;
+        }
+    } else {
+        // rows of one wave, in halves: lanes that hold the same columns
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int k = 0; k < VEC; ++k)
+                for (int o = 32; o >= P.group; o >>= 1) {
+                    sum_h[i][k] += __shfl_xor(sum_h[i][k], o);
+                    sum_b[i][k] += __shfl_xor(sum_b[i][k], o);
+                }
+    }
+    // the rows of the four waves
+    __shared__ float of_wave[THREADS / 64][64 * VEC];
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            __syncthreads();
+            if ((int)(threadIdx.x & 63) < P.group) {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k)
+                    of_wave[threadIdx.x >> 6][lane * VEC + k] = which == 0 ? sum_h[i][k] : sum_b[i][k];
+            }
+            __syncthreads();
+            for (int c = threadIdx.x; c < P.group * VEC; c += THREADS)
+                out[which * columns + i * P.group * VEC + c] =
+                    (of_wave[0][c] + of_wave[1][c]) + (of_wave[2][c] + of_wave[3][c]);
+        }
+}
+
+// Place of column j of a row's last, partial vector (row_vectors.h)
+__device__ __forceinline__ int tail_place(int j, int tail)
+{
+    if (j < (tail & 4)) return j;
+    return j < (tail & 6) ? 4 + j - (tail & 4) : 6;
+}
+
+// Sums the workgroups' sums, 64 columns a workgroup, each by 16 threads that take every 16th in turn
+__global__ void __launch_bounds__(1024)
+    block_bwd_sums_kernel(capscaps_block B, capscaps_block_bwd_args A, RowPlan P, const float* partial)
+{
+    __shared__ float lds[16][64];
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), share = threadIdx.x >> 6;
+    const int columns = P.vectors * P.group * VEC;
+    float s = 0.0f;
+    if (c < B.width) {
+        const int place = c / VEC < P.full ? c : P.full * VEC + tail_place(c % VEC, P.tail);
+        const float* p = partial + (long long)blockIdx.y * columns + place;
+#pragma unroll 8
+        for (int k = share; k < (int)P.blocks; k += 16) s += p[(long long)k * 2 * columns];
+    }
+    lds[share][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (share != 0 || c >= B.width) return;
+    for (int k = 1; k < 16; ++k) s += lds[k][threadIdx.x];
+    if (blockIdx.y == 0) {
+        if (A.dpre_weight != nullptr) A.dpre_weight[c] = s;
+        return;
+    }
+    s *= B.branch_scale;
+    const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
+    const float g = shared ? static_cast<const float*>(A.gate)[c] : 1.0f;
+    if (A.dpost_weight != nullptr) A.dpost_weight[c] = shared ? s * gate_value(B.gate_act, g) : s;
+    if (shared && A.dgate != nullptr)
+        static_cast<float*>(A.dgate)[c] = s * (B.post_norm && A.post_weight != nullptr ? A.post_weight[c] : 1.0f) *
+                                          gate_slope(B.gate_act, g);
 }
 
 // ------------------------------------------------------------------------------------ rows of any width
@@ -378,7 +599,7 @@ int check_block(const capscaps_block* B)
 
 // The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024; two vectors each for rows of
 // more than 8192 values.
-RowPlan row_plan(const capscaps_block& B)
+RowPlan row_plan(const capscaps_block& B, int threads_per_cu)
 {
     RowPlan P;
     const int vectors = (B.width + VEC - 1) / VEC;
@@ -387,7 +608,7 @@ RowPlan row_plan(const capscaps_block& B)
     P.vectors = (vectors + P.group - 1) / P.group;
     P.threads = P.group <= 64 ? 256 : P.group;
     P.per_block = P.threads / P.group;
-    const long long blocks = (B.rows + P.per_block - 1) / P.per_block, most = CUS * 2048 / P.threads;
+    const long long blocks = (B.rows + P.per_block - 1) / P.per_block, most = CUS * threads_per_cu / P.threads;
     P.blocks = (unsigned)(blocks < most ? blocks : most);
     P.full = B.width / VEC;
     P.tail = B.width % VEC;
@@ -408,6 +629,40 @@ void launch_fwd(const capscaps_block& B, const capscaps_block_fwd_args& A, const
             block_fwd_kernel<DT, S16, B16, 2, true><<<grid, threads, 0, st>>>(B, A, P);
         else
             block_fwd_kernel<DT, S16, B16, 2, false><<<grid, threads, 0, st>>>(B, A, P);
+    }
+}
+
+template <int DT, bool S16, bool B16>
+void launch_bwd(const capscaps_block& B, const capscaps_block_bwd_args& A, const RowPlan& P, float* partial,
+                hipStream_t st)
+{
+    const dim3 grid(P.blocks), threads(P.threads);
+    if (P.vectors == 1) {
+        if (P.tail)
+            block_bwd_kernel<DT, S16, B16, 1, true><<<grid, threads, 0, st>>>(B, A, P, partial);
+        else
+            block_bwd_kernel<DT, S16, B16, 1, false><<<grid, threads, 0, st>>>(B, A, P, partial);
+    } else {
+        if (P.tail)
+            block_bwd_kernel<DT, S16, B16, 2, true><<<grid, threads, 0, st>>>(B, A, P, partial);
+        else
+            block_bwd_kernel<DT, S16, B16, 2, false><<<grid, threads, 0, st>>>(B, A, P, partial);
+    }
+}
+
+template <int DT>
+void launch_bwd(const capscaps_block& B, const capscaps_block_bwd_args& A, const RowPlan& P, float* partial,
+                hipStream_t st)
+{
+    if constexpr (DT == CAPSCAPS_FP32) {
+        launch_bwd<DT, false, false>(B, A, P, partial, st);
+    } else {
+        const bool s16 = B.stream_dtype == DT, b16 = B.branch_dtype == DT || A.branch == nullptr;
+        if (s16)
+            b16 ? launch_bwd<DT, true, true>(B, A, P, partial, st) : launch_bwd<DT, true, false>(B, A, P, partial, st);
+        else
+            b16 ? launch_bwd<DT, false, true>(B, A, P, partial, st)
+                : launch_bwd<DT, false, false>(B, A, P, partial, st);
     }
 }
 
@@ -457,17 +712,21 @@ int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fw
     if (B.width > WIDEST)
         block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A);
     else if (B.dtype == CAPSCAPS_FP32)
-        launch_fwd<CAPSCAPS_FP32>(B, A, row_plan(B), st);
+        launch_fwd<CAPSCAPS_FP32>(B, A, row_plan(B, FWD_THREADS), st);
     else if (B.dtype == CAPSCAPS_BF16)
-        launch_fwd<CAPSCAPS_BF16>(B, A, row_plan(B), st);
+        launch_fwd<CAPSCAPS_BF16>(B, A, row_plan(B, FWD_THREADS), st);
     else
-        launch_fwd<CAPSCAPS_FP16>(B, A, row_plan(B), st);
+        launch_fwd<CAPSCAPS_FP16>(B, A, row_plan(B, FWD_THREADS), st);
     return status_from_hip(hipGetLastError());
 }
 
 size_t capscaps_block_norm_bwd_workspace_bytes(const capscaps_block* block)
 {
     if (check_block(block) != CAPSCAPS_OK) return 0;
+    if (block->width <= WIDEST) {
+        const RowPlan P = row_plan(*block, BWD_THREADS);
+        return (size_t)P.blocks * 2 * P.vectors * P.group * VEC * 4;
+    }
     const size_t means = (size_t)block->rows * 4, sums = (size_t)row_shares(block->rows) * 3 * block->width * 4;
     return (means + 255) / 256 * 256 + sums;
 }
@@ -510,6 +769,20 @@ int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bw
         if ((reinterpret_cast<uintptr_t>(workspace) & 15u) != 0) return CAPSCAPS_EINVAL;
     }
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (B.width <= WIDEST) {
+        const RowPlan P = row_plan(B, BWD_THREADS);
+        float* partial = sums ? static_cast<float*>(workspace) : nullptr;
+        if (B.dtype == CAPSCAPS_FP32)
+            launch_bwd<CAPSCAPS_FP32>(B, A, P, partial, st);
+        else if (B.dtype == CAPSCAPS_BF16)
+            launch_bwd<CAPSCAPS_BF16>(B, A, P, partial, st);
+        else
+            launch_bwd<CAPSCAPS_FP16>(B, A, P, partial, st);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess || !sums) return status_from_hip(err);
+        block_bwd_sums_kernel<<<dim3((B.width + 63) / 64, 2), dim3(1024), 0, st>>>(B, A, P, partial);
+        return status_from_hip(hipGetLastError());
+    }
     float* mean = sums ? static_cast<float*>(workspace) : nullptr;
     block_bwd_rows_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A, mean);
     hipError_t err = hipGetLastError();
