@@ -10,6 +10,9 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <initializer_list>
+#include <type_traits>
+
 #include "../../include/capscaps.h"
 #include "conv_shape.h"
 #include "element.h"
@@ -21,19 +24,19 @@ namespace {
 constexpr int THREADS = 256;
 constexpr int CUS = 256;
 
-// act(g) and its derivative
-__device__ __forceinline__ float gate_value(int act, float g)
+// act(g) and its derivative (v_rcp_f32 is off by one unit in the last place)
+struct Gate {
+    float value, slope;
+};
+__device__ __forceinline__ Gate gate_both(int act, float g)
 {
-    if (act == CAPSCAPS_ACT_LINEAR) return g;
-    const float q = 1.0f / (1.0f + __expf(-g));
-    return act == CAPSCAPS_ACT_SIGMOID ? q : g * q;
+    if (act == CAPSCAPS_ACT_LINEAR) return {g, 1.0f};
+    const float q = __builtin_amdgcn_rcpf(1.0f + __expf(-g));
+    if (act == CAPSCAPS_ACT_SIGMOID) return {q, q * (1.0f - q)};
+    return {g * q, q * (1.0f + g * (1.0f - q))};
 }
-__device__ __forceinline__ float gate_slope(int act, float g)
-{
-    if (act == CAPSCAPS_ACT_LINEAR) return 1.0f;
-    const float q = 1.0f / (1.0f + __expf(-g));
-    return act == CAPSCAPS_ACT_SIGMOID ? q * (1.0f - q) : q * (1.0f + g * (1.0f - q));
-}
+__device__ __forceinline__ float gate_value(int act, float g) { return gate_both(act, g).value; }
+__device__ __forceinline__ float gate_slope(int act, float g) { return gate_both(act, g).slope; }
 
 // sum over the workgroup, in every thread
 __device__ __forceinline__ float block_sum(float v, float* lds)
@@ -83,78 +86,101 @@ struct RowSum {
     }
 };
 
-template <int DT, bool S16, bool B16, int I>
-struct FwdRow {
-    static constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
+// A tensor's rows as the lanes of a workgroup see them: where its rows of this round begin (the same for all lanes, so
+// it stays in scalar registers), and a lane's place from there
+struct Rows {
+    const char* base;
+    long long step;  // bytes to the next round's
+    unsigned at;
+    template <typename T>
+    __device__ __forceinline__ Rows(T* p, long long stride, int bytes, const RowPlan& P, int slot, int lane)
+    {
+        base = (const char*)p + (long long)blockIdx.x * P.per_block * stride * bytes;
+        step = (long long)gridDim.x * P.per_block * stride * bytes;
+        at = (unsigned)(slot * stride * bytes) + (unsigned)(lane * VEC * bytes);
+    }
+    __device__ __forceinline__ const char* get(int i, const RowPlan& P, int bytes) const
+    {
+        return base + (long long)(i * P.group * VEC * bytes) + at;
+    }
+    __device__ __forceinline__ char* put(int i, const RowPlan& P, int bytes) const { return const_cast<char*>(get(i, P, bytes)); }
+    __device__ __forceinline__ void next() { base += step; }
+};
+
+// What a column's factors are from pre-norm weight, post-norm weight and a shared gate
+template <int I, bool TAIL>
+struct Columns {
+    float to_b[I][VEC], to_h[I][VEC];
+    __device__ __forceinline__ void load_all(const capscaps_block& B, const float* pre_weight, const float* post_weight,
+                                             const void* gate, const RowPlan& P, int lane)
+    {
+        const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int v = lane + i * P.group;
+            const bool full = v < P.full, part = TAIL && v == P.full;
+            load_column<TAIL>(to_b[i], post_weight, v, full, part, P.tail, 1.0f);
+            load_column<TAIL>(to_h[i], pre_weight, v, full, part, P.tail, 1.0f);
+            float g[VEC];
+            load_column<TAIL>(g, shared ? static_cast<const float*>(gate) : nullptr, v, full, part, P.tail, 1.0f);
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) to_b[i][k] *= B.branch_scale * (shared ? gate_value(B.gate_act, g[k]) : 1.0f);
+        }
+    }
+};
+
+// GATE: a gate for every value
+template <int DT, bool S16, bool B16, bool GATE, int I, bool TAIL>
+__global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capscaps_block_fwd_args A, RowPlan P)
+{
+    constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
+    constexpr int SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
+    __shared__ float lds[32];
+    RowSum sum{lds, P.group, 0};
+    const int lane = threadIdx.x & (P.group - 1), slot = threadIdx.x / P.group;
+    const bool branch = A.branch != nullptr, post = branch && B.post_norm, pre = A.h != nullptr;
+    const float inv_width = 1.0f / (float)B.width;
+    Columns<I, TAIL> col;
+    col.load_all(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane);
+    Rows rx(A.x, A.x_stride, SB, P, slot, lane), rb(A.branch, A.branch_stride, BB, P, slot, lane);
+    Rows rg(A.gate, A.gate_stride, LB, P, slot, lane);
+    Rows ry(A.y, A.y_stride, SB, P, slot, lane), rh(A.h, A.h_stride, LB, P, slot, lane);
     Raw<SD> x[I];
     Raw<BD> b[I];
     Raw<DT> g[I];
-};
-
-template <int DT, bool S16, bool B16, int I, bool TAIL>
-__global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capscaps_block_fwd_args A, RowPlan P)
-{
-    typedef FwdRow<DT, S16, B16, I> Row;
-    constexpr int SD = Row::SD, BD = Row::BD;
-    constexpr long long SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
-    __shared__ float lds[32];
-    RowSum sum{lds, P.group, 0};
-    const int lane = threadIdx.x & (P.group - 1);
-    const bool branch = A.branch != nullptr, gate = B.gate == CAPSCAPS_GATE_FULL;
-    const bool post = branch && B.post_norm, pre = A.h != nullptr;
-    const float inv_width = 1.0f / (float)B.width;
-    bool full[I], part[I];
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
-        full[i] = lane + i * P.group < P.full;
-        part[i] = TAIL && lane + i * P.group == P.full;
-    }
-    // of a column: what multiplies b, apart from its statistic and a gate for every value; and h's weight
-    float cb[I][VEC], wh[I][VEC];
-#pragma unroll
-    for (int i = 0; i < I; ++i) {
-        const int v = lane + i * P.group;
-        load_column<TAIL>(cb[i], post ? A.post_weight : nullptr, v, full[i], part[i], P.tail, 1.0f);
-        load_column<TAIL>(wh[i], A.pre_weight, v, full[i], part[i], P.tail, 1.0f);
-        float g[VEC];
-        const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
-        load_column<TAIL>(g, shared ? static_cast<const float*>(A.gate) : nullptr, v, full[i], part[i], P.tail, 1.0f);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) cb[i][k] *= B.branch_scale * (shared ? gate_value(B.gate_act, g[k]) : 1.0f);
-    }
-    const long long first = (long long)blockIdx.x * P.per_block + threadIdx.x / P.group;
-    const long long step = (long long)gridDim.x * P.per_block;
-    const char* px = static_cast<const char*>(A.x) + (first * A.x_stride + lane * VEC) * SB;
-    const char* pb = static_cast<const char*>(A.branch) + (first * A.branch_stride + lane * VEC) * BB;
-    const char* pg = static_cast<const char*>(A.gate) + (first * A.gate_stride + lane * VEC) * LB;
-    char* py = static_cast<char*>(A.y) + (first * A.y_stride + lane * VEC) * SB;
-    char* ph = static_cast<char*>(A.h) + (first * A.h_stride + lane * VEC) * LB;
-    auto fetch = [&](Row& R) {
+    auto fetch = [&](bool in) {
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            clear(R.x[i]);
-            clear(R.b[i]);
-            clear(R.g[i]);
-            load<SD, TAIL>(R.x[i], px + (long long)i * P.group * VEC * SB, full[i], part[i], P.tail);
-            if (branch) load<BD, TAIL>(R.b[i], pb + (long long)i * P.group * VEC * BB, full[i], part[i], P.tail);
-            if (gate) load<DT, TAIL>(R.g[i], pg + (long long)i * P.group * VEC * LB, full[i], part[i], P.tail);
+            const int v = lane + i * P.group;
+            const bool full = in && v < P.full, part = TAIL && in && v == P.full;
+            clear(x[i]);
+            clear(b[i]);
+            load<SD, TAIL>(x[i], rx.get(i, P, SB), full, part, P.tail);
+            if (branch) load<BD, TAIL>(b[i], rb.get(i, P, BB), full, part, P.tail);
+            if constexpr (GATE) {
+                clear(g[i]);
+                load<DT, TAIL>(g[i], rg.get(i, P, LB), full, part, P.tail);
+            }
         }
-        px += step * A.x_stride * SB;
-        pb += step * A.branch_stride * BB;
-        pg += step * A.gate_stride * LB;
+        rx.next();
+        rb.next();
+        rg.next();
     };
-    Row R;
-    if (first < B.rows) fetch(R);
-    for (long long r = first; r < B.rows; r += step) {
+    const long long step = (long long)gridDim.x * P.per_block;
+    long long left = B.rows - (long long)blockIdx.x * P.per_block;  // rows from this round's first one on
+    fetch(slot < left);
+    for (; left > 0; left -= step) {
+        const bool in = slot < left;
+        const long long r = B.rows - left + slot;
         float rpost = 1.0f;
         if (post) {
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) s += value<BD>(R.b[i], k) * value<BD>(R.b[i], k);
+                for (int k = 0; k < VEC; ++k) s += value<BD>(b[i], k) * value<BD>(b[i], k);
             rpost = __builtin_amdgcn_rsqf(sum(s) * inv_width + B.eps);
-            if (A.rstd_post != nullptr && lane == 0) A.rstd_post[r] = rpost;
+            if (A.rstd_post != nullptr && lane == 0 && in) A.rstd_post[r] = rpost;
         }
         float y[I][VEC];
         float s = 0.0f;
@@ -162,34 +188,37 @@ __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capsc
         for (int i = 0; i < I; ++i)
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
-                y[i][k] = value<SD>(R.x[i], k);
+                y[i][k] = value<SD>(x[i], k);
                 if (branch) {
-                    float u = value<BD>(R.b[i], k) * rpost * cb[i][k];
-                    if (gate) u *= gate_value(B.gate_act, value<DT>(R.g[i], k));
+                    float u = value<BD>(b[i], k) * rpost * col.to_b[i][k];
+                    if constexpr (GATE) u *= gate_value(B.gate_act, value<DT>(g[i], k));
                     y[i][k] = B.residual_scale * y[i][k] + u;
                 }
                 s += y[i][k] * y[i][k];
             }
-        // the next row's values are under way while this one's are summed and written
-        if (r + step < B.rows) fetch(R);
+        // the next rows' values are under way while these are summed and written
+        if (left > step) fetch(slot < left - step);
         if (A.y != nullptr) {
 #pragma unroll
-            for (int i = 0; i < I; ++i)
-                store<SD, TAIL>(py + (long long)i * P.group * VEC * SB, y[i], full[i], part[i], P.tail);
+            for (int i = 0; i < I; ++i) {
+                const int v = lane + i * P.group;
+                store<SD, TAIL>(ry.put(i, P, SB), y[i], in && v < P.full, in && v == P.full, P.tail);
+            }
         }
         if (pre) {
             const float rpre = __builtin_amdgcn_rsqf(sum(s) * inv_width + B.eps);
-            if (A.rstd_pre != nullptr && lane == 0) A.rstd_pre[r] = rpre;
+            if (A.rstd_pre != nullptr && lane == 0 && in) A.rstd_pre[r] = rpre;
 #pragma unroll
             for (int i = 0; i < I; ++i) {
+                const int v = lane + i * P.group;
                 float h[VEC];
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) h[k] = y[i][k] * rpre * wh[i][k];
-                store<DT, TAIL>(ph + (long long)i * P.group * VEC * LB, h, full[i], part[i], P.tail);
+                for (int k = 0; k < VEC; ++k) h[k] = y[i][k] * rpre * col.to_h[i][k];
+                store<DT, TAIL>(rh.put(i, P, LB), h, in && v < P.full, in && v == P.full, P.tail);
             }
         }
-        py += step * A.y_stride * SB;
-        ph += step * A.h_stride * LB;
+        ry.next();
+        rh.next();
     }
 }
 
@@ -197,164 +226,152 @@ __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capsc
 // pair is fetched while the other is worked on.  Sums over rows stay in registers, two for each column:
 // of dh * yn, and of d * act * bn, from which both dpost_weight and a shared gate's gradient follow, since all their other
 // factors are the column's.  A workgroup's sums go to `partial` [block][2][columns], columns in the order of lanes' places.
-template <int DT, bool S16, bool B16, int I, bool TAIL>
+template <int DT, bool S16, bool B16, bool GATE, int I, bool TAIL>
 __global__ void __launch_bounds__(1024)
     block_bwd_kernel(capscaps_block B, capscaps_block_bwd_args A, RowPlan P, float* partial)
 {
     constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
-    constexpr long long SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
+    constexpr int SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
     __shared__ float lds[32];
     RowSum sum{lds, P.group, 0};
-    const int lane = threadIdx.x & (P.group - 1);
-    const bool branch = A.branch != nullptr, gate = B.gate == CAPSCAPS_GATE_FULL, has_h = A.dh != nullptr;
+    const int lane = threadIdx.x & (P.group - 1), slot = threadIdx.x / P.group;
+    const bool branch = A.branch != nullptr, has_h = A.dh != nullptr;
     const bool post = branch && B.post_norm && A.rstd_post != nullptr;
     const float inv_width = 1.0f / (float)B.width;
     const float to_x = branch ? B.residual_scale : 1.0f;
-    bool full[I], part[I];
+    Columns<I, TAIL> col;
+    col.load_all(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane);
+    float sum_h[I][VEC], sum_b[I][VEC];
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-        full[i] = lane + i * P.group < P.full;
-        part[i] = TAIL && lane + i * P.group == P.full;
-    }
-    // of a column: what leads from d to e, apart from a gate for every value; h's weight; the sums
-    float ce[I][VEC], wh[I][VEC], sum_h[I][VEC], sum_b[I][VEC];
+    for (int i = 0; i < I; ++i)
 #pragma unroll
-    for (int i = 0; i < I; ++i) {
-        const int v = lane + i * P.group;
-        load_column<TAIL>(ce[i], post ? A.post_weight : nullptr, v, full[i], part[i], P.tail, 1.0f);
-        load_column<TAIL>(wh[i], A.pre_weight, v, full[i], part[i], P.tail, 1.0f);
-        float g[VEC];
-        const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
-        load_column<TAIL>(g, shared ? static_cast<const float*>(A.gate) : nullptr, v, full[i], part[i], P.tail, 1.0f);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            ce[i][k] *= B.branch_scale * (shared ? gate_value(B.gate_act, g[k]) : 1.0f);
-            sum_h[i][k] = sum_b[i][k] = 0.0f;
-        }
-    }
-    const long long first = (long long)blockIdx.x * P.per_block + threadIdx.x / P.group;
-    const long long step = (long long)gridDim.x * P.per_block;
-    const char* py = static_cast<const char*>(A.y) + (first * A.y_stride + lane * VEC) * SB;
-    const char* pdh = static_cast<const char*>(A.dh) + (first * A.dh_stride + lane * VEC) * LB;
-    const char* pdy = static_cast<const char*>(A.dy) + (first * A.dy_stride + lane * VEC) * SB;
-    const char* pb = static_cast<const char*>(A.branch) + (first * A.branch_stride + lane * VEC) * BB;
-    const char* pg = static_cast<const char*>(A.gate) + (first * A.gate_stride + lane * VEC) * LB;
-    char* pdx = static_cast<char*>(A.dx) + (first * A.dx_stride + lane * VEC) * SB;
-    char* pdb = static_cast<char*>(A.dbranch) + (first * A.dbranch_stride + lane * VEC) * LB;
-    char* pdg = static_cast<char*>(A.dgate) + (first * A.dgate_stride + lane * VEC) * LB;
+        for (int k = 0; k < VEC; ++k) sum_h[i][k] = sum_b[i][k] = 0.0f;
+    Rows ry(A.y, A.y_stride, SB, P, slot, lane), rdh(A.dh, A.dh_stride, LB, P, slot, lane);
+    Rows rdy(A.dy, A.dy_stride, SB, P, slot, lane), rb(A.branch, A.branch_stride, BB, P, slot, lane);
+    Rows rg(A.gate, A.gate_stride, LB, P, slot, lane), rdg(A.dgate, A.dgate_stride, LB, P, slot, lane);
+    Rows rdx(A.dx, A.dx_stride, SB, P, slot, lane), rdb(A.dbranch, A.dbranch_stride, LB, P, slot, lane);
     Raw<SD> y[I], dy[I];
     Raw<DT> dh[I], g[I];
     Raw<BD> b[I];
     float rpre = 1.0f, rpost = 1.0f;
-    auto fetch_h = [&](long long r) {
+    auto fetch_h = [&](bool in, long long r) {
 #pragma unroll
         for (int i = 0; i < I; ++i) {
+            const int v = lane + i * P.group;
+            const bool full = in && v < P.full, part = TAIL && in && v == P.full;
             clear(y[i]);
             clear(dh[i]);
             if (has_h) {
-                load<SD, TAIL>(y[i], py + (long long)i * P.group * VEC * SB, full[i], part[i], P.tail);
-                load<DT, TAIL>(dh[i], pdh + (long long)i * P.group * VEC * LB, full[i], part[i], P.tail);
+                load<SD, TAIL>(y[i], ry.get(i, P, SB), full, part, P.tail);
+                load<DT, TAIL>(dh[i], rdh.get(i, P, LB), full, part, P.tail);
             }
         }
-        if (has_h) rpre = A.rstd_pre[r];
-        py += step * A.y_stride * SB;
-        pdh += step * A.dh_stride * LB;
+        if (has_h && in) rpre = A.rstd_pre[r];
+        ry.next();
+        rdh.next();
     };
-    auto fetch_b = [&](long long r) {
+    auto fetch_b = [&](bool in, long long r) {
 #pragma unroll
         for (int i = 0; i < I; ++i) {
+            const int v = lane + i * P.group;
+            const bool full = in && v < P.full, part = TAIL && in && v == P.full;
             clear(dy[i]);
             clear(b[i]);
-            clear(g[i]);
-            if (A.dy != nullptr) load<SD, TAIL>(dy[i], pdy + (long long)i * P.group * VEC * SB, full[i], part[i], P.tail);
-            if (branch) load<BD, TAIL>(b[i], pb + (long long)i * P.group * VEC * BB, full[i], part[i], P.tail);
-            if (gate) load<DT, TAIL>(g[i], pg + (long long)i * P.group * VEC * LB, full[i], part[i], P.tail);
+            if (A.dy != nullptr) load<SD, TAIL>(dy[i], rdy.get(i, P, SB), full, part, P.tail);
+            if (branch) load<BD, TAIL>(b[i], rb.get(i, P, BB), full, part, P.tail);
+            if constexpr (GATE) {
+                clear(g[i]);
+                load<DT, TAIL>(g[i], rg.get(i, P, LB), full, part, P.tail);
+            }
         }
-        if (post) rpost = A.rstd_post[r];
-        pdy += step * A.dy_stride * SB;
-        pb += step * A.branch_stride * BB;
-        pg += step * A.gate_stride * LB;
+        if (post && in) rpost = A.rstd_post[r];
+        rdy.next();
+        rb.next();
+        rg.next();
     };
-    if (first < B.rows) fetch_h(first);
-    for (long long r = first; r < B.rows; r += step) {
-        fetch_b(r);
+    const long long step = (long long)gridDim.x * P.per_block;
+    long long left = B.rows - (long long)blockIdx.x * P.per_block;  // rows from this round's first one on
+    fetch_h(slot < left, B.rows - left + slot);
+    for (; left > 0; left -= step) {
+        const bool in = slot < left;
+        const long long r = B.rows - left + slot;
+        fetch_b(in, r);
         float s = 0.0f, mean = 0.0f;
         if (has_h) {
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
-                for (int k = 0; k < VEC; ++k)
-                    s += value<DT>(dh[i], k) * wh[i][k] * (value<SD>(y[i], k) * rpre);
+                for (int k = 0; k < VEC; ++k) s += value<DT>(dh[i], k) * col.to_h[i][k] * (value<SD>(y[i], k) * rpre);
             mean = sum(s) * inv_width;
         }
         float e[I][VEC];
         s = 0.0f;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
+            const int v = lane + i * P.group;
             float dx[VEC], dg[VEC];
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
                 const float yn = value<SD>(y[i], k) * rpre, h = value<DT>(dh[i], k);
                 sum_h[i][k] += h * yn;
                 float d = value<SD>(dy[i], k);
-                if (has_h) d += rpre * (h * wh[i][k] - yn * mean);
+                if (has_h) d += rpre * (h * col.to_h[i][k] - yn * mean);
                 dx[k] = to_x * d;
                 const float bn = value<BD>(b[i], k) * rpost;
-                if (gate) {
-                    const float gk = value<DT>(g[i], k);
-                    dg[k] = d * ce[i][k] * bn * gate_slope(B.gate_act, gk);
-                    d *= gate_value(B.gate_act, gk);
+                if constexpr (GATE) {
+                    const Gate q = gate_both(B.gate_act, value<DT>(g[i], k));
+                    dg[k] = d * col.to_b[i][k] * bn * q.slope;
+                    d *= q.value;
                 }
                 sum_b[i][k] += d * bn;
-                e[i][k] = d * ce[i][k];
+                e[i][k] = d * col.to_b[i][k];
                 s += e[i][k] * bn;
             }
             if (A.dx != nullptr)
-                store<SD, TAIL>(pdx + (long long)i * P.group * VEC * SB, dx, full[i], part[i], P.tail);
-            if (gate && A.dgate != nullptr)
-                store<DT, TAIL>(pdg + (long long)i * P.group * VEC * LB, dg, full[i], part[i], P.tail);
+                store<SD, TAIL>(rdx.put(i, P, SB), dx, in && v < P.full, in && v == P.full, P.tail);
+            if constexpr (GATE) {
+                if (A.dgate != nullptr)
+                    store<DT, TAIL>(rdg.put(i, P, LB), dg, in && v < P.full, in && v == P.full, P.tail);
+            }
         }
-        if (r + step < B.rows) fetch_h(r + step);
+        if (left > step) fetch_h(slot < left - step, r + step);
         if (A.dbranch != nullptr) {
             mean = post ? sum(s) * inv_width : 0.0f;
 #pragma unroll
             for (int i = 0; i < I; ++i) {
+                const int v = lane + i * P.group;
                 float db[VEC];
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) db[k] = rpost * (e[i][k] - value<BD>(b[i], k) * rpost * mean);
-                store<DT, TAIL>(pdb + (long long)i * P.group * VEC * LB, db, full[i], part[i], P.tail);
+                store<DT, TAIL>(rdb.put(i, P, LB), db, in && v < P.full, in && v == P.full, P.tail);
             }
         }
-        pdx += step * A.dx_stride * SB;
-        pdb += step * A.dbranch_stride * LB;
-        pdg += step * A.dgate_stride * LB;
+        rdx.next();
+        rdb.next();
+        rdg.next();
     }
     if (partial == nullptr) return;
     const int columns = P.vectors * P.group * VEC;
     float* out = partial + (long long)blockIdx.x * 2 * columns;
-    if (P.group >= 64) {
-        // (one row at a time in a wave; waves that share columns are of different rows only where group = 64)
-        if (P.group > 64) {
-#pragma unroll
-            for (int i = 0; i < I; ++i)
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) {
-                    out[(lane + i * P.group) * VEC + k] = sum_h[i][k];
-                    out[columns + (lane + i * P.group) * VEC + k] = sum_b[i][k];
-                }
-            return;
-        }
-    } else {
-        // rows of one wave, in halves: lanes that hold the same columns
+    if (P.per_block == 1) {
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
-            for (int k = 0; k < VEC; ++k)
-                for (int o = 32; o >= P.group; o >>= 1) {
-                    sum_h[i][k] += __shfl_xor(sum_h[i][k], o);
-                    sum_b[i][k] += __shfl_xor(sum_b[i][k], o);
-                }
+            for (int k = 0; k < VEC; ++k) {
+                out[(lane + i * P.group) * VEC + k] = sum_h[i][k];
+                out[columns + (lane + i * P.group) * VEC + k] = sum_b[i][k];
+            }
+        return;
     }
+    // rows of one wave, in halves: lanes that hold the same columns
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+            for (int o = 32; o >= P.group; o >>= 1) {
+                sum_h[i][k] += __shfl_xor(sum_h[i][k], o);
+                sum_b[i][k] += __shfl_xor(sum_b[i][k], o);
+            }
     // the rows of the four waves
     __shared__ float of_wave[THREADS / 64][64 * VEC];
 #pragma unroll
@@ -598,86 +615,74 @@ int check_block(const capscaps_block* B)
 }
 
 // The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024; two vectors each for rows of
-// more than 8192 values.
-RowPlan row_plan(const capscaps_block& B, int threads_per_cu)
+// more than 8192 values.  `apart`: rows so far apart that those of one workgroup are not within reach of 32-bit offsets, one at a
+// time in a workgroup.
+RowPlan row_plan(const capscaps_block& B, int threads_per_cu, bool apart)
 {
     RowPlan P;
     const int vectors = (B.width + VEC - 1) / VEC;
-    P.group = 1;
+    P.group = apart ? 64 : 1;
     while (P.group < vectors && P.group < 1024) P.group *= 2;
     P.vectors = (vectors + P.group - 1) / P.group;
-    P.threads = P.group <= 64 ? 256 : P.group;
+    P.threads = P.group > 64 || apart ? P.group : THREADS;
     P.per_block = P.threads / P.group;
-    const long long blocks = (B.rows + P.per_block - 1) / P.per_block, most = CUS * threads_per_cu / P.threads;
+    const long long blocks = (B.rows + P.per_block - 1) / P.per_block;
+    const long long most = apart ? CUS : CUS * threads_per_cu / P.threads;
     P.blocks = (unsigned)(blocks < most ? blocks : most);
     P.full = B.width / VEC;
     P.tail = B.width % VEC;
     return P;
 }
-
-template <int DT, bool S16, bool B16>
-void launch_fwd(const capscaps_block& B, const capscaps_block_fwd_args& A, const RowPlan& P, hipStream_t st)
+bool rows_apart(std::initializer_list<long long> strides)
 {
-    const dim3 grid(P.blocks), threads(P.threads);
-    if (P.vectors == 1) {
-        if (P.tail)
-            block_fwd_kernel<DT, S16, B16, 1, true><<<grid, threads, 0, st>>>(B, A, P);
-        else
-            block_fwd_kernel<DT, S16, B16, 1, false><<<grid, threads, 0, st>>>(B, A, P);
-    } else {
-        if (P.tail)
-            block_fwd_kernel<DT, S16, B16, 2, true><<<grid, threads, 0, st>>>(B, A, P);
-        else
-            block_fwd_kernel<DT, S16, B16, 2, false><<<grid, threads, 0, st>>>(B, A, P);
-    }
+    for (long long s : strides)
+        if (s > (1 << 20)) return true;  // 256 rows of fp32 within 2^30 bytes
+    return false;
 }
 
-template <int DT, bool S16, bool B16>
-void launch_bwd(const capscaps_block& B, const capscaps_block_bwd_args& A, const RowPlan& P, float* partial,
-                hipStream_t st)
+// calls `launch` with the kernel's compile-time properties: stream and branch of 16 bits, a gate for every value, one vector a lane, a
+// partial vector
+template <int DT, typename F>
+void with_properties(const capscaps_block& B, bool branch, const RowPlan& P, F launch)
 {
-    const dim3 grid(P.blocks), threads(P.threads);
-    if (P.vectors == 1) {
-        if (P.tail)
-            block_bwd_kernel<DT, S16, B16, 1, true><<<grid, threads, 0, st>>>(B, A, P, partial);
+    auto yes = std::true_type();
+    auto no = std::false_type();
+    auto by_vectors = [&](auto s, auto b, auto g) {
+        if (P.vectors == 1)
+            P.tail ? launch(s, b, g, yes, yes) : launch(s, b, g, yes, no);
         else
-            block_bwd_kernel<DT, S16, B16, 1, false><<<grid, threads, 0, st>>>(B, A, P, partial);
-    } else {
-        if (P.tail)
-            block_bwd_kernel<DT, S16, B16, 2, true><<<grid, threads, 0, st>>>(B, A, P, partial);
-        else
-            block_bwd_kernel<DT, S16, B16, 2, false><<<grid, threads, 0, st>>>(B, A, P, partial);
-    }
-}
-
-template <int DT>
-void launch_bwd(const capscaps_block& B, const capscaps_block_bwd_args& A, const RowPlan& P, float* partial,
-                hipStream_t st)
-{
+            P.tail ? launch(s, b, g, no, yes) : launch(s, b, g, no, no);
+    };
+    auto by_gate = [&](auto s, auto b) {
+        B.gate == CAPSCAPS_GATE_FULL ? by_vectors(s, b, yes) : by_vectors(s, b, no);
+    };
     if constexpr (DT == CAPSCAPS_FP32) {
-        launch_bwd<DT, false, false>(B, A, P, partial, st);
+        by_gate(no, no);
     } else {
-        const bool s16 = B.stream_dtype == DT, b16 = B.branch_dtype == DT || A.branch == nullptr;
+        const bool s16 = B.stream_dtype == DT, b16 = B.branch_dtype == DT || !branch;
         if (s16)
-            b16 ? launch_bwd<DT, true, true>(B, A, P, partial, st) : launch_bwd<DT, true, false>(B, A, P, partial, st);
+            b16 ? by_gate(yes, yes) : by_gate(yes, no);
         else
-            b16 ? launch_bwd<DT, false, true>(B, A, P, partial, st)
-                : launch_bwd<DT, false, false>(B, A, P, partial, st);
+            b16 ? by_gate(no, yes) : by_gate(no, no);
     }
 }
 
 template <int DT>
 void launch_fwd(const capscaps_block& B, const capscaps_block_fwd_args& A, const RowPlan& P, hipStream_t st)
 {
-    if constexpr (DT == CAPSCAPS_FP32) {
-        launch_fwd<DT, false, false>(B, A, P, st);
-    } else {
-        const bool s16 = B.stream_dtype == DT, b16 = B.branch_dtype == DT || A.branch == nullptr;
-        if (s16)
-            b16 ? launch_fwd<DT, true, true>(B, A, P, st) : launch_fwd<DT, true, false>(B, A, P, st);
-        else
-            b16 ? launch_fwd<DT, false, true>(B, A, P, st) : launch_fwd<DT, false, false>(B, A, P, st);
-    }
+    with_properties<DT>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto one, auto tail) {
+        block_fwd_kernel<DT, s.value, b.value, g.value, one.value ? 1 : 2, tail.value>
+            <<<dim3(P.blocks), dim3(P.threads), 0, st>>>(B, A, P);
+    });
+}
+template <int DT>
+void launch_bwd(const capscaps_block& B, const capscaps_block_bwd_args& A, const RowPlan& P, float* partial,
+                hipStream_t st)
+{
+    with_properties<DT>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto one, auto tail) {
+        block_bwd_kernel<DT, s.value, b.value, g.value, one.value ? 1 : 2, tail.value>
+            <<<dim3(P.blocks), dim3(P.threads), 0, st>>>(B, A, P, partial);
+    });
 }
 
 unsigned row_blocks(const capscaps_block& B) { return (unsigned)(B.rows < (1 << 20) ? B.rows : (1 << 20)); }
@@ -709,14 +714,16 @@ int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fw
         if (misaligned(p, CAPSCAPS_FP32)) return CAPSCAPS_EINVAL;
     if (A.y == A.x && A.y_stride != A.x_stride) return CAPSCAPS_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool apart = rows_apart({A.x_stride, A.branch_stride, A.gate_stride, A.y_stride, A.h_stride});
+    const RowPlan P = row_plan(B, FWD_THREADS, apart);
     if (B.width > WIDEST)
         block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A);
     else if (B.dtype == CAPSCAPS_FP32)
-        launch_fwd<CAPSCAPS_FP32>(B, A, row_plan(B, FWD_THREADS), st);
+        launch_fwd<CAPSCAPS_FP32>(B, A, P, st);
     else if (B.dtype == CAPSCAPS_BF16)
-        launch_fwd<CAPSCAPS_BF16>(B, A, row_plan(B, FWD_THREADS), st);
+        launch_fwd<CAPSCAPS_BF16>(B, A, P, st);
     else
-        launch_fwd<CAPSCAPS_FP16>(B, A, row_plan(B, FWD_THREADS), st);
+        launch_fwd<CAPSCAPS_FP16>(B, A, P, st);
     return status_from_hip(hipGetLastError());
 }
 
@@ -724,8 +731,13 @@ size_t capscaps_block_norm_bwd_workspace_bytes(const capscaps_block* block)
 {
     if (check_block(block) != CAPSCAPS_OK) return 0;
     if (block->width <= WIDEST) {
-        const RowPlan P = row_plan(*block, BWD_THREADS);
-        return (size_t)P.blocks * 2 * P.vectors * P.group * VEC * 4;
+        size_t most = 0;
+        for (const bool apart : {false, true}) {
+            const RowPlan P = row_plan(*block, BWD_THREADS, apart);
+            const size_t bytes = (size_t)P.blocks * 2 * P.vectors * P.group * VEC * 4;
+            most = bytes > most ? bytes : most;
+        }
+        return most;
     }
     const size_t means = (size_t)block->rows * 4, sums = (size_t)row_shares(block->rows) * 3 * block->width * 4;
     return (means + 255) / 256 * 256 + sums;
@@ -770,7 +782,9 @@ int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bw
     }
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (B.width <= WIDEST) {
-        const RowPlan P = row_plan(B, BWD_THREADS);
+        const bool apart = rows_apart({A.y_stride, A.branch_stride, A.gate_stride, A.dh_stride, A.dy_stride, A.dx_stride,
+                                       A.dbranch_stride, A.dgate_stride});
+        const RowPlan P = row_plan(B, BWD_THREADS, apart);
         float* partial = sums ? static_cast<float*>(workspace) : nullptr;
         if (B.dtype == CAPSCAPS_FP32)
             launch_bwd<CAPSCAPS_FP32>(B, A, P, partial, st);
