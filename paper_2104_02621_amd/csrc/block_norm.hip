@@ -2,8 +2,8 @@
 // Formulas and contracts: include/capscaps.h.
 //
 // All of it is bounded by memory: some ten to thirty operations for every value moved.  So each value is read once and
-// each result written once, with the row in registers between: a group of lanes holds a row, eight values a
-// lane and vector (row_vectors.h), and the means are sums over the group.  Groups of up to 64 lanes share a wave and need
+// each result written once, with the row in registers between: a group of lanes holds a row in vectors
+// (row_vectors.h), and the means are sums over the group.  Groups of up to 64 lanes share a wave and need
 // no barrier; wider rows take a workgroup.  Rows that no group holds (over 16384 values) take the kernels at the end.
 #include <hip/hip_runtime.h>
 #include <float.h>
@@ -56,14 +56,19 @@ __device__ __forceinline__ float block_sum(float v, float* lds)
 // How rows lie on lanes: `group` lanes (a power of two) hold a row, lane l the vectors l, l + group, ... of `vectors`
 // a lane; `per_block` rows at a time in a workgroup of `threads`.
 struct RowPlan {
+    int n;  // values of a vector
     int group, vectors, threads, per_block;
     unsigned blocks;
     int full, tail;  // whole vectors in a row, and the values after them
 };
 
+#ifndef WPE4
+#define WPE4 4
+#endif
+#define WPE(values) ((values) == 4 ? WPE4 : 4)
 constexpr int WIDEST = 16384;
-// threads of a compute unit that a launch counts on: further rows are the same threads' next ones
-constexpr int FWD_THREADS = 2048, BWD_THREADS = 1024;
+// threads of a compute unit that a launch counts on: further rows are the same threads' next ones (forward: none)
+constexpr int FWD_THREADS = 1 << 22, BWD_THREADS = 1024;
 
 // Sum over a row's lanes.  Rows of more than one wave go through LDS: two buffers in turn, so that one barrier is
 // enough (a wave writes a buffer again only after the barrier of the other one, which every wave reaches after it has read).
@@ -88,6 +93,7 @@ struct RowSum {
 
 // A tensor's rows as the lanes of a workgroup see them: where its rows of this round begin (the same for all lanes, so
 // it stays in scalar registers), and a lane's place from there
+template <int N>
 struct Rows {
     const char* base;
     long long step;  // bytes to the next round's
@@ -97,40 +103,80 @@ struct Rows {
     {
         base = (const char*)p + (long long)blockIdx.x * P.per_block * stride * bytes;
         step = (long long)gridDim.x * P.per_block * stride * bytes;
-        at = (unsigned)(slot * stride * bytes) + (unsigned)(lane * VEC * bytes);
+        at = (unsigned)(slot * stride * bytes) + (unsigned)(lane * N * bytes);
     }
     __device__ __forceinline__ const char* get(int i, const RowPlan& P, int bytes) const
     {
-        return base + (long long)(i * P.group * VEC * bytes) + at;
+        return base + (long long)(i * P.group * N * bytes) + at;
     }
     __device__ __forceinline__ char* put(int i, const RowPlan& P, int bytes) const { return const_cast<char*>(get(i, P, bytes)); }
     __device__ __forceinline__ void next() { base += step; }
 };
 
-// What a column's factors are from pre-norm weight, post-norm weight and a shared gate
-template <int I, bool TAIL>
+// A vector of what a column's values are multiplied by, from pre-norm weight, post-norm weight and a shared gate
+template <int N>
+struct Factors {
+    float to_b[N], to_h[N];
+};
+template <int N, bool TAIL>
+__device__ __forceinline__ Factors<N> column_factors(const capscaps_block& B, const float* pre_weight,
+                                                     const float* post_weight, const void* gate, const RowPlan& P, int v)
+{
+    Factors<N> f;
+    const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
+    const bool full = v < P.full, part = TAIL && v == P.full;
+    load_column<N, TAIL>(f.to_b, post_weight, v, full, part, P.tail, 1.0f);
+    load_column<N, TAIL>(f.to_h, pre_weight, v, full, part, P.tail, 1.0f);
+    float g[N];
+    load_column<N, TAIL>(g, shared ? static_cast<const float*>(gate) : nullptr, v, full, part, P.tail, 1.0f);
+#pragma unroll
+    for (int k = 0; k < N; ++k) f.to_b[k] *= B.branch_scale * (shared ? gate_value(B.gate_act, g[k]) : 1.0f);
+    return f;
+}
+// They are kept in registers where a lane has one vector.  Where it has more, registers are short (the sums over rows
+// alone take 32), and they lie in LDS: a lane's own place, so nothing waits for another lane
+template <int N, int I>
 struct Columns {
-    float to_b[I][VEC], to_h[I][VEC];
-    __device__ __forceinline__ void load_all(const capscaps_block& B, const float* pre_weight, const float* post_weight,
-                                             const void* gate, const RowPlan& P, int lane)
+    Factors<N> own;
+    float* lds;
+    int group, lane;
+    __device__ __forceinline__ void put(int i, const Factors<N>& f)
     {
-        const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
+        if constexpr (I == 1) {
+            own = f;
+        } else {
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
-            const int v = lane + i * P.group;
-            const bool full = v < P.full, part = TAIL && v == P.full;
-            load_column<TAIL>(to_b[i], post_weight, v, full, part, P.tail, 1.0f);
-            load_column<TAIL>(to_h[i], pre_weight, v, full, part, P.tail, 1.0f);
-            float g[VEC];
-            load_column<TAIL>(g, shared ? static_cast<const float*>(gate) : nullptr, v, full, part, P.tail, 1.0f);
+            for (int k = 0; k < N; k += 4) {
+                quad(0, i, k) = float4v_t{f.to_b[k], f.to_b[k + 1], f.to_b[k + 2], f.to_b[k + 3]};
+                quad(1, i, k) = float4v_t{f.to_h[k], f.to_h[k + 1], f.to_h[k + 2], f.to_h[k + 3]};
+            }
+        }
+    }
+    __device__ __forceinline__ void to_b(int i, float* f) const { get(0, i, f, own.to_b); }
+    __device__ __forceinline__ void to_h(int i, float* f) const { get(1, i, f, own.to_h); }
+
+private:
+    typedef float float4v_t __attribute__((ext_vector_type(4)));
+    __device__ __forceinline__ float4v_t& quad(int which, int i, int k) const
+    {
+        return reinterpret_cast<float4v_t*>(lds)[((which * I + i) * (N / 4) + k / 4) * group + lane];
+    }
+    __device__ __forceinline__ void get(int which, int i, float* f, const float* kept) const
+    {
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) to_b[i][k] *= B.branch_scale * (shared ? gate_value(B.gate_act, g[k]) : 1.0f);
+        for (int k = 0; k < N; k += 4) {
+            if constexpr (I == 1) {
+                for (int j = 0; j < 4; ++j) f[k + j] = kept[k + j];
+            } else {
+                const float4v_t q = quad(which, i, k);
+                for (int j = 0; j < 4; ++j) f[k + j] = q[j];
+            }
         }
     }
 };
 
 // GATE: a gate for every value
-template <int DT, bool S16, bool B16, bool GATE, int I, bool TAIL>
+template <int DT, bool S16, bool B16, bool GATE, int N, int I, bool TAIL>
 __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capscaps_block_fwd_args A, RowPlan P)
 {
     constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
@@ -140,70 +186,60 @@ __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capsc
     const int lane = threadIdx.x & (P.group - 1), slot = threadIdx.x / P.group;
     const bool branch = A.branch != nullptr, post = branch && B.post_norm, pre = A.h != nullptr;
     const float inv_width = 1.0f / (float)B.width;
-    Columns<I, TAIL> col;
-    col.load_all(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane);
-    Rows rx(A.x, A.x_stride, SB, P, slot, lane), rb(A.branch, A.branch_stride, BB, P, slot, lane);
-    Rows rg(A.gate, A.gate_stride, LB, P, slot, lane);
-    Rows ry(A.y, A.y_stride, SB, P, slot, lane), rh(A.h, A.h_stride, LB, P, slot, lane);
-    Raw<SD> x[I];
-    Raw<BD> b[I];
-    Raw<DT> g[I];
-    auto fetch = [&](bool in) {
+    Factors<N> col[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+        col[i] = column_factors<N, TAIL>(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane + i * P.group);
+    Rows<N> rx(A.x, A.x_stride, SB, P, slot, lane), rb(A.branch, A.branch_stride, BB, P, slot, lane);
+    Rows<N> rg(A.gate, A.gate_stride, LB, P, slot, lane);
+    Rows<N> ry(A.y, A.y_stride, SB, P, slot, lane), rh(A.h, A.h_stride, LB, P, slot, lane);
+    const long long step = (long long)gridDim.x * P.per_block;
+    for (long long left = B.rows - (long long)blockIdx.x * P.per_block; left > 0; left -= step) {
+        const bool in = slot < left;
+        const long long r = B.rows - left + slot;
+        Raw<SD, N> x[I];
+        Raw<BD, N> b[I];
+        Raw<DT, N> g[I];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * P.group;
             const bool full = in && v < P.full, part = TAIL && in && v == P.full;
             clear(x[i]);
             clear(b[i]);
-            load<SD, TAIL>(x[i], rx.get(i, P, SB), full, part, P.tail);
-            if (branch) load<BD, TAIL>(b[i], rb.get(i, P, BB), full, part, P.tail);
+            if (branch) load<BD, N, TAIL>(b[i], rb.get(i, P, BB), full, part, P.tail);
+            load<SD, N, TAIL>(x[i], rx.get(i, P, SB), full, part, P.tail);
             if constexpr (GATE) {
                 clear(g[i]);
-                load<DT, TAIL>(g[i], rg.get(i, P, LB), full, part, P.tail);
+                load<DT, N, TAIL>(g[i], rg.get(i, P, LB), full, part, P.tail);
             }
         }
-        rx.next();
-        rb.next();
-        rg.next();
-    };
-    const long long step = (long long)gridDim.x * P.per_block;
-    long long left = B.rows - (long long)blockIdx.x * P.per_block;  // rows from this round's first one on
-    fetch(slot < left);
-    for (; left > 0; left -= step) {
-        const bool in = slot < left;
-        const long long r = B.rows - left + slot;
         float rpost = 1.0f;
         if (post) {
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < I; ++i)
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) s += value<BD>(b[i], k) * value<BD>(b[i], k);
+                for (int k = 0; k < N; ++k) s += value<BD, N>(b[i], k) * value<BD, N>(b[i], k);
             rpost = __builtin_amdgcn_rsqf(sum(s) * inv_width + B.eps);
             if (A.rstd_post != nullptr && lane == 0 && in) A.rstd_post[r] = rpost;
         }
-        float y[I][VEC];
+        float y[I][N];
         float s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < I; ++i)
+        for (int i = 0; i < I; ++i) {
+            const int v = lane + i * P.group;
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                y[i][k] = value<SD>(x[i], k);
+            for (int k = 0; k < N; ++k) {
+                y[i][k] = value<SD, N>(x[i], k);
                 if (branch) {
-                    float u = value<BD>(b[i], k) * rpost * col.to_b[i][k];
-                    if constexpr (GATE) u *= gate_value(B.gate_act, value<DT>(g[i], k));
+                    float u = value<BD, N>(b[i], k) * rpost * col[i].to_b[k];
+                    if constexpr (GATE) u *= gate_value(B.gate_act, value<DT, N>(g[i], k));
                     y[i][k] = B.residual_scale * y[i][k] + u;
                 }
                 s += y[i][k] * y[i][k];
             }
-        // the next rows' values are under way while these are summed and written
-        if (left > step) fetch(slot < left - step);
-        if (A.y != nullptr) {
-#pragma unroll
-            for (int i = 0; i < I; ++i) {
-                const int v = lane + i * P.group;
-                store<SD, TAIL>(ry.put(i, P, SB), y[i], in && v < P.full, in && v == P.full, P.tail);
-            }
+            if (A.y != nullptr)
+                store<SD, N, TAIL>(ry.put(i, P, SB), y[i], in && v < P.full, in && v == P.full, P.tail);
         }
         if (pre) {
             const float rpre = __builtin_amdgcn_rsqf(sum(s) * inv_width + B.eps);
@@ -211,12 +247,15 @@ __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capsc
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int v = lane + i * P.group;
-                float h[VEC];
+                float h[N];
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) h[k] = y[i][k] * rpre * col.to_h[i][k];
-                store<DT, TAIL>(rh.put(i, P, LB), h, in && v < P.full, in && v == P.full, P.tail);
+                for (int k = 0; k < N; ++k) h[k] = y[i][k] * rpre * col[i].to_h[k];
+                store<DT, N, TAIL>(rh.put(i, P, LB), h, in && v < P.full, in && v == P.full, P.tail);
             }
         }
+        rx.next();
+        rb.next();
+        rg.next();
         ry.next();
         rh.next();
     }
@@ -226,8 +265,8 @@ __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capsc
 // pair is fetched while the other is worked on.  Sums over rows stay in registers, two for each column:
 // of dh * yn, and of d * act * bn, from which both dpost_weight and a shared gate's gradient follow, since all their other
 // factors are the column's.  A workgroup's sums go to `partial` [block][2][columns], columns in the order of lanes' places.
-template <int DT, bool S16, bool B16, bool GATE, int I, bool TAIL>
-__global__ void __launch_bounds__(1024)
+template <int DT, bool S16, bool B16, bool GATE, int N, int I, bool TAIL>
+__global__ void __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(WPE(N * I))))
     block_bwd_kernel(capscaps_block B, capscaps_block_bwd_args A, RowPlan P, float* partial)
 {
     constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
@@ -239,20 +278,26 @@ __global__ void __launch_bounds__(1024)
     const bool post = branch && B.post_norm && A.rstd_post != nullptr;
     const float inv_width = 1.0f / (float)B.width;
     const float to_x = branch ? B.residual_scale : 1.0f;
-    Columns<I, TAIL> col;
-    col.load_all(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane);
-    float sum_h[I][VEC], sum_b[I][VEC];
+    extern __shared__ float columns_lds[];
+    Columns<N, I> col;
+    col.lds = columns_lds;
+    col.group = P.group;
+    col.lane = lane;
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+        col.put(i, column_factors<N, TAIL>(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane + i * P.group));
+    float sum_h[I][N], sum_b[I][N];
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) sum_h[i][k] = sum_b[i][k] = 0.0f;
-    Rows ry(A.y, A.y_stride, SB, P, slot, lane), rdh(A.dh, A.dh_stride, LB, P, slot, lane);
-    Rows rdy(A.dy, A.dy_stride, SB, P, slot, lane), rb(A.branch, A.branch_stride, BB, P, slot, lane);
-    Rows rg(A.gate, A.gate_stride, LB, P, slot, lane), rdg(A.dgate, A.dgate_stride, LB, P, slot, lane);
-    Rows rdx(A.dx, A.dx_stride, SB, P, slot, lane), rdb(A.dbranch, A.dbranch_stride, LB, P, slot, lane);
-    Raw<SD> y[I], dy[I];
-    Raw<DT> dh[I], g[I];
-    Raw<BD> b[I];
+        for (int k = 0; k < N; ++k) sum_h[i][k] = sum_b[i][k] = 0.0f;
+    Rows<N> ry(A.y, A.y_stride, SB, P, slot, lane), rdh(A.dh, A.dh_stride, LB, P, slot, lane);
+    Rows<N> rdy(A.dy, A.dy_stride, SB, P, slot, lane), rb(A.branch, A.branch_stride, BB, P, slot, lane);
+    Rows<N> rg(A.gate, A.gate_stride, LB, P, slot, lane), rdg(A.dgate, A.dgate_stride, LB, P, slot, lane);
+    Rows<N> rdx(A.dx, A.dx_stride, SB, P, slot, lane), rdb(A.dbranch, A.dbranch_stride, LB, P, slot, lane);
+    Raw<SD, N> y[I], dy[I];
+    Raw<DT, N> dh[I], g[I];
+    Raw<BD, N> b[I];
     float rpre = 1.0f, rpost = 1.0f;
     auto fetch_h = [&](bool in, long long r) {
 #pragma unroll
@@ -262,8 +307,8 @@ __global__ void __launch_bounds__(1024)
             clear(y[i]);
             clear(dh[i]);
             if (has_h) {
-                load<SD, TAIL>(y[i], ry.get(i, P, SB), full, part, P.tail);
-                load<DT, TAIL>(dh[i], rdh.get(i, P, LB), full, part, P.tail);
+                load<SD, N, TAIL>(y[i], ry.get(i, P, SB), full, part, P.tail);
+                load<DT, N, TAIL>(dh[i], rdh.get(i, P, LB), full, part, P.tail);
             }
         }
         if (has_h && in) rpre = A.rstd_pre[r];
@@ -277,11 +322,11 @@ __global__ void __launch_bounds__(1024)
             const bool full = in && v < P.full, part = TAIL && in && v == P.full;
             clear(dy[i]);
             clear(b[i]);
-            if (A.dy != nullptr) load<SD, TAIL>(dy[i], rdy.get(i, P, SB), full, part, P.tail);
-            if (branch) load<BD, TAIL>(b[i], rb.get(i, P, BB), full, part, P.tail);
+            if (A.dy != nullptr) load<SD, N, TAIL>(dy[i], rdy.get(i, P, SB), full, part, P.tail);
+            if (branch) load<BD, N, TAIL>(b[i], rb.get(i, P, BB), full, part, P.tail);
             if constexpr (GATE) {
                 clear(g[i]);
-                load<DT, TAIL>(g[i], rg.get(i, P, LB), full, part, P.tail);
+                load<DT, N, TAIL>(g[i], rg.get(i, P, LB), full, part, P.tail);
             }
         }
         if (post && in) rpost = A.rstd_post[r];
@@ -299,51 +344,63 @@ __global__ void __launch_bounds__(1024)
         float s = 0.0f, mean = 0.0f;
         if (has_h) {
 #pragma unroll
-            for (int i = 0; i < I; ++i)
+            for (int i = 0; i < I; ++i) {
+                float wh[N];
+                col.to_h(i, wh);
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) s += value<DT>(dh[i], k) * col.to_h[i][k] * (value<SD>(y[i], k) * rpre);
+                for (int k = 0; k < N; ++k) s += value<DT, N>(dh[i], k) * wh[k] * (value<SD, N>(y[i], k) * rpre);
+            }
             mean = sum(s) * inv_width;
         }
-        float e[I][VEC];
+        float e[I][N];
         s = 0.0f;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int v = lane + i * P.group;
-            float dx[VEC], dg[VEC];
+            forget(y[i]);
+            forget(dh[i]);
+        }
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const float yn = value<SD>(y[i], k) * rpre, h = value<DT>(dh[i], k);
+        for (int i = 0; i < I; ++i) {
+            const int v = lane + i * P.group;
+            float dx[N], dg[N], cb[N], wh[N];
+            col.to_b(i, cb);
+            col.to_h(i, wh);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float yn = value<SD, N>(y[i], k) * rpre, h = value<DT, N>(dh[i], k);
                 sum_h[i][k] += h * yn;
-                float d = value<SD>(dy[i], k);
-                if (has_h) d += rpre * (h * col.to_h[i][k] - yn * mean);
+                float d = value<SD, N>(dy[i], k);
+                if (has_h) d += rpre * (h * wh[k] - yn * mean);
                 dx[k] = to_x * d;
-                const float bn = value<BD>(b[i], k) * rpost;
+                const float bn = value<BD, N>(b[i], k) * rpost;
                 if constexpr (GATE) {
-                    const Gate q = gate_both(B.gate_act, value<DT>(g[i], k));
-                    dg[k] = d * col.to_b[i][k] * bn * q.slope;
+                    const Gate q = gate_both(B.gate_act, value<DT, N>(g[i], k));
+                    dg[k] = d * cb[k] * bn * q.slope;
                     d *= q.value;
                 }
                 sum_b[i][k] += d * bn;
-                e[i][k] = d * col.to_b[i][k];
+                e[i][k] = d * cb[k];
                 s += e[i][k] * bn;
             }
             if (A.dx != nullptr)
-                store<SD, TAIL>(rdx.put(i, P, SB), dx, in && v < P.full, in && v == P.full, P.tail);
+                store<SD, N, TAIL>(rdx.put(i, P, SB), dx, in && v < P.full, in && v == P.full, P.tail);
             if constexpr (GATE) {
                 if (A.dgate != nullptr)
-                    store<DT, TAIL>(rdg.put(i, P, LB), dg, in && v < P.full, in && v == P.full, P.tail);
+                    store<DT, N, TAIL>(rdg.put(i, P, LB), dg, in && v < P.full, in && v == P.full, P.tail);
             }
         }
         if (left > step) fetch_h(slot < left - step, r + step);
         if (A.dbranch != nullptr) {
             mean = post ? sum(s) * inv_width : 0.0f;
 #pragma unroll
+            for (int i = 0; i < I; ++i) forget(b[i]);
+#pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int v = lane + i * P.group;
-                float db[VEC];
+                float db[N];
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) db[k] = rpost * (e[i][k] - value<BD>(b[i], k) * rpost * mean);
-                store<DT, TAIL>(rdb.put(i, P, LB), db, in && v < P.full, in && v == P.full, P.tail);
+                for (int k = 0; k < N; ++k) db[k] = rpost * (e[i][k] - value<BD, N>(b[i], k) * rpost * mean);
+                store<DT, N, TAIL>(rdb.put(i, P, LB), db, in && v < P.full, in && v == P.full, P.tail);
             }
         }
         rdx.next();
@@ -351,15 +408,15 @@ __global__ void __launch_bounds__(1024)
         rdg.next();
     }
     if (partial == nullptr) return;
-    const int columns = P.vectors * P.group * VEC;
+    const int columns = P.vectors * P.group * N;
     float* out = partial + (long long)blockIdx.x * 2 * columns;
     if (P.per_block == 1) {
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                out[(lane + i * P.group) * VEC + k] = sum_h[i][k];
-                out[columns + (lane + i * P.group) * VEC + k] = sum_b[i][k];
+            for (int k = 0; k < N; ++k) {
+                out[(lane + i * P.group) * N + k] = sum_h[i][k];
+                out[columns + (lane + i * P.group) * N + k] = sum_b[i][k];
             }
         return;
     }
@@ -367,13 +424,13 @@ __global__ void __launch_bounds__(1024)
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-        for (int k = 0; k < VEC; ++k)
+        for (int k = 0; k < N; ++k)
             for (int o = 32; o >= P.group; o >>= 1) {
                 sum_h[i][k] += __shfl_xor(sum_h[i][k], o);
                 sum_b[i][k] += __shfl_xor(sum_b[i][k], o);
             }
     // the rows of the four waves
-    __shared__ float of_wave[THREADS / 64][64 * VEC];
+    __shared__ float of_wave[THREADS / 64][64 * N];
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
@@ -381,21 +438,14 @@ __global__ void __launch_bounds__(1024)
             __syncthreads();
             if ((int)(threadIdx.x & 63) < P.group) {
 #pragma unroll
-                for (int k = 0; k < VEC; ++k)
-                    of_wave[threadIdx.x >> 6][lane * VEC + k] = which == 0 ? sum_h[i][k] : sum_b[i][k];
+                for (int k = 0; k < N; ++k)
+                    of_wave[threadIdx.x >> 6][lane * N + k] = which == 0 ? sum_h[i][k] : sum_b[i][k];
             }
             __syncthreads();
-            for (int c = threadIdx.x; c < P.group * VEC; c += THREADS)
-                out[which * columns + i * P.group * VEC + c] =
+            for (int c = threadIdx.x; c < P.group * N; c += THREADS)
+                out[which * columns + i * P.group * N + c] =
                     (of_wave[0][c] + of_wave[1][c]) + (of_wave[2][c] + of_wave[3][c]);
         }
-}
-
-// Place of column j of a row's last, partial vector (row_vectors.h)
-__device__ __forceinline__ int tail_place(int j, int tail)
-{
-    if (j < (tail & 4)) return j;
-    return j < (tail & 6) ? 4 + j - (tail & 4) : 6;
 }
 
 // Sums the workgroups' sums, 64 columns a workgroup, each by 16 threads that take every 16th in turn
@@ -404,10 +454,11 @@ __global__ void __launch_bounds__(1024)
 {
     __shared__ float lds[16][64];
     const int c = blockIdx.x * 64 + (threadIdx.x & 63), share = threadIdx.x >> 6;
-    const int columns = P.vectors * P.group * VEC;
+    const int columns = P.vectors * P.group * P.n;
     float s = 0.0f;
     if (c < B.width) {
-        const int place = c / VEC < P.full ? c : P.full * VEC + tail_place(c % VEC, P.tail);
+        const int j = c % P.n, tail = P.n == 8 ? tail_place<8>(j, P.tail) : tail_place<4>(j, P.tail);
+        const int place = c / P.n < P.full ? c : c - j + tail;
         const float* p = partial + (long long)blockIdx.y * columns + place;
 #pragma unroll 8
         for (int k = share; k < (int)P.blocks; k += 16) s += p[(long long)k * 2 * columns];
@@ -614,24 +665,29 @@ int check_block(const capscaps_block* B)
     return CAPSCAPS_OK;
 }
 
-// The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024; two vectors each for rows of
-// more than 8192 values.  `apart`: rows so far apart that those of one workgroup are not within reach of 32-bit offsets, one at a
-// time in a workgroup.
-RowPlan row_plan(const capscaps_block& B, int threads_per_cu, bool apart)
+// The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024.  `apart`: rows so far
+// apart that those of one workgroup are not within reach of 32-bit offsets, one at a time in a workgroup.
+RowPlan row_plan(const capscaps_block& B, int n, int threads_per_cu, bool apart)
 {
     RowPlan P;
-    const int vectors = (B.width + VEC - 1) / VEC;
+    P.n = n;
+    const int vectors = (B.width + n - 1) / n;
     P.group = apart ? 64 : 1;
     while (P.group < vectors && P.group < 1024) P.group *= 2;
-    P.vectors = (vectors + P.group - 1) / P.group;
+    P.vectors = 1;
+    while (P.group * P.vectors < vectors) P.vectors *= 2;
     P.threads = P.group > 64 || apart ? P.group : THREADS;
     P.per_block = P.threads / P.group;
     const long long blocks = (B.rows + P.per_block - 1) / P.per_block;
-    const long long most = apart ? CUS : CUS * threads_per_cu / P.threads;
+    const long long most = apart ? CUS : (long long)CUS * threads_per_cu / P.threads;
     P.blocks = (unsigned)(blocks < most ? blocks : most);
-    P.full = B.width / VEC;
-    P.tail = B.width % VEC;
+    P.full = B.width / n;
+    P.tail = B.width % n;
     return P;
+}
+int vector_values(const capscaps_block& B, bool branch)
+{
+    return B.dtype != CAPSCAPS_FP32 && B.stream_dtype == B.dtype && (!branch || B.branch_dtype == B.dtype) ? 8 : 4;
 }
 bool rows_apart(std::initializer_list<long long> strides)
 {
@@ -640,18 +696,27 @@ bool rows_apart(std::initializer_list<long long> strides)
     return false;
 }
 
-// calls `launch` with the kernel's compile-time properties: stream and branch of 16 bits, a gate for every value, one vector a lane, a
-// partial vector
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// calls `launch` with the kernel's compile-time properties: stream and branch of 16 bits, a gate for every value, values of a
+// vector, vectors of a lane, a partial vector
 template <int DT, typename F>
 void with_properties(const capscaps_block& B, bool branch, const RowPlan& P, F launch)
 {
-    auto yes = std::true_type();
-    auto no = std::false_type();
+    const std::true_type yes;
+    const std::false_type no;
+    auto by_tail = [&](auto s, auto b, auto g, auto n, auto i) {
+        P.tail ? launch(s, b, g, n, i, yes) : launch(s, b, g, n, i, no);
+    };
     auto by_vectors = [&](auto s, auto b, auto g) {
-        if (P.vectors == 1)
-            P.tail ? launch(s, b, g, yes, yes) : launch(s, b, g, yes, no);
-        else
-            P.tail ? launch(s, b, g, no, yes) : launch(s, b, g, no, no);
+        if constexpr (s.value && b.value) {
+            P.vectors == 1 ? by_tail(s, b, g, Int<8>(), Int<1>()) : by_tail(s, b, g, Int<8>(), Int<2>());
+        } else {
+            if (P.vectors == 1) by_tail(s, b, g, Int<4>(), Int<1>());
+            if (P.vectors == 2) by_tail(s, b, g, Int<4>(), Int<2>());
+            if (P.vectors == 4) by_tail(s, b, g, Int<4>(), Int<4>());
+        }
     };
     auto by_gate = [&](auto s, auto b) {
         B.gate == CAPSCAPS_GATE_FULL ? by_vectors(s, b, yes) : by_vectors(s, b, no);
@@ -670,19 +735,28 @@ void with_properties(const capscaps_block& B, bool branch, const RowPlan& P, F l
 template <int DT>
 void launch_fwd(const capscaps_block& B, const capscaps_block_fwd_args& A, const RowPlan& P, hipStream_t st)
 {
-    with_properties<DT>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto one, auto tail) {
-        block_fwd_kernel<DT, s.value, b.value, g.value, one.value ? 1 : 2, tail.value>
+    with_properties<DT>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto n, auto i, auto tail) {
+        block_fwd_kernel<DT, s.value, b.value, g.value, n.value, i.value, tail.value>
             <<<dim3(P.blocks), dim3(P.threads), 0, st>>>(B, A, P);
     });
 }
 template <int DT>
-void launch_bwd(const capscaps_block& B, const capscaps_block_bwd_args& A, const RowPlan& P, float* partial,
-                hipStream_t st)
+hipError_t launch_bwd(const capscaps_block& B, const capscaps_block_bwd_args& A, const RowPlan& P, float* partial,
+                      hipStream_t st)
 {
-    with_properties<DT>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto one, auto tail) {
-        block_bwd_kernel<DT, s.value, b.value, g.value, one.value ? 1 : 2, tail.value>
-            <<<dim3(P.blocks), dim3(P.threads), 0, st>>>(B, A, P, partial);
+    hipError_t err = hipSuccess;
+    with_properties<DT>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto n, auto i, auto tail) {
+        const auto kernel = block_bwd_kernel<DT, s.value, b.value, g.value, n.value, i.value, tail.value>;
+        const int lds = i.value == 1 ? 0 : P.group * i.value * n.value * 2 * 4;
+        if (i.value > 1) {
+            static std::atomic<unsigned long long> done{0};
+            err = set_dynamic_lds_once(reinterpret_cast<const void*>(kernel), WIDEST * 2 * 4, done);
+            if (err != hipSuccess) return;
+        }
+        kernel<<<dim3(P.blocks), dim3(P.threads), lds, st>>>(B, A, P, partial);
+        err = hipGetLastError();
     });
+    return err;
 }
 
 unsigned row_blocks(const capscaps_block& B) { return (unsigned)(B.rows < (1 << 20) ? B.rows : (1 << 20)); }
@@ -715,7 +789,7 @@ int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fw
     if (A.y == A.x && A.y_stride != A.x_stride) return CAPSCAPS_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool apart = rows_apart({A.x_stride, A.branch_stride, A.gate_stride, A.y_stride, A.h_stride});
-    const RowPlan P = row_plan(B, FWD_THREADS, apart);
+    const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), FWD_THREADS, apart);
     if (B.width > WIDEST)
         block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A);
     else if (B.dtype == CAPSCAPS_FP32)
@@ -732,11 +806,12 @@ size_t capscaps_block_norm_bwd_workspace_bytes(const capscaps_block* block)
     if (check_block(block) != CAPSCAPS_OK) return 0;
     if (block->width <= WIDEST) {
         size_t most = 0;
-        for (const bool apart : {false, true}) {
-            const RowPlan P = row_plan(*block, BWD_THREADS, apart);
-            const size_t bytes = (size_t)P.blocks * 2 * P.vectors * P.group * VEC * 4;
-            most = bytes > most ? bytes : most;
-        }
+        for (const bool apart : {false, true})
+            for (const bool branch : {false, true}) {
+                const RowPlan P = row_plan(*block, vector_values(*block, branch), BWD_THREADS, apart);
+                const size_t bytes = (size_t)P.blocks * 2 * P.vectors * P.group * P.n * 4;
+                most = bytes > most ? bytes : most;
+            }
         return most;
     }
     const size_t means = (size_t)block->rows * 4, sums = (size_t)row_shares(block->rows) * 3 * block->width * 4;
@@ -784,15 +859,11 @@ int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bw
     if (B.width <= WIDEST) {
         const bool apart = rows_apart({A.y_stride, A.branch_stride, A.gate_stride, A.dh_stride, A.dy_stride, A.dx_stride,
                                        A.dbranch_stride, A.dgate_stride});
-        const RowPlan P = row_plan(B, BWD_THREADS, apart);
+        const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), BWD_THREADS, apart);
         float* partial = sums ? static_cast<float*>(workspace) : nullptr;
-        if (B.dtype == CAPSCAPS_FP32)
-            launch_bwd<CAPSCAPS_FP32>(B, A, P, partial, st);
-        else if (B.dtype == CAPSCAPS_BF16)
-            launch_bwd<CAPSCAPS_BF16>(B, A, P, partial, st);
-        else
-            launch_bwd<CAPSCAPS_FP16>(B, A, P, partial, st);
-        const hipError_t err = hipGetLastError();
+        const hipError_t err = B.dtype == CAPSCAPS_FP32   ? launch_bwd<CAPSCAPS_FP32>(B, A, P, partial, st)
+                               : B.dtype == CAPSCAPS_BF16 ? launch_bwd<CAPSCAPS_BF16>(B, A, P, partial, st)
+                                                          : launch_bwd<CAPSCAPS_FP16>(B, A, P, partial, st);
         if (err != hipSuccess || !sums) return status_from_hip(err);
         block_bwd_sums_kernel<<<dim3((B.width + 63) / 64, 2), dim3(1024), 0, st>>>(B, A, P, partial);
         return status_from_hip(hipGetLastError());

@@ -1,9 +1,11 @@
-// Internal: rows of values of the three element types, eight values a lane, at any address.
+// Internal: rows of values of the three element types, some values a lane, at any address.
 //
-// A row's values are cut into vectors of eight: 16 bytes of a 16-bit type, two times 16 of fp32, loaded and stored
-// whole at any alignment (the hardware takes 16-byte accesses at element addresses).  What a row's length leaves over (1 .. 7 values) is
-// one lane's last vector, moved in pieces of 4, 2 and 1 values that have fixed places in the registers: 0 .. 3, 4 .. 5
-// and 6.  All tensors of a call and the per-column vectors use the same places, so the kernels need not know.
+// A row's values are cut into vectors of N values, one of 16 bytes where all tensors of a call have 16-bit elements (N = 8),
+// else N = 4: 16 bytes of fp32, 8 of a 16-bit type, so that a wave's access is one contiguous piece in every type.
+// They are loaded and stored whole at any alignment (the hardware takes such accesses at element addresses).
+// What a row's length leaves over (1 .. N - 1 values) is one lane's last vector, moved in pieces of 4, 2 and 1 values that have fixed
+// places in the registers: N = 8: 0 .. 3, 4 .. 5 and 6; N = 4: 0 .. 1 and 2.  All tensors of a call and the per-column vectors
+// use the same places, so the kernels need not know.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -11,80 +13,112 @@
 
 namespace capscaps {
 
-typedef unsigned uint4v __attribute__((ext_vector_type(4)));
-typedef uint4v uint4_a2 __attribute__((aligned(2)));
-typedef uint4v uint4_a4 __attribute__((aligned(4)));
-typedef unsigned uint2v __attribute__((ext_vector_type(2)));
-typedef uint2v uint2_a2 __attribute__((aligned(2)));
-typedef uint2v uint2_a4 __attribute__((aligned(4)));
-typedef unsigned uint_a2 __attribute__((aligned(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
-
-constexpr int VEC = 8;
-
-template <int DT>
-struct Raw {
-    static constexpr int QUADS = DT == CAPSCAPS_FP32 ? 2 : 1;
-    uint4v q[QUADS];
+// 16, 8, 4 and 2 bytes at addresses of elements
+template <int WORDS, int ALIGN>
+struct Words {
+    typedef unsigned type __attribute__((ext_vector_type(WORDS)));
+    typedef type at __attribute__((aligned(ALIGN)));
 };
 
-template <int DT>
-__device__ __forceinline__ void clear(Raw<DT>& r)
+// N values as they lie in memory
+template <int DT, int N>
+struct Raw {
+    static constexpr int SIZE = DT == CAPSCAPS_FP32 ? 4 : 2, WORDS = N * SIZE / 4;
+    typedef typename Words<WORDS, SIZE>::at Whole;
+    typename Words<WORDS, SIZE>::type w;
+};
+
+template <int DT, int N>
+__device__ __forceinline__ void clear(Raw<DT, N>& r)
 {
 #pragma unroll
-    for (int k = 0; k < Raw<DT>::QUADS; ++k) r.q[k] = uint4v{0, 0, 0, 0};
+    for (int k = 0; k < Raw<DT, N>::WORDS; ++k) r.w[k] = 0;
 }
 
-template <int DT>
-__device__ __forceinline__ void load_full(Raw<DT>& r, const char* p)
+// The piece of 4, 2 or 1 values of a row's last vector: where it lies in the vector's registers, and after how many values in memory
+template <int N>
+__device__ __forceinline__ constexpr int piece_place(int values)
 {
-    if constexpr (DT == CAPSCAPS_FP32) {
-        r.q[0] = reinterpret_cast<const uint4_a4*>(p)[0];
-        r.q[1] = reinterpret_cast<const uint4_a4*>(p)[1];
-    } else {
-        r.q[0] = *reinterpret_cast<const uint4_a2*>(p);
+    return N == 8 ? (values == 4 ? 0 : values == 2 ? 4 : 6) : (values == 2 ? 0 : 2);
+}
+__device__ __forceinline__ int piece_offset(int values, int tail)
+{
+    return values == 4 ? 0 : values == 2 ? tail & 4 : tail & 6;
+}
+// place of value j of the last vector
+template <int N>
+__device__ __forceinline__ int tail_place(int j, int tail)
+{
+    for (int values = 4; values > 0; values /= 2) {
+        const int k = j - piece_offset(values, tail);
+        if ((tail & values) && k >= 0 && k < values) return piece_place<N>(values) + k;
+    }
+    return 0;
+}
+
+template <int DT, int N, int VALUES>
+__device__ __forceinline__ void load_piece(Raw<DT, N>& r, const char* p, int tail)
+{
+    if constexpr (VALUES < N) {
+        if (!(tail & VALUES)) return;
+        typedef Raw<DT, N> R;
+        constexpr int words = VALUES * R::SIZE / 4, at = piece_place<N>(VALUES) * R::SIZE / 4;
+        p += piece_offset(VALUES, tail) * R::SIZE;
+        if constexpr (words == 0) {
+            r.w[at] = *reinterpret_cast<const unsigned short*>(p);
+        } else {
+            const typename Words<words, R::SIZE>::type v = *reinterpret_cast<const typename Words<words, R::SIZE>::at*>(p);
+#pragma unroll
+            for (int k = 0; k < words; ++k) r.w[at + k] = v[k];
+        }
     }
 }
-template <int DT>
-__device__ __forceinline__ void load_tail(Raw<DT>& r, const char* p, int tail)
+template <int DT, int N, int VALUES>
+__device__ __forceinline__ void store_piece(char* p, const Raw<DT, N>& r, int tail)
 {
-    if constexpr (DT == CAPSCAPS_FP32) {
-        if (tail & 4) r.q[0] = *reinterpret_cast<const uint4_a4*>(p);
-        if (tail & 2) {
-            const uint2v w = *reinterpret_cast<const uint2_a4*>(p + (tail & 4) * 4);
-            r.q[1].x = w.x;
-            r.q[1].y = w.y;
+    if constexpr (VALUES < N) {
+        if (!(tail & VALUES)) return;
+        typedef Raw<DT, N> R;
+        constexpr int words = VALUES * R::SIZE / 4, at = piece_place<N>(VALUES) * R::SIZE / 4;
+        p += piece_offset(VALUES, tail) * R::SIZE;
+        if constexpr (words == 0) {
+            *reinterpret_cast<unsigned short*>(p) = (unsigned short)r.w[at];
+        } else {
+            typename Words<words, R::SIZE>::type v;
+#pragma unroll
+            for (int k = 0; k < words; ++k) v[k] = r.w[at + k];
+            *reinterpret_cast<typename Words<words, R::SIZE>::at*>(p) = v;
         }
-        if (tail & 1) r.q[1].z = *reinterpret_cast<const unsigned*>(p + (tail & 6) * 4);
-    } else {
-        if (tail & 4) {
-            const uint2v w = *reinterpret_cast<const uint2_a2*>(p);
-            r.q[0].x = w.x;
-            r.q[0].y = w.y;
-        }
-        if (tail & 2) r.q[0].z = *reinterpret_cast<const uint_a2*>(p + (tail & 4) * 2);
-        if (tail & 1) r.q[0].w = *reinterpret_cast<const unsigned short*>(p + (tail & 6) * 2);
     }
 }
-// a lane's vector: whole, the row's remainder, or nothing (zeros)
-template <int DT, bool TAIL>
-__device__ __forceinline__ void load(Raw<DT>& r, const char* p, bool full, bool part, int tail)
+
+// a lane's vector: whole, the row's remainder, or nothing (the registers stay as they are)
+template <int DT, int N, bool TAIL>
+__device__ __forceinline__ void load(Raw<DT, N>& r, const char* p, bool full, bool part, int tail)
 {
-    if (full) load_full<DT>(r, p);
+    // (rows without a remainder: lines that no other access of the wave touches, and that nothing reads again)
     if constexpr (TAIL) {
-        if (part) load_tail<DT>(r, p, tail);
+        if (full) r.w = *reinterpret_cast<const typename Raw<DT, N>::Whole*>(p);
+        if (part) {
+            load_piece<DT, N, 4>(r, p, tail);
+            load_piece<DT, N, 2>(r, p, tail);
+            load_piece<DT, N, 1>(r, p, tail);
+        }
+    } else if (full) {
+        r.w = __builtin_nontemporal_load(reinterpret_cast<const typename Raw<DT, N>::Whole*>(p));
     }
 }
 
-template <int DT>
-__device__ __forceinline__ float value(const Raw<DT>& r, int k)  // (k is a constant after unrolling)
+template <int DT, int N>
+__device__ __forceinline__ float value(const Raw<DT, N>& r, int k)  // (k is a constant after unrolling)
 {
     if constexpr (DT == CAPSCAPS_FP32) {
-        return __builtin_bit_cast(float, (unsigned)r.q[k / 4][k % 4]);
+        return __builtin_bit_cast(float, (unsigned)r.w[k]);
     } else {
-        const unsigned w = r.q[0][k / 2];
+        const unsigned w = r.w[k / 2];
         if constexpr (DT == CAPSCAPS_BF16)
             return __builtin_bit_cast(float, (k & 1) ? (w & 0xffff0000u) : (w << 16));
         else
@@ -92,59 +126,80 @@ __device__ __forceinline__ float value(const Raw<DT>& r, int k)  // (k is a cons
     }
 }
 
-template <int DT>
-__device__ __forceinline__ Raw<DT> pack(const float* f)
+template <int DT, int N>
+__device__ __forceinline__ Raw<DT, N> pack(const float* f)
 {
-    Raw<DT> r;
+    Raw<DT, N> r;
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) {
+    for (int k = 0; k < N; ++k) {
         if constexpr (DT == CAPSCAPS_FP32) {
-            r.q[k / 4][k % 4] = __builtin_bit_cast(unsigned, f[k]);
+            r.w[k] = __builtin_bit_cast(unsigned, f[k]);
         } else if ((k & 1) == 0) {
             const float2v pair = {f[k], f[k + 1]};
             if constexpr (DT == CAPSCAPS_BF16)
-                r.q[0][k / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, bf16x2v));
+                r.w[k / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, bf16x2v));
             else
-                r.q[0][k / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, half2v));
+                r.w[k / 2] = __builtin_bit_cast(unsigned, __builtin_convertvector(pair, half2v));
         }
     }
     return r;
 }
-template <int DT, bool TAIL>
+template <int DT, int N, bool TAIL>
 __device__ __forceinline__ void store(char* p, const float* f, bool full, bool part, int tail)
 {
-    if (!full && !(TAIL && part)) return;
-    const Raw<DT> r = pack<DT>(f);
-    if constexpr (DT == CAPSCAPS_FP32) {
-        if (full) {
-            reinterpret_cast<uint4_a4*>(p)[0] = r.q[0];
-            reinterpret_cast<uint4_a4*>(p)[1] = r.q[1];
-        } else if constexpr (TAIL) {
-            if (tail & 4) *reinterpret_cast<uint4_a4*>(p) = r.q[0];
-            if (tail & 2) *reinterpret_cast<uint2_a4*>(p + (tail & 4) * 4) = uint2v{r.q[1].x, r.q[1].y};
-            if (tail & 1) *reinterpret_cast<unsigned*>(p + (tail & 6) * 4) = r.q[1].z;
+    const Raw<DT, N> r = pack<DT, N>(f);
+    if constexpr (TAIL) {
+        if (full) *reinterpret_cast<typename Raw<DT, N>::Whole*>(p) = r.w;
+        if (part) {
+            store_piece<DT, N, 4>(p, r, tail);
+            store_piece<DT, N, 2>(p, r, tail);
+            store_piece<DT, N, 1>(p, r, tail);
         }
-    } else {
-        if (full) {
-            *reinterpret_cast<uint4_a2*>(p) = r.q[0];
-        } else if constexpr (TAIL) {
-            if (tail & 4) *reinterpret_cast<uint2_a2*>(p) = uint2v{r.q[0].x, r.q[0].y};
-            if (tail & 2) *reinterpret_cast<uint_a2*>(p + (tail & 4) * 2) = r.q[0].z;
-            if (tail & 1) *reinterpret_cast<unsigned short*>(p + (tail & 6) * 2) = (unsigned short)r.q[0].w;
-        }
+    } else if (full) {
+        __builtin_nontemporal_store(r.w, reinterpret_cast<typename Raw<DT, N>::Whole*>(p));
+    }
+}
+// The compiler may not know from here on what the registers were: what was computed from them is computed again
+// instead of being kept
+template <int DT, int N>
+__device__ __forceinline__ void forget(Raw<DT, N>& r)
+{
+#pragma unroll
+    for (int k = 0; k < Raw<DT, N>::WORDS; ++k) {
+        unsigned w = r.w[k];
+        asm("" : "+v"(w));
+        r.w[k] = w;
     }
 }
 
-// a vector of a per-column fp32 tensor (ones where there is none)
-template <bool TAIL>
+// a vector of a per-column fp32 tensor (`none` where there is no tensor)
+template <int N, bool TAIL>
 __device__ __forceinline__ void load_column(float* f, const float* p, int vector, bool full, bool part, int tail,
                                             float none)
 {
-    Raw<CAPSCAPS_FP32> r;
-    clear(r);
-    if (p != nullptr) load<CAPSCAPS_FP32, TAIL>(r, reinterpret_cast<const char*>(p + (size_t)vector * VEC), full, part, tail);
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) f[k] = p != nullptr ? value<CAPSCAPS_FP32>(r, k) : none;
+    for (int h = 0; h < N / 4; ++h) {  // (quads: 16 bytes)
+        Raw<CAPSCAPS_FP32, 4> r;
+        clear(r);
+        if (p != nullptr) {
+            const float* q = p + (size_t)vector * N + 4 * h;
+            if (full) r.w = *reinterpret_cast<const typename Raw<CAPSCAPS_FP32, 4>::Whole*>(q);
+            if constexpr (TAIL) {
+                if (part) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        // the value whose place is 4 h + k
+                        const int place = 4 * h + k, values = N == 8 ? (place < 4 ? 4 : place < 6 ? 2 : 1) : (place < 2 ? 2 : 1);
+                        const int j = piece_offset(values, tail) + place - piece_place<N>(values);
+                        if ((tail & values) && place - piece_place<N>(values) < values)
+                            r.w[k] = __builtin_bit_cast(unsigned, p[(size_t)vector * N + j]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[4 * h + k] = p != nullptr ? value<CAPSCAPS_FP32, 4>(r, k) : none;
+    }
 }
 
 template <int CTRL>
