@@ -62,11 +62,16 @@ struct RowPlan {
     int full, tail;  // whole vectors in a row, and the values after them
 };
 
-#ifndef WPE4
-#define WPE4 4
-#endif
-#define WPE(values) ((values) == 4 ? WPE4 : 4)
 constexpr int WIDEST = 16384;
+// vectors of a lane: 1, 2 in workgroups of up to 1024; 4, 8 in such of 512, whose waves have twice the registers
+constexpr int widest_workgroup(int vectors) { return vectors > 2 ? 512 : 1024; }
+// (lanes of several vectors are those of a whole workgroup: known to the compiler, which then needs no register for every
+// distance between them)
+template <int I>
+__device__ __forceinline__ int group_of(const RowPlan& P)
+{
+    return I > 1 ? widest_workgroup(I) : P.group;
+}
 // threads of a compute unit that a launch counts on: further rows are the same threads' next ones (forward: none)
 constexpr int FWD_THREADS = 1 << 22, BWD_THREADS = 1024;
 
@@ -85,8 +90,9 @@ struct RowSum {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-        const int wave = threadIdx.x & 15;  // (every 16 lanes add up the same sums)
-        v = wave < group >> 6 ? buffer[wave] : 0.0f;
+        // the waves of this row; every 16 lanes add up the same sums
+        const int waves = group >> 6, wave = threadIdx.x & 15;
+        v = wave < waves ? buffer[((threadIdx.x >> 6) & ~(waves - 1)) + wave] : 0.0f;
         return lanes_sum(v, 16);
     }
 };
@@ -96,21 +102,23 @@ struct RowSum {
 template <int N>
 struct Rows {
     const char* base;
-    long long step;  // bytes to the next round's
+    long long round;  // bytes of a workgroup's rows of one round
     unsigned at;
     template <typename T>
     __device__ __forceinline__ Rows(T* p, long long stride, int bytes, const RowPlan& P, int slot, int lane)
     {
-        base = (const char*)p + (long long)blockIdx.x * P.per_block * stride * bytes;
-        step = (long long)gridDim.x * P.per_block * stride * bytes;
+        base = (const char*)p;
+        round = P.per_block * stride * bytes;
         at = (unsigned)(slot * stride * bytes) + (unsigned)(lane * N * bytes);
     }
-    __device__ __forceinline__ const char* get(int i, const RowPlan& P, int bytes) const
+    __device__ __forceinline__ const char* get(long long n, int vectors, int bytes) const
     {
-        return base + (long long)(i * P.group * N * bytes) + at;
+        return base + n * round + (long long)(vectors * N * bytes) + at;
     }
-    __device__ __forceinline__ char* put(int i, const RowPlan& P, int bytes) const { return const_cast<char*>(get(i, P, bytes)); }
-    __device__ __forceinline__ void next() { base += step; }
+    __device__ __forceinline__ char* put(long long n, int vectors, int bytes) const
+    {
+        return const_cast<char*>(get(n, vectors, bytes));
+    }
 };
 
 // A vector of what a column's values are multiplied by, from pre-norm weight, post-norm weight and a shared gate
@@ -139,7 +147,7 @@ template <int N, int I>
 struct Columns {
     Factors<N> own;
     float* lds;
-    int group, lane;
+    int lane;
     __device__ __forceinline__ void put(int i, const Factors<N>& f)
     {
         if constexpr (I == 1) {
@@ -159,7 +167,7 @@ private:
     typedef float float4v_t __attribute__((ext_vector_type(4)));
     __device__ __forceinline__ float4v_t& quad(int which, int i, int k) const
     {
-        return reinterpret_cast<float4v_t*>(lds)[((which * I + i) * (N / 4) + k / 4) * group + lane];
+        return reinterpret_cast<float4v_t*>(lds)[((which * I + i) * (N / 4) + k / 4) * widest_workgroup(I) + lane];
     }
     __device__ __forceinline__ void get(int which, int i, float* f, const float* kept) const
     {
@@ -177,40 +185,40 @@ private:
 
 // GATE: a gate for every value
 template <int DT, bool S16, bool B16, bool GATE, int N, int I, bool TAIL>
-__global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capscaps_block_fwd_args A, RowPlan P)
+__global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps_block B, capscaps_block_fwd_args A, RowPlan P)
 {
     constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
     constexpr int SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
     __shared__ float lds[32];
-    RowSum sum{lds, P.group, 0};
-    const int lane = threadIdx.x & (P.group - 1), slot = threadIdx.x / P.group;
+    const int group = group_of<I>(P);
+    RowSum sum{lds, group, 0};
+    const int lane = threadIdx.x & (group - 1), slot = threadIdx.x / group;
     const bool branch = A.branch != nullptr, post = branch && B.post_norm, pre = A.h != nullptr;
     const float inv_width = 1.0f / (float)B.width;
     Factors<N> col[I];
 #pragma unroll
     for (int i = 0; i < I; ++i)
-        col[i] = column_factors<N, TAIL>(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane + i * P.group);
+        col[i] = column_factors<N, TAIL>(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane + i * group);
     Rows<N> rx(A.x, A.x_stride, SB, P, slot, lane), rb(A.branch, A.branch_stride, BB, P, slot, lane);
     Rows<N> rg(A.gate, A.gate_stride, LB, P, slot, lane);
     Rows<N> ry(A.y, A.y_stride, SB, P, slot, lane), rh(A.h, A.h_stride, LB, P, slot, lane);
-    const long long step = (long long)gridDim.x * P.per_block;
-    for (long long left = B.rows - (long long)blockIdx.x * P.per_block; left > 0; left -= step) {
-        const bool in = slot < left;
-        const long long r = B.rows - left + slot;
+    {
+        const long long n = blockIdx.x, r = n * P.per_block + slot;
+        const bool in = r < B.rows;
         Raw<SD, N> x[I];
         Raw<BD, N> b[I];
         Raw<DT, N> g[I];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int v = lane + i * P.group;
+            const int v = lane + i * group;
             const bool full = in && v < P.full, part = TAIL && in && v == P.full;
             clear(x[i]);
             clear(b[i]);
-            if (branch) load<BD, N, TAIL>(b[i], rb.get(i, P, BB), full, part, P.tail);
-            load<SD, N, TAIL>(x[i], rx.get(i, P, SB), full, part, P.tail);
+            if (branch) load<BD, N, TAIL>(b[i], rb.get(n, i * group, BB), full, part, P.tail);
+            load<SD, N, TAIL>(x[i], rx.get(n, i * group, SB), full, part, P.tail);
             if constexpr (GATE) {
                 clear(g[i]);
-                load<DT, N, TAIL>(g[i], rg.get(i, P, LB), full, part, P.tail);
+                load<DT, N, TAIL>(g[i], rg.get(n, i * group, LB), full, part, P.tail);
             }
         }
         float rpost = 1.0f;
@@ -227,7 +235,7 @@ __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capsc
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int v = lane + i * P.group;
+            const int v = lane + i * group;
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 y[i][k] = value<SD, N>(x[i], k);
@@ -239,25 +247,20 @@ __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capsc
                 s += y[i][k] * y[i][k];
             }
             if (A.y != nullptr)
-                store<SD, N, TAIL>(ry.put(i, P, SB), y[i], in && v < P.full, in && v == P.full, P.tail);
+                store<SD, N, TAIL>(ry.put(n, i * group, SB), y[i], in && v < P.full, in && v == P.full, P.tail);
         }
         if (pre) {
             const float rpre = __builtin_amdgcn_rsqf(sum(s) * inv_width + B.eps);
             if (A.rstd_pre != nullptr && lane == 0 && in) A.rstd_pre[r] = rpre;
 #pragma unroll
             for (int i = 0; i < I; ++i) {
-                const int v = lane + i * P.group;
+                const int v = lane + i * group;
                 float h[N];
 #pragma unroll
                 for (int k = 0; k < N; ++k) h[k] = y[i][k] * rpre * col[i].to_h[k];
-                store<DT, N, TAIL>(rh.put(i, P, LB), h, in && v < P.full, in && v == P.full, P.tail);
+                store<DT, N, TAIL>(rh.put(n, i * group, LB), h, in && v < P.full, in && v == P.full, P.tail);
             }
         }
-        rx.next();
-        rb.next();
-        rg.next();
-        ry.next();
-        rh.next();
     }
 }
 
@@ -266,14 +269,15 @@ __global__ void __launch_bounds__(1024) block_fwd_kernel(capscaps_block B, capsc
 // of dh * yn, and of d * act * bn, from which both dpost_weight and a shared gate's gradient follow, since all their other
 // factors are the column's.  A workgroup's sums go to `partial` [block][2][columns], columns in the order of lanes' places.
 template <int DT, bool S16, bool B16, bool GATE, int N, int I, bool TAIL>
-__global__ void __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(WPE(N * I))))
+__global__ void __launch_bounds__(widest_workgroup(I))
     block_bwd_kernel(capscaps_block B, capscaps_block_bwd_args A, RowPlan P, float* partial)
 {
     constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
     constexpr int SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
     __shared__ float lds[32];
-    RowSum sum{lds, P.group, 0};
-    const int lane = threadIdx.x & (P.group - 1), slot = threadIdx.x / P.group;
+    const int group = group_of<I>(P);
+    RowSum sum{lds, group, 0};
+    const int lane = threadIdx.x & (group - 1), slot = threadIdx.x / group;
     const bool branch = A.branch != nullptr, has_h = A.dh != nullptr;
     const bool post = branch && B.post_norm && A.rstd_post != nullptr;
     const float inv_width = 1.0f / (float)B.width;
@@ -281,11 +285,10 @@ __global__ void __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(WPE(N
     extern __shared__ float columns_lds[];
     Columns<N, I> col;
     col.lds = columns_lds;
-    col.group = P.group;
     col.lane = lane;
 #pragma unroll
     for (int i = 0; i < I; ++i)
-        col.put(i, column_factors<N, TAIL>(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane + i * P.group));
+        col.put(i, column_factors<N, TAIL>(B, A.pre_weight, post ? A.post_weight : nullptr, A.gate, P, lane + i * group));
     float sum_h[I][N], sum_b[I][N];
 #pragma unroll
     for (int i = 0; i < I; ++i)
@@ -299,48 +302,51 @@ __global__ void __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(WPE(N
     Raw<DT, N> dh[I], g[I];
     Raw<BD, N> b[I];
     float rpre = 1.0f, rpost = 1.0f;
-    auto fetch_h = [&](bool in, long long r) {
+    auto fetch_h = [&](long long n) {
+        const long long r = n * P.per_block + slot;
+        const bool in = r < B.rows;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int v = lane + i * P.group;
+            const int v = lane + i * group;
             const bool full = in && v < P.full, part = TAIL && in && v == P.full;
             clear(y[i]);
             clear(dh[i]);
             if (has_h) {
-                load<SD, N, TAIL>(y[i], ry.get(i, P, SB), full, part, P.tail);
-                load<DT, N, TAIL>(dh[i], rdh.get(i, P, LB), full, part, P.tail);
+                load<SD, N, TAIL>(y[i], ry.get(n, i * group, SB), full, part, P.tail);
+                load<DT, N, TAIL>(dh[i], rdh.get(n, i * group, LB), full, part, P.tail);
             }
         }
         if (has_h && in) rpre = A.rstd_pre[r];
-        ry.next();
-        rdh.next();
     };
-    auto fetch_b = [&](bool in, long long r) {
+    auto fetch_b = [&](long long n) {
+        const long long r = n * P.per_block + slot;
+        const bool in = r < B.rows;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int v = lane + i * P.group;
+            const int v = lane + i * group;
             const bool full = in && v < P.full, part = TAIL && in && v == P.full;
             clear(dy[i]);
             clear(b[i]);
-            if (A.dy != nullptr) load<SD, N, TAIL>(dy[i], rdy.get(i, P, SB), full, part, P.tail);
-            if (branch) load<BD, N, TAIL>(b[i], rb.get(i, P, BB), full, part, P.tail);
+            if (A.dy != nullptr) load<SD, N, TAIL>(dy[i], rdy.get(n, i * group, SB), full, part, P.tail);
+            if (branch) load<BD, N, TAIL>(b[i], rb.get(n, i * group, BB), full, part, P.tail);
             if constexpr (GATE) {
                 clear(g[i]);
-                load<DT, N, TAIL>(g[i], rg.get(i, P, LB), full, part, P.tail);
+                load<DT, N, TAIL>(g[i], rg.get(n, i * group, LB), full, part, P.tail);
             }
         }
         if (post && in) rpost = A.rstd_post[r];
-        rdy.next();
-        rb.next();
-        rg.next();
     };
-    const long long step = (long long)gridDim.x * P.per_block;
-    long long left = B.rows - (long long)blockIdx.x * P.per_block;  // rows from this round's first one on
-    fetch_h(slot < left, B.rows - left + slot);
-    for (; left > 0; left -= step) {
-        const bool in = slot < left;
-        const long long r = B.rows - left + slot;
-        fetch_b(in, r);
+    const long long rounds = (B.rows + P.per_block - 1) / P.per_block;
+    long long n = blockIdx.x;
+    constexpr bool AHEAD = I < 8;  // (fp32 rows on 512 threads: no registers for it)
+    if constexpr (AHEAD) fetch_h(n);
+    for (; n < rounds; n += gridDim.x) {
+        const bool in = n * P.per_block + slot < B.rows;
+        // waves that hold rows by themselves stay together (wider rows' sums keep them so): their accesses are then one
+        // piece of memory after another (6.4M rows of 64 bf16 values: 285 us, without 325; rows of 1024, eight to a workgroup: 139, one: 163)
+        if (group <= 64) __builtin_amdgcn_s_barrier();
+        if constexpr (!AHEAD) fetch_h(n);
+        fetch_b(n);
         float s = 0.0f, mean = 0.0f;
         if (has_h) {
 #pragma unroll
@@ -356,12 +362,7 @@ __global__ void __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(WPE(N
         s = 0.0f;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            forget(y[i]);
-            forget(dh[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < I; ++i) {
-            const int v = lane + i * P.group;
+            const int v = lane + i * group;
             float dx[N], dg[N], cb[N], wh[N];
             col.to_b(i, cb);
             col.to_h(i, wh);
@@ -380,72 +381,74 @@ __global__ void __launch_bounds__(1024) __attribute__((amdgpu_waves_per_eu(WPE(N
                 }
                 sum_b[i][k] += d * bn;
                 e[i][k] = d * cb[k];
+                // (here, not where they are used: the compiler would keep the factors of all these products until then)
+                asm volatile("" : "+v"(sum_h[i][k]), "+v"(sum_b[i][k]), "+v"(e[i][k]));
                 s += e[i][k] * bn;
             }
             if (A.dx != nullptr)
-                store<SD, N, TAIL>(rdx.put(i, P, SB), dx, in && v < P.full, in && v == P.full, P.tail);
+                store<SD, N, TAIL>(rdx.put(n, i * group, SB), dx, in && v < P.full, in && v == P.full, P.tail);
             if constexpr (GATE) {
                 if (A.dgate != nullptr)
-                    store<DT, N, TAIL>(rdg.put(i, P, LB), dg, in && v < P.full, in && v == P.full, P.tail);
+                    store<DT, N, TAIL>(rdg.put(n, i * group, LB), dg, in && v < P.full, in && v == P.full, P.tail);
             }
         }
-        if (left > step) fetch_h(slot < left - step, r + step);
+        if (AHEAD && n + gridDim.x < rounds) fetch_h(n + gridDim.x);
         if (A.dbranch != nullptr) {
             mean = post ? sum(s) * inv_width : 0.0f;
 #pragma unroll
-            for (int i = 0; i < I; ++i) forget(b[i]);
-#pragma unroll
             for (int i = 0; i < I; ++i) {
-                const int v = lane + i * P.group;
+                const int v = lane + i * group;
                 float db[N];
 #pragma unroll
                 for (int k = 0; k < N; ++k) db[k] = rpost * (e[i][k] - value<BD, N>(b[i], k) * rpost * mean);
-                store<DT, N, TAIL>(rdb.put(i, P, LB), db, in && v < P.full, in && v == P.full, P.tail);
+                store<DT, N, TAIL>(rdb.put(n, i * group, LB), db, in && v < P.full, in && v == P.full, P.tail);
             }
         }
-        rdx.next();
-        rdb.next();
-        rdg.next();
     }
     if (partial == nullptr) return;
-    const int columns = P.vectors * P.group * N;
+    const int columns = P.vectors * group * N;
     float* out = partial + (long long)blockIdx.x * 2 * columns;
     if (P.per_block == 1) {
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
             for (int k = 0; k < N; ++k) {
-                out[(lane + i * P.group) * N + k] = sum_h[i][k];
-                out[columns + (lane + i * P.group) * N + k] = sum_b[i][k];
+                out[(lane + i * group) * N + k] = sum_h[i][k];
+                out[columns + (lane + i * group) * N + k] = sum_b[i][k];
             }
         return;
     }
-    // rows of one wave, in halves: lanes that hold the same columns
+    if (group < 64) {
+        // rows of one wave, in halves: lanes that hold the same columns
 #pragma unroll
-    for (int i = 0; i < I; ++i)
+        for (int i = 0; i < I; ++i)
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-            for (int o = 32; o >= P.group; o >>= 1) {
-                sum_h[i][k] += __shfl_xor(sum_h[i][k], o);
-                sum_b[i][k] += __shfl_xor(sum_b[i][k], o);
-            }
-    // the rows of the four waves
-    __shared__ float of_wave[THREADS / 64][64 * N];
-#pragma unroll
-    for (int i = 0; i < I; ++i)
+            for (int k = 0; k < N; ++k)
+                for (int o = 32; o >= group; o >>= 1) {
+                    sum_h[i][k] += __shfl_xor(sum_h[i][k], o);
+                    sum_b[i][k] += __shfl_xor(sum_b[i][k], o);
+                }
+    }
+    // the rows of the workgroup's waves: `slots` of them hold the same columns (a lane has one vector, or the row a workgroup)
+    if constexpr (I == 1) {
+        __shared__ float of_slot[1024 * N];
+        const int wide = group < 64 ? 64 : group, slots = P.threads / wide, in_row = group * N;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             __syncthreads();
-            if ((int)(threadIdx.x & 63) < P.group) {
+            if ((int)(threadIdx.x & (wide - 1)) < group) {
 #pragma unroll
                 for (int k = 0; k < N; ++k)
-                    of_wave[threadIdx.x >> 6][lane * N + k] = which == 0 ? sum_h[i][k] : sum_b[i][k];
+                    of_slot[threadIdx.x / wide * in_row + lane * N + k] = which == 0 ? sum_h[0][k] : sum_b[0][k];
             }
             __syncthreads();
-            for (int c = threadIdx.x; c < P.group * N; c += THREADS)
-                out[which * columns + i * P.group * N + c] =
-                    (of_wave[0][c] + of_wave[1][c]) + (of_wave[2][c] + of_wave[3][c]);
+            for (int c = threadIdx.x; c < in_row; c += P.threads) {
+                float s = of_slot[c];
+                for (int j = 1; j < slots; ++j) s += of_slot[j * in_row + c];
+                out[which * columns + c] = s;
+            }
         }
+    }
 }
 
 // Sums the workgroups' sums, 64 columns a workgroup, each by 16 threads that take every 16th in turn
@@ -665,18 +668,23 @@ int check_block(const capscaps_block* B)
     return CAPSCAPS_OK;
 }
 
-// The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024.  `apart`: rows so far
+// The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024; then two vectors of four values,
+// or 32 values in a workgroup of 512.  `apart`: rows so far
 // apart that those of one workgroup are not within reach of 32-bit offsets, one at a time in a workgroup.
-RowPlan row_plan(const capscaps_block& B, int n, int threads_per_cu, bool apart)
+RowPlan row_plan(const capscaps_block& B, int n, int workgroup, int threads_per_cu, bool apart)
 {
     RowPlan P;
     P.n = n;
     const int vectors = (B.width + n - 1) / n;
     P.group = apart ? 64 : 1;
     while (P.group < vectors && P.group < 1024) P.group *= 2;
-    P.vectors = 1;
-    while (P.group * P.vectors < vectors) P.vectors *= 2;
-    P.threads = P.group > 64 || apart ? P.group : THREADS;
+    P.vectors = vectors <= P.group ? 1 : n == 4 && vectors <= 2 * P.group ? 2 : 32 / n;
+    if (P.vectors > 2) P.group = 512;
+    // (backward: as many rows as fill a workgroup of 1024, whose sums over rows are then one; but where there are few
+    // rows, more workgroups)
+    const bool many = P.vectors == 1 && B.rows * P.group >= (long long)workgroup * CUS;
+    P.threads = many ? workgroup : THREADS;
+    if (P.group > P.threads || apart) P.threads = P.group;
     P.per_block = P.threads / P.group;
     const long long blocks = (B.rows + P.per_block - 1) / P.per_block;
     const long long most = apart ? CUS : (long long)CUS * threads_per_cu / P.threads;
@@ -711,11 +719,11 @@ void with_properties(const capscaps_block& B, bool branch, const RowPlan& P, F l
     };
     auto by_vectors = [&](auto s, auto b, auto g) {
         if constexpr (s.value && b.value) {
-            P.vectors == 1 ? by_tail(s, b, g, Int<8>(), Int<1>()) : by_tail(s, b, g, Int<8>(), Int<2>());
+            P.vectors == 1 ? by_tail(s, b, g, Int<8>(), Int<1>()) : by_tail(s, b, g, Int<8>(), Int<4>());
         } else {
             if (P.vectors == 1) by_tail(s, b, g, Int<4>(), Int<1>());
             if (P.vectors == 2) by_tail(s, b, g, Int<4>(), Int<2>());
-            if (P.vectors == 4) by_tail(s, b, g, Int<4>(), Int<4>());
+            if (P.vectors == 8) by_tail(s, b, g, Int<4>(), Int<8>());
         }
     };
     auto by_gate = [&](auto s, auto b) {
@@ -789,7 +797,7 @@ int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fw
     if (A.y == A.x && A.y_stride != A.x_stride) return CAPSCAPS_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool apart = rows_apart({A.x_stride, A.branch_stride, A.gate_stride, A.y_stride, A.h_stride});
-    const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), FWD_THREADS, apart);
+    const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), THREADS, FWD_THREADS, apart);
     if (B.width > WIDEST)
         block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A);
     else if (B.dtype == CAPSCAPS_FP32)
@@ -808,7 +816,7 @@ size_t capscaps_block_norm_bwd_workspace_bytes(const capscaps_block* block)
         size_t most = 0;
         for (const bool apart : {false, true})
             for (const bool branch : {false, true}) {
-                const RowPlan P = row_plan(*block, vector_values(*block, branch), BWD_THREADS, apart);
+                const RowPlan P = row_plan(*block, vector_values(*block, branch), 1024, BWD_THREADS, apart);
                 const size_t bytes = (size_t)P.blocks * 2 * P.vectors * P.group * P.n * 4;
                 most = bytes > most ? bytes : most;
             }
@@ -859,7 +867,7 @@ int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bw
     if (B.width <= WIDEST) {
         const bool apart = rows_apart({A.y_stride, A.branch_stride, A.gate_stride, A.dh_stride, A.dy_stride, A.dx_stride,
                                        A.dbranch_stride, A.dgate_stride});
-        const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), BWD_THREADS, apart);
+        const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), 1024, BWD_THREADS, apart);
         float* partial = sums ? static_cast<float*>(workspace) : nullptr;
         const hipError_t err = B.dtype == CAPSCAPS_FP32   ? launch_bwd<CAPSCAPS_FP32>(B, A, P, partial, st)
                                : B.dtype == CAPSCAPS_BF16 ? launch_bwd<CAPSCAPS_BF16>(B, A, P, partial, st)

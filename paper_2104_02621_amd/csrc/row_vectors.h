@@ -159,19 +159,6 @@ __device__ __forceinline__ void store(char* p, const float* f, bool full, bool p
         __builtin_nontemporal_store(r.w, reinterpret_cast<typename Raw<DT, N>::Whole*>(p));
     }
 }
-// The compiler may not know from here on what the registers were: what was computed from them is computed again
-// instead of being kept
-template <int DT, int N>
-__device__ __forceinline__ void forget(Raw<DT, N>& r)
-{
-#pragma unroll
-    for (int k = 0; k < Raw<DT, N>::WORDS; ++k) {
-        unsigned w = r.w[k];
-        asm("" : "+v"(w));
-        r.w[k] = w;
-    }
-}
-
 // a vector of a per-column fp32 tensor (`none` where there is no tensor)
 template <int N, bool TAIL>
 __device__ __forceinline__ void load_column(float* f, const float* p, int vector, bool full, bool part, int tail,
