@@ -60,6 +60,7 @@ struct RowPlan {
     int group, vectors, threads, per_block;
     unsigned blocks;
     int full, tail;  // whole vectors in a row, and the values after them
+    bool turns;      // more than one round of rows for a workgroup
 };
 
 constexpr int WIDEST = 16384;
@@ -72,9 +73,6 @@ __device__ __forceinline__ int group_of(const RowPlan& P)
 {
     return I > 1 ? widest_workgroup(I) : P.group;
 }
-// threads of a compute unit that a launch counts on: further rows are the same threads' next ones (forward: none)
-constexpr int FWD_THREADS = 1 << 22, BWD_THREADS = 1024;
-
 // Sum over a row's lanes.  Rows of more than one wave go through LDS: two buffers in turn, so that one barrier is
 // enough (a wave writes a buffer again only after the barrier of the other one, which every wave reaches after it has read).
 struct RowSum {
@@ -183,8 +181,8 @@ private:
     }
 };
 
-// GATE: a gate for every value
-template <int DT, bool S16, bool B16, bool GATE, int N, int I, bool TAIL>
+// GATE: a gate for every value.  TURNS: a workgroup takes one round of rows after another (else one round)
+template <int DT, bool S16, bool B16, bool GATE, int N, int I, bool TAIL, bool TURNS>
 __global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps_block B, capscaps_block_fwd_args A, RowPlan P)
 {
     constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
@@ -202,8 +200,10 @@ __global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps
     Rows<N> rx(A.x, A.x_stride, SB, P, slot, lane), rb(A.branch, A.branch_stride, BB, P, slot, lane);
     Rows<N> rg(A.gate, A.gate_stride, LB, P, slot, lane);
     Rows<N> ry(A.y, A.y_stride, SB, P, slot, lane), rh(A.h, A.h_stride, LB, P, slot, lane);
-    {
-        const long long n = blockIdx.x, r = n * P.per_block + slot;
+    const long long rounds = (B.rows + P.per_block - 1) / P.per_block;
+    long long n = blockIdx.x;
+    do {
+        const long long r = n * P.per_block + slot;
         const bool in = r < B.rows;
         Raw<SD, N> x[I];
         Raw<BD, N> b[I];
@@ -261,7 +261,8 @@ __global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps
                 store<DT, N, TAIL>(rh.put(n, i * group, LB), h, in && v < P.full, in && v == P.full, P.tail);
             }
         }
-    }
+        n += gridDim.x;
+    } while (TURNS && n < rounds);
 }
 
 // The way back.  Of the two sums over a row, the first (of dh * pre_weight * yn) needs y and dh, the second dy and b: each
@@ -669,9 +670,14 @@ int check_block(const capscaps_block* B)
 }
 
 // The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024; then two vectors of four values,
-// or 32 values in a workgroup of 512.  `apart`: rows so far
-// apart that those of one workgroup are not within reach of 32-bit offsets, one at a time in a workgroup.
-RowPlan row_plan(const capscaps_block& B, int n, int workgroup, int threads_per_cu, bool apart)
+// or 32 values in a workgroup of 512.  `apart`: rows so far apart that those of one workgroup are not within reach of
+// 32-bit offsets, one at a time in a workgroup.
+//
+// Workgroups of 1024 that go through many rows in step read memory in large pieces, and need the columns' factors once; rows
+// of few lanes do better as they come, four waves a workgroup (us, forward, 134M bf16 values a tensor, 173 at 6.2 TB/s: rows of 512
+// 183 as they come, 202 in turns; of 1024 192 and 183, of 4096 239 and 182; 67M fp32 values: rows of 1024 178 and 188, of 4096 192 and
+// 180).  The way back keeps sums over rows in registers, so it always goes in turns.
+RowPlan row_plan(const capscaps_block& B, int n, bool forward, bool apart)
 {
     RowPlan P;
     P.n = n;
@@ -680,28 +686,28 @@ RowPlan row_plan(const capscaps_block& B, int n, int workgroup, int threads_per_
     while (P.group < vectors && P.group < 1024) P.group *= 2;
     P.vectors = vectors <= P.group ? 1 : n == 4 && vectors <= 2 * P.group ? 2 : 32 / n;
     if (P.vectors > 2) P.group = 512;
-    // (backward: as many rows as fill a workgroup of 1024, whose sums over rows are then one; but where there are few
-    // rows, more workgroups)
-    const bool many = P.vectors == 1 && B.rows * P.group >= (long long)workgroup * CUS;
-    P.threads = many ? workgroup : THREADS;
+    const bool in_step = !forward || (vectors > 64 && (n == 8 || B.width > 2048));
+    // (several rows in a workgroup of 1024 where there are rows for every unit)
+    P.threads = in_step && P.vectors == 1 && B.rows * P.group >= 1024LL * CUS ? 1024 : THREADS;
     if (P.group > P.threads || apart) P.threads = P.group;
     P.per_block = P.threads / P.group;
     const long long blocks = (B.rows + P.per_block - 1) / P.per_block;
-    const long long most = apart ? CUS : (long long)CUS * threads_per_cu / P.threads;
+    const long long most = apart ? CUS : !in_step ? 1LL << 30 : (long long)CUS * (forward ? 2048 : 1024) / P.threads;
     P.blocks = (unsigned)(blocks < most ? blocks : most);
+    P.turns = P.blocks < blocks;
     P.full = B.width / n;
     P.tail = B.width % n;
     return P;
 }
-int vector_values(const capscaps_block& B, bool branch)
-{
-    return B.dtype != CAPSCAPS_FP32 && B.stream_dtype == B.dtype && (!branch || B.branch_dtype == B.dtype) ? 8 : 4;
-}
 bool rows_apart(std::initializer_list<long long> strides)
 {
     for (long long s : strides)
-        if (s > (1 << 20)) return true;  // 256 rows of fp32 within 2^30 bytes
+        if (s > (1 << 18)) return true;  // 1024 rows of fp32 within 2^30 bytes
     return false;
+}
+int vector_values(const capscaps_block& B, bool branch)
+{
+    return B.dtype != CAPSCAPS_FP32 && B.stream_dtype == B.dtype && (!branch || B.branch_dtype == B.dtype) ? 8 : 4;
 }
 
 template <int V>
@@ -744,7 +750,14 @@ template <int DT>
 void launch_fwd(const capscaps_block& B, const capscaps_block_fwd_args& A, const RowPlan& P, hipStream_t st)
 {
     with_properties<DT>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto n, auto i, auto tail) {
-        block_fwd_kernel<DT, s.value, b.value, g.value, n.value, i.value, tail.value>
+        if constexpr (i.value == 1) {
+            if (!P.turns) {
+                block_fwd_kernel<DT, s.value, b.value, g.value, n.value, i.value, tail.value, false>
+                    <<<dim3(P.blocks), dim3(P.threads), 0, st>>>(B, A, P);
+                return;
+            }
+        }
+        block_fwd_kernel<DT, s.value, b.value, g.value, n.value, i.value, tail.value, true>
             <<<dim3(P.blocks), dim3(P.threads), 0, st>>>(B, A, P);
     });
 }
@@ -797,7 +810,7 @@ int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fw
     if (A.y == A.x && A.y_stride != A.x_stride) return CAPSCAPS_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool apart = rows_apart({A.x_stride, A.branch_stride, A.gate_stride, A.y_stride, A.h_stride});
-    const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), THREADS, FWD_THREADS, apart);
+    const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), true, apart);
     if (B.width > WIDEST)
         block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A);
     else if (B.dtype == CAPSCAPS_FP32)
@@ -816,7 +829,7 @@ size_t capscaps_block_norm_bwd_workspace_bytes(const capscaps_block* block)
         size_t most = 0;
         for (const bool apart : {false, true})
             for (const bool branch : {false, true}) {
-                const RowPlan P = row_plan(*block, vector_values(*block, branch), 1024, BWD_THREADS, apart);
+                const RowPlan P = row_plan(*block, vector_values(*block, branch), false, apart);
                 const size_t bytes = (size_t)P.blocks * 2 * P.vectors * P.group * P.n * 4;
                 most = bytes > most ? bytes : most;
             }
@@ -867,7 +880,7 @@ int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bw
     if (B.width <= WIDEST) {
         const bool apart = rows_apart({A.y_stride, A.branch_stride, A.gate_stride, A.dh_stride, A.dy_stride, A.dx_stride,
                                        A.dbranch_stride, A.dgate_stride});
-        const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), 1024, BWD_THREADS, apart);
+        const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), false, apart);
         float* partial = sums ? static_cast<float*>(workspace) : nullptr;
         const hipError_t err = B.dtype == CAPSCAPS_FP32   ? launch_bwd<CAPSCAPS_FP32>(B, A, P, partial, st)
                                : B.dtype == CAPSCAPS_BF16 ? launch_bwd<CAPSCAPS_BF16>(B, A, P, partial, st)
