@@ -102,11 +102,13 @@ struct Rows {
     const char* base;
     long long round;  // bytes of a workgroup's rows of one round
     unsigned at;
+    bool over;  // what follows a row, up to a vector, is the next one's or lies before it
     template <typename T>
     __device__ __forceinline__ Rows(T* p, long long stride, int bytes, const RowPlan& P, int slot, int lane)
     {
         base = (const char*)p;
         round = P.per_block * stride * bytes;
+        over = stride >= N;
         at = (unsigned)(slot * stride * bytes) + (unsigned)(lane * N * bytes);
     }
     __device__ __forceinline__ const char* get(long long n, int vectors, int bytes) const
@@ -130,11 +132,11 @@ __device__ __forceinline__ Factors<N> column_factors(const capscaps_block& B, co
 {
     Factors<N> f;
     const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
-    const bool full = v < P.full, part = TAIL && v == P.full;
-    load_column<N, TAIL>(f.to_b, post_weight, v, full, part, P.tail, 1.0f);
-    load_column<N, TAIL>(f.to_h, pre_weight, v, full, part, P.tail, 1.0f);
+    const Share has{v < P.full, TAIL && v == P.full, P.tail};
+    load_column<N, TAIL>(f.to_b, post_weight, v, has, 1.0f);
+    load_column<N, TAIL>(f.to_h, pre_weight, v, has, 1.0f);
     float g[N];
-    load_column<N, TAIL>(g, shared ? static_cast<const float*>(gate) : nullptr, v, full, part, P.tail, 1.0f);
+    load_column<N, TAIL>(g, shared ? static_cast<const float*>(gate) : nullptr, v, has, 1.0f);
 #pragma unroll
     for (int k = 0; k < N; ++k) f.to_b[k] *= B.branch_scale * (shared ? gate_value(B.gate_act, g[k]) : 1.0f);
     return f;
@@ -204,21 +206,21 @@ __global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps
     long long n = blockIdx.x;
     do {
         const long long r = n * P.per_block + slot;
-        const bool in = r < B.rows;
+        const bool in = r < B.rows, last = r + 1 >= B.rows;
         Raw<SD, N> x[I];
         Raw<BD, N> b[I];
         Raw<DT, N> g[I];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
-            const bool full = in && v < P.full, part = TAIL && in && v == P.full;
+            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
             clear(x[i]);
             clear(b[i]);
-            if (branch) load<BD, N, TAIL>(b[i], rb.get(n, i * group, BB), full, part, P.tail);
-            load<SD, N, TAIL>(x[i], rx.get(n, i * group, SB), full, part, P.tail);
+            if (branch) load<BD, N, TAIL>(b[i], rb.get(n, i * group, BB), has, rb.over && !last);
+            load<SD, N, TAIL>(x[i], rx.get(n, i * group, SB), has, rx.over && !last);
             if constexpr (GATE) {
                 clear(g[i]);
-                load<DT, N, TAIL>(g[i], rg.get(n, i * group, LB), full, part, P.tail);
+                load<DT, N, TAIL>(g[i], rg.get(n, i * group, LB), has, rg.over && !last);
             }
         }
         float rpost = 1.0f;
@@ -236,6 +238,7 @@ __global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
+            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 y[i][k] = value<SD, N>(x[i], k);
@@ -247,7 +250,7 @@ __global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps
                 s += y[i][k] * y[i][k];
             }
             if (A.y != nullptr)
-                store<SD, N, TAIL>(ry.put(n, i * group, SB), y[i], in && v < P.full, in && v == P.full, P.tail);
+                store<SD, N, TAIL>(ry.put(n, i * group, SB), y[i], has);
         }
         if (pre) {
             const float rpre = __builtin_amdgcn_rsqf(sum(s) * inv_width + B.eps);
@@ -255,10 +258,11 @@ __global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int v = lane + i * group;
+                const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
                 float h[N];
 #pragma unroll
                 for (int k = 0; k < N; ++k) h[k] = y[i][k] * rpre * col[i].to_h[k];
-                store<DT, N, TAIL>(rh.put(n, i * group, LB), h, in && v < P.full, in && v == P.full, P.tail);
+                store<DT, N, TAIL>(rh.put(n, i * group, LB), h, has);
             }
         }
         n += gridDim.x;
@@ -305,34 +309,34 @@ __global__ void __launch_bounds__(widest_workgroup(I))
     float rpre = 1.0f, rpost = 1.0f;
     auto fetch_h = [&](long long n) {
         const long long r = n * P.per_block + slot;
-        const bool in = r < B.rows;
+        const bool in = r < B.rows, last = r + 1 >= B.rows;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
-            const bool full = in && v < P.full, part = TAIL && in && v == P.full;
+            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
             clear(y[i]);
             clear(dh[i]);
             if (has_h) {
-                load<SD, N, TAIL>(y[i], ry.get(n, i * group, SB), full, part, P.tail);
-                load<DT, N, TAIL>(dh[i], rdh.get(n, i * group, LB), full, part, P.tail);
+                load<SD, N, TAIL>(y[i], ry.get(n, i * group, SB), has, ry.over && !last);
+                load<DT, N, TAIL>(dh[i], rdh.get(n, i * group, LB), has, rdh.over && !last);
             }
         }
         if (has_h && in) rpre = A.rstd_pre[r];
     };
     auto fetch_b = [&](long long n) {
         const long long r = n * P.per_block + slot;
-        const bool in = r < B.rows;
+        const bool in = r < B.rows, last = r + 1 >= B.rows;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
-            const bool full = in && v < P.full, part = TAIL && in && v == P.full;
+            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
             clear(dy[i]);
             clear(b[i]);
-            if (A.dy != nullptr) load<SD, N, TAIL>(dy[i], rdy.get(n, i * group, SB), full, part, P.tail);
-            if (branch) load<BD, N, TAIL>(b[i], rb.get(n, i * group, BB), full, part, P.tail);
+            if (A.dy != nullptr) load<SD, N, TAIL>(dy[i], rdy.get(n, i * group, SB), has, rdy.over && !last);
+            if (branch) load<BD, N, TAIL>(b[i], rb.get(n, i * group, BB), has, rb.over && !last);
             if constexpr (GATE) {
                 clear(g[i]);
-                load<DT, N, TAIL>(g[i], rg.get(n, i * group, LB), full, part, P.tail);
+                load<DT, N, TAIL>(g[i], rg.get(n, i * group, LB), has, rg.over && !last);
             }
         }
         if (post && in) rpost = A.rstd_post[r];
@@ -364,6 +368,7 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
+            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
             float dx[N], dg[N], cb[N], wh[N];
             col.to_b(i, cb);
             col.to_h(i, wh);
@@ -387,10 +392,10 @@ __global__ void __launch_bounds__(widest_workgroup(I))
                 s += e[i][k] * bn;
             }
             if (A.dx != nullptr)
-                store<SD, N, TAIL>(rdx.put(n, i * group, SB), dx, in && v < P.full, in && v == P.full, P.tail);
+                store<SD, N, TAIL>(rdx.put(n, i * group, SB), dx, has);
             if constexpr (GATE) {
                 if (A.dgate != nullptr)
-                    store<DT, N, TAIL>(rdg.put(n, i * group, LB), dg, in && v < P.full, in && v == P.full, P.tail);
+                    store<DT, N, TAIL>(rdg.put(n, i * group, LB), dg, has);
             }
         }
         if (AHEAD && n + gridDim.x < rounds) fetch_h(n + gridDim.x);
@@ -399,10 +404,11 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int v = lane + i * group;
+                const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
                 float db[N];
 #pragma unroll
                 for (int k = 0; k < N; ++k) db[k] = rpost * (e[i][k] - value<BD, N>(b[i], k) * rpost * mean);
-                store<DT, N, TAIL>(rdb.put(n, i * group, LB), db, in && v < P.full, in && v == P.full, P.tail);
+                store<DT, N, TAIL>(rdb.put(n, i * group, LB), db, has);
             }
         }
     }
@@ -461,9 +467,7 @@ __global__ void __launch_bounds__(1024)
     const int columns = P.vectors * P.group * P.n;
     float s = 0.0f;
     if (c < B.width) {
-        const int j = c % P.n, tail = P.n == 8 ? tail_place<8>(j, P.tail) : tail_place<4>(j, P.tail);
-        const int place = c / P.n < P.full ? c : c - j + tail;
-        const float* p = partial + (long long)blockIdx.y * columns + place;
+        const float* p = partial + (long long)blockIdx.y * columns + c;
 #pragma unroll 8
         for (int k = share; k < (int)P.blocks; k += 16) s += p[(long long)k * 2 * columns];
     }

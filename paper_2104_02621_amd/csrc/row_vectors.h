@@ -3,11 +3,13 @@
 // A row's values are cut into vectors of N values, one of 16 bytes where all tensors of a call have 16-bit elements (N = 8),
 // else N = 4: 16 bytes of fp32, 8 of a 16-bit type, so that a wave's access is one contiguous piece in every type.
 // They are loaded and stored whole at any alignment (the hardware takes such accesses at element addresses).
-// What a row's length leaves over (1 .. N - 1 values) is one lane's last vector, moved in pieces of 4, 2 and 1 values that have fixed
-// places in the registers: N = 8: 0 .. 3, 4 .. 5 and 6; N = 4: 0 .. 1 and 2.  All tensors of a call and the per-column vectors
-// use the same places, so the kernels need not know.
+// What a row's length leaves over (1 .. N - 1 values) is one lane's last vector.  It is loaded whole too, with the beginning of
+// what follows in memory, which is masked (a load for 1, 2 and 4 values each would be three, and as many waits for the same
+// lines); in a tensor's last row, and where rows are not apart, in pieces.  It is stored in pieces.
 #pragma once
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "element.h"
 
@@ -38,77 +40,82 @@ __device__ __forceinline__ void clear(Raw<DT, N>& r)
     for (int k = 0; k < Raw<DT, N>::WORDS; ++k) r.w[k] = 0;
 }
 
-// The piece of 4, 2 or 1 values of a row's last vector: where it lies in the vector's registers, and after how many values in memory
-template <int N>
-__device__ __forceinline__ constexpr int piece_place(int values)
+// The first `tail` (1 .. N - 1) values of a vector in memory, as pieces of 4, 2 and 1 values (tail is the same for all lanes)
+template <int DT, int N, int FIRST, int VALUES>
+__device__ __forceinline__ void load_piece(Raw<DT, N>& r, const char* p)
 {
-    return N == 8 ? (values == 4 ? 0 : values == 2 ? 4 : 6) : (values == 2 ? 0 : 2);
-}
-__device__ __forceinline__ int piece_offset(int values, int tail)
-{
-    return values == 4 ? 0 : values == 2 ? tail & 4 : tail & 6;
-}
-// place of value j of the last vector
-template <int N>
-__device__ __forceinline__ int tail_place(int j, int tail)
-{
-    for (int values = 4; values > 0; values /= 2) {
-        const int k = j - piece_offset(values, tail);
-        if ((tail & values) && k >= 0 && k < values) return piece_place<N>(values) + k;
-    }
-    return 0;
-}
-
-template <int DT, int N, int VALUES>
-__device__ __forceinline__ void load_piece(Raw<DT, N>& r, const char* p, int tail)
-{
-    if constexpr (VALUES < N) {
-        if (!(tail & VALUES)) return;
-        typedef Raw<DT, N> R;
-        constexpr int words = VALUES * R::SIZE / 4, at = piece_place<N>(VALUES) * R::SIZE / 4;
-        p += piece_offset(VALUES, tail) * R::SIZE;
-        if constexpr (words == 0) {
-            r.w[at] = *reinterpret_cast<const unsigned short*>(p);
-        } else {
-            const typename Words<words, R::SIZE>::type v = *reinterpret_cast<const typename Words<words, R::SIZE>::at*>(p);
+    typedef Raw<DT, N> R;
+    constexpr int words = VALUES * R::SIZE / 4, at = FIRST * R::SIZE / 4;
+    p += FIRST * R::SIZE;
+    if constexpr (words == 0) {
+        r.w[at] = *reinterpret_cast<const unsigned short*>(p);
+    } else {
+        const typename Words<words, R::SIZE>::type v = *reinterpret_cast<const typename Words<words, R::SIZE>::at*>(p);
 #pragma unroll
-            for (int k = 0; k < words; ++k) r.w[at + k] = v[k];
+        for (int k = 0; k < words; ++k) r.w[at + k] = v[k];
+    }
+}
+template <int DT, int N, int FIRST, int VALUES>
+__device__ __forceinline__ void store_piece(char* p, const Raw<DT, N>& r)
+{
+    typedef Raw<DT, N> R;
+    constexpr int words = VALUES * R::SIZE / 4, at = FIRST * R::SIZE / 4;
+    p += FIRST * R::SIZE;
+    if constexpr (words == 0) {
+        *reinterpret_cast<unsigned short*>(p) = (unsigned short)r.w[at];
+    } else {
+        typename Words<words, R::SIZE>::type v;
+#pragma unroll
+        for (int k = 0; k < words; ++k) v[k] = r.w[at + k];
+        *reinterpret_cast<typename Words<words, R::SIZE>::at*>(p) = v;
+    }
+}
+// calls f with the (first value, values) of each piece as compile-time numbers
+template <int N, typename F>
+__device__ __forceinline__ void pieces(int tail, F f)
+{
+    auto of = [&](auto first) {  // what is left after `first` values: 0 .. 3
+        if (tail & 2) {
+            f(first, std::integral_constant<int, 2>());
+            if (tail & 1) f(std::integral_constant<int, first.value + 2>(), std::integral_constant<int, 1>());
+        } else if (tail & 1) {
+            f(first, std::integral_constant<int, 1>());
+        }
+    };
+    if constexpr (N == 8) {
+        if (tail & 4) {
+            f(std::integral_constant<int, 0>(), std::integral_constant<int, 4>());
+            of(std::integral_constant<int, 4>());
+            return;
         }
     }
-}
-template <int DT, int N, int VALUES>
-__device__ __forceinline__ void store_piece(char* p, const Raw<DT, N>& r, int tail)
-{
-    if constexpr (VALUES < N) {
-        if (!(tail & VALUES)) return;
-        typedef Raw<DT, N> R;
-        constexpr int words = VALUES * R::SIZE / 4, at = piece_place<N>(VALUES) * R::SIZE / 4;
-        p += piece_offset(VALUES, tail) * R::SIZE;
-        if constexpr (words == 0) {
-            *reinterpret_cast<unsigned short*>(p) = (unsigned short)r.w[at];
-        } else {
-            typename Words<words, R::SIZE>::type v;
-#pragma unroll
-            for (int k = 0; k < words; ++k) v[k] = r.w[at + k];
-            *reinterpret_cast<typename Words<words, R::SIZE>::at*>(p) = v;
-        }
-    }
+    of(std::integral_constant<int, 0>());
 }
 
-// a lane's vector: whole, the row's remainder, or nothing (the registers stay as they are)
+// What of a lane's vector is the row's: whole, `tail` values, or nothing
+struct Share {
+    bool full, part;
+    int tail;
+};
+
+// (nothing: the registers stay as they are).  `over`: what follows the row in memory may be read
 template <int DT, int N, bool TAIL>
-__device__ __forceinline__ void load(Raw<DT, N>& r, const char* p, bool full, bool part, int tail)
+__device__ __forceinline__ void load(Raw<DT, N>& r, const char* p, const Share& has, bool over)
 {
-    // (rows without a remainder: lines that no other access of the wave touches, and that nothing reads again)
-    if constexpr (TAIL) {
-        if (full) r.w = *reinterpret_cast<const typename Raw<DT, N>::Whole*>(p);
-        if (part) {
-            load_piece<DT, N, 4>(r, p, tail);
-            load_piece<DT, N, 2>(r, p, tail);
-            load_piece<DT, N, 1>(r, p, tail);
+    typedef Raw<DT, N> R;
+    if constexpr (!TAIL) {
+        // (lines that no other access of the wave touches, and that nothing reads again)
+        if (has.full) r.w = __builtin_nontemporal_load(reinterpret_cast<const typename R::Whole*>(p));
+    } else {
+        if (has.full || (has.part && over)) r.w = *reinterpret_cast<const typename R::Whole*>(p);
+        if (has.part && !over)
+            pieces<N>(has.tail, [&](auto first, auto values) { load_piece<DT, N, first.value, values.value>(r, p); });
+#pragma unroll
+        for (int k = 0; k < R::WORDS; ++k) {
+            const int values = has.tail - k * (4 / R::SIZE);  // of this word
+            const unsigned keep = values <= 0 ? 0u : R::SIZE == 2 && values == 1 ? 0xffffu : ~0u;
+            r.w[k] &= has.part ? keep : ~0u;
         }
-    } else if (full) {
-        r.w = __builtin_nontemporal_load(reinterpret_cast<const typename Raw<DT, N>::Whole*>(p));
     }
 }
 
@@ -145,47 +152,38 @@ __device__ __forceinline__ Raw<DT, N> pack(const float* f)
     return r;
 }
 template <int DT, int N, bool TAIL>
-__device__ __forceinline__ void store(char* p, const float* f, bool full, bool part, int tail)
+__device__ __forceinline__ void store(char* p, const float* f, const Share& has)
 {
-    const Raw<DT, N> r = pack<DT, N>(f);
+    typedef Raw<DT, N> R;
+    const R r = pack<DT, N>(f);
     if constexpr (TAIL) {
-        if (full) *reinterpret_cast<typename Raw<DT, N>::Whole*>(p) = r.w;
-        if (part) {
-            store_piece<DT, N, 4>(p, r, tail);
-            store_piece<DT, N, 2>(p, r, tail);
-            store_piece<DT, N, 1>(p, r, tail);
-        }
-    } else if (full) {
-        __builtin_nontemporal_store(r.w, reinterpret_cast<typename Raw<DT, N>::Whole*>(p));
+        if (has.full) *reinterpret_cast<typename R::Whole*>(p) = r.w;
+        if (has.part)
+            pieces<N>(has.tail, [&](auto first, auto values) { store_piece<DT, N, first.value, values.value>(p, r); });
+    } else if (has.full) {
+        __builtin_nontemporal_store(r.w, reinterpret_cast<typename R::Whole*>(p));
     }
 }
+
 // a vector of a per-column fp32 tensor (`none` where there is no tensor)
 template <int N, bool TAIL>
-__device__ __forceinline__ void load_column(float* f, const float* p, int vector, bool full, bool part, int tail,
-                                            float none)
+__device__ __forceinline__ void load_column(float* f, const float* p, int vector, const Share& has, float none)
 {
 #pragma unroll
-    for (int h = 0; h < N / 4; ++h) {  // (quads: 16 bytes)
+    for (int h = 0; h < N; h += 4) {  // (16 bytes)
         Raw<CAPSCAPS_FP32, 4> r;
         clear(r);
         if (p != nullptr) {
-            const float* q = p + (size_t)vector * N + 4 * h;
-            if (full) r.w = *reinterpret_cast<const typename Raw<CAPSCAPS_FP32, 4>::Whole*>(q);
+            const float* q = p + (size_t)vector * N + h;
+            if (has.full) r.w = *reinterpret_cast<const typename Raw<CAPSCAPS_FP32, 4>::Whole*>(q);
             if constexpr (TAIL) {
-                if (part) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        // the value whose place is 4 h + k
-                        const int place = 4 * h + k, values = N == 8 ? (place < 4 ? 4 : place < 6 ? 2 : 1) : (place < 2 ? 2 : 1);
-                        const int j = piece_offset(values, tail) + place - piece_place<N>(values);
-                        if ((tail & values) && place - piece_place<N>(values) < values)
-                            r.w[k] = __builtin_bit_cast(unsigned, p[(size_t)vector * N + j]);
-                    }
-                }
+                for (int k = 0; k < 4; ++k)
+                    if (has.part && h + k < has.tail) r.w[k] = __builtin_bit_cast(unsigned, q[k]);
             }
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) f[4 * h + k] = p != nullptr ? value<CAPSCAPS_FP32, 4>(r, k) : none;
+        for (int k = 0; k < 4; ++k) f[h + k] = p != nullptr ? value<CAPSCAPS_FP32, 4>(r, k) : none;
     }
 }
 
