@@ -2,7 +2,10 @@
 //
 // Lists of tensors travel in the kernel arguments (nothing is copied to the device before a launch, so calls can be
 // captured and the lists may change from call to call): a launch takes as many tensors as 4 KB of arguments hold,
-// and a workgroup finds its tensor and its share of it from the running number of shares.
+// and a workgroup finds its tensor and its share of it from the running number of shares (one load and a vote).
+//
+// Everything here is bounded by memory.  A lane has four neighbouring values of a tensor, so that every access of a wave is
+// one contiguous piece (1 KB of fp32), at any address, and a workgroup takes its share in one pass.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -19,6 +22,68 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int STATE_BLOCK = 256;  // values that share an exponent byte
+
+typedef unsigned uint4v __attribute__((ext_vector_type(4)));
+typedef unsigned uint2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint4v uint4_a4 __attribute__((aligned(4)));
+typedef uint2v uint2_a2 __attribute__((aligned(2)));
+typedef uint4v uint4_a2 __attribute__((aligned(2)));
+typedef unsigned uint_a1 __attribute__((aligned(1)));
+typedef uint2v uint2_a1 __attribute__((aligned(1)));
+
+// The tensor whose shares hold number `share`: the last one that begins at or before it (`first` rises, empty tensors
+// begin where the next one does)
+__device__ __forceinline__ int tensor_of(const int* first, int count, int share)
+{
+    int k = -1;
+    for (int at = 0; at < count; at += 64) {
+        const int i = at + (threadIdx.x & 63);
+        k += __popcll(__ballot(i < count && first[i] <= share));
+    }
+    return __builtin_amdgcn_readfirstlane(k);
+}
+
+// Four neighbouring values from element i on, of which `n` (1 .. 4) are the tensor's; the others are zeros
+__device__ __forceinline__ float4v load4(const void* p, long long i, int n, int dtype)
+{
+    if (n == 4) {
+        if (dtype == CAPSCAPS_FP32) {
+            const uint4v w = __builtin_nontemporal_load(reinterpret_cast<const uint4_a4*>(static_cast<const float*>(p) + i));
+            return __builtin_bit_cast(float4v, w);
+        }
+        const uint2v w =
+            __builtin_nontemporal_load(reinterpret_cast<const uint2_a2*>(static_cast<const unsigned short*>(p) + i));
+        if (dtype == CAPSCAPS_BF16)
+            return float4v{__builtin_bit_cast(float, w.x << 16), __builtin_bit_cast(float, w.x & 0xffff0000u),
+                           __builtin_bit_cast(float, w.y << 16), __builtin_bit_cast(float, w.y & 0xffff0000u)};
+        typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+        return __builtin_convertvector(__builtin_bit_cast(half4v, w), float4v);
+    }
+    float4v v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < n) v[k] = load_element(p, i + k, dtype);
+    return v;
+}
+__device__ __forceinline__ void store4(void* p, long long i, const float4v& v, int n, int dtype)
+{
+    if (n == 4) {
+        if (dtype == CAPSCAPS_FP32) {
+            __builtin_nontemporal_store(__builtin_bit_cast(uint4v, v), reinterpret_cast<uint4_a4*>(static_cast<float*>(p) + i));
+            return;
+        }
+        typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+        typedef __bf16 bf16x4v __attribute__((ext_vector_type(4)));
+        const uint2v w = dtype == CAPSCAPS_BF16 ? __builtin_bit_cast(uint2v, __builtin_convertvector(v, bf16x4v))
+                                                : __builtin_bit_cast(uint2v, __builtin_convertvector(v, half4v));
+        __builtin_nontemporal_store(w, reinterpret_cast<uint2_a2*>(static_cast<unsigned short*>(p) + i));
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < n) store_element(p, i + k, v[k], dtype);
+}
 
 bool misaligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
 
@@ -51,14 +116,25 @@ __global__ void __launch_bounds__(THREADS) grad_norm_kernel(NormList L, double* 
 {
     __shared__ double lds[THREADS / 64];
     double s = 0.0;
-    for (int k = blockIdx.x; k < L.first[L.count]; k += gridDim.x) {
-        int t = 0;
-        while (L.first[t + 1] <= k) ++t;
-        const long long i0 = (long long)(k - L.first[t]) * NORM_SHARE;
-        const long long i1 = i0 + NORM_SHARE < L.n[t] ? i0 + NORM_SHARE : L.n[t];
-        for (long long i = i0 + threadIdx.x; i < i1; i += THREADS) {
-            const double g = load_element(L.grad[t], i, L.dtype[t]);
-            s += g * g;
+    const int shares = L.first[L.count];
+    for (int share = blockIdx.x; share < shares; share += gridDim.x) {
+        const int t = tensor_of(L.first, L.count, share);
+        const void* grad = L.grad[t];
+        const int dtype = L.dtype[t];
+        const long long base = (long long)(share - L.first[t]) * NORM_SHARE, left = L.n[t] - base;
+        constexpr int STEP = 4 * THREADS, UNROLL = 4;
+        for (int i = 4 * threadIdx.x; i < NORM_SHARE && i < left; i += UNROLL * STEP) {
+            float4v g[UNROLL];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const long long rest = left - (i + u * STEP);
+                g[u] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+                if (rest > 0) g[u] = load4(grad, base + i + u * STEP, rest < 4 ? (int)rest : 4, dtype);
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s += (double)g[u][k] * (double)g[u][k];
         }
     }
     s = block_sum(s, lds);
@@ -86,7 +162,8 @@ __global__ void __launch_bounds__(1024)
 
 // ------------------------------------------------------------------------------------ AdamW
 constexpr int ADAM_TENSORS = 44;
-constexpr int ADAM_SHARE = 2048;  // values that a workgroup updates
+constexpr int UNITS = 2;                             // fours of values that a lane updates
+constexpr int ADAM_SHARE = UNITS * 4 * THREADS;  // values that a workgroup updates
 
 struct AdamTensor {
     float* param;
@@ -197,70 +274,133 @@ __device__ __forceinline__ Moments adam_value(const AdamHyper& H, const AdamStep
     return {p, m, v};
 }
 
-__device__ __forceinline__ unsigned block_max(unsigned v, unsigned* lds)
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp_max(unsigned v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const unsigned w = (unsigned)__shfl_xor((int)v, o);
-        v = v > w ? v : w;
-    }
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-    for (int w = 1; w < THREADS / 64; ++w) v = v > lds[w] ? v : lds[w];
-    __syncthreads();
-    return v;
+    const unsigned w = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+    return v > w ? v : w;
+}
+// largest over the wave, in a scalar register
+__device__ __forceinline__ unsigned wave_max(unsigned v)
+{
+    v = dpp_max<0xB1>(v);   // quad_perm 1 0 3 2
+    v = dpp_max<0x4E>(v);   // quad_perm 2 3 0 1
+    v = dpp_max<0x141>(v);  // row_half_mirror
+    v = dpp_max<0x140>(v);  // row_mirror: the largest of 16 lanes in each of them
+    const unsigned a = (unsigned)__builtin_amdgcn_readlane((int)v, 0), b = (unsigned)__builtin_amdgcn_readlane((int)v, 16);
+    const unsigned c = (unsigned)__builtin_amdgcn_readlane((int)v, 32), d = (unsigned)__builtin_amdgcn_readlane((int)v, 48);
+    const unsigned ab = a > b ? a : b, cd = c > d ? c : d;
+    return ab > cd ? ab : cd;
 }
 
+// Four codes, a byte each; `n` of them are the tensor's
+__device__ __forceinline__ unsigned load_codes(const unsigned char* p, long long i, int n)
+{
+    if (n == 4) return __builtin_nontemporal_load(reinterpret_cast<const uint_a1*>(p + i));
+    unsigned c = 0;
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < n) c |= (unsigned)p[i + k] << (8 * k);
+    return c;
+}
+__device__ __forceinline__ void store_codes(unsigned char* p, long long i, unsigned c, int n)
+{
+    if (n == 4) {
+        __builtin_nontemporal_store(c, reinterpret_cast<uint_a1*>(p + i));
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < n) p[i + k] = (unsigned char)(c >> (8 * k));
+}
+
+// A share of a tensor: each wave 256 neighbouring values at a time, which in 8 bits are a block of the state, so that the
+// largest magnitudes are the wave's and nothing waits for other waves
 template <int BITS>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(AdamList L, AdamHyper H)
 {
-    __shared__ unsigned lds[THREADS / 64];
-    int k = 0;
-    while (L.first[k + 1] <= (int)blockIdx.x) ++k;
+    static_assert(STATE_BLOCK == 4 * 64, "a wave's values share an exponent");
+    const int k = tensor_of(L.first, L.count, blockIdx.x);
     const AdamTensor& T = L.t[k];
     const AdamStep S = adam_step(H);
     if (S.skip) return;
     const float keep = 1.0f - H.lr * T.weight_decay;
     const unsigned key = mix(H.seed + 0x9E3779B1u * (unsigned)(L.index0 + k) + 0x6A09E667u * mix((unsigned)S.t));
     const long long base = (long long)((int)blockIdx.x - L.first[k]) * ADAM_SHARE;
-    for (int j = 0; j < ADAM_SHARE / THREADS; ++j) {
-        const long long i = base + j * THREADS + threadIdx.x, block = i / STATE_BLOCK;
-        if (base + j * THREADS >= T.n) break;
-        const bool in = i < T.n;
-        Moments r{0.0f, 0.0f, 0.0f};
-        if (in) {
-            const float p = T.param[i], g = load_element(T.grad, i, T.grad_dtype);
-            float m, v;
+    const long long i0 = base + (threadIdx.x >> 6) * STATE_BLOCK;  // this wave's values: from here, and each 4 * THREADS on
+    const int lane4 = 4 * (threadIdx.x & 63);
+    float4v p[UNITS], g[UNITS], m[UNITS], v[UNITS];
+    unsigned cm[UNITS], cv[UNITS], em[UNITS], ev[UNITS];
+    int n[UNITS];  // of the four, the tensor's
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        const long long first = i0 + u * 4 * THREADS, i = first + lane4, rest = T.n - i;
+        n[u] = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
+        p[u] = g[u] = m[u] = v[u] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        cm[u] = cv[u] = em[u] = ev[u] = 0;
+        if (n[u] == 0) continue;
+        p[u] = load4(T.param, i, n[u], CAPSCAPS_FP32);
+        g[u] = load4(T.grad, i, n[u], T.grad_dtype);
+        if constexpr (BITS == 8) {
+            cm[u] = load_codes(static_cast<const unsigned char*>(T.m), i, n[u]);
+            cv[u] = load_codes(static_cast<const unsigned char*>(T.v), i, n[u]);
+            em[u] = T.m_exp[first / STATE_BLOCK];
+            ev[u] = T.v_exp[first / STATE_BLOCK];
+        } else {
+            m[u] = load4(T.m, i, n[u], CAPSCAPS_FP32);
+            v[u] = load4(T.v, i, n[u], CAPSCAPS_FP32);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        const long long first = i0 + u * 4 * THREADS, i = first + lane4;
+        if (first >= T.n) break;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
             if constexpr (BITS == 8) {
-                m = decode_m(static_cast<const unsigned char*>(T.m)[i], T.m_exp[block]);
-                v = decode_magnitude(static_cast<const unsigned char*>(T.v)[i], T.v_exp[block], 31);
-            } else {
-                m = static_cast<const float*>(T.m)[i];
-                v = static_cast<const float*>(T.v)[i];
+                m[u][j] = decode_m((cm[u] >> (8 * j)) & 255u, em[u]);
+                v[u][j] = decode_magnitude((cv[u] >> (8 * j)) & 255u, ev[u], 31);
             }
-            r = adam_value(H, S, keep, p, g, m, v);
-            T.param[i] = r.p;
-            if (T.copy != nullptr) store_element(T.copy, i, r.p, T.copy_dtype);
+            const Moments r = adam_value(H, S, keep, p[u][j], g[u][j], m[u][j], v[u][j]);
+            p[u][j] = r.p;
+            m[u][j] = r.m;
+            v[u][j] = r.v;
+        }
+        if (n[u] > 0) {
+            store4(T.param, i, p[u], n[u], CAPSCAPS_FP32);
+            if (T.copy != nullptr) store4(T.copy, i, p[u], n[u], T.copy_dtype);
         }
         if constexpr (BITS == 8) {
-            static_assert(THREADS == STATE_BLOCK, "a value per thread");
-            const unsigned top_m = block_max(__builtin_bit_cast(unsigned, r.m) & 0x7fffffffu, lds);
-            const unsigned top_v = block_max(__builtin_bit_cast(unsigned, r.v) & 0x7fffffffu, lds);
-            const int em = shared_exponent(top_m, 15), ev = shared_exponent(top_v, 31);
-            // (a third factor for the high half of an index that passes 32 bits)
-            const unsigned x = mix((unsigned)i * 0x9E3779B1u + (unsigned)(i >> 32) * 0xBB67AE85u + key);
-            if (in) {
-                static_cast<unsigned char*>(T.m)[i] = (unsigned char)encode_m(r.m, x & 0xffffu, em);
-                static_cast<unsigned char*>(T.v)[i] = (unsigned char)encode_v(r.v, x >> 16, ev);
+            unsigned top_m = 0, top_v = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // (values past the tensor's end count for nothing)
+                const float mj = m[u][j], vj = v[u][j];  // (a bit cast of a vector's element takes the first one)
+                const unsigned am = j < n[u] ? __builtin_bit_cast(unsigned, mj) & 0x7fffffffu : 0u;
+                const unsigned av = j < n[u] ? __builtin_bit_cast(unsigned, vj) & 0x7fffffffu : 0u;
+                top_m = top_m > am ? top_m : am;
+                top_v = top_v > av ? top_v : av;
             }
-            if (threadIdx.x == 0) {
-                T.m_exp[block] = (unsigned char)em;
-                T.v_exp[block] = (unsigned char)ev;
+            const int new_em = shared_exponent(wave_max(top_m), 15), new_ev = shared_exponent(wave_max(top_v), 31);
+            unsigned new_m = 0, new_v = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // (a third factor for the high half of an index that passes 32 bits)
+                const unsigned x = mix((unsigned)(i + j) * 0x9E3779B1u + (unsigned)((i + j) >> 32) * 0xBB67AE85u + key);
+                new_m |= encode_m(m[u][j], x & 0xffffu, new_em) << (8 * j);
+                new_v |= encode_v(v[u][j], x >> 16, new_ev) << (8 * j);
             }
-        } else if (in) {
-            static_cast<float*>(T.m)[i] = r.m;
-            static_cast<float*>(T.v)[i] = r.v;
+            if (n[u] > 0) {
+                store_codes(static_cast<unsigned char*>(T.m), i, new_m, n[u]);
+                store_codes(static_cast<unsigned char*>(T.v), i, new_v, n[u]);
+            }
+            if (lane4 == 0) {
+                T.m_exp[first / STATE_BLOCK] = (unsigned char)new_em;
+                T.v_exp[first / STATE_BLOCK] = (unsigned char)new_ev;
+            }
+        } else if (n[u] > 0) {
+            store4(T.m, i, m[u], n[u], CAPSCAPS_FP32);
+            store4(T.v, i, v[u], n[u], CAPSCAPS_FP32);
         }
     }
 }
@@ -273,16 +413,40 @@ struct ValuesList {
     int count;
 };
 
+// Eight codes to 16 bytes of bfloat16 (the lower 16 bits of every value are zero)
+template <bool M>
+__device__ __forceinline__ void values8(const unsigned char* codes, unsigned exponent, unsigned short* out, long long i,
+                                        int n)
+{
+    auto bits = [&](unsigned c) {
+        const float v = M ? decode_m(c, exponent) : decode_magnitude(c, exponent, 31);
+        return __builtin_bit_cast(unsigned, v) >> 16;
+    };
+    if (n == 8) {
+        const uint2v c = __builtin_nontemporal_load(reinterpret_cast<const uint2_a1*>(codes + i));
+        uint4v w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned pair = c[k / 2] >> (16 * (k & 1));
+            w[k] = bits(pair & 255u) | bits((pair >> 8) & 255u) << 16;
+        }
+        __builtin_nontemporal_store(w, reinterpret_cast<uint4_a2*>(out + i));
+        return;
+    }
+    for (int k = 0; k < n; ++k) out[i + k] = (unsigned short)bits(codes[i + k]);
+}
+
 __global__ void __launch_bounds__(THREADS) state_values_kernel(ValuesList L)
 {
-    int k = 0;
-    while (L.first[k + 1] <= (int)blockIdx.x) ++k;
+    const int k = tensor_of(L.first, L.count, blockIdx.x);
     const long long base = (long long)((int)blockIdx.x - L.first[k]) * ADAM_SHARE;
-    for (int j = 0; j < ADAM_SHARE / THREADS; ++j) {
-        const long long i = base + j * THREADS + threadIdx.x, block = i / STATE_BLOCK;
-        if (i >= L.n[k]) break;
-        store_element(L.m_out[k], i, decode_m(L.m[k][i], L.m_exp[k][block]), CAPSCAPS_BF16);
-        store_element(L.v_out[k], i, decode_magnitude(L.v[k][i], L.v_exp[k][block], 31), CAPSCAPS_BF16);
+#pragma unroll
+    for (int u = 0; u < ADAM_SHARE; u += 8 * THREADS) {
+        const long long i = base + u + 8 * threadIdx.x, rest = L.n[k] - i;
+        if (rest <= 0) return;
+        const int n = rest < 8 ? (int)rest : 8;
+        values8<true>(L.m[k], L.m_exp[k][i / STATE_BLOCK], L.m_out[k], i, n);
+        values8<false>(L.v[k], L.v_exp[k][i / STATE_BLOCK], L.v_out[k], i, n);
     }
 }
 
