@@ -162,8 +162,11 @@ __global__ void __launch_bounds__(1024)
 
 // ------------------------------------------------------------------------------------ AdamW
 constexpr int ADAM_TENSORS = 44;
-constexpr int UNITS = 2;                             // fours of values that a lane updates
-constexpr int ADAM_SHARE = UNITS * 4 * THREADS;  // values that a workgroup updates
+// Fours of values that a lane updates, and a workgroup's share.  113M values with fp16 copies, us: 32-bit moments 618, 635 and
+// 616 with one, two and four of them; 8-bit ones 378 with two and with four, and 7M values 32 and 34
+constexpr int units_of(int bits) { return bits == 8 ? 2 : 4; }
+constexpr int share_of(int bits) { return units_of(bits) * 4 * THREADS; }
+constexpr int VALUES_SHARE = 16 * THREADS;  // values that a workgroup decodes
 
 struct AdamTensor {
     float* param;
@@ -320,13 +323,14 @@ template <int BITS>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(AdamList L, AdamHyper H)
 {
     static_assert(STATE_BLOCK == 4 * 64, "a wave's values share an exponent");
+    constexpr int UNITS = units_of(BITS);
     const int k = tensor_of(L.first, L.count, blockIdx.x);
     const AdamTensor& T = L.t[k];
     const AdamStep S = adam_step(H);
     if (S.skip) return;
     const float keep = 1.0f - H.lr * T.weight_decay;
     const unsigned key = mix(H.seed + 0x9E3779B1u * (unsigned)(L.index0 + k) + 0x6A09E667u * mix((unsigned)S.t));
-    const long long base = (long long)((int)blockIdx.x - L.first[k]) * ADAM_SHARE;
+    const long long base = (long long)((int)blockIdx.x - L.first[k]) * share_of(BITS);
     const long long i0 = base + (threadIdx.x >> 6) * STATE_BLOCK;  // this wave's values: from here, and each 4 * THREADS on
     const int lane4 = 4 * (threadIdx.x & 63);
     float4v p[UNITS], g[UNITS], m[UNITS], v[UNITS];
@@ -415,38 +419,52 @@ struct ValuesList {
 
 // Eight codes to 16 bytes of bfloat16 (the lower 16 bits of every value are zero)
 template <bool M>
-__device__ __forceinline__ void values8(const unsigned char* codes, unsigned exponent, unsigned short* out, long long i,
-                                        int n)
+__device__ __forceinline__ void decode8(uint2v codes, unsigned exponent, unsigned short* out)
 {
     auto bits = [&](unsigned c) {
         const float v = M ? decode_m(c, exponent) : decode_magnitude(c, exponent, 31);
         return __builtin_bit_cast(unsigned, v) >> 16;
     };
-    if (n == 8) {
-        const uint2v c = __builtin_nontemporal_load(reinterpret_cast<const uint2_a1*>(codes + i));
-        uint4v w;
+    uint4v w;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const unsigned pair = c[k / 2] >> (16 * (k & 1));
-            w[k] = bits(pair & 255u) | bits((pair >> 8) & 255u) << 16;
-        }
-        __builtin_nontemporal_store(w, reinterpret_cast<uint4_a2*>(out + i));
-        return;
+    for (int k = 0; k < 4; ++k) {
+        const unsigned pair = codes[k / 2] >> (16 * (k & 1));
+        w[k] = bits(pair & 255u) | bits((pair >> 8) & 255u) << 16;
     }
-    for (int k = 0; k < n; ++k) out[i + k] = (unsigned short)bits(codes[i + k]);
+    __builtin_nontemporal_store(w, reinterpret_cast<uint4_a2*>(out));
 }
 
 __global__ void __launch_bounds__(THREADS) state_values_kernel(ValuesList L)
 {
     const int k = tensor_of(L.first, L.count, blockIdx.x);
-    const long long base = (long long)((int)blockIdx.x - L.first[k]) * ADAM_SHARE;
+    const long long base = (long long)((int)blockIdx.x - L.first[k]) * VALUES_SHARE;
+    constexpr int UNITS = VALUES_SHARE / (8 * THREADS);
+    const long long n = L.n[k];
+    const unsigned char *m = L.m[k], *v = L.v[k], *m_exp = L.m_exp[k], *v_exp = L.v_exp[k];
+    unsigned short *m_out = L.m_out[k], *v_out = L.v_out[k];
+    uint2v cm[UNITS], cv[UNITS];
+    unsigned em[UNITS], ev[UNITS];
 #pragma unroll
-    for (int u = 0; u < ADAM_SHARE; u += 8 * THREADS) {
-        const long long i = base + u + 8 * threadIdx.x, rest = L.n[k] - i;
-        if (rest <= 0) return;
-        const int n = rest < 8 ? (int)rest : 8;
-        values8<true>(L.m[k], L.m_exp[k][i / STATE_BLOCK], L.m_out[k], i, n);
-        values8<false>(L.v[k], L.v_exp[k][i / STATE_BLOCK], L.v_out[k], i, n);
+    for (int u = 0; u < UNITS; ++u) {
+        const long long i = base + 8 * (u * THREADS + threadIdx.x);
+        if (i + 8 > n) continue;
+        cm[u] = __builtin_nontemporal_load(reinterpret_cast<const uint2_a1*>(m + i));
+        cv[u] = __builtin_nontemporal_load(reinterpret_cast<const uint2_a1*>(v + i));
+        em[u] = m_exp[i / STATE_BLOCK];
+        ev[u] = v_exp[i / STATE_BLOCK];
+    }
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+        const long long i = base + 8 * (u * THREADS + threadIdx.x);
+        if (i + 8 <= n) {
+            decode8<true>(cm[u], em[u], m_out + i);
+            decode8<false>(cv[u], ev[u], v_out + i);
+        } else {
+            for (long long j = i; j < n; ++j) {
+                store_element(m_out, j, decode_m(m[j], m_exp[j / STATE_BLOCK]), CAPSCAPS_BF16);
+                store_element(v_out, j, decode_magnitude(v[j], v_exp[j / STATE_BLOCK], 31), CAPSCAPS_BF16);
+            }
+        }
     }
 }
 
@@ -532,7 +550,7 @@ int capscaps_adamw_step(const capscaps_adamw_tensor* tensors, int count, int sta
             misaligned(t.grad, element_bytes(t.grad_dtype)) || misaligned(t.copy, 2))
             return CAPSCAPS_EINVAL;
         if (state_bits == 8 ? !t.m_exp || !t.v_exp : misaligned(t.m, 4) || misaligned(t.v, 4)) return CAPSCAPS_EINVAL;
-        if (t.n > (0x7fffffffLL / ADAM_TENSORS - 1) * ADAM_SHARE) return CAPSCAPS_EUNSUPPORTED;
+        if (t.n > (0x7fffffffLL / ADAM_TENSORS - 1) * share_of(state_bits)) return CAPSCAPS_EUNSUPPORTED;
     }
     AdamHyper H;
     H.lr = (float)lr;
@@ -559,7 +577,7 @@ int capscaps_adamw_step(const capscaps_adamw_tensor* tensors, int count, int sta
             const capscaps_adamw_tensor& t = tensors[k];
             L.t[L.count] = {t.param, t.grad, t.m, t.v, t.m_exp, t.v_exp, t.copy, t.n, t.weight_decay,
                             (unsigned short)t.grad_dtype, (unsigned short)t.copy_dtype};
-            add_shares(L.first, L.count, t.n, ADAM_SHARE);
+            add_shares(L.first, L.count, t.n, share_of(state_bits));
             ++L.count;
         }
         if (L.first[L.count] == 0) continue;
@@ -586,7 +604,7 @@ int capscaps_adamw_state_values(const capscaps_adamw_tensor* tensors, int count,
         if (!t.m || !t.v || !t.m_exp || !t.v_exp || !m_out[k] || !v_out[k] || misaligned(m_out[k], 2) ||
             misaligned(v_out[k], 2))
             return CAPSCAPS_EINVAL;
-        if (t.n > (0x7fffffffLL / ADAM_TENSORS - 1) * ADAM_SHARE) return CAPSCAPS_EUNSUPPORTED;
+        if (t.n > (0x7fffffffLL / ADAM_TENSORS - 1) * VALUES_SHARE) return CAPSCAPS_EUNSUPPORTED;
     }
     const hipStream_t st = static_cast<hipStream_t>(stream);
     for (int k = 0; k < count;) {
@@ -604,7 +622,7 @@ int capscaps_adamw_state_values(const capscaps_adamw_tensor* tensors, int count,
             L.m_out[j] = static_cast<unsigned short*>(m_out[k]);
             L.v_out[j] = static_cast<unsigned short*>(v_out[k]);
             L.n[j] = t.n;
-            add_shares(L.first, j, t.n, ADAM_SHARE);
+            add_shares(L.first, j, t.n, VALUES_SHARE);
         }
         if (L.count == 0) break;
         state_values_kernel<<<dim3(L.first[L.count]), dim3(THREADS), 0, st>>>(L);
