@@ -305,7 +305,7 @@ int capscaps_scheme2_fwd(const void* input, const void* kernel, void* out, const
 #define CAPSCAPS_ACT_SILU 2    /* g / (1 + exp(-g)) */
 typedef struct capscaps_block {
     long long rows;
-    int width;
+    int width; /* up to 2^30 */
     int dtype, stream_dtype, branch_dtype;
     int post_norm;      /* 0 or 1 */
     int gate, gate_act; /* CAPSCAPS_GATE_*, CAPSCAPS_ACT_* */

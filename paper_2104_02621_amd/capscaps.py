@@ -527,7 +527,8 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
     residual stream, and branch, a layer's output, are each float32 or `dtype`.  Weights are float32 of a row's
     size; the gate is such a vector, or a tensor of x's shape and `dtype`.  Without a branch only h is computed.
     Returns BlockNorm(y, h, rstd_pre, rstd_post); the statistics only with `save`, for block_norm_bwd.  `y` and `h`
-    may be given to write to; y may be x.  Enqueues on torch's current stream; does not synchronise."""
+    may be given to write to; y may be x.  Enqueues on torch's current stream; does not synchronise (tensors made on another
+    stream have to be ready and, if they are freed early, recorded there, as for torch's own operations)."""
     import torch
     dtype = x.dtype if dtype is None else dtype
     block, bp, bs, gp, gs = _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scale,
@@ -538,7 +539,7 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
         if y is not None:
             raise ValueError("without a branch there is no y")
     elif y is None and want_y:
-        y = torch.empty(shape, dtype=x.dtype, device=device)
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
     if h is None and want_h:
         h = torch.empty(shape, dtype=dtype, device=device)
     if y is not None and y.dtype != x.dtype or h is not None and h.dtype != dtype:
@@ -654,11 +655,11 @@ class AdamW:
     a list of 16-bit tensors (None where there is none) of the parameters' sizes; each step writes the rounded
     parameters there, for the layers to read.  `state_bits`: 32 (float32 moments) or 8 (a byte for each, and a
     byte for each 256 values that share an exponent; rounded at random by a hash of `seed`, the step and the
-    position).  `state`: moments to go on from, (m, v) or (m, v, m_exp, v_exp), lists of tensors in that format; kept, not
-    copied."""
+    position).  `state`: moments to go on from, (m, v) or (m, v, m_exp, v_exp), lists of tensors in that format (those
+    of another AdamW, saved); kept, not copied; `steps`: the steps they have seen."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, state_bits=32, copies=None,
-                 seed=0, state=None):
+                 seed=0, state=None, steps=0):
         import torch
         if state_bits not in (32, 8):
             raise ValueError("state_bits is 32 or 8")
@@ -667,7 +668,7 @@ class AdamW:
             raise ValueError("AdamW needs parameters")
         count, eight = len(self.params), state_bits == 8
         self.lr, self.betas, self.eps, self.state_bits, self.seed = lr, betas, eps, state_bits, seed
-        self.steps = 0
+        self.steps = steps
         for p in self.params:
             if p.dtype != torch.float32:
                 raise ValueError("parameters are float32")

@@ -669,7 +669,7 @@ int check_block(const capscaps_block* B)
     if ((unsigned)B->post_norm > 1 || (unsigned)B->gate > 2 || (unsigned)B->gate_act > 2) return CAPSCAPS_EINVAL;
     if (!isfinite(B->residual_scale) || !isfinite(B->branch_scale)) return CAPSCAPS_EINVAL;
     if (!(B->eps >= FLT_MIN) || !isfinite(B->eps)) return CAPSCAPS_EINVAL;  // (a normal number, for v_rsq_f32)
-    if ((long double)B->rows * B->width > 1e17L) return CAPSCAPS_EINVAL;
+    if (B->width > (1 << 30) || (long double)B->rows * B->width > 1e17L) return CAPSCAPS_EINVAL;
     return CAPSCAPS_OK;
 }
 
@@ -696,7 +696,8 @@ RowPlan row_plan(const capscaps_block& B, int n, bool forward, bool apart)
     if (P.group > P.threads || apart) P.threads = P.group;
     P.per_block = P.threads / P.group;
     const long long blocks = (B.rows + P.per_block - 1) / P.per_block;
-    const long long most = apart ? CUS : !in_step ? 1LL << 30 : (long long)CUS * (forward ? 2048 : 1024) / P.threads;
+    // (a launch has less than 2^32 threads)
+    const long long most = apart ? CUS : !in_step ? 1LL << 23 : (long long)CUS * (forward ? 2048 : 1024) / P.threads;
     P.blocks = (unsigned)(blocks < most ? blocks : most);
     P.turns = P.blocks < blocks;
     P.full = B.width / n;
@@ -814,10 +815,12 @@ int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fw
     if (A.y == A.x && A.y_stride != A.x_stride) return CAPSCAPS_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool apart = rows_apart({A.x_stride, A.branch_stride, A.gate_stride, A.y_stride, A.h_stride});
-    const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), true, apart);
-    if (B.width > WIDEST)
+    if (B.width > WIDEST) {
         block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A);
-    else if (B.dtype == CAPSCAPS_FP32)
+        return status_from_hip(hipGetLastError());
+    }
+    const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), true, apart);
+    if (B.dtype == CAPSCAPS_FP32)
         launch_fwd<CAPSCAPS_FP32>(B, A, P, st);
     else if (B.dtype == CAPSCAPS_BF16)
         launch_fwd<CAPSCAPS_BF16>(B, A, P, st);

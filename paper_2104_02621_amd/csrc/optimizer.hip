@@ -468,11 +468,12 @@ __global__ void __launch_bounds__(THREADS) state_values_kernel(ValuesList L)
     }
 }
 
-// adds the shares of a tensor of n values; false: more than a launch can count
+// Adds the shares of a tensor of n values; false: more workgroups of 256 than a launch takes (less than 2^32 threads)
+constexpr long long MOST_SHARES = (1LL << 24) - 1;
 bool add_shares(int* first, int count, long long n, int share)
 {
     const long long total = first[count] + (n + share - 1) / share;
-    if (total > 0x7fffffffLL) return false;
+    if (total > MOST_SHARES) return false;
     first[count + 1] = (int)total;
     return true;
 }
@@ -490,12 +491,13 @@ int capscaps_grad_norm(const capscaps_grad_tensor* grads, int count, float grad_
     if (count < 0 || (count > 0 && grads == nullptr) || control == nullptr || misaligned(control, 16))
         return CAPSCAPS_EINVAL;
     if (!isfinite(grad_scale) || isnan(max_norm)) return CAPSCAPS_EINVAL;
-    long long used = 0;
+    long long used = 0, shares = 0;
     for (int k = 0; k < count; ++k) {
         const capscaps_grad_tensor& g = grads[k];
         if (g.n < 0 || !known_dtype(g.dtype)) return CAPSCAPS_EINVAL;
         if (g.n > 0 && (g.grad == nullptr || misaligned(g.grad, element_bytes(g.dtype)))) return CAPSCAPS_EINVAL;
-        if (g.n > (0x7fffffffLL / NORM_TENSORS - 1) * NORM_SHARE) return CAPSCAPS_EUNSUPPORTED;
+        shares += g.n / NORM_SHARE + 1;
+        if (shares > MOST_SHARES) return CAPSCAPS_EUNSUPPORTED;  // (so that every launch's can be counted)
         used += g.n > 0;
     }
     if (workspace == nullptr || workspace_bytes < CAPSCAPS_GRAD_NORM_WORKSPACE_BYTES) return CAPSCAPS_EWORKSPACE;
@@ -512,10 +514,10 @@ int capscaps_grad_norm(const capscaps_grad_tensor* grads, int count, float grad_
         L.first[0] = 0;
         for (; k < count && L.count < NORM_TENSORS; ++k) {
             if (grads[k].n == 0) continue;
+            add_shares(L.first, L.count, grads[k].n, NORM_SHARE);
             L.grad[L.count] = grads[k].grad;
             L.n[L.count] = grads[k].n;
             L.dtype[L.count] = (unsigned char)grads[k].dtype;
-            add_shares(L.first, L.count, grads[k].n, NORM_SHARE);
             ++L.count;
         }
         if (L.count == 0) break;
@@ -550,7 +552,7 @@ int capscaps_adamw_step(const capscaps_adamw_tensor* tensors, int count, int sta
             misaligned(t.grad, element_bytes(t.grad_dtype)) || misaligned(t.copy, 2))
             return CAPSCAPS_EINVAL;
         if (state_bits == 8 ? !t.m_exp || !t.v_exp : misaligned(t.m, 4) || misaligned(t.v, 4)) return CAPSCAPS_EINVAL;
-        if (t.n > (0x7fffffffLL / ADAM_TENSORS - 1) * share_of(state_bits)) return CAPSCAPS_EUNSUPPORTED;
+        if (t.n > MOST_SHARES * share_of(state_bits)) return CAPSCAPS_EUNSUPPORTED;
     }
     AdamHyper H;
     H.lr = (float)lr;
@@ -575,9 +577,9 @@ int capscaps_adamw_step(const capscaps_adamw_tensor* tensors, int count, int sta
         // (empty tensors take a place, so that t[j] is the caller's tensor index0 + j)
         for (; k < count && L.count < ADAM_TENSORS; ++k) {
             const capscaps_adamw_tensor& t = tensors[k];
+            if (!add_shares(L.first, L.count, t.n, share_of(state_bits))) break;  // (the next launch's)
             L.t[L.count] = {t.param, t.grad, t.m, t.v, t.m_exp, t.v_exp, t.copy, t.n, t.weight_decay,
                             (unsigned short)t.grad_dtype, (unsigned short)t.copy_dtype};
-            add_shares(L.first, L.count, t.n, share_of(state_bits));
             ++L.count;
         }
         if (L.first[L.count] == 0) continue;
@@ -604,7 +606,7 @@ int capscaps_adamw_state_values(const capscaps_adamw_tensor* tensors, int count,
         if (!t.m || !t.v || !t.m_exp || !t.v_exp || !m_out[k] || !v_out[k] || misaligned(m_out[k], 2) ||
             misaligned(v_out[k], 2))
             return CAPSCAPS_EINVAL;
-        if (t.n > (0x7fffffffLL / ADAM_TENSORS - 1) * VALUES_SHARE) return CAPSCAPS_EUNSUPPORTED;
+        if (t.n > MOST_SHARES * VALUES_SHARE) return CAPSCAPS_EUNSUPPORTED;
     }
     const hipStream_t st = static_cast<hipStream_t>(stream);
     for (int k = 0; k < count;) {
@@ -614,7 +616,9 @@ int capscaps_adamw_state_values(const capscaps_adamw_tensor* tensors, int count,
         for (; k < count && L.count < ADAM_TENSORS; ++k) {
             const capscaps_adamw_tensor& t = tensors[k];
             if (t.n == 0) continue;
-            const int j = L.count++;
+            const int j = L.count;
+            if (!add_shares(L.first, j, t.n, VALUES_SHARE)) break;  // (the next launch's)
+            ++L.count;
             L.m[j] = static_cast<const unsigned char*>(t.m);
             L.v[j] = static_cast<const unsigned char*>(t.v);
             L.m_exp[j] = t.m_exp;
@@ -622,7 +626,6 @@ int capscaps_adamw_state_values(const capscaps_adamw_tensor* tensors, int count,
             L.m_out[j] = static_cast<unsigned short*>(m_out[k]);
             L.v_out[j] = static_cast<unsigned short*>(v_out[k]);
             L.n[j] = t.n;
-            add_shares(L.first, j, t.n, VALUES_SHARE);
         }
         if (L.count == 0) break;
         state_values_kernel<<<dim3(L.first[L.count]), dim3(THREADS), 0, st>>>(L);

@@ -41,7 +41,7 @@ def bwd(**over):
 BAD_BLOCKS = [dict(rows=0), dict(rows=-1), dict(width=0), dict(dtype=3), dict(dtype=cc.FP16), dict(stream_dtype=cc.FP16),
               dict(branch_dtype=7), dict(post_norm=2), dict(gate=3), dict(gate=-1), dict(gate_act=3), dict(eps=0.0),
               dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(residual_scale=NAN), dict(branch_scale=INF),
-              dict(rows=1 << 62), dict(gate=cc.GATE_NONE)]
+              dict(rows=1 << 62), dict(width=(1 << 30) + 1), dict(gate=cc.GATE_NONE)]
 
 
 @pytest.mark.parametrize("over", BAD_BLOCKS, ids=str)
@@ -108,6 +108,8 @@ def test_gradient_norm_workspace_is_checked():
     assert cc.capscaps_grad_norm(grads((FAKE, 5, 0)), 1, 1.0, 1.0, FAKE, None, 0) == cc.EWORKSPACE
     assert cc.capscaps_grad_norm(grads((FAKE, 5, 0)), 1, 1.0, 1.0, FAKE, FAKE, 65535) == cc.EWORKSPACE
     assert cc.capscaps_grad_norm(grads((FAKE, 1 << 50, 0)), 1, 1.0, 1.0, FAKE, FAKE, 65536) == cc.EUNSUPPORTED
+    many = grads(*[(FAKE, 1 << 32, 0)] * 100)
+    assert cc.capscaps_grad_norm(many, 100, 1.0, 1.0, FAKE, FAKE, 65536) == cc.EUNSUPPORTED
 
 
 def tensor(**over):

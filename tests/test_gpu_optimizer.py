@@ -248,6 +248,22 @@ def test_steps_repeat_bit_for_bit_and_seeds_differ():
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_a_saved_state_goes_on_as_it_was(bits):
+    def run(stop):
+        rng = torch.Generator().manual_seed(12)
+        params, grads, _ = tensors([3000, 41], rng)
+        opt = cc.AdamW(params, state_bits=bits, seed=4)
+        for k in range(4):
+            if k == stop:
+                state = [[t.clone() for t in s] for s in (opt.m, opt.v, opt.m_exp, opt.v_exp)[:4 if bits == 8 else 2]]
+                opt = cc.AdamW(params, state_bits=bits, seed=4, state=state, steps=opt.steps)
+            opt.step(grads)
+        return params + opt.m + opt.v
+    for a, b in zip(run(None), run(2)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_a_tensor_past_32_bits(bits):
     """2^31 + 300 values: the last ones against the reference."""
     n, tail = (1 << 31) + 300, 812          # (whole blocks of 256 from n - 812 on)
