@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(1024)
 // ------------------------------------------------------------------------------------ AdamW
 constexpr int ADAM_TENSORS = 44;
 // Fours of values that a lane updates, and a workgroup's share.  113M values with fp16 copies, us: 32-bit moments 618, 635 and
-// 616 with one, two and four of them; 8-bit ones 378 with two and with four, and 7M values 32 and 34
+// 616 with one, two and four of them; 8-bit ones the same with two and with four, and 7M values 32 and 34
 constexpr int units_of(int bits) { return bits == 8 ? 2 : 4; }
 constexpr int share_of(int bits) { return units_of(bits) * 4 * THREADS; }
 constexpr int VALUES_SHARE = 16 * THREADS;  // values that a workgroup decodes
@@ -194,13 +194,13 @@ struct AdamHyper {
 };
 // What a step needs of the host's or the device's counters
 struct AdamStep {
-    bool skip;
+    int skip;
     float scale, step_size, inv_sqrt_bias2;
     int t;
 };
 __device__ __forceinline__ AdamStep adam_step(const AdamHyper& H)
 {
-    AdamStep s{false, 1.0f, 0.0f, H.inv_sqrt_bias2, H.step};
+    AdamStep s{0, 1.0f, 0.0f, H.inv_sqrt_bias2, H.step};
     float bias1 = H.bias1;
     if (H.control != nullptr) {
         s.skip = H.control->skip != 0;
@@ -227,16 +227,18 @@ __host__ __device__ __forceinline__ unsigned mix(unsigned x)
     return x ^ (x >> 16);
 }
 
-// 8-bit codes (capscaps.h): `below` is the number of octaves below the shared exponent
+// 8-bit codes (capscaps.h): `below` is the number of octaves below the shared exponent.  A block's exponent is the same for
+// a wave, so what depends on it alone is in scalar registers.
 __device__ __forceinline__ float decode_magnitude(unsigned c, int exponent, int below)
 {
-    if (exponent == 255) return __builtin_nanf("");
-    return c == 0 ? 0.0f : __builtin_bit_cast(float, (c + 8u * (unsigned)(exponent - below)) << 20);
+    const unsigned bits = c == 0 ? 0u : (c << 20) + ((unsigned)(exponent - below) << 23);
+    return __builtin_bit_cast(float, exponent == 255 ? 0x7fc00000u : bits);
 }
+// (the code is the lowest byte of `c`)
 __device__ __forceinline__ float decode_m(unsigned c, int exponent)
 {
     const float v = decode_magnitude(c & 127u, exponent, 15);
-    return (c & 128u) != 0 ? -v : v;
+    return __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v) | ((c << 24) & 0x80000000u));
 }
 // The exponent that a block with the largest magnitude `top` (as bits) shares: one more where three bits of mantissa
 // cannot reach it, at least what keeps all codes normal numbers
@@ -246,22 +248,22 @@ __device__ __forceinline__ int shared_exponent(unsigned top, int below)
     const int e = (int)((top + 0xfffffu) >> 23);
     return e < below + 1 ? below + 1 : e > 254 ? 254 : e;
 }
-// `random`: 16 bits; a carry out of the 20 bits of mantissa that are cut off rounds up
+// `random`: 20 bits, of which the upper 16 count; a carry out of the 20 bits of mantissa that are cut off rounds up
 __device__ __forceinline__ int encode_magnitude(unsigned bits, unsigned random, int exponent, int below)
 {
-    return (int)((bits + (random << 4)) >> 20) - 8 * (exponent - below);
+    return (int)((bits + random) >> 20) - 8 * (exponent - below);
 }
+__device__ __forceinline__ int between(int c, int least, int most) { return c < least ? least : c > most ? most : c; }
 __device__ __forceinline__ unsigned encode_m(float v, unsigned random, int exponent)
 {
     const unsigned bits = __builtin_bit_cast(unsigned, v);
     const int c = encode_magnitude(bits & 0x7fffffffu, random, exponent, 15);
-    return (unsigned)(c < 0 ? 0 : c > 127 ? 127 : c) | (v < 0.0f ? 128u : 0u);
+    return (unsigned)between(c, 0, 127) | ((bits >> 24) & 128u);
 }
 __device__ __forceinline__ unsigned encode_v(float v, unsigned random, int exponent)
 {
-    const unsigned bits = __builtin_bit_cast(unsigned, v) & 0x7fffffffu;
-    const int c = encode_magnitude(bits, random, exponent, 31), least = bits != 0 ? 1 : 0;
-    return (unsigned)(c < least ? least : c > 255 ? 255 : c);
+    const unsigned bits = __builtin_bit_cast(unsigned, v);  // (never negative)
+    return (unsigned)between(encode_magnitude(bits, random, exponent, 31), bits != 0 ? 1 : 0, 255);
 }
 
 struct Moments {
@@ -273,7 +275,8 @@ __device__ __forceinline__ Moments adam_value(const AdamHyper& H, const AdamStep
     g = g * S.scale;
     m = m * H.beta1 + g * H.one_minus_beta1;
     v = v * H.beta2 + (g * g) * H.one_minus_beta2;
-    p = p * keep - S.step_size * (m / (sqrtf(v) * S.inv_sqrt_bias2 + H.eps));
+    // (v_sqrt_f32 and v_rcp_f32 are off by one unit in the last place, of a step that is added to p; v below 2^-126 counts as 0)
+    p = p * keep - S.step_size * (m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v) * S.inv_sqrt_bias2 + H.eps));
     return {p, m, v};
 }
 
@@ -318,51 +321,73 @@ __device__ __forceinline__ void store_codes(unsigned char* p, long long i, unsig
 }
 
 // A share of a tensor: each wave 256 neighbouring values at a time, which in 8 bits are a block of the state, so that the
-// largest magnitudes are the wave's and nothing waits for other waves
-template <int BITS>
-__global__ void __launch_bounds__(THREADS) adamw_kernel(AdamList L, AdamHyper H)
+// largest magnitudes are the wave's and nothing waits for other waves.  WHOLE: the share lies within the tensor.
+//
+// Bounded by memory, with 8-bit moments only just: decoding, two correctly rounded moments and encoding with random bits are
+// some eighty vector instructions a value (113M values: 332 us at 6.1 TB/s; 380 with a quotient and a square root rounded to
+// the last bit, 64-bit addresses and a product for each value's random bits).  So the bits come from sums, the square root and the
+// quotient from the fast instructions, and exponents, addresses and the step's factors are scalars.
+template <int BITS, bool WHOLE>
+__device__ __forceinline__ void adamw_share(const AdamTensor& T, const AdamHyper& H, unsigned key, long long base,
+                                            AdamStep* shared_step)
 {
     static_assert(STATE_BLOCK == 4 * 64, "a wave's values share an exponent");
     constexpr int UNITS = units_of(BITS);
-    const int k = tensor_of(L.first, L.count, blockIdx.x);
-    const AdamTensor& T = L.t[k];
-    const AdamStep S = adam_step(H);
-    if (S.skip) return;
-    const float keep = 1.0f - H.lr * T.weight_decay;
-    const unsigned key = mix(H.seed + 0x9E3779B1u * (unsigned)(L.index0 + k) + 0x6A09E667u * mix((unsigned)S.t));
-    const long long base = (long long)((int)blockIdx.x - L.first[k]) * share_of(BITS);
-    const long long i0 = base + (threadIdx.x >> 6) * STATE_BLOCK;  // this wave's values: from here, and each 4 * THREADS on
+    // this wave's values: from here, and each 4 * THREADS on
+    const long long i0 = base + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * STATE_BLOCK;
     const int lane4 = 4 * (threadIdx.x & 63);
     float4v p[UNITS], g[UNITS], m[UNITS], v[UNITS];
-    unsigned cm[UNITS], cv[UNITS], em[UNITS], ev[UNITS];
-    int n[UNITS];  // of the four, the tensor's
+    unsigned cm[UNITS], cv[UNITS];
+    int em[UNITS], ev[UNITS];
+    auto count = [&](int u) {  // of a lane's four values, the tensor's
+        if (WHOLE) return 4;
+        const long long rest = T.n - (i0 + u * 4 * THREADS + lane4);
+        return rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
+    };
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-        const long long first = i0 + u * 4 * THREADS, i = first + lane4, rest = T.n - i;
-        n[u] = rest >= 4 ? 4 : rest > 0 ? (int)rest : 0;
+        const long long first = i0 + u * 4 * THREADS;
+        const int n = count(u);
         p[u] = g[u] = m[u] = v[u] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
         cm[u] = cv[u] = em[u] = ev[u] = 0;
-        if (n[u] == 0) continue;
-        p[u] = load4(T.param, i, n[u], CAPSCAPS_FP32);
-        g[u] = load4(T.grad, i, n[u], T.grad_dtype);
+        if (!WHOLE && first >= T.n) break;
         if constexpr (BITS == 8) {
-            cm[u] = load_codes(static_cast<const unsigned char*>(T.m), i, n[u]);
-            cv[u] = load_codes(static_cast<const unsigned char*>(T.v), i, n[u]);
-            em[u] = T.m_exp[first / STATE_BLOCK];
-            ev[u] = T.v_exp[first / STATE_BLOCK];
+            em[u] = __builtin_amdgcn_readfirstlane(T.m_exp[first / STATE_BLOCK]);
+            ev[u] = __builtin_amdgcn_readfirstlane(T.v_exp[first / STATE_BLOCK]);
+        }
+        if (n == 0) continue;
+        p[u] = load4(T.param + first, lane4, n, CAPSCAPS_FP32);
+        g[u] = load4(static_cast<const char*>(T.grad) + first * (T.grad_dtype == CAPSCAPS_FP32 ? 4 : 2), lane4, n,
+                     T.grad_dtype);
+        if constexpr (BITS == 8) {
+            cm[u] = load_codes(static_cast<const unsigned char*>(T.m) + first, lane4, n);
+            cv[u] = load_codes(static_cast<const unsigned char*>(T.v) + first, lane4, n);
         } else {
-            m[u] = load4(T.m, i, n[u], CAPSCAPS_FP32);
-            v[u] = load4(T.v, i, n[u], CAPSCAPS_FP32);
+            m[u] = load4(static_cast<const float*>(T.m) + first, lane4, n, CAPSCAPS_FP32);
+            v[u] = load4(static_cast<const float*>(T.v) + first, lane4, n, CAPSCAPS_FP32);
         }
     }
+    // (the loads above are under way while one wave computes the step's factors)
+    if (threadIdx.x < 64) {
+        const AdamStep s = adam_step(H);
+        if (threadIdx.x == 0) *shared_step = s;
+    }
+    __syncthreads();
+    AdamStep S = *shared_step;
+    S.skip = __builtin_amdgcn_readfirstlane(S.skip);
+    S.t = __builtin_amdgcn_readfirstlane(S.t);
+    if (S.skip) return;
+    const float keep = 1.0f - H.lr * T.weight_decay;
+    key = mix(key + 0x6A09E667u * mix((unsigned)S.t));
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-        const long long first = i0 + u * 4 * THREADS, i = first + lane4;
-        if (first >= T.n) break;
+        const long long first = i0 + u * 4 * THREADS;
+        const int n = count(u);
+        if (!WHOLE && first >= T.n) break;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if constexpr (BITS == 8) {
-                m[u][j] = decode_m((cm[u] >> (8 * j)) & 255u, em[u]);
+                m[u][j] = decode_m(cm[u] >> (8 * j), em[u]);
                 v[u][j] = decode_magnitude((cv[u] >> (8 * j)) & 255u, ev[u], 31);
             }
             const Moments r = adam_value(H, S, keep, p[u][j], g[u][j], m[u][j], v[u][j]);
@@ -370,43 +395,59 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(AdamList L, AdamHyper H)
             m[u][j] = r.m;
             v[u][j] = r.v;
         }
-        if (n[u] > 0) {
-            store4(T.param, i, p[u], n[u], CAPSCAPS_FP32);
-            if (T.copy != nullptr) store4(T.copy, i, p[u], n[u], T.copy_dtype);
+        if (n > 0) {
+            store4(T.param + first, lane4, p[u], n, CAPSCAPS_FP32);
+            if (T.copy != nullptr) store4(static_cast<unsigned short*>(T.copy) + first, lane4, p[u], n, T.copy_dtype);
         }
         if constexpr (BITS == 8) {
             unsigned top_m = 0, top_v = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                // (values past the tensor's end count for nothing)
                 const float mj = m[u][j], vj = v[u][j];  // (a bit cast of a vector's element takes the first one)
-                const unsigned am = j < n[u] ? __builtin_bit_cast(unsigned, mj) & 0x7fffffffu : 0u;
-                const unsigned av = j < n[u] ? __builtin_bit_cast(unsigned, vj) & 0x7fffffffu : 0u;
+                // (values past the tensor's end count for nothing)
+                const unsigned am = WHOLE || j < n ? __builtin_bit_cast(unsigned, mj) & 0x7fffffffu : 0u;
+                const unsigned av = WHOLE || j < n ? __builtin_bit_cast(unsigned, vj) : 0u;
                 top_m = top_m > am ? top_m : am;
                 top_v = top_v > av ? top_v : av;
             }
             const int new_em = shared_exponent(wave_max(top_m), 15), new_ev = shared_exponent(wave_max(top_v), 31);
+            // (a third factor for the high half of an index that passes 32 bits; 256 values never cross that line)
+            const unsigned at = (unsigned)first * 0x9E3779B1u + (unsigned)(first >> 32) * 0xBB67AE85u + key;
+            const unsigned x0 = (unsigned)lane4 * 0x9E3779B1u + at;
             unsigned new_m = 0, new_v = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                // (a third factor for the high half of an index that passes 32 bits)
-                const unsigned x = mix((unsigned)(i + j) * 0x9E3779B1u + (unsigned)((i + j) >> 32) * 0xBB67AE85u + key);
-                new_m |= encode_m(m[u][j], x & 0xffffu, new_em) << (8 * j);
-                new_v |= encode_v(v[u][j], x >> 16, new_ev) << (8 * j);
+                const unsigned x = mix(x0 + (unsigned)j * 0x9E3779B1u);
+                new_m |= encode_m(m[u][j], (x & 0xffffu) << 4, new_em) << (8 * j);
+                new_v |= encode_v(v[u][j], (x >> 16) << 4, new_ev) << (8 * j);
             }
-            if (n[u] > 0) {
-                store_codes(static_cast<unsigned char*>(T.m), i, new_m, n[u]);
-                store_codes(static_cast<unsigned char*>(T.v), i, new_v, n[u]);
+            if (n > 0) {
+                store_codes(static_cast<unsigned char*>(T.m) + first, lane4, new_m, n);
+                store_codes(static_cast<unsigned char*>(T.v) + first, lane4, new_v, n);
             }
             if (lane4 == 0) {
                 T.m_exp[first / STATE_BLOCK] = (unsigned char)new_em;
                 T.v_exp[first / STATE_BLOCK] = (unsigned char)new_ev;
             }
-        } else if (n[u] > 0) {
-            store4(T.m, i, m[u], n[u], CAPSCAPS_FP32);
-            store4(T.v, i, v[u], n[u], CAPSCAPS_FP32);
+        } else if (n > 0) {
+            store4(static_cast<float*>(T.m) + first, lane4, m[u], n, CAPSCAPS_FP32);
+            store4(static_cast<float*>(T.v) + first, lane4, v[u], n, CAPSCAPS_FP32);
         }
     }
+}
+
+template <int BITS>
+__global__ void __launch_bounds__(THREADS) adamw_kernel(AdamList L, AdamHyper H)
+{
+    __shared__ AdamStep step;
+    const int k = tensor_of(L.first, L.count, blockIdx.x);
+    const AdamTensor& T = L.t[k];
+    const unsigned key = H.seed + 0x9E3779B1u * (unsigned)(L.index0 + k);
+    const long long base = (long long)((int)blockIdx.x - L.first[k]) * share_of(BITS);
+    if (base + share_of(BITS) <= T.n)
+        adamw_share<BITS, true>(T, H, key, base, &step);
+    else
+        adamw_share<BITS, false>(T, H, key, base, &step);
 }
 
 struct ValuesList {
