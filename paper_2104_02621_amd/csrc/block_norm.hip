@@ -691,13 +691,18 @@ RowPlan row_plan(const capscaps_block& B, int n, bool forward, bool apart)
     P.vectors = vectors <= P.group ? 1 : n == 4 && vectors <= 2 * P.group ? 2 : 32 / n;
     if (P.vectors > 2) P.group = 512;
     const bool in_step = !forward || (vectors > 64 && (n == 8 || B.width > 2048));
-    // (several rows in a workgroup of 1024 where there are rows for every unit)
-    P.threads = in_step && P.vectors == 1 && B.rows * P.group >= 1024LL * CUS ? 1024 : THREADS;
+    // Backward, rows within a wave that no vector divides: their accesses cross lines, and their waves wait longer than others, so
+    // more of them, in smaller workgroups (2.1M rows of 27 fp32 values with a gate: 387 us, as the others 420; bf16 and fp32
+    // mixed 300, 365; of 27 bf16 values, whose lanes take more registers, two workgroups 170, one 176, three 216)
+    const bool crossing = !forward && B.width % n != 0 && vectors <= 64;
+    const int step = crossing ? 512 : 1024;
+    // (several rows in such a workgroup where there are rows for every unit)
+    P.threads = in_step && P.vectors == 1 && B.rows * P.group >= (long long)step * CUS ? step : THREADS;
     if (P.group > P.threads || apart) P.threads = P.group;
     P.per_block = P.threads / P.group;
     const long long blocks = (B.rows + P.per_block - 1) / P.per_block;
     // (a launch has less than 2^32 threads)
-    const long long most = apart ? CUS : !in_step ? 1LL << 23 : (long long)CUS * (forward ? 2048 : 1024) / P.threads;
+    const long long most = apart ? CUS : !in_step ? 1LL << 23 : (long long)CUS * (forward ? 2048 : crossing && n == 4 ? 1536 : 1024) / P.threads;
     P.blocks = (unsigned)(blocks < most ? blocks : most);
     P.turns = P.blocks < blocks;
     P.full = B.width / n;
