@@ -433,6 +433,18 @@ BlockNorm = namedtuple("BlockNorm", "y h rstd_pre rstd_post")
 BlockNormGrads = namedtuple("BlockNormGrads", "dx dbranch dpre_weight dpost_weight dgate")
 _ACTS = {"linear": ACT_LINEAR, "sigmoid": ACT_SIGMOID, "silu": ACT_SILU}
 _codes = None
+_raw_stream = None
+
+
+def _stream(device):
+    """Handle of torch's current stream on `device`, by the short way (1.8 us less than through a Stream object, of the 20
+    that a call on small tensors takes) where this torch has it."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
+    return _raw_stream(device.index)
 
 
 def _code(dtype):
@@ -450,12 +462,12 @@ def _code(dtype):
 def _row_stride(t, shape, width, norm_dims, name):
     """Distance between the rows of `t`, whose last `norm_dims` axes are one dense row and whose other axes follow
     each other at equal distances."""
+    if t.is_cuda and t.shape == shape and t.is_contiguous():
+        return width
     if not t.is_cuda:
         raise ValueError("capscaps runs on the GPU only: pass device tensors")
     if t.shape != shape:
         raise ValueError(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
-    if t.is_contiguous():
-        return width
     strides, dense = t.stride(), 1
     for k in range(len(shape) - 1, len(shape) - 1 - norm_dims, -1):
         if shape[k] != 1 and strides[k] != dense:
@@ -476,7 +488,7 @@ def _row_stride(t, shape, width, norm_dims, name):
 def _vector(t, width, device, name):
     if t is None:
         return None
-    if _code(t.dtype) != FP32 or t.numel() != width or not t.is_contiguous() or t.device != device:
+    if t.numel() != width or _code(t.dtype) != FP32 or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name} must be {width} contiguous float32 values on {device}")
     return t.data_ptr()
 
@@ -557,7 +569,7 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
         None if rpost is None else rpost.data_ptr(), xs, bs, gs,
         0 if y is None else _row_stride(y, shape, width, norm_dims, "y"),
         0 if h is None else _row_stride(h, shape, width, norm_dims, "h"))
-    rc = capscaps_block_norm_fwd(block, args, torch.cuda.current_stream(device).cuda_stream)
+    rc = capscaps_block_norm_fwd(block, args, _stream(device))
     if rc != OK:
         raise CapscapsError(rc)
     return BlockNorm(y, h, rpre, rpost)
@@ -605,7 +617,7 @@ def block_norm_bwd(y, branch, rstd_pre, rstd_post, dh, dy, *, pre_weight=None, p
         _row_stride(y, shape, width, norm_dims, "y"), bs, gs,
         0 if dh is None else _row_stride(dh, shape, width, norm_dims, "dh"),
         0 if dy is None else _row_stride(dy, shape, width, norm_dims, "dy"), width, width, width)
-    rc = capscaps_block_norm_bwd(block, args, ws.data_ptr(), need, torch.cuda.current_stream(device).cuda_stream)
+    rc = capscaps_block_norm_bwd(block, args, ws.data_ptr(), need, _stream(device))
     if rc != OK:
         raise CapscapsError(rc)
     return BlockNormGrads(dx, db, dpre, dpost, dgate)
@@ -642,7 +654,7 @@ def grad_norm(grads, max_norm=None, grad_scale=1.0, control=None, workspace=None
     items = (GradTensor * max(1, len(grads)))(*[(_dense(g, "gradients"), g.numel(), _code(g.dtype)) for g in grads])
     rc = capscaps_grad_norm(items, len(grads), grad_scale, 0.0 if max_norm is None else max_norm,
                             _control_ptr(control), workspace.data_ptr(), workspace.numel(),
-                            torch.cuda.current_stream(device).cuda_stream)
+                            _stream(device))
     if rc != OK:
         raise CapscapsError(rc)
     return control
@@ -718,7 +730,7 @@ class AdamW:
         step = 0 if control is not None else self.steps + 1
         rc = capscaps_adamw_step(self._items, len(self._items), self.state_bits, self.lr if lr is None else lr,
                                  self.betas[0], self.betas[1], self.eps, step, self.seed & 0xFFFFFFFF,
-                                 _control_ptr(control), torch.cuda.current_stream(self.params[0].device).cuda_stream)
+                                 _control_ptr(control), _stream(self.params[0].device))
         if rc != OK:
             raise CapscapsError(rc)
         if control is None:
@@ -739,7 +751,7 @@ class AdamW:
         count = len(self._items)
         pointers = [(ctypes.c_void_p * count)(*[_dense(t, "values") for t in o]) for o in out]
         rc = capscaps_adamw_state_values(self._items, count, pointers[0], pointers[1],
-                                         torch.cuda.current_stream(self.params[0].device).cuda_stream)
+                                         _stream(self.params[0].device))
         if rc != OK:
             raise CapscapsError(rc)
         return out[0], out[1]
