@@ -139,6 +139,19 @@ def test_row_counts(rows, width):
     c.check_backward(c.backward())
 
 
+@pytest.mark.parametrize("rows,width,types,gate", [
+    (1100, 9000, TYPES[1], "shared"), (1100, 9001, TYPES[0], "shared"), (700, 16384, TYPES[6], "full"),
+    (2300, 5003, TYPES[0], "full"), (2300, 6000, TYPES[2], None), (9001, 1100, TYPES[1], "shared"),
+    (9000, 1027, TYPES[3], "full"), (150001, 27, TYPES[0], "full"), (300001, 16, TYPES[1], "shared"),
+    (300001, 13, TYPES[5], "full"), (70001, 64, TYPES[4], "shared"), (1000003, 3, TYPES[1], None)],
+    ids=lambda v: v if isinstance(v, (int, str)) else None)
+def test_more_rows_than_workgroups(rows, width, types, gate):
+    """Each kernel with workgroups that take several rounds of rows, the last one ragged."""
+    c = Case(rows, width, types, gate, "silu" if gate == "full" else "linear", rs=0.9)
+    c.check_forward(c.forward())
+    c.check_backward(c.backward())
+
+
 @pytest.mark.parametrize("width", [8, 27, 64, 600, 2048, 4100])
 @pytest.mark.parametrize("gap,shift", [(0, 1), (8, 0), (5, 0), (3, 3)])
 @pytest.mark.parametrize("types", [TYPES[0], TYPES[1], TYPES[4]], ids=lambda t: "-".join(NAMES[x] for x in t))
