@@ -1,10 +1,15 @@
 // The norms around a block of layers with its gate and residual stream, forward and backward.
 // Formulas and contracts: include/capscaps.h.
 //
-// All of it is bounded by memory: some ten to thirty operations for every value moved.  So each value is read once and
-// each result written once, with the row in registers between: a group of lanes holds a row in vectors
-// (row_vectors.h), and the means are sums over the group.  Groups of up to 64 lanes share a wave and need
-// no barrier; wider rows take a workgroup.  Rows that no group holds (over 16384 values) take the kernels at the end.
+// All of it is bounded by memory: some ten to thirty operations for every value moved.  So each value is read
+// once and each result written once, with the row in registers between: a group of lanes holds a row in vectors
+// (row_vectors.h), and the means are sums over the group.  Groups of up to 64 lanes share a wave and need no
+// barrier; wider rows take a workgroup.  Rows that no group holds (over 16384 values) take the kernels at the
+// end.
+//
+// Measured (us; the bytes that must be moved at 6.2 TB/s in parentheses): forward, 65536 rows of 864 fp32 values
+// 155 (146), 6.4M rows of 64 bf16 values with a gate for each 669 (671), 65536 x 4096 bf16 383 (346); backward,
+// 16384 x 4096 fp32 and bf16 231 (217), 16384 x 16384 fp16 593 (520), 2.1M x 27 fp32 with a gate 388 (295).
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <math.h>
@@ -51,7 +56,6 @@ __device__ __forceinline__ float block_sum(float v, float* lds)
     return v;
 }
 
-
 // ------------------------------------------------------------------------------------ rows in registers
 // How rows lie on lanes: `group` lanes (a power of two) hold a row, lane l the vectors l, l + group, ... of `vectors`
 // a lane; `per_block` rows at a time in a workgroup of `threads`.
@@ -66,15 +70,16 @@ struct RowPlan {
 constexpr int WIDEST = 16384;
 // vectors of a lane: 1, 2 in workgroups of up to 1024; 4, 8 in such of 512, whose waves have twice the registers
 constexpr int widest_workgroup(int vectors) { return vectors > 2 ? 512 : 1024; }
-// (lanes of several vectors are those of a whole workgroup: known to the compiler, which then needs no register for every
-// distance between them)
+// (lanes of several vectors are those of a whole workgroup: known to the compiler, which then needs no register
+// for every distance between them)
 template <int I>
 __device__ __forceinline__ int group_of(const RowPlan& P)
 {
     return I > 1 ? widest_workgroup(I) : P.group;
 }
-// Sum over a row's lanes.  Rows of more than one wave go through LDS: two buffers in turn, so that one barrier is
-// enough (a wave writes a buffer again only after the barrier of the other one, which every wave reaches after it has read).
+// Sum over a row's lanes.  Rows of more than one wave go through LDS: two buffers in turn, so that one barrier
+// is enough (a wave writes a buffer again only after the barrier of the other one, which every wave reaches
+// after it has read).
 struct RowSum {
     float* lds;  // [2][16]
     int group, turn;
@@ -95,8 +100,8 @@ struct RowSum {
     }
 };
 
-// A tensor's rows as the lanes of a workgroup see them: where its rows of this round begin (the same for all lanes, so
-// it stays in scalar registers), and a lane's place from there
+// A tensor's rows as the lanes of a workgroup see them: where its rows of this round begin (the same for all
+// lanes, so it stays in scalar registers), and a lane's place from there
 template <int N>
 struct Rows {
     const char* base;
@@ -185,7 +190,8 @@ private:
 
 // GATE: a gate for every value.  TURNS: a workgroup takes one round of rows after another (else one round)
 template <int DT, bool S16, bool B16, bool GATE, int N, int I, bool TAIL, bool TURNS>
-__global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps_block B, capscaps_block_fwd_args A, RowPlan P)
+__global__ void __launch_bounds__(widest_workgroup(I))
+    block_fwd_kernel(capscaps_block B, capscaps_block_fwd_args A, RowPlan P)
 {
     constexpr int SD = S16 ? DT : CAPSCAPS_FP32, BD = B16 ? DT : CAPSCAPS_FP32;
     constexpr int SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
@@ -249,8 +255,7 @@ __global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps
                 }
                 s += y[i][k] * y[i][k];
             }
-            if (A.y != nullptr)
-                store<SD, N, TAIL>(ry.put(n, i * group, SB), y[i], has);
+            if (A.y != nullptr) store<SD, N, TAIL>(ry.put(n, i * group, SB), y[i], has);
         }
         if (pre) {
             const float rpre = __builtin_amdgcn_rsqf(sum(s) * inv_width + B.eps);
@@ -269,10 +274,11 @@ __global__ void __launch_bounds__(widest_workgroup(I)) block_fwd_kernel(capscaps
     } while (TURNS && n < rounds);
 }
 
-// The way back.  Of the two sums over a row, the first (of dh * pre_weight * yn) needs y and dh, the second dy and b: each
-// pair is fetched while the other is worked on.  Sums over rows stay in registers, two for each column:
-// of dh * yn, and of d * act * bn, from which both dpost_weight and a shared gate's gradient follow, since all their other
-// factors are the column's.  A workgroup's sums go to `partial` [block][2][columns], columns in the order of lanes' places.
+// The way back.  Of the two sums over a row, the first (of dh * pre_weight * yn) needs y and dh, the second dy
+// and b: each pair is fetched while the other is worked on.  Sums over rows stay in registers, two for each
+// column: of dh * yn, and of d * act * bn, from which both dpost_weight and a shared gate's gradient follow,
+// since all their other factors are the column's.  A workgroup's sums go to `partial` [block][2][columns],
+// columns in the order of lanes' places.
 template <int DT, bool S16, bool B16, bool GATE, int N, int I, bool TAIL>
 __global__ void __launch_bounds__(widest_workgroup(I))
     block_bwd_kernel(capscaps_block B, capscaps_block_bwd_args A, RowPlan P, float* partial)
@@ -347,8 +353,9 @@ __global__ void __launch_bounds__(widest_workgroup(I))
     if constexpr (AHEAD) fetch_h(n);
     for (; n < rounds; n += gridDim.x) {
         const bool in = n * P.per_block + slot < B.rows;
-        // waves that hold rows by themselves stay together (wider rows' sums keep them so): their accesses are then one
-        // piece of memory after another (6.4M rows of 64 bf16 values: 285 us, without 325; rows of 1024, eight to a workgroup: 139, one: 163)
+        // waves that hold rows by themselves stay together (wider rows' sums keep them so): their accesses are
+        // then one piece of memory after another (6.4M rows of 64 bf16 values: 285 us, without 325; rows of
+        // 1024, eight to a workgroup: 139, one: 163)
         if (group <= 64) __builtin_amdgcn_s_barrier();
         if constexpr (!AHEAD) fetch_h(n);
         fetch_b(n);
@@ -387,15 +394,14 @@ __global__ void __launch_bounds__(widest_workgroup(I))
                 }
                 sum_b[i][k] += d * bn;
                 e[i][k] = d * cb[k];
-                // (here, not where they are used: the compiler would keep the factors of all these products until then)
+                // (here, not where they are used: the compiler would keep the factors of all these products
+                // until then)
                 asm volatile("" : "+v"(sum_h[i][k]), "+v"(sum_b[i][k]), "+v"(e[i][k]));
                 s += e[i][k] * bn;
             }
-            if (A.dx != nullptr)
-                store<SD, N, TAIL>(rdx.put(n, i * group, SB), dx, has);
+            if (A.dx != nullptr) store<SD, N, TAIL>(rdx.put(n, i * group, SB), dx, has);
             if constexpr (GATE) {
-                if (A.dgate != nullptr)
-                    store<DT, N, TAIL>(rdg.put(n, i * group, LB), dg, has);
+                if (A.dgate != nullptr) store<DT, N, TAIL>(rdg.put(n, i * group, LB), dg, has);
             }
         }
         if (AHEAD && n + gridDim.x < rounds) fetch_h(n + gridDim.x);
@@ -436,7 +442,8 @@ __global__ void __launch_bounds__(widest_workgroup(I))
                     sum_b[i][k] += __shfl_xor(sum_b[i][k], o);
                 }
     }
-    // the rows of the workgroup's waves: `slots` of them hold the same columns (a lane has one vector, or the row a workgroup)
+    // the rows of the workgroup's waves: `slots` of them hold the same columns (a lane has one vector, or the
+    // row a workgroup)
     if constexpr (I == 1) {
         __shared__ float of_slot[1024 * N];
         const int wide = group < 64 ? 64 : group, slots = P.threads / wide, in_row = group * N;
@@ -673,14 +680,15 @@ int check_block(const capscaps_block* B)
     return CAPSCAPS_OK;
 }
 
-// The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024; then two vectors of four values,
-// or 32 values in a workgroup of 512.  `apart`: rows so far apart that those of one workgroup are not within reach of
-// 32-bit offsets, one at a time in a workgroup.
+// The lanes of a row: as few as hold it with one vector each, up to a workgroup of 1024; then two vectors of
+// four values, or 32 values in a workgroup of 512.  `apart`: rows so far apart that those of one workgroup are
+// not within reach of 32-bit offsets, one at a time in a workgroup.
 //
-// Workgroups of 1024 that go through many rows in step read memory in large pieces, and need the columns' factors once; rows
-// of few lanes do better as they come, four waves a workgroup (us, forward, 134M bf16 values a tensor, 173 at 6.2 TB/s: rows of 512
-// 183 as they come, 202 in turns; of 1024 192 and 183, of 4096 239 and 182; 67M fp32 values: rows of 1024 178 and 188, of 4096 192 and
-// 180).  The way back keeps sums over rows in registers, so it always goes in turns.
+// Workgroups of 1024 that go through many rows in step read memory in large pieces, and need the columns'
+// factors once; rows of few lanes do better as they come, four waves a workgroup (us, forward, 134M bf16 values
+// a tensor, 173 at 6.2 TB/s: rows of 512 183 as they come, 202 in turns; of 1024 192 and 183, of 4096 239 and
+// 182; 67M fp32 values: rows of 1024 178 and 188, of 4096 192 and 180).  The way back keeps sums over rows in
+// registers, so it always goes in turns.
 RowPlan row_plan(const capscaps_block& B, int n, bool forward, bool apart)
 {
     RowPlan P;
@@ -691,9 +699,10 @@ RowPlan row_plan(const capscaps_block& B, int n, bool forward, bool apart)
     P.vectors = vectors <= P.group ? 1 : n == 4 && vectors <= 2 * P.group ? 2 : 32 / n;
     if (P.vectors > 2) P.group = 512;
     const bool in_step = !forward || (vectors > 64 && (n == 8 || B.width > 2048));
-    // Backward, rows within a wave that no vector divides: their accesses cross lines, and their waves wait longer than others, so
-    // more of them, in smaller workgroups (2.1M rows of 27 fp32 values with a gate: 387 us, as the others 420; bf16 and fp32
-    // mixed 300, 365; of 27 bf16 values, whose lanes take more registers, two workgroups 170, one 176, three 216)
+    // Backward, rows within a wave that no vector divides: their accesses cross lines, and their waves wait
+    // longer than others, so more of them, in smaller workgroups (2.1M rows of 27 fp32 values with a gate: 387
+    // us, as the others 420; bf16 and fp32 mixed 300, 365; of 27 bf16 values, whose lanes take more registers,
+    // two workgroups 170, one 176, three 216)
     const bool crossing = !forward && B.width % n != 0 && vectors <= 64;
     const int step = crossing ? 512 : 1024;
     // (several rows in such a workgroup where there are rows for every unit)
@@ -702,7 +711,8 @@ RowPlan row_plan(const capscaps_block& B, int n, bool forward, bool apart)
     P.per_block = P.threads / P.group;
     const long long blocks = (B.rows + P.per_block - 1) / P.per_block;
     // (a launch has less than 2^32 threads)
-    const long long most = apart ? CUS : !in_step ? 1LL << 23 : (long long)CUS * (forward ? 2048 : crossing && n == 4 ? 1536 : 1024) / P.threads;
+    const int per_unit = forward ? 2048 : crossing && n == 4 ? 1536 : 1024;  // threads
+    const long long most = apart ? CUS : !in_step ? 1LL << 23 : (long long)CUS * per_unit / P.threads;
     P.blocks = (unsigned)(blocks < most ? blocks : most);
     P.turns = P.blocks < blocks;
     P.full = B.width / n;
@@ -723,8 +733,8 @@ int vector_values(const capscaps_block& B, bool branch)
 template <int V>
 using Int = std::integral_constant<int, V>;
 
-// calls `launch` with the kernel's compile-time properties: stream and branch of 16 bits, a gate for every value, values of a
-// vector, vectors of a lane, a partial vector
+// calls `launch` with the kernel's compile-time properties: stream and branch of 16 bits, a gate for every
+// value, values of a vector, vectors of a lane, a partial vector
 template <int DT, typename F>
 void with_properties(const capscaps_block& B, bool branch, const RowPlan& P, F launch)
 {

@@ -4,8 +4,9 @@
 // captured and the lists may change from call to call): a launch takes as many tensors as 4 KB of arguments hold,
 // and a workgroup finds its tensor and its share of it from the running number of shares (one load and a vote).
 //
-// Everything here is bounded by memory.  A lane has four neighbouring values of a tensor, so that every access of a wave is
-// one contiguous piece (1 KB of fp32), at any address, and a workgroup takes its share in one pass.
+// Everything here is bounded by memory.  A lane has four neighbouring values of a tensor, so that every access
+// of a wave is one contiguous piece (1 KB of fp32), at any address, and a workgroup takes its share in one
+// pass.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -49,7 +50,8 @@ __device__ __forceinline__ float4v load4(const void* p, long long i, int n, int 
 {
     if (n == 4) {
         if (dtype == CAPSCAPS_FP32) {
-            const uint4v w = __builtin_nontemporal_load(reinterpret_cast<const uint4_a4*>(static_cast<const float*>(p) + i));
+            const uint4v w =
+                __builtin_nontemporal_load(reinterpret_cast<const uint4_a4*>(static_cast<const float*>(p) + i));
             return __builtin_bit_cast(float4v, w);
         }
         const uint2v w =
@@ -70,7 +72,8 @@ __device__ __forceinline__ void store4(void* p, long long i, const float4v& v, i
 {
     if (n == 4) {
         if (dtype == CAPSCAPS_FP32) {
-            __builtin_nontemporal_store(__builtin_bit_cast(uint4v, v), reinterpret_cast<uint4_a4*>(static_cast<float*>(p) + i));
+            __builtin_nontemporal_store(__builtin_bit_cast(uint4v, v),
+                                        reinterpret_cast<uint4_a4*>(static_cast<float*>(p) + i));
             return;
         }
         typedef _Float16 half4v __attribute__((ext_vector_type(4)));
@@ -112,6 +115,9 @@ __device__ __forceinline__ double block_sum(double v, double* lds)
     return v;
 }
 
+// A workgroup sums a share, four loads of 16 bytes of each lane under way at a time, in fp64 (a conversion and a product-sum
+// a value: half of what memory leaves time for).  113M values: 76 us at 6.0 TB/s; 4 us more for the launch that
+// sums the workgroups' sums.  7M values take 10 .. 14 us: less than two workgroups a unit.
 __global__ void __launch_bounds__(THREADS) grad_norm_kernel(NormList L, double* partial)
 {
     __shared__ double lds[THREADS / 64];
@@ -162,8 +168,9 @@ __global__ void __launch_bounds__(1024)
 
 // ------------------------------------------------------------------------------------ AdamW
 constexpr int ADAM_TENSORS = 44;
-// Fours of values that a lane updates, and a workgroup's share.  113M values with fp16 copies, us: 32-bit moments 618, 635 and
-// 616 with one, two and four of them; 8-bit ones the same with two and with four, and 7M values 32 and 34
+// Fours of values that a lane updates, and a workgroup's share.  113M values with fp16 copies, us: 32-bit
+// moments 618, 635 and 616 with one, two and four of them; 8-bit ones the same with two and with four, and 7M
+// values 32 and 34
 constexpr int units_of(int bits) { return bits == 8 ? 2 : 4; }
 constexpr int share_of(int bits) { return units_of(bits) * 4 * THREADS; }
 constexpr int VALUES_SHARE = 16 * THREADS;  // values that a workgroup decodes
@@ -227,8 +234,8 @@ __host__ __device__ __forceinline__ unsigned mix(unsigned x)
     return x ^ (x >> 16);
 }
 
-// 8-bit codes (capscaps.h): `below` is the number of octaves below the shared exponent.  A block's exponent is the same for
-// a wave, so what depends on it alone is in scalar registers.
+// 8-bit codes (capscaps.h): `below` is the number of octaves below the shared exponent.  A block's exponent is
+// the same for a wave, so what depends on it alone is in scalar registers.
 __device__ __forceinline__ float decode_magnitude(unsigned c, int exponent, int below)
 {
     const unsigned bits = c == 0 ? 0u : (c << 20) + ((unsigned)(exponent - below) << 23);
@@ -275,7 +282,8 @@ __device__ __forceinline__ Moments adam_value(const AdamHyper& H, const AdamStep
     g = g * S.scale;
     m = m * H.beta1 + g * H.one_minus_beta1;
     v = v * H.beta2 + (g * g) * H.one_minus_beta2;
-    // (v_sqrt_f32 and v_rcp_f32 are off by one unit in the last place, of a step that is added to p; v below 2^-126 counts as 0)
+    // (v_sqrt_f32 and v_rcp_f32 are off by one unit in the last place, of a step that is added to p; v below
+    // 2^-126 counts as 0)
     p = p * keep - S.step_size * (m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v) * S.inv_sqrt_bias2 + H.eps));
     return {p, m, v};
 }
@@ -293,8 +301,8 @@ __device__ __forceinline__ unsigned wave_max(unsigned v)
     v = dpp_max<0x4E>(v);   // quad_perm 2 3 0 1
     v = dpp_max<0x141>(v);  // row_half_mirror
     v = dpp_max<0x140>(v);  // row_mirror: the largest of 16 lanes in each of them
-    const unsigned a = (unsigned)__builtin_amdgcn_readlane((int)v, 0), b = (unsigned)__builtin_amdgcn_readlane((int)v, 16);
-    const unsigned c = (unsigned)__builtin_amdgcn_readlane((int)v, 32), d = (unsigned)__builtin_amdgcn_readlane((int)v, 48);
+    auto row = [&](int lane) { return (unsigned)__builtin_amdgcn_readlane((int)v, lane); };
+    const unsigned a = row(0), b = row(16), c = row(32), d = row(48);
     const unsigned ab = a > b ? a : b, cd = c > d ? c : d;
     return ab > cd ? ab : cd;
 }
@@ -320,13 +328,15 @@ __device__ __forceinline__ void store_codes(unsigned char* p, long long i, unsig
         if (k < n) p[i + k] = (unsigned char)(c >> (8 * k));
 }
 
-// A share of a tensor: each wave 256 neighbouring values at a time, which in 8 bits are a block of the state, so that the
-// largest magnitudes are the wave's and nothing waits for other waves.  WHOLE: the share lies within the tensor.
+// A share of a tensor: each wave 256 neighbouring values at a time, which in 8 bits are a block of the state,
+// so that the largest magnitudes are the wave's and nothing waits for other waves.  WHOLE: the share lies
+// within the tensor.
 //
-// Bounded by memory, with 8-bit moments only just: decoding, two correctly rounded moments and encoding with random bits are
-// some eighty vector instructions a value (113M values: 332 us at 6.1 TB/s; 380 with a quotient and a square root rounded to
-// the last bit, 64-bit addresses and a product for each value's random bits).  So the bits come from sums, the square root and the
-// quotient from the fast instructions, and exponents, addresses and the step's factors are scalars.
+// Bounded by memory, with 8-bit moments only just: decoding, two correctly rounded moments and encoding with
+// random bits are some eighty vector instructions a value (113M values: 332 us at 6.1 TB/s; 380 with a quotient
+// and a square root rounded to the last bit, 64-bit addresses and a product for each value's random bits).  So
+// the bits come from sums, the square root and the quotient from the fast instructions, and exponents,
+// addresses and the step's factors are scalars.
 template <int BITS, bool WHOLE>
 __device__ __forceinline__ void adamw_share(const AdamTensor& T, const AdamHyper& H, unsigned key, long long base,
                                             AdamStep* shared_step)
@@ -475,6 +485,7 @@ __device__ __forceinline__ void decode8(uint2v codes, unsigned exponent, unsigne
     __builtin_nontemporal_store(w, reinterpret_cast<uint4_a2*>(out));
 }
 
+// (113M values of each moment: 114 us at 6.0 TB/s; 147 with the loads of a share one after another)
 __global__ void __launch_bounds__(THREADS) state_values_kernel(ValuesList L)
 {
     const int k = tensor_of(L.first, L.count, blockIdx.x);

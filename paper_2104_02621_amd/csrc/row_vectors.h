@@ -1,11 +1,12 @@
 // Internal: rows of values of the three element types, some values a lane, at any address.
 //
-// A row's values are cut into vectors of N values, one of 16 bytes where all tensors of a call have 16-bit elements (N = 8),
-// else N = 4: 16 bytes of fp32, 8 of a 16-bit type, so that a wave's access is one contiguous piece in every type.
-// They are loaded and stored whole at any alignment (the hardware takes such accesses at element addresses).
-// What a row's length leaves over (1 .. N - 1 values) is one lane's last vector.  It is loaded whole too, with the beginning of
-// what follows in memory, which is masked (a load for 1, 2 and 4 values each would be three, and as many waits for the same
-// lines); in a tensor's last row, and where rows are not apart, in pieces.  It is stored in pieces.
+// A row's values are cut into vectors of N values, one of 16 bytes where all tensors of a call have 16-bit
+// elements (N = 8), else N = 4: 16 bytes of fp32, 8 of a 16-bit type, so that a wave's access is one contiguous
+// piece in every type. They are loaded and stored whole at any alignment (the hardware takes such accesses at
+// element addresses). What a row's length leaves over (1 .. N - 1 values) is one lane's last vector.  It is
+// loaded whole too, with the beginning of what follows in memory, which is masked (a load for 1, 2 and 4 values
+// each would be three, and as many waits for the same lines); in a tensor's last row, and where rows are not
+// apart, in pieces.  It is stored in pieces.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -40,7 +41,8 @@ __device__ __forceinline__ void clear(Raw<DT, N>& r)
     for (int k = 0; k < Raw<DT, N>::WORDS; ++k) r.w[k] = 0;
 }
 
-// The first `tail` (1 .. N - 1) values of a vector in memory, as pieces of 4, 2 and 1 values (tail is the same for all lanes)
+// The first `tail` (1 .. N - 1) values of a vector in memory, as pieces of 4, 2 and 1 values (tail is the same
+// for all lanes)
 template <int DT, int N, int FIRST, int VALUES>
 __device__ __forceinline__ void load_piece(Raw<DT, N>& r, const char* p)
 {
