@@ -57,13 +57,14 @@ __device__ __forceinline__ float block_sum(float v, float* lds)
 }
 
 // ------------------------------------------------------------------------------------ rows in registers
-// How rows lie on lanes: `group` lanes (a power of two) hold a row, lane l the vectors l, l + group, ... of `vectors`
+// How rows lie on lanes: `group` lanes (a power of two up to 64, or so many waves) hold a row, lane l the vectors l, l + group, ... of `vectors`
 // a lane; `per_block` rows at a time in a workgroup of `threads`.
 struct RowPlan {
     int n;  // values of a vector
     int group, vectors, threads, per_block;
     unsigned blocks;
     int full, tail;  // whole vectors in a row, and the values after them
+    int part;        // the vector that those are in (-1: none)
     bool turns;      // more than one round of rows for a workgroup
 };
 
@@ -82,7 +83,7 @@ __device__ __forceinline__ int group_of(const RowPlan& P)
 // after it has read).
 struct RowSum {
     float* lds;  // [2][16]
-    int group, turn;
+    int group, slot, turn;
     __device__ __forceinline__ float operator()(float v)
     {
         if (group <= 64) return lanes_sum(v, group);
@@ -95,7 +96,7 @@ struct RowSum {
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
         // the waves of this row; every 16 lanes add up the same sums
         const int waves = group >> 6, wave = threadIdx.x & 15;
-        v = wave < waves ? buffer[((threadIdx.x >> 6) & ~(waves - 1)) + wave] : 0.0f;
+        v = wave < waves ? buffer[slot * waves + wave] : 0.0f;
         return lanes_sum(v, 16);
     }
 };
@@ -137,7 +138,7 @@ __device__ __forceinline__ Factors<N> column_factors(const capscaps_block& B, co
 {
     Factors<N> f;
     const bool shared = B.gate == CAPSCAPS_GATE_SHARED;
-    const Share has{v < P.full, TAIL && v == P.full, P.tail};
+    const Share has{v < P.full, TAIL && v == P.part, P.tail};
     load_column<N, TAIL>(f.to_b, post_weight, v, has, 1.0f);
     load_column<N, TAIL>(f.to_h, pre_weight, v, has, 1.0f);
     float g[N];
@@ -197,8 +198,8 @@ __global__ void __launch_bounds__(widest_workgroup(I))
     constexpr int SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
     __shared__ float lds[32];
     const int group = group_of<I>(P);
-    RowSum sum{lds, group, 0};
-    const int lane = threadIdx.x & (group - 1), slot = threadIdx.x / group;
+    const int slot = threadIdx.x / group, lane = threadIdx.x - slot * group;
+    RowSum sum{lds, group, slot, 0};
     const bool branch = A.branch != nullptr, post = branch && B.post_norm, pre = A.h != nullptr;
     const float inv_width = 1.0f / (float)B.width;
     Factors<N> col[I];
@@ -219,7 +220,7 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
-            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
+            const Share has{in && v < P.full, TAIL && in && v == P.part, P.tail};
             clear(x[i]);
             clear(b[i]);
             if (branch) load<BD, N, TAIL>(b[i], rb.get(n, i * group, BB), has, rb.over && !last);
@@ -244,7 +245,7 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
-            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
+            const Share has{in && v < P.full, TAIL && in && v == P.part, P.tail};
 #pragma unroll
             for (int k = 0; k < N; ++k) {
                 y[i][k] = value<SD, N>(x[i], k);
@@ -263,7 +264,7 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int v = lane + i * group;
-                const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
+                const Share has{in && v < P.full, TAIL && in && v == P.part, P.tail};
                 float h[N];
 #pragma unroll
                 for (int k = 0; k < N; ++k) h[k] = y[i][k] * rpre * col[i].to_h[k];
@@ -287,8 +288,8 @@ __global__ void __launch_bounds__(widest_workgroup(I))
     constexpr int SB = S16 ? 2 : 4, BB = B16 ? 2 : 4, LB = DT == CAPSCAPS_FP32 ? 4 : 2;
     __shared__ float lds[32];
     const int group = group_of<I>(P);
-    RowSum sum{lds, group, 0};
-    const int lane = threadIdx.x & (group - 1), slot = threadIdx.x / group;
+    const int slot = threadIdx.x / group, lane = threadIdx.x - slot * group;
+    RowSum sum{lds, group, slot, 0};
     const bool branch = A.branch != nullptr, has_h = A.dh != nullptr;
     const bool post = branch && B.post_norm && A.rstd_post != nullptr;
     const float inv_width = 1.0f / (float)B.width;
@@ -319,7 +320,7 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
-            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
+            const Share has{in && v < P.full, TAIL && in && v == P.part, P.tail};
             clear(y[i]);
             clear(dh[i]);
             if (has_h) {
@@ -335,7 +336,7 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
-            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
+            const Share has{in && v < P.full, TAIL && in && v == P.part, P.tail};
             clear(dy[i]);
             clear(b[i]);
             if (A.dy != nullptr) load<SD, N, TAIL>(dy[i], rdy.get(n, i * group, SB), has, rdy.over && !last);
@@ -375,7 +376,7 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const int v = lane + i * group;
-            const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
+            const Share has{in && v < P.full, TAIL && in && v == P.part, P.tail};
             float dx[N], dg[N], cb[N], wh[N];
             col.to_b(i, cb);
             col.to_h(i, wh);
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const int v = lane + i * group;
-                const Share has{in && v < P.full, TAIL && in && v == P.full, P.tail};
+                const Share has{in && v < P.full, TAIL && in && v == P.part, P.tail};
                 float db[N];
 #pragma unroll
                 for (int k = 0; k < N; ++k) db[k] = rpost * (e[i][k] - value<BD, N>(b[i], k) * rpost * mean);
@@ -450,7 +451,7 @@ __global__ void __launch_bounds__(widest_workgroup(I))
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             __syncthreads();
-            if ((int)(threadIdx.x & (wide - 1)) < group) {
+            if (group >= 64 || (int)(threadIdx.x & 63) < group) {
 #pragma unroll
                 for (int k = 0; k < N; ++k)
                     of_slot[threadIdx.x / wide * in_row + lane * N + k] = which == 0 ? sum_h[0][k] : sum_b[0][k];
@@ -694,10 +695,16 @@ RowPlan row_plan(const capscaps_block& B, int n, bool forward, bool apart)
     RowPlan P;
     P.n = n;
     const int vectors = (B.width + n - 1) / n;
-    P.group = apart ? 64 : 1;
-    while (P.group < vectors && P.group < 1024) P.group *= 2;
-    P.vectors = vectors <= P.group ? 1 : n == 4 && vectors <= 2 * P.group ? 2 : 32 / n;
-    if (P.vectors > 2) P.group = 512;
+    P.vectors = 1;
+    if (vectors <= 64) {
+        P.group = apart ? 64 : 1;
+        while (P.group < vectors) P.group *= 2;
+    } else if (vectors <= 1024) {
+        P.group = (vectors + 63) / 64 * 64;
+    } else {
+        P.vectors = n == 4 && vectors <= 2048 ? 2 : 32 / n;
+        P.group = widest_workgroup(P.vectors);
+    }
     const bool in_step = !forward || (vectors > 64 && (n == 8 || B.width > 2048));
     // Backward, rows within a wave that no vector divides: their accesses cross lines, and their waves wait
     // longer than others, so more of them, in smaller workgroups (2.1M rows of 27 fp32 values with a gate: 387
@@ -706,17 +713,18 @@ RowPlan row_plan(const capscaps_block& B, int n, bool forward, bool apart)
     const bool crossing = !forward && B.width % n != 0 && vectors <= 64;
     const int step = crossing ? 512 : 1024;
     // (several rows in such a workgroup where there are rows for every unit)
-    P.threads = in_step && P.vectors == 1 && B.rows * P.group >= (long long)step * CUS ? step : THREADS;
-    if (P.group > P.threads || apart) P.threads = P.group;
-    P.per_block = P.threads / P.group;
+    const int threads = in_step && B.rows * P.group >= (long long)step * CUS ? step : THREADS;
+    P.per_block = apart || P.group >= threads || P.vectors > 1 ? 1 : threads / P.group;
+    P.threads = P.per_block * P.group;
     const long long blocks = (B.rows + P.per_block - 1) / P.per_block;
     // (a launch has less than 2^32 threads)
     const int per_unit = forward ? 2048 : crossing && n == 4 ? 1536 : 1024;  // threads
-    const long long most = apart ? CUS : !in_step ? 1LL << 23 : (long long)CUS * per_unit / P.threads;
+    const long long most = apart ? CUS : !in_step ? 1LL << 23 : CUS * (per_unit / P.threads);
     P.blocks = (unsigned)(blocks < most ? blocks : most);
     P.turns = P.blocks < blocks;
     P.full = B.width / n;
     P.tail = B.width % n;
+    P.part = P.tail != 0 ? P.full : -1;
     return P;
 }
 bool rows_apart(std::initializer_list<long long> strides)
