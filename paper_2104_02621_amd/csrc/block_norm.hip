@@ -733,9 +733,13 @@ bool rows_apart(std::initializer_list<long long> strides)
         if (s > (1 << 18)) return true;  // 1024 rows of fp32 within 2^30 bytes
     return false;
 }
-int vector_values(const capscaps_block& B, bool branch)
+// Values of a vector.  An fp32 branch between 16-bit tensors is taken in eights too in the forward pass, whose waves
+// are many and short: half as many of them (us: 192544 rows of 400 values 140, in fours 186; 1.6M of 64 164 and 196;
+// 91557 of 2112, in turns, 352 and 335)
+int vector_values(const capscaps_block& B, bool branch, bool forward)
 {
-    return B.dtype != CAPSCAPS_FP32 && B.stream_dtype == B.dtype && (!branch || B.branch_dtype == B.dtype) ? 8 : 4;
+    const bool s16 = B.dtype != CAPSCAPS_FP32 && B.stream_dtype == B.dtype;
+    return s16 && (forward || !branch || B.branch_dtype == B.dtype) ? 8 : 4;
 }
 
 template <int V>
@@ -743,7 +747,7 @@ using Int = std::integral_constant<int, V>;
 
 // calls `launch` with the kernel's compile-time properties: stream and branch of 16 bits, a gate for every
 // value, values of a vector, vectors of a lane, a partial vector
-template <int DT, typename F>
+template <int DT, bool FORWARD, typename F>
 void with_properties(const capscaps_block& B, bool branch, const RowPlan& P, F launch)
 {
     const std::true_type yes;
@@ -752,7 +756,7 @@ void with_properties(const capscaps_block& B, bool branch, const RowPlan& P, F l
         P.tail ? launch(s, b, g, n, i, yes) : launch(s, b, g, n, i, no);
     };
     auto by_vectors = [&](auto s, auto b, auto g) {
-        if constexpr (s.value && b.value) {
+        if constexpr (s.value && (b.value || FORWARD)) {
             P.vectors == 1 ? by_tail(s, b, g, Int<8>(), Int<1>()) : by_tail(s, b, g, Int<8>(), Int<4>());
         } else {
             if (P.vectors == 1) by_tail(s, b, g, Int<4>(), Int<1>());
@@ -777,7 +781,7 @@ void with_properties(const capscaps_block& B, bool branch, const RowPlan& P, F l
 template <int DT>
 void launch_fwd(const capscaps_block& B, const capscaps_block_fwd_args& A, const RowPlan& P, hipStream_t st)
 {
-    with_properties<DT>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto n, auto i, auto tail) {
+    with_properties<DT, true>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto n, auto i, auto tail) {
         if constexpr (i.value == 1) {
             if (!P.turns) {
                 block_fwd_kernel<DT, s.value, b.value, g.value, n.value, i.value, tail.value, false>
@@ -794,7 +798,7 @@ hipError_t launch_bwd(const capscaps_block& B, const capscaps_block_bwd_args& A,
                       hipStream_t st)
 {
     hipError_t err = hipSuccess;
-    with_properties<DT>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto n, auto i, auto tail) {
+    with_properties<DT, false>(B, A.branch != nullptr, P, [&](auto s, auto b, auto g, auto n, auto i, auto tail) {
         const auto kernel = block_bwd_kernel<DT, s.value, b.value, g.value, n.value, i.value, tail.value>;
         const int lds = i.value == 1 ? 0 : P.group * i.value * n.value * 2 * 4;
         if (i.value > 1) {
@@ -842,7 +846,7 @@ int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fw
         block_fwd_any_kernel<<<dim3(row_blocks(B)), dim3(THREADS), 0, st>>>(B, A);
         return status_from_hip(hipGetLastError());
     }
-    const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), true, apart);
+    const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr, true), true, apart);
     if (B.dtype == CAPSCAPS_FP32)
         launch_fwd<CAPSCAPS_FP32>(B, A, P, st);
     else if (B.dtype == CAPSCAPS_BF16)
@@ -859,7 +863,7 @@ size_t capscaps_block_norm_bwd_workspace_bytes(const capscaps_block* block)
         size_t most = 0;
         for (const bool apart : {false, true})
             for (const bool branch : {false, true}) {
-                const RowPlan P = row_plan(*block, vector_values(*block, branch), false, apart);
+                const RowPlan P = row_plan(*block, vector_values(*block, branch, false), false, apart);
                 const size_t bytes = (size_t)P.blocks * 2 * P.vectors * P.group * P.n * 4;
                 most = bytes > most ? bytes : most;
             }
@@ -910,7 +914,7 @@ int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bw
     if (B.width <= WIDEST) {
         const bool apart = rows_apart({A.y_stride, A.branch_stride, A.gate_stride, A.dh_stride, A.dy_stride, A.dx_stride,
                                        A.dbranch_stride, A.dgate_stride});
-        const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr), false, apart);
+        const RowPlan P = row_plan(B, vector_values(B, A.branch != nullptr, false), false, apart);
         float* partial = sums ? static_cast<float*>(workspace) : nullptr;
         const hipError_t err = B.dtype == CAPSCAPS_FP32   ? launch_bwd<CAPSCAPS_FP32>(B, A, P, partial, st)
                                : B.dtype == CAPSCAPS_BF16 ? launch_bwd<CAPSCAPS_BF16>(B, A, P, partial, st)

@@ -1,6 +1,6 @@
 // Internal: rows of values of the three element types, some values a lane, at any address.
 //
-// A row's values are cut into vectors of N values, one of 16 bytes where all tensors of a call have 16-bit
+// A row's values are cut into vectors of N values: 16 bytes where (nearly) all tensors of a call have 16-bit
 // elements (N = 8), else N = 4: 16 bytes of fp32, 8 of a 16-bit type, so that a wave's access is one contiguous
 // piece in every type. They are loaded and stored whole at any alignment (the hardware takes such accesses at
 // element addresses). What a row's length leaves over (1 .. N - 1 values) is one lane's last vector.  It is
@@ -105,9 +105,12 @@ template <int DT, int N, bool TAIL>
 __device__ __forceinline__ void load(Raw<DT, N>& r, const char* p, const Share& has, bool over)
 {
     typedef Raw<DT, N> R;
-    if constexpr (!TAIL) {
+    if constexpr (!TAIL && R::WORDS <= 4) {
         // (lines that no other access of the wave touches, and that nothing reads again)
         if (has.full) r.w = __builtin_nontemporal_load(reinterpret_cast<const typename R::Whole*>(p));
+    } else if constexpr (!TAIL) {
+        // (eight fp32 values are two accesses that share lines)
+        if (has.full) r.w = *reinterpret_cast<const typename R::Whole*>(p);
     } else {
         if (has.full || (has.part && over)) r.w = *reinterpret_cast<const typename R::Whole*>(p);
         if (has.part && !over)
