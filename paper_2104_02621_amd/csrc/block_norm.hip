@@ -735,11 +735,12 @@ bool rows_apart(std::initializer_list<long long> strides)
 }
 // Values of a vector.  An fp32 branch between 16-bit tensors is taken in eights too in the forward pass, whose waves
 // are many and short: half as many of them (us: 192544 rows of 400 values 140, in fours 186; 1.6M of 64 164 and 196;
-// 91557 of 2112, in turns, 352 and 335)
+// 91557 of 2112, in turns, 352 and 335).  On the way back up to 8192 values, where it fits one vector a lane (733139 rows
+// of 280 507 and 754, 40685 of 4096 525 and 559, 1.6M of 64 246 and 236; 16384 of 10000 596 and 487)
 int vector_values(const capscaps_block& B, bool branch, bool forward)
 {
     const bool s16 = B.dtype != CAPSCAPS_FP32 && B.stream_dtype == B.dtype;
-    return s16 && (forward || !branch || B.branch_dtype == B.dtype) ? 8 : 4;
+    return s16 && (forward || !branch || B.branch_dtype == B.dtype || B.width <= 8192) ? 8 : 4;
 }
 
 template <int V>
@@ -758,6 +759,8 @@ void with_properties(const capscaps_block& B, bool branch, const RowPlan& P, F l
     auto by_vectors = [&](auto s, auto b, auto g) {
         if constexpr (s.value && (b.value || FORWARD)) {
             P.vectors == 1 ? by_tail(s, b, g, Int<8>(), Int<1>()) : by_tail(s, b, g, Int<8>(), Int<4>());
+        } else if constexpr (s.value) {
+            P.n == 8 ? by_tail(s, b, g, Int<8>(), Int<1>()) : by_tail(s, b, g, Int<4>(), Int<8>());
         } else {
             if (P.vectors == 1) by_tail(s, b, g, Int<4>(), Int<1>());
             if (P.vectors == 2) by_tail(s, b, g, Int<4>(), Int<2>());
