@@ -8,8 +8,8 @@
 // end.
 //
 // Measured (us; the bytes that must be moved at 6.2 TB/s in parentheses): forward, 65536 rows of 864 fp32 values
-// 155 (146), 6.4M rows of 64 bf16 values with a gate for each 669 (671), 65536 x 4096 bf16 383 (346); backward,
-// 16384 x 4096 fp32 and bf16 231 (217), 16384 x 16384 fp16 593 (520), 2.1M x 27 fp32 with a gate 388 (295).
+// 155 (146), 6.4M rows of 64 bf16 values with a gate for each 667 (671), 65536 x 4096 bf16 376 (346); backward,
+// 16384 x 4096 fp32 and bf16 230 (217), 16384 x 16384 fp16 591 (520), 2.1M x 27 fp32 with a gate 386 (295).
 #include <hip/hip_runtime.h>
 #include <float.h>
 #include <math.h>
