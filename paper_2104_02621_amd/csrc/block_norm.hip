@@ -108,7 +108,8 @@ struct Rows {
     const char* base;
     long long round;  // bytes of a workgroup's rows of one round
     unsigned at;
-    bool over;  // what follows a row, up to a vector, is the next one's or lies before it
+    // what follows a row, up to a vector, is the next row's or lies before it (it is masked: it may be written meanwhile)
+    bool over;
     template <typename T>
     __device__ __forceinline__ Rows(T* p, long long stride, int bytes, const RowPlan& P, int slot, int lane)
     {

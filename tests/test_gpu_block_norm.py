@@ -167,6 +167,23 @@ def test_strides_and_addresses(width, gap, shift, types):
     c.check_backward(c.backward())
 
 
+@pytest.mark.parametrize("width", [13, 64, 1027])
+def test_one_row_broadcast_to_many(width):
+    """Inputs of stride 0, and rows that overlap their neighbours: nothing behind the last value is read."""
+    c = Case(1, width, TYPES[1])
+    many = [t.expand(70, width) for t in (c.x, c.b, c.dh, c.dy)]
+    dense = [t.contiguous() for t in many]
+    stats = [torch.rsqrt(t.double().square().mean(1) + c.eps).float() for t in dense[:2]]
+    for a, b in zip(cc.block_norm_fwd(*many[:2], pre_weight=c.wpre), cc.block_norm_fwd(*dense[:2], pre_weight=c.wpre)):
+        assert a is None or torch.equal(a, b)
+    for a, b in zip(cc.block_norm_bwd(*many[:2], *stats, *many[2:], pre_weight=c.wpre),
+                    cc.block_norm_bwd(*dense[:2], *stats, *dense[2:], pre_weight=c.wpre)):
+        assert a is None or torch.equal(a, b)
+    line = torch.randn(width + 30, device="cuda").to(BF16)
+    sliding = line.as_strided((31, width), (1, 1))
+    assert torch.equal(cc.block_norm_fwd(sliding).h, cc.block_norm_fwd(sliding.contiguous()).h)
+
+
 def test_without_a_branch_and_with_one_gradient():
     for types in (TYPES[0], TYPES[2]):
         c = Case(19, 200, types, "shared")
