@@ -630,6 +630,16 @@ def _dense(t, what):
     return t.data_ptr()
 
 
+def _grad_codes(grads):
+    """Type codes of gradients that the library can read where they are.  (No call for each: lists are long, steps short.)"""
+    if not all([g.is_cuda and g.is_contiguous() for g in grads]):
+        raise ValueError("gradients must be contiguous device tensors")
+    try:
+        return [_codes[g.dtype] for g in grads]
+    except (KeyError, TypeError):  # a type of no code, or the first call: no codes yet
+        return [_code(g.dtype) for g in grads]
+
+
 def _control_ptr(control):
     if control is None:
         return None
@@ -651,7 +661,8 @@ def grad_norm(grads, max_norm=None, grad_scale=1.0, control=None, workspace=None
         control = torch.zeros(4, dtype=torch.float32, device=device)
     if workspace is None:
         workspace = torch.empty(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
-    items = (GradTensor * max(1, len(grads)))(*[(_dense(g, "gradients"), g.numel(), _code(g.dtype)) for g in grads])
+    items = (GradTensor * max(1, len(grads)))(
+        *[(g.data_ptr(), g.numel(), code) for g, code in zip(grads, _grad_codes(grads))])
     rc = capscaps_grad_norm(items, len(grads), grad_scale, 0.0 if max_norm is None else max_norm,
                             _control_ptr(control), workspace.data_ptr(), workspace.numel(),
                             _stream(device))
@@ -723,10 +734,10 @@ class AdamW:
         import torch
         if len(grads) != len(self._items):
             raise ValueError(f"{len(self._items)} parameters need as many gradients")
-        for t, g, n in zip(self._items, grads, self._sizes):
-            if g.numel() != n:
-                raise ValueError("gradients have the parameters' sizes")
-            t.grad, t.grad_dtype = _dense(g, "gradients"), _code(g.dtype)
+        if [g.numel() for g in grads] != self._sizes:
+            raise ValueError("gradients have the parameters' sizes")
+        for t, g, code in zip(self._items, grads, _grad_codes(grads)):
+            t.grad, t.grad_dtype = g.data_ptr(), code
         step = 0 if control is not None else self.steps + 1
         rc = capscaps_adamw_step(self._items, len(self._items), self.state_bits, self.lr if lr is None else lr,
                                  self.betas[0], self.betas[1], self.eps, step, self.seed & 0xFFFFFFFF,

@@ -92,7 +92,9 @@ bool misaligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_
 
 // ------------------------------------------------------------------------------------ gradient norm
 constexpr int NORM_TENSORS = 128;
-constexpr int NORM_SHARE = 16384;  // values that a workgroup sums at a time
+// Values that a workgroup sums at a time: as many as keep four loads of each lane under way for four turns, or for one where
+// that would leave units without work (7M values: 14 us, with the shorter shares 9)
+constexpr int NORM_SHARE = 16384, SHORT_SHARE = 4096;
 constexpr int NORM_SLOTS = CAPSCAPS_GRAD_NORM_WORKSPACE_BYTES / sizeof(double);
 
 struct NormList {
@@ -100,7 +102,7 @@ struct NormList {
     long long n[NORM_TENSORS];
     int first[NORM_TENSORS + 1];  // shares before the tensor
     unsigned char dtype[NORM_TENSORS];
-    int count;
+    int count, share;
 };
 
 __device__ __forceinline__ double block_sum(double v, double* lds)
@@ -117,7 +119,7 @@ __device__ __forceinline__ double block_sum(double v, double* lds)
 
 // A workgroup sums a share, four loads of 16 bytes of each lane under way at a time, in fp64 (a conversion and a product-sum
 // a value: half of what memory leaves time for).  113M values: 76 us at 6.0 TB/s; 4 us more for the launch that
-// sums the workgroups' sums.  7M values take 10 .. 14 us: less than two workgroups a unit.
+// sums the workgroups' sums.
 __global__ void __launch_bounds__(THREADS) grad_norm_kernel(NormList L, double* partial)
 {
     __shared__ double lds[THREADS / 64];
@@ -127,9 +129,9 @@ __global__ void __launch_bounds__(THREADS) grad_norm_kernel(NormList L, double* 
         const int t = tensor_of(L.first, L.count, share);
         const void* grad = L.grad[t];
         const int dtype = L.dtype[t];
-        const long long base = (long long)(share - L.first[t]) * NORM_SHARE, left = L.n[t] - base;
+        const long long base = (long long)(share - L.first[t]) * L.share, left = L.n[t] - base;
         constexpr int STEP = 4 * THREADS, UNROLL = 4;
-        for (int i = 4 * threadIdx.x; i < NORM_SHARE && i < left; i += UNROLL * STEP) {
+        for (int i = 4 * threadIdx.x; i < L.share && i < left; i += UNROLL * STEP) {
             float4v g[UNROLL];
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) {
@@ -543,7 +545,7 @@ int capscaps_grad_norm(const capscaps_grad_tensor* grads, int count, float grad_
     if (count < 0 || (count > 0 && grads == nullptr) || control == nullptr || misaligned(control, 16))
         return CAPSCAPS_EINVAL;
     if (!isfinite(grad_scale) || isnan(max_norm)) return CAPSCAPS_EINVAL;
-    long long used = 0, shares = 0;
+    long long used = 0, shares = 0, values = 0;
     for (int k = 0; k < count; ++k) {
         const capscaps_grad_tensor& g = grads[k];
         if (g.n < 0 || !known_dtype(g.dtype)) return CAPSCAPS_EINVAL;
@@ -551,6 +553,7 @@ int capscaps_grad_norm(const capscaps_grad_tensor* grads, int count, float grad_
         shares += g.n / NORM_SHARE + 1;
         if (shares > MOST_SHARES) return CAPSCAPS_EUNSUPPORTED;  // (so that every launch's can be counted)
         used += g.n > 0;
+        values += g.n;
     }
     if (workspace == nullptr || workspace_bytes < CAPSCAPS_GRAD_NORM_WORKSPACE_BYTES) return CAPSCAPS_EWORKSPACE;
     if (misaligned(workspace, 16)) return CAPSCAPS_EINVAL;
@@ -562,11 +565,12 @@ int capscaps_grad_norm(const capscaps_grad_tensor* grads, int count, float grad_
     int slots = 0;
     for (int k = 0; k < count;) {
         NormList L;
+        L.share = values < 2048LL * NORM_SHARE ? SHORT_SHARE : NORM_SHARE;
         L.count = 0;
         L.first[0] = 0;
         for (; k < count && L.count < NORM_TENSORS; ++k) {
             if (grads[k].n == 0) continue;
-            add_shares(L.first, L.count, grads[k].n, NORM_SHARE);
+            add_shares(L.first, L.count, grads[k].n, L.share);
             L.grad[L.count] = grads[k].grad;
             L.n[L.count] = grads[k].n;
             L.dtype[L.count] = (unsigned char)grads[k].dtype;
