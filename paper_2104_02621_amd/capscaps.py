@@ -679,7 +679,10 @@ class AdamW:
     parameters there, for the layers to read.  `state_bits`: 32 (float32 moments) or 8 (a byte for each, and a
     byte for each 256 values that share an exponent; rounded at random by a hash of `seed`, the step and the
     position).  `state`: moments to go on from, (m, v) or (m, v, m_exp, v_exp), lists of tensors in that format (those
-    of another AdamW, saved); kept, not copied; `steps`: the steps they have seen."""
+    of another AdamW, saved); kept, not copied; `steps`: the steps they have seen.
+
+    Tensors of `params`, `m`, `v`, `m_exp`, `v_exp` and `copies` may get other storage, or be replaced in the lists, between
+    steps (a captured step keeps the ones it was captured with)."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, state_bits=32, copies=None,
                  seed=0, state=None, steps=0):
@@ -692,9 +695,6 @@ class AdamW:
         count, eight = len(self.params), state_bits == 8
         self.lr, self.betas, self.eps, self.state_bits, self.seed = lr, betas, eps, state_bits, seed
         self.steps = steps
-        for p in self.params:
-            if p.dtype != torch.float32:
-                raise ValueError("parameters are float32")
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
         if isinstance(copies, torch.dtype):
             copies = [p.detach().to(copies) for p in self.params]
@@ -710,13 +710,23 @@ class AdamW:
                 raise ValueError("state is (m, v), or (m, v, m_exp, v_exp) in 8 bits")
             self.m, self.v, self.m_exp, self.v_exp = [list(s) for s in state] + (
                 [] if eight else [[None] * count, [None] * count])
-        if any(len(s) != count for s in (decay, self.copies, self.m, self.v, self.m_exp, self.v_exp)):
+        self._decay = decay
+        self._fill()
+
+    def _fill(self):
+        """Checks the tensors and writes the library's table of them."""
+        import torch
+        count, eight = len(self.params), self.state_bits == 8
+        if any(len(s) != count for s in (self._decay, self.copies, self.m, self.v, self.m_exp, self.v_exp)):
             raise ValueError(f"{count} parameters need as many copies, moments and decays")
+        self._held = None  # (nothing to step with if a check below fails)
         self._items = (AdamwTensor * count)()
         self._sizes = [p.numel() for p in self.params]
         for t, p, m, v, me, ve, c, d in zip(self._items, self.params, self.m, self.v, self.m_exp, self.v_exp,
-                                            self.copies, decay):
+                                            self.copies, self._decay):
             kind, n = (torch.uint8 if eight else torch.float32), p.numel()
+            if p.dtype != torch.float32:
+                raise ValueError("parameters are float32")
             if m.dtype != kind or v.dtype != kind or m.numel() != n or v.numel() != n:
                 raise ValueError(f"moments are {kind} of the parameters' sizes")
             if eight and any(e.dtype != torch.uint8 or e.numel() != (n + 255) // 256 for e in (me, ve)):
@@ -726,12 +736,25 @@ class AdamW:
             t.param, t.m, t.v, t.n, t.weight_decay = _dense(p, "parameters"), _dense(m, "moments"), _dense(v, "moments"), n, d
             t.m_exp, t.v_exp = (_dense(me, "exponents"), _dense(ve, "exponents")) if eight else (None, None)
             t.copy, t.copy_dtype = (None, BF16) if c is None else (_dense(c, "copies"), _code(c.dtype))
+        self._held = self._addresses()
+
+    def _addresses(self):
+        """Where the tensors lie now: storage may be replaced (`p.data = ...`), and so may entries of the lists."""
+        held = [*self.params, *self.m, *self.v]
+        if self.state_bits == 8:
+            held += [*self.m_exp, *self.v_exp]
+        return [t.data_ptr() for t in held] + [0 if c is None else c.data_ptr() for c in self.copies]
+
+    def _refresh(self):
+        """Before each call: the table is of the tensors as they are."""
+        if self._held != self._addresses() or not all([p.is_contiguous() for p in self.params]):
+            self._fill()
 
     def step(self, grads, control=None, lr=None):
         """One step with these gradients (float32, bfloat16 or float16, contiguous).  With `control`, what
         grad_norm returned: their scale, the number of the step and whether it is skipped come from there;
         without, steps are counted here.  Enqueues on torch's current stream."""
-        import torch
+        self._refresh()
         if len(grads) != len(self._items):
             raise ValueError(f"{len(self._items)} parameters need as many gradients")
         if [g.numel() for g in grads] != self._sizes:
@@ -753,6 +776,7 @@ class AdamW:
         import torch
         if self.state_bits == 32:
             return self.m, self.v
+        self._refresh()
         if out is None:
             out = [[torch.empty(p.shape, dtype=torch.bfloat16, device=p.device) for p in self.params]
                    for _ in range(2)]
