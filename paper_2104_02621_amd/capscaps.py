@@ -22,6 +22,7 @@ STATIC_SCRATCH_BYTES = 80 << 20
 GATE_NONE, GATE_SHARED, GATE_FULL = 0, 1, 2
 ACT_LINEAR, ACT_SIGMOID, ACT_SILU = 0, 1, 2
 GRAD_NORM_WORKSPACE_BYTES = 65536
+MOST_ROW_VALUES = 1 << 30
 
 # CAPSCAPS_SANITIZE=1 selects the build whose host code is instrumented (see build.py)
 _LIB_PATH = Path(__file__).resolve().parent / (
@@ -499,6 +500,8 @@ def _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scal
     if not 1 <= norm_dims <= len(shape) or x.numel() == 0:
         raise ValueError(f"{norm_dims} axes of a tensor of shape {tuple(shape)} are no rows")
     width = math.prod(shape[len(shape) - norm_dims:])
+    if width > MOST_ROW_VALUES:  # (a C int, to which ctypes would cut it without a word)
+        raise ValueError(f"rows of {width} values: up to 2^30 are supported")
     layer, stream = _code(dtype), _code(x.dtype)
     kind, gate_ptr, gate_stride = GATE_NONE, None, 0
     if gate is not None:
