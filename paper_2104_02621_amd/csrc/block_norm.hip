@@ -718,9 +718,10 @@ RowPlan row_plan(const capscaps_block& B, int n, bool forward, bool apart)
     P.per_block = apart || P.group >= threads || P.vectors > 1 ? 1 : threads / P.group;
     P.threads = P.per_block * P.group;
     const long long blocks = (B.rows + P.per_block - 1) / P.per_block;
-    // (a launch has less than 2^32 threads)
+    // (a launch has less than 2^32 threads, and rows of 1793 .. 2048 values in fours are workgroups of 512)
+    const long long as_they_come = (1LL << 23) - 1;
     const int per_unit = forward ? 2048 : crossing && n == 4 ? 1536 : 1024;  // threads
-    const long long most = apart ? CUS : !in_step ? 1LL << 23 : CUS * (per_unit / P.threads);
+    const long long most = apart ? CUS : !in_step ? as_they_come : CUS * (per_unit / P.threads);
     P.blocks = (unsigned)(blocks < most ? blocks : most);
     P.turns = P.blocks < blocks;
     P.full = B.width / n;
@@ -858,6 +859,17 @@ int capscaps_block_norm_fwd(const capscaps_block* block, const capscaps_block_fw
     else
         launch_fwd<CAPSCAPS_FP16>(B, A, P, st);
     return status_from_hip(hipGetLastError());
+}
+
+// (for tests) workgroups and threads of the launch for rows of up to 16384 values; 0: an invalid block, or wider rows
+int capscaps_testing_block_norm_launch(const capscaps_block* block, int branch, int forward, int apart,
+                                       long long* workgroups_threads)
+{
+    if (check_block(block) != CAPSCAPS_OK || block->width > WIDEST) return 0;
+    const RowPlan P = row_plan(*block, vector_values(*block, branch != 0, forward != 0), forward != 0, apart != 0);
+    workgroups_threads[0] = P.blocks;
+    workgroups_threads[1] = P.threads;
+    return 1;
 }
 
 size_t capscaps_block_norm_bwd_workspace_bytes(const capscaps_block* block)
