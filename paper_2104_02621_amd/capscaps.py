@@ -655,13 +655,16 @@ def grad_norm(grads, max_norm=None, grad_scale=1.0, control=None, workspace=None
     """The 2-norm of all gradients together, on the device: writes `control`, four values of 4 bytes that AdamW.step
     reads: the norm (of grad_scale * gradients), the factor that scales and clips the gradients to `max_norm`
     (None: no clipping), whether the step is to be skipped because the norm is not finite (int32), and the number of steps
-    not skipped so far (int32, counted up here; make `control` of zeros).  Returns it."""
+    not skipped so far (int32, counted up here).  Returns it.  `control`: an optimizer's `control`, or a tensor of zeros
+    that is kept for the whole training.  Without one a new tensor is returned, for this step alone: it counts nothing
+    but this step, and AdamW.step counts the steps itself then."""
     import torch
     if not grads and control is None:
         raise ValueError("grad_norm of no tensors needs a control to write to")
     device = control.device if control is not None else grads[0].device
     if control is None:
         control = torch.zeros(4, dtype=torch.float32, device=device)
+        control.capscaps_for_one_step = True
     if workspace is None:
         workspace = torch.empty(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
     items = (GradTensor * max(1, len(grads)))(
@@ -682,7 +685,13 @@ class AdamW:
     parameters there, for the layers to read.  `state_bits`: 32 (float32 moments) or 8 (a byte for each, and a
     byte for each 256 values that share an exponent; rounded at random by a hash of `seed`, the step and the
     position).  `state`: moments to go on from, (m, v) or (m, v, m_exp, v_exp), lists of tensors in that format (those
-    of another AdamW, saved); kept, not copied; `steps`: the steps they have seen.
+    of another AdamW, saved); kept, not copied; `steps`: the steps they have seen (`steps` of that AdamW).
+
+    Steps are counted on the host, or, so that one that is not finite can be skipped without waiting for the GPU, on the
+    device.  For the latter give `step` what grad_norm returned: grad_norm(grads, max_norm, control=opt.control) counts in
+    `control`, the optimizer's own, which begins at `steps`; grad_norm(grads, max_norm) leaves the counting to `step`. A
+    control of the caller's own counts by itself, from zero, and is refused by an optimizer that has counted steps
+    otherwise.  `steps` is the number of steps taken either way (on the device, reading it waits for the GPU).
 
     Tensors of `params`, `m`, `v`, `m_exp`, `v_exp` and `copies` may get other storage, or be replaced in the lists, between
     steps (a captured step keeps the ones it was captured with)."""
@@ -697,6 +706,7 @@ class AdamW:
             raise ValueError("AdamW needs parameters")
         count, eight = len(self.params), state_bits == 8
         self.lr, self.betas, self.eps, self.state_bits, self.seed = lr, betas, eps, state_bits, seed
+        self._control, self._int32 = torch.zeros(4, dtype=torch.float32, device=self.params[0].device), torch.int32
         self.steps = steps
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
         if isinstance(copies, torch.dtype):
@@ -713,7 +723,7 @@ class AdamW:
                 raise ValueError("state is (m, v), or (m, v, m_exp, v_exp) in 8 bits")
             self.m, self.v, self.m_exp, self.v_exp = [list(s) for s in state] + (
                 [] if eight else [[None] * count, [None] * count])
-        self._decay = decay
+        self._decay, self._address = decay, torch.Tensor.data_ptr
         self._fill()
 
     def _fill(self):
@@ -746,7 +756,7 @@ class AdamW:
         held = [*self.params, *self.m, *self.v]
         if self.state_bits == 8:
             held += [*self.m_exp, *self.v_exp]
-        return [t.data_ptr() for t in held] + [0 if c is None else c.data_ptr() for c in self.copies]
+        return [*map(self._address, held)] + [0 if c is None else c.data_ptr() for c in self.copies]
 
     def _refresh(self):
         """Before each call: the table is of the tensors as they are."""
@@ -764,14 +774,67 @@ class AdamW:
             raise ValueError("gradients have the parameters' sizes")
         for t, g, code in zip(self._items, grads, _grad_codes(grads)):
             t.grad, t.grad_dtype = g.data_ptr(), code
-        step = 0 if control is not None else self.steps + 1
+        step = self.steps + 1 if control is None else 0
+        counter = None if control is None else _control_ptr(self._counting(control))
         rc = capscaps_adamw_step(self._items, len(self._items), self.state_bits, self.lr if lr is None else lr,
                                  self.betas[0], self.betas[1], self.eps, step, self.seed & 0xFFFFFFFF,
-                                 _control_ptr(control), _stream(self.params[0].device))
+                                 counter, _stream(self.params[0].device))
         if rc != OK:
             raise CapscapsError(rc)
-        if control is None:
-            self.steps = step
+        if control is None:  # what the optimizer's control has not counted
+            if self._counter is not None:
+                self._lacking = 0 if self._counter is self._control else step - 1
+            self._lacking += 1
+            self._host, self._counter = step, None
+
+    def _counting(self, control):
+        """The control that counts this step, for the one that `step` was given."""
+        if control is self._counter:
+            return control
+        own, single = self._control, getattr(control, "capscaps_for_one_step", False)
+        _control_ptr(control)
+        if not single and control.data_ptr() != own.data_ptr():
+            if self._counter is own or self._host:
+                raise ValueError("this optimizer has counted steps without this control: give grad_norm the "
+                                 "optimizer's `control`, or none")
+            self._counter = control
+            return control
+        if self._counter is not None and self._counter is not own:  # the caller's has counted until now
+            self._lacking = self.steps
+        self._catch_up()
+        if single:
+            own[:3].copy_(control[:3])
+            own.view(self._int32)[3:].add_(control.view(self._int32)[2:3] == 0)
+        self._counter = own
+        return own
+
+    def _catch_up(self):
+        """Counts in the optimizer's control the steps that were counted elsewhere."""
+        import torch
+        if not self._lacking:
+            return
+        if torch.cuda.is_current_stream_capturing():  # (each replay would count them again)
+            raise RuntimeError("steps have been counted on the host: read the optimizer's `control` once before the capture")
+        self._control.view(torch.int32)[3:].add_(self._lacking)
+        self._lacking = 0
+
+    @property
+    def control(self):
+        """The optimizer's own control, for grad_norm to write: it counts the steps on the device."""
+        self._catch_up()
+        return self._control
+
+    @property
+    def steps(self):
+        """Steps taken.  Where the device counts them, this waits for it."""
+        if self._counter is None:
+            return self._host
+        return self._counter.cpu().flatten().view(self._int32)[3].item()
+
+    @steps.setter
+    def steps(self, steps):
+        self._host, self._counter, self._lacking = steps, None, 0
+        self._control.view(self._int32)[3] = steps
 
     def state_values(self, out=None):
         """The moments (m, v) as lists of tensors; in 8 bits, the values their codes stand for, in bfloat16, which

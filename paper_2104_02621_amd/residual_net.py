@@ -42,7 +42,7 @@ class ResidualCapsNet:
         vectors = len(self.params) - len(self.kernels)
         self.opt = cc.AdamW(self.params, lr=lr, state_bits=state_bits, seed=seed, copies=low + [None] * vectors,
                             weight_decay=[weight_decay] * len(self.kernels) + [0.0] * vectors)
-        self.control = torch.zeros(4, device="cuda")
+        self.control = self.opt.control
 
     def forward(self, images, save=False):
         """Poses; with `save` also what `backward` needs."""

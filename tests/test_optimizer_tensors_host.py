@@ -109,3 +109,16 @@ def test_replaced_tensors_are_checked(calls, bits):
         calls.clear()
         opt.params[0].data = opt.params[0].data.t()    # same address, values in another order
     refused(strided, "contiguous")
+
+
+def test_a_capture_does_not_count_the_steps_before_it(calls, monkeypatch):
+    """Steps that were counted on the host are added to the optimizer's control once, not by each replay of a graph."""
+    opt = make(32)
+    opt.step([on_gpu(n) for n in SIZES])
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="before the capture"):
+        opt.control
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    assert opt.control.view(torch.int32)[3] == 1
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    assert opt.control.view(torch.int32)[3] == 1
