@@ -460,13 +460,14 @@ def _code(dtype):
         raise ValueError(f"{dtype}: float32, bfloat16 and float16 are supported") from None
 
 
-def _row_stride(t, shape, width, norm_dims, name):
+def _row_stride(t, shape, width, norm_dims, name, gpu):
     """Distance between the rows of `t`, whose last `norm_dims` axes are one dense row and whose other axes follow
-    each other at equal distances."""
-    if t.is_cuda and t.shape == shape and t.is_contiguous():
+    each other at equal distances.  `gpu`: where it has to be."""
+    if t.get_device() != gpu or not t.is_cuda:
+        raise ValueError("capscaps runs on the GPU only: pass device tensors" if not t.is_cuda else
+                         f"{name} is not on the GPU that the other tensors are on")
+    if t.shape == shape and t.is_contiguous():
         return width
-    if not t.is_cuda:
-        raise ValueError("capscaps runs on the GPU only: pass device tensors")
     if t.shape != shape:
         raise ValueError(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
     strides, dense = t.stride(), 1
@@ -508,7 +509,7 @@ def _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scal
         if gate.shape == shape and gate.dim() > norm_dims:
             if gate.dtype != dtype:
                 raise ValueError(f"a gate for every value must be {dtype}")
-            kind, gate_stride = GATE_FULL, _row_stride(gate, shape, width, norm_dims, "gate")
+            kind, gate_stride = GATE_FULL, _row_stride(gate, shape, width, norm_dims, "gate", x.get_device())
             gate_ptr = gate.data_ptr()
         else:
             kind, gate_ptr = GATE_SHARED, _vector(gate, width, x.device, "gate")
@@ -516,7 +517,7 @@ def _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scal
         raise ValueError(f"gate_act is one of {', '.join(_ACTS)}")
     branch_ptr, branch_stride, branch_code = None, 0, FP32
     if branch is not None:
-        branch_stride = _row_stride(branch, shape, width, norm_dims, "branch")
+        branch_stride = _row_stride(branch, shape, width, norm_dims, "branch", x.get_device())
         branch_ptr, branch_code = branch.data_ptr(), _code(branch.dtype)
     elif gate is not None:
         raise ValueError("a gate needs a branch")
@@ -548,8 +549,8 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
     dtype = x.dtype if dtype is None else dtype
     block, bp, bs, gp, gs = _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scale,
                                    branch_scale, eps)
-    shape, width, device = x.shape, block.width, x.device
-    xs = _row_stride(x, shape, width, norm_dims, "x")
+    shape, width, device, gpu = x.shape, block.width, x.device, x.get_device()
+    xs = _row_stride(x, shape, width, norm_dims, "x", gpu)
     if branch is None:
         if y is not None:
             raise ValueError("without a branch there is no y")
@@ -570,8 +571,8 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
         _vector(post_weight, width, device, "post_weight"), None if y is None else y.data_ptr(),
         None if h is None else h.data_ptr(), None if rpre is None else rpre.data_ptr(),
         None if rpost is None else rpost.data_ptr(), xs, bs, gs,
-        0 if y is None else _row_stride(y, shape, width, norm_dims, "y"),
-        0 if h is None else _row_stride(h, shape, width, norm_dims, "h"))
+        0 if y is None else _row_stride(y, shape, width, norm_dims, "y", gpu),
+        0 if h is None else _row_stride(h, shape, width, norm_dims, "h", gpu))
     rc = capscaps_block_norm_fwd(block, args, _stream(device))
     if rc != OK:
         raise CapscapsError(rc)
@@ -592,7 +593,7 @@ def block_norm_bwd(y, branch, rstd_pre, rstd_post, dh, dy, *, pre_weight=None, p
         dtype = y.dtype if dh is None else dh.dtype
     block, bp, bs, gp, gs = _block(y, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scale,
                                    branch_scale, 1.0)
-    shape, width, device = y.shape, block.width, y.device
+    shape, width, device, gpu = y.shape, block.width, y.device, y.get_device()
     if dh is not None and dh.dtype != dtype or dy is not None and dy.dtype != y.dtype:
         raise ValueError("dh has `dtype`, dy has y's type")
     post = branch is not None and post_norm
@@ -617,9 +618,9 @@ def block_norm_bwd(y, branch, rstd_pre, rstd_post, dh, dy, *, pre_weight=None, p
         None if dh is None else dh.data_ptr(), None if dy is None else dy.data_ptr(), dx.data_ptr(),
         None if db is None else db.data_ptr(), None if dgate is None else dgate.data_ptr(),
         None if dpre is None else dpre.data_ptr(), None if dpost is None else dpost.data_ptr(),
-        _row_stride(y, shape, width, norm_dims, "y"), bs, gs,
-        0 if dh is None else _row_stride(dh, shape, width, norm_dims, "dh"),
-        0 if dy is None else _row_stride(dy, shape, width, norm_dims, "dy"), width, width, width)
+        _row_stride(y, shape, width, norm_dims, "y", gpu), bs, gs,
+        0 if dh is None else _row_stride(dh, shape, width, norm_dims, "dh", gpu),
+        0 if dy is None else _row_stride(dy, shape, width, norm_dims, "dy", gpu), width, width, width)
     rc = capscaps_block_norm_bwd(block, args, ws.data_ptr(), need, _stream(device))
     if rc != OK:
         raise CapscapsError(rc)
@@ -627,28 +628,29 @@ def block_norm_bwd(y, branch, rstd_pre, rstd_post, dh, dy, *, pre_weight=None, p
 
 
 # ------------------------------------------------------------------ gradient norm, AdamW
-def _dense(t, what):
+def _dense(t, what, gpu):
+    """Address of a contiguous tensor on that GPU."""
     if not (t.is_cuda and t.is_contiguous()):
         raise ValueError(f"{what} must be contiguous device tensors")
+    if t.get_device() != gpu:
+        raise ValueError(f"{what} must be on one GPU")
     return t.data_ptr()
 
 
-def _grad_codes(grads):
+def _grad_codes(grads, gpu):
     """Type codes of gradients that the library can read where they are.  (No call for each: lists are long, steps short.)"""
-    if not all([g.is_cuda and g.is_contiguous() for g in grads]):
-        raise ValueError("gradients must be contiguous device tensors")
+    if not all([g.get_device() == gpu and g.is_contiguous() for g in grads]) or (grads and not grads[0].is_cuda):
+        raise ValueError("gradients must be contiguous device tensors, on the GPU of the other tensors")
     try:
         return [_codes[g.dtype] for g in grads]
     except (KeyError, TypeError):  # a type of no code, or the first call: no codes yet
         return [_code(g.dtype) for g in grads]
 
 
-def _control_ptr(control):
-    if control is None:
-        return None
+def _control_ptr(control, gpu):
     if control.element_size() * control.numel() != 16:
         raise ValueError("control is 16 bytes: norm, scale (float32), skip, step (int32)")
-    return _dense(control, "control")
+    return _dense(control, "control and gradients", gpu)
 
 
 def grad_norm(grads, max_norm=None, grad_scale=1.0, control=None, workspace=None):
@@ -661,16 +663,20 @@ def grad_norm(grads, max_norm=None, grad_scale=1.0, control=None, workspace=None
     import torch
     if not grads and control is None:
         raise ValueError("grad_norm of no tensors needs a control to write to")
-    device = control.device if control is not None else grads[0].device
+    first = control if control is not None else grads[0]
+    device, gpu = first.device, first.get_device()
+    codes = _grad_codes(grads, gpu)
     if control is None:
         control = torch.zeros(4, dtype=torch.float32, device=device)
         control.capscaps_for_one_step = True
     if workspace is None:
         workspace = torch.empty(GRAD_NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+    elif workspace.get_device() != gpu or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the gradients' GPU")
     items = (GradTensor * max(1, len(grads)))(
-        *[(g.data_ptr(), g.numel(), code) for g, code in zip(grads, _grad_codes(grads))])
+        *[(g.data_ptr(), g.numel(), code) for g, code in zip(grads, codes)])
     rc = capscaps_grad_norm(items, len(grads), grad_scale, 0.0 if max_norm is None else max_norm,
-                            _control_ptr(control), workspace.data_ptr(), workspace.numel(),
+                            _control_ptr(control, gpu), workspace.data_ptr(), workspace.numel(),
                             _stream(device))
     if rc != OK:
         raise CapscapsError(rc)
@@ -723,7 +729,8 @@ class AdamW:
                 raise ValueError("state is (m, v), or (m, v, m_exp, v_exp) in 8 bits")
             self.m, self.v, self.m_exp, self.v_exp = [list(s) for s in state] + (
                 [] if eight else [[None] * count, [None] * count])
-        self._decay, self._address = decay, torch.Tensor.data_ptr
+        # (methods of the class, to map over lists: these are long, steps short)
+        self._decay, self._address, self._contiguous = decay, torch.Tensor.data_ptr, torch.Tensor.is_contiguous
         self._fill()
 
     def _fill(self):
@@ -733,6 +740,7 @@ class AdamW:
         if any(len(s) != count for s in (self._decay, self.copies, self.m, self.v, self.m_exp, self.v_exp)):
             raise ValueError(f"{count} parameters need as many copies, moments and decays")
         self._held = None  # (nothing to step with if a check below fails)
+        self._gpu = gpu = self.params[0].get_device()
         self._items = (AdamwTensor * count)()
         self._sizes = [p.numel() for p in self.params]
         for t, p, m, v, me, ve, c, d in zip(self._items, self.params, self.m, self.v, self.m_exp, self.v_exp,
@@ -746,9 +754,14 @@ class AdamW:
                 raise ValueError("exponents are bytes, one for each 256 values")
             if c is not None and (c.numel() != n or _code(c.dtype) == FP32):
                 raise ValueError("copies are 16-bit tensors of the parameters' sizes")
-            t.param, t.m, t.v, t.n, t.weight_decay = _dense(p, "parameters"), _dense(m, "moments"), _dense(v, "moments"), n, d
-            t.m_exp, t.v_exp = (_dense(me, "exponents"), _dense(ve, "exponents")) if eight else (None, None)
-            t.copy, t.copy_dtype = (None, BF16) if c is None else (_dense(c, "copies"), _code(c.dtype))
+            t.param, t.n, t.weight_decay = _dense(p, "parameters", gpu), n, d
+            t.m, t.v = _dense(m, "parameters and moments", gpu), _dense(v, "parameters and moments", gpu)
+            t.m_exp, t.v_exp = [_dense(e, "parameters and exponents", gpu) for e in (me, ve)] if eight else (None, None)
+            t.copy, t.copy_dtype = (None, BF16) if c is None else (_dense(c, "parameters and copies", gpu), _code(c.dtype))
+        if self._control.get_device() != gpu:  # the parameters moved
+            own = self._counter is self._control
+            self._control = self._control.to(self.params[0].device)
+            self._counter = self._control if own else self._counter
         self._held = self._addresses()
 
     def _addresses(self):
@@ -760,7 +773,7 @@ class AdamW:
 
     def _refresh(self):
         """Before each call: the table is of the tensors as they are."""
-        if self._held != self._addresses() or not all([p.is_contiguous() for p in self.params]):
+        if self._held != self._addresses() or not all(map(self._contiguous, self.params)):
             self._fill()
 
     def step(self, grads, control=None, lr=None):
@@ -772,10 +785,10 @@ class AdamW:
             raise ValueError(f"{len(self._items)} parameters need as many gradients")
         if [g.numel() for g in grads] != self._sizes:
             raise ValueError("gradients have the parameters' sizes")
-        for t, g, code in zip(self._items, grads, _grad_codes(grads)):
-            t.grad, t.grad_dtype = g.data_ptr(), code
+        for t, at, code in zip(self._items, map(self._address, grads), _grad_codes(grads, self._gpu)):
+            t.grad, t.grad_dtype = at, code
         step = self.steps + 1 if control is None else 0
-        counter = None if control is None else _control_ptr(self._counting(control))
+        counter = None if control is None else _control_ptr(self._counting(control), self._gpu)
         rc = capscaps_adamw_step(self._items, len(self._items), self.state_bits, self.lr if lr is None else lr,
                                  self.betas[0], self.betas[1], self.eps, step, self.seed & 0xFFFFFFFF,
                                  counter, _stream(self.params[0].device))
@@ -792,7 +805,7 @@ class AdamW:
         if control is self._counter:
             return control
         own, single = self._control, getattr(control, "capscaps_for_one_step", False)
-        _control_ptr(control)
+        _control_ptr(control, self._gpu)
         if not single and control.data_ptr() != own.data_ptr():
             if self._counter is own or self._host:
                 raise ValueError("this optimizer has counted steps without this control: give grad_norm the "
@@ -850,7 +863,7 @@ class AdamW:
             if t.dtype != torch.bfloat16 or t.numel() != n:
                 raise ValueError("moments' values are bfloat16 of the parameters' sizes")
         count = len(self._items)
-        pointers = [(ctypes.c_void_p * count)(*[_dense(t, "values") for t in o]) for o in out]
+        pointers = [(ctypes.c_void_p * count)(*[_dense(t, "parameters and values", self._gpu) for t in o]) for o in out]
         rc = capscaps_adamw_state_values(self._items, count, pointers[0], pointers[1],
                                          _stream(self.params[0].device))
         if rc != OK:
