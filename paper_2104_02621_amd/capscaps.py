@@ -448,6 +448,25 @@ def _stream(device):
     return _raw_stream(device.index)
 
 
+def _current_gpu():
+    """Index of torch's current GPU, the one that kernels go to, whatever the stream."""
+    global _current_gpu
+    import torch
+    _current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _current_gpu()
+
+
+def _enqueue(call, device, *args):
+    """A call of the library on torch's current stream of the tensors' GPU, made the current one where it is not."""
+    if _current_gpu() != device.index:
+        import torch
+        with torch.cuda.device(device):
+            return _enqueue(call, device, *args)
+    rc = call(*args, _stream(device))
+    if rc != OK:
+        raise CapscapsError(rc)
+
+
 def _code(dtype):
     """The library's code of a torch dtype."""
     global _codes
@@ -460,12 +479,17 @@ def _code(dtype):
         raise ValueError(f"{dtype}: float32, bfloat16 and float16 are supported") from None
 
 
+def _gpu_of(t):
+    if not t.is_cuda:
+        raise ValueError("capscaps runs on the GPU only: pass device tensors")
+    return t.get_device()
+
+
 def _row_stride(t, shape, width, norm_dims, name, gpu):
     """Distance between the rows of `t`, whose last `norm_dims` axes are one dense row and whose other axes follow
-    each other at equal distances.  `gpu`: where it has to be."""
-    if t.get_device() != gpu or not t.is_cuda:
-        raise ValueError("capscaps runs on the GPU only: pass device tensors" if not t.is_cuda else
-                         f"{name} is not on the GPU that the other tensors are on")
+    each other at equal distances; it has to be on that `gpu`."""
+    if t.get_device() != gpu:
+        raise ValueError(f"{name} is not on the GPU that the other tensors are on")
     if t.shape == shape and t.is_contiguous():
         return width
     if t.shape != shape:
@@ -509,7 +533,7 @@ def _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scal
         if gate.shape == shape and gate.dim() > norm_dims:
             if gate.dtype != dtype:
                 raise ValueError(f"a gate for every value must be {dtype}")
-            kind, gate_stride = GATE_FULL, _row_stride(gate, shape, width, norm_dims, "gate", x.get_device())
+            kind, gate_stride = GATE_FULL, _row_stride(gate, shape, width, norm_dims, "gate", _gpu_of(x))
             gate_ptr = gate.data_ptr()
         else:
             kind, gate_ptr = GATE_SHARED, _vector(gate, width, x.device, "gate")
@@ -517,7 +541,7 @@ def _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scal
         raise ValueError(f"gate_act is one of {', '.join(_ACTS)}")
     branch_ptr, branch_stride, branch_code = None, 0, FP32
     if branch is not None:
-        branch_stride = _row_stride(branch, shape, width, norm_dims, "branch", x.get_device())
+        branch_stride = _row_stride(branch, shape, width, norm_dims, "branch", _gpu_of(x))
         branch_ptr, branch_code = branch.data_ptr(), _code(branch.dtype)
     elif gate is not None:
         raise ValueError("a gate needs a branch")
@@ -549,17 +573,18 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
     dtype = x.dtype if dtype is None else dtype
     block, bp, bs, gp, gs = _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scale,
                                    branch_scale, eps)
-    shape, width, device, gpu = x.shape, block.width, x.device, x.get_device()
+    shape, width, device, gpu = x.shape, block.width, x.device, _gpu_of(x)
     xs = _row_stride(x, shape, width, norm_dims, "x", gpu)
-    if branch is None:
-        if y is not None:
-            raise ValueError("without a branch there is no y")
-    elif y is None and want_y:
+    if branch is None and y is not None:
+        raise ValueError("without a branch there is no y")
+    if y is not None and y.dtype != x.dtype or h is not None and h.dtype != dtype:
+        raise ValueError("y has x's type, h has `dtype`")
+    ys = width if y is None else _row_stride(y, shape, width, norm_dims, "y", gpu)
+    hs = width if h is None else _row_stride(h, shape, width, norm_dims, "h", gpu)
+    if y is None and want_y and branch is not None:
         y = torch.empty_like(x, memory_format=torch.contiguous_format)
     if h is None and want_h:
         h = torch.empty(shape, dtype=dtype, device=device)
-    if y is not None and y.dtype != x.dtype or h is not None and h.dtype != dtype:
-        raise ValueError("y has x's type, h has `dtype`")
     rpre = rpost = None
     if save:
         if h is not None:
@@ -570,12 +595,8 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
         x.data_ptr(), bp, gp, _vector(pre_weight, width, device, "pre_weight"),
         _vector(post_weight, width, device, "post_weight"), None if y is None else y.data_ptr(),
         None if h is None else h.data_ptr(), None if rpre is None else rpre.data_ptr(),
-        None if rpost is None else rpost.data_ptr(), xs, bs, gs,
-        0 if y is None else _row_stride(y, shape, width, norm_dims, "y", gpu),
-        0 if h is None else _row_stride(h, shape, width, norm_dims, "h", gpu))
-    rc = capscaps_block_norm_fwd(block, args, _stream(device))
-    if rc != OK:
-        raise CapscapsError(rc)
+        None if rpost is None else rpost.data_ptr(), xs, bs, gs, ys, hs)
+    _enqueue(capscaps_block_norm_fwd, device, block, args)
     return BlockNorm(y, h, rpre, rpost)
 
 
@@ -593,7 +614,7 @@ def block_norm_bwd(y, branch, rstd_pre, rstd_post, dh, dy, *, pre_weight=None, p
         dtype = y.dtype if dh is None else dh.dtype
     block, bp, bs, gp, gs = _block(y, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scale,
                                    branch_scale, 1.0)
-    shape, width, device, gpu = y.shape, block.width, y.device, y.get_device()
+    shape, width, device, gpu = y.shape, block.width, y.device, _gpu_of(y)
     if dh is not None and dh.dtype != dtype or dy is not None and dy.dtype != y.dtype:
         raise ValueError("dh has `dtype`, dy has y's type")
     post = branch is not None and post_norm
@@ -621,9 +642,7 @@ def block_norm_bwd(y, branch, rstd_pre, rstd_post, dh, dy, *, pre_weight=None, p
         _row_stride(y, shape, width, norm_dims, "y", gpu), bs, gs,
         0 if dh is None else _row_stride(dh, shape, width, norm_dims, "dh", gpu),
         0 if dy is None else _row_stride(dy, shape, width, norm_dims, "dy", gpu), width, width, width)
-    rc = capscaps_block_norm_bwd(block, args, ws.data_ptr(), need, _stream(device))
-    if rc != OK:
-        raise CapscapsError(rc)
+    _enqueue(capscaps_block_norm_bwd, device, block, args, ws.data_ptr(), need)
     return BlockNormGrads(dx, db, dpre, dpost, dgate)
 
 
@@ -648,7 +667,7 @@ def _grad_codes(grads, gpu):
 
 
 def _control_ptr(control, gpu):
-    if control.element_size() * control.numel() != 16:
+    if control.nbytes != 16:
         raise ValueError("control is 16 bytes: norm, scale (float32), skip, step (int32)")
     return _dense(control, "control and gradients", gpu)
 
@@ -675,11 +694,8 @@ def grad_norm(grads, max_norm=None, grad_scale=1.0, control=None, workspace=None
         raise ValueError("workspace must be a contiguous tensor on the gradients' GPU")
     items = (GradTensor * max(1, len(grads)))(
         *[(g.data_ptr(), g.numel(), code) for g, code in zip(grads, codes)])
-    rc = capscaps_grad_norm(items, len(grads), grad_scale, 0.0 if max_norm is None else max_norm,
-                            _control_ptr(control, gpu), workspace.data_ptr(), workspace.numel(),
-                            _stream(device))
-    if rc != OK:
-        raise CapscapsError(rc)
+    _enqueue(capscaps_grad_norm, device, items, len(grads), grad_scale, 0.0 if max_norm is None else max_norm,
+             _control_ptr(control, gpu), workspace.data_ptr(), workspace.numel())
     return control
 
 
@@ -740,7 +756,8 @@ class AdamW:
         if any(len(s) != count for s in (self._decay, self.copies, self.m, self.v, self.m_exp, self.v_exp)):
             raise ValueError(f"{count} parameters need as many copies, moments and decays")
         self._held = None  # (nothing to step with if a check below fails)
-        self._gpu = gpu = self.params[0].get_device()
+        self._device, self._gpu = self.params[0].device, self.params[0].get_device()
+        gpu = self._gpu
         self._items = (AdamwTensor * count)()
         self._sizes = [p.numel() for p in self.params]
         for t, p, m, v, me, ve, c, d in zip(self._items, self.params, self.m, self.v, self.m_exp, self.v_exp,
@@ -781,6 +798,10 @@ class AdamW:
         grad_norm returned: their scale, the number of the step and whether it is skipped come from there;
         without, steps are counted here.  Enqueues on torch's current stream."""
         self._refresh()
+        if _current_gpu() != self._device.index:
+            import torch
+            with torch.cuda.device(self._device):
+                return self.step(grads, control, lr)
         if len(grads) != len(self._items):
             raise ValueError(f"{len(self._items)} parameters need as many gradients")
         if [g.numel() for g in grads] != self._sizes:
@@ -790,8 +811,8 @@ class AdamW:
         step = self.steps + 1 if control is None else 0
         counter = None if control is None else _control_ptr(self._counting(control), self._gpu)
         rc = capscaps_adamw_step(self._items, len(self._items), self.state_bits, self.lr if lr is None else lr,
-                                 self.betas[0], self.betas[1], self.eps, step, self.seed & 0xFFFFFFFF,
-                                 counter, _stream(self.params[0].device))
+                                 self.betas[0], self.betas[1], self.eps, step, self.seed & 0xFFFFFFFF, counter,
+                                 _stream(self._device))
         if rc != OK:
             raise CapscapsError(rc)
         if control is None:  # what the optimizer's control has not counted
@@ -864,8 +885,5 @@ class AdamW:
                 raise ValueError("moments' values are bfloat16 of the parameters' sizes")
         count = len(self._items)
         pointers = [(ctypes.c_void_p * count)(*[_dense(t, "parameters and values", self._gpu) for t in o]) for o in out]
-        rc = capscaps_adamw_state_values(self._items, count, pointers[0], pointers[1],
-                                         _stream(self.params[0].device))
-        if rc != OK:
-            raise CapscapsError(rc)
+        _enqueue(capscaps_adamw_state_values, self._device, self._items, count, *pointers)
         return out[0], out[1]

@@ -29,6 +29,7 @@ def reached(monkeypatch):
                  "capscaps_adamw_state_values"):
         monkeypatch.setattr(cc, name, lambda *a, name=name, **k: calls.append(name) or cc.OK)
     monkeypatch.setattr(cc, "_stream", lambda device: 0)
+    monkeypatch.setattr(cc, "_current_gpu", lambda: None)   # (as a host tensor's index)
     return calls
 
 

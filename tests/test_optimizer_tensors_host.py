@@ -34,6 +34,7 @@ def calls(monkeypatch):
     monkeypatch.setattr(cc, "capscaps_adamw_step", step)
     monkeypatch.setattr(cc, "capscaps_adamw_state_values", values)
     monkeypatch.setattr(cc, "_stream", lambda device: 0)
+    monkeypatch.setattr(cc, "_current_gpu", lambda: None)   # (as a host tensor's index)
     return seen
 
 
