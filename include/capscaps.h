@@ -393,7 +393,8 @@ int capscaps_grad_norm(const capscaps_grad_tensor* grads, int count, float grad_
  *
  * and, where a tensor has a `copy`, p rounded to nearest even to that 16-bit type (the kernel that the next forward
  * pass reads).  `tensors` is an array in HOST memory, read during the call; 44 tensors are one launch.  n = 0 is allowed.
- * Pointers are device pointers aligned to their elements; no two tensors overlap.
+ * Pointers are device pointers aligned to their elements; no two tensors overlap.  eps is used as a float and must be > 0 as
+ * one; v is held in one, also where it is below the smallest normal number (a g' below 1e-22 has no square there).
  *
  * `control`: NULL, or what capscaps_grad_norm wrote on the same stream: `scale` comes from there then, `skip` leaves
  * every buffer as it is, and with step = 0 the step count t does too (so a graph replay counts its steps; a count

@@ -278,17 +278,24 @@ __device__ __forceinline__ unsigned encode_v(float v, unsigned random, int expon
 struct Moments {
     float p, m, v;
 };
+// FAST: v_sqrt_f32 and v_rcp_f32, which are off by one unit in the last place, of a step that is added to p.  They take
+// subnormal numbers for 0, so this is for an eps against which the root of such a v is nothing (fast_quotient).
+template <bool FAST>
 __device__ __forceinline__ Moments adam_value(const AdamHyper& H, const AdamStep& S, float keep, float p, float g,
                                               float m, float v)
 {
     g = g * S.scale;
     m = m * H.beta1 + g * H.one_minus_beta1;
     v = v * H.beta2 + (g * g) * H.one_minus_beta2;
-    // (v_sqrt_f32 and v_rcp_f32 are off by one unit in the last place, of a step that is added to p; v below
-    // 2^-126 counts as 0)
-    p = p * keep - S.step_size * (m * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v) * S.inv_sqrt_bias2 + H.eps));
+    const float root = FAST ? __builtin_amdgcn_sqrtf(v) : sqrtf(v), under = root * S.inv_sqrt_bias2 + H.eps;
+    p = p * keep - S.step_size * (FAST ? m * __builtin_amdgcn_rcpf(under) : m / under);
     return {p, m, v};
 }
+// v below 2^-126 has a root below 2^-63, which the bias correction makes at most 1 / sqrt(1 - beta2) times as large:
+// less than half a unit in the last place of eps if eps * sqrt(1 - beta2) is at least 2^-39 (beta2 = 0.999: eps from
+// 5.8e-11 on; 113M values with 8-bit moments: 329 us, with the exact root and quotient 336).  Past 2^100 the quotient's
+// divisor could have a subnormal reciprocal.
+bool fast_quotient(double eps, double beta2) { return eps * sqrt(1.0 - beta2) >= 0x1p-39 && eps <= 0x1p100; }
 
 template <int CTRL>
 __device__ __forceinline__ unsigned dpp_max(unsigned v)
@@ -339,7 +346,7 @@ __device__ __forceinline__ void store_codes(unsigned char* p, long long i, unsig
 // and a square root rounded to the last bit, 64-bit addresses and a product for each value's random bits).  So
 // the bits come from sums, the square root and the quotient from the fast instructions, and exponents,
 // addresses and the step's factors are scalars.
-template <int BITS, bool WHOLE>
+template <int BITS, bool FAST, bool WHOLE>
 __device__ __forceinline__ void adamw_share(const AdamTensor& T, const AdamHyper& H, unsigned key, long long base,
                                             AdamStep* shared_step)
 {
@@ -402,7 +409,7 @@ __device__ __forceinline__ void adamw_share(const AdamTensor& T, const AdamHyper
                 m[u][j] = decode_m(cm[u] >> (8 * j), em[u]);
                 v[u][j] = decode_magnitude((cv[u] >> (8 * j)) & 255u, ev[u], 31);
             }
-            const Moments r = adam_value(H, S, keep, p[u][j], g[u][j], m[u][j], v[u][j]);
+            const Moments r = adam_value<FAST>(H, S, keep, p[u][j], g[u][j], m[u][j], v[u][j]);
             p[u][j] = r.p;
             m[u][j] = r.m;
             v[u][j] = r.v;
@@ -448,7 +455,7 @@ __device__ __forceinline__ void adamw_share(const AdamTensor& T, const AdamHyper
     }
 }
 
-template <int BITS>
+template <int BITS, bool FAST>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(AdamList L, AdamHyper H)
 {
     __shared__ AdamStep step;
@@ -457,9 +464,9 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(AdamList L, AdamHyper H)
     const unsigned key = H.seed + 0x9E3779B1u * (unsigned)(L.index0 + k);
     const long long base = (long long)((int)blockIdx.x - L.first[k]) * share_of(BITS);
     if (base + share_of(BITS) <= T.n)
-        adamw_share<BITS, true>(T, H, key, base, &step);
+        adamw_share<BITS, FAST, true>(T, H, key, base, &step);
     else
-        adamw_share<BITS, false>(T, H, key, base, &step);
+        adamw_share<BITS, FAST, false>(T, H, key, base, &step);
 }
 
 struct ValuesList {
@@ -624,6 +631,7 @@ int capscaps_adamw_step(const capscaps_adamw_tensor* tensors, int count, int sta
     H.step = (int)step;
     H.seed = seed;
     H.control = control;
+    const bool fast = fast_quotient(eps, beta2);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     for (int k = 0; k < count;) {
         AdamList L;
@@ -640,10 +648,10 @@ int capscaps_adamw_step(const capscaps_adamw_tensor* tensors, int count, int sta
         }
         if (L.first[L.count] == 0) continue;
         const dim3 grid(L.first[L.count]);
-        if (state_bits == 8)
-            adamw_kernel<8><<<grid, dim3(THREADS), 0, st>>>(L, H);
-        else
-            adamw_kernel<32><<<grid, dim3(THREADS), 0, st>>>(L, H);
+        const auto kernel = state_bits == 8 ? fast ? adamw_kernel<8, true> : adamw_kernel<8, false>
+                            : fast          ? adamw_kernel<32, true>
+                                            : adamw_kernel<32, false>;
+        kernel<<<grid, dim3(THREADS), 0, st>>>(L, H);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return status_from_hip(err);
     }
