@@ -415,7 +415,10 @@ __global__ void __launch_bounds__(widest_workgroup(I))
                 const Share has{in && v < P.full, TAIL && in && v == P.part, P.tail};
                 float db[N];
 #pragma unroll
-                for (int k = 0; k < N; ++k) db[k] = rpost * (e[i][k] - value<BD, N>(b[i], k) * rpost * mean);
+                for (int k = 0; k < N; ++k) {
+                    // (without the norm the gradient does not depend on b, which may be infinite)
+                    db[k] = post ? rpost * (e[i][k] - value<BD, N>(b[i], k) * rpost * mean) : e[i][k];
+                }
                 store<DT, N, TAIL>(rdb.put(n, i * group, LB), db, has);
             }
         }
@@ -614,7 +617,8 @@ __global__ void __launch_bounds__(THREADS)
             if (A.dgate != nullptr && B.gate == CAPSCAPS_GATE_FULL)
                 store_element(A.dgate, r * A.dgate_stride + c, k.t * k.u * gate_slope(B.gate_act, k.g), B.dtype);
             if (A.dbranch != nullptr)
-                store_element(A.dbranch, r * A.dbranch_stride + c, rpost * (e_of(k, c) - k.bn * mean_post), B.dtype);
+                store_element(A.dbranch, r * A.dbranch_stride + c,
+                              B.post_norm ? rpost * (e_of(k, c) - k.bn * mean_post) : e_of(k, c), B.dtype);
         }
     }
 }

@@ -19,3 +19,32 @@ def test_more_rows_than_one_launch_has_workgroups_for():
     want = cc.block_norm_fwd(row, dtype=BF16).h
     for part in h.split(1 << 20):
         assert bool((part == want).all())
+
+
+def rows_of(rows, width, dtype, seed):
+    return torch.randn((rows, width), generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+
+
+# (layers, stream, branch): vectors of eight and of four, one and several a lane, remainders, rows of no group
+KERNELS = [(27, (FP32, FP32, FP32)), (64, (BF16, BF16, BF16)), (600, (FP16, FP16, FP32)), (1027, (BF16, FP32, BF16)),
+           (5000, (FP32, FP32, FP32)), (9000, (BF16, BF16, BF16)), (9001, (FP16, FP16, FP32)), (12000, (FP16, FP32, FP16)),
+           (20001, (BF16, FP32, FP32))]
+
+
+@pytest.mark.parametrize("gate", [None, "shared", "full"])
+@pytest.mark.parametrize("width,types", KERNELS, ids=lambda v: v if isinstance(v, int) else None)
+def test_without_a_norm_the_branch_gradient_does_not_depend_on_the_branch(width, types, gate):
+    layer, stream, branch = types
+    rows = 37
+    y, dh, dy = (rows_of(rows, width, t, k) for k, t in enumerate((stream, layer, stream)))
+    rpre = torch.rsqrt(y.double().square().mean(1) + 1e-6).float()
+    b = rows_of(rows, width, branch, 7)
+    g = None if gate is None else rows_of(rows, width, layer, 8) if gate == "full" else torch.randn(width, device="cuda")
+    same = dict(post_norm=False, gate=g, gate_act="sigmoid" if gate else "linear", branch_scale=0.5, dtype=layer)
+    bad = b.clone()
+    bad[3, width // 2], bad[4, width - 1], bad[5, 0] = float("inf"), float("nan"), float("-inf")
+    for grads in ((None, dy), (dh, dy), (dh, None)):
+        want = cc.block_norm_bwd(y, b, rpre, None, *grads, **same)
+        got = cc.block_norm_bwd(y, bad, rpre, None, *grads, **same)
+        assert torch.isfinite(got.dbranch).all()
+        assert torch.equal(got.dbranch, want.dbranch) and torch.equal(got.dx, want.dx)
