@@ -530,7 +530,9 @@ def _block(x, branch, gate, gate_act, dtype, norm_dims, post_norm, residual_scal
     layer, stream = _code(dtype), _code(x.dtype)
     kind, gate_ptr, gate_stride = GATE_NONE, None, 0
     if gate is not None:
-        if gate.shape == shape and gate.dim() > norm_dims:
+        # (for one row the type says which it is: a vector is float32, a gate for every value `dtype`)
+        if gate.shape == shape and (x.numel() > width or
+                                    gate.dtype == dtype and (layer != FP32 or gate.dim() > norm_dims)):
             if gate.dtype != dtype:
                 raise ValueError(f"a gate for every value must be {dtype}")
             kind, gate_stride = GATE_FULL, _row_stride(gate, shape, width, norm_dims, "gate", _gpu_of(x))
@@ -565,7 +567,7 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
     The last `norm_dims` axes of x [N, ...] are a row: of an activation [N,H,W,C,D0,D1,D2], 4 normalises all
     capsules of a pixel together, 3 every capsule by itself.  `dtype` is the layers' element type (that of h; default: x's): x, the
     residual stream, and branch, a layer's output, are each float32 or `dtype`.  Weights are float32 of a row's
-    size; the gate is such a vector, or a tensor of x's shape and `dtype`.  Without a branch only h is computed.
+    size; the gate is such a vector, or a tensor of x's shape and `dtype` (of one row, the type says which).  Without a branch only h is computed.
     Returns BlockNorm(y, h, rstd_pre, rstd_post); the statistics only with `save`, for block_norm_bwd.  `y` and `h`
     may be given to write to; y may be x.  Enqueues on torch's current stream; does not synchronise (tensors made on another
     stream have to be ready and, if they are freed early, recorded there, as for torch's own operations)."""

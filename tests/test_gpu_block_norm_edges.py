@@ -48,3 +48,35 @@ def test_without_a_norm_the_branch_gradient_does_not_depend_on_the_branch(width,
         got = cc.block_norm_bwd(y, bad, rpre, None, *grads, **same)
         assert torch.isfinite(got.dbranch).all()
         assert torch.equal(got.dbranch, want.dbranch) and torch.equal(got.dx, want.dx)
+
+
+@pytest.mark.parametrize("layer", [BF16, FP16])
+@pytest.mark.parametrize("shape,dims", [((1, 200), 1), ((200,), 1), ((1, 1, 1, 8, 1, 5, 5), 4), ((8, 1, 5, 5), 4)])
+def test_one_row_takes_the_gates_that_many_rows_take(shape, dims, layer):
+    """A learned scale of shape [1, ..., width] for all rows, and a gate for every value: for one row of a tensor what they
+    are for many.  (In float32 layers both have one type and mean the same for one row.)"""
+    many = (3,) + shape if shape[0] != 1 else (3,) + shape[1:]
+    x, b, per_value, dy = (rows_of(3, 200, t, k).reshape(many) for k, t in enumerate((FP32, layer, layer, FP32)))
+    vector = torch.randn(200, generator=torch.Generator().manual_seed(9)).cuda()
+    weight = torch.rand(200, device="cuda")
+
+    def one(t):
+        return t[1].reshape(shape)
+
+    for gate_of_all, gate in ((vector.view((1,) + many[1:]), vector.view(shape)), (per_value, one(per_value))):
+        same = dict(post_weight=weight, gate_act="silu", norm_dims=dims, dtype=layer)
+        want = cc.block_norm_fwd(x, b, gate=gate_of_all, save=True, **same)
+        got = cc.block_norm_fwd(one(x), one(b), gate=gate, save=True, **same)
+        assert torch.equal(got.y, one(want.y)) and torch.equal(got.h, one(want.h))
+        back = cc.block_norm_bwd(got.y, one(b), None, got.rstd_post.reshape(1), None, one(dy), gate=gate, **same)
+        assert back.dgate.shape == gate.shape and back.dgate.dtype == gate.dtype
+        few = cc.block_norm_bwd(want.y, b, None, want.rstd_post.reshape(3), None, dy, gate=gate_of_all, **same)
+        assert torch.equal(back.dbranch, one(few.dbranch))
+        if gate_of_all is per_value:
+            assert torch.equal(back.dgate, one(few.dgate))
+    other = FP16 if layer == BF16 else BF16
+    for bad in (per_value.to(other), vector.view((1,) + many[1:]).expand(many)):
+        with pytest.raises(ValueError, match="gate"):
+            cc.block_norm_fwd(x, b, gate=bad, norm_dims=dims, dtype=layer)
+    with pytest.raises(ValueError):
+        cc.block_norm_fwd(one(x), one(b), gate=one(per_value).to(other), norm_dims=dims, dtype=layer)
