@@ -467,6 +467,14 @@ def _enqueue(call, device, *args):
         raise CapscapsError(rc)
 
 
+def _overwritten(tensors):
+    """Tells autograd that the caller's tensors have other values now, as torch's own in-place operations do."""
+    global _overwritten
+    import torch
+    _overwritten = torch.autograd.graph.increment_version
+    _overwritten(tensors)
+
+
 def _code(dtype):
     """The library's code of a torch dtype."""
     global _codes
@@ -569,7 +577,7 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
     residual stream, and branch, a layer's output, are each float32 or `dtype`.  Weights are float32 of a row's
     size; the gate is such a vector, or a tensor of x's shape and `dtype` (of one row, the type says which).  Without a branch only h is computed.
     Returns BlockNorm(y, h, rstd_pre, rstd_post); the statistics only with `save`, for block_norm_bwd.  `y` and `h`
-    may be given to write to; y may be x.  Enqueues on torch's current stream; does not synchronise (tensors made on another
+    may be given to write to; y may be x.  The results have no autograd history: gradients are block_norm_bwd's.  Enqueues on torch's current stream; does not synchronise (tensors made on another
     stream have to be ready and, if they are freed early, recorded there, as for torch's own operations)."""
     import torch
     dtype = x.dtype if dtype is None else dtype
@@ -581,6 +589,7 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
         raise ValueError("without a branch there is no y")
     if y is not None and y.dtype != x.dtype or h is not None and h.dtype != dtype:
         raise ValueError("y has x's type, h has `dtype`")
+    given = [t for t in (y, h) if t is not None]
     ys = width if y is None else _row_stride(y, shape, width, norm_dims, "y", gpu)
     hs = width if h is None else _row_stride(h, shape, width, norm_dims, "h", gpu)
     if y is None and want_y and branch is not None:
@@ -599,6 +608,8 @@ def block_norm_fwd(x, branch=None, *, pre_weight=None, post_weight=None, gate=No
         None if h is None else h.data_ptr(), None if rpre is None else rpre.data_ptr(),
         None if rpost is None else rpost.data_ptr(), xs, bs, gs, ys, hs)
     _enqueue(capscaps_block_norm_fwd, device, block, args)
+    if given:
+        _overwritten(given)
     return BlockNorm(y, h, rpre, rpost)
 
 
@@ -781,6 +792,7 @@ class AdamW:
             own = self._counter is self._control
             self._control = self._control.to(self.params[0].device)
             self._counter = self._control if own else self._counter
+        self._written = self.params + [c for c in self.copies if c is not None]
         self._held = self._addresses()
 
     def _addresses(self):
@@ -817,6 +829,7 @@ class AdamW:
                                  _stream(self._device))
         if rc != OK:
             raise CapscapsError(rc)
+        _overwritten(self._written)
         if control is None:  # what the optimizer's control has not counted
             if self._counter is not None:
                 self._lacking = 0 if self._counter is self._control else step - 1
