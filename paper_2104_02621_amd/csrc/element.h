@@ -13,16 +13,9 @@ inline bool known_dtype(int dtype)
 inline size_t element_bytes(int dtype) { return dtype == CAPSCAPS_FP32 ? 4 : 2; }
 
 template <int DT>
-struct Element;
-template <>
-struct Element<CAPSCAPS_FP32> {
-    typedef float type;
-    static __device__ __forceinline__ float get(float v) { return v; }
-    static __device__ __forceinline__ float put(float v) { return v; }
-};
+struct Element;  // of the 16-bit types
 template <>
 struct Element<CAPSCAPS_BF16> {
-    typedef unsigned short type;
     static __device__ __forceinline__ float get(unsigned short v)
     {
         return __builtin_bit_cast(float, (unsigned)v << 16);
@@ -35,7 +28,6 @@ struct Element<CAPSCAPS_BF16> {
 };
 template <>
 struct Element<CAPSCAPS_FP16> {
-    typedef unsigned short type;
     static __device__ __forceinline__ float get(unsigned short v)
     {
         return (float)__builtin_bit_cast(_Float16, v);
