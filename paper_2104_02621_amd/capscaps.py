@@ -688,7 +688,7 @@ def _control_ptr(control, gpu):
 def grad_norm(grads, max_norm=None, grad_scale=1.0, control=None, workspace=None):
     """The 2-norm of all gradients together, on the device: writes `control`, four values of 4 bytes that AdamW.step
     reads: the norm (of grad_scale * gradients), the factor that scales and clips the gradients to `max_norm`
-    (None: no clipping), whether the step is to be skipped because the norm is not finite (int32), and the number of steps
+    (None, or 0 and below: no clipping), whether the step is to be skipped because the norm is not finite (int32), and the number of steps
     not skipped so far (int32, counted up here).  Returns it.  `control`: an optimizer's `control`, or a tensor of zeros
     that is kept for the whole training.  Without one a new tensor is returned, for this step alone: it counts nothing
     but this step, and AdamW.step counts the steps itself then."""
@@ -741,8 +741,12 @@ class AdamW:
             raise ValueError("AdamW needs parameters")
         count, eight = len(self.params), state_bits == 8
         self.lr, self.betas, self.eps, self.state_bits, self.seed = lr, betas, eps, state_bits, seed
-        self._control, self._int32 = torch.zeros(4, dtype=torch.float32, device=self.params[0].device), torch.int32
-        self.steps = steps
+        # steps counted on the host; the control that counts them on the device, if one does; the optimizer's own control, and
+        # the steps that it has not counted
+        self._control = torch.zeros(4, dtype=torch.float32, device=self.params[0].device)
+        self._host, self._counter, self._lacking, self._int32 = steps, None, 0, torch.int32
+        if steps:
+            self.steps = steps
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
         if isinstance(copies, torch.dtype):
             copies = [p.detach().to(copies) for p in self.params]
@@ -843,35 +847,34 @@ class AdamW:
         own, single = self._control, getattr(control, "capscaps_for_one_step", False)
         _control_ptr(control, self._gpu)
         if not single and control.data_ptr() != own.data_ptr():
-            if self._counter is own or self._host:
+            if self._host or self._counter is own:
                 raise ValueError("this optimizer has counted steps without this control: give grad_norm the "
                                  "optimizer's `control`, or none")
             self._counter = control
             return control
         if self._counter is not None and self._counter is not own:  # the caller's has counted until now
             self._lacking = self.steps
-        self._catch_up()
+        self._own_control()
         if single:
             own[:3].copy_(control[:3])
             own.view(self._int32)[3:].add_(control.view(self._int32)[2:3] == 0)
         self._counter = own
         return own
 
-    def _catch_up(self):
-        """Counts in the optimizer's control the steps that were counted elsewhere."""
+    def _own_control(self):
+        """The optimizer's control, with the steps that were counted elsewhere."""
         import torch
-        if not self._lacking:
-            return
-        if torch.cuda.is_current_stream_capturing():  # (each replay would count them again)
-            raise RuntimeError("steps have been counted on the host: read the optimizer's `control` once before the capture")
-        self._control.view(torch.int32)[3:].add_(self._lacking)
-        self._lacking = 0
+        if self._lacking:
+            if torch.cuda.is_current_stream_capturing():  # (each replay would count them again)
+                raise RuntimeError("steps were counted on the host: read the optimizer's `control` once before the capture")
+            self._control.view(self._int32)[3:].add_(self._lacking)
+            self._lacking = 0
+        return self._control
 
     @property
     def control(self):
         """The optimizer's own control, for grad_norm to write: it counts the steps on the device."""
-        self._catch_up()
-        return self._control
+        return self._own_control()
 
     @property
     def steps(self):
@@ -883,7 +886,7 @@ class AdamW:
     @steps.setter
     def steps(self, steps):
         self._host, self._counter, self._lacking = steps, None, 0
-        self._control.view(self._int32)[3] = steps
+        self._control.view(self._int32)[3:].fill_(steps)
 
     def state_values(self, out=None):
         """The moments (m, v) as lists of tensors; in 8 bits, the values their codes stand for, in bfloat16, which
