@@ -3,7 +3,8 @@
 Argument marshalling only: every step of the capsule convolution runs in the HIP library.
 Functions carry the C names; ``conv_fwd`` is a convenience wrapper that takes torch tensors
 (torch is used for device memory and streams only).  There is no CPU fallback: if the
-library is missing or no GPU is present, calls fail.
+library is missing or no GPU is present, calls fail.  They take no part in autograd: results have no history, also of inputs
+that require gradients; the gradients are calls of their own.
 """
 from __future__ import annotations
 
