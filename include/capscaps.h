@@ -359,6 +359,62 @@ int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bw
                             size_t workspace_bytes, void* stream);
 
 /*
+ * Group norm with its activation, channels last.  x is [images][positions][width]: position p of image n begins at
+ * element (n * positions + p) * stride.  The width is cut into `groups` groups of neighbouring columns (it has to be a
+ * multiple), and a group of an image, its columns at all positions, is normalised by its own mean and variance:
+ *
+ *     mean = mean(x)      rstd = 1 / sqrt(mean((x - mean)^2) + eps)           (over the group)
+ *     a = (x - mean) * rstd * weight + bias               y = act(a)
+ *
+ * Everything is computed in fp32 and y rounded to nearest even once, at the store.  weight and bias are fp32 vectors of
+ * `width` values (NULL = ones, zeros); `act` is CAPSCAPS_ACT_*.  `dtype` is that of the layers around (y, dy, dx); x has
+ * it too, or is fp32 (a layer's fp32 result).  Pointers are device pointers, aligned to their elements (whole 16-byte vectors are
+ * fastest); strides of inputs are >= 0, of outputs >= width where there is more than one position.  y may be x where type
+ * and stride are x's, dx may be dy likewise; nothing else overlaps.  Infinities and NaN of a group of an image stay in it, but for
+ * dweight and dbias.  Stream and error rules as for the calls above.
+ */
+typedef struct capscaps_group_norm {
+    long long images, positions; /* positions up to 2^31 - 1 */
+    int width, groups;           /* up to 2^30 */
+    int x_dtype, dtype;
+    int act;
+    float eps; /* > 0, a normal number */
+} capscaps_group_norm;
+/* mean, rstd: images * groups floats each for the backward pass, or NULL.  The workspace may be NULL where 0 bytes are wanted
+ * (host-only; 0 also for an invalid norm). */
+typedef struct capscaps_group_fwd_args {
+    const void* x;
+    const float *weight, *bias;
+    void* y;
+    float *mean, *rstd;
+    long long x_stride, y_stride;
+} capscaps_group_fwd_args;
+size_t capscaps_group_norm_fwd_workspace_bytes(const capscaps_group_norm* norm);
+int capscaps_group_norm_fwd(const capscaps_group_norm* norm, const capscaps_group_fwd_args* args, void* workspace,
+                            size_t workspace_bytes, void* stream);
+/*
+ * Backward, given the statistics that the forward pass stored and the gradient dy of y: with xn = (x - mean) * rstd and
+ * da = dy * act'(a),
+ *
+ *     dx = rstd * (da * weight - mean(da * weight) - xn * mean(da * weight * xn))        (means over the group)
+ *     dweight = sum over images and positions of da * xn            dbias = the same of da
+ *
+ * dweight and dbias are fp32 vectors (NULL = not wanted), overwritten, summed in an order that depends on the sizes alone, so
+ * runs repeat bit for bit.  The workspace may be NULL where 0 bytes are wanted.
+ */
+typedef struct capscaps_group_bwd_args {
+    const void* x;
+    const float *weight, *bias, *mean, *rstd;
+    const void* dy;
+    void* dx;
+    float *dweight, *dbias;
+    long long x_stride, dy_stride, dx_stride;
+} capscaps_group_bwd_args;
+size_t capscaps_group_norm_bwd_workspace_bytes(const capscaps_group_norm* norm);
+int capscaps_group_norm_bwd(const capscaps_group_norm* norm, const capscaps_group_bwd_args* args, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
  * The norm of all gradients of a step, and what an optimizer step makes of it.  `control` (device memory, 16-byte
  * aligned) is written so:
  *

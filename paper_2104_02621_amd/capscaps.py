@@ -56,6 +56,23 @@ class BlockBwdArgs(ctypes.Structure):
                           "dgate_stride", ctypes.c_longlong))
 
 
+class GroupNormArgs(ctypes.Structure):
+    """capscaps_group_norm"""
+    _fields_ = (_fields("images positions", ctypes.c_longlong)
+                + _fields("width groups x_dtype dtype act", ctypes.c_int) + [("eps", ctypes.c_float)])
+
+
+class GroupFwdArgs(ctypes.Structure):
+    """capscaps_group_fwd_args"""
+    _fields_ = (_fields("x weight bias y mean rstd", ctypes.c_void_p) + _fields("x_stride y_stride", ctypes.c_longlong))
+
+
+class GroupBwdArgs(ctypes.Structure):
+    """capscaps_group_bwd_args"""
+    _fields_ = (_fields("x weight bias mean rstd dy dx dweight dbias", ctypes.c_void_p)
+                + _fields("x_stride dy_stride dx_stride", ctypes.c_longlong))
+
+
 class GradTensor(ctypes.Structure):
     """capscaps_grad_tensor"""
     _fields_ = [("grad", ctypes.c_void_p), ("n", ctypes.c_longlong), ("dtype", ctypes.c_int)]
@@ -135,6 +152,11 @@ def _load():
     lib.capscaps_block_norm_bwd_workspace_bytes.restype = sz
     lib.capscaps_block_norm_bwd.argtypes = [p, p, p, sz, p]
     lib.capscaps_block_norm_bwd.restype = i
+    for name in ("capscaps_group_norm_fwd", "capscaps_group_norm_bwd"):
+        getattr(lib, name).argtypes = [p, p, p, sz, p]
+        getattr(lib, name).restype = i
+        getattr(lib, name + "_workspace_bytes").argtypes = [p]
+        getattr(lib, name + "_workspace_bytes").restype = sz
     lib.capscaps_grad_norm.argtypes = [p, i, f, f, p, p, sz, p]
     lib.capscaps_grad_norm.restype = i
     lib.capscaps_adamw_step.argtypes = [p, i, i, d, d, d, d, ll, ctypes.c_uint, p, p]
@@ -287,6 +309,24 @@ def capscaps_block_norm_bwd_workspace_bytes(block) -> int:
 def capscaps_block_norm_bwd(block, args, workspace, workspace_bytes, stream=None) -> int:
     """`block`, `args`: BlockArgs and BlockBwdArgs."""
     return _load().capscaps_block_norm_bwd(_ref(block), _ref(args), workspace, workspace_bytes, stream)
+
+
+def capscaps_group_norm_fwd_workspace_bytes(norm) -> int:
+    return int(_load().capscaps_group_norm_fwd_workspace_bytes(_ref(norm)))
+
+
+def capscaps_group_norm_fwd(norm, args, workspace, workspace_bytes, stream=None) -> int:
+    """`norm`, `args`: GroupNormArgs and GroupFwdArgs."""
+    return _load().capscaps_group_norm_fwd(_ref(norm), _ref(args), workspace, workspace_bytes, stream)
+
+
+def capscaps_group_norm_bwd_workspace_bytes(norm) -> int:
+    return int(_load().capscaps_group_norm_bwd_workspace_bytes(_ref(norm)))
+
+
+def capscaps_group_norm_bwd(norm, args, workspace, workspace_bytes, stream=None) -> int:
+    """`norm`, `args`: GroupNormArgs and GroupBwdArgs."""
+    return _load().capscaps_group_norm_bwd(_ref(norm), _ref(args), workspace, workspace_bytes, stream)
 
 
 def capscaps_grad_norm(grads, count, grad_scale, max_norm, control, workspace, workspace_bytes, stream=None) -> int:
@@ -658,6 +698,91 @@ def block_norm_bwd(y, branch, rstd_pre, rstd_post, dh, dy, *, pre_weight=None, p
         0 if dy is None else _row_stride(dy, shape, width, norm_dims, "dy", gpu), width, width, width)
     _enqueue(capscaps_block_norm_bwd, device, block, args, ws.data_ptr(), need)
     return BlockNormGrads(dx, db, dpre, dpost, dgate)
+
+
+# ------------------------------------------------------------------ group norm
+GroupNorm = namedtuple("GroupNorm", "y mean rstd")
+GroupNormGrads = namedtuple("GroupNormGrads", "dx dweight dbias")
+
+
+def _group(x, groups, act, dtype, eps, channel_dims):
+    """(GroupNormArgs, width): what both directions check."""
+    shape = x.shape
+    if not 1 <= channel_dims < len(shape) or x.numel() == 0:
+        raise ValueError(f"a tensor of shape {tuple(shape)} has no images and {channel_dims} axes of channels")
+    width = math.prod(shape[len(shape) - channel_dims:])
+    if width > MOST_ROW_VALUES:
+        raise ValueError(f"{width} values of a position: up to 2^30 are supported")
+    if not 1 <= groups <= width or width % groups:
+        raise ValueError(f"{width} values of a position are not {groups} groups")
+    if act not in _ACTS:
+        raise ValueError(f"act is one of {', '.join(_ACTS)}")
+    layer, code = _code(dtype), _code(x.dtype)
+    if code not in (FP32, layer):
+        raise ValueError(f"x must be float32 or {dtype}")
+    images = shape[0]
+    return GroupNormArgs(images, x.numel() // (width * images), width, groups, code, layer, _ACTS[act], eps), width
+
+
+def group_norm_fwd(x, groups, *, weight=None, bias=None, act="linear", eps=1e-5, channel_dims=1, dtype=None, save=False,
+                   y=None):
+    """Group norm and activation, channels last:
+
+        y = act((x - mean) / sqrt(var + eps) * weight + bias)
+
+    x is [N, ..., channels]: its last `channel_dims` axes are the values of a position (of an activation
+    [N,H,W,C,D0,D1,D2], 4), cut into `groups` groups of neighbours, and mean and variance are those of a group over all
+    positions of an image.  `dtype` is the layers' element type (that of y; default: x's); x is float32 or `dtype`.  Weight
+    and bias are float32, of a position's size.  Returns GroupNorm(y, mean, rstd); the statistics [N, groups] only with
+    `save`, for group_norm_bwd.  `y` may be given to write to, and may be x.  The results have no autograd history.  Enqueues on torch's
+    current stream; does not synchronise."""
+    import torch
+    dtype = x.dtype if dtype is None else dtype
+    norm, width = _group(x, groups, act, dtype, eps, channel_dims)
+    shape, device, gpu, given = x.shape, x.device, _gpu_of(x), y is not None
+    xs = _row_stride(x, shape, width, channel_dims, "x", gpu)
+    if given:
+        if y.dtype != dtype:
+            raise ValueError("y has `dtype`")
+        ys = _row_stride(y, shape, width, channel_dims, "y", gpu)
+    else:
+        y, ys = torch.empty(shape, dtype=dtype, device=device), width
+    mean = rstd = None
+    if save:
+        mean, rstd = torch.empty((2, shape[0], groups), dtype=torch.float32, device=device)
+    need = capscaps_group_norm_fwd_workspace_bytes(norm)
+    ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    args = GroupFwdArgs(x.data_ptr(), _vector(weight, width, device, "weight"), _vector(bias, width, device, "bias"),
+                        y.data_ptr(), None if mean is None else mean.data_ptr(),
+                        None if rstd is None else rstd.data_ptr(), xs, ys)
+    _enqueue(capscaps_group_norm_fwd, device, norm, args, ws.data_ptr() if need else None, need)
+    if given:
+        _overwritten([y])
+    return GroupNorm(y, mean, rstd)
+
+
+def group_norm_bwd(x, groups, mean, rstd, dy, *, weight=None, bias=None, act="linear", channel_dims=1):
+    """The gradients of group_norm_fwd, from its input, the statistics that it returned with `save` and the gradient of y.
+    dy has the layers' type, and so has dx; x is float32 or of that type.  Returns GroupNormGrads(dx, dweight, dbias), the latter
+    two float32 of a position's size, None without a weight or bias."""
+    import torch
+    norm, width = _group(x, groups, act, dy.dtype, 1.0, channel_dims)
+    shape, device, gpu = x.shape, x.device, _gpu_of(x)
+    dx = torch.empty(shape, dtype=dy.dtype, device=device)
+    dweight, dbias = (None if t is None else torch.empty(t.shape, dtype=torch.float32, device=device)
+                      for t in (weight, bias))
+    need = capscaps_group_norm_bwd_workspace_bytes(norm)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+    many = shape[0] * groups
+    args = GroupBwdArgs(
+        x.data_ptr(), _vector(weight, width, device, "weight"), _vector(bias, width, device, "bias"),
+        _vector(mean, many, device, "mean"), _vector(rstd, many, device, "rstd"), dy.data_ptr(), dx.data_ptr(),
+        None if dweight is None else dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
+        _row_stride(x, shape, width, channel_dims, "x", gpu), _row_stride(dy, shape, width, channel_dims, "dy", gpu), width)
+    if args.mean is None or args.rstd is None:
+        raise ValueError("group_norm_bwd needs the mean and rstd that group_norm_fwd returned with `save`")
+    _enqueue(capscaps_group_norm_bwd, device, norm, args, ws.data_ptr(), need)
+    return GroupNormGrads(dx, dweight, dbias)
 
 
 # ------------------------------------------------------------------ gradient norm, AdamW
