@@ -415,6 +415,76 @@ int capscaps_group_norm_bwd(const capscaps_group_norm* norm, const capscaps_grou
                             size_t workspace_bytes, void* stream);
 
 /*
+ * The losses of a linear head over many classes: softmax cross entropy, and distillation from a teacher's top logits.  With
+ * x [rows][width], weight [classes][width], bias [classes] (fp32; NULL = zeros; -infinity rules a class out), z = x weight^T + bias
+ * and tau the temperature,
+ *
+ *     lse  = log(sum over classes of exp(z / tau))             log q = z / tau - lse
+ *     loss = tau^2 * sum_k t_k (log t_k - log q[index_k])      t = softmax over the row's entries k of teacher_k / tau
+ *
+ * The class loss has one entry, the row's target, with t = 1 and tau = 1: loss = lse - z[target].  The logits, rows * classes
+ * values, are never kept: they are computed piece by piece, in each direction.
+ *
+ * Entries whose index is not 0 .. classes - 1 do not count (any negative one is as good as another).  A row without an entry that
+ * counts, or whose entries' teacher logits are all -infinity, is left out: its loss, lse and logq are 0, it has no gradient, and nothing of it
+ * is computed; what stands in it does not matter.  An entry with t = 0 adds 0 to the loss.  An index that comes twice in a row is two entries.
+ * Infinities and NaN of a row that counts make its loss NaN or infinite by the formulas (a row whose every class is ruled out: NaN), and those
+ * of a row's gradient reach dweight.
+ *
+ * Sums are held in fp32.  dtype is that of x, weight, dx and dweight.  The gradient of z is rounded to it once, piece by piece (fp32: not
+ * rounded; fp32 values of 2^104 and more in magnitude count as infinite, and infinities there make their sums NaN).  Pointers are device pointers, aligned to their
+ * elements (16 bits with whole 16-byte vectors, rows of a multiple of 32 values: read in place, else copied to the workspace); strides, in
+ * elements, are those from row to row and >= 0.  Nothing overlaps.  Runs repeat bit for bit.  Stream and error rules as for the calls above.
+ */
+typedef struct capscaps_head {
+    long long rows;     /* 0 .. 2^20 */
+    int width, classes; /* up to 2^20, 2^26 */
+    int dtype;
+    int index_bits;      /* 32 or 64 */
+    int top;             /* entries of a row, up to 1024 (class loss: 1) */
+    int teacher_dtype;   /* distillation only */
+    float temperature;   /* 1e-6 .. 1e6 (class loss: 1) */
+} capscaps_head;
+typedef struct capscaps_head_tensors {
+    const void *x, *weight;
+    const float* bias;
+    const void* index;   /* [rows][top]; class loss: the targets */
+    const void* teacher; /* [rows][top]; class loss: NULL */
+    long long x_stride, weight_stride, index_stride, teacher_stride;
+} capscaps_head_tensors;
+/* loss, lse: `rows` floats; logq (distillation): rows * top floats, 0 where an entry does not count. */
+typedef struct capscaps_head_fwd_args {
+    capscaps_head_tensors tensors;
+    float *loss, *lse, *logq;
+} capscaps_head_fwd_args;
+/*
+ * Backward, from what the forward pass wrote and dloss, the gradient of the rows' losses (fp32, `dloss_stride` apart; 0: one for all): with
+ * g = dloss * tau * (q - sum_k t_k onehot(index_k)),
+ *
+ *     dx = g weight [rows][width]      dweight = g^T x [classes][width]      dbias = sum over rows of g (fp32)
+ *
+ * each NULL = not wanted (one must be).  The class loss needs `loss`, distillation `logq`.
+ */
+typedef struct capscaps_head_bwd_args {
+    capscaps_head_tensors tensors;
+    const float *loss, *lse, *logq, *dloss;
+    void *dx, *dweight;
+    float* dbias;
+    long long dloss_stride;
+} capscaps_head_bwd_args;
+/* (host-only; 0 for an invalid head) */
+size_t capscaps_class_loss_workspace_bytes(const capscaps_head* head, int backward);
+size_t capscaps_distill_loss_workspace_bytes(const capscaps_head* head, int backward);
+int capscaps_class_loss_fwd(const capscaps_head* head, const capscaps_head_fwd_args* args, void* workspace,
+                            size_t workspace_bytes, void* stream);
+int capscaps_class_loss_bwd(const capscaps_head* head, const capscaps_head_bwd_args* args, void* workspace,
+                            size_t workspace_bytes, void* stream);
+int capscaps_distill_loss_fwd(const capscaps_head* head, const capscaps_head_fwd_args* args, void* workspace,
+                              size_t workspace_bytes, void* stream);
+int capscaps_distill_loss_bwd(const capscaps_head* head, const capscaps_head_bwd_args* args, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/*
  * The norm of all gradients of a step, and what an optimizer step makes of it.  `control` (device memory, 16-byte
  * aligned) is written so:
  *

@@ -73,6 +73,28 @@ class GroupBwdArgs(ctypes.Structure):
                 + _fields("x_stride dy_stride dx_stride", ctypes.c_longlong))
 
 
+class HeadArgs(ctypes.Structure):
+    """capscaps_head"""
+    _fields_ = ([("rows", ctypes.c_longlong)]
+                + _fields("width classes dtype index_bits top teacher_dtype", ctypes.c_int)
+                + [("temperature", ctypes.c_float)])
+
+
+_HEAD_TENSORS = (_fields("x weight bias index teacher", ctypes.c_void_p)
+                 + _fields("x_stride weight_stride index_stride teacher_stride", ctypes.c_longlong))
+
+
+class HeadFwdArgs(ctypes.Structure):
+    """capscaps_head_fwd_args"""
+    _fields_ = _HEAD_TENSORS + _fields("loss lse logq", ctypes.c_void_p)
+
+
+class HeadBwdArgs(ctypes.Structure):
+    """capscaps_head_bwd_args"""
+    _fields_ = (_HEAD_TENSORS + _fields("loss lse logq dloss dx dweight dbias", ctypes.c_void_p)
+                + [("dloss_stride", ctypes.c_longlong)])
+
+
 class GradTensor(ctypes.Structure):
     """capscaps_grad_tensor"""
     _fields_ = [("grad", ctypes.c_void_p), ("n", ctypes.c_longlong), ("dtype", ctypes.c_int)]
@@ -156,6 +178,12 @@ def _load():
         getattr(lib, name).argtypes = [p, p, p, sz, p]
         getattr(lib, name).restype = i
         getattr(lib, name + "_workspace_bytes").argtypes = [p]
+        getattr(lib, name + "_workspace_bytes").restype = sz
+    for name in ("capscaps_class_loss", "capscaps_distill_loss"):
+        for way in ("_fwd", "_bwd"):
+            getattr(lib, name + way).argtypes = [p, p, p, sz, p]
+            getattr(lib, name + way).restype = i
+        getattr(lib, name + "_workspace_bytes").argtypes = [p, i]
         getattr(lib, name + "_workspace_bytes").restype = sz
     lib.capscaps_grad_norm.argtypes = [p, i, f, f, p, p, sz, p]
     lib.capscaps_grad_norm.restype = i
@@ -327,6 +355,34 @@ def capscaps_group_norm_bwd_workspace_bytes(norm) -> int:
 def capscaps_group_norm_bwd(norm, args, workspace, workspace_bytes, stream=None) -> int:
     """`norm`, `args`: GroupNormArgs and GroupBwdArgs."""
     return _load().capscaps_group_norm_bwd(_ref(norm), _ref(args), workspace, workspace_bytes, stream)
+
+
+def capscaps_class_loss_workspace_bytes(head, backward) -> int:
+    return int(_load().capscaps_class_loss_workspace_bytes(_ref(head), backward))
+
+
+def capscaps_class_loss_fwd(head, args, workspace, workspace_bytes, stream=None) -> int:
+    """`head`, `args`: HeadArgs and HeadFwdArgs."""
+    return _load().capscaps_class_loss_fwd(_ref(head), _ref(args), workspace, workspace_bytes, stream)
+
+
+def capscaps_class_loss_bwd(head, args, workspace, workspace_bytes, stream=None) -> int:
+    """`head`, `args`: HeadArgs and HeadBwdArgs."""
+    return _load().capscaps_class_loss_bwd(_ref(head), _ref(args), workspace, workspace_bytes, stream)
+
+
+def capscaps_distill_loss_workspace_bytes(head, backward) -> int:
+    return int(_load().capscaps_distill_loss_workspace_bytes(_ref(head), backward))
+
+
+def capscaps_distill_loss_fwd(head, args, workspace, workspace_bytes, stream=None) -> int:
+    """`head`, `args`: HeadArgs and HeadFwdArgs."""
+    return _load().capscaps_distill_loss_fwd(_ref(head), _ref(args), workspace, workspace_bytes, stream)
+
+
+def capscaps_distill_loss_bwd(head, args, workspace, workspace_bytes, stream=None) -> int:
+    """`head`, `args`: HeadArgs and HeadBwdArgs."""
+    return _load().capscaps_distill_loss_bwd(_ref(head), _ref(args), workspace, workspace_bytes, stream)
 
 
 def capscaps_grad_norm(grads, count, grad_scale, max_norm, control, workspace, workspace_bytes, stream=None) -> int:
@@ -783,6 +839,126 @@ def group_norm_bwd(x, groups, mean, rstd, dy, *, weight=None, bias=None, act="li
         raise ValueError("group_norm_bwd needs the mean and rstd that group_norm_fwd returned with `save`")
     _enqueue(capscaps_group_norm_bwd, device, norm, args, ws.data_ptr(), need)
     return GroupNormGrads(dx, dweight, dbias)
+
+
+# ------------------------------------------------------------------ losses of a head over many classes
+ClassLoss = namedtuple("ClassLoss", "loss lse")
+DistillLoss = namedtuple("DistillLoss", "loss lse logq")
+HeadGrads = namedtuple("HeadGrads", "dx dweight dbias")
+MOST_ROWS, MOST_WIDTH, MOST_CLASSES, MOST_TOP = 1 << 20, 1 << 20, 1 << 26, 1024
+
+
+def _head(x, weight, bias, index, teacher, temperature):
+    """(HeadArgs, what the tensors are as HeadFwdArgs and HeadBwdArgs have them): what both losses and directions check."""
+    import torch
+    gpu, device = _gpu_of(x), x.device
+    if x.dim() < 1 or weight.dim() != 2 or weight.shape[1] != x.shape[-1] or not weight.numel():
+        raise ValueError(f"x [..., width] and weight [classes, width]: not {tuple(x.shape)} and {tuple(weight.shape)}")
+    if weight.dtype != x.dtype:
+        raise ValueError("x and weight have one dtype")
+    shape, (classes, width) = x.shape[:-1], weight.shape
+    rows = math.prod(shape)
+    if rows > MOST_ROWS or width > MOST_WIDTH or classes > MOST_CLASSES:  # (C ints, to which ctypes would cut them)
+        raise ValueError(f"{rows} rows of {width} values, {classes} classes: up to 2^20, 2^20 and 2^26 are supported")
+    if index.dtype not in (torch.int64, torch.int32):
+        raise ValueError("indices of classes are int64 or int32")
+    top, teacher_dtype, teacher_ptr, ts = 1, FP32, None, 0
+    if teacher is None:
+        ins = _row_stride(index, shape, 1, 0, "targets", gpu)
+    else:
+        if teacher.dim() != len(shape) + 1 or not 1 <= teacher.shape[-1] <= MOST_TOP:
+            raise ValueError(f"the teacher has 1 to {MOST_TOP} logits for each of {tuple(shape)} rows")
+        top, teacher_dtype, teacher_ptr = teacher.shape[-1], _code(teacher.dtype), teacher.data_ptr()
+        ins = _row_stride(index, (*shape, top), top, 1, "teacher_index", gpu)
+        ts = _row_stride(teacher, (*shape, top), top, 1, "teacher_logits", gpu)
+    if not 1e-6 <= temperature <= 1e6:
+        raise ValueError("temperature is 1e-6 to 1e6")
+    head = HeadArgs(rows, width, classes, _code(x.dtype), 64 if index.dtype == torch.int64 else 32, top, teacher_dtype,
+                    temperature)
+    return head, (x.data_ptr(), weight.data_ptr(), _vector(bias, classes, device, "bias"), index.data_ptr(), teacher_ptr,
+                  _row_stride(x, x.shape, width, 1, "x", gpu), _row_stride(weight, weight.shape, width, 1, "weight", gpu),
+                  ins, ts)
+
+
+def _head_fwd(call, need, x, head, tensors, logq_shape=None):
+    import torch
+    device, shape = x.device, x.shape[:-1]
+    loss, lse = (torch.empty(shape, dtype=torch.float32, device=device) for _ in range(2))
+    logq = None if logq_shape is None else torch.empty(logq_shape, dtype=torch.float32, device=device)
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    args = HeadFwdArgs(*tensors, loss.data_ptr(), lse.data_ptr(), None if logq is None else logq.data_ptr())
+    _enqueue(call, device, head, args, ws.data_ptr(), need)
+    return loss, lse, logq
+
+
+def _head_bwd(call, need, x, weight, bias, head, tensors, loss, lse, logq, dloss, want_dx, want_dweight):
+    import torch
+    device, rows = x.device, head.rows
+    if not (want_dx or want_dweight or bias is not None):
+        raise ValueError("no gradient is wanted")
+    if dloss.dtype != torch.float32 or dloss.device != device or dloss.numel() not in (1, rows):
+        raise ValueError(f"dloss is a float32 for each of {rows} rows, or one for all, on {device}")
+    if dloss.numel() == 1 or all(s == 0 for s in dloss.stride()):
+        step = 0
+    elif dloss.is_contiguous():
+        step = 1
+    else:
+        raise ValueError("dloss must be contiguous, or one value for all rows")
+    dx = torch.empty(x.shape, dtype=x.dtype, device=device) if want_dx else None
+    dweight = torch.empty(weight.shape, dtype=weight.dtype, device=device) if want_dweight else None
+    dbias = None if bias is None else torch.empty(bias.shape, dtype=torch.float32, device=device)
+    ws = torch.empty(need, dtype=torch.uint8, device=device)
+    args = HeadBwdArgs(*tensors, _vector(loss, rows, device, "loss"), _vector(lse, rows, device, "lse"),
+                       _vector(logq, rows * head.top, device, "logq"), dloss.data_ptr(),
+                       *(None if t is None else t.data_ptr() for t in (dx, dweight, dbias)), step)
+    _enqueue(call, device, head, args, ws.data_ptr(), need)
+    return HeadGrads(dx, dweight, dbias)
+
+
+def class_loss_fwd(x, weight, targets, *, bias=None):
+    """Softmax cross entropy of a linear head over many classes, the logits z = x weight^T + bias computed piece by piece
+    and never kept:
+
+        loss = lse - z[target]          lse = log(sum(exp(z)))
+
+    x [..., width] and weight [classes, width] of one dtype, targets [...] int64 or int32, bias [classes] float32 (-inf
+    rules a class out).  A row whose target is no class (any negative one) is left out: its loss is 0.  Returns
+    ClassLoss(loss, lse), float32 [...].  The results have no autograd history: gradients are class_loss_bwd's.  Enqueues on torch's current
+    stream; does not synchronise."""
+    head, tensors = _head(x, weight, bias, targets, None, 1.0)
+    loss, lse, _ = _head_fwd(capscaps_class_loss_fwd, capscaps_class_loss_workspace_bytes(head, 0), x, head, tensors)
+    return ClassLoss(loss, lse)
+
+
+def class_loss_bwd(x, weight, targets, loss, lse, dloss, *, bias=None, want_dx=True, want_dweight=True):
+    """The gradients of class_loss_fwd, from its arguments, what it returned and the gradient of the loss: float32, one for each row
+    or one for all (a mean's: 1 / rows that have a target).  Returns HeadGrads(dx, dweight, dbias): dx and dweight in x's dtype
+    (None where not wanted), dbias float32, None without a bias."""
+    head, tensors = _head(x, weight, bias, targets, None, 1.0)
+    return _head_bwd(capscaps_class_loss_bwd, capscaps_class_loss_workspace_bytes(head, 1), x, weight, bias, head, tensors,
+                     loss, lse, None, dloss, want_dx, want_dweight)
+
+
+def distill_loss_fwd(x, weight, teacher_index, teacher_logits, *, bias=None, temperature=1.0):
+    """Distillation from a teacher's top logits through a linear head, z = x weight^T + bias as in class_loss_fwd:
+
+        loss = temperature^2 * sum_k t_k (log t_k - logq_k)
+        t = softmax(teacher_logits / temperature)      logq_k = z[teacher_index_k] / temperature - lse
+
+    teacher_index [..., top] (int64 or int32) and teacher_logits [..., top] (float32, bfloat16 or float16) are a row's entries;
+    those whose index is no class (any negative one) do not count, and a row without entries is left out.  Returns
+    DistillLoss(loss, lse, logq), float32 [...] and [..., top]; lse is that of z / temperature."""
+    head, tensors = _head(x, weight, bias, teacher_index, teacher_logits, temperature)
+    return DistillLoss(*_head_fwd(capscaps_distill_loss_fwd, capscaps_distill_loss_workspace_bytes(head, 0), x, head, tensors,
+                                  teacher_index.shape))
+
+
+def distill_loss_bwd(x, weight, teacher_index, teacher_logits, lse, logq, dloss, *, bias=None, temperature=1.0, want_dx=True,
+                     want_dweight=True):
+    """The gradients of distill_loss_fwd, as class_loss_bwd's, from the lse and logq that it returned."""
+    head, tensors = _head(x, weight, bias, teacher_index, teacher_logits, temperature)
+    return _head_bwd(capscaps_distill_loss_bwd, capscaps_distill_loss_workspace_bytes(head, 1), x, weight, bias, head, tensors,
+                     None, lse, logq, dloss, want_dx, want_dweight)
 
 
 # ------------------------------------------------------------------ gradient norm, AdamW

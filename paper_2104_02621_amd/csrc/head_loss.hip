@@ -1,0 +1,962 @@
+// The losses of a linear head over many classes, forward and backward: softmax cross entropy, and distillation from a
+// teacher's top logits.  With x the rows, W the classes' weights and z = x W^T + bias, q = softmax(z / tau),
+//
+//     loss = tau^2 sum_k t_k (log t_k - log q_k)         g = dloss tau (q - sum_k t_k onehot_k)
+//     dx = g W        dW = g^T x        dbias = sum over rows of g
+//
+// where t are the shares of the row's entries k: one entry with t = 1 for the cross entropy (tau = 1).
+//
+// z is T x V values, far more than x and W for many classes; it is computed by pieces of the classes, once in each
+// direction, and never kept whole.  A piece of g is rounded to the operands' 16 bits (fp32: three bf16 terms) for the
+// two products that read it, which takes a relative error of half a step to each term of sums over classes or rows, as the storage type of a
+// gradient anywhere else does.  It is scaled by the power of two that brings the largest row's dloss to 2^13, so that fp16, whose
+// smallest step is 2^-24, holds shares down to 1e-11 of it.
+//
+// Rows that are left out (no class for a target, no entry) take no part at all: the rows that are kept are counted and gathered on
+// the device first, and the products run over these.  So what stands in the others does not matter, and they cost nothing.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "bf16_split.h"
+#include "conv_shape.h"
+#include "head_gemm.h"
+#include "row_vectors.h"
+
+namespace capscaps {
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int MOST_TOP = 1024;
+// (256 rows of an operand are within a signed 32-bit offset: rows of up to 2^20 values of three terms)
+constexpr long long MOST_ROWS = 1 << 20, MOST_PIECE = 1 << 20;
+constexpr long long PIECE_BYTES = 512ll << 20;  // of a piece's logits, and of its gradients
+
+// What both directions of both losses are given
+struct Head {
+    long long rows, classes;
+    int width, dtype, top;
+    float tau;
+    bool wide_index;  // 64-bit indices
+    const void *x, *weight;
+    long long x_stride, weight_stride;
+    const float* bias;
+    const void* index;  // [rows][top]
+    long long index_stride;
+    const void* teacher;  // [rows][top] logits, NULL: cross entropy
+    long long teacher_stride;
+    int teacher_dtype;
+    // in the workspace
+    int *keep, *rows_of, *pos, *count;  // count: also the two scales, see rows_kernel
+    float *share, *entropy, *coef;
+};
+
+__device__ __forceinline__ long long index_of(const Head& H, long long row, int k)
+{
+    const long long at = row * H.index_stride + k;
+    const long long v = H.wide_index ? static_cast<const long long*>(H.index)[at] : static_cast<const int*>(H.index)[at];
+    return v >= 0 && v < H.classes ? v : -1;
+}
+__device__ __forceinline__ float share_of(const Head& H, long long row, int k)
+{
+    return H.teacher != nullptr ? H.share[row * H.top + k] : 1.0f;
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) v = __builtin_fmaxf(v, __shfl_xor(v, k));
+    return v;
+}
+
+// share = softmax over the row's entries of the teacher's logits / tau, entropy = sum share log(share), keep: whether there is
+// an entry that counts.  A wave for a row.
+__global__ void __launch_bounds__(THREADS) teacher_kernel(Head H)
+{
+    const int lane = threadIdx.x & 63;
+    const float inv = 1.0f / H.tau;
+    for (long long r = blockIdx.x * 4ll + (threadIdx.x >> 6); r < H.rows; r += gridDim.x * 4ll) {
+        float top = -__builtin_inff();
+        bool nan = false;
+        for (int k = lane; k < H.top; k += 64)
+            if (index_of(H, r, k) >= 0) {
+                const float l = load_element(H.teacher, r * H.teacher_stride + k, H.teacher_dtype) * inv;
+                nan |= l != l;
+                top = __builtin_fmaxf(top, l);
+            }
+        top = wave_max(top);
+        nan = __any(nan);
+        const bool some = nan || top > -__builtin_inff();
+        float s = 0.0f;
+        for (int k = lane; k < H.top; k += 64)
+            if (some && index_of(H, r, k) >= 0)
+                s += expf(load_element(H.teacher, r * H.teacher_stride + k, H.teacher_dtype) * inv - top);
+        s = lanes_sum(s, 64);
+        const float log_s = logf(s);
+        float entropy = 0.0f;
+        for (int k = lane; k < H.top; k += 64) {
+            float t = 0.0f;
+            if (some && index_of(H, r, k) >= 0) {
+                const float l = load_element(H.teacher, r * H.teacher_stride + k, H.teacher_dtype) * inv - top;
+                t = expf(l) / s;
+                if (t != 0.0f) entropy += t * (l - log_s);  // (and where it is NaN)
+            }
+            H.share[r * H.top + k] = t;
+        }
+        entropy = lanes_sum(entropy, 64);
+        if (lane == 0) {
+            H.entropy[r] = entropy;
+            H.keep[r] = some ? 1 : 0;
+        }
+    }
+}
+
+// The rows that are kept, in their order: rows_of[i], pos[row] (-1: left out), count[0]; coef[i] = dloss tau 2^e, count[1] the
+// bits of 2^-e.  One workgroup.
+__global__ void __launch_bounds__(1024) rows_kernel(Head H, const float* dloss, long long dloss_stride)
+{
+    __shared__ int sums[16];
+    __shared__ float tops[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto kept = [&](long long r) {
+        return r < H.rows && (H.teacher != nullptr ? H.keep[r] != 0 : index_of(H, r, 0) >= 0);
+    };
+    float scale = 1.0f;
+    if (dloss != nullptr) {
+        float top = 0.0f;
+        bool bad = false;
+        for (long long r = threadIdx.x; r < H.rows; r += 1024)
+            if (kept(r)) {
+                const float d = __builtin_fabsf(dloss[r * dloss_stride] * H.tau);
+                bad |= !(d <= 3.4e38f);
+                top = __builtin_fmaxf(top, d);
+            }
+        top = wave_max(bad ? __builtin_inff() : top);
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+        top = 0.0f;
+        for (int k = 0; k < 16; ++k) top = __builtin_fmaxf(top, tops[k]);
+        int e = 0;
+        if (top > 0.0f && top <= 3.4e38f) {
+            e = 127 + 13 - (int)(__builtin_bit_cast(unsigned, top) >> 23);
+            e = e > 126 ? 126 : e;
+        }
+        scale = __builtin_bit_cast(float, (unsigned)(127 + e) << 23);
+        if (threadIdx.x == 0) H.count[1] = (127 - e) << 23;
+    }
+    int before = 0;
+    for (long long at = 0; at < H.rows; at += 1024) {
+        const long long r = at + threadIdx.x;
+        const bool mine = kept(r);
+        const unsigned long long mask = __builtin_amdgcn_ballot_w64(mine);
+        if (lane == 0) sums[wave] = __builtin_popcountll(mask);
+        __syncthreads();
+        int i = before + __builtin_popcountll(mask & ((1ull << lane) - 1));
+        for (int k = 0; k < 16; ++k) {
+            if (k < wave) i += sums[k];
+            before += sums[k];
+        }
+        __syncthreads();
+        if (r < H.rows) H.pos[r] = mine ? i : -1;
+        if (mine) {
+            H.rows_of[i] = (int)r;
+            if (dloss != nullptr) H.coef[i] = dloss[r * dloss_stride] * H.tau * scale;
+        }
+    }
+    if (threadIdx.x == 0) H.count[0] = before;
+}
+
+// ---------------------------------------------------------------------------------------- operands
+// Eight values as a product's operand: one 16-byte vector, or three of bf16 terms
+template <bool TERMS>
+__device__ __forceinline__ void put_operand(unsigned short* to, long long plane, const unsigned short* raw, const float* f)
+{
+    if constexpr (!TERMS) {
+        chunk_t c;
+        __builtin_memcpy(&c, raw, 16);
+        *reinterpret_cast<chunk_t*>(to) = c;
+    } else {
+        unsigned short t[3][8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float xs = f[j] * SPLIT_SCALE;
+            t[0][j] = round_to_16(xs, 1);
+            // (what is not finite, or 2^104 and more, makes its sums NaN or infinite)
+            const bool out = (t[0][j] & 0x7f80u) == 0x7f80u;
+            const float r1 = out ? 0.0f : xs - low_half(t[0][j]);
+            t[1][j] = round_to_16(r1, 1);
+            t[2][j] = round_to_16(r1 - low_half(t[1][j]), 1);
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            chunk_t c;
+            __builtin_memcpy(&c, t[p], 16);
+            *reinterpret_cast<chunk_t*>(to + p * plane) = c;
+        }
+    }
+}
+
+// to[i][terms][padded] = from[rows_of[i]][columns], zeros past the columns and, up to `rows`, past *count
+template <bool TERMS>
+__global__ void __launch_bounds__(THREADS) pack_kernel(const void* from, long long stride, int columns, long long rows,
+                                                       const int* rows_of, const int* count, unsigned short* to,
+                                                       int padded, bool vectors)
+{
+    const int vecs = padded / 8;
+    const long long kept = count != nullptr ? *count : rows, all = rows * vecs;
+    for (long long t = blockIdx.x * (long long)THREADS + threadIdx.x; t < all; t += (long long)gridDim.x * THREADS) {
+        const long long i = t / vecs;
+        const int c = (int)(t - i * vecs) * 8;
+        unsigned short raw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (i < kept) {
+            const long long at = (rows_of != nullptr ? rows_of[i] : i) * stride + c;
+            if (vectors && c + 8 <= columns) {
+                if constexpr (TERMS) {
+                    const float4v *p = reinterpret_cast<const float4v*>(static_cast<const float*>(from) + at), a = p[0], b = p[1];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = a[j], f[4 + j] = b[j];
+                } else {
+                    const chunk_t a = *reinterpret_cast<const chunk_t*>(static_cast<const unsigned short*>(from) + at);
+                    __builtin_memcpy(raw, &a, 16);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < columns) {
+                        if constexpr (TERMS)
+                            f[j] = static_cast<const float*>(from)[at + j];
+                        else
+                            raw[j] = static_cast<const unsigned short*>(from)[at + j];
+                    }
+            }
+        }
+        put_operand<TERMS>(to + i * (TERMS ? 3 : 1) * (long long)padded + c, padded, raw, f);
+    }
+}
+
+// to[c][terms][padded] = from[rows_of[i]][c] with i innermost, zeros past the rows that count; tiles of 64 x 64
+template <bool TERMS>
+__global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* from, long long stride, int columns,
+                                                                  long long rows, const int* rows_of, const int* count,
+                                                                  unsigned short* to, long long padded)
+{
+    typedef std::conditional_t<TERMS, float, unsigned short> E;
+    __shared__ E tile[64][TERMS ? 65 : 66];
+    long long kept = rows;
+    if (count != nullptr && *count < kept) kept = *count;
+    const int across = (columns + 63) / 64;
+    const long long tiles = (padded + 63) / 64 * across;
+    for (long long b = blockIdx.x; b < tiles; b += gridDim.x) {
+        const long long i0 = b / across * 64;
+        const int c0 = (int)(b % across) * 64;
+        if (i0 >= (kept + HEAD_K - 1) / HEAD_K * HEAD_K) continue;  // (nothing reads it)
+        for (int t = threadIdx.x; t < 64 * 64; t += THREADS) {
+            const int i = t >> 6, c = t & 63;
+            E v = 0;
+            if (i0 + i < kept && c0 + c < columns) {
+                const long long row = rows_of != nullptr ? rows_of[i0 + i] : i0 + i;
+                v = static_cast<const E*>(from)[row * stride + c0 + c];
+            }
+            tile[i][c] = v;
+        }
+        __syncthreads();
+        for (int t = threadIdx.x; t < 64 * 8; t += THREADS) {
+            const int c = t >> 3, i = (t & 7) * 8;
+            if (c0 + c < columns && i0 + i < padded) {
+                unsigned short raw[8];
+                float f[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (TERMS)
+                        f[j] = tile[i + j][c];
+                    else
+                        raw[j] = tile[i + j][c];
+                }
+                put_operand<TERMS>(to + (c0 + c) * (TERMS ? 3 : 1) * padded + i0 + i, padded, raw, f);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------------------- forward
+struct Stat {
+    float top, sum;  // the largest value, and the sum of exp(value - largest)
+};
+__device__ __forceinline__ Stat join(const Stat& a, const Stat& b)
+{
+    const float top = __builtin_fmaxf(a.top, b.top);
+    // (nothing but -infinity so far: no sum)
+    const float fa = a.top == top ? 1.0f : __expf(a.top - top), fb = b.top == top ? 1.0f : __expf(b.top - top);
+    return {top, (a.sum > 0.0f || a.sum != a.sum ? a.sum * fa : 0.0f) + (b.sum > 0.0f || b.sum != b.sum ? b.sum * fb : 0.0f)};
+}
+__device__ __forceinline__ Stat wave_join(Stat s)
+{
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) s = join(s, {__shfl_xor(s.top, k), __shfl_xor(s.sum, k)});
+    return s;
+}
+
+// stats[i][piece] of the logits of a piece (sums of `splits` parts).  A wave for a row.
+__global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, long long ldz, int splits, long long split,
+                                                        long long first, long long classes, Stat* stats, int pieces, int piece)
+{
+    const int lane = threadIdx.x & 63;
+    const float inv = 1.0f / H.tau;
+    const long long kept = *H.count;
+    for (long long i = blockIdx.x * 4ll + (threadIdx.x >> 6); i < kept; i += gridDim.x * 4ll) {
+        Stat s = {-__builtin_inff(), 0.0f};
+        for (long long c = lane; c < classes; c += 64) {
+            float v = 0.0f;
+            for (int p = 0; p < splits; ++p) v += z[p * split + i * ldz + c];
+            if (H.bias != nullptr) v += H.bias[first + c];
+            v *= inv;
+            if (v != v)
+                s.sum = v;
+            else if (v > -__builtin_inff())
+                s = join(s, {v, 1.0f});
+        }
+        s = wave_join(s);
+        if (lane == 0) stats[i * pieces + piece] = s;
+    }
+}
+
+// z[row][class] from the operands, in fp32, by a wave
+__device__ __forceinline__ float logit(const Head& H, long long row, long long cls, int lane, bool vectors)
+{
+    float s = 0.0f;
+    const long long xa = row * H.x_stride, wa = cls * H.weight_stride;
+    if (vectors && H.dtype != CAPSCAPS_FP32) {
+        const unsigned short *x = static_cast<const unsigned short*>(H.x) + xa, *w = static_cast<const unsigned short*>(H.weight) + wa;
+        for (int c = lane * 8; c < H.width; c += 512) {
+            const chunk_t a = *reinterpret_cast<const chunk_t*>(x + c), b = *reinterpret_cast<const chunk_t*>(w + c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (H.dtype == CAPSCAPS_BF16) {
+                    s = __builtin_fmaf(low_half(a[j]), low_half(b[j]), s);
+                    s = __builtin_fmaf(high_half(a[j]), high_half(b[j]), s);
+                } else {
+                    const half2v p = __builtin_bit_cast(half2v, (unsigned)a[j]), q = __builtin_bit_cast(half2v, (unsigned)b[j]);
+                    s = __builtin_fmaf((float)p[0], (float)q[0], s);
+                    s = __builtin_fmaf((float)p[1], (float)q[1], s);
+                }
+            }
+        }
+    } else {
+        for (int c = lane; c < H.width; c += 64)
+            s = __builtin_fmaf(load_element(H.x, xa + c, H.dtype), load_element(H.weight, wa + c, H.dtype), s);
+    }
+    s = lanes_sum(s, 64);
+    return H.bias != nullptr ? s + H.bias[cls] : s;
+}
+
+// loss, lse, logq of all rows, from the statistics of the pieces.  A workgroup for a row.
+__global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int pieces, float* loss, float* lse,
+                                                       float* logq, bool vectors)
+{
+    __shared__ Stat parts[4];
+    __shared__ float sums[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float inv = 1.0f / H.tau;
+    for (long long r = blockIdx.x; r < H.rows; r += gridDim.x) {
+        const int i = H.pos[r];
+        if (i < 0) {
+            if (threadIdx.x == 0) loss[r] = 0.0f, lse[r] = 0.0f;
+            if (logq != nullptr)
+                for (int k = threadIdx.x; k < H.top; k += THREADS) logq[r * H.top + k] = 0.0f;
+            continue;
+        }
+        Stat s = {-__builtin_inff(), 0.0f};
+        for (int p = threadIdx.x; p < pieces; p += THREADS) s = join(s, stats[(long long)i * pieces + p]);
+        s = wave_join(s);
+        if (lane == 0) parts[wave] = s;
+        __syncthreads();
+        s = join(join(parts[0], parts[1]), join(parts[2], parts[3]));
+        const float all = s.top + logf(s.sum);
+        float cross = 0.0f;
+        for (int k = wave; k < H.top; k += 4) {
+            const long long cls = index_of(H, r, k);
+            float l = 0.0f;
+            if (cls >= 0) {
+                l = logit(H, r, cls, lane, vectors) * inv - all;
+                const float t = share_of(H, r, k);
+                if (t != 0.0f) cross += t * l;
+            }
+            if (logq != nullptr && lane == 0) logq[r * H.top + k] = l;
+        }
+        if (lane == 0) sums[wave] = cross;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const float entropy = H.teacher != nullptr ? H.entropy[r] : 0.0f;
+            loss[r] = H.tau * H.tau * (entropy - ((sums[0] + sums[1]) + (sums[2] + sums[3])));
+            lse[r] = all;
+        }
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------------------- backward
+// A piece's gradients without the entries' shares: g = coef exp(z - lse), as operands, rows innermost (gt) and classes
+// innermost (gn), and their sums over 64 rows (sums[row tile][class], for the bias).  Tiles of 64 x 64.
+template <bool TERMS>
+__global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* lse, const float* z, long long ldz, int splits,
+                                                           long long split, long long first, int classes, unsigned short* gn,
+                                                           int padded_classes, unsigned short* gt, long long padded_rows,
+                                                           float* sums)
+{
+    __shared__ float tile[64][65];
+    const float inv = 1.0f / H.tau;
+    const long long kept = *H.count;
+    const int across = (padded_classes + 63) / 64, terms = TERMS ? 3 : 1;
+    const long long tiles = (padded_rows + 63) / 64 * across;
+    for (long long b = blockIdx.x; b < tiles; b += gridDim.x) {
+        const long long i0 = b / across * 64;
+        const int c0 = (int)(b % across) * 64;
+        if (i0 >= (kept + HEAD_K - 1) / HEAD_K * HEAD_K) continue;
+        for (int t = threadIdx.x; t < 64 * 64; t += THREADS) {
+            const int i = t >> 6, c = c0 + (t & 63);
+            float g = 0.0f;
+            if (i0 + i < kept && c < classes) {
+                float v = 0.0f;
+                for (int p = 0; p < splits; ++p) v += z[p * split + (i0 + i) * ldz + c];
+                if (H.bias != nullptr) v += H.bias[first + c];
+                const float l = __builtin_fmaf(v, inv, -lse[H.rows_of[i0 + i]]);
+                g = H.coef[i0 + i] * (TERMS ? expf(l) : __expf(l));
+            }
+            tile[i][t & 63] = g;
+        }
+        __syncthreads();
+        for (int t = threadIdx.x; t < 2 * 64 * 8; t += THREADS) {
+            const bool across_rows = t >= 64 * 8;
+            const int a = (t & 511) >> 3, k = (t & 7) * 8;
+            float f[8];
+            unsigned short raw[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                f[j] = across_rows ? tile[k + j][a] : tile[a][k + j];
+                if constexpr (!TERMS) raw[j] = round_to_16(f[j], H.dtype == CAPSCAPS_FP16 ? 2 : 1);
+            }
+            if (across_rows) {
+                if (c0 + a < classes && i0 + k < padded_rows)
+                    put_operand<TERMS>(gt + (c0 + a) * terms * padded_rows + i0 + k, padded_rows, raw, f);
+            } else if (i0 + a < kept && c0 + k < padded_classes) {
+                put_operand<TERMS>(gn + (i0 + a) * terms * padded_classes + c0 + k, padded_classes, raw, f);
+            }
+        }
+        if (sums != nullptr && threadIdx.x < 64 && c0 + threadIdx.x < classes) {
+            float s = 0.0f;
+            for (int i = 0; i < 64; ++i) s += tile[i][threadIdx.x];
+            sums[b / across * padded_classes + c0 + threadIdx.x] = s;
+        }
+        __syncthreads();
+    }
+}
+
+// ... with them: g = coef (exp(logq) - share) at the rows' entries in the piece.  An index that comes twice is one
+// entry with both shares, written by the first.  `taken`: sums of coef share over rows for each class, as whole numbers of
+// 2^-24 (their order does not matter then).  A wave for a row.
+template <bool TERMS>
+__global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* loss, const float* logq, long long first,
+                                                          int classes, unsigned short* gn, int padded_classes,
+                                                          unsigned short* gt, long long padded_rows, long long* taken)
+{
+    const int lane = threadIdx.x & 63, terms = TERMS ? 3 : 1;
+    const long long kept = *H.count;
+    for (long long i = blockIdx.x * 4ll + (threadIdx.x >> 6); i < kept; i += gridDim.x * 4ll) {
+        const long long r = H.rows_of[i];
+        for (int k = lane; k < H.top; k += 64) {
+            const long long cls = index_of(H, r, k), c = cls - first;
+            if (cls < 0 || c < 0 || c >= classes) continue;
+            float t = share_of(H, r, k);
+            bool again = false;
+            for (int j = 0; j < H.top && !again; ++j) {
+                if (j == k || index_of(H, r, j) != cls) continue;
+                if (j < k)
+                    again = true;
+                else
+                    t += share_of(H, r, j);
+            }
+            if (again) continue;
+            const float q = expf(logq != nullptr ? logq[r * H.top + k] : -loss[r]);
+            const float g = H.coef[i] * (q - t);
+            unsigned short v[3];
+            if constexpr (TERMS) {
+                const float xs = g * SPLIT_SCALE;
+                v[0] = round_to_16(xs, 1);
+                const float r1 = (v[0] & 0x7f80u) == 0x7f80u ? 0.0f : xs - low_half(v[0]);
+                v[1] = round_to_16(r1, 1);
+                v[2] = round_to_16(r1 - low_half(v[1]), 1);
+            } else {
+                v[0] = round_to_16(g, H.dtype == CAPSCAPS_FP16 ? 2 : 1);
+            }
+#pragma unroll
+            for (int p = 0; p < (TERMS ? 3 : 1); ++p) {
+                gn[(i * terms + p) * padded_classes + c] = v[p];
+                gt[(c * terms + p) * padded_rows + i] = v[p];
+            }
+            if (taken != nullptr) {
+                const long long whole = (long long)__builtin_rintf(H.coef[i] * t * 0x1p24f);
+                atomicAdd(reinterpret_cast<unsigned long long*>(taken + cls), (unsigned long long)whole);
+            }
+        }
+    }
+}
+
+__global__ void __launch_bounds__(THREADS) clear_kernel(long long* p, long long n)
+{
+    for (long long t = blockIdx.x * (long long)THREADS + threadIdx.x; t < n; t += (long long)gridDim.x * THREADS) p[t] = 0;
+}
+
+// dbias of a piece
+__global__ void __launch_bounds__(THREADS) bias_kernel(Head H, const float* sums, int padded_classes, int tile_rows,
+                                                       const long long* taken, long long first, int classes, float* dbias)
+{
+    const int c = blockIdx.x * THREADS + threadIdx.x;
+    if (c >= classes) return;
+    const long long tiles = (*H.count + tile_rows - 1) / tile_rows;
+    double s = 0.0;
+    for (long long t = 0; t < tiles; ++t) s += sums[t * padded_classes + c];
+    s -= (double)taken[first + c] * 0x1p-24;
+    dbias[first + c] = (float)(s * __builtin_bit_cast(float, H.count[1]));
+}
+
+// out[r][c] = 2^-e sum of `splits` parts of sums[pos[r]][c] (pos NULL: r), 0 where a row is left out
+__global__ void __launch_bounds__(THREADS) finish_kernel(const int* count, const int* pos, const float* sums, long long ld, int splits,
+                                                         long long split, long long rows, int columns, void* out, int dtype)
+{
+    const float scale = __builtin_bit_cast(float, count[1]);
+    const int vecs = (columns + 3) / 4;
+    const long long all = rows * vecs;
+    const bool none = *count == 0;  // (nothing was added up then)
+    for (long long t = blockIdx.x * (long long)THREADS + threadIdx.x; t < all; t += (long long)gridDim.x * THREADS) {
+        const long long r = t / vecs;
+        const int c = (int)(t - r * vecs) * 4;
+        const long long i = pos != nullptr ? pos[r] : r;
+        float4v v = {0, 0, 0, 0};
+        if (i >= 0 && !none) {
+            for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const float4v*>(sums + p * split + i * ld + c);
+            v *= scale;
+        }
+        const long long at = r * columns + c;
+        if ((columns & 3) == 0 && dtype == CAPSCAPS_FP32) {
+            typedef float at4 __attribute__((ext_vector_type(4), aligned(4)));
+            *reinterpret_cast<at4*>(static_cast<float*>(out) + at) = v;
+        } else if ((columns & 3) == 0) {
+            typedef unsigned u2 __attribute__((ext_vector_type(2)));
+            typedef u2 at2 __attribute__((aligned(2)));
+            const int kind = dtype == CAPSCAPS_FP16 ? 2 : 1;
+            const u2 w = {round_to_16(v[0], kind) | (unsigned)round_to_16(v[1], kind) << 16,
+                          round_to_16(v[2], kind) | (unsigned)round_to_16(v[3], kind) << 16};
+            *reinterpret_cast<at2*>(static_cast<unsigned short*>(out) + at) = w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < columns) store_element(out, at + j, v[j], dtype);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------- host
+long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+unsigned blocks_for(long long work, long long per) { return (unsigned)std::max<long long>(1, std::min<long long>((work + per - 1) / per, 1 << 20)); }
+
+// Tile and parts of a product: the least of an estimate in units of a 256 x 256 tile's stage (1024 matrix cycles).  A CU
+// takes one such tile, or two of the others, whose stage costs a quarter of it in instructions and 1.25 times that
+// with their operands' reads.  A tile begins and ends in the time of some stages, and parts are added up at memory speed.
+struct Pick {
+    int tile, splits;
+};
+Pick pick_tile(long long m, long long n, long long k, int terms, bool may_split)
+{
+    const long long stages = std::max<long long>(1, (k + HEAD_K - 1) / HEAD_K) * (terms > 1 ? HEAD_PRODUCTS : 1);
+    Pick best{HEAD_TILE_128, 1};
+    double least = 1e300;
+    for (const int tile : {HEAD_TILE_256, HEAD_TILE_128, HEAD_TILE_FEW_ROWS}) {
+        const HeadTileShape s = head_tile_shape(tile);
+        const double tiles = (double)((m + s.m - 1) / s.m) * (double)((n + s.n - 1) / s.n);
+        const double slots = tile == HEAD_TILE_256 ? 256 : 512, cost = tile == HEAD_TILE_256 ? 1.0 : 0.625;
+        const double ends = tile == HEAD_TILE_256 ? 24 : 20;
+        for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts * 2) {
+            if (parts > 1 && (!may_split || stages / parts < 8)) break;
+            if (tiles * parts > (1 << 23)) continue;
+            const double rounds = std::max(1.0, tiles * parts <= slots * 4 ? (double)(long long)((tiles * parts + slots - 1) / slots) : tiles * parts / slots);
+            double t = rounds * ((double)((stages + parts - 1) / parts) + ends) * cost;
+            // 0.43 us a stage; 8 bytes a value and part at 4 TB/s, and a launch
+            if (parts > 1) t += ((double)m * n * 8 * parts / 4e6 + 3.0) / 0.43;
+            if (t < least) least = t, best = {tile, parts};
+        }
+    }
+    return best;
+}
+
+int check_head(const capscaps_head* h)
+{
+    if (h == nullptr || h->rows < 0 || h->rows > MOST_ROWS || h->width < 1 || h->classes < 1) return CAPSCAPS_EINVAL;
+    if (h->width > (1 << 20) || h->classes > (1 << 26) || !known_dtype(h->dtype)) return CAPSCAPS_EINVAL;
+    if (h->index_bits != 32 && h->index_bits != 64) return CAPSCAPS_EINVAL;
+    if (h->top < 1 || h->top > MOST_TOP) return CAPSCAPS_EINVAL;
+    if (!(h->temperature >= 1e-6f && h->temperature <= 1e6f)) return CAPSCAPS_EINVAL;
+    return CAPSCAPS_OK;
+}
+
+// The workspace, piece by piece
+struct Layout {
+    char* base;
+    size_t at = 0;
+    template <typename T>
+    T* take(long long n)
+    {
+        T* p = reinterpret_cast<T*>(base + at);
+        at = (at + (size_t)std::max<long long>(n, 1) * sizeof(T) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+struct Plan {
+    int terms, padded;            // terms of an operand's value, contracted width
+    bool weight_in_place;
+    long long piece;              // classes of a piece
+    int pieces, padded_piece;
+    long long padded_rows;
+    Pick z, dx, dw;
+    bool distill, backward, bias;
+    size_t bytes;
+    // the workspace
+    unsigned short *x, *xt, *w, *wt, *gn, *gt;
+    float *logits, *dx_sums, *dw_sums, *bias_sums;
+    Stat* stats;
+    long long* taken;
+};
+
+bool vectors_of(const void* p, long long stride, int dtype)
+{
+    const int per = dtype == CAPSCAPS_FP32 ? 4 : 8;
+    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && stride % per == 0;
+}
+
+// (sizes and addresses in one; the addresses mean nothing where `base` is NULL, and the sizes do not depend on the operands' places)
+Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, Head* H)
+{
+    Plan P{};
+    P.distill = distill, P.backward = backward;
+    P.terms = A.dtype == CAPSCAPS_FP32 ? 3 : 1;
+    P.padded = (int)round_up(A.width, HEAD_K);
+    P.padded_rows = round_up(std::max<long long>(A.rows, 1), HEAD_K);
+    const long long rows = std::max<long long>(A.rows, 1);
+    const long long row_bytes = rows * std::max(4, backward ? 2 * P.terms : 0);
+    P.piece = std::max<long long>(256, std::min(MOST_PIECE, PIECE_BYTES / row_bytes / 256 * 256));
+    P.piece = std::min<long long>(round_up(A.classes, HEAD_K), P.piece);
+    P.pieces = (int)((A.classes + P.piece - 1) / P.piece);
+    P.padded_piece = (int)P.piece;
+    const long long most = std::min<long long>(P.piece, A.classes);
+    // (the parts of a product's logits lie in the piece's room for them: as many as that allows)
+    P.z = pick_tile(rows, most, A.width, P.terms, P.pieces == 1 && rows * P.piece * 4 <= PIECE_BYTES / 8);
+    Layout L{static_cast<char*>(base)};
+    Head unused;
+    Head& W = H != nullptr ? *H : unused;
+    W.count = L.take<int>(2);
+    W.rows_of = L.take<int>(A.rows);
+    W.pos = L.take<int>(A.rows);
+    W.keep = distill ? L.take<int>(A.rows) : nullptr;
+    W.share = distill ? L.take<float>(A.rows * A.top) : nullptr;
+    W.entropy = distill ? L.take<float>(A.rows) : nullptr;
+    P.x = L.take<unsigned short>(rows * P.terms * P.padded);
+    P.w = L.take<unsigned short>(most * P.terms * P.padded);
+    P.logits = L.take<float>(rows * P.piece * P.z.splits);
+    if (!backward) {
+        P.stats = L.take<Stat>(rows * P.pieces);
+        P.bytes = L.at;
+        return P;
+    }
+    W.coef = L.take<float>(A.rows);
+    P.dx = pick_tile(rows, A.width, P.piece, P.terms, true);
+    P.dw = pick_tile(most, A.width, rows, P.terms, true);
+    if (P.pieces > 1) P.dx.splits = 1;  // (added up piece after piece instead)
+    const long long ld = round_up(A.width, 4);
+    P.xt = L.take<unsigned short>((long long)A.width * P.terms * P.padded_rows);
+    P.wt = L.take<unsigned short>((long long)A.width * P.terms * P.padded_piece);
+    P.gn = L.take<unsigned short>(rows * P.terms * P.padded_piece);
+    P.gt = L.take<unsigned short>(most * P.terms * P.padded_rows);
+    P.dx_sums = L.take<float>(rows * ld * P.dx.splits);
+    P.dw_sums = P.dw.splits > 1 ? L.take<float>(most * ld * P.dw.splits) : nullptr;
+    P.bias_sums = L.take<float>((rows + 63) / 64 * P.padded_piece);
+    P.taken = L.take<long long>(A.classes);
+    P.bytes = L.at;
+    return P;
+}
+
+template <typename K, typename... Args>
+hipError_t run(K kernel, unsigned blocks, unsigned threads, hipStream_t st, Args... args)
+{
+    kernel<<<dim3(blocks), dim3(threads), 0, st>>>(args...);
+    return hipGetLastError();
+}
+#define CAPSCAPS_TRY(call)                                        \
+    do {                                                          \
+        const hipError_t err_ = (call);                           \
+        if (err_ != hipSuccess) return status_from_hip(err_);     \
+    } while (0)
+
+hipError_t pack(const Plan& P, const void* from, long long stride, int columns, long long rows, const Head* kept, int dtype,
+                unsigned short* to, hipStream_t st)
+{
+    const int* rows_of = kept != nullptr ? kept->rows_of : nullptr;
+    const int* count = kept != nullptr ? kept->count : nullptr;
+    const unsigned blocks = blocks_for(rows * (P.padded / 8), THREADS);
+    const bool vectors = vectors_of(from, stride, dtype);
+    return P.terms == 3 ? run(pack_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, P.padded, vectors)
+                        : run(pack_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, P.padded, vectors);
+}
+hipError_t pack_transposed(const Plan& P, const void* from, long long stride, int columns, long long rows, const Head* kept,
+                           unsigned short* to, long long padded, hipStream_t st)
+{
+    const int* rows_of = kept != nullptr ? kept->rows_of : nullptr;
+    const int* count = kept != nullptr ? kept->count : nullptr;
+    const unsigned blocks = blocks_for((padded + 63) / 64 * ((columns + 63) / 64), 1);
+    return P.terms == 3 ? run(pack_transposed_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, padded)
+                        : run(pack_transposed_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, padded);
+}
+
+const void* weight_at(const Head& H, long long cls)
+{
+    return static_cast<const char*>(H.weight) + cls * H.weight_stride * (long long)element_bytes(H.dtype);
+}
+
+// The rows that count, and x of these as an operand
+int begin(const Head& H, const Plan& P, const float* dloss, long long dloss_stride, hipStream_t st)
+{
+    if (P.distill) CAPSCAPS_TRY(run(teacher_kernel, blocks_for(H.rows, 4), THREADS, st, H));
+    CAPSCAPS_TRY(run(rows_kernel, 1, 1024, st, H, dloss, dloss_stride));
+    CAPSCAPS_TRY(pack(P, H.x, H.x_stride, H.width, H.rows, &H, H.dtype, P.x, st));
+    return CAPSCAPS_OK;
+}
+
+// A piece's logits without the bias
+int logits_of(const Head& H, const Plan& P, long long first, long long classes, hipStream_t st)
+{
+    const void* w = weight_at(H, first);
+    long long ldw = H.weight_stride * 2;
+    // (read in place: 16 bits, whole vectors, whole stages, rows near enough for 32-bit offsets)
+    if (P.terms != 1 || H.width % HEAD_K != 0 || !vectors_of(H.weight, H.weight_stride, H.dtype) || H.weight_stride > (1 << 21)) {
+        CAPSCAPS_TRY(pack(P, w, H.weight_stride, H.width, classes, nullptr, H.dtype, P.w, st));
+        w = P.w;
+        ldw = (long long)P.terms * P.padded * 2;
+    }
+    HeadGemm g{};
+    g.a = P.x, g.b = w;
+    g.lda = (long long)P.terms * P.padded * 2, g.ldb = ldw;
+    g.m_rows = H.rows, g.n_rows = classes, g.m_count = H.count, g.k = H.width;
+    g.plane_a = g.plane_b = P.padded * 2;
+    g.dtype = H.dtype, g.out = P.logits, g.ldo = P.piece, g.out_split = H.rows * P.piece, g.out_dtype = CAPSCAPS_FP32;
+    g.splits = P.z.splits;
+    CAPSCAPS_TRY(launch_head_gemm(g, P.z.tile, st));
+    return CAPSCAPS_OK;
+}
+
+int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, hipStream_t st)
+{
+    if (H.rows == 0) return CAPSCAPS_OK;
+    int rc = begin(H, P, nullptr, 0, st);
+    if (rc != CAPSCAPS_OK) return rc;
+    for (int piece = 0; piece < P.pieces; ++piece) {
+        const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
+        rc = logits_of(H, P, first, classes, st);
+        if (rc != CAPSCAPS_OK) return rc;
+        CAPSCAPS_TRY(run(stats_kernel, blocks_for(H.rows, 4), THREADS, st, H, (const float*)P.logits, P.piece, P.z.splits,
+                         H.rows * P.piece, first, classes, P.stats, P.pieces, piece));
+    }
+    const bool vectors = vectors_of(H.x, H.x_stride, H.dtype) && vectors_of(H.weight, H.weight_stride, H.dtype) && H.width % 8 == 0;
+    CAPSCAPS_TRY(run(loss_kernel, blocks_for(H.rows, 1), THREADS, st, H, (const Stat*)P.stats, P.pieces, loss, lse, logq, vectors));
+    return CAPSCAPS_OK;
+}
+
+struct Gradients {
+    const float *loss, *lse, *logq, *dloss;
+    long long dloss_stride;
+    void *dx, *dweight;
+    float* dbias;
+};
+
+template <bool TERMS>
+int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_t st)
+{
+    const long long ld = round_up(H.width, 4);
+    const float* scale = reinterpret_cast<const float*>(H.count + 1);
+    const int size = (int)element_bytes(H.dtype);
+    for (int piece = 0; piece < P.pieces; ++piece) {
+        const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
+        int rc = logits_of(H, P, first, classes, st);
+        if (rc != CAPSCAPS_OK) return rc;
+        const int padded = (int)round_up(classes, HEAD_K);
+        const long long tiles = (P.padded_rows + 63) / 64 * ((padded + 63) / 64);
+        CAPSCAPS_TRY(run(gradient_kernel<TERMS>, blocks_for(tiles, 1), THREADS, st, H, G.lse, (const float*)P.logits, P.piece, P.z.splits,
+                         H.rows * P.piece, first, (int)classes, P.gn, padded, P.gt, P.padded_rows,
+                         G.dbias != nullptr ? P.bias_sums : nullptr));
+        CAPSCAPS_TRY(run(entries_kernel<TERMS>, blocks_for(H.rows, 4), THREADS, st, H, G.loss, G.logq, first, (int)classes, P.gn,
+                         padded, P.gt, P.padded_rows, G.dbias != nullptr ? P.taken : nullptr));
+        if (G.dbias != nullptr)
+            CAPSCAPS_TRY(run(bias_kernel, (unsigned)((classes + THREADS - 1) / THREADS), THREADS, st, H, (const float*)P.bias_sums, padded, 64,
+                             (const long long*)P.taken, first, (int)classes, G.dbias));
+        if (G.dx != nullptr) {
+            CAPSCAPS_TRY(pack_transposed(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, P.wt, padded, st));
+            HeadGemm g{};
+            g.a = P.gn, g.b = P.wt;
+            g.lda = g.ldb = (long long)P.terms * padded * 2;
+            g.m_rows = H.rows, g.n_rows = H.width, g.m_count = H.count, g.k = classes;
+            g.plane_a = g.plane_b = padded * 2;
+            g.dtype = H.dtype, g.out = P.dx_sums, g.ldo = ld, g.out_split = H.rows * ld, g.out_dtype = CAPSCAPS_FP32;
+            g.splits = P.dx.splits, g.accumulate = piece > 0;
+            CAPSCAPS_TRY(launch_head_gemm(g, P.dx.tile, st));
+        }
+        if (G.dweight != nullptr) {
+            char* out = static_cast<char*>(G.dweight) + first * H.width * size;
+            HeadGemm g{};
+            g.a = P.gt, g.b = P.xt;
+            g.lda = g.ldb = (long long)P.terms * P.padded_rows * 2;
+            g.m_rows = classes, g.n_rows = H.width, g.k = H.rows, g.k_count = H.count;
+            g.plane_a = g.plane_b = (int)(P.padded_rows * 2);
+            g.dtype = H.dtype, g.splits = P.dw.splits;
+            const bool direct = P.dw.splits == 1;
+            g.out = direct ? out : (void*)P.dw_sums;
+            g.ldo = direct ? H.width : ld, g.out_split = classes * ld, g.out_dtype = direct ? H.dtype : CAPSCAPS_FP32;
+            if (direct) g.scale = scale;
+            CAPSCAPS_TRY(launch_head_gemm(g, P.dw.tile, st));
+            if (!direct)
+                CAPSCAPS_TRY(run(finish_kernel, blocks_for(classes * (ld / 4), THREADS), THREADS, st, (const int*)H.count, (const int*)nullptr,
+                                 (const float*)P.dw_sums, ld, P.dw.splits, classes * ld, classes, H.width, (void*)out, H.dtype));
+        }
+    }
+    if (G.dx != nullptr)
+        CAPSCAPS_TRY(run(finish_kernel, blocks_for(H.rows * (ld / 4), THREADS), THREADS, st, (const int*)H.count, (const int*)H.pos,
+                         (const float*)P.dx_sums, ld, P.dx.splits, H.rows * ld, H.rows, H.width, G.dx, H.dtype));
+    return CAPSCAPS_OK;
+}
+
+__global__ void __launch_bounds__(THREADS) zero_kernel(unsigned short* p, long long n)
+{
+    for (long long t = blockIdx.x * (long long)THREADS + threadIdx.x; t < n; t += (long long)gridDim.x * THREADS) p[t] = 0;
+}
+
+int backward(const Head& H, const Plan& P, const Gradients& G, hipStream_t st)
+{
+    if (H.rows == 0) {  // (sums over no rows)
+        const long long n = H.classes * H.width * (long long)(element_bytes(H.dtype) / 2);
+        if (G.dweight != nullptr)
+            CAPSCAPS_TRY(run(zero_kernel, blocks_for(n, THREADS), THREADS, st, static_cast<unsigned short*>(G.dweight), n));
+        if (G.dbias != nullptr)
+            CAPSCAPS_TRY(run(zero_kernel, blocks_for(H.classes * 2, THREADS), THREADS, st, reinterpret_cast<unsigned short*>(G.dbias), H.classes * 2));
+        return CAPSCAPS_OK;
+    }
+    const int rc = begin(H, P, G.dloss, G.dloss_stride, st);
+    if (rc != CAPSCAPS_OK) return rc;
+    if (G.dbias != nullptr) CAPSCAPS_TRY(run(clear_kernel, blocks_for(H.classes, THREADS), THREADS, st, P.taken, H.classes));
+    if (G.dweight != nullptr)
+        CAPSCAPS_TRY(pack_transposed(P, H.x, H.x_stride, H.width, H.rows, &H, P.xt, P.padded_rows, st));
+    return P.terms == 3 ? backward_pieces<true>(H, P, G, st) : backward_pieces<false>(H, P, G, st);
+}
+
+bool misaligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+// The head of a call; false where something about it is wrong
+bool make_head(const capscaps_head& A, const capscaps_head_tensors& T, bool distill, Head& H)
+{
+    const size_t size = element_bytes(A.dtype), index = A.index_bits / 8;
+    if (T.weight == nullptr || misaligned(T.weight, size) || misaligned(T.bias, 4)) return false;
+    if (A.rows > 0 && (T.x == nullptr || T.index == nullptr || misaligned(T.x, size) || misaligned(T.index, index))) return false;
+    constexpr long long far = 1ll << 40;
+    if (T.x_stride < 0 || T.x_stride > far || T.weight_stride < 0 || T.weight_stride > far || T.index_stride < 0 ||
+        T.index_stride > far)
+        return false;
+    if (distill) {
+        if (!known_dtype(A.teacher_dtype) || T.teacher_stride < 0 || T.teacher_stride > far) return false;
+        if (A.rows > 0 && (T.teacher == nullptr || misaligned(T.teacher, element_bytes(A.teacher_dtype)))) return false;
+    } else if (A.top != 1 || A.temperature != 1.0f || T.teacher != nullptr) {
+        return false;
+    }
+    H = Head{};
+    H.rows = A.rows, H.classes = A.classes, H.width = A.width, H.dtype = A.dtype, H.top = A.top, H.tau = A.temperature;
+    H.wide_index = A.index_bits == 64;
+    H.x = T.x, H.weight = T.weight, H.bias = T.bias, H.index = T.index, H.teacher = T.teacher;
+    H.x_stride = T.x_stride, H.weight_stride = T.weight_stride, H.index_stride = T.index_stride;
+    H.teacher_stride = T.teacher_stride, H.teacher_dtype = A.teacher_dtype;
+    return true;
+}
+
+int run_forward(const capscaps_head* head, const capscaps_head_fwd_args* args, bool distill, void* workspace,
+                size_t workspace_bytes, void* stream)
+{
+    const int rc = check_head(head);
+    if (rc != CAPSCAPS_OK) return rc;
+    if (args == nullptr) return CAPSCAPS_EINVAL;
+    Head H;
+    if (!make_head(*head, args->tensors, distill, H)) return CAPSCAPS_EINVAL;
+    if (head->rows > 0 && (args->loss == nullptr || args->lse == nullptr || (distill && args->logq == nullptr)))
+        return CAPSCAPS_EINVAL;
+    if (misaligned(args->loss, 4) || misaligned(args->lse, 4) || misaligned(args->logq, 4) || (!distill && args->logq != nullptr))
+        return CAPSCAPS_EINVAL;
+    const Plan P = make_plan(*head, distill, false, workspace, &H);
+    if (workspace == nullptr || workspace_bytes < P.bytes) return CAPSCAPS_EWORKSPACE;
+    if (misaligned(workspace, 16)) return CAPSCAPS_EINVAL;
+    return forward(H, P, args->loss, args->lse, args->logq, static_cast<hipStream_t>(stream));
+}
+
+int run_backward(const capscaps_head* head, const capscaps_head_bwd_args* args, bool distill, void* workspace,
+                 size_t workspace_bytes, void* stream)
+{
+    const int rc = check_head(head);
+    if (rc != CAPSCAPS_OK) return rc;
+    if (args == nullptr) return CAPSCAPS_EINVAL;
+    Head H;
+    if (!make_head(*head, args->tensors, distill, H)) return CAPSCAPS_EINVAL;
+    const capscaps_head_bwd_args& A = *args;
+    if (head->rows > 0 && (A.lse == nullptr || A.dloss == nullptr || (distill ? A.logq : A.loss) == nullptr)) return CAPSCAPS_EINVAL;
+    if ((A.dx == nullptr || head->rows == 0) && A.dweight == nullptr && A.dbias == nullptr) return head->rows == 0 && A.dx != nullptr ? CAPSCAPS_OK : CAPSCAPS_EINVAL;
+    if (A.dloss_stride < 0 || A.dloss_stride > (1ll << 40)) return CAPSCAPS_EINVAL;
+    const size_t size = element_bytes(head->dtype);
+    for (const void* p : {(const void*)A.loss, (const void*)A.lse, (const void*)A.logq, (const void*)A.dloss, (const void*)A.dbias})
+        if (misaligned(p, 4)) return CAPSCAPS_EINVAL;
+    if (misaligned(A.dx, size) || misaligned(A.dweight, size)) return CAPSCAPS_EINVAL;
+    const Plan P = make_plan(*head, distill, true, workspace, &H);
+    if (workspace == nullptr || workspace_bytes < P.bytes) return CAPSCAPS_EWORKSPACE;
+    if (misaligned(workspace, 16)) return CAPSCAPS_EINVAL;
+    const Gradients G{A.loss, A.lse, distill ? A.logq : nullptr, A.dloss, A.dloss_stride, A.dx, A.dweight, A.dbias};
+    return backward(H, P, G, static_cast<hipStream_t>(stream));
+}
+
+}  // namespace
+}  // namespace capscaps
+
+using namespace capscaps;
+
+extern "C" {
+
+size_t capscaps_class_loss_workspace_bytes(const capscaps_head* head, int backward)
+{
+    return check_head(head) == CAPSCAPS_OK ? make_plan(*head, false, backward != 0, nullptr, nullptr).bytes : 0;
+}
+size_t capscaps_distill_loss_workspace_bytes(const capscaps_head* head, int backward)
+{
+    return check_head(head) == CAPSCAPS_OK ? make_plan(*head, true, backward != 0, nullptr, nullptr).bytes : 0;
+}
+int capscaps_class_loss_fwd(const capscaps_head* head, const capscaps_head_fwd_args* args, void* workspace,
+                            size_t workspace_bytes, void* stream)
+{
+    return run_forward(head, args, false, workspace, workspace_bytes, stream);
+}
+int capscaps_class_loss_bwd(const capscaps_head* head, const capscaps_head_bwd_args* args, void* workspace,
+                            size_t workspace_bytes, void* stream)
+{
+    return run_backward(head, args, false, workspace, workspace_bytes, stream);
+}
+int capscaps_distill_loss_fwd(const capscaps_head* head, const capscaps_head_fwd_args* args, void* workspace,
+                              size_t workspace_bytes, void* stream)
+{
+    return run_forward(head, args, true, workspace, workspace_bytes, stream);
+}
+int capscaps_distill_loss_bwd(const capscaps_head* head, const capscaps_head_bwd_args* args, void* workspace,
+                              size_t workspace_bytes, void* stream)
+{
+    return run_backward(head, args, true, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,355 @@
+"""GPU parity of the class loss and of distillation (forward and backward) against their formulas in 64 bits: every element
+type, one row to many, one class to more than a piece holds, odd sizes, strides and addresses, rows left out with NaN in
+them, classes ruled out, indices that come twice, gradients wanted one by one, streams and graphs.
+Tolerances: tests/head_loss_ref.py, from the number of roundings."""
+import math
+
+import pytest
+import torch
+
+from paper_2104_02621_amd import capscaps as cc
+from tests import head_loss_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+FP32, BF16, FP16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [FP32, BF16, FP16]
+NAMES = {FP32: "fp32", BF16: "bf16", FP16: "fp16"}
+
+
+def close(got, want, err, what):
+    got = got.double()
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    assert torch.isfinite(got).all(), what
+    over = ((got - want).abs() - err).flatten()
+    at = int(over.argmax())
+    assert over[at] <= 0, f"{what}[{at}]: {got.flatten()[at]} for {want.flatten()[at]}, bound {err.flatten()[at]}"
+
+
+class Case:
+    def __init__(self, rows, width, classes, dtype, top=None, bias=False, tau=1.0, left=0.0, gap=0, shift=0, index=torch.int64,
+                 teacher=FP32, seed=0, scale=2.0):
+        self.rows, self.classes, self.dtype, self.tau, self.top = rows, classes, dtype, tau, top
+        gen = torch.Generator(device="cuda").manual_seed(seed + 7 * rows + 11 * width + classes)
+
+        def normal(*shape):
+            return torch.randn(shape, generator=gen, device="cuda")
+
+        weight, x = normal(classes, width) * scale * width ** -0.5, normal(rows, width)
+        first = torch.randint(0, classes, (rows,), generator=gen, device="cuda")
+        x += weight[first] * torch.rand((rows, 1), generator=gen, device="cuda")
+        self.x, self.w = self.place(x.to(dtype), gap, shift), self.place(weight.to(dtype), gap, shift)
+        self.bias = normal(classes) if bias else None
+        self.dloss = torch.rand(rows, generator=gen, device="cuda") + 0.1
+        out = torch.rand(rows, generator=gen, device="cuda") < left
+        if top is None:
+            self.index = first.masked_fill(out, -1).to(index)
+            self.teacher = None
+        else:
+            # (indices may come twice: few classes)
+            self.index = torch.randint(0, classes, (rows, top), generator=gen, device="cuda")
+            self.index = self.index.masked_fill(out[:, None] | (torch.rand((rows, top), generator=gen, device="cuda") < 0.1), -1)
+            self.index = self.index.to(index)
+            self.teacher = (normal(rows, top) * 2).to(teacher)
+
+    @staticmethod
+    def place(t, gap, shift):
+        """Rows `gap` values apart, the first `shift` values into its allocation."""
+        if not gap and not shift:
+            return t
+        wide = torch.full((t.shape[0] * (t.shape[1] + gap) + shift,), float("nan"), dtype=t.dtype, device="cuda")
+        view = wide[shift:].view(t.shape[0], t.shape[1] + gap)[:, :t.shape[1]]
+        view.copy_(t)
+        return view
+
+    def head(self):
+        index = self.index.long() if self.teacher is not None else self.index.long()[:, None]
+        return ref.Head(self.x, self.w, self.bias, index, self.teacher, self.tau)
+
+    def forward(self):
+        if self.teacher is None:
+            return cc.class_loss_fwd(self.x, self.w, self.index, bias=self.bias)
+        return cc.distill_loss_fwd(self.x, self.w, self.index, self.teacher, bias=self.bias, temperature=self.tau)
+
+    def backward(self, r, dloss=None, **more):
+        dloss = self.dloss if dloss is None else dloss
+        if self.teacher is None:
+            return cc.class_loss_bwd(self.x, self.w, self.index, r.loss, r.lse, dloss, bias=self.bias, **more)
+        return cc.distill_loss_bwd(self.x, self.w, self.index, self.teacher, r.lse, r.logq, dloss, bias=self.bias,
+                                   temperature=self.tau, **more)
+
+    def check(self):
+        h, r = self.head(), self.forward()
+        loss, lse, logq, eloss, else_, elogq = h.forward()
+        close(r.lse, lse, else_, "lse")
+        close(r.loss, loss, eloss, "loss")
+        if self.teacher is not None:
+            close(r.logq, logq, elogq, "logq")
+            kept = r.logq
+        else:
+            kept = -r.loss[:, None]
+        g = self.backward(r)
+        dx, dw, db, edx, edw, edb = h.backward(r.lse, kept, self.dloss)
+        assert g.dx.dtype == self.dtype and g.dweight.dtype == self.dtype
+        close(g.dx, dx, edx, "dx")
+        close(g.dweight, dw, edw, "dweight")
+        if self.bias is not None:
+            close(g.dbias, db, edb, "dbias")
+        return r, g
+
+
+# one of everything; odd sizes; widths of whole stages and not; rows and classes below, at and above tiles; long contractions in
+# parts
+SHAPES = [(1, 1, 1), (1, 8, 10), (3, 5, 7), (5, 33, 100), (64, 64, 64), (65, 96, 257), (127, 864, 1001), (130, 128, 3000),
+          (300, 40, 513), (256, 256, 256), (1, 4096, 5000), (2, 31, 70000), (1000, 32, 10), (513, 1000, 300)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_class_loss(shape, dtype):
+    Case(*shape, dtype, bias=shape[0] % 2 == 1, left=0.2 if shape[0] > 4 else 0.0).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("top,tau", [(1, 1.0), (8, 2.0), (70, 4.0), (300, 0.5)])
+@pytest.mark.parametrize("shape", [(1, 8, 10), (5, 33, 100), (127, 864, 1001), (300, 40, 513)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_distillation(shape, top, tau, dtype):
+    Case(*shape, dtype, top=top, tau=tau, bias=top == 8, left=0.2).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("gap,shift", [(8, 0), (5, 0), (0, 3), (1, 1), (64, 8)])
+def test_strides_and_addresses(gap, shift, dtype):
+    Case(70, 64, 300, dtype, gap=gap, shift=shift, left=0.1).check()
+    Case(70, 50, 300, dtype, gap=gap, shift=shift, top=5, bias=True).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_narrow_indices_and_teachers(dtype):
+    Case(50, 64, 200, dtype, index=torch.int32, left=0.3).check()
+    for teacher in TYPES:
+        Case(50, 64, 200, dtype, top=9, index=torch.int32, teacher=teacher).check()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=NAMES.get)
+@pytest.mark.parametrize("top", [None, 6])
+def test_several_pieces_of_the_classes(top, dtype):
+    Case(4096, 64, 70001, dtype, top=top, bias=True, left=0.1).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("top", [None, 4])
+def test_rows_left_out(top, dtype):
+    """What stands in a row that is left out does not matter, also where it is not finite; nothing is left of it."""
+    c = Case(90, 64, 130, dtype, top=top, bias=True, left=0.5)
+    out = c.index < 0 if top is None else (c.index < 0).all(1)
+    want = c.forward()
+    grads = c.backward(want)
+    c.x[out] = float("nan")
+    c.dloss[out] = float("inf")
+    r = c.forward()
+    g = c.backward(r)
+    for a, b in zip((*r, *g), (*want, *grads)):
+        assert torch.equal(a, b)
+    assert 0 < int(out.sum()) < 90 and (r.loss[out] == 0).all() and (g.dx[out] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("top", [None, 4])
+def test_no_row_counts(top, dtype):
+    c = Case(70, 64, 130, dtype, top=top, bias=True, left=1.0)
+    r = c.forward()
+    assert (r.loss == 0).all() and (r.lse == 0).all()
+    for t in c.backward(r):
+        assert (t == 0).all()
+    # indices past the classes are as good as negative ones
+    c.index = torch.full_like(c.index, 130)
+    for t in (*c.forward(), *c.backward(r)):
+        assert (t == 0).all()
+
+
+def test_no_rows():
+    c = Case(3, 64, 130, BF16, bias=True)
+    x, index, none = c.x[:0], c.index[:0], torch.empty(0, device="cuda")
+    r = cc.class_loss_fwd(x, c.w, index, bias=c.bias)
+    assert r.loss.shape == (0,)
+    g = cc.class_loss_bwd(x, c.w, index, r.loss, r.lse, none, bias=c.bias)
+    assert g.dx.shape == (0, 64) and (g.dweight == 0).all() and (g.dbias == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_classes_ruled_out(dtype):
+    """A bias of -inf: a class of probability 0, without gradient."""
+    c = Case(60, 64, 300, dtype, bias=True)
+    ruled = torch.arange(300, device="cuda") % 3 == 0
+    c.index = torch.where(ruled[c.index], c.index + 1, c.index)
+    c.bias[ruled] = float("-inf")
+    r, g = c.check()
+    assert (g.dweight[ruled] == 0).all() and (g.dbias[ruled] == 0).all()
+    keep = ~ruled
+    fewer = cc.class_loss_fwd(c.x, c.w[keep].contiguous(), (keep.cumsum(0) - 1)[c.index], bias=c.bias[keep])
+    close(r.lse, fewer.lse.double(), 1e-4 * fewer.lse.abs().double(), "lse")
+    # every class of a call ruled out: NaN; the target's class alone: infinite
+    c.bias.fill_(float("-inf"))
+    assert torch.isnan(c.forward().loss).all()
+    c.bias.zero_()
+    c.bias[int(c.index[0])] = float("-inf")
+    assert c.forward().loss[0] == float("inf")
+
+
+def test_teacher_logits_that_are_not_finite():
+    c = Case(6, 64, 100, BF16, top=4, bias=True)
+    c.index = torch.arange(4, device="cuda").repeat(6, 1)
+    inf = float("inf")
+    c.teacher[0] = torch.tensor([1.0, -inf, 0.5, -inf])
+    c.teacher[1] = -inf
+    c.teacher[2, 1] = float("nan")
+    r = c.forward()
+    rows = torch.tensor([0, 1, 3, 4, 5], device="cuda")
+    loss, lse, _, eloss, else_, _ = c.head().forward()
+    close(r.loss[rows], loss[rows], eloss[rows], "loss")
+    assert r.loss[1] == 0 and r.lse[1] == 0 and torch.isnan(r.loss[2])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_nan_stays_in_its_row(dtype):
+    c = Case(100, 64, 300, dtype)
+    want = c.forward()
+    grads = c.backward(want)
+    c.x[17, 3] = float("nan")
+    r = c.forward()
+    g = c.backward(r)
+    others = torch.arange(100, device="cuda") != 17
+    assert torch.isnan(r.loss[17]) and torch.equal(r.loss[others], want.loss[others])
+    assert torch.isnan(g.dx[17]).all() and torch.equal(g.dx[others], grads.dx[others])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("top", [None, 4])
+def test_gradients_one_by_one(top, dtype):
+    c = Case(90, 64, 130, dtype, top=top, bias=True)
+    r = c.forward()
+    want = c.backward(r)
+    a, b, e = c.backward(r, want_dweight=False), c.backward(r, want_dx=False), c.backward(r, want_dx=False, want_dweight=False)
+    assert torch.equal(a.dx, want.dx) and a.dweight is None and torch.equal(b.dweight, want.dweight) and b.dx is None
+    assert torch.equal(e.dbias, want.dbias) and e.dx is None and e.dweight is None
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_one_gradient_for_all_rows(dtype):
+    c = Case(90, 64, 130, dtype)
+    r = c.forward()
+    one = torch.tensor(1.0 / 90, device="cuda")
+    want = c.backward(r, one.repeat(90))
+    for dloss in (one, one.view(1), one.expand(90)):
+        for a, b in zip(c.backward(r, dloss), want):
+            assert a is None and b is None or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-6, 1e20])
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_sizes_of_dloss(size, dtype):
+    """A loss scale goes through: fp16's range is no limit to the gradients' products, only to what is stored."""
+    c = Case(90, 64, 130, dtype, bias=True, scale=1.0)
+    r = c.forward()
+    one = c.backward(r)
+    two = 2.0 ** round(math.log2(size))
+    g = c.backward(r, c.dloss * two)
+    assert torch.equal(g.dbias, one.dbias * two)
+    if dtype != FP16:
+        assert torch.equal(g.dx, one.dx * two) and torch.equal(g.dweight, one.dweight * two)
+
+
+def test_leading_axes():
+    c = Case(24, 64, 130, BF16, top=3)
+    want = c.forward()
+    grads = c.backward(want)
+    x, index, teacher = c.x.view(2, 3, 4, 64), c.index.view(2, 3, 4, 3), c.teacher.view(2, 3, 4, 3)
+    r = cc.distill_loss_fwd(x, c.w, index, teacher)
+    assert r.loss.shape == (2, 3, 4) and r.logq.shape == index.shape
+    g = cc.distill_loss_bwd(x, c.w, index, teacher, r.lse, r.logq, c.dloss.view(2, 3, 4))
+    assert g.dx.shape == x.shape and torch.equal(g.dx.view(24, 64), grads.dx) and torch.equal(r.loss.flatten(), want.loss)
+
+
+@pytest.mark.parametrize("shape", [(100, 864, 1001), (300, 64, 5000)])
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_graph_stream_and_repeats(shape, dtype):
+    """Captured and replayed with other values and other rows left out, between eager calls; another stream; bit for bit."""
+    c = Case(*shape, dtype, top=5, bias=True, left=0.3)
+    first, index = c.x.clone(), c.index.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        r = c.forward()
+        g = c.backward(r)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cr = c.forward()
+        cg = c.backward(cr)
+    for k in range(4):
+        c.x.copy_(first * (1.0 + 0.25 * k))
+        c.index.copy_(index.roll(k, 0))
+        graph.replay()
+        want = c.forward()
+        grads = c.backward(want)
+        torch.cuda.synchronize()
+        for a, b in zip((*cr, *cg), (*want, *grads)):
+            assert torch.equal(a, b), k
+    c.x.copy_(first), c.index.copy_(index)
+    again = c.forward()
+    for a, b in zip((*again, *c.backward(again)), (*r, *g)):
+        assert torch.equal(a, b)
+
+
+def test_two_calls_at_once():
+    """Each call has its own workspace."""
+    a, b = Case(300, 128, 4000, BF16, left=0.2), Case(200, 64, 3000, FP32, top=7, bias=True)
+    want = [(*r, *g) for r, g in ((c.forward(), None) for c in (a, b)) for g in [()]]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = []
+        for c, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                r = c.forward()
+                got.append((r, c.backward(r)))
+        torch.cuda.synchronize()
+        for (r, g), c, w in zip(got, (a, b), want):
+            for p, q in zip(r, w):
+                assert torch.equal(p, q)
+            for p, q in zip(g, c.backward(r)):
+                assert p is None and q is None or torch.equal(p, q)
+
+
+def test_weight_rows_past_32_bits():
+    """Rows of the weight 2^20 values apart: the last lie past 4 GB."""
+    c = Case(40, 64, 3000, BF16)
+    wide = torch.empty((3000, 1 << 20), dtype=BF16, device="cuda")
+    want = c.forward()
+    grads = c.backward(want)
+    wide[:, :64] = c.w
+    c.w = wide[:, :64]
+    r = c.forward()
+    for a, b in zip((*r, *c.backward(r)), (*want, *grads)):
+        assert a is None and b is None or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("top", [None, 5])
+@pytest.mark.parametrize("shape", [(7, 12, 30), (40, 64, 300)])
+def test_gradients_against_differences(shape, top):
+    """Along the gradients themselves, the sum of loss * dloss changes by their squares."""
+    c = Case(*shape, FP32, top=top, tau=1.0 if top is None else 2.0, bias=True, left=0.2)
+    r = c.forward()
+    g = c.backward(r)
+    for at, grad in ((c.x, g.dx), (c.w, g.dweight), (c.bias, g.dbias)):
+        before, want = at.clone(), float(grad.double().square().sum())
+        step = 1e-2 / math.sqrt(want)
+        value = []
+        for sign in (1, -1):
+            at.copy_(before + sign * step * grad)
+            value.append(float((c.head().forward()[0] * c.dloss).sum()))
+        at.copy_(before)
+        # (the losses in 64 bits, a third derivative of order one along a step of 1e-2: 1e-4, and fp32's rounding of the step)
+        assert abs((value[0] - value[1]) / (2 * step) - want) <= 2e-3 * want
