@@ -1,0 +1,457 @@
+// Internal: the matrix products of a linear head over many classes (included by the files of its tiles), on the bf16 and fp16 matrix instructions:
+//
+//     out[m][n] = sum over k of a[m][k] * b[n][k]
+//
+// with the contracted index innermost in both operands.  fp32 operands lie in memory as three bf16 terms each (see
+// bf16_split.h); the six products of terms that count are the same loop run six times, smallest products first.
+//
+// A workgroup of four waves owns a tile of out (256 x 256: 128 x 128 a wave).  A stage is 32 contracted values; LDS holds a
+// ring of four stages, filled by copies that pass no registers.  Per stage a wave issues two steps of 16 matrix
+// instructions (32x32x16); between them go, one at a time, the LDS reads of the next step's operands and the copies of
+// the stage four ahead.  One barrier a stage, before its second step, whose operands are in registers by then.
+//
+// LDS stage: rows of 64 bytes, four 16-byte chunks, chunk c of row r in place c ^ (r / 4 % 4): four neighbouring lanes of a
+// copy bring one row's 64 contiguous bytes, and the 16 lanes that read one chunk of 16 rows touch 16 different 16-byte
+// columns of the banks.  The n side is the matrix instruction's row operand, so that a lane ends up with runs of four
+// neighbouring n of one m.
+#pragma once
+#include "head_gemm.h"
+
+#include "bf16_split.h"
+#include "conv_shape.h"
+#include "igemm_common.h"
+#include "lds_dma.h"
+#include "row_vectors.h"
+
+namespace capscaps {
+namespace {
+
+constexpr int OUT_OF_RANGE = (int)0x80000000u;
+
+__device__ __forceinline__ unsigned half_pair(float lo, float hi)
+{
+    const float2v v = {lo, hi};
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(v, half2v));
+}
+
+// A row's part of 32 n values, for lanes of both halves: after it a lane holds eight neighbouring ones, those of
+// lane half h beginning at 8 (2 pair + h).  v: packed pairs of 8g + 4h + 0..3 in v[2g], v[2g + 1].
+__device__ __forceinline__ chunk_t neighbours(const unsigned* v, int pair)
+{
+    // (the upper half's register of run 2 pair goes to the lower half, the lower half's of run 2 pair + 1 to the upper)
+    const auto a = __builtin_amdgcn_permlane32_swap(v[4 * pair], v[4 * pair + 2], false, false);
+    const auto b = __builtin_amdgcn_permlane32_swap(v[4 * pair + 1], v[4 * pair + 3], false, false);
+    return {a[0], b[0], a[1], b[1]};
+}
+
+// Four lanes hold four n values each (two packed words), of neighbouring m; after it lane j of the four holds the
+// four m values of n value j.
+__device__ __forceinline__ void turn(unsigned& lo, unsigned& hi, int lane)
+{
+    auto moved = [](unsigned v, auto CTRL) {
+        return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, decltype(CTRL)::value, 0xf, 0xf, true);
+    };
+    typedef std::integral_constant<int, 0xB1> One;  // quad_perm 1 0 3 2
+    typedef std::integral_constant<int, 0x4E> Two;  // quad_perm 2 3 0 1
+    const unsigned pick = lane & 1 ? 0x03020706u : 0x05040100u;
+    const unsigned a = __builtin_amdgcn_perm(moved(lo, One()), lo, pick), b = __builtin_amdgcn_perm(moved(hi, One()), hi, pick);
+    const bool late = lane & 2;
+    const unsigned got = moved(late ? a : b, Two());
+    lo = late ? got : a;
+    hi = late ? b : got;
+}
+
+// NB: stages of the ring
+template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, int END>
+__global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kernel(const HeadGemm G, int tiles_m, int tiles_n)
+{
+    constexpr int NWN = 4 / NWM, WM = BM / NWM, WN = BN / NWN, TM = WM / 32, TN = WN / 32;
+    constexpr int A_BYTES = BM * 64, STAGE = (BM + BN) * 64;
+    constexpr int CA = BM / 64, CB = BN / 64;  // copies of a wave and stage
+    constexpr int NMMA = TM * TN, NFRAG = TM + TN;
+    constexpr int KEEP = (NB - 2) * (CA + CB);
+    static_assert(KEEP + CA < 64, "vmcnt is a 6-bit counter");
+    static_assert(CA >= 1 && CB >= 1, "copies of every wave");
+    extern __shared__ char smem[];
+
+    // Tiles: an XCD (workgroups go to the eight in turn) takes a run of them, bands of eight rows of tiles, so that the 32
+    // tiles its CUs work on at a time share operands in its L2.
+    const int tiles = tiles_m * tiles_n;
+    int part, L;
+    {
+        const int all = gridDim.x, span = all & ~7;
+        const int id = (int)blockIdx.x < span ? ((int)blockIdx.x & 7) * (span >> 3) + ((int)blockIdx.x >> 3) : blockIdx.x;
+        part = id / tiles;
+        L = id - part * tiles;
+    }
+    const int band = L / (8 * tiles_n), in_band = L - band * 8 * tiles_n;
+    const int high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+    const long long m0 = (long long)(band * 8 + in_band % high) * BM;
+    const long long n0 = (long long)(in_band / high) * BN;
+    long long m_end = G.m_rows;
+    if (G.m_count != nullptr) {
+        const long long c = *G.m_count;
+        m_end = c < m_end ? c : m_end;
+    }
+    if (m0 >= m_end) return;
+    // stages of this part
+    long long k = G.k;
+    if (G.k_count != nullptr) {
+        const long long c = *G.k_count;
+        k = c < k ? c : k;
+    }
+    const int all_stages = (int)((k + HEAD_K - 1) / HEAD_K);
+    const int per = (all_stages + G.splits - 1) / G.splits;
+    const int first = part * per < all_stages ? part * per : all_stages;
+    const int run = all_stages - first < per ? all_stages - first : per;  // of each product of terms
+    const int stages = __builtin_amdgcn_readfirstlane(TERMS ? run * HEAD_PRODUCTS : run);
+
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % NWM, wn = wave / NWM;
+    const int h = lane >> 5, lr = lane & 31;
+
+    auto rows_of = [](const void* base, long long ld, long long first_row, long long rows) {
+        const long long bytes = (rows - first_row) * ld;
+        return make_rsrc(static_cast<const char*>(base) + first_row * ld,
+                         (unsigned)(bytes < 0x7fffffffll ? bytes : 0x7fffffffll));
+    };
+    const rsrc_t rs_a = rows_of(G.a, G.lda, m0, m_end), rs_b = rows_of(G.b, G.ldb, n0, G.n_rows);
+    const int lda = __builtin_amdgcn_readfirstlane((int)G.lda), ldb = __builtin_amdgcn_readfirstlane((int)G.ldb);
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem;
+    const unsigned lds_a = __builtin_amdgcn_readfirstlane((int)(lds0 + wave * CA * 1024));
+    const unsigned lds_b = __builtin_amdgcn_readfirstlane((int)(lds0 + A_BYTES + wave * CB * 1024));
+    // a copy is 16 rows; a lane's row of them and chunk
+    const int copy_row = lane >> 2, copy_chunk = (lane & 3) ^ ((copy_row >> 2) & 3);
+    const unsigned a_voff = copy_row * lda + copy_chunk * 16, b_voff = copy_row * ldb + copy_chunk * 16;
+    int a_row[CA], b_row[CB];
+#pragma unroll
+    for (int j = 0; j < CA; ++j) a_row[j] = __builtin_amdgcn_readfirstlane((wave * CA + j) * 16 * lda);
+#pragma unroll
+    for (int j = 0; j < CB; ++j) b_row[j] = __builtin_amdgcn_readfirstlane((wave * CB + j) * 16 * ldb);
+
+    // the stage whose copies go out next: byte offsets within a row (out of range past the last stage)
+    int next = 0, product = 0, left = run;
+    int a_off = stages > 0 ? first * 64 : OUT_OF_RANGE, b_off = a_off;
+    if (TERMS && stages > 0) {
+        a_off += SPLIT_TERM_A[0] * G.plane_a;
+        b_off += SPLIT_TERM_B[0] * G.plane_b;
+    }
+    auto advance = [&]() {
+        ++next;
+        a_off += 64;
+        b_off += 64;
+        if constexpr (TERMS) {
+            if (--left == 0) {
+                left = run;
+                ++product;
+                // (terms of the products, two bits each)
+                constexpr int ta = SPLIT_TERM_A[0] | SPLIT_TERM_A[1] << 2 | SPLIT_TERM_A[2] << 4 | SPLIT_TERM_A[3] << 6 |
+                                   SPLIT_TERM_A[4] << 8 | SPLIT_TERM_A[5] << 10;
+                constexpr int tb = SPLIT_TERM_B[0] | SPLIT_TERM_B[1] << 2 | SPLIT_TERM_B[2] << 4 | SPLIT_TERM_B[3] << 6 |
+                                   SPLIT_TERM_B[4] << 8 | SPLIT_TERM_B[5] << 10;
+                a_off = first * 64 + (ta >> 2 * product & 3) * G.plane_a;
+                b_off = first * 64 + (tb >> 2 * product & 3) * G.plane_b;
+            }
+        }
+        a_off = next < stages ? a_off : OUT_OF_RANGE;
+        b_off = next < stages ? b_off : OUT_OF_RANGE;
+    };
+    auto copy_a = [&](auto SLOT, auto J) {
+        constexpr int slot = decltype(SLOT)::value, j = decltype(J)::value;
+        copy_to_lds_16B<slot * STAGE + j * 1024>(rs_a, lds_a, a_voff, a_off, a_row[j]);
+    };
+    auto copy_b = [&](auto SLOT, auto J) {
+        constexpr int slot = decltype(SLOT)::value, j = decltype(J)::value;
+        copy_to_lds_16B<slot * STAGE + j * 1024>(rs_b, lds_b, b_voff, b_off, b_row[j]);
+    };
+
+    // operand reads: chunk 2t + h of row lr of a 32-row tile, in place (2t + h) ^ (lr / 4 % 4)
+    const int place = h ^ ((lr >> 2) & 3);
+    const char* const a_rd[2] = {smem + (wm * WM + lr) * 64 + place * 16, smem + (wm * WM + lr) * 64 + (place ^ 2) * 16};
+    const char* const b_rd[2] = {smem + A_BYTES + (wn * WN + lr) * 64 + place * 16,
+                                 smem + A_BYTES + (wn * WN + lr) * 64 + (place ^ 2) * 16};
+    auto read_frag = [&](int slot, int t, int f) -> chunk_t {
+        const char* p = f < TN ? b_rd[t] + slot * STAGE + f * 2048 : a_rd[t] + slot * STAGE + (f - TN) * 2048;
+        return *reinterpret_cast<const chunk_t*>(p);
+    };
+
+    float16v acc[TN][TM];
+#pragma unroll
+    for (int a = 0; a < TN; ++a)
+#pragma unroll
+        for (int b = 0; b < TM; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[a][b][r] = 0.f;
+
+    // stages 0 .. NB-2 whole, the m side of stage NB-1
+    static_for<NB - 1>([&](auto S) {
+        static_for<CA>([&](auto J) { copy_a(S, J); });
+        static_for<CB>([&](auto J) { copy_b(S, J); });
+        advance();
+    });
+    static_for<CA>([&](auto J) { copy_a(std::integral_constant<int, NB - 1>{}, J); });
+#pragma unroll
+    for (int a = 0; a < TN; ++a)
+#pragma unroll
+        for (int b = 0; b < TM; ++b) asm volatile("" : "+a"(acc[a][b]));
+    {
+        constexpr int keep0 = KEEP + CA;
+        __builtin_amdgcn_s_waitcnt(0x0F70 | (keep0 & 15) | ((keep0 >> 4) << 14));
+    }
+    __syncthreads();
+    chunk_t frag[2][NFRAG];
+#pragma unroll
+    for (int f = 0; f < NFRAG; ++f) frag[0][f] = read_frag(0, 0, f);
+
+    auto mma = [&](const chunk_t& ka, const chunk_t& ib, float16v& c) {
+        if constexpr (NMMA < 16) asm volatile("" : "+a"(c));
+        Mma<Tag>::run(ka, ib, c);
+        if constexpr (NMMA < 16) asm volatile("" : "+a"(c));
+    };
+    // reads before gap i of a step's gaps, one in each of the first; copies, spread over all
+    static_assert(NFRAG <= NMMA, "a read in a gap");
+    constexpr auto reads_before = [](int i) { return i < NFRAG ? i : NFRAG; };
+    constexpr auto copies_before = [](int i, int count) { return (i * count + NMMA / 2 - 1) / NMMA; };
+    for (int st = 0; st < stages; st += NB) {
+        static_for<NB>([&](auto SLOT) {
+            constexpr int slot = decltype(SLOT)::value;
+            constexpr int slot_next = (slot + 1) % NB;
+            typedef std::integral_constant<int, (slot + NB - 1) % NB> SlotPrev;
+            static_for<NMMA>([&](auto I) {
+                constexpr int i = decltype(I)::value;
+                mma(frag[0][i / TM], frag[0][TN + i % TM], acc[i / TM][i % TM]);
+                static_for<NFRAG>([&](auto F) {
+                    constexpr int f = decltype(F)::value;
+                    if constexpr (f >= reads_before(i) && f < reads_before(i + 1)) frag[1][f] = read_frag(slot, 1, f);
+                });
+                static_for<CB>([&](auto J) {
+                    constexpr int j = decltype(J)::value;
+                    if constexpr (j >= copies_before(i, CB) && j < copies_before(i + 1, CB)) copy_b(SlotPrev{}, J);
+                });
+                if constexpr (i == NMMA - 1) advance();
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            // what this wave still needs of `slot` is in registers and its copies of the next stage have landed; after the
+            // barrier that holds for all waves
+            __builtin_amdgcn_s_waitcnt((0x0F70 | (KEEP & 15) | ((KEEP >> 4) << 14)) & 0xF0FF);
+            __syncthreads();
+            static_for<NMMA>([&](auto I) {
+                constexpr int i = decltype(I)::value;
+                mma(frag[1][i / TM], frag[1][TN + i % TM], acc[i / TM][i % TM]);
+                static_for<NFRAG>([&](auto F) {
+                    constexpr int f = decltype(F)::value;
+                    if constexpr (f >= reads_before(i) && f < reads_before(i + 1))
+                        frag[0][f] = read_frag(slot_next, 0, f);
+                });
+                static_for<CA>([&](auto J) {
+                    constexpr int j = decltype(J)::value;
+                    if constexpr (j >= copies_before(i, CA) && j < copies_before(i + 1, CA)) copy_a(SLOT, J);
+                });
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+    }
+    // the copies of the surplus stages still write (zeros) into this workgroup's LDS
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+
+    // lane (h, lr) of tile (a, b) holds in registers 4g .. 4g+3 the n values 8g + 4h + 0..3 of row lr
+    const int n_left = (int)(G.n_rows - n0 < BN ? G.n_rows - n0 : BN) - wn * WN;  // columns of this wave's that exist
+    if constexpr (END == HEAD_OUT) {
+        const float scale = G.scale != nullptr ? *G.scale : 1.0f;
+        const bool vectors = (G.ldo & 3) == 0;
+        const long long base = (m0 + wm * WM) * G.ldo + part * G.out_split + n0 + wn * WN;
+        static_for<TM>([&](auto B) {
+            constexpr int b = decltype(B)::value;
+            if (m0 + wm * WM + b * 32 + lr < m_end)
+                static_for<TN * 4>([&](auto Q) {
+                    constexpr int a = decltype(Q)::value / 4, g = decltype(Q)::value % 4;
+                    const int n = a * 32 + 8 * g + 4 * h;
+                    const long long at = base + (b * 32 + lr) * G.ldo + n;
+                    float v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)  // (one factor after the other: their product may be too small)
+                        v[j] = (TERMS ? acc[a][b][4 * g + j] * SPLIT_UNSCALE : acc[a][b][4 * g + j]) * scale;
+                    if (vectors && n + 4 <= n_left) {
+                        if (G.out_dtype == CAPSCAPS_FP32) {
+                            typedef float4v at4 __attribute__((aligned(4)));
+                            at4* to = reinterpret_cast<at4*>(static_cast<float*>(G.out) + at);
+                            float4v r = {v[0], v[1], v[2], v[3]};
+                            if (G.accumulate) r += *to;
+                            *to = r;
+                        } else {
+                            typedef unsigned u2 __attribute__((ext_vector_type(2)));
+                            typedef u2 at2 __attribute__((aligned(2)));
+                            const u2 r = G.out_dtype == CAPSCAPS_FP16 ? u2{half_pair(v[0], v[1]), half_pair(v[2], v[3])}
+                                                                      : u2{round_pair(v[0], v[1]), round_pair(v[2], v[3])};
+                            *reinterpret_cast<at2*>(static_cast<unsigned short*>(G.out) + at) = r;
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (n + j < n_left) {
+                                if (G.accumulate) v[j] += static_cast<const float*>(G.out)[at + j];
+                                store_element(G.out, at + j, v[j], G.out_dtype);
+                            }
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+        });
+        return;
+    }
+    // (z + bias) of the lane's values, in place
+    static_for<TN * 4>([&](auto Q) {
+        constexpr int a = decltype(Q)::value / 4, g = decltype(Q)::value % 4;
+        float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (G.bias != nullptr)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = a * 32 + 8 * g + 4 * h + j;
+                if (n < n_left) bias[j] = G.bias[n0 + wn * WN + n];
+            }
+        static_for<TM>([&](auto B) {
+            constexpr int b = decltype(B)::value;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float z = acc[a][b][4 * g + j];
+                acc[a][b][4 * g + j] = (TERMS ? z * SPLIT_UNSCALE : z) + bias[j];
+            }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+    });
+    if (n_left < WN)  // (columns past the last class count nothing)
+        static_for<TN * 16>([&](auto Q) {
+            constexpr int a = decltype(Q)::value / 16, r = decltype(Q)::value % 16;
+            const bool past = a * 32 + 8 * (r / 4) + 4 * h + r % 4 >= n_left;
+#pragma unroll
+            for (int b = 0; b < TM; ++b) acc[a][b][r] = past ? -__builtin_inff() : acc[a][b][r];
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    if constexpr (END == HEAD_STATS) {
+        const long long first = (G.first_part + (n0 + wn * WN) / WN) * G.m_rows;
+        const float minus = -__builtin_inff();
+        static_for<TM>([&](auto B) {
+            constexpr int b = decltype(B)::value;
+            float top = minus, sum = 0.0f;
+#pragma unroll
+            for (int a = 0; a < TN; ++a)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, acc[a][b][r]);
+            top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+            // (nothing but -infinity: every difference would be NaN)
+            const float about = top == minus ? 0.0f : top;
+            static_for<TN>([&](auto A) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += __expf((acc[decltype(A)::value][b][r] - about) * G.inv_tau);
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            sum += __shfl_xor(sum, 32);
+            const long long m = m0 + wm * WM + b * 32 + lr;
+            if (h == 0 && m < m_end && n_left > 0) G.stats[first + m] = {top * G.inv_tau, sum};
+        });
+        return;
+    }
+    if constexpr (END == HEAD_GRADIENT) {
+        constexpr int terms = TERMS ? 3 : 1;
+        constexpr bool half = std::is_same<Tag, f16_tag>::value;
+        float sums[TN * 16];
+        static_for<TN * 16>([&](auto Q) { sums[decltype(Q)::value] = 0.0f; });
+        // (columns up to a whole stage of the product that contracts classes are written, as zeros; so are rows up to one)
+        const int n_out = ((n_left + wn * WN + HEAD_K - 1) / HEAD_K) * HEAD_K - wn * WN;
+        const long long m_out = (m_end + HEAD_K - 1) / HEAD_K * HEAD_K;
+        static_for<TM>([&](auto B) {
+            constexpr int b = decltype(B)::value;
+            const long long m = m0 + wm * WM + b * 32 + lr;
+            const bool row = m < m_end;
+            const float lse = row ? G.lse[G.rows_of[m]] : 0.0f, coef = row ? G.coef[m] : 0.0f;
+            unsigned short* const gn = G.gn + m * terms * G.ldn + n0 + wn * WN;
+            unsigned short* const gt = G.gt + (n0 + wn * WN) * terms * G.ldt + (m0 + wm * WM + b * 32);
+            static_for<TN>([&](auto A) {
+                constexpr int a = decltype(A)::value;
+                float v[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float l = __builtin_fmaf(acc[a][b][r], G.inv_tau, -lse);
+                    v[r] = coef * (TERMS ? expf(l) : __expf(l));
+                    if (G.sums != nullptr) sums[a * 16 + r] += row ? v[r] : 0.0f;
+                    if constexpr (TERMS) v[r] *= SPLIT_SCALE;
+                }
+#pragma unroll
+                for (int p = 0; p < terms; ++p) {
+                    unsigned w[8];
+#pragma unroll
+                    for (int r = 0; r < 16; r += 2) {
+                        w[r / 2] = half ? half_pair(v[r], v[r + 1]) : round_pair(v[r], v[r + 1]);
+                        if (!row) w[r / 2] = 0;  // (exp of a bias, with factor 0, may be NaN)
+                        if (p + 1 < terms) {
+                            const bool lo = (w[r / 2] & 0x7f80u) == 0x7f80u, hi = (w[r / 2] & 0x7f800000u) == 0x7f800000u;
+                            v[r] = lo ? 0.0f : v[r] - low_half(w[r / 2]);
+                            v[r + 1] = hi ? 0.0f : v[r + 1] - high_half(w[r / 2]);
+                        }
+                    }
+#pragma unroll
+                    for (int pair = 0; pair < 2; ++pair) {
+                        const chunk_t c = neighbours(w, pair);
+                        const int n = a * 32 + 16 * pair + 8 * h;
+                        if (row && n < n_out) *reinterpret_cast<chunk_t*>(gn + p * G.ldn + n) = c;
+                    }
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        typedef unsigned u2 __attribute__((ext_vector_type(2)));
+                        u2 t = {w[2 * g], w[2 * g + 1]};
+                        unsigned lo = t[0], hi = t[1];
+                        turn(lo, hi, lane);
+                        t = u2{lo, hi};
+                        const int n = a * 32 + 8 * g + 4 * h + (lane & 3);
+                        if (n < n_left && m - (lane & 3) < m_out)
+                            *reinterpret_cast<u2*>(gt + ((long long)n * terms + p) * G.ldt + (lr & ~3)) = t;
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+        if (G.sums != nullptr) {
+            float* const to = G.sums + ((m0 + wm * WM) / WM) * G.ldn + n0 + wn * WN;
+            static_for<TN * 16>([&](auto Q) {
+                constexpr int a = decltype(Q)::value / 16, r = decltype(Q)::value % 16;
+                const float s = lanes_sum(sums[decltype(Q)::value], 32);
+                const int n = a * 32 + 8 * (r / 4) + 4 * h + r % 4;
+                if (lr == 0 && n < n_left) to[n] = s;
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        }
+    }
+}
+
+template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, int END>
+hipError_t launch(const HeadGemm& g, hipStream_t st)
+{
+    const long long tm = (g.m_rows + BM - 1) / BM, tn = (g.n_rows + BN - 1) / BN;
+    if (tm * tn * g.splits > (1 << 23) || tm < 1 || tn < 1) return hipErrorInvalidValue;
+    const auto kernel = head_gemm_kernel<Tag, BM, BN, NWM, NB, TERMS, END>;
+    constexpr int lds = (BM + BN) * 64 * NB;
+    static std::atomic<unsigned long long> done{0};
+    const hipError_t err = set_dynamic_lds_once(reinterpret_cast<const void*>(kernel), lds, done);
+    if (err != hipSuccess) return err;
+    kernel<<<dim3((unsigned)(tm * tn * g.splits)), dim3(256), lds, st>>>(g, (int)tm, (int)tn);
+    return hipGetLastError();
+}
+
+template <int BM, int BN, int NWM, int NB, int END>
+hipError_t launch_type(const HeadGemm& g, hipStream_t st)
+{
+    if (g.dtype == CAPSCAPS_FP32) return launch<bf16_tag, BM, BN, NWM, NB, true, END>(g, st);
+    if (g.dtype == CAPSCAPS_BF16) return launch<bf16_tag, BM, BN, NWM, NB, false, END>(g, st);
+    return launch<f16_tag, BM, BN, NWM, NB, false, END>(g, st);
+}
+
+template <int BM, int BN, int NWM, int NB>
+hipError_t launch_end(const HeadGemm& g, HeadEnd end, hipStream_t st)
+{
+    if (end == HEAD_OUT) return launch_type<BM, BN, NWM, NB, HEAD_OUT>(g, st);
+    if (end == HEAD_STATS) return launch_type<BM, BN, NWM, NB, HEAD_STATS>(g, st);
+    return launch_type<BM, BN, NWM, NB, HEAD_GRADIENT>(g, st);
+}
+
+}  // namespace
+}  // namespace capscaps

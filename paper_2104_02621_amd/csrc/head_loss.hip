@@ -280,9 +280,7 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* fr
 }
 
 // ---------------------------------------------------------------------------------------- forward
-struct Stat {
-    float top, sum;  // the largest value, and the sum of exp(value - largest)
-};
+typedef HeadStat Stat;
 __device__ __forceinline__ Stat join(const Stat& a, const Stat& b)
 {
     const float top = __builtin_fmaxf(a.top, b.top);
@@ -297,19 +295,19 @@ __device__ __forceinline__ Stat wave_join(Stat s)
     return s;
 }
 
-// stats[i][piece] of the logits of a piece (sums of `splits` parts).  A wave for a row.
+// stats[i] of logits that lie in parts.  A wave for a row.
 __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, long long ldz, int splits, long long split,
-                                                        long long first, long long classes, Stat* stats, int pieces, int piece)
+                                                        Stat* stats)
 {
     const int lane = threadIdx.x & 63;
     const float inv = 1.0f / H.tau;
     const long long kept = *H.count;
     for (long long i = blockIdx.x * 4ll + (threadIdx.x >> 6); i < kept; i += gridDim.x * 4ll) {
         Stat s = {-__builtin_inff(), 0.0f};
-        for (long long c = lane; c < classes; c += 64) {
+        for (long long c = lane; c < H.classes; c += 64) {
             float v = 0.0f;
             for (int p = 0; p < splits; ++p) v += z[p * split + i * ldz + c];
-            if (H.bias != nullptr) v += H.bias[first + c];
+            if (H.bias != nullptr) v += H.bias[c];
             v *= inv;
             if (v != v)
                 s.sum = v;
@@ -317,7 +315,7 @@ __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, 
                 s = join(s, {v, 1.0f});
         }
         s = wave_join(s);
-        if (lane == 0) stats[i * pieces + piece] = s;
+        if (lane == 0) stats[i] = s;
     }
 }
 
@@ -350,46 +348,59 @@ __device__ __forceinline__ float logit(const Head& H, long long row, long long c
     return H.bias != nullptr ? s + H.bias[cls] : s;
 }
 
-// loss, lse, logq of all rows, from the statistics of the pieces.  A workgroup for a row.
-__global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int pieces, float* loss, float* lse,
+// loss, lse, logq of all rows, from stats[part][i].  A workgroup for eight of the rows that are kept, and for the zeros
+// of eight rows that are not.
+__global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int parts, float* loss, float* lse,
                                                        float* logq, bool vectors)
 {
-    __shared__ Stat parts[4];
-    __shared__ float sums[4];
+    __shared__ Stat joined[4][8];
+    __shared__ float lses[8], sums[4][8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float inv = 1.0f / H.tau;
-    for (long long r = blockIdx.x; r < H.rows; r += gridDim.x) {
-        const int i = H.pos[r];
-        if (i < 0) {
-            if (threadIdx.x == 0) loss[r] = 0.0f, lse[r] = 0.0f;
-            if (logq != nullptr)
-                for (int k = threadIdx.x; k < H.top; k += THREADS) logq[r * H.top + k] = 0.0f;
-            continue;
-        }
-        Stat s = {-__builtin_inff(), 0.0f};
-        for (int p = threadIdx.x; p < pieces; p += THREADS) s = join(s, stats[(long long)i * pieces + p]);
-        s = wave_join(s);
-        if (lane == 0) parts[wave] = s;
-        __syncthreads();
-        s = join(join(parts[0], parts[1]), join(parts[2], parts[3]));
-        const float all = s.top + logf(s.sum);
-        float cross = 0.0f;
-        for (int k = wave; k < H.top; k += 4) {
-            const long long cls = index_of(H, r, k);
-            float l = 0.0f;
-            if (cls >= 0) {
-                l = logit(H, r, cls, lane, vectors) * inv - all;
-                const float t = share_of(H, r, k);
-                if (t != 0.0f) cross += t * l;
+    const int kept = *H.count;
+    for (long long i0 = blockIdx.x * 8ll; i0 < H.rows; i0 += gridDim.x * 8ll) {
+        for (int t = threadIdx.x; t < 8 * H.top; t += THREADS) {
+            const long long r = i0 + t / H.top;
+            if (r < H.rows && H.pos[r] < 0) {
+                if (t % H.top == 0) loss[r] = 0.0f, lse[r] = 0.0f;
+                if (logq != nullptr) logq[r * H.top + t % H.top] = 0.0f;
             }
-            if (logq != nullptr && lane == 0) logq[r * H.top + k] = l;
         }
-        if (lane == 0) sums[wave] = cross;
+        if (i0 >= kept) continue;
+        const int rows = kept - i0 < 8 ? (int)(kept - i0) : 8;
+        Stat s = {-__builtin_inff(), 0.0f};
+        if ((lane & 7) < rows)
+            for (int p = threadIdx.x >> 3; p < parts; p += THREADS / 8) s = join(s, stats[p * H.rows + i0 + (lane & 7)]);
+#pragma unroll
+        for (int k = 8; k < 64; k <<= 1) s = join(s, {__shfl_xor(s.top, k), __shfl_xor(s.sum, k)});
+        if (lane < 8) joined[wave][lane] = s;
         __syncthreads();
-        if (threadIdx.x == 0) {
+        if (threadIdx.x < 8) {
+            s = join(join(joined[0][lane], joined[1][lane]), join(joined[2][lane], joined[3][lane]));
+            lses[lane] = s.top + logf(s.sum);
+        }
+        __syncthreads();
+        for (int j = 0; j < rows; ++j) {
+            const long long r = H.rows_of[i0 + j];
+            float cross = 0.0f;
+            for (int k = wave; k < H.top; k += 4) {
+                const long long cls = index_of(H, r, k);
+                float l = 0.0f;
+                if (cls >= 0) {
+                    l = logit(H, r, cls, lane, vectors) * inv - lses[j];
+                    const float t = share_of(H, r, k);
+                    if (t != 0.0f) cross += t * l;
+                }
+                if (logq != nullptr && lane == 0) logq[r * H.top + k] = l;
+            }
+            if (lane == 0) sums[wave][j] = cross;
+        }
+        __syncthreads();
+        if (threadIdx.x < rows) {
+            const long long r = H.rows_of[i0 + lane];
             const float entropy = H.teacher != nullptr ? H.entropy[r] : 0.0f;
-            loss[r] = H.tau * H.tau * (entropy - ((sums[0] + sums[1]) + (sums[2] + sums[3])));
-            lse[r] = all;
+            loss[r] = H.tau * H.tau * (entropy - ((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane])));
+            lse[r] = lses[lane];
         }
         __syncthreads();
     }
@@ -558,31 +569,33 @@ __global__ void __launch_bounds__(THREADS) finish_kernel(const int* count, const
 
 // ---------------------------------------------------------------------------------------- host
 long long round_up(long long v, long long to) { return (v + to - 1) / to * to; }
+int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 unsigned blocks_for(long long work, long long per) { return (unsigned)std::max<long long>(1, std::min<long long>((work + per - 1) / per, 1 << 20)); }
 
-// Tile and parts of a product: the least of an estimate in units of a 256 x 256 tile's stage (1024 matrix cycles).  A CU
-// takes one such tile, or two of the others, whose stage costs a quarter of it in instructions and 1.25 times that
-// with their operands' reads.  A tile begins and ends in the time of some stages, and parts are added up at memory speed.
+// Tile and parts of a product: the least of an estimate in units of a 256 x 256 tile's stage on a CU (1024 matrix
+// cycles, 0.43 us).  A tile begins and ends in the time of some stages; parts are written and added up at memory speed.
 struct Pick {
     int tile, splits;
 };
-Pick pick_tile(long long m, long long n, long long k, int terms, bool may_split)
+Pick pick_tile(long long m, long long n, long long k, int terms, bool may_split, double part_us)
 {
     const long long stages = std::max<long long>(1, (k + HEAD_K - 1) / HEAD_K) * (terms > 1 ? HEAD_PRODUCTS : 1);
     Pick best{HEAD_TILE_128, 1};
     double least = 1e300;
-    for (const int tile : {HEAD_TILE_256, HEAD_TILE_128, HEAD_TILE_FEW_ROWS}) {
+    for (const int tile : {HEAD_TILE_256, HEAD_TILE_HALF, HEAD_TILE_128, HEAD_TILE_FEW_ROWS}) {
         const HeadTileShape s = head_tile_shape(tile);
         const double tiles = (double)((m + s.m - 1) / s.m) * (double)((n + s.n - 1) / s.n);
-        const double slots = tile == HEAD_TILE_256 ? 256 : 512, cost = tile == HEAD_TILE_256 ? 1.0 : 0.625;
-        const double ends = tile == HEAD_TILE_256 ? 24 : 20;
+        const double slots = 256.0 * s.per_cu;
+        // time of a stage of as many tiles as a CU holds, and stages' time to begin and end
+        const double cost = tile == HEAD_TILE_256 ? 1.0 : tile == HEAD_TILE_HALF ? 1.04 : 0.625;
+        const double ends = tile == HEAD_TILE_256 ? 24 : tile == HEAD_TILE_HALF ? 12 : 10;
         for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts * 2) {
             if (parts > 1 && (!may_split || stages / parts < 8)) break;
             if (tiles * parts > (1 << 23)) continue;
-            const double rounds = std::max(1.0, tiles * parts <= slots * 4 ? (double)(long long)((tiles * parts + slots - 1) / slots) : tiles * parts / slots);
+            const double load = tiles * parts / slots;
+            const double rounds = load <= 4 ? std::max(1.0, (double)(long long)(load + 0.999)) : load;
             double t = rounds * ((double)((stages + parts - 1) / parts) + ends) * cost;
-            // 0.43 us a stage; 8 bytes a value and part at 4 TB/s, and a launch
-            if (parts > 1) t += ((double)m * n * 8 * parts / 4e6 + 3.0) / 0.43;
+            if (parts > 1) t += ((double)m * n * 8 * parts / 4e6 + part_us) / 0.43;
             if (t < least) least = t, best = {tile, parts};
         }
     }
@@ -613,13 +626,13 @@ struct Layout {
 };
 
 struct Plan {
-    int terms, padded;            // terms of an operand's value, contracted width
-    bool weight_in_place;
-    long long piece;              // classes of a piece
-    int pieces, padded_piece;
+    int terms, padded;  // terms of an operand's value, contracted width
+    bool in_parts;      // logits in parts: few enough to lie in memory
+    long long piece;    // classes of a piece
+    int pieces, stat_parts;
     long long padded_rows;
     Pick z, dx, dw;
-    bool distill, backward, bias;
+    bool distill, backward;
     size_t bytes;
     // the workspace
     unsigned short *x, *xt, *w, *wt, *gn, *gt;
@@ -643,14 +656,15 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     P.padded = (int)round_up(A.width, HEAD_K);
     P.padded_rows = round_up(std::max<long long>(A.rows, 1), HEAD_K);
     const long long rows = std::max<long long>(A.rows, 1);
-    const long long row_bytes = rows * std::max(4, backward ? 2 * P.terms : 0);
-    P.piece = std::max<long long>(256, std::min(MOST_PIECE, PIECE_BYTES / row_bytes / 256 * 256));
+    // a piece's weights as operands, and its gradients
+    const long long per_class = 2ll * P.terms * std::max<long long>(P.padded, backward ? rows : 0);
+    P.piece = std::max<long long>(256, std::min(MOST_PIECE, PIECE_BYTES / per_class / 256 * 256));
     P.piece = std::min<long long>(round_up(A.classes, HEAD_K), P.piece);
     P.pieces = (int)((A.classes + P.piece - 1) / P.piece);
-    P.padded_piece = (int)P.piece;
     const long long most = std::min<long long>(P.piece, A.classes);
-    // (the parts of a product's logits lie in the piece's room for them: as many as that allows)
-    P.z = pick_tile(rows, most, A.width, P.terms, P.pieces == 1 && rows * P.piece * 4 <= PIECE_BYTES / 8);
+    P.z = pick_tile(rows, most, A.width, P.terms, P.pieces == 1 && rows * P.piece * 64 * 4 <= PIECE_BYTES, 6.0);
+    P.in_parts = P.z.splits > 1;
+    P.stat_parts = P.in_parts ? 1 : ceil_div(A.classes, head_tile_shape(P.z.tile).stat_columns);
     Layout L{static_cast<char*>(base)};
     Head unused;
     Head& W = H != nullptr ? *H : unused;
@@ -662,24 +676,23 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     W.entropy = distill ? L.take<float>(A.rows) : nullptr;
     P.x = L.take<unsigned short>(rows * P.terms * P.padded);
     P.w = L.take<unsigned short>(most * P.terms * P.padded);
-    P.logits = L.take<float>(rows * P.piece * P.z.splits);
+    P.logits = P.in_parts ? L.take<float>(rows * P.piece * P.z.splits) : nullptr;
     if (!backward) {
-        P.stats = L.take<Stat>(rows * P.pieces);
+        P.stats = L.take<Stat>(rows * P.stat_parts);
         P.bytes = L.at;
         return P;
     }
     W.coef = L.take<float>(A.rows);
-    P.dx = pick_tile(rows, A.width, P.piece, P.terms, true);
-    P.dw = pick_tile(most, A.width, rows, P.terms, true);
-    if (P.pieces > 1) P.dx.splits = 1;  // (added up piece after piece instead)
+    P.dx = pick_tile(rows, A.width, P.piece, P.terms, P.pieces == 1, 0.0);  // (several: added up piece after piece)
+    P.dw = pick_tile(most, A.width, rows, P.terms, true, 3.0);
     const long long ld = round_up(A.width, 4);
     P.xt = L.take<unsigned short>((long long)A.width * P.terms * P.padded_rows);
-    P.wt = L.take<unsigned short>((long long)A.width * P.terms * P.padded_piece);
-    P.gn = L.take<unsigned short>(rows * P.terms * P.padded_piece);
+    P.wt = L.take<unsigned short>((long long)A.width * P.terms * P.piece);
+    P.gn = L.take<unsigned short>(rows * P.terms * P.piece);
     P.gt = L.take<unsigned short>(most * P.terms * P.padded_rows);
     P.dx_sums = L.take<float>(rows * ld * P.dx.splits);
     P.dw_sums = P.dw.splits > 1 ? L.take<float>(most * ld * P.dw.splits) : nullptr;
-    P.bias_sums = L.take<float>((rows + 63) / 64 * P.padded_piece);
+    P.bias_sums = L.take<float>((rows + 63) / 64 * P.piece);
     P.taken = L.take<long long>(A.classes);
     P.bytes = L.at;
     return P;
@@ -731,8 +744,8 @@ int begin(const Head& H, const Plan& P, const float* dloss, long long dloss_stri
     return CAPSCAPS_OK;
 }
 
-// A piece's logits without the bias
-int logits_of(const Head& H, const Plan& P, long long first, long long classes, hipStream_t st)
+// The product of x and a piece's weights, for launch_head_gemm with an end of the caller's
+int logits_of(const Head& H, const Plan& P, long long first, long long classes, HeadGemm& g, hipStream_t st)
 {
     const void* w = weight_at(H, first);
     long long ldw = H.weight_stride * 2;
@@ -742,14 +755,18 @@ int logits_of(const Head& H, const Plan& P, long long first, long long classes, 
         w = P.w;
         ldw = (long long)P.terms * P.padded * 2;
     }
-    HeadGemm g{};
+    g = HeadGemm{};
     g.a = P.x, g.b = w;
     g.lda = (long long)P.terms * P.padded * 2, g.ldb = ldw;
     g.m_rows = H.rows, g.n_rows = classes, g.m_count = H.count, g.k = H.width;
     g.plane_a = g.plane_b = P.padded * 2;
-    g.dtype = H.dtype, g.out = P.logits, g.ldo = P.piece, g.out_split = H.rows * P.piece, g.out_dtype = CAPSCAPS_FP32;
-    g.splits = P.z.splits;
-    CAPSCAPS_TRY(launch_head_gemm(g, P.z.tile, st));
+    g.dtype = H.dtype, g.splits = P.z.splits;
+    if (P.in_parts) {
+        g.out = P.logits, g.ldo = P.piece, g.out_split = H.rows * P.piece, g.out_dtype = CAPSCAPS_FP32;
+    } else {
+        g.bias = H.bias != nullptr ? H.bias + first : nullptr;
+        g.inv_tau = 1.0f / H.tau;
+    }
     return CAPSCAPS_OK;
 }
 
@@ -760,13 +777,18 @@ int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, 
     if (rc != CAPSCAPS_OK) return rc;
     for (int piece = 0; piece < P.pieces; ++piece) {
         const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
-        rc = logits_of(H, P, first, classes, st);
+        HeadGemm g;
+        rc = logits_of(H, P, first, classes, g, st);
         if (rc != CAPSCAPS_OK) return rc;
-        CAPSCAPS_TRY(run(stats_kernel, blocks_for(H.rows, 4), THREADS, st, H, (const float*)P.logits, P.piece, P.z.splits,
-                         H.rows * P.piece, first, classes, P.stats, P.pieces, piece));
+        g.stats = P.stats;
+        g.first_part = (int)(first / head_tile_shape(P.z.tile).stat_columns);
+        CAPSCAPS_TRY(launch_head_gemm(g, P.z.tile, P.in_parts ? HEAD_OUT : HEAD_STATS, st));
+        if (P.in_parts)
+            CAPSCAPS_TRY(run(stats_kernel, blocks_for(H.rows, 4), THREADS, st, H, (const float*)P.logits, P.piece, P.z.splits,
+                             H.rows * P.piece, P.stats));
     }
     const bool vectors = vectors_of(H.x, H.x_stride, H.dtype) && vectors_of(H.weight, H.weight_stride, H.dtype) && H.width % 8 == 0;
-    CAPSCAPS_TRY(run(loss_kernel, blocks_for(H.rows, 1), THREADS, st, H, (const Stat*)P.stats, P.pieces, loss, lse, logq, vectors));
+    CAPSCAPS_TRY(run(loss_kernel, blocks_for(H.rows, 8), THREADS, st, H, (const Stat*)P.stats, P.stat_parts, loss, lse, logq, vectors));
     return CAPSCAPS_OK;
 }
 
@@ -785,17 +807,26 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
     const int size = (int)element_bytes(H.dtype);
     for (int piece = 0; piece < P.pieces; ++piece) {
         const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
-        int rc = logits_of(H, P, first, classes, st);
+        HeadGemm z;
+        const int rc = logits_of(H, P, first, classes, z, st);
         if (rc != CAPSCAPS_OK) return rc;
         const int padded = (int)round_up(classes, HEAD_K);
-        const long long tiles = (P.padded_rows + 63) / 64 * ((padded + 63) / 64);
-        CAPSCAPS_TRY(run(gradient_kernel<TERMS>, blocks_for(tiles, 1), THREADS, st, H, G.lse, (const float*)P.logits, P.piece, P.z.splits,
-                         H.rows * P.piece, first, (int)classes, P.gn, padded, P.gt, P.padded_rows,
-                         G.dbias != nullptr ? P.bias_sums : nullptr));
+        float* const sums = G.dbias != nullptr ? P.bias_sums : nullptr;
+        if (P.in_parts) {
+            CAPSCAPS_TRY(launch_head_gemm(z, P.z.tile, HEAD_OUT, st));
+            const long long tiles = (P.padded_rows + 63) / 64 * ((padded + 63) / 64);
+            CAPSCAPS_TRY(run(gradient_kernel<TERMS>, blocks_for(tiles, 1), THREADS, st, H, G.lse, (const float*)P.logits, P.piece,
+                             P.z.splits, H.rows * P.piece, first, (int)classes, P.gn, padded, P.gt, P.padded_rows, sums));
+        } else {
+            z.coef = H.coef, z.lse = G.lse, z.rows_of = H.rows_of;
+            z.gn = P.gn, z.gt = P.gt, z.ldn = padded, z.ldt = P.padded_rows, z.sums = sums;
+            CAPSCAPS_TRY(launch_head_gemm(z, P.z.tile, HEAD_GRADIENT, st));
+        }
         CAPSCAPS_TRY(run(entries_kernel<TERMS>, blocks_for(H.rows, 4), THREADS, st, H, G.loss, G.logq, first, (int)classes, P.gn,
                          padded, P.gt, P.padded_rows, G.dbias != nullptr ? P.taken : nullptr));
         if (G.dbias != nullptr)
-            CAPSCAPS_TRY(run(bias_kernel, (unsigned)((classes + THREADS - 1) / THREADS), THREADS, st, H, (const float*)P.bias_sums, padded, 64,
+            CAPSCAPS_TRY(run(bias_kernel, (unsigned)((classes + THREADS - 1) / THREADS), THREADS, st, H, (const float*)P.bias_sums, padded,
+                             P.in_parts ? 64 : head_tile_shape(P.z.tile).sum_rows,
                              (const long long*)P.taken, first, (int)classes, G.dbias));
         if (G.dx != nullptr) {
             CAPSCAPS_TRY(pack_transposed(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, P.wt, padded, st));
@@ -806,7 +837,7 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
             g.plane_a = g.plane_b = padded * 2;
             g.dtype = H.dtype, g.out = P.dx_sums, g.ldo = ld, g.out_split = H.rows * ld, g.out_dtype = CAPSCAPS_FP32;
             g.splits = P.dx.splits, g.accumulate = piece > 0;
-            CAPSCAPS_TRY(launch_head_gemm(g, P.dx.tile, st));
+            CAPSCAPS_TRY(launch_head_gemm(g, P.dx.tile, HEAD_OUT, st));
         }
         if (G.dweight != nullptr) {
             char* out = static_cast<char*>(G.dweight) + first * H.width * size;
@@ -820,7 +851,7 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
             g.out = direct ? out : (void*)P.dw_sums;
             g.ldo = direct ? H.width : ld, g.out_split = classes * ld, g.out_dtype = direct ? H.dtype : CAPSCAPS_FP32;
             if (direct) g.scale = scale;
-            CAPSCAPS_TRY(launch_head_gemm(g, P.dw.tile, st));
+            CAPSCAPS_TRY(launch_head_gemm(g, P.dw.tile, HEAD_OUT, st));
             if (!direct)
                 CAPSCAPS_TRY(run(finish_kernel, blocks_for(classes * (ld / 4), THREADS), THREADS, st, (const int*)H.count, (const int*)nullptr,
                                  (const float*)P.dw_sums, ld, P.dw.splits, classes * ld, classes, H.width, (void*)out, H.dtype));
