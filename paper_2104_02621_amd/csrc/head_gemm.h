@@ -6,8 +6,21 @@
 
 namespace capscaps {
 
-constexpr int HEAD_K = 32;        // contracted values of a stage; rows are padded with zeros to a multiple
+constexpr int HEAD_K = 32;        // contracted values of a stage; operands are padded with zeros to a multiple
 constexpr int HEAD_PRODUCTS = 6;  // fp32 operands: products of their bf16 terms
+
+// An operand in blocks: 16 rows of a stage, 1 KB, in the order in which they lie in LDS, so that one copy of a wave is one
+// run of memory.  (Copies of 64 bytes from each of 16 rows make half as wide requests of the L2, of which a CU has only so
+// many on their way: a product of 8192 x 2048 x 32768 runs at 700 TFLOP/s so on tiles of 256 x 256, and at 1450 with
+// blocks.)
+// `stages`: those of a row block, the terms of fp32 operands one after another.  Offset of value k of a row, in values:
+__host__ __device__ inline long long head_block_at(long long row, long long k, long long stages)
+{
+    const long long block = (row >> 4) * stages + (k >> 5);
+    const int r = (int)(row & 15), chunk = (int)(k >> 3) & 3;
+    return block * 512 + r * 32 + ((chunk ^ (r >> 2)) << 3) + (int)(k & 7);
+}
+inline long long head_block_values(long long rows, long long stages) { return (rows + 15) / 16 * stages * 512; }
 
 // What a product's tiles become
 enum HeadEnd {
@@ -20,16 +33,16 @@ struct HeadStat {
     float top, sum;
 };
 
-// z[m][n] = sum over k of a[m][k] * b[n][k].  Rows of a and b are whole 16-byte vectors at 16-byte addresses, zeros from the
-// contracted length up to a multiple of HEAD_K; fp32 operands lie there as three bf16 terms one after another (`plane` bytes each).
+// z[m][n] = sum over k of a[m][k] * b[n][k], both in blocks; or b as rows (16 bits, whole stages, whole 16-byte vectors).
 struct HeadGemm {
     const void *a, *b;
-    long long lda, ldb;        // bytes from row to row
-    long long m_rows, n_rows;  // rows that may be read (beyond them: zeros)
+    long long stages_a, stages_b;  // stages of a row block, all terms together; b as rows: 0
+    long long ldb;                 // b as rows: bytes from row to row
+    long long m_rows, n_rows;
     const int* m_count;        // NULL, or how many of the m rows count, in device memory
     const int* k_count;        // NULL, or how many contracted values count, in device memory
     long long k;
-    int plane_a, plane_b;
+    int plane_a, plane_b;  // stages of a term of fp32 operands
     int dtype;
     // HEAD_OUT: fp32 (out_dtype) or 16 bits; parts of the contracted length go to copies `out_split` elements apart
     void* out;
@@ -40,13 +53,13 @@ struct HeadGemm {
     // the others: logit = (z + bias[n]) * inv_tau
     const float* bias;  // or NULL
     float inv_tau;
-    HeadStat* stats;  // [first_part + n / head_stat_columns(tile)][m_rows]
+    HeadStat* stats;  // [first_part + n / stat_columns][m_rows]
     int first_part;
     const float *coef, *lse;  // of row m, and of row rows_of[m]
     const int* rows_of;
-    unsigned short *gn, *gt;        // [m][terms][ldn] and [n][terms][ldt]
-    long long ldn, ldt;
-    float* sums;  // NULL, or [m / head_sum_rows(tile)][ldn]
+    unsigned short *gn, *gt;  // rows m and rows n, in blocks of planes_n and planes_t stages a term
+    int planes_n, planes_t;
+    float* sums;  // NULL, or [m / sum_rows][planes_n * HEAD_K]
 };
 
 // tile shapes, the columns of a statistic and the rows of a sum over rows (those of a wave)

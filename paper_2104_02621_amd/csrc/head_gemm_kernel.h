@@ -10,9 +10,9 @@
 // instructions (32x32x16); between them go, one at a time, the LDS reads of the next step's operands and the copies of
 // the stage four ahead.  One barrier a stage, before its second step, whose operands are in registers by then.
 //
-// LDS stage: rows of 64 bytes, four 16-byte chunks, chunk c of row r in place c ^ (r / 4 % 4): four neighbouring lanes of a
-// copy bring one row's 64 contiguous bytes, and the 16 lanes that read one chunk of 16 rows touch 16 different 16-byte
-// columns of the banks.  The n side is the matrix instruction's row operand, so that a lane ends up with runs of four
+// LDS stage: rows of 64 bytes, four 16-byte chunks, chunk c of row r in place c ^ (r / 4 % 4): the 16 lanes that read one
+// chunk of 16 rows touch 16 different 16-byte columns of the banks.  Operands in blocks lie so in memory; of one that is
+// rows, four neighbouring lanes of a copy bring a row's 64 bytes.  The n side is the matrix instruction's row operand, so that a lane ends up with runs of four
 // neighbouring n of one m.
 #pragma once
 #include "head_gemm.h"
@@ -62,7 +62,7 @@ __device__ __forceinline__ void turn(unsigned& lo, unsigned& hi, int lane)
 }
 
 // NB: stages of the ring
-template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, int END>
+template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, bool ROWS, int END>
 __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kernel(const HeadGemm G, int tiles_m, int tiles_n)
 {
     constexpr int NWN = 4 / NWM, WM = BM / NWM, WN = BN / NWN, TM = WM / 32, TN = WN / 32;
@@ -90,20 +90,20 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
     const long long n0 = (long long)(in_band / high) * BN;
     long long m_end = G.m_rows;
     if (G.m_count != nullptr) {
-        const long long c = *G.m_count;
+        const long long c = __builtin_amdgcn_readfirstlane(*G.m_count);
         m_end = c < m_end ? c : m_end;
     }
     if (m0 >= m_end) return;
     // stages of this part
     long long k = G.k;
     if (G.k_count != nullptr) {
-        const long long c = *G.k_count;
+        const long long c = __builtin_amdgcn_readfirstlane(*G.k_count);
         k = c < k ? c : k;
     }
     const int all_stages = (int)((k + HEAD_K - 1) / HEAD_K);
-    const int per = (all_stages + G.splits - 1) / G.splits;
-    const int first = part * per < all_stages ? part * per : all_stages;
-    const int run = all_stages - first < per ? all_stages - first : per;  // of each product of terms
+    const int per = __builtin_amdgcn_readfirstlane((all_stages + G.splits - 1) / G.splits);
+    const int first = __builtin_amdgcn_readfirstlane(part * per < all_stages ? part * per : all_stages);
+    const int run = __builtin_amdgcn_readfirstlane(all_stages - first < per ? all_stages - first : per);  // of each product of terms
     const int stages = __builtin_amdgcn_readfirstlane(TERMS ? run * HEAD_PRODUCTS : run);
 
     const int lane = threadIdx.x & 63;
@@ -111,48 +111,58 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
     const int wm = wave % NWM, wn = wave / NWM;
     const int h = lane >> 5, lr = lane & 31;
 
-    auto rows_of = [](const void* base, long long ld, long long first_row, long long rows) {
-        const long long bytes = (rows - first_row) * ld;
-        return make_rsrc(static_cast<const char*>(base) + first_row * ld,
+    auto blocks_of = [](const void* base, long long stages, long long first_row, long long rows) {
+        const long long bytes = ((rows + 15) / 16 - first_row / 16) * stages * 1024;
+        return make_rsrc(static_cast<const char*>(base) + first_row / 16 * stages * 1024,
                          (unsigned)(bytes < 0x7fffffffll ? bytes : 0x7fffffffll));
     };
-    const rsrc_t rs_a = rows_of(G.a, G.lda, m0, m_end), rs_b = rows_of(G.b, G.ldb, n0, G.n_rows);
-    const int lda = __builtin_amdgcn_readfirstlane((int)G.lda), ldb = __builtin_amdgcn_readfirstlane((int)G.ldb);
+    const rsrc_t rs_a = blocks_of(G.a, G.stages_a, m0, m_end);
+    rsrc_t rs_b;
+    if constexpr (ROWS) {
+        const long long bytes = (G.n_rows - n0) * G.ldb;
+        rs_b = make_rsrc(static_cast<const char*>(G.b) + n0 * G.ldb, (unsigned)(bytes < 0x7fffffffll ? bytes : 0x7fffffffll));
+    } else {
+        rs_b = blocks_of(G.b, G.stages_b, n0, G.n_rows);
+    }
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) char*)smem;
     const unsigned lds_a = __builtin_amdgcn_readfirstlane((int)(lds0 + wave * CA * 1024));
     const unsigned lds_b = __builtin_amdgcn_readfirstlane((int)(lds0 + A_BYTES + wave * CB * 1024));
-    // a copy is 16 rows; a lane's row of them and chunk
-    const int copy_row = lane >> 2, copy_chunk = (lane & 3) ^ ((copy_row >> 2) & 3);
-    const unsigned a_voff = copy_row * lda + copy_chunk * 16, b_voff = copy_row * ldb + copy_chunk * 16;
+    // a copy is a block: 16 rows
+    const int row_step_a = __builtin_amdgcn_readfirstlane((int)(G.stages_a * 1024));
+    const int row_step_b = __builtin_amdgcn_readfirstlane((int)(ROWS ? 16 * G.ldb : G.stages_b * 1024));
+    constexpr int step_b = ROWS ? 64 : 1024;  // bytes from stage to stage
+    const unsigned a_voff = lane * 16;
+    const unsigned b_voff = ROWS ? (lane >> 2) * (row_step_b >> 4) + ((lane & 3) ^ (lane >> 4)) * 16 : lane * 16;
     int a_row[CA], b_row[CB];
 #pragma unroll
-    for (int j = 0; j < CA; ++j) a_row[j] = __builtin_amdgcn_readfirstlane((wave * CA + j) * 16 * lda);
+    for (int j = 0; j < CA; ++j) a_row[j] = __builtin_amdgcn_readfirstlane((wave * CA + j) * row_step_a);
 #pragma unroll
-    for (int j = 0; j < CB; ++j) b_row[j] = __builtin_amdgcn_readfirstlane((wave * CB + j) * 16 * ldb);
+    for (int j = 0; j < CB; ++j) b_row[j] = __builtin_amdgcn_readfirstlane((wave * CB + j) * row_step_b);
 
-    // the stage whose copies go out next: byte offsets within a row (out of range past the last stage)
+    // the stage whose copies go out next: byte offsets from a row's beginning (out of range past the last stage)
     int next = 0, product = 0, left = run;
-    int a_off = stages > 0 ? first * 64 : OUT_OF_RANGE, b_off = a_off;
+    int a_off = stages > 0 ? first * 1024 : OUT_OF_RANGE, b_off = stages > 0 ? first * step_b : OUT_OF_RANGE;
     if (TERMS && stages > 0) {
-        a_off += SPLIT_TERM_A[0] * G.plane_a;
-        b_off += SPLIT_TERM_B[0] * G.plane_b;
+        a_off += SPLIT_TERM_A[0] * G.plane_a * 1024;
+        b_off += SPLIT_TERM_B[0] * G.plane_b * 1024;
     }
     auto advance = [&]() {
         ++next;
-        a_off += 64;
-        b_off += 64;
+        a_off += 1024;
+        b_off += step_b;
         if constexpr (TERMS) {
-            if (--left == 0) {
-                left = run;
-                ++product;
-                // (terms of the products, two bits each)
-                constexpr int ta = SPLIT_TERM_A[0] | SPLIT_TERM_A[1] << 2 | SPLIT_TERM_A[2] << 4 | SPLIT_TERM_A[3] << 6 |
-                                   SPLIT_TERM_A[4] << 8 | SPLIT_TERM_A[5] << 10;
-                constexpr int tb = SPLIT_TERM_B[0] | SPLIT_TERM_B[1] << 2 | SPLIT_TERM_B[2] << 4 | SPLIT_TERM_B[3] << 6 |
-                                   SPLIT_TERM_B[4] << 8 | SPLIT_TERM_B[5] << 10;
-                a_off = first * 64 + (ta >> 2 * product & 3) * G.plane_a;
-                b_off = first * 64 + (tb >> 2 * product & 3) * G.plane_b;
-            }
+            // (terms of the products, two bits each)
+            constexpr int ta = SPLIT_TERM_A[0] | SPLIT_TERM_A[1] << 2 | SPLIT_TERM_A[2] << 4 | SPLIT_TERM_A[3] << 6 |
+                               SPLIT_TERM_A[4] << 8 | SPLIT_TERM_A[5] << 10;
+            constexpr int tb = SPLIT_TERM_B[0] | SPLIT_TERM_B[1] << 2 | SPLIT_TERM_B[2] << 4 | SPLIT_TERM_B[3] << 6 |
+                               SPLIT_TERM_B[4] << 8 | SPLIT_TERM_B[5] << 10;
+            const bool wrap = --left == 0;
+            product += wrap ? 1 : 0;
+            left = wrap ? run : left;
+            const int at_a = (first + (ta >> 2 * product & 3) * G.plane_a) * 1024;
+            const int at_b = (first + (tb >> 2 * product & 3) * G.plane_b) * 1024;
+            a_off = wrap ? at_a : a_off;
+            b_off = wrap ? at_b : b_off;
         }
         a_off = next < stages ? a_off : OUT_OF_RANGE;
         b_off = next < stages ? b_off : OUT_OF_RANGE;
@@ -359,13 +369,15 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
         // (columns up to a whole stage of the product that contracts classes are written, as zeros; so are rows up to one)
         const int n_out = ((n_left + wn * WN + HEAD_K - 1) / HEAD_K) * HEAD_K - wn * WN;
         const long long m_out = (m_end + HEAD_K - 1) / HEAD_K * HEAD_K;
+        const long long sn = (long long)terms * G.planes_n, stt = (long long)terms * G.planes_t;
         static_for<TM>([&](auto B) {
             constexpr int b = decltype(B)::value;
             const long long m = m0 + wm * WM + b * 32 + lr;
             const bool row = m < m_end;
             const float lse = row ? G.lse[G.rows_of[m]] : 0.0f, coef = row ? G.coef[m] : 0.0f;
-            unsigned short* const gn = G.gn + m * terms * G.ldn + n0 + wn * WN;
-            unsigned short* const gt = G.gt + (n0 + wn * WN) * terms * G.ldt + (m0 + wm * WM + b * 32);
+            // row m at the wave's first class, without its chunk; stage of these 32 rows in gt
+            unsigned short* const gn = G.gn + ((m >> 4) * sn + ((n0 + wn * WN) >> 5)) * 512 + (m & 15) * 32;
+            const long long stage_t = (m0 + wm * WM + b * 32) >> 5;
             static_for<TN>([&](auto A) {
                 constexpr int a = decltype(A)::value;
                 float v[16];
@@ -392,8 +404,9 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
 #pragma unroll
                     for (int pair = 0; pair < 2; ++pair) {
                         const chunk_t c = neighbours(w, pair);
-                        const int n = a * 32 + 16 * pair + 8 * h;
-                        if (row && n < n_out) *reinterpret_cast<chunk_t*>(gn + p * G.ldn + n) = c;
+                        const int place = (2 * pair + h) ^ ((lr >> 2) & 3);
+                        if (row && a * 32 < n_out)
+                            *reinterpret_cast<chunk_t*>(gn + ((long long)p * G.planes_n + a) * 512 + place * 8) = c;
                     }
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
@@ -403,15 +416,17 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
                         turn(lo, hi, lane);
                         t = u2{lo, hi};
                         const int n = a * 32 + 8 * g + 4 * h + (lane & 3);
+                        const int nr = n & 15, place = (lr >> 3) ^ (nr >> 2);
                         if (n < n_left && m - (lane & 3) < m_out)
-                            *reinterpret_cast<u2*>(gt + ((long long)n * terms + p) * G.ldt + (lr & ~3)) = t;
+                            *reinterpret_cast<u2*>(G.gt + (((n0 + wn * WN + n) >> 4) * stt + p * G.planes_t + stage_t) * 512 +
+                                                   nr * 32 + place * 8 + (lr & 4)) = t;
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
         if (G.sums != nullptr) {
-            float* const to = G.sums + ((m0 + wm * WM) / WM) * G.ldn + n0 + wn * WN;
+            float* const to = G.sums + ((m0 + wm * WM) / WM) * G.planes_n * HEAD_K + n0 + wn * WN;
             static_for<TN * 16>([&](auto Q) {
                 constexpr int a = decltype(Q)::value / 16, r = decltype(Q)::value % 16;
                 const float s = lanes_sum(sums[decltype(Q)::value], 32);
@@ -423,12 +438,12 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
     }
 }
 
-template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, int END>
+template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, bool ROWS, int END>
 hipError_t launch(const HeadGemm& g, hipStream_t st)
 {
     const long long tm = (g.m_rows + BM - 1) / BM, tn = (g.n_rows + BN - 1) / BN;
     if (tm * tn * g.splits > (1 << 23) || tm < 1 || tn < 1) return hipErrorInvalidValue;
-    const auto kernel = head_gemm_kernel<Tag, BM, BN, NWM, NB, TERMS, END>;
+    const auto kernel = head_gemm_kernel<Tag, BM, BN, NWM, NB, TERMS, ROWS, END>;
     constexpr int lds = (BM + BN) * 64 * NB;
     static std::atomic<unsigned long long> done{0};
     const hipError_t err = set_dynamic_lds_once(reinterpret_cast<const void*>(kernel), lds, done);
@@ -440,9 +455,13 @@ hipError_t launch(const HeadGemm& g, hipStream_t st)
 template <int BM, int BN, int NWM, int NB, int END>
 hipError_t launch_type(const HeadGemm& g, hipStream_t st)
 {
-    if (g.dtype == CAPSCAPS_FP32) return launch<bf16_tag, BM, BN, NWM, NB, true, END>(g, st);
-    if (g.dtype == CAPSCAPS_BF16) return launch<bf16_tag, BM, BN, NWM, NB, false, END>(g, st);
-    return launch<f16_tag, BM, BN, NWM, NB, false, END>(g, st);
+    if (g.dtype == CAPSCAPS_FP32) return launch<bf16_tag, BM, BN, NWM, NB, true, false, END>(g, st);
+    if (g.stages_b == 0) {
+        if (g.dtype == CAPSCAPS_BF16) return launch<bf16_tag, BM, BN, NWM, NB, false, true, END>(g, st);
+        return launch<f16_tag, BM, BN, NWM, NB, false, true, END>(g, st);
+    }
+    if (g.dtype == CAPSCAPS_BF16) return launch<bf16_tag, BM, BN, NWM, NB, false, false, END>(g, st);
+    return launch<f16_tag, BM, BN, NWM, NB, false, false, END>(g, st);
 }
 
 template <int BM, int BN, int NWM, int NB>

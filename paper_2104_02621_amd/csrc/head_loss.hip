@@ -166,10 +166,12 @@ __global__ void __launch_bounds__(1024) rows_kernel(Head H, const float* dloss, 
 }
 
 // ---------------------------------------------------------------------------------------- operands
-// Eight values as a product's operand: one 16-byte vector, or three of bf16 terms
+// Eight values of a row as a product's operand: one 16-byte vector, or one in each of three terms (`stages` of a term)
 template <bool TERMS>
-__device__ __forceinline__ void put_operand(unsigned short* to, long long plane, const unsigned short* raw, const float* f)
+__device__ __forceinline__ void put_operand(unsigned short* to, long long row, long long k, long long stages,
+                                            const unsigned short* raw, const float* f)
 {
+    to += head_block_at(row, k, (TERMS ? 3 : 1) * stages);
     if constexpr (!TERMS) {
         chunk_t c;
         __builtin_memcpy(&c, raw, 16);
@@ -190,34 +192,34 @@ __device__ __forceinline__ void put_operand(unsigned short* to, long long plane,
         for (int p = 0; p < 3; ++p) {
             chunk_t c;
             __builtin_memcpy(&c, t[p], 16);
-            *reinterpret_cast<chunk_t*>(to + p * plane) = c;
+            *reinterpret_cast<chunk_t*>(to + p * stages * 512) = c;
         }
     }
 }
 
-// to[i][terms][padded] = from[rows_of[i]][columns], zeros past the columns and, up to `rows`, past *count
+// Rows of `from` (rows_of[i], those that count) as an operand; zeros past the columns and the rows.  A wave writes a block.
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) pack_kernel(const void* from, long long stride, int columns, long long rows,
                                                        const int* rows_of, const int* count, unsigned short* to,
-                                                       int padded, bool vectors)
+                                                       long long stages, bool vectors)
 {
-    const int vecs = padded / 8;
-    const long long kept = count != nullptr ? *count : rows, all = rows * vecs;
-    for (long long t = blockIdx.x * (long long)THREADS + threadIdx.x; t < all; t += (long long)gridDim.x * THREADS) {
-        const long long i = t / vecs;
-        const int c = (int)(t - i * vecs) * 8;
+    const long long kept = count != nullptr ? *count : rows, blocks = (kept + 15) / 16 * stages;
+    const int lane = threadIdx.x & 63;
+    for (long long b = blockIdx.x * 4ll + (threadIdx.x >> 6); b < blocks; b += gridDim.x * 4ll) {
+        const long long rb = b / stages, i = rb * 16 + (lane >> 2);
+        const int c = (int)(b - rb * stages) * HEAD_K + ((lane & 3) ^ (lane >> 4)) * 8;
         unsigned short raw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (i < kept) {
             const long long at = (rows_of != nullptr ? rows_of[i] : i) * stride + c;
             if (vectors && c + 8 <= columns) {
                 if constexpr (TERMS) {
-                    const float4v *p = reinterpret_cast<const float4v*>(static_cast<const float*>(from) + at), a = p[0], b = p[1];
+                    const float4v *p = reinterpret_cast<const float4v*>(static_cast<const float*>(from) + at), u = p[0], v = p[1];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) f[j] = a[j], f[4 + j] = b[j];
+                    for (int j = 0; j < 4; ++j) f[j] = u[j], f[4 + j] = v[j];
                 } else {
-                    const chunk_t a = *reinterpret_cast<const chunk_t*>(static_cast<const unsigned short*>(from) + at);
-                    __builtin_memcpy(raw, &a, 16);
+                    const chunk_t u = *reinterpret_cast<const chunk_t*>(static_cast<const unsigned short*>(from) + at);
+                    __builtin_memcpy(raw, &u, 16);
                 }
             } else {
 #pragma unroll
@@ -230,26 +232,26 @@ __global__ void __launch_bounds__(THREADS) pack_kernel(const void* from, long lo
                     }
             }
         }
-        put_operand<TERMS>(to + i * (TERMS ? 3 : 1) * (long long)padded + c, padded, raw, f);
+        put_operand<TERMS>(to, i, c, stages, raw, f);
     }
 }
 
-// to[c][terms][padded] = from[rows_of[i]][c] with i innermost, zeros past the rows that count; tiles of 64 x 64
+// Columns of `from` as an operand that contracts its rows (rows_of[i], those that count); zeros past them.  Tiles of 64 x 64.
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* from, long long stride, int columns,
                                                                   long long rows, const int* rows_of, const int* count,
-                                                                  unsigned short* to, long long padded)
+                                                                  unsigned short* to, long long stages)
 {
     typedef std::conditional_t<TERMS, float, unsigned short> E;
     __shared__ E tile[64][TERMS ? 65 : 66];
     long long kept = rows;
     if (count != nullptr && *count < kept) kept = *count;
+    const long long used = (kept + HEAD_K - 1) / HEAD_K;  // stages that are read
     const int across = (columns + 63) / 64;
-    const long long tiles = (padded + 63) / 64 * across;
+    const long long tiles = (used + 1) / 2 * across;
     for (long long b = blockIdx.x; b < tiles; b += gridDim.x) {
         const long long i0 = b / across * 64;
         const int c0 = (int)(b % across) * 64;
-        if (i0 >= (kept + HEAD_K - 1) / HEAD_K * HEAD_K) continue;  // (nothing reads it)
         for (int t = threadIdx.x; t < 64 * 64; t += THREADS) {
             const int i = t >> 6, c = t & 63;
             E v = 0;
@@ -261,8 +263,10 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* fr
         }
         __syncthreads();
         for (int t = threadIdx.x; t < 64 * 8; t += THREADS) {
-            const int c = t >> 3, i = (t & 7) * 8;
-            if (c0 + c < columns && i0 + i < padded) {
+            // (a wave: a block)
+            const int block = t >> 6, c = (block >> 1) * 16 + ((t & 63) >> 2);
+            const int i = (block & 1) * HEAD_K + ((t & 3) ^ ((t & 63) >> 4)) * 8;
+            if (c0 + c < (columns + 15) / 16 * 16 && i0 + i < used * HEAD_K) {
                 unsigned short raw[8];
                 float f[8];
 #pragma unroll
@@ -272,7 +276,7 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* fr
                     else
                         raw[j] = tile[i + j][c];
                 }
-                put_operand<TERMS>(to + (c0 + c) * (TERMS ? 3 : 1) * padded + i0 + i, padded, raw, f);
+                put_operand<TERMS>(to, c0 + c, i0 + i, stages, raw, f);
             }
         }
         __syncthreads();
@@ -418,7 +422,7 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
     __shared__ float tile[64][65];
     const float inv = 1.0f / H.tau;
     const long long kept = *H.count;
-    const int across = (padded_classes + 63) / 64, terms = TERMS ? 3 : 1;
+    const int across = (padded_classes + 63) / 64;
     const long long tiles = (padded_rows + 63) / 64 * across;
     for (long long b = blockIdx.x; b < tiles; b += gridDim.x) {
         const long long i0 = b / across * 64;
@@ -449,9 +453,9 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
             }
             if (across_rows) {
                 if (c0 + a < classes && i0 + k < padded_rows)
-                    put_operand<TERMS>(gt + (c0 + a) * terms * padded_rows + i0 + k, padded_rows, raw, f);
+                    put_operand<TERMS>(gt, c0 + a, i0 + k, padded_rows / HEAD_K, raw, f);
             } else if (i0 + a < kept && c0 + k < padded_classes) {
-                put_operand<TERMS>(gn + (i0 + a) * terms * padded_classes + c0 + k, padded_classes, raw, f);
+                put_operand<TERMS>(gn, i0 + a, c0 + k, padded_classes / HEAD_K, raw, f);
             }
         }
         if (sums != nullptr && threadIdx.x < 64 && c0 + threadIdx.x < classes) {
@@ -502,8 +506,8 @@ __global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* l
             }
 #pragma unroll
             for (int p = 0; p < (TERMS ? 3 : 1); ++p) {
-                gn[(i * terms + p) * padded_classes + c] = v[p];
-                gt[(c * terms + p) * padded_rows + i] = v[p];
+                gn[head_block_at(i, c, terms * (padded_classes / HEAD_K)) + p * (padded_classes / HEAD_K) * 512ll] = v[p];
+                gt[head_block_at(c, i, terms * (padded_rows / HEAD_K)) + p * (padded_rows / HEAD_K) * 512] = v[p];
             }
             if (taken != nullptr) {
                 const long long whole = (long long)__builtin_rintf(H.coef[i] * t * 0x1p24f);
@@ -674,8 +678,9 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     W.keep = distill ? L.take<int>(A.rows) : nullptr;
     W.share = distill ? L.take<float>(A.rows * A.top) : nullptr;
     W.entropy = distill ? L.take<float>(A.rows) : nullptr;
-    P.x = L.take<unsigned short>(rows * P.terms * P.padded);
-    P.w = L.take<unsigned short>(most * P.terms * P.padded);
+    const long long stages = (long long)P.terms * P.padded / HEAD_K;
+    P.x = L.take<unsigned short>(head_block_values(rows, stages));
+    P.w = L.take<unsigned short>(head_block_values(most, stages));
     P.logits = P.in_parts ? L.take<float>(rows * P.piece * P.z.splits) : nullptr;
     if (!backward) {
         P.stats = L.take<Stat>(rows * P.stat_parts);
@@ -686,10 +691,11 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     P.dx = pick_tile(rows, A.width, P.piece, P.terms, P.pieces == 1, 0.0);  // (several: added up piece after piece)
     P.dw = pick_tile(most, A.width, rows, P.terms, true, 3.0);
     const long long ld = round_up(A.width, 4);
-    P.xt = L.take<unsigned short>((long long)A.width * P.terms * P.padded_rows);
-    P.wt = L.take<unsigned short>((long long)A.width * P.terms * P.piece);
-    P.gn = L.take<unsigned short>(rows * P.terms * P.piece);
-    P.gt = L.take<unsigned short>(most * P.terms * P.padded_rows);
+    const long long row_stages = P.terms * P.padded_rows / HEAD_K, class_stages = P.terms * round_up(P.piece, HEAD_K) / HEAD_K;
+    P.xt = L.take<unsigned short>(head_block_values(A.width, row_stages));
+    P.wt = L.take<unsigned short>(head_block_values(A.width, class_stages));
+    P.gn = L.take<unsigned short>(head_block_values(rows, class_stages));
+    P.gt = L.take<unsigned short>(head_block_values(most, row_stages));
     P.dx_sums = L.take<float>(rows * ld * P.dx.splits);
     P.dw_sums = P.dw.splits > 1 ? L.take<float>(most * ld * P.dw.splits) : nullptr;
     P.bias_sums = L.take<float>((rows + 63) / 64 * P.piece);
@@ -715,19 +721,21 @@ hipError_t pack(const Plan& P, const void* from, long long stride, int columns, 
 {
     const int* rows_of = kept != nullptr ? kept->rows_of : nullptr;
     const int* count = kept != nullptr ? kept->count : nullptr;
-    const unsigned blocks = blocks_for(rows * (P.padded / 8), THREADS);
+    const long long stages = P.padded / HEAD_K;
+    const unsigned blocks = blocks_for((rows + 15) / 16 * stages, 4);
     const bool vectors = vectors_of(from, stride, dtype);
-    return P.terms == 3 ? run(pack_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, P.padded, vectors)
-                        : run(pack_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, P.padded, vectors);
+    return P.terms == 3 ? run(pack_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors)
+                        : run(pack_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors);
 }
 hipError_t pack_transposed(const Plan& P, const void* from, long long stride, int columns, long long rows, const Head* kept,
                            unsigned short* to, long long padded, hipStream_t st)
 {
     const int* rows_of = kept != nullptr ? kept->rows_of : nullptr;
     const int* count = kept != nullptr ? kept->count : nullptr;
+    const long long stages = padded / HEAD_K;
     const unsigned blocks = blocks_for((padded + 63) / 64 * ((columns + 63) / 64), 1);
-    return P.terms == 3 ? run(pack_transposed_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, padded)
-                        : run(pack_transposed_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, padded);
+    return P.terms == 3 ? run(pack_transposed_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages)
+                        : run(pack_transposed_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages);
 }
 
 const void* weight_at(const Head& H, long long cls)
@@ -747,19 +755,21 @@ int begin(const Head& H, const Plan& P, const float* dloss, long long dloss_stri
 // The product of x and a piece's weights, for launch_head_gemm with an end of the caller's
 int logits_of(const Head& H, const Plan& P, long long first, long long classes, HeadGemm& g, hipStream_t st)
 {
-    const void* w = weight_at(H, first);
-    long long ldw = H.weight_stride * 2;
-    // (read in place: 16 bits, whole vectors, whole stages, rows near enough for 32-bit offsets)
-    if (P.terms != 1 || H.width % HEAD_K != 0 || !vectors_of(H.weight, H.weight_stride, H.dtype) || H.weight_stride > (1 << 21)) {
-        CAPSCAPS_TRY(pack(P, w, H.weight_stride, H.width, classes, nullptr, H.dtype, P.w, st));
-        w = P.w;
-        ldw = (long long)P.terms * P.padded * 2;
-    }
     g = HeadGemm{};
-    g.a = P.x, g.b = w;
-    g.lda = (long long)P.terms * P.padded * 2, g.ldb = ldw;
+    const int stages = P.padded / HEAD_K;
+    g.a = P.x, g.stages_a = (long long)P.terms * stages;
+    // Weights are read in place where they can be (16 bits, whole vectors, whole stages, rows near enough for 32-bit
+    // offsets) and rows are few: the copy in blocks costs 4 bytes a value at 4.5 TB/s and raises the product from 960
+    // to 1250 TFLOP/s, which is as much for 1900 rows.
+    if (P.terms == 1 && H.rows < 2048 && H.width % HEAD_K == 0 && vectors_of(H.weight, H.weight_stride, H.dtype) &&
+        H.weight_stride <= (1 << 21)) {
+        g.b = weight_at(H, first), g.ldb = H.weight_stride * 2;
+    } else {
+        CAPSCAPS_TRY(pack(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, H.dtype, P.w, st));
+        g.b = P.w, g.stages_b = g.stages_a;
+    }
     g.m_rows = H.rows, g.n_rows = classes, g.m_count = H.count, g.k = H.width;
-    g.plane_a = g.plane_b = P.padded * 2;
+    g.plane_a = g.plane_b = stages;
     g.dtype = H.dtype, g.splits = P.z.splits;
     if (P.in_parts) {
         g.out = P.logits, g.ldo = P.piece, g.out_split = H.rows * P.piece, g.out_dtype = CAPSCAPS_FP32;
@@ -819,7 +829,7 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
                              P.z.splits, H.rows * P.piece, first, (int)classes, P.gn, padded, P.gt, P.padded_rows, sums));
         } else {
             z.coef = H.coef, z.lse = G.lse, z.rows_of = H.rows_of;
-            z.gn = P.gn, z.gt = P.gt, z.ldn = padded, z.ldt = P.padded_rows, z.sums = sums;
+            z.gn = P.gn, z.gt = P.gt, z.planes_n = padded / HEAD_K, z.planes_t = (int)(P.padded_rows / HEAD_K), z.sums = sums;
             CAPSCAPS_TRY(launch_head_gemm(z, P.z.tile, HEAD_GRADIENT, st));
         }
         CAPSCAPS_TRY(run(entries_kernel<TERMS>, blocks_for(H.rows, 4), THREADS, st, H, G.loss, G.logq, first, (int)classes, P.gn,
@@ -832,9 +842,9 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
             CAPSCAPS_TRY(pack_transposed(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, P.wt, padded, st));
             HeadGemm g{};
             g.a = P.gn, g.b = P.wt;
-            g.lda = g.ldb = (long long)P.terms * padded * 2;
+            g.plane_a = g.plane_b = padded / HEAD_K;
+            g.stages_a = g.stages_b = P.terms * g.plane_a;
             g.m_rows = H.rows, g.n_rows = H.width, g.m_count = H.count, g.k = classes;
-            g.plane_a = g.plane_b = padded * 2;
             g.dtype = H.dtype, g.out = P.dx_sums, g.ldo = ld, g.out_split = H.rows * ld, g.out_dtype = CAPSCAPS_FP32;
             g.splits = P.dx.splits, g.accumulate = piece > 0;
             CAPSCAPS_TRY(launch_head_gemm(g, P.dx.tile, HEAD_OUT, st));
@@ -843,9 +853,9 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
             char* out = static_cast<char*>(G.dweight) + first * H.width * size;
             HeadGemm g{};
             g.a = P.gt, g.b = P.xt;
-            g.lda = g.ldb = (long long)P.terms * P.padded_rows * 2;
+            g.plane_a = g.plane_b = (int)(P.padded_rows / HEAD_K);
+            g.stages_a = g.stages_b = P.terms * g.plane_a;
             g.m_rows = classes, g.n_rows = H.width, g.k = H.rows, g.k_count = H.count;
-            g.plane_a = g.plane_b = (int)(P.padded_rows * 2);
             g.dtype = H.dtype, g.splits = P.dw.splits;
             const bool direct = P.dw.splits == 1;
             g.out = direct ? out : (void*)P.dw_sums;
