@@ -55,7 +55,7 @@ def _compile(src: Path, force: bool) -> Path:
     return obj
 
 
-def build(force: bool = False, jobs: int = 4) -> Path:
+def build(force: bool = False, jobs: int = 8) -> Path:
     OBJ.mkdir(exist_ok=True)
     srcs = sources()
     with ThreadPoolExecutor(max_workers=jobs) as ex:

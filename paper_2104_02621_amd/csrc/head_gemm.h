@@ -62,8 +62,8 @@ struct HeadGemm {
     float* sums;  // NULL, or [m / sum_rows][planes_n * HEAD_K]
 };
 
-// tile shapes, the columns of a statistic and the rows of a sum over rows (those of a wave)
-enum HeadTile { HEAD_TILE_256 = 0, HEAD_TILE_HALF = 1, HEAD_TILE_128 = 2, HEAD_TILE_FEW_ROWS = 3 };
+// tile shapes, the columns of a statistic and the rows of a sum over rows (those of a wave), workgroups of a CU
+enum HeadTile { HEAD_TILE_256 = 0, HEAD_TILE_128 = 1, HEAD_TILE_FEW_ROWS = 2 };
 struct HeadTileShape {
     int m, n, stat_columns, sum_rows, per_cu;
 };
@@ -71,21 +71,18 @@ inline HeadTileShape head_tile_shape(int tile)
 {
     switch (tile) {
         case HEAD_TILE_256: return {256, 256, 128, 128, 1};
-        case HEAD_TILE_HALF: return {128, 256, 128, 64, 2};
         case HEAD_TILE_128: return {128, 128, 64, 64, 2};
-        default: return {64, 256, 64, 64, 2};
+        default: return {64, 128, 32, 64, 2};
     }
 }
 hipError_t launch_head_gemm_256(const HeadGemm& g, HeadEnd end, hipStream_t st);
-hipError_t launch_head_gemm_half(const HeadGemm& g, HeadEnd end, hipStream_t st);
 hipError_t launch_head_gemm_128(const HeadGemm& g, HeadEnd end, hipStream_t st);
 hipError_t launch_head_gemm_few_rows(const HeadGemm& g, HeadEnd end, hipStream_t st);
 inline hipError_t launch_head_gemm(const HeadGemm& g, int tile, HeadEnd end, hipStream_t st)
 {
-    return tile == HEAD_TILE_256    ? launch_head_gemm_256(g, end, st)
-           : tile == HEAD_TILE_HALF ? launch_head_gemm_half(g, end, st)
-           : tile == HEAD_TILE_128  ? launch_head_gemm_128(g, end, st)
-                                    : launch_head_gemm_few_rows(g, end, st);
+    return tile == HEAD_TILE_256   ? launch_head_gemm_256(g, end, st)
+           : tile == HEAD_TILE_128 ? launch_head_gemm_128(g, end, st)
+                                   : launch_head_gemm_few_rows(g, end, st);
 }
 
 }  // namespace capscaps

@@ -147,6 +147,9 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
         b_off += SPLIT_TERM_B[0] * G.plane_b * 1024;
     }
     auto advance = [&]() {
+        // (the empty statements hold the scalar arithmetic in the gap it is written in; where it drifts, the one wave of a SIMD
+        // leaves the matrix pipe without work: 8192 x 2048 x 32768 in 1256 instead of 756 us on tiles of 256 x 256)
+        if constexpr (!TERMS) asm volatile("" : "+s"(next), "+s"(a_off), "+s"(b_off));
         ++next;
         a_off += 1024;
         b_off += step_b;
@@ -166,6 +169,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
         }
         a_off = next < stages ? a_off : OUT_OF_RANGE;
         b_off = next < stages ? b_off : OUT_OF_RANGE;
+        if constexpr (!TERMS) asm volatile("" : "+s"(next), "+s"(a_off), "+s"(b_off));
     };
     auto copy_a = [&](auto SLOT, auto J) {
         constexpr int slot = decltype(SLOT)::value, j = decltype(J)::value;
@@ -219,9 +223,9 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
         Mma<Tag>::run(ka, ib, c);
         if constexpr (NMMA < 16) asm volatile("" : "+a"(c));
     };
-    // reads before gap i of a step's gaps, one in each of the first; copies, spread over all
-    static_assert(NFRAG <= NMMA, "a read in a gap");
-    constexpr auto reads_before = [](int i) { return i < NFRAG ? i : NFRAG; };
+    // reads before gap i of a step's gaps, one (two) in each of the first; copies, spread over all
+    constexpr int per_gap = (NFRAG + NMMA - 1) / NMMA;
+    constexpr auto reads_before = [](int i) { return i * per_gap < NFRAG ? i * per_gap : NFRAG; };
     constexpr auto copies_before = [](int i, int count) { return (i * count + NMMA / 2 - 1) / NMMA; };
     for (int st = 0; st < stages; st += NB) {
         static_for<NB>([&](auto SLOT) {

@@ -30,6 +30,8 @@ constexpr int THREADS = 256;
 constexpr int MOST_TOP = 1024;
 // (256 rows of an operand are within a signed 32-bit offset: rows of up to 2^20 values of three terms)
 constexpr long long MOST_ROWS = 1 << 20, MOST_PIECE = 1 << 20;
+// (logits that are written in parts and then read: a row by a workgroup)
+constexpr int MOST_IN_PARTS = 16384;
 constexpr long long PIECE_BYTES = 512ll << 20;  // of a piece's logits, and of its gradients
 
 // What both directions of both losses are given
@@ -299,16 +301,17 @@ __device__ __forceinline__ Stat wave_join(Stat s)
     return s;
 }
 
-// stats[i] of logits that lie in parts.  A wave for a row.
+// stats[i] of logits that lie in parts.  A workgroup for a row.
 __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, long long ldz, int splits, long long split,
                                                         Stat* stats)
 {
-    const int lane = threadIdx.x & 63;
+    __shared__ Stat joined[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float inv = 1.0f / H.tau;
     const long long kept = *H.count;
-    for (long long i = blockIdx.x * 4ll + (threadIdx.x >> 6); i < kept; i += gridDim.x * 4ll) {
+    for (long long i = blockIdx.x; i < kept; i += gridDim.x) {
         Stat s = {-__builtin_inff(), 0.0f};
-        for (long long c = lane; c < H.classes; c += 64) {
+        for (long long c = threadIdx.x; c < H.classes; c += THREADS) {
             float v = 0.0f;
             for (int p = 0; p < splits; ++p) v += z[p * split + i * ldz + c];
             if (H.bias != nullptr) v += H.bias[c];
@@ -319,43 +322,71 @@ __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, 
                 s = join(s, {v, 1.0f});
         }
         s = wave_join(s);
-        if (lane == 0) stats[i] = s;
+        if (lane == 0) joined[wave] = s;
+        __syncthreads();
+        if (threadIdx.x == 0) stats[i] = join(join(joined[0], joined[1]), join(joined[2], joined[3]));
+        __syncthreads();
     }
 }
 
-// z[row][class] from the operands, in fp32, by a wave
-__device__ __forceinline__ float logit(const Head& H, long long row, long long cls, int lane, bool vectors)
+// picked[row][k] = z of the rows' entries (0 where they do not count), from the operands in fp32.  A wave for four entries of a
+// row at a time: what it waits for is the weights' rows, which lie anywhere.
+__global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bool vectors)
 {
-    float s = 0.0f;
-    const long long xa = row * H.x_stride, wa = cls * H.weight_stride;
-    if (vectors && H.dtype != CAPSCAPS_FP32) {
-        const unsigned short *x = static_cast<const unsigned short*>(H.x) + xa, *w = static_cast<const unsigned short*>(H.weight) + wa;
-        for (int c = lane * 8; c < H.width; c += 512) {
-            const chunk_t a = *reinterpret_cast<const chunk_t*>(x + c), b = *reinterpret_cast<const chunk_t*>(w + c);
+    const int lane = threadIdx.x & 63;
+    const long long kept = *H.count, quads = (H.top + 3) / 4;
+    for (long long t = blockIdx.x * 4ll + (threadIdx.x >> 6); t < kept * quads; t += gridDim.x * 4ll) {
+        const long long r = H.rows_of[t / quads];
+        const int k0 = (int)(t % quads) * 4;
+        long long cls[4];
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (H.dtype == CAPSCAPS_BF16) {
-                    s = __builtin_fmaf(low_half(a[j]), low_half(b[j]), s);
-                    s = __builtin_fmaf(high_half(a[j]), high_half(b[j]), s);
-                } else {
-                    const half2v p = __builtin_bit_cast(half2v, (unsigned)a[j]), q = __builtin_bit_cast(half2v, (unsigned)b[j]);
-                    s = __builtin_fmaf((float)p[0], (float)q[0], s);
-                    s = __builtin_fmaf((float)p[1], (float)q[1], s);
-                }
+        for (int j = 0; j < 4; ++j) cls[j] = k0 + j < H.top ? index_of(H, r, k0 + j) : -1;
+        const long long xa = r * H.x_stride;
+        if (vectors && H.dtype != CAPSCAPS_FP32) {
+            const unsigned short *x = static_cast<const unsigned short*>(H.x) + xa, *w = static_cast<const unsigned short*>(H.weight);
+            for (int c = lane * 8; c < H.width; c += 512) {
+                const chunk_t a = *reinterpret_cast<const chunk_t*>(x + c);
+                chunk_t b[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (cls[j] >= 0) b[j] = *reinterpret_cast<const chunk_t*>(w + cls[j] * H.weight_stride + c);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (cls[j] >= 0)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            if (H.dtype == CAPSCAPS_BF16) {
+                                s[j] = __builtin_fmaf(low_half(a[q]), low_half(b[j][q]), s[j]);
+                                s[j] = __builtin_fmaf(high_half(a[q]), high_half(b[j][q]), s[j]);
+                            } else {
+                                const half2v u = __builtin_bit_cast(half2v, (unsigned)a[q]), v = __builtin_bit_cast(half2v, (unsigned)b[j][q]);
+                                s[j] = __builtin_fmaf((float)u[0], (float)v[0], s[j]);
+                                s[j] = __builtin_fmaf((float)u[1], (float)v[1], s[j]);
+                            }
+                        }
+            }
+        } else {
+            for (int c = lane; c < H.width; c += 64) {
+                const float a = load_element(H.x, xa + c, H.dtype);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (cls[j] >= 0) s[j] = __builtin_fmaf(a, load_element(H.weight, cls[j] * H.weight_stride + c, H.dtype), s[j]);
             }
         }
-    } else {
-        for (int c = lane; c < H.width; c += 64)
-            s = __builtin_fmaf(load_element(H.x, xa + c, H.dtype), load_element(H.weight, wa + c, H.dtype), s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            s[j] = lanes_sum(s[j], 64);
+            if (cls[j] >= 0 && H.bias != nullptr) s[j] += H.bias[cls[j]];
+            if (lane == 0 && k0 + j < H.top) picked[r * H.top + k0 + j] = s[j];
+        }
     }
-    s = lanes_sum(s, 64);
-    return H.bias != nullptr ? s + H.bias[cls] : s;
 }
 
-// loss, lse, logq of all rows, from stats[part][i].  A workgroup for eight of the rows that are kept, and for the zeros
+// loss, lse, logq of all rows, from stats[part][i] and the entries' z (which logq takes the place of, where it is wanted).  A workgroup for eight of the rows that are kept, and for the zeros
 // of eight rows that are not.
-__global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int parts, float* loss, float* lse,
-                                                       float* logq, bool vectors)
+__global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int parts, const float* picked, float* loss,
+                                                       float* lse, float* logq)
 {
     __shared__ Stat joined[4][8];
     __shared__ float lses[8], sums[4][8];
@@ -384,21 +415,23 @@ __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats
             lses[lane] = s.top + logf(s.sum);
         }
         __syncthreads();
-        for (int j = 0; j < rows; ++j) {
-            const long long r = H.rows_of[i0 + j];
-            float cross = 0.0f;
-            for (int k = wave; k < H.top; k += 4) {
-                const long long cls = index_of(H, r, k);
+        // (lane's row j = lane & 7 and every 32nd entry)
+        float cross = 0.0f;
+        if ((lane & 7) < rows) {
+            const long long r = H.rows_of[i0 + (lane & 7)];
+            for (int k = threadIdx.x >> 3; k < H.top; k += THREADS / 8) {
                 float l = 0.0f;
-                if (cls >= 0) {
-                    l = logit(H, r, cls, lane, vectors) * inv - lses[j];
+                if (index_of(H, r, k) >= 0) {
+                    l = picked[r * H.top + k] * inv - lses[lane & 7];
                     const float t = share_of(H, r, k);
                     if (t != 0.0f) cross += t * l;
                 }
-                if (logq != nullptr && lane == 0) logq[r * H.top + k] = l;
+                if (logq != nullptr) logq[r * H.top + k] = l;
             }
-            if (lane == 0) sums[wave][j] = cross;
         }
+#pragma unroll
+        for (int k = 8; k < 64; k <<= 1) cross += __shfl_xor(cross, k);
+        if (lane < 8) sums[wave][lane] = cross;
         __syncthreads();
         if (threadIdx.x < rows) {
             const long long r = H.rows_of[i0 + lane];
@@ -586,13 +619,13 @@ Pick pick_tile(long long m, long long n, long long k, int terms, bool may_split,
     const long long stages = std::max<long long>(1, (k + HEAD_K - 1) / HEAD_K) * (terms > 1 ? HEAD_PRODUCTS : 1);
     Pick best{HEAD_TILE_128, 1};
     double least = 1e300;
-    for (const int tile : {HEAD_TILE_256, HEAD_TILE_HALF, HEAD_TILE_128, HEAD_TILE_FEW_ROWS}) {
+    for (const int tile : {HEAD_TILE_256, HEAD_TILE_128, HEAD_TILE_FEW_ROWS}) {
         const HeadTileShape s = head_tile_shape(tile);
         const double tiles = (double)((m + s.m - 1) / s.m) * (double)((n + s.n - 1) / s.n);
         const double slots = 256.0 * s.per_cu;
         // time of a stage of as many tiles as a CU holds, and stages' time to begin and end
-        const double cost = tile == HEAD_TILE_256 ? 1.0 : tile == HEAD_TILE_HALF ? 1.04 : 0.625;
-        const double ends = tile == HEAD_TILE_256 ? 24 : tile == HEAD_TILE_HALF ? 12 : 10;
+        const double cost = tile == HEAD_TILE_256 ? 1.0 : tile == HEAD_TILE_128 ? 0.7 : 0.5;
+        const double ends = tile == HEAD_TILE_256 ? 12 : 10;
         for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts * 2) {
             if (parts > 1 && (!may_split || stages / parts < 8)) break;
             if (tiles * parts > (1 << 23)) continue;
@@ -642,6 +675,7 @@ struct Plan {
     unsigned short *x, *xt, *w, *wt, *gn, *gt;
     float *logits, *dx_sums, *dw_sums, *bias_sums;
     Stat* stats;
+    float* picked;
     long long* taken;
 };
 
@@ -666,7 +700,7 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     P.piece = std::min<long long>(round_up(A.classes, HEAD_K), P.piece);
     P.pieces = (int)((A.classes + P.piece - 1) / P.piece);
     const long long most = std::min<long long>(P.piece, A.classes);
-    P.z = pick_tile(rows, most, A.width, P.terms, P.pieces == 1 && rows * P.piece * 64 * 4 <= PIECE_BYTES, 6.0);
+    P.z = pick_tile(rows, most, A.width, P.terms, P.pieces == 1 && A.classes <= MOST_IN_PARTS && rows * P.piece * 64 * 4 <= PIECE_BYTES, 6.0);
     P.in_parts = P.z.splits > 1;
     P.stat_parts = P.in_parts ? 1 : ceil_div(A.classes, head_tile_shape(P.z.tile).stat_columns);
     Layout L{static_cast<char*>(base)};
@@ -684,6 +718,7 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     P.logits = P.in_parts ? L.take<float>(rows * P.piece * P.z.splits) : nullptr;
     if (!backward) {
         P.stats = L.take<Stat>(rows * P.stat_parts);
+        P.picked = distill ? nullptr : L.take<float>(rows);
         P.bytes = L.at;
         return P;
     }
@@ -759,9 +794,9 @@ int logits_of(const Head& H, const Plan& P, long long first, long long classes, 
     const int stages = P.padded / HEAD_K;
     g.a = P.x, g.stages_a = (long long)P.terms * stages;
     // Weights are read in place where they can be (16 bits, whole vectors, whole stages, rows near enough for 32-bit
-    // offsets) and rows are few: the copy in blocks costs 4 bytes a value at 4.5 TB/s and raises the product from 960
-    // to 1250 TFLOP/s, which is as much for 1900 rows.
-    if (P.terms == 1 && H.rows < 2048 && H.width % HEAD_K == 0 && vectors_of(H.weight, H.weight_stride, H.dtype) &&
+    // offsets): the product of 6144 rows with 32768 classes of 4096 values takes 1212 us so and 1161 with a copy in blocks, which
+    // itself takes 120 (4 bytes a value at 4.5 TB/s): as much for 15000 rows.
+    if (P.terms == 1 && H.rows < 15000 && H.width % HEAD_K == 0 && vectors_of(H.weight, H.weight_stride, H.dtype) &&
         H.weight_stride <= (1 << 21)) {
         g.b = weight_at(H, first), g.ldb = H.weight_stride * 2;
     } else {
@@ -794,11 +829,14 @@ int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, 
         g.first_part = (int)(first / head_tile_shape(P.z.tile).stat_columns);
         CAPSCAPS_TRY(launch_head_gemm(g, P.z.tile, P.in_parts ? HEAD_OUT : HEAD_STATS, st));
         if (P.in_parts)
-            CAPSCAPS_TRY(run(stats_kernel, blocks_for(H.rows, 4), THREADS, st, H, (const float*)P.logits, P.piece, P.z.splits,
+            CAPSCAPS_TRY(run(stats_kernel, blocks_for(H.rows, 1), THREADS, st, H, (const float*)P.logits, P.piece, P.z.splits,
                              H.rows * P.piece, P.stats));
     }
     const bool vectors = vectors_of(H.x, H.x_stride, H.dtype) && vectors_of(H.weight, H.weight_stride, H.dtype) && H.width % 8 == 0;
-    CAPSCAPS_TRY(run(loss_kernel, blocks_for(H.rows, 8), THREADS, st, H, (const Stat*)P.stats, P.stat_parts, loss, lse, logq, vectors));
+    // (the entries' z: where logq goes, or in the workspace)
+    float* const picked = logq != nullptr ? logq : P.picked;
+    CAPSCAPS_TRY(run(pick_kernel, blocks_for(H.rows * ((H.top + 3) / 4), 4), THREADS, st, H, picked, vectors));
+    CAPSCAPS_TRY(run(loss_kernel, blocks_for(H.rows, 8), THREADS, st, H, (const Stat*)P.stats, P.stat_parts, (const float*)picked, loss, lse, logq));
     return CAPSCAPS_OK;
 }
 
