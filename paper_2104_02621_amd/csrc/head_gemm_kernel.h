@@ -63,7 +63,7 @@ __device__ __forceinline__ void turn(unsigned& lo, unsigned& hi, int lane)
 
 // NB: stages of the ring
 template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, bool ROWS, int END>
-__global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kernel(const HeadGemm G, int tiles_m, int tiles_n)
+__global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kernel(const HeadGemm G, int tiles_n)
 {
     constexpr int NWN = 4 / NWM, WM = BM / NWM, WN = BN / NWN, TM = WM / 32, TN = WN / 32;
     constexpr int A_BYTES = BM * 64, STAGE = (BM + BN) * 64;
@@ -76,24 +76,21 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
 
     // Tiles: an XCD (workgroups go to the eight in turn) takes a run of them, bands of eight rows of tiles, so that the 32
     // tiles its CUs work on at a time share operands in its L2.
-    const int tiles = tiles_m * tiles_n;
-    int part, L;
-    {
-        const int all = gridDim.x, span = all & ~7;
-        const int id = (int)blockIdx.x < span ? ((int)blockIdx.x & 7) * (span >> 3) + ((int)blockIdx.x >> 3) : blockIdx.x;
-        part = id / tiles;
-        L = id - part * tiles;
-    }
-    const int band = L / (8 * tiles_n), in_band = L - band * 8 * tiles_n;
-    const int high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
-    const long long m0 = (long long)(band * 8 + in_band % high) * BM;
-    const long long n0 = (long long)(in_band / high) * BN;
     long long m_end = G.m_rows;
     if (G.m_count != nullptr) {
         const long long c = __builtin_amdgcn_readfirstlane(*G.m_count);
         m_end = c < m_end ? c : m_end;
     }
-    if (m0 >= m_end) return;
+    // (of the rows that count: the others' workgroups end here, and leave no XCD without work)
+    const int tiles_m = (int)((m_end + BM - 1) / BM), tiles = tiles_m * tiles_n, all = tiles * G.splits;
+    if ((int)blockIdx.x >= all) return;
+    const int span = all & ~7;
+    const int id = (int)blockIdx.x < span ? ((int)blockIdx.x & 7) * (span >> 3) + ((int)blockIdx.x >> 3) : blockIdx.x;
+    const int part = id / tiles, L = id - part * tiles;
+    const int band = L / (8 * tiles_n), in_band = L - band * 8 * tiles_n;
+    const int high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+    const long long m0 = (long long)(band * 8 + in_band % high) * BM;
+    const long long n0 = (long long)(in_band / high) * BN;
     // stages of this part
     long long k = G.k;
     if (G.k_count != nullptr) {
@@ -313,26 +310,27 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
         });
         return;
     }
-    // (z + bias) of the lane's values, in place
-    static_for<TN * 4>([&](auto Q) {
-        constexpr int a = decltype(Q)::value / 4, g = decltype(Q)::value % 4;
-        float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (G.bias != nullptr)
+    // z + bias of the lane's values, in place
+    if (TERMS || G.bias != nullptr)
+        static_for<TN * 4>([&](auto Q) {
+            constexpr int a = decltype(Q)::value / 4, g = decltype(Q)::value % 4;
+            float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (G.bias != nullptr)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int n = a * 32 + 8 * g + 4 * h + j;
-                if (n < n_left) bias[j] = G.bias[n0 + wn * WN + n];
-            }
-        static_for<TM>([&](auto B) {
-            constexpr int b = decltype(B)::value;
+                for (int j = 0; j < 4; ++j) {
+                    const int n = a * 32 + 8 * g + 4 * h + j;
+                    if (n < n_left) bias[j] = G.bias[n0 + wn * WN + n];
+                }
+            static_for<TM>([&](auto B) {
+                constexpr int b = decltype(B)::value;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float z = acc[a][b][4 * g + j];
-                acc[a][b][4 * g + j] = (TERMS ? z * SPLIT_UNSCALE : z) + bias[j];
-            }
+                for (int j = 0; j < 4; ++j) {
+                    const float z = acc[a][b][4 * g + j];
+                    acc[a][b][4 * g + j] = (TERMS ? z * SPLIT_UNSCALE : z) + bias[j];
+                }
+            });
+            __builtin_amdgcn_sched_barrier(0);
         });
-        __builtin_amdgcn_sched_barrier(0);
-    });
     if (n_left < WN)  // (columns past the last class count nothing)
         static_for<TN * 16>([&](auto Q) {
             constexpr int a = decltype(Q)::value / 16, r = decltype(Q)::value % 16;
@@ -343,22 +341,28 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
         });
     if constexpr (END == HEAD_STATS) {
         const long long first = (G.first_part + (n0 + wn * WN) / WN) * G.m_rows;
-        const float minus = -__builtin_inff();
+        const float minus = -__builtin_inff(), inv_log2 = G.inv_tau * 1.44269504f;
         static_for<TM>([&](auto B) {
             constexpr int b = decltype(B)::value;
-            float top = minus, sum = 0.0f;
+            // (four chains: one wave on a SIMD waits for what it needs next.  v_max3_f32 by name: the compiler would make sure
+            // of quiet NaN first, which v_exp_f32 does)
+            float tops[4] = {minus, minus, minus, minus}, sums[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int a = 0; a < TN; ++a)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, acc[a][b][r]);
+                for (int r = 0; r < 16; r += 2)
+                    asm("v_max3_f32 %0, %1, %2, %0" : "+v"(tops[r / 2 & 3]) : "v"(acc[a][b][r]), "v"(acc[a][b][r + 1]));
+            float top = __builtin_fmaxf(__builtin_fmaxf(tops[0], tops[1]), __builtin_fmaxf(tops[2], tops[3]));
             top = __builtin_fmaxf(top, __shfl_xor(top, 32));
             // (nothing but -infinity: every difference would be NaN)
             const float about = top == minus ? 0.0f : top;
             static_for<TN>([&](auto A) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum += __expf((acc[decltype(A)::value][b][r] - about) * G.inv_tau);
+                for (int r = 0; r < 16; ++r)
+                    sums[r & 3] += __builtin_amdgcn_exp2f((acc[decltype(A)::value][b][r] - about) * inv_log2);
                 __builtin_amdgcn_sched_barrier(0);
             });
+            float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
             sum += __shfl_xor(sum, 32);
             const long long m = m0 + wm * WM + b * 32 + lr;
             if (h == 0 && m < m_end && n_left > 0) G.stats[first + m] = {top * G.inv_tau, sum};
@@ -379,6 +383,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
             const long long m = m0 + wm * WM + b * 32 + lr;
             const bool row = m < m_end;
             const float lse = row ? G.lse[G.rows_of[m]] : 0.0f, coef = row ? G.coef[m] : 0.0f;
+            const float inv_log2 = G.inv_tau * 1.44269504f, lse_log2 = lse * -1.44269504f;
             // row m at the wave's first class, without its chunk; stage of these 32 rows in gt
             unsigned short* const gn = G.gn + ((m >> 4) * sn + ((n0 + wn * WN) >> 5)) * 512 + (m & 15) * 32;
             const long long stage_t = (m0 + wm * WM + b * 32) >> 5;
@@ -387,8 +392,9 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
                 float v[16];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const float l = __builtin_fmaf(acc[a][b][r], G.inv_tau, -lse);
-                    v[r] = coef * (TERMS ? expf(l) : __expf(l));
+                    // (16 bits: the logarithm's base taken into both factors, an error of 2^-24 |lse| and |z|)
+                    v[r] = coef * (TERMS ? expf(__builtin_fmaf(acc[a][b][r], G.inv_tau, -lse))
+                                         : __builtin_amdgcn_exp2f(__builtin_fmaf(acc[a][b][r], inv_log2, lse_log2)));
                     if (G.sums != nullptr) sums[a * 16 + r] += row ? v[r] : 0.0f;
                     if constexpr (TERMS) v[r] *= SPLIT_SCALE;
                 }
@@ -452,7 +458,7 @@ hipError_t launch(const HeadGemm& g, hipStream_t st)
     static std::atomic<unsigned long long> done{0};
     const hipError_t err = set_dynamic_lds_once(reinterpret_cast<const void*>(kernel), lds, done);
     if (err != hipSuccess) return err;
-    kernel<<<dim3((unsigned)(tm * tn * g.splits)), dim3(256), lds, st>>>(g, (int)tm, (int)tn);
+    kernel<<<dim3((unsigned)(tm * tn * g.splits)), dim3(256), lds, st>>>(g, (int)tn);
     return hipGetLastError();
 }
 

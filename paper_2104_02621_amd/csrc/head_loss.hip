@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(THREADS) pack_kernel(const void* from, long lo
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* from, long long stride, int columns,
                                                                   long long rows, const int* rows_of, const int* count,
-                                                                  unsigned short* to, long long stages)
+                                                                  unsigned short* to, long long stages, bool vectors)
 {
     typedef std::conditional_t<TERMS, float, unsigned short> E;
     __shared__ E tile[64][TERMS ? 65 : 66];
@@ -254,14 +254,32 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* fr
     for (long long b = blockIdx.x; b < tiles; b += gridDim.x) {
         const long long i0 = b / across * 64;
         const int c0 = (int)(b % across) * 64;
-        for (int t = threadIdx.x; t < 64 * 64; t += THREADS) {
-            const int i = t >> 6, c = t & 63;
-            E v = 0;
-            if (i0 + i < kept && c0 + c < columns) {
-                const long long row = rows_of != nullptr ? rows_of[i0 + i] : i0 + i;
-                v = static_cast<const E*>(from)[row * stride + c0 + c];
+        constexpr int PER = 16 / sizeof(E), ROW = 64 / PER;  // values of a vector, vectors of a tile's row
+        if (vectors && c0 + 64 <= columns) {
+#pragma unroll
+            for (int u = 0; u < 64 * ROW / THREADS; ++u) {
+                const int t = u * THREADS + threadIdx.x, i = t / ROW, c = t % ROW * PER;
+                chunk_t v = {0, 0, 0, 0};
+                if (i0 + i < kept) {
+                    const long long row = rows_of != nullptr ? rows_of[i0 + i] : i0 + i;
+                    v = *reinterpret_cast<const chunk_t*>(static_cast<const E*>(from) + row * stride + c0 + c);
+                }
+                E e[PER];
+                __builtin_memcpy(e, &v, 16);
+#pragma unroll
+                for (int j = 0; j < PER; ++j) tile[i][c + j] = e[j];
             }
-            tile[i][c] = v;
+        } else {
+#pragma unroll 8
+            for (int u = 0; u < 16; ++u) {
+                const int t = u * THREADS + threadIdx.x, i = t >> 6, c = t & 63;
+                E v = 0;
+                if (i0 + i < kept && c0 + c < columns) {
+                    const long long row = rows_of != nullptr ? rows_of[i0 + i] : i0 + i;
+                    v = static_cast<const E*>(from)[row * stride + c0 + c];
+                }
+                tile[i][c] = v;
+            }
         }
         __syncthreads();
         for (int t = threadIdx.x; t < 64 * 8; t += THREADS) {
@@ -345,6 +363,7 @@ __global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bo
         const long long xa = r * H.x_stride;
         if (vectors && H.dtype != CAPSCAPS_FP32) {
             const unsigned short *x = static_cast<const unsigned short*>(H.x) + xa, *w = static_cast<const unsigned short*>(H.weight);
+#pragma unroll 2
             for (int c = lane * 8; c < H.width; c += 512) {
                 const chunk_t a = *reinterpret_cast<const chunk_t*>(x + c);
                 chunk_t b[4];
@@ -383,18 +402,20 @@ __global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bo
     }
 }
 
-// loss, lse, logq of all rows, from stats[part][i] and the entries' z (which logq takes the place of, where it is wanted).  A workgroup for eight of the rows that are kept, and for the zeros
-// of eight rows that are not.
+// loss, lse, logq of all rows, from stats[part][i] and the entries' z (which logq takes the place of, where it is wanted).
+// A workgroup for ROWS of the rows that are kept, and for the zeros of as many that are not (eight: whole 64-byte pieces of a
+// part's statistics; one where rows are few).
+template <int ROWS>
 __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int parts, const float* picked, float* loss,
                                                        float* lse, float* logq)
 {
-    __shared__ Stat joined[4][8];
-    __shared__ float lses[8], sums[4][8];
+    __shared__ Stat joined[4][ROWS];
+    __shared__ float lses[ROWS], sums[4][ROWS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float inv = 1.0f / H.tau;
     const int kept = *H.count;
-    for (long long i0 = blockIdx.x * 8ll; i0 < H.rows; i0 += gridDim.x * 8ll) {
-        for (int t = threadIdx.x; t < 8 * H.top; t += THREADS) {
+    for (long long i0 = blockIdx.x * (long long)ROWS; i0 < H.rows; i0 += gridDim.x * (long long)ROWS) {
+        for (int t = threadIdx.x; t < ROWS * H.top; t += THREADS) {
             const long long r = i0 + t / H.top;
             if (r < H.rows && H.pos[r] < 0) {
                 if (t % H.top == 0) loss[r] = 0.0f, lse[r] = 0.0f;
@@ -402,27 +423,27 @@ __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats
             }
         }
         if (i0 >= kept) continue;
-        const int rows = kept - i0 < 8 ? (int)(kept - i0) : 8;
+        const int rows = kept - i0 < ROWS ? (int)(kept - i0) : ROWS;
         Stat s = {-__builtin_inff(), 0.0f};
-        if ((lane & 7) < rows)
-            for (int p = threadIdx.x >> 3; p < parts; p += THREADS / 8) s = join(s, stats[p * H.rows + i0 + (lane & 7)]);
+        if ((lane & (ROWS - 1)) < rows)
+            for (int p = threadIdx.x / ROWS; p < parts; p += THREADS / ROWS) s = join(s, stats[p * H.rows + i0 + (lane & (ROWS - 1))]);
 #pragma unroll
-        for (int k = 8; k < 64; k <<= 1) s = join(s, {__shfl_xor(s.top, k), __shfl_xor(s.sum, k)});
-        if (lane < 8) joined[wave][lane] = s;
+        for (int k = ROWS; k < 64; k <<= 1) s = join(s, {__shfl_xor(s.top, k), __shfl_xor(s.sum, k)});
+        if (lane < ROWS) joined[wave][lane] = s;
         __syncthreads();
-        if (threadIdx.x < 8) {
+        if (threadIdx.x < ROWS) {
             s = join(join(joined[0][lane], joined[1][lane]), join(joined[2][lane], joined[3][lane]));
             lses[lane] = s.top + logf(s.sum);
         }
         __syncthreads();
-        // (lane's row j = lane & 7 and every 32nd entry)
+        // (lane's row and every 256 / ROWS-th entry)
         float cross = 0.0f;
-        if ((lane & 7) < rows) {
-            const long long r = H.rows_of[i0 + (lane & 7)];
-            for (int k = threadIdx.x >> 3; k < H.top; k += THREADS / 8) {
+        if ((lane & (ROWS - 1)) < rows) {
+            const long long r = H.rows_of[i0 + (lane & (ROWS - 1))];
+            for (int k = threadIdx.x / ROWS; k < H.top; k += THREADS / ROWS) {
                 float l = 0.0f;
                 if (index_of(H, r, k) >= 0) {
-                    l = picked[r * H.top + k] * inv - lses[lane & 7];
+                    l = picked[r * H.top + k] * inv - lses[lane & (ROWS - 1)];
                     const float t = share_of(H, r, k);
                     if (t != 0.0f) cross += t * l;
                 }
@@ -430,8 +451,8 @@ __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats
             }
         }
 #pragma unroll
-        for (int k = 8; k < 64; k <<= 1) cross += __shfl_xor(cross, k);
-        if (lane < 8) sums[wave][lane] = cross;
+        for (int k = ROWS; k < 64; k <<= 1) cross += __shfl_xor(cross, k);
+        if (lane < ROWS) sums[wave][lane] = cross;
         __syncthreads();
         if (threadIdx.x < rows) {
             const long long r = H.rows_of[i0 + lane];
@@ -461,17 +482,25 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
         const long long i0 = b / across * 64;
         const int c0 = (int)(b % across) * 64;
         if (i0 >= (kept + HEAD_K - 1) / HEAD_K * HEAD_K) continue;
-        for (int t = threadIdx.x; t < 64 * 64; t += THREADS) {
-            const int i = t >> 6, c = c0 + (t & 63);
-            float g = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {  // (four columns a thread, of four rows)
+            const int i = u * 16 + (threadIdx.x >> 4), c = c0 + (threadIdx.x & 15) * 4;
+            float4v g = {0.0f, 0.0f, 0.0f, 0.0f};
             if (i0 + i < kept && c < classes) {
-                float v = 0.0f;
-                for (int p = 0; p < splits; ++p) v += z[p * split + (i0 + i) * ldz + c];
-                if (H.bias != nullptr) v += H.bias[first + c];
-                const float l = __builtin_fmaf(v, inv, -lse[H.rows_of[i0 + i]]);
-                g = H.coef[i0 + i] * (TERMS ? expf(l) : __expf(l));
+                float4v v = g;
+                const float* from = z + (i0 + i) * ldz + c;  // (rows are a multiple of 32 long)
+#pragma unroll 4
+                for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const float4v*>(from + p * split);
+                const float all = lse[H.rows_of[i0 + i]], coef = H.coef[i0 + i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (H.bias != nullptr && c + j < classes) v[j] += H.bias[first + c + j];
+                    const float l = __builtin_fmaf(v[j], inv, -all);
+                    g[j] = c + j < classes ? coef * (TERMS ? expf(l) : __expf(l)) : 0.0f;
+                }
             }
-            tile[i][t & 63] = g;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) tile[i][(threadIdx.x & 15) * 4 + j] = g[j];
         }
         __syncthreads();
         for (int t = threadIdx.x; t < 2 * 64 * 8; t += THREADS) {
@@ -769,8 +798,9 @@ hipError_t pack_transposed(const Plan& P, const void* from, long long stride, in
     const int* count = kept != nullptr ? kept->count : nullptr;
     const long long stages = padded / HEAD_K;
     const unsigned blocks = blocks_for((padded + 63) / 64 * ((columns + 63) / 64), 1);
-    return P.terms == 3 ? run(pack_transposed_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages)
-                        : run(pack_transposed_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages);
+    const bool vectors = vectors_of(from, stride, P.terms == 3 ? CAPSCAPS_FP32 : CAPSCAPS_BF16);
+    return P.terms == 3 ? run(pack_transposed_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors)
+                        : run(pack_transposed_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors);
 }
 
 const void* weight_at(const Head& H, long long cls)
@@ -836,7 +866,9 @@ int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, 
     // (the entries' z: where logq goes, or in the workspace)
     float* const picked = logq != nullptr ? logq : P.picked;
     CAPSCAPS_TRY(run(pick_kernel, blocks_for(H.rows * ((H.top + 3) / 4), 4), THREADS, st, H, picked, vectors));
-    CAPSCAPS_TRY(run(loss_kernel, blocks_for(H.rows, 8), THREADS, st, H, (const Stat*)P.stats, P.stat_parts, (const float*)picked, loss, lse, logq));
+    const bool few = H.rows < 512;
+    CAPSCAPS_TRY(run(few ? loss_kernel<1> : loss_kernel<8>, blocks_for(H.rows, few ? 1 : 8), THREADS, st, H, (const Stat*)P.stats,
+                     P.stat_parts, (const float*)picked, loss, lse, logq));
     return CAPSCAPS_OK;
 }
 
