@@ -805,7 +805,8 @@ def group_norm_fwd(x, groups, *, weight=None, bias=None, act="linear", eps=1e-5,
         y, ys = torch.empty(shape, dtype=dtype, device=device), width
     mean = rstd = None
     if save:
-        mean, rstd = torch.empty((2, shape[0], groups), dtype=torch.float32, device=device)
+        mean = torch.empty((shape[0], groups), dtype=torch.float32, device=device)
+        rstd = torch.empty((shape[0], groups), dtype=torch.float32, device=device)
     need = capscaps_group_norm_fwd_workspace_bytes(norm)
     ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     args = GroupFwdArgs(x.data_ptr(), _vector(weight, width, device, "weight"), _vector(bias, width, device, "bias"),

@@ -29,7 +29,7 @@ namespace capscaps {
 namespace {
 
 constexpr int CUS = 256;
-constexpr int RESIDENT = 512;  // threads of a workgroup at most
+constexpr int RESIDENT = 1024;  // threads of a workgroup at most
 constexpr int SHARED = 256;    // ... in two passes
 constexpr int MOST_BLOCKS = 1 << 22;
 
@@ -78,6 +78,13 @@ struct Packed {
 #pragma unroll
             for (int k = 0; k < WORDS; ++k) w[k] = r[k];
         }
+    }
+    // From here on the values are taken out of their words again (kept as fp32 from one phase to the next they fill twice
+    // the registers, and fewer workgroups of a CU run)
+    __device__ __forceinline__ void hold()
+    {
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) asm volatile("" : "+v"(w[k]));
     }
     __device__ __forceinline__ float value(int k) const  // (k is a constant after unrolling)
     {
@@ -132,23 +139,47 @@ __device__ __forceinline__ void load_columns(float* f, const float* p, long long
     for (int k = 0; k < V; ++k) f[k] = p != nullptr ? p[at + k] : none;
 }
 
-// Sums over each group of a slab of what the working lanes hold for their columns (f[0] alone where a vector is of
-// one group): to total[group], read after the barrier that ends this.
+// What a table of the slab's groups holds for a lane's columns: one value where a vector is of one group
+template <int V, bool FOLD>
+struct OfGroups {
+    float f[FOLD ? 1 : V];
+    __device__ __forceinline__ OfGroups(const float* table, int c, int columns, float factor = 1.0f)
+    {
+#pragma unroll
+        for (int k = 0; k < (FOLD ? 1 : V); ++k) f[k] = table[(c * V + k) / columns] * factor;
+    }
+    __device__ __forceinline__ float operator[](int k) const { return f[FOLD ? 0 : k]; }
+};
+
 template <int V>
-__device__ __forceinline__ void group_totals(const GroupPlan& P, int columns, const float* f, int q, int c, float* lds,
+__device__ __forceinline__ void put_columns(float* to, const float* f)  // (to LDS, at a multiple of V)
+{
+    if constexpr (V % 4 == 0) {
+        typedef float four __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int k = 0; k < V; k += 4) *reinterpret_cast<four*>(to + k) = four{f[k], f[k + 1], f[k + 2], f[k + 3]};
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) to[k] = f[k];
+    }
+}
+
+// Sums over each group of a slab of what the working lanes hold for their columns (summed first where a vector is of
+// one group): to total[group], read after the barrier that ends this.
+template <int V, bool FOLD>
+__device__ __forceinline__ void group_totals(const GroupPlan& P, const float* f, int q, int c, float* lds,
                                              float* total)
 {
-    const int per = P.fold == V ? 1 : V;              // values of a lane
+    constexpr int per = FOLD ? 1 : V;                    // values of a lane
     const int row = P.vecs * per, mine = row / P.whole;  // ... of a position, and of a group of it
     if (q < P.rows) {
-        if (per == 1) {
+        if constexpr (FOLD) {
             float s = f[0];
 #pragma unroll
             for (int k = 1; k < V; ++k) s += f[k];
             lds[q * row + c] = s;
         } else {
-#pragma unroll
-            for (int k = 0; k < V; ++k) lds[q * row + c * V + k] = f[k];
+            put_columns<V>(lds + q * row + c * V, f);
         }
     }
     __syncthreads();
@@ -165,88 +196,79 @@ __device__ __forceinline__ void group_totals(const GroupPlan& P, int columns, co
     __syncthreads();
 }
 
-// the groups of a slab that a lane's columns are in, and what `table` holds of them
-template <int V>
-__device__ __forceinline__ void of_groups(float* f, const GroupPlan& P, int columns, int c, const float* table)
-{
-    if (P.fold == V) {
-        const float t = table[c * V / columns];
-#pragma unroll
-        for (int k = 0; k < V; ++k) f[k] = t;
-    } else {
-#pragma unroll
-        for (int k = 0; k < V; ++k) f[k] = table[(c * V + k) / columns];
-    }
-}
-
 // ---------------------------------------------------------------------------------------- resident
-template <int XD, int YD, int V, int I>
+template <int XD, int YD, int V, int I, bool FOLD>
 __global__ void __launch_bounds__(RESIDENT) group_fwd_resident_kernel(GroupCall C)
 {
-    extern __shared__ float lds[];
+    extern __shared__ __attribute__((aligned(16))) float lds[];
     const GroupPlan& P = C.P;
     typedef Packed<XD, V> X;
     constexpr int YB = YD == CAPSCAPS_FP32 ? 4 : 2;
-    float* total = lds + P.rows * P.vecs * (P.fold == V ? 1 : V);
+    float* total = lds + P.rows * P.vecs * (FOLD ? 1 : V);
     const int q = threadIdx.x / P.vecs, c = threadIdx.x - q * P.vecs;
-    const bool works = q < P.rows;
     const float m = 1.0f / ((float)C.G.positions * (float)C.columns);
     const long long b = by_xcd(blockIdx.x, gridDim.x);
     const int slab = (int)(b % P.slabs);
     const long long col = (long long)slab * P.slab + c * V;
-    float w[V], bias[V];
-    load_columns<V>(w, works ? C.weight : nullptr, col, 1.0f);
-    load_columns<V>(bias, works ? C.bias : nullptr, col, 0.0f);
     const int positions = (int)C.G.positions;
+    // a lane's vectors: positions q, q + rows, ...
+    const int mine = q < P.rows && q < positions ? (positions - q + P.rows - 1) / P.rows : 0;
+    float w[V], bias[V];
+    load_columns<V>(w, mine ? C.weight : nullptr, col, 1.0f);
+    load_columns<V>(bias, mine ? C.bias : nullptr, col, 0.0f);
+    const long long x_step = P.rows * C.x_stride * X::SIZE, y_step = P.rows * C.out_stride * YB;
     for (long long n = b / P.slabs; n < C.G.images; n += P.shares) {
-        const char* x = C.x + (n * positions * C.x_stride + col) * X::SIZE;
+        const char* x = C.x + ((n * positions + q) * C.x_stride + col) * X::SIZE;
         X v[I];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int p = q + i * P.rows;
             v[i].clear();
-            if (works && p < positions) v[i].load(x + p * C.x_stride * X::SIZE);
+            if (i < mine) v[i].load(x + i * x_step);
         }
-        float s[V], mean[V];
+        float s[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) s[k] = 0.0f;
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
             for (int k = 0; k < V; ++k) s[k] += v[i].value(k);
-        group_totals<V>(P, C.columns, s, q, c, lds, total);
-        of_groups<V>(mean, P, C.columns, c, total);
-#pragma unroll
-        for (int k = 0; k < V; ++k) mean[k] *= m, s[k] = 0.0f;
+        group_totals<V, FOLD>(P, s, q, c, lds, total);
+        const OfGroups<V, FOLD> mean(total, c, C.columns, m);
         const long long stat = n * C.G.groups + (long long)slab * P.whole;
         if (C.mean != nullptr)
             for (int g = threadIdx.x; g < P.whole; g += P.threads) C.mean[stat + g] = total[g] * m;
 #pragma unroll
-        for (int i = 0; i < I; ++i)
-            if (works && q + i * P.rows < positions)
+        for (int k = 0; k < V; ++k) s[k] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            v[i].hold();
+            if (i < mine)
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
                     const float d = v[i].value(k) - mean[k];
                     s[k] = __builtin_fmaf(d, d, s[k]);
                 }
+        }
         __syncthreads();  // (everybody has read the totals)
-        group_totals<V>(P, C.columns, s, q, c, lds, total);
-        of_groups<V>(s, P, C.columns, c, total);
-#pragma unroll
-        for (int k = 0; k < V; ++k) s[k] = w[k] / __builtin_sqrtf(s[k] * m + C.G.eps);
+        group_totals<V, FOLD>(P, s, q, c, lds, total);
         if (C.rstd != nullptr)
             for (int g = threadIdx.x; g < P.whole; g += P.threads)
                 C.rstd[stat + g] = 1.0f / __builtin_sqrtf(total[g] * m + C.G.eps);
-        char* y = C.out + (n * positions * C.out_stride + col) * YB;
+        OfGroups<V, FOLD> rstd(total, c, C.columns, m);
+#pragma unroll
+        for (int k = 0; k < (FOLD ? 1 : V); ++k) rstd.f[k] = 1.0f / __builtin_sqrtf(rstd.f[k] + C.G.eps);
+#pragma unroll
+        for (int k = 0; k < V; ++k) s[k] = w[k] * rstd[k];
+        char* y = C.out + ((n * positions + q) * C.out_stride + col) * YB;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int p = q + i * P.rows;
-            if (works && p < positions) {
+            v[i].hold();
+            if (i < mine) {
                 float f[V];
 #pragma unroll
                 for (int k = 0; k < V; ++k)
                     f[k] = act_value(C.G.act, __builtin_fmaf(v[i].value(k) - mean[k], s[k], bias[k]));
-                store_values<YD, V>(y + p * C.out_stride * YB, f);
+                store_values<YD, V>(y + i * y_step, f);
             }
         }
         __syncthreads();  // (... and the totals of the squares)
@@ -265,68 +287,75 @@ __device__ __forceinline__ GroupBack group_back(int act, float x, float dy, floa
     return k;
 }
 
-// partial[workgroup of the slab][2][width]: sums of da * xn and of da over its images
-template <int XD, int YD, int V, int I>
+// partial[workgroup of the slab][2][width]: sums of da * xn and of da over its images.  What bounds it besides HBM is the
+// exponential and the quotient of act': da is kept (in fp32, where dy was) for the second use of it, unless registers
+// are short (16-bit values, eight vectors).
+template <int XD, int YD, int V, int I, bool FOLD>
 __global__ void __launch_bounds__(RESIDENT) group_bwd_resident_kernel(GroupCall C)
 {
-    extern __shared__ float lds[];  // [2][rows][slab] sums of lanes, [2][slab] of columns, [2][slab] over images, [2][whole]
+    // [2][rows][slab] sums of lanes, [2][slab] of columns, [2][slab] over images, [2][whole]
+    extern __shared__ __attribute__((aligned(16))) float lds[];
     const GroupPlan& P = C.P;
     typedef Packed<XD, V> X;
     typedef Packed<YD, V> Y;
     constexpr int YB = Y::SIZE;
+    constexpr bool KEEP = I <= 4 || YD == CAPSCAPS_FP32;
     const int cells = P.rows * P.slab;
     float *column = lds + 2 * cells, *over = column + 2 * P.slab, *total = over + 2 * P.slab;
     const int q = threadIdx.x / P.vecs, c = threadIdx.x - q * P.vecs;
-    const bool works = q < P.rows;
     const float m = 1.0f / ((float)C.G.positions * (float)C.columns);
     const long long b = by_xcd(blockIdx.x, gridDim.x);
     const int slab = (int)(b % P.slabs), lane = threadIdx.x & 63, waves = P.threads >> 6;
     const long long col = (long long)slab * P.slab + c * V;
-    float w[V], bias[V];
-    load_columns<V>(w, works ? C.weight : nullptr, col, 1.0f);
-    load_columns<V>(bias, works ? C.bias : nullptr, col, 0.0f);
     const int positions = (int)C.G.positions;
+    const int mine = q < P.rows && q < positions ? (positions - q + P.rows - 1) / P.rows : 0;
+    float w[V], bias[V];
+    load_columns<V>(w, mine ? C.weight : nullptr, col, 1.0f);
+    load_columns<V>(bias, mine ? C.bias : nullptr, col, 0.0f);
+    const long long x_step = P.rows * C.x_stride * X::SIZE, dy_step = P.rows * C.dy_stride * YB;
+    const long long out_step = P.rows * C.out_stride * YB;
     for (int t = threadIdx.x; t < 2 * P.slab; t += P.threads) over[t] = 0.0f;
     for (long long n = b / P.slabs; n < C.G.images; n += P.shares) {
-        const char* x = C.x + (n * positions * C.x_stride + col) * X::SIZE;
-        const char* dy = C.dy + (n * positions * C.dy_stride + col) * YB;
+        const char* x = C.x + ((n * positions + q) * C.x_stride + col) * X::SIZE;
+        const char* dy = C.dy + ((n * positions + q) * C.dy_stride + col) * YB;
         X v[I];
         Y d[I];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int p = q + i * P.rows;
             v[i].clear(), d[i].clear();
-            if (works && p < positions) {
-                v[i].load(x + p * C.x_stride * X::SIZE);
-                d[i].load(dy + p * C.dy_stride * YB);
+            if (i < mine) {
+                v[i].load(x + i * x_step);
+                d[i].load(dy + i * dy_step);
             }
         }
-        float mean[V], rstd[V], s1[V], s2[V];
         const long long stat = n * C.G.groups + (long long)slab * P.whole;
-        of_groups<V>(mean, P, C.columns, works ? c : 0, C.mean + stat);
-        of_groups<V>(rstd, P, C.columns, works ? c : 0, C.rstd + stat);
+        const OfGroups<V, FOLD> mean(C.mean + stat, c, C.columns), rstd(C.rstd + stat, c, C.columns);
+        float da[KEEP ? I : 1][V];
+        {
+            float s1[V], s2[V];
 #pragma unroll
-        for (int k = 0; k < V; ++k) s1[k] = s2[k] = 0.0f;
+            for (int k = 0; k < V; ++k) s1[k] = s2[k] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < I; ++i)
-            if (works && q + i * P.rows < positions)
+            for (int i = 0; i < I; ++i)
+                if (i < mine)
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const GroupBack g =
-                        group_back(C.G.act, v[i].value(k), d[i].value(k), mean[k], rstd[k], w[k], bias[k]);
-                    s1[k] = __builtin_fmaf(g.da, g.xn, s1[k]);
-                    s2[k] += g.da;
-                }
-        if (works)
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                lds[q * P.slab + c * V + k] = s1[k];
-                lds[cells + q * P.slab + c * V + k] = s2[k];
+                    for (int k = 0; k < V; ++k) {
+                        const GroupBack g =
+                            group_back(C.G.act, v[i].value(k), d[i].value(k), mean[k], rstd[k], w[k], bias[k]);
+                        s1[k] = __builtin_fmaf(g.da, g.xn, s1[k]);
+                        s2[k] += g.da;
+                        if constexpr (KEEP) da[i][k] = g.da;
+                    }
+            if (q < P.rows) {
+                put_columns<V>(lds + q * P.slab + c * V, s1);
+                put_columns<V>(lds + cells + q * P.slab + c * V, s2);
             }
+        }
         __syncthreads();
         for (int t = threadIdx.x; t < 2 * P.slab; t += P.threads) {
             const float* of = lds + (t < P.slab ? t : cells + t - P.slab);
             float s = 0.0f;
+#pragma unroll 8
             for (int r = 0; r < P.rows; ++r) s += of[r * P.slab];
             column[t] = s;
             over[t] += s;
@@ -343,21 +372,24 @@ __global__ void __launch_bounds__(RESIDENT) group_bwd_resident_kernel(GroupCall 
             if (lane == 0) total[g] = s * m;
         }
         __syncthreads();
-        of_groups<V>(s1, P, C.columns, works ? c : 0, total);
-        of_groups<V>(s2, P, C.columns, works ? c : 0, total + P.whole);
-        char* dx = C.out + (n * positions * C.out_stride + col) * YB;
+        const OfGroups<V, FOLD> m1(total, c, C.columns), m2(total + P.whole, c, C.columns);
+        char* dx = C.out + ((n * positions + q) * C.out_stride + col) * YB;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int p = q + i * P.rows;
-            if (works && p < positions) {
+            v[i].hold();
+            if constexpr (!KEEP) d[i].hold();
+            if (i < mine) {
                 float f[V];
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
-                    const GroupBack g =
-                        group_back(C.G.act, v[i].value(k), d[i].value(k), mean[k], rstd[k], w[k], bias[k]);
-                    f[k] = rstd[k] * (__builtin_fmaf(g.da, w[k], -s2[k]) - g.xn * s1[k]);
+                    GroupBack g;
+                    if constexpr (KEEP)
+                        g = {(v[i].value(k) - mean[k]) * rstd[k], da[i][k]};
+                    else
+                        g = group_back(C.G.act, v[i].value(k), d[i].value(k), mean[k], rstd[k], w[k], bias[k]);
+                    f[k] = rstd[k] * (__builtin_fmaf(g.da, w[k], -m2[k]) - g.xn * m1[k]);
                 }
-                store_values<YD, V>(dx + p * C.out_stride * YB, f);
+                store_values<YD, V>(dx + i * out_step, f);
             }
         }
     }
@@ -728,8 +760,8 @@ int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 template <bool FORWARD>
 int resident_items(int v, int widest, long long need)
 {
-    for (const int i : {4, 8, 16, 32, 64}) {
-        const bool built = v == widest ? i <= (FORWARD ? 32 : 16) : i == 8 || i == 64;
+    for (const int i : {2, 4, 8, 16}) {
+        const bool built = v == widest ? i <= (FORWARD ? 16 : 8) : i == 8;
         if (built && need <= i) return i;
     }
     return 0;
@@ -744,32 +776,33 @@ GroupPlan group_plan(const capscaps_group_norm& G)
     auto vector = [&](long long cols) { return cols % widest == 0 ? widest : cols % 2 == 0 ? 2 : 1; };
     // Resident: the fewest whole groups whose vectors are whole and whose rows fill a line of memory; more of them
     // where an image's positions leave lanes without work.
-    for (int narrow = 0; narrow < 2; ++narrow) {
-        int k = 1;
-        for (; k <= G.groups; ++k) {
-            if (G.groups % k != 0) continue;
-            const long long slab = (long long)k * columns;
-            if (narrow || k == G.groups) break;
-            if (vector(slab) == widest && slab * size >= 128 &&
-                slab / widest * G.positions >= 256) break;
-        }
+    int k = 1;
+    for (; k < G.groups; ++k) {
+        if (G.groups % k != 0) continue;
         const long long slab = (long long)k * columns;
-        const int v = vector(slab);
-        const long long vecs = slab / v;
-        if (vecs > (FORWARD ? RESIDENT : RESIDENT / 4)) continue;  // (backward: sums of 1024 columns in LDS)
-        // as many lanes as there are vectors, in whole waves
+        if (vector(slab) == widest && slab * size >= 128 && slab / widest * G.positions >= 256) break;
+    }
+    const long long wide = (long long)k * columns;
+    const long long most = FORWARD ? RESIDENT : RESIDENT / 8;  // vectors (backward: sums of 1024 columns in LDS)
+    if (wide / vector(wide) <= most) {
+        const int v = vector(wide);
+        const long long vecs = wide / v;
+        // As few lanes, in whole waves, as hold the slab: more workgroups of a CU then read and write at a time while others
+        // compute.  Where there are few workgroups, as many lanes as there are vectors.
         int threads = RESIDENT;
-        while (threads > 64 && (threads / 2) / vecs * 4 >= G.positions && threads / 2 >= vecs) threads /= 2;
+        const bool few = G.images * (G.groups / k) < 2 * CUS;
+        const int aim = few ? 2 : v == widest ? (FORWARD ? 16 : 4) : 8;
+        while (threads > 64 && threads / 2 >= vecs && ceil_div(G.positions, threads / 2 / vecs) <= aim) threads /= 2;
         const int rows = threads / (int)vecs;
         const int items = resident_items<FORWARD>(v, widest, ceil_div(G.positions, rows));
-        if (items == 0) continue;
-        P.v = v, P.items = items, P.threads = threads, P.rows = rows, P.vecs = (int)vecs, P.slab = (int)slab;
-        P.whole = k, P.parts = 1, P.slabs = G.groups / k, P.fold = columns % v == 0 ? v : 1;
-        // (backward: a workgroup's images share its sums over columns)
-        P.shares = std::max<long long>(1, std::min<long long>(G.images, (FORWARD ? MOST_BLOCKS : 8 * CUS) / P.slabs));
-        P.per = 0;
-        P.blocks = P.shares * P.slabs;
-        return P;
+        if (items > 0) {
+            P.v = v, P.items = items, P.threads = threads, P.rows = rows, P.vecs = (int)vecs, P.slab = (int)wide;
+            P.whole = k, P.parts = 1, P.slabs = G.groups / k, P.fold = columns % v == 0 ? v : 1;
+            // (backward: a workgroup's images share its sums over columns)
+            P.shares = std::max<long long>(1, std::min<long long>(G.images, (FORWARD ? MOST_BLOCKS : 8 * CUS) / P.slabs));
+            P.blocks = P.shares * P.slabs;
+            return P;
+        }
     }
     // Two passes
     P.threads = SHARED;
@@ -849,9 +882,14 @@ void with_types(const capscaps_group_norm& G, const GroupPlan& P, F f)
         by_x(Int<CAPSCAPS_FP16>());
 }
 
-template <typename K>
-hipError_t launch_resident(K kernel, const GroupCall& C, size_t lds, hipStream_t st)
+template <auto kernel>
+hipError_t launch_resident(const GroupCall& C, size_t lds, hipStream_t st)
 {
+    if (lds > 65536) {  // (1024 lanes: 64 KB and the columns' sums)
+        static std::atomic<unsigned long long> done{0};
+        const hipError_t err = set_dynamic_lds_once(reinterpret_cast<const void*>(kernel), 96 << 10, done);
+        if (err != hipSuccess) return err;
+    }
     kernel<<<dim3((unsigned)C.P.blocks), dim3(C.P.threads), lds, st>>>(C);
     return hipGetLastError();
 }
@@ -863,20 +901,26 @@ hipError_t run_resident(const GroupCall& C, hipStream_t st)
     const size_t lds = group_lds<FORWARD>(C.P);
     with_types(C.G, C.P, [&](auto xd, auto yd, auto v) {
         constexpr int X = xd.value, Y = yd.value, V = v.value;
-        auto with = [&](auto i) {
+        auto folded = [&](auto i, auto fold) {
             if constexpr (FORWARD)
-                err = launch_resident(group_fwd_resident_kernel<X, Y, V, i.value>, C, lds, st);
+                err = launch_resident<group_fwd_resident_kernel<X, Y, V, i.value, fold.value>>(C, lds, st);
             else
-                err = launch_resident(group_bwd_resident_kernel<X, Y, V, i.value>, C, lds, st);
+                err = launch_resident<group_bwd_resident_kernel<X, Y, V, i.value, fold.value>>(C, lds, st);
+        };
+        auto with = [&](auto i) {
+            if constexpr (V == 1)
+                folded(i, std::true_type());
+            else
+                C.P.fold == V ? folded(i, std::true_type()) : folded(i, std::false_type());
         };
         if constexpr (V > 2) {
+            if (C.P.items == 2) with(Int<2>());
             if (C.P.items == 4) with(Int<4>());
             if (C.P.items == 8) with(Int<8>());
-            if (C.P.items == 16) with(Int<16>());
             if constexpr (FORWARD)
-                if (C.P.items == 32) with(Int<32>());
+                if (C.P.items == 16) with(Int<16>());
         } else {
-            C.P.items == 8 ? with(Int<8>()) : with(Int<64>());
+            with(Int<8>());
         }
     });
     return err;
