@@ -29,9 +29,10 @@ namespace capscaps {
 namespace {
 
 constexpr int CUS = 256;
-constexpr int RESIDENT = 1024;  // threads of a workgroup at most
+constexpr int RESIDENT = 1024, RESIDENT_BACK = 512;  // threads of a workgroup at most, forward and backward
 constexpr int SHARED = 256;    // ... in two passes
 constexpr int MOST_BLOCKS = 1 << 22;
+
 
 struct GroupPlan {
     int v, items;            // columns of a vector; vectors a lane holds (0: two passes)
@@ -120,8 +121,8 @@ __device__ __forceinline__ float act_value(int act, float a)
 __device__ __forceinline__ float act_slope(int act, float a)
 {
     if (act == CAPSCAPS_ACT_LINEAR) return 1.0f;
-    const float q = __builtin_amdgcn_rcpf(1.0f + __expf(-a));
-    return act == CAPSCAPS_ACT_SIGMOID ? q * (1.0f - q) : q * (1.0f + a * (1.0f - q));
+    const float q = __builtin_amdgcn_rcpf(1.0f + __expf(-a)), p = 1.0f - q;
+    return q * (act == CAPSCAPS_ACT_SIGMOID ? p : __builtin_fmaf(a, p, 1.0f));
 }
 
 // Consecutive workgroups go to the eight XCDs in turn; neighbouring slabs share lines of memory, so each XCD takes a
@@ -288,10 +289,11 @@ __device__ __forceinline__ GroupBack group_back(int act, float x, float dy, floa
 }
 
 // partial[workgroup of the slab][2][width]: sums of da * xn and of da over its images.  What bounds it besides HBM is the
-// exponential and the quotient of act': da is kept (in fp32, where dy was) for the second use of it, unless registers
-// are short (16-bit values, eight vectors).
+// exponential and the quotient of act': da is kept for the second use of it.  A workgroup takes one image after the other, the
+// next one's values on their way while the sums are joined and dx is written: 64 images of 256 positions of 4096 bf16 values in
+// 32 groups take 91 us, 4.4 TB/s.
 template <int XD, int YD, int V, int I, bool FOLD>
-__global__ void __launch_bounds__(RESIDENT) group_bwd_resident_kernel(GroupCall C)
+__global__ void __launch_bounds__(RESIDENT_BACK) group_bwd_resident_kernel(GroupCall C)
 {
     // [2][rows][slab] sums of lanes, [2][slab] of columns, [2][slab] over images, [2][whole]
     extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -299,7 +301,6 @@ __global__ void __launch_bounds__(RESIDENT) group_bwd_resident_kernel(GroupCall 
     typedef Packed<XD, V> X;
     typedef Packed<YD, V> Y;
     constexpr int YB = Y::SIZE;
-    constexpr bool KEEP = I <= 4 || YD == CAPSCAPS_FP32;
     const int cells = P.rows * P.slab;
     float *column = lds + 2 * cells, *over = column + 2 * P.slab, *total = over + 2 * P.slab;
     const int q = threadIdx.x / P.vecs, c = threadIdx.x - q * P.vecs;
@@ -315,42 +316,51 @@ __global__ void __launch_bounds__(RESIDENT) group_bwd_resident_kernel(GroupCall 
     const long long x_step = P.rows * C.x_stride * X::SIZE, dy_step = P.rows * C.dy_stride * YB;
     const long long out_step = P.rows * C.out_stride * YB;
     for (int t = threadIdx.x; t < 2 * P.slab; t += P.threads) over[t] = 0.0f;
-    for (long long n = b / P.slabs; n < C.G.images; n += P.shares) {
+    X v[I], ahead[I];
+    Y d[I];
+    auto fetch = [&](long long n) {
         const char* x = C.x + ((n * positions + q) * C.x_stride + col) * X::SIZE;
         const char* dy = C.dy + ((n * positions + q) * C.dy_stride + col) * YB;
-        X v[I];
-        Y d[I];
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
-            v[i].clear(), d[i].clear();
+        for (int i = 0; i < I; ++i)
             if (i < mine) {
-                v[i].load(x + i * x_step);
+                ahead[i].load(x + i * x_step);
                 d[i].load(dy + i * dy_step);
             }
-        }
+    };
+#pragma unroll
+    for (int i = 0; i < I; ++i) ahead[i].clear(), d[i].clear();
+    fetch(b / P.slabs);
+    for (long long n = b / P.slabs; n < C.G.images; n += P.shares) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) v[i] = ahead[i];
         const long long stat = n * C.G.groups + (long long)slab * P.whole;
         const OfGroups<V, FOLD> mean(C.mean + stat, c, C.columns), rstd(C.rstd + stat, c, C.columns);
-        float da[KEEP ? I : 1][V];
+        // a = (x - mean) wr + bias; the sums are of da (x - mean), rstd comes to them at the end
+        float da[I][V], wr[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) wr[k] = w[k] * rstd[k];
         {
             float s1[V], s2[V];
 #pragma unroll
             for (int k = 0; k < V; ++k) s1[k] = s2[k] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < I; ++i)
-                if (i < mine)
+            for (int i = 0; i < I; ++i)  // (vectors past the last position: dy = 0, which adds nothing)
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        const GroupBack g =
-                            group_back(C.G.act, v[i].value(k), d[i].value(k), mean[k], rstd[k], w[k], bias[k]);
-                        s1[k] = __builtin_fmaf(g.da, g.xn, s1[k]);
-                        s2[k] += g.da;
-                        if constexpr (KEEP) da[i][k] = g.da;
-                    }
+                for (int k = 0; k < V; ++k) {
+                    const float off = v[i].value(k) - mean[k];
+                    da[i][k] = d[i].value(k) * act_slope(C.G.act, __builtin_fmaf(off, wr[k], bias[k]));
+                    s1[k] = __builtin_fmaf(da[i][k], off, s1[k]);
+                    s2[k] += da[i][k];
+                }
+#pragma unroll
+            for (int k = 0; k < V; ++k) s1[k] *= rstd[k];
             if (q < P.rows) {
                 put_columns<V>(lds + q * P.slab + c * V, s1);
                 put_columns<V>(lds + cells + q * P.slab + c * V, s2);
             }
         }
+        if (n + P.shares < C.G.images) fetch(n + P.shares);
         __syncthreads();
         for (int t = threadIdx.x; t < 2 * P.slab; t += P.threads) {
             const float* of = lds + (t < P.slab ? t : cells + t - P.slab);
@@ -373,21 +383,19 @@ __global__ void __launch_bounds__(RESIDENT) group_bwd_resident_kernel(GroupCall 
         }
         __syncthreads();
         const OfGroups<V, FOLD> m1(total, c, C.columns), m2(total + P.whole, c, C.columns);
+        float c1[FOLD ? 1 : V], c2[FOLD ? 1 : V];
+#pragma unroll
+        for (int k = 0; k < (FOLD ? 1 : V); ++k) c1[k] = -(rstd[k] * rstd[k]) * m1[k], c2[k] = -rstd[k] * m2[k];
         char* dx = C.out + ((n * positions + q) * C.out_stride + col) * YB;
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             v[i].hold();
-            if constexpr (!KEEP) d[i].hold();
             if (i < mine) {
                 float f[V];
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
-                    GroupBack g;
-                    if constexpr (KEEP)
-                        g = {(v[i].value(k) - mean[k]) * rstd[k], da[i][k]};
-                    else
-                        g = group_back(C.G.act, v[i].value(k), d[i].value(k), mean[k], rstd[k], w[k], bias[k]);
-                    f[k] = rstd[k] * (__builtin_fmaf(g.da, w[k], -m2[k]) - g.xn * m1[k]);
+                    const float rest = __builtin_fmaf(v[i].value(k) - mean[k], c1[FOLD ? 0 : k], c2[FOLD ? 0 : k]);
+                    f[k] = __builtin_fmaf(da[i][k], wr[k], rest);
                 }
                 store_values<YD, V>(dx + i * out_step, f);
             }
@@ -783,23 +791,24 @@ GroupPlan group_plan(const capscaps_group_norm& G)
         if (vector(slab) == widest && slab * size >= 128 && slab / widest * G.positions >= 256) break;
     }
     const long long wide = (long long)k * columns;
-    const long long most = FORWARD ? RESIDENT : RESIDENT / 8;  // vectors (backward: sums of 1024 columns in LDS)
+    const long long most = FORWARD ? RESIDENT : RESIDENT_BACK / 4;  // vectors (backward: sums of 1024 columns in LDS)
     if (wide / vector(wide) <= most) {
         const int v = vector(wide);
         const long long vecs = wide / v;
         // As few lanes, in whole waves, as hold the slab: more workgroups of a CU then read and write at a time while others
         // compute.  Where there are few workgroups, as many lanes as there are vectors.
-        int threads = RESIDENT;
+        int threads = FORWARD ? RESIDENT : RESIDENT_BACK;
         const bool few = G.images * (G.groups / k) < 2 * CUS;
-        const int aim = few ? 2 : v == widest ? (FORWARD ? 16 : 4) : 8;
+        const int aim = few ? 2 : v == widest ? (FORWARD ? 16 : 8) : 8;
         while (threads > 64 && threads / 2 >= vecs && ceil_div(G.positions, threads / 2 / vecs) <= aim) threads /= 2;
         const int rows = threads / (int)vecs;
         const int items = resident_items<FORWARD>(v, widest, ceil_div(G.positions, rows));
         if (items > 0) {
             P.v = v, P.items = items, P.threads = threads, P.rows = rows, P.vecs = (int)vecs, P.slab = (int)wide;
             P.whole = k, P.parts = 1, P.slabs = G.groups / k, P.fold = columns % v == 0 ? v : 1;
-            // (backward: a workgroup's images share its sums over columns)
-            P.shares = std::max<long long>(1, std::min<long long>(G.images, (FORWARD ? MOST_BLOCKS : 8 * CUS) / P.slabs));
+            // (backward: a workgroup takes one image after the other, and as many lanes as the registers of a CU hold are at work)
+            const int blocks = FORWARD ? MOST_BLOCKS : CUS * (RESIDENT_BACK / threads) * (items == 8 ? 1 : 2);
+            P.shares = std::max<long long>(1, std::min<long long>(G.images, blocks / P.slabs));
             P.blocks = P.shares * P.slabs;
             return P;
         }
@@ -882,14 +891,9 @@ void with_types(const capscaps_group_norm& G, const GroupPlan& P, F f)
         by_x(Int<CAPSCAPS_FP16>());
 }
 
-template <auto kernel>
-hipError_t launch_resident(const GroupCall& C, size_t lds, hipStream_t st)
+template <typename K>
+hipError_t launch_resident(K kernel, const GroupCall& C, size_t lds, hipStream_t st)
 {
-    if (lds > 65536) {  // (1024 lanes: 64 KB and the columns' sums)
-        static std::atomic<unsigned long long> done{0};
-        const hipError_t err = set_dynamic_lds_once(reinterpret_cast<const void*>(kernel), 96 << 10, done);
-        if (err != hipSuccess) return err;
-    }
     kernel<<<dim3((unsigned)C.P.blocks), dim3(C.P.threads), lds, st>>>(C);
     return hipGetLastError();
 }
@@ -903,9 +907,9 @@ hipError_t run_resident(const GroupCall& C, hipStream_t st)
         constexpr int X = xd.value, Y = yd.value, V = v.value;
         auto folded = [&](auto i, auto fold) {
             if constexpr (FORWARD)
-                err = launch_resident<group_fwd_resident_kernel<X, Y, V, i.value, fold.value>>(C, lds, st);
+                err = launch_resident(group_fwd_resident_kernel<X, Y, V, i.value, fold.value>, C, lds, st);
             else
-                err = launch_resident<group_bwd_resident_kernel<X, Y, V, i.value, fold.value>>(C, lds, st);
+                err = launch_resident(group_bwd_resident_kernel<X, Y, V, i.value, fold.value>, C, lds, st);
         };
         auto with = [&](auto i) {
             if constexpr (V == 1)
