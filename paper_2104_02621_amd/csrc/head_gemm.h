@@ -49,6 +49,7 @@ struct HeadGemm {
     long long ldo, out_split;
     int out_dtype, splits;
     bool accumulate;     // add to what is there (fp32, one part)
+    bool whole_vectors;  // set by the launcher: rows of out are whole 16-byte vectors, 256 of them within 32 bits
     const float* scale;  // NULL, or what to multiply by, in device memory
     // the others: logit = (z + bias[n]) * inv_tau
     const float* bias;  // or NULL

@@ -271,6 +271,66 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
     if constexpr (END == HEAD_OUT) {
         const float scale = G.scale != nullptr ? *G.scale : 1.0f;
         const bool vectors = (G.ldo & 3) == 0;
+        if (G.whole_vectors && n_left >= WN) {
+            // All columns exist: 16 bytes a lane, two lanes side by side, at 32-bit offsets from the wave's first value; rows past
+            // the last are dropped by the range check.  (Column by column with 64-bit addresses, below, a tile of 256 x 256 takes 25 us to
+            // end.)
+            // (The offsets within a row go into the instructions, not into a scalar register: after a 16-byte store with a scalar
+            // offset the compiler lets the next instruction overwrite the stored registers, and some lanes then store the new value.)
+            const int size = G.out_dtype == CAPSCAPS_FP32 ? 4 : 2;
+            const long long first_row = m0 + wm * WM;
+            const long long rows = m_end - first_row < WM ? m_end - first_row : WM;
+            if (rows <= 0) return;
+            const rsrc_t raw = make_rsrc(static_cast<char*>(G.out) + (first_row * G.ldo + part * G.out_split + n0 + wn * WN) * size,
+                                         (unsigned)(((rows - 1) * G.ldo + WN) * size));
+            const unsigned long long base = (unsigned long long)(unsigned)raw[0] | (unsigned long long)(unsigned)raw[1] << 32;
+            const __amdgpu_buffer_rsrc_t rs =
+                __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(base), 0, raw[2], 0x00020000);
+            static_for<TM>([&](auto B) {
+                constexpr int b = decltype(B)::value;
+                // (a row past the last may lie before the next one's end: its own mark)
+                const int voff = b * 32 + lr < rows ? ((b * 32 + lr) * (int)G.ldo + (size == 4 ? 4 : 8) * h) * size : OUT_OF_RANGE;
+                if (G.out_dtype == CAPSCAPS_FP32) {
+                    float4v old[TN * 4];
+                    if (G.accumulate)
+                        static_for<TN * 4>([&](auto Q) {
+                            constexpr int q = decltype(Q)::value;
+                            old[q] = __builtin_bit_cast(float4v, __builtin_amdgcn_raw_buffer_load_b128(rs, voff + q * 32, 0, 0));
+                        });
+                    static_for<TN * 4>([&](auto Q) {
+                        constexpr int q = decltype(Q)::value, a = q / 4, g = q % 4;
+                        float4v r;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float z = acc[a][b][4 * g + j];
+                            r[j] = (TERMS ? z * SPLIT_UNSCALE : z) * scale;
+                        }
+                        if (G.accumulate) r += old[q];
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(chunk_t, r), rs, voff + q * 32, 0, 0);
+                    });
+                } else {
+                    static_for<TN>([&](auto A) {
+                        constexpr int a = decltype(A)::value;
+                        unsigned w[8];
+#pragma unroll
+                        for (int r = 0; r < 16; r += 2) {
+                            float v[2];
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const float z = acc[a][b][r + j];
+                                v[j] = (TERMS ? z * SPLIT_UNSCALE : z) * scale;
+                            }
+                            w[r / 2] = G.out_dtype == CAPSCAPS_FP16 ? half_pair(v[0], v[1]) : round_pair(v[0], v[1]);
+                        }
+#pragma unroll
+                        for (int pair = 0; pair < 2; ++pair)
+                            __builtin_amdgcn_raw_buffer_store_b128(neighbours(w, pair), rs, voff + (a * 64 + pair * 32), 0, 0);
+                    });
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            return;
+        }
         const long long base = (m0 + wm * WM) * G.ldo + part * G.out_split + n0 + wn * WN;
         static_for<TM>([&](auto B) {
             constexpr int b = decltype(B)::value;
@@ -449,8 +509,11 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
 }
 
 template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, bool ROWS, int END>
-hipError_t launch(const HeadGemm& g, hipStream_t st)
+hipError_t launch(HeadGemm g, hipStream_t st)
 {
+    const int size = g.out_dtype == CAPSCAPS_FP32 ? 4 : 2;
+    g.whole_vectors = (reinterpret_cast<uintptr_t>(g.out) & 15) == 0 && g.ldo * size % 16 == 0 && g.out_split * size % 16 == 0 &&
+                      g.ldo * size * BM < 0x7fffffffll;
     const long long tm = (g.m_rows + BM - 1) / BM, tn = (g.n_rows + BN - 1) / BN;
     if (tm * tn * g.splits > (1 << 23) || tm < 1 || tn < 1) return hipErrorInvalidValue;
     const auto kernel = head_gemm_kernel<Tag, BM, BN, NWM, NB, TERMS, ROWS, END>;

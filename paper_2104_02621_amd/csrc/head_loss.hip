@@ -32,7 +32,7 @@ constexpr int MOST_TOP = 1024;
 constexpr long long MOST_ROWS = 1 << 20, MOST_PIECE = 1 << 20;
 // (logits that are written in parts and then read: a row by a workgroup)
 constexpr int MOST_IN_PARTS = 16384;
-constexpr long long PIECE_BYTES = 512ll << 20;  // of a piece's logits, and of its gradients
+constexpr long long PIECE_BYTES = 1ll << 30;  // of a piece's logits, and of its gradients
 
 // What both directions of both losses are given
 struct Head {
@@ -639,7 +639,7 @@ int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 unsigned blocks_for(long long work, long long per) { return (unsigned)std::max<long long>(1, std::min<long long>((work + per - 1) / per, 1 << 20)); }
 
 // Tile and parts of a product: the least of an estimate in units of a 256 x 256 tile's stage on a CU (1024 matrix
-// cycles, 0.43 us).  A tile begins and ends in the time of some stages; parts are written and added up at memory speed.
+// cycles, 0.7 us at the clock that large products run at).  A tile begins and ends in the time of some stages; parts are written and added up at memory speed.
 struct Pick {
     int tile, splits;
 };
@@ -653,15 +653,15 @@ Pick pick_tile(long long m, long long n, long long k, int terms, bool may_split,
         const double tiles = (double)((m + s.m - 1) / s.m) * (double)((n + s.n - 1) / s.n);
         const double slots = 256.0 * s.per_cu;
         // time of a stage of as many tiles as a CU holds, and stages' time to begin and end
-        const double cost = tile == HEAD_TILE_256 ? 1.0 : tile == HEAD_TILE_128 ? 0.7 : 0.5;
-        const double ends = tile == HEAD_TILE_256 ? 12 : 10;
+        const double cost = tile == HEAD_TILE_256 ? 1.0 : tile == HEAD_TILE_128 ? 0.75 : 0.5;
+        const double ends = tile == HEAD_TILE_256 ? 24 : 8;
         for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts * 2) {
             if (parts > 1 && (!may_split || stages / parts < 8)) break;
             if (tiles * parts > (1 << 23)) continue;
             const double load = tiles * parts / slots;
             const double rounds = load <= 4 ? std::max(1.0, (double)(long long)(load + 0.999)) : load;
             double t = rounds * ((double)((stages + parts - 1) / parts) + ends) * cost;
-            if (parts > 1) t += ((double)m * n * 8 * parts / 4e6 + part_us) / 0.43;
+            if (parts > 1) t += ((double)m * n * 8 * parts / 4e6 + part_us) / 0.7;
             if (t < least) least = t, best = {tile, parts};
         }
     }

@@ -95,7 +95,7 @@ def test_workspaces_hold_a_piece_of_the_logits():
     """... and not all of them."""
     large = head(rows=1 << 16, width=64, classes=1 << 18)
     for back in (0, 1):
-        assert cc.capscaps_class_loss_workspace_bytes(large, back) < 2 << 30
+        assert cc.capscaps_class_loss_workspace_bytes(large, back) < 4 << 30  # (the logits: 64 GB)
 
 
 def test_structures_have_the_headers_sizes():
