@@ -238,11 +238,13 @@ __global__ void __launch_bounds__(THREADS) pack_kernel(const void* from, long lo
     }
 }
 
-// Columns of `from` as an operand that contracts its rows (rows_of[i], those that count); zeros past them.  Tiles of 64 x 64.
+// Columns of `from` as an operand that contracts its rows (rows_of[i], those that count); zeros past them.  And, where
+// `straight` is not NULL, what pack_kernel makes of it.  Tiles of 64 x 64.
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* from, long long stride, int columns,
                                                                   long long rows, const int* rows_of, const int* count,
-                                                                  unsigned short* to, long long stages, bool vectors)
+                                                                  unsigned short* to, long long stages,
+                                                                  unsigned short* straight, long long straight_stages, bool vectors)
 {
     typedef std::conditional_t<TERMS, float, unsigned short> E;
     __shared__ E tile[64][TERMS ? 65 : 66];
@@ -299,6 +301,23 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* fr
                 put_operand<TERMS>(to, c0 + c, i0 + i, stages, raw, f);
             }
         }
+        if (straight != nullptr)
+            for (int t = threadIdx.x; t < 64 * 8; t += THREADS) {
+                const int block = t >> 6, i = (block >> 1) * 16 + ((t & 63) >> 2);
+                const int c = (block & 1) * HEAD_K + ((t & 3) ^ ((t & 63) >> 4)) * 8;
+                if (i0 + i < (kept + 15) / 16 * 16 && c0 + c < straight_stages * HEAD_K) {
+                    unsigned short raw[8];
+                    float f[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        if constexpr (TERMS)
+                            f[j] = tile[i][c + j];
+                        else
+                            raw[j] = tile[i][c + j];
+                    }
+                    put_operand<TERMS>(straight, i0 + i, c0 + c, straight_stages, raw, f);
+                }
+            }
         __syncthreads();
     }
 }
@@ -348,12 +367,15 @@ __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, 
 }
 
 // picked[row][k] = z of the rows' entries (0 where they do not count), from the operands in fp32.  A wave for four entries of a
-// row at a time: what it waits for is the weights' rows, which lie anywhere.
+// row at a time: what it waits for is the weights' rows, which lie anywhere.  Where there are few, the four waves of a workgroup (WIDE).
+template <bool WIDE>
 __global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bool vectors)
 {
-    const int lane = threadIdx.x & 63;
+    constexpr int LANES = WIDE ? THREADS : 64, PER = THREADS / LANES;
+    __shared__ float parts[4][4];
+    const int lane = threadIdx.x & (LANES - 1);
     const long long kept = *H.count, quads = (H.top + 3) / 4;
-    for (long long t = blockIdx.x * 4ll + (threadIdx.x >> 6); t < kept * quads; t += gridDim.x * 4ll) {
+    for (long long t = blockIdx.x * (long long)PER + threadIdx.x / LANES; t < kept * quads; t += gridDim.x * (long long)PER) {
         const long long r = H.rows_of[t / quads];
         const int k0 = (int)(t % quads) * 4;
         long long cls[4];
@@ -364,7 +386,7 @@ __global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bo
         if (vectors && H.dtype != CAPSCAPS_FP32) {
             const unsigned short *x = static_cast<const unsigned short*>(H.x) + xa, *w = static_cast<const unsigned short*>(H.weight);
 #pragma unroll 2
-            for (int c = lane * 8; c < H.width; c += 512) {
+            for (int c = lane * 8; c < H.width; c += LANES * 8) {
                 const chunk_t a = *reinterpret_cast<const chunk_t*>(x + c);
                 chunk_t b[4];
 #pragma unroll
@@ -386,7 +408,7 @@ __global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bo
                         }
             }
         } else {
-            for (int c = lane; c < H.width; c += 64) {
+            for (int c = lane; c < H.width; c += LANES) {
                 const float a = load_element(H.x, xa + c, H.dtype);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -396,9 +418,15 @@ __global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bo
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             s[j] = lanes_sum(s[j], 64);
+            if constexpr (WIDE) {
+                if ((lane & 63) == 0) parts[lane >> 6][j] = s[j];
+                __syncthreads();
+                s[j] = (parts[0][j] + parts[1][j]) + (parts[2][j] + parts[3][j]);
+            }
             if (cls[j] >= 0 && H.bias != nullptr) s[j] += H.bias[cls[j]];
             if (lane == 0 && k0 + j < H.top) picked[r * H.top + k0 + j] = s[j];
         }
+        if constexpr (WIDE) __syncthreads();
     }
 }
 
@@ -792,15 +820,16 @@ hipError_t pack(const Plan& P, const void* from, long long stride, int columns, 
                         : run(pack_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors);
 }
 hipError_t pack_transposed(const Plan& P, const void* from, long long stride, int columns, long long rows, const Head* kept,
-                           unsigned short* to, long long padded, hipStream_t st)
+                           unsigned short* to, long long padded, unsigned short* straight, hipStream_t st)
 {
     const int* rows_of = kept != nullptr ? kept->rows_of : nullptr;
     const int* count = kept != nullptr ? kept->count : nullptr;
     const long long stages = padded / HEAD_K;
     const unsigned blocks = blocks_for((padded + 63) / 64 * ((columns + 63) / 64), 1);
     const bool vectors = vectors_of(from, stride, P.terms == 3 ? CAPSCAPS_FP32 : CAPSCAPS_BF16);
-    return P.terms == 3 ? run(pack_transposed_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors)
-                        : run(pack_transposed_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors);
+    const long long across = P.padded / HEAD_K;
+    return P.terms == 3 ? run(pack_transposed_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, straight, across, vectors)
+                        : run(pack_transposed_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, straight, across, vectors);
 }
 
 const void* weight_at(const Head& H, long long cls)
@@ -808,17 +837,19 @@ const void* weight_at(const Head& H, long long cls)
     return static_cast<const char*>(H.weight) + cls * H.weight_stride * (long long)element_bytes(H.dtype);
 }
 
-// The rows that count, and x of these as an operand
-int begin(const Head& H, const Plan& P, const float* dloss, long long dloss_stride, hipStream_t st)
+// The rows that count, and x of these as an operand (and one that contracts rows)
+int begin(const Head& H, const Plan& P, const float* dloss, long long dloss_stride, bool both, hipStream_t st)
 {
     if (P.distill) CAPSCAPS_TRY(run(teacher_kernel, blocks_for(H.rows, 4), THREADS, st, H));
     CAPSCAPS_TRY(run(rows_kernel, 1, 1024, st, H, dloss, dloss_stride));
-    CAPSCAPS_TRY(pack(P, H.x, H.x_stride, H.width, H.rows, &H, H.dtype, P.x, st));
+    CAPSCAPS_TRY(both ? pack_transposed(P, H.x, H.x_stride, H.width, H.rows, &H, P.xt, P.padded_rows, P.x, st)
+                      : pack(P, H.x, H.x_stride, H.width, H.rows, &H, H.dtype, P.x, st));
     return CAPSCAPS_OK;
 }
 
-// The product of x and a piece's weights, for launch_head_gemm with an end of the caller's
-int logits_of(const Head& H, const Plan& P, long long first, long long classes, HeadGemm& g, hipStream_t st)
+// The product of x and a piece's weights, for launch_head_gemm with an end of the caller's; with `both`, the weights as an
+// operand that contracts classes too
+int logits_of(const Head& H, const Plan& P, long long first, long long classes, bool both, HeadGemm& g, hipStream_t st)
 {
     g = HeadGemm{};
     const int stages = P.padded / HEAD_K;
@@ -830,9 +861,12 @@ int logits_of(const Head& H, const Plan& P, long long first, long long classes, 
         H.weight_stride <= (1 << 21)) {
         g.b = weight_at(H, first), g.ldb = H.weight_stride * 2;
     } else {
-        CAPSCAPS_TRY(pack(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, H.dtype, P.w, st));
+        if (!both) CAPSCAPS_TRY(pack(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, H.dtype, P.w, st));
         g.b = P.w, g.stages_b = g.stages_a;
     }
+    if (both)
+        CAPSCAPS_TRY(pack_transposed(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, P.wt, round_up(classes, HEAD_K),
+                                     g.b == P.w ? P.w : nullptr, st));
     g.m_rows = H.rows, g.n_rows = classes, g.m_count = H.count, g.k = H.width;
     g.plane_a = g.plane_b = stages;
     g.dtype = H.dtype, g.splits = P.z.splits;
@@ -848,12 +882,12 @@ int logits_of(const Head& H, const Plan& P, long long first, long long classes, 
 int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, hipStream_t st)
 {
     if (H.rows == 0) return CAPSCAPS_OK;
-    int rc = begin(H, P, nullptr, 0, st);
+    int rc = begin(H, P, nullptr, 0, false, st);
     if (rc != CAPSCAPS_OK) return rc;
     for (int piece = 0; piece < P.pieces; ++piece) {
         const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
         HeadGemm g;
-        rc = logits_of(H, P, first, classes, g, st);
+        rc = logits_of(H, P, first, classes, false, g, st);
         if (rc != CAPSCAPS_OK) return rc;
         g.stats = P.stats;
         g.first_part = (int)(first / head_tile_shape(P.z.tile).stat_columns);
@@ -865,7 +899,8 @@ int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, 
     const bool vectors = vectors_of(H.x, H.x_stride, H.dtype) && vectors_of(H.weight, H.weight_stride, H.dtype) && H.width % 8 == 0;
     // (the entries' z: where logq goes, or in the workspace)
     float* const picked = logq != nullptr ? logq : P.picked;
-    CAPSCAPS_TRY(run(pick_kernel, blocks_for(H.rows * ((H.top + 3) / 4), 4), THREADS, st, H, picked, vectors));
+    const long long quads = H.rows * ((H.top + 3) / 4);
+    CAPSCAPS_TRY(run(quads < 1024 ? pick_kernel<true> : pick_kernel<false>, blocks_for(quads, quads < 1024 ? 1 : 4), THREADS, st, H, picked, vectors));
     const bool few = H.rows < 512;
     CAPSCAPS_TRY(run(few ? loss_kernel<1> : loss_kernel<8>, blocks_for(H.rows, few ? 1 : 8), THREADS, st, H, (const Stat*)P.stats,
                      P.stat_parts, (const float*)picked, loss, lse, logq));
@@ -888,7 +923,7 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
     for (int piece = 0; piece < P.pieces; ++piece) {
         const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
         HeadGemm z;
-        const int rc = logits_of(H, P, first, classes, z, st);
+        const int rc = logits_of(H, P, first, classes, G.dx != nullptr, z, st);
         if (rc != CAPSCAPS_OK) return rc;
         const int padded = (int)round_up(classes, HEAD_K);
         float* const sums = G.dbias != nullptr ? P.bias_sums : nullptr;
@@ -909,7 +944,6 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
                              P.in_parts ? 64 : head_tile_shape(P.z.tile).sum_rows,
                              (const long long*)P.taken, first, (int)classes, G.dbias));
         if (G.dx != nullptr) {
-            CAPSCAPS_TRY(pack_transposed(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, P.wt, padded, st));
             HeadGemm g{};
             g.a = P.gn, g.b = P.wt;
             g.plane_a = g.plane_b = padded / HEAD_K;
@@ -958,11 +992,9 @@ int backward(const Head& H, const Plan& P, const Gradients& G, hipStream_t st)
             CAPSCAPS_TRY(run(zero_kernel, blocks_for(H.classes * 2, THREADS), THREADS, st, reinterpret_cast<unsigned short*>(G.dbias), H.classes * 2));
         return CAPSCAPS_OK;
     }
-    const int rc = begin(H, P, G.dloss, G.dloss_stride, st);
+    const int rc = begin(H, P, G.dloss, G.dloss_stride, G.dweight != nullptr, st);
     if (rc != CAPSCAPS_OK) return rc;
     if (G.dbias != nullptr) CAPSCAPS_TRY(run(clear_kernel, blocks_for(H.classes, THREADS), THREADS, st, P.taken, H.classes));
-    if (G.dweight != nullptr)
-        CAPSCAPS_TRY(pack_transposed(P, H.x, H.x_stride, H.width, H.rows, &H, P.xt, P.padded_rows, st));
     return P.terms == 3 ? backward_pieces<true>(H, P, G, st) : backward_pieces<false>(H, P, G, st);
 }
 
