@@ -374,7 +374,7 @@ int capscaps_block_norm_bwd(const capscaps_block* block, const capscaps_block_bw
  * dweight and dbias.  Stream and error rules as for the calls above.
  */
 typedef struct capscaps_group_norm {
-    long long images, positions; /* positions up to 2^31 - 1 */
+    long long images, positions; /* positions up to 2^30 */
     int width, groups;           /* up to 2^30 */
     int x_dtype, dtype;
     int act;

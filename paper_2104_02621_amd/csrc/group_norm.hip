@@ -742,7 +742,7 @@ __global__ void __launch_bounds__(1024) group_column_sums_kernel(const float* pa
 int check_group(const capscaps_group_norm* g)
 {
     if (g == nullptr || g->images < 1 || g->positions < 1 || g->width < 1 || g->groups < 1) return CAPSCAPS_EINVAL;
-    if (g->width > (1 << 30) || g->width % g->groups != 0 || g->positions > (1ll << 31) - 1) return CAPSCAPS_EINVAL;
+    if (g->width > (1 << 30) || g->width % g->groups != 0 || g->positions > (1ll << 30)) return CAPSCAPS_EINVAL;
     if (!known_dtype(g->dtype) || (g->x_dtype != CAPSCAPS_FP32 && g->x_dtype != g->dtype)) return CAPSCAPS_EINVAL;
     if (g->act < CAPSCAPS_ACT_LINEAR || g->act > CAPSCAPS_ACT_SILU) return CAPSCAPS_EINVAL;
     if (!(g->eps >= 1.17549435e-38f && g->eps <= 3.4e38f)) return CAPSCAPS_EINVAL;

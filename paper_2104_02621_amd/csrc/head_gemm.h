@@ -54,8 +54,7 @@ struct HeadGemm {
     // the others: logit = (z + bias[n]) * inv_tau
     const float* bias;  // or NULL
     float inv_tau;
-    HeadStat* stats;  // [first_part + n / stat_columns][m_rows]
-    int first_part;
+    HeadStat* stats;  // [n / stat_columns][m_rows]
     const float *coef, *lse;  // of row m, and of row rows_of[m]
     const int* rows_of;
     unsigned short *gn, *gt;  // rows m and rows n, in blocks of planes_n and planes_t stages a term

@@ -400,7 +400,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
             __builtin_amdgcn_sched_barrier(0);
         });
     if constexpr (END == HEAD_STATS) {
-        const long long first = (G.first_part + (n0 + wn * WN) / WN) * G.m_rows;
+        const long long first = (n0 + wn * WN) / WN * G.m_rows;
         const float minus = -__builtin_inff(), inv_log2 = G.inv_tau * 1.44269504f;
         static_for<TM>([&](auto B) {
             constexpr int b = decltype(B)::value;
@@ -495,7 +495,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
-        if (G.sums != nullptr) {
+        if (G.sums != nullptr && m0 + wm * WM < m_end) {
             float* const to = G.sums + ((m0 + wm * WM) / WM) * G.planes_n * HEAD_K + n0 + wn * WN;
             static_for<TN * 16>([&](auto Q) {
                 constexpr int a = decltype(Q)::value / 16, r = decltype(Q)::value % 16;
@@ -515,7 +515,7 @@ hipError_t launch(HeadGemm g, hipStream_t st)
     g.whole_vectors = (reinterpret_cast<uintptr_t>(g.out) & 15) == 0 && g.ldo * size % 16 == 0 && g.out_split * size % 16 == 0 &&
                       g.ldo * size * BM < 0x7fffffffll;
     const long long tm = (g.m_rows + BM - 1) / BM, tn = (g.n_rows + BN - 1) / BN;
-    if (tm * tn * g.splits > (1 << 23) || tm < 1 || tn < 1) return hipErrorInvalidValue;
+    if (tm * tn * g.splits > (1 << 23) || tm < 1 || tn < 1) return hipErrorInvalidValue;  // (the plan keeps within it)
     const auto kernel = head_gemm_kernel<Tag, BM, BN, NWM, NB, TERMS, ROWS, END>;
     constexpr int lds = (BM + BN) * 64 * NB;
     static std::atomic<unsigned long long> done{0};

@@ -30,6 +30,7 @@ constexpr int THREADS = 256;
 constexpr int MOST_TOP = 1024;
 // (256 rows of an operand are within a signed 32-bit offset: rows of up to 2^20 values of three terms)
 constexpr long long MOST_ROWS = 1 << 20, MOST_PIECE = 1 << 20;
+constexpr long long MOST_TILES = 1 << 23;  // of a launch
 // (logits that are written in parts and then read: a row by a workgroup)
 constexpr int MOST_IN_PARTS = 16384;
 constexpr long long PIECE_BYTES = 1ll << 30;  // of a piece's logits, and of its gradients
@@ -430,6 +431,40 @@ __global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bo
     }
 }
 
+// The parts of the statistics of ROWS rows from i0 on (lane & (ROWS - 1) is a lane's), joined by a workgroup: to joined[row] for
+// the first ROWS threads, after the barrier that ends this
+template <int ROWS>
+__device__ __forceinline__ Stat join_parts(const Stat* stats, long long stride, int parts, long long i0, int rows, Stat (*waves)[ROWS])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Stat s = {-__builtin_inff(), 0.0f};
+    if ((lane & (ROWS - 1)) < rows)
+        for (int p = threadIdx.x / ROWS; p < parts; p += THREADS / ROWS) s = join(s, stats[p * stride + i0 + (lane & (ROWS - 1))]);
+#pragma unroll
+    for (int k = ROWS; k < 64; k <<= 1) s = join(s, {__shfl_xor(s.top, k), __shfl_xor(s.sum, k)});
+    if (lane < ROWS) waves[wave][lane] = s;
+    __syncthreads();
+    if (threadIdx.x < ROWS) s = join(join(waves[0][lane], waves[1][lane]), join(waves[2][lane], waves[3][lane]));
+    return s;
+}
+
+// A piece's parts, and what the pieces before it left in part 0 (`more`), joined into part 0
+template <int ROWS>
+__global__ void __launch_bounds__(THREADS) fold_kernel(Head H, Stat* stats, int parts, bool more)
+{
+    __shared__ Stat waves[4][ROWS];
+    const int kept = *H.count;
+    for (long long i0 = blockIdx.x * (long long)ROWS; i0 < kept; i0 += gridDim.x * (long long)ROWS) {
+        const int rows = kept - i0 < ROWS ? (int)(kept - i0) : ROWS;
+        Stat s = join_parts<ROWS>(stats + H.rows, H.rows, parts, i0, rows, waves);
+        if (threadIdx.x < rows) {
+            if (more) s = join(stats[i0 + threadIdx.x], s);
+            stats[i0 + threadIdx.x] = s;
+        }
+        __syncthreads();
+    }
+}
+
 // loss, lse, logq of all rows, from stats[part][i] and the entries' z (which logq takes the place of, where it is wanted).
 // A workgroup for ROWS of the rows that are kept, and for the zeros of as many that are not (eight: whole 64-byte pieces of a
 // part's statistics; one where rows are few).
@@ -452,15 +487,8 @@ __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats
         }
         if (i0 >= kept) continue;
         const int rows = kept - i0 < ROWS ? (int)(kept - i0) : ROWS;
-        Stat s = {-__builtin_inff(), 0.0f};
-        if ((lane & (ROWS - 1)) < rows)
-            for (int p = threadIdx.x / ROWS; p < parts; p += THREADS / ROWS) s = join(s, stats[p * H.rows + i0 + (lane & (ROWS - 1))]);
-#pragma unroll
-        for (int k = ROWS; k < 64; k <<= 1) s = join(s, {__shfl_xor(s.top, k), __shfl_xor(s.sum, k)});
-        if (lane < ROWS) joined[wave][lane] = s;
-        __syncthreads();
+        const Stat s = join_parts<ROWS>(stats, H.rows, parts, i0, rows, joined);
         if (threadIdx.x < ROWS) {
-            s = join(join(joined[0][lane], joined[1][lane]), join(joined[2][lane], joined[3][lane]));
             lses[lane] = s.top + logf(s.sum);
         }
         __syncthreads();
@@ -685,7 +713,7 @@ Pick pick_tile(long long m, long long n, long long k, int terms, bool may_split,
         const double ends = tile == HEAD_TILE_256 ? 24 : 8;
         for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts * 2) {
             if (parts > 1 && (!may_split || stages / parts < 8)) break;
-            if (tiles * parts > (1 << 23)) continue;
+            if (tiles * parts > MOST_TILES) continue;
             const double load = tiles * parts / slots;
             const double rounds = load <= 4 ? std::max(1.0, (double)(long long)(load + 0.999)) : load;
             double t = rounds * ((double)((stages + parts - 1) / parts) + ends) * cost;
@@ -696,13 +724,14 @@ Pick pick_tile(long long m, long long n, long long k, int terms, bool may_split,
     return best;
 }
 
-int check_head(const capscaps_head* h)
+int check_head(const capscaps_head* h, bool distill)
 {
     if (h == nullptr || h->rows < 0 || h->rows > MOST_ROWS || h->width < 1 || h->classes < 1) return CAPSCAPS_EINVAL;
     if (h->width > (1 << 20) || h->classes > (1 << 26) || !known_dtype(h->dtype)) return CAPSCAPS_EINVAL;
     if (h->index_bits != 32 && h->index_bits != 64) return CAPSCAPS_EINVAL;
     if (h->top < 1 || h->top > MOST_TOP) return CAPSCAPS_EINVAL;
     if (!(h->temperature >= 1e-6f && h->temperature <= 1e6f)) return CAPSCAPS_EINVAL;
+    if (distill ? !known_dtype(h->teacher_dtype) : h->top != 1 || h->temperature != 1.0f) return CAPSCAPS_EINVAL;
     return CAPSCAPS_OK;
 }
 
@@ -731,7 +760,7 @@ struct Plan {
     // the workspace
     unsigned short *x, *xt, *w, *wt, *gn, *gt;
     float *logits, *dx_sums, *dw_sums, *bias_sums;
-    Stat* stats;
+    Stat* stats;  // [part][rows]; several pieces: part 0 of all, the others of a piece
     float* picked;
     long long* taken;
 };
@@ -754,12 +783,15 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     // a piece's weights as operands, and its gradients
     const long long per_class = 2ll * P.terms * std::max<long long>(P.padded, backward ? rows : 0);
     P.piece = std::max<long long>(256, std::min(MOST_PIECE, PIECE_BYTES / per_class / 256 * 256));
+    P.piece = std::min(P.piece, MOST_TILES / ((rows + 255) / 256) * 256);  // (a launch of tiles of 256 x 256)
     P.piece = std::min<long long>(round_up(A.classes, HEAD_K), P.piece);
+    // (a piece's statistics: 8 bytes for as few as 32 classes of a row)
+    if (!backward) P.piece = std::min(P.piece, std::max<long long>(256, PIECE_BYTES / 8 / rows * 32 / 256 * 256));
     P.pieces = (int)((A.classes + P.piece - 1) / P.piece);
     const long long most = std::min<long long>(P.piece, A.classes);
     P.z = pick_tile(rows, most, A.width, P.terms, P.pieces == 1 && A.classes <= MOST_IN_PARTS && rows * P.piece * 64 * 4 <= PIECE_BYTES, 6.0);
     P.in_parts = P.z.splits > 1;
-    P.stat_parts = P.in_parts ? 1 : ceil_div(A.classes, head_tile_shape(P.z.tile).stat_columns);
+    P.stat_parts = P.in_parts ? 1 : ceil_div(most, head_tile_shape(P.z.tile).stat_columns);  // of a piece
     Layout L{static_cast<char*>(base)};
     Head unused;
     Head& W = H != nullptr ? *H : unused;
@@ -774,7 +806,7 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     P.w = L.take<unsigned short>(head_block_values(most, stages));
     P.logits = P.in_parts ? L.take<float>(rows * P.piece * P.z.splits) : nullptr;
     if (!backward) {
-        P.stats = L.take<Stat>(rows * P.stat_parts);
+        P.stats = L.take<Stat>(rows * (P.stat_parts + (P.pieces > 1)));
         P.picked = distill ? nullptr : L.take<float>(rows);
         P.bytes = L.at;
         return P;
@@ -882,6 +914,7 @@ int logits_of(const Head& H, const Plan& P, long long first, long long classes, 
 int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, hipStream_t st)
 {
     if (H.rows == 0) return CAPSCAPS_OK;
+    const bool few = H.rows < 512;
     int rc = begin(H, P, nullptr, 0, false, st);
     if (rc != CAPSCAPS_OK) return rc;
     for (int piece = 0; piece < P.pieces; ++piece) {
@@ -889,21 +922,22 @@ int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, 
         HeadGemm g;
         rc = logits_of(H, P, first, classes, false, g, st);
         if (rc != CAPSCAPS_OK) return rc;
-        g.stats = P.stats;
-        g.first_part = (int)(first / head_tile_shape(P.z.tile).stat_columns);
+        g.stats = P.pieces > 1 ? P.stats + H.rows : P.stats;
         CAPSCAPS_TRY(launch_head_gemm(g, P.z.tile, P.in_parts ? HEAD_OUT : HEAD_STATS, st));
         if (P.in_parts)
             CAPSCAPS_TRY(run(stats_kernel, blocks_for(H.rows, 1), THREADS, st, H, (const float*)P.logits, P.piece, P.z.splits,
                              H.rows * P.piece, P.stats));
+        if (P.pieces > 1)
+            CAPSCAPS_TRY(run(few ? fold_kernel<1> : fold_kernel<8>, blocks_for(H.rows, few ? 1 : 8), THREADS, st, H, P.stats,
+                             ceil_div(classes, head_tile_shape(P.z.tile).stat_columns), piece > 0));
     }
     const bool vectors = vectors_of(H.x, H.x_stride, H.dtype) && vectors_of(H.weight, H.weight_stride, H.dtype) && H.width % 8 == 0;
     // (the entries' z: where logq goes, or in the workspace)
     float* const picked = logq != nullptr ? logq : P.picked;
     const long long quads = H.rows * ((H.top + 3) / 4);
     CAPSCAPS_TRY(run(quads < 1024 ? pick_kernel<true> : pick_kernel<false>, blocks_for(quads, quads < 1024 ? 1 : 4), THREADS, st, H, picked, vectors));
-    const bool few = H.rows < 512;
     CAPSCAPS_TRY(run(few ? loss_kernel<1> : loss_kernel<8>, blocks_for(H.rows, few ? 1 : 8), THREADS, st, H, (const Stat*)P.stats,
-                     P.stat_parts, (const float*)picked, loss, lse, logq));
+                     P.pieces > 1 ? 1 : P.stat_parts, (const float*)picked, loss, lse, logq));
     return CAPSCAPS_OK;
 }
 
@@ -1011,9 +1045,9 @@ bool make_head(const capscaps_head& A, const capscaps_head_tensors& T, bool dist
         T.index_stride > far)
         return false;
     if (distill) {
-        if (!known_dtype(A.teacher_dtype) || T.teacher_stride < 0 || T.teacher_stride > far) return false;
+        if (T.teacher_stride < 0 || T.teacher_stride > far) return false;
         if (A.rows > 0 && (T.teacher == nullptr || misaligned(T.teacher, element_bytes(A.teacher_dtype)))) return false;
-    } else if (A.top != 1 || A.temperature != 1.0f || T.teacher != nullptr) {
+    } else if (T.teacher != nullptr) {
         return false;
     }
     H = Head{};
@@ -1028,7 +1062,7 @@ bool make_head(const capscaps_head& A, const capscaps_head_tensors& T, bool dist
 int run_forward(const capscaps_head* head, const capscaps_head_fwd_args* args, bool distill, void* workspace,
                 size_t workspace_bytes, void* stream)
 {
-    const int rc = check_head(head);
+    const int rc = check_head(head, distill);
     if (rc != CAPSCAPS_OK) return rc;
     if (args == nullptr) return CAPSCAPS_EINVAL;
     Head H;
@@ -1046,7 +1080,7 @@ int run_forward(const capscaps_head* head, const capscaps_head_fwd_args* args, b
 int run_backward(const capscaps_head* head, const capscaps_head_bwd_args* args, bool distill, void* workspace,
                  size_t workspace_bytes, void* stream)
 {
-    const int rc = check_head(head);
+    const int rc = check_head(head, distill);
     if (rc != CAPSCAPS_OK) return rc;
     if (args == nullptr) return CAPSCAPS_EINVAL;
     Head H;
@@ -1075,11 +1109,11 @@ extern "C" {
 
 size_t capscaps_class_loss_workspace_bytes(const capscaps_head* head, int backward)
 {
-    return check_head(head) == CAPSCAPS_OK ? make_plan(*head, false, backward != 0, nullptr, nullptr).bytes : 0;
+    return check_head(head, false) == CAPSCAPS_OK ? make_plan(*head, false, backward != 0, nullptr, nullptr).bytes : 0;
 }
 size_t capscaps_distill_loss_workspace_bytes(const capscaps_head* head, int backward)
 {
-    return check_head(head) == CAPSCAPS_OK ? make_plan(*head, true, backward != 0, nullptr, nullptr).bytes : 0;
+    return check_head(head, true) == CAPSCAPS_OK ? make_plan(*head, true, backward != 0, nullptr, nullptr).bytes : 0;
 }
 int capscaps_class_loss_fwd(const capscaps_head* head, const capscaps_head_fwd_args* args, void* workspace,
                             size_t workspace_bytes, void* stream)

@@ -138,6 +138,41 @@ def test_several_pieces_of_the_classes(top, dtype):
     Case(4096, 64, 70001, dtype, top=top, bias=True, left=0.1).check()
 
 
+@pytest.mark.parametrize("rows", [40, 129, 200, 257, 600])
+def test_many_classes_in_pieces_with_a_bias(rows):
+    """More classes than a piece may have, rows that end inside a tile: the bias's sums over rows stay within theirs."""
+    c = Case(rows, 8, (1 << 20) + 70, BF16, bias=True)
+    c.index[::3] = torch.arange(len(c.index[::3]), device="cuda")  # (classes of the first piece)
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+def test_one_row_without_axes(dtype):
+    c = Case(1, 64, 130, dtype, top=4)
+    want = c.forward()
+    grads = c.backward(want)
+    r = cc.distill_loss_fwd(c.x[0], c.w, c.index[0], c.teacher[0])
+    g = cc.distill_loss_bwd(c.x[0], c.w, c.index[0], c.teacher[0], r.lse, r.logq, c.dloss[0])
+    assert r.loss.shape == () and torch.equal(r.loss, want.loss[0]) and torch.equal(r.logq, want.logq[0])
+    assert torch.equal(g.dx, grads.dx[0]) and torch.equal(g.dweight, grads.dweight)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32], ids=NAMES.get)
+def test_strided_targets_and_teachers(dtype):
+    c = Case(60, 64, 130, dtype)
+    want = c.forward()
+    wide = torch.full((60, 3), -1, device="cuda")
+    wide[:, 1] = c.index
+    got = cc.class_loss_fwd(c.x, c.w, wide[:, 1])
+    assert torch.equal(got.loss, want.loss)
+    c = Case(60, 64, 130, dtype, top=5)
+    want = c.forward()
+    index, teacher = (torch.zeros((60, 9), dtype=t.dtype, device="cuda") for t in (c.index, c.teacher))
+    index[:, :5], teacher[:, :5] = c.index, c.teacher
+    got = cc.distill_loss_fwd(c.x, c.w, index[:, :5], teacher[:, :5])
+    assert torch.equal(got.loss, want.loss) and torch.equal(got.logq, want.logq)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
 @pytest.mark.parametrize("top", [None, 4])
 def test_rows_left_out(top, dtype):

@@ -98,6 +98,23 @@ def test_workspaces_hold_a_piece_of_the_logits():
         assert cc.capscaps_class_loss_workspace_bytes(large, back) < 4 << 30  # (the logits: 64 GB)
 
 
+@pytest.mark.parametrize("rows,width,classes", [(1 << 20, 8, 1 << 26), (1 << 20, 1 << 20, 256), (1, 1, 1 << 26), (1, 1 << 20, 1 << 20)])
+@pytest.mark.parametrize("dtype", [cc.BF16, cc.FP32])
+def test_the_largest_heads_have_workspaces(rows, width, classes, dtype):
+    for back in (0, 1):
+        need = cc.capscaps_class_loss_workspace_bytes(head(rows=rows, width=width, classes=classes, dtype=dtype), back)
+        x = rows * width * (6 if dtype == cc.FP32 else 2)
+        assert 0 < need < 3 * x + (1 << 30) * 8 + (8 * classes + 8 * width * rows if back else 0) + 4 * rows * width * back
+
+
+def test_workspaces_of_heads_that_are_refused():
+    """A class loss has one entry and no temperature, a teacher's logits a type."""
+    assert cc.capscaps_class_loss_workspace_bytes(head(top=2), 0) == 0
+    assert cc.capscaps_class_loss_workspace_bytes(head(temperature=2.0), 1) == 0
+    assert cc.capscaps_distill_loss_workspace_bytes(head(top=2, teacher_dtype=9), 0) == 0
+    assert cc.capscaps_distill_loss_workspace_bytes(head(top=2, temperature=2.0), 0) > 0
+
+
 def test_structures_have_the_headers_sizes():
     assert ctypes.sizeof(cc.HeadArgs) == 40
     assert ctypes.sizeof(cc.HeadFwdArgs) == 96
