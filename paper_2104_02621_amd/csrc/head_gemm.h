@@ -7,13 +7,16 @@
 namespace capscaps {
 
 constexpr int HEAD_K = 32;        // contracted values of a stage; operands are padded with zeros to a multiple
-constexpr int HEAD_PRODUCTS = 6;  // fp32 operands: products of their bf16 terms
+
+// Terms of a value of the m side, and the products of terms that a contraction is made of: 1; 2, a 16-bit rounding and that of
+// what it leaves over, where the n side has one; 3, fp32 values as bf16 terms on both sides (bf16_split.h)
+inline int head_products(int terms) { return terms == 3 ? 6 : terms; }
 
 // An operand in blocks: 16 rows of a stage, 1 KB, in the order in which they lie in LDS, so that one copy of a wave is one
 // run of memory.  (Copies of 64 bytes from each of 16 rows make half as wide requests of the L2, of which a CU has only so
 // many on their way: a product of 8192 x 2048 x 32768 runs at 700 TFLOP/s so on tiles of 256 x 256, and at 1450 with
 // blocks.)
-// `stages`: those of a row block, the terms of fp32 operands one after another.  Offset of value k of a row, in values:
+// `stages`: those of a row block, the terms one after another.  Offset of value k of a row, in values:
 __host__ __device__ inline long long head_block_at(long long row, long long k, long long stages)
 {
     const long long block = (row >> 4) * stages + (k >> 5);
@@ -42,8 +45,8 @@ struct HeadGemm {
     const int* m_count;        // NULL, or how many of the m rows count, in device memory
     const int* k_count;        // NULL, or how many contracted values count, in device memory
     long long k;
-    int plane_a, plane_b;  // stages of a term of fp32 operands
-    int dtype;
+    int plane_a, plane_b;  // stages of a term
+    int terms, dtype;      // terms of a; fp32: 3
     // HEAD_OUT: fp32 (out_dtype) or 16 bits; parts of the contracted length go to copies `out_split` elements apart
     void* out;
     long long ldo, out_split;
@@ -58,7 +61,7 @@ struct HeadGemm {
     const float *coef, *lse;  // of row m, and of row rows_of[m]
     const int* rows_of;
     unsigned short *gn, *gt;  // rows m and rows n, in blocks of planes_n and planes_t stages a term
-    int planes_n, planes_t;
+    int planes_n, planes_t, grad_terms;
     float* sums;  // NULL, or [m / sum_rows][planes_n * HEAD_K]
 };
 

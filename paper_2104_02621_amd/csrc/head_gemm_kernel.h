@@ -62,7 +62,7 @@ __device__ __forceinline__ void turn(unsigned& lo, unsigned& hi, int lane)
 }
 
 // NB: stages of the ring
-template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, bool ROWS, int END>
+template <typename Tag, int BM, int BN, int NWM, int NB, int TERMS, bool ROWS, int END>
 __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kernel(const HeadGemm G, int tiles_n)
 {
     constexpr int NWN = 4 / NWM, WM = BM / NWM, WN = BN / NWN, TM = WM / 32, TN = WN / 32;
@@ -101,7 +101,8 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
     const int per = __builtin_amdgcn_readfirstlane((all_stages + G.splits - 1) / G.splits);
     const int first = __builtin_amdgcn_readfirstlane(part * per < all_stages ? part * per : all_stages);
     const int run = __builtin_amdgcn_readfirstlane(all_stages - first < per ? all_stages - first : per);  // of each product of terms
-    const int stages = __builtin_amdgcn_readfirstlane(TERMS ? run * HEAD_PRODUCTS : run);
+    constexpr int PRODUCTS = TERMS == 3 ? SPLIT_PRODUCTS : TERMS;
+    const int stages = __builtin_amdgcn_readfirstlane(run * PRODUCTS);
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -139,23 +140,25 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
     // the stage whose copies go out next: byte offsets from a row's beginning (out of range past the last stage)
     int next = 0, product = 0, left = run;
     int a_off = stages > 0 ? first * 1024 : OUT_OF_RANGE, b_off = stages > 0 ? first * step_b : OUT_OF_RANGE;
-    if (TERMS && stages > 0) {
-        a_off += SPLIT_TERM_A[0] * G.plane_a * 1024;
-        b_off += SPLIT_TERM_B[0] * G.plane_b * 1024;
+    // terms of the products, two bits each, smallest products first
+    constexpr int ta = TERMS == 3 ? SPLIT_TERM_A[0] | SPLIT_TERM_A[1] << 2 | SPLIT_TERM_A[2] << 4 | SPLIT_TERM_A[3] << 6 |
+                                        SPLIT_TERM_A[4] << 8 | SPLIT_TERM_A[5] << 10
+                                  : 1;
+    constexpr int tb = TERMS == 3 ? SPLIT_TERM_B[0] | SPLIT_TERM_B[1] << 2 | SPLIT_TERM_B[2] << 4 | SPLIT_TERM_B[3] << 6 |
+                                        SPLIT_TERM_B[4] << 8 | SPLIT_TERM_B[5] << 10
+                                  : 0;
+    if (TERMS > 1 && stages > 0) {
+        a_off += (ta & 3) * G.plane_a * 1024;
+        b_off += (tb & 3) * G.plane_b * 1024;
     }
     auto advance = [&]() {
         // (the empty statements hold the scalar arithmetic in the gap it is written in; where it drifts, the one wave of a SIMD
         // leaves the matrix pipe without work: 8192 x 2048 x 32768 in 1256 instead of 756 us on tiles of 256 x 256)
-        if constexpr (!TERMS) asm volatile("" : "+s"(next), "+s"(a_off), "+s"(b_off));
+        if constexpr (TERMS == 1) asm volatile("" : "+s"(next), "+s"(a_off), "+s"(b_off));
         ++next;
         a_off += 1024;
         b_off += step_b;
-        if constexpr (TERMS) {
-            // (terms of the products, two bits each)
-            constexpr int ta = SPLIT_TERM_A[0] | SPLIT_TERM_A[1] << 2 | SPLIT_TERM_A[2] << 4 | SPLIT_TERM_A[3] << 6 |
-                               SPLIT_TERM_A[4] << 8 | SPLIT_TERM_A[5] << 10;
-            constexpr int tb = SPLIT_TERM_B[0] | SPLIT_TERM_B[1] << 2 | SPLIT_TERM_B[2] << 4 | SPLIT_TERM_B[3] << 6 |
-                               SPLIT_TERM_B[4] << 8 | SPLIT_TERM_B[5] << 10;
+        if constexpr (TERMS > 1) {
             const bool wrap = --left == 0;
             product += wrap ? 1 : 0;
             left = wrap ? run : left;
@@ -166,7 +169,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
         }
         a_off = next < stages ? a_off : OUT_OF_RANGE;
         b_off = next < stages ? b_off : OUT_OF_RANGE;
-        if constexpr (!TERMS) asm volatile("" : "+s"(next), "+s"(a_off), "+s"(b_off));
+        if constexpr (TERMS == 1) asm volatile("" : "+s"(next), "+s"(a_off), "+s"(b_off));
     };
     auto copy_a = [&](auto SLOT, auto J) {
         constexpr int slot = decltype(SLOT)::value, j = decltype(J)::value;
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float z = acc[a][b][4 * g + j];
-                            r[j] = (TERMS ? z * SPLIT_UNSCALE : z) * scale;
+                            r[j] = (TERMS == 3 ? z * SPLIT_UNSCALE : z) * scale;
                         }
                         if (G.accumulate) r += old[q];
                         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(chunk_t, r), rs, voff + q * 32, 0, 0);
@@ -318,7 +321,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
                                 const float z = acc[a][b][r + j];
-                                v[j] = (TERMS ? z * SPLIT_UNSCALE : z) * scale;
+                                v[j] = (TERMS == 3 ? z * SPLIT_UNSCALE : z) * scale;
                             }
                             w[r / 2] = G.out_dtype == CAPSCAPS_FP16 ? half_pair(v[0], v[1]) : round_pair(v[0], v[1]);
                         }
@@ -342,7 +345,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
                     float v[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j)  // (one factor after the other: their product may be too small)
-                        v[j] = (TERMS ? acc[a][b][4 * g + j] * SPLIT_UNSCALE : acc[a][b][4 * g + j]) * scale;
+                        v[j] = (TERMS == 3 ? acc[a][b][4 * g + j] * SPLIT_UNSCALE : acc[a][b][4 * g + j]) * scale;
                     if (vectors && n + 4 <= n_left) {
                         if (G.out_dtype == CAPSCAPS_FP32) {
                             typedef float4v at4 __attribute__((aligned(4)));
@@ -371,7 +374,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
         return;
     }
     // z + bias of the lane's values, in place
-    if (TERMS || G.bias != nullptr)
+    if (TERMS == 3 || G.bias != nullptr)
         static_for<TN * 4>([&](auto Q) {
             constexpr int a = decltype(Q)::value / 4, g = decltype(Q)::value % 4;
             float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -386,7 +389,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float z = acc[a][b][4 * g + j];
-                    acc[a][b][4 * g + j] = (TERMS ? z * SPLIT_UNSCALE : z) + bias[j];
+                    acc[a][b][4 * g + j] = (TERMS == 3 ? z * SPLIT_UNSCALE : z) + bias[j];
                 }
             });
             __builtin_amdgcn_sched_barrier(0);
@@ -430,7 +433,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
         return;
     }
     if constexpr (END == HEAD_GRADIENT) {
-        constexpr int terms = TERMS ? 3 : 1;
+        const int terms = TERMS == 3 ? 3 : G.grad_terms;
         constexpr bool half = std::is_same<Tag, f16_tag>::value;
         float sums[TN * 16];
         static_for<TN * 16>([&](auto Q) { sums[decltype(Q)::value] = 0.0f; });
@@ -453,22 +456,31 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     // (16 bits: the logarithm's base taken into both factors, an error of 2^-24 |lse| and |z|)
-                    v[r] = coef * (TERMS ? expf(__builtin_fmaf(acc[a][b][r], G.inv_tau, -lse))
+                    v[r] = coef * (TERMS == 3 ? expf(__builtin_fmaf(acc[a][b][r], G.inv_tau, -lse))
                                          : __builtin_amdgcn_exp2f(__builtin_fmaf(acc[a][b][r], inv_log2, lse_log2)));
                     if (G.sums != nullptr) sums[a * 16 + r] += row ? v[r] : 0.0f;
-                    if constexpr (TERMS) v[r] *= SPLIT_SCALE;
+                    if constexpr (TERMS == 3) v[r] *= SPLIT_SCALE;
                 }
 #pragma unroll
-                for (int p = 0; p < terms; ++p) {
+                for (int p = 0; p < (TERMS == 3 ? 3 : 2); ++p) {
+                    if (p >= terms) break;
                     unsigned w[8];
 #pragma unroll
                     for (int r = 0; r < 16; r += 2) {
                         w[r / 2] = half ? half_pair(v[r], v[r + 1]) : round_pair(v[r], v[r + 1]);
                         if (!row) w[r / 2] = 0;  // (exp of a bias, with factor 0, may be NaN)
-                        if (p + 1 < terms) {
+                        if constexpr (TERMS == 3) {
                             const bool lo = (w[r / 2] & 0x7f80u) == 0x7f80u, hi = (w[r / 2] & 0x7f800000u) == 0x7f800000u;
                             v[r] = lo ? 0.0f : v[r] - low_half(w[r / 2]);
                             v[r + 1] = hi ? 0.0f : v[r + 1] - high_half(w[r / 2]);
+                        } else if (p == 0 && terms > 1) {
+                            // (what is not finite: NaN in the second term too, as in the sums)
+                            if constexpr (half) {
+                                const half2v u = __builtin_bit_cast(half2v, w[r / 2]);
+                                v[r] -= (float)u[0], v[r + 1] -= (float)u[1];
+                            } else {
+                                v[r] -= low_half(w[r / 2]), v[r + 1] -= high_half(w[r / 2]);
+                            }
                         }
                     }
 #pragma unroll
@@ -508,7 +520,7 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
     }
 }
 
-template <typename Tag, int BM, int BN, int NWM, int NB, bool TERMS, bool ROWS, int END>
+template <typename Tag, int BM, int BN, int NWM, int NB, int TERMS, bool ROWS, int END>
 hipError_t launch(HeadGemm g, hipStream_t st)
 {
     const int size = g.out_dtype == CAPSCAPS_FP32 ? 4 : 2;
@@ -528,13 +540,16 @@ hipError_t launch(HeadGemm g, hipStream_t st)
 template <int BM, int BN, int NWM, int NB, int END>
 hipError_t launch_type(const HeadGemm& g, hipStream_t st)
 {
-    if (g.dtype == CAPSCAPS_FP32) return launch<bf16_tag, BM, BN, NWM, NB, true, false, END>(g, st);
-    if (g.stages_b == 0) {
-        if (g.dtype == CAPSCAPS_BF16) return launch<bf16_tag, BM, BN, NWM, NB, false, true, END>(g, st);
-        return launch<f16_tag, BM, BN, NWM, NB, false, true, END>(g, st);
+    if (g.terms == 3) return launch<bf16_tag, BM, BN, NWM, NB, 3, false, END>(g, st);
+    const bool bf16 = g.dtype == CAPSCAPS_BF16;
+    if constexpr (END == HEAD_OUT && BM < 256) {  // (few rows: the plan takes small tiles)
+        if (g.terms == 2)
+            return bf16 ? launch<bf16_tag, BM, BN, NWM, NB, 2, false, END>(g, st) : launch<f16_tag, BM, BN, NWM, NB, 2, false, END>(g, st);
     }
-    if (g.dtype == CAPSCAPS_BF16) return launch<bf16_tag, BM, BN, NWM, NB, false, false, END>(g, st);
-    return launch<f16_tag, BM, BN, NWM, NB, false, false, END>(g, st);
+    if (g.terms != 1) return hipErrorInvalidValue;
+    if (g.stages_b == 0)
+        return bf16 ? launch<bf16_tag, BM, BN, NWM, NB, 1, true, END>(g, st) : launch<f16_tag, BM, BN, NWM, NB, 1, true, END>(g, st);
+    return bf16 ? launch<bf16_tag, BM, BN, NWM, NB, 1, false, END>(g, st) : launch<f16_tag, BM, BN, NWM, NB, 1, false, END>(g, st);
 }
 
 template <int BM, int BN, int NWM, int NB>

@@ -9,7 +9,8 @@
 // z is T x V values, far more than x and W for many classes; it is computed by pieces of the classes, once in each
 // direction, and never kept whole.  A piece of g is rounded to the operands' 16 bits (fp32: three bf16 terms) for the
 // two products that read it, which takes a relative error of half a step to each term of sums over classes or rows, as the storage type of a
-// gradient anywhere else does.  It is scaled by the power of two that brings the largest row's dloss to 2^13, so that fp16, whose
+// gradient anywhere else does.  Where rows are few (up to 256) a row of dx or dweight hangs on one or two values of g and their error
+// would be that row's: g is two terms there, the rounding and that of what it leaves over.  It is scaled by the power of two that brings the largest row's dloss to 2^13, so that fp16, whose
 // smallest step is 2^-24, holds shares down to 1e-11 of it.
 //
 // Rows that are left out (no class for a target, no entry) take no part at all: the rows that are kept are counted and gathered on
@@ -28,6 +29,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MOST_TOP = 1024;
+constexpr int FEW_ROWS = 256;  // whose gradients are two terms of 16 bits
 // (256 rows of an operand are within a signed 32-bit offset: rows of up to 2^20 values of three terms)
 constexpr long long MOST_ROWS = 1 << 20, MOST_PIECE = 1 << 20;
 constexpr long long MOST_TILES = 1 << 23;  // of a launch
@@ -195,6 +197,32 @@ __device__ __forceinline__ void put_operand(unsigned short* to, long long row, l
         for (int p = 0; p < 3; ++p) {
             chunk_t c;
             __builtin_memcpy(&c, t[p], 16);
+            *reinterpret_cast<chunk_t*>(to + p * stages * 512) = c;
+        }
+    }
+}
+
+// Eight gradients as an operand of `terms` (16 bits: 1 or 2; fp32: 3)
+template <bool TERMS>
+__device__ __forceinline__ void put_gradients(unsigned short* to, long long row, long long k, long long stages, int terms, int dtype,
+                                              const float* f)
+{
+    unsigned short raw[8];
+    if constexpr (TERMS) {
+        put_operand<true>(to, row, k, stages, raw, f);
+    } else {
+        to += head_block_at(row, k, terms * stages);
+        float left[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) left[j] = f[j];
+        for (int p = 0; p < terms; ++p) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                raw[j] = round_to_16(left[j], dtype == CAPSCAPS_FP16 ? 2 : 1);
+                left[j] -= dtype == CAPSCAPS_FP16 ? Element<CAPSCAPS_FP16>::get(raw[j]) : Element<CAPSCAPS_BF16>::get(raw[j]);
+            }
+            chunk_t c;
+            __builtin_memcpy(&c, raw, 16);
             *reinterpret_cast<chunk_t*>(to + p * stages * 512) = c;
         }
     }
@@ -527,7 +555,7 @@ template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* lse, const float* z, long long ldz, int splits,
                                                            long long split, long long first, int classes, unsigned short* gn,
                                                            int padded_classes, unsigned short* gt, long long padded_rows,
-                                                           float* sums)
+                                                           int terms, float* sums)
 {
     __shared__ float tile[64][65];
     const float inv = 1.0f / H.tau;
@@ -563,17 +591,13 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
             const bool across_rows = t >= 64 * 8;
             const int a = (t & 511) >> 3, k = (t & 7) * 8;
             float f[8];
-            unsigned short raw[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                f[j] = across_rows ? tile[k + j][a] : tile[a][k + j];
-                if constexpr (!TERMS) raw[j] = round_to_16(f[j], H.dtype == CAPSCAPS_FP16 ? 2 : 1);
-            }
+            for (int j = 0; j < 8; ++j) f[j] = across_rows ? tile[k + j][a] : tile[a][k + j];
             if (across_rows) {
                 if (c0 + a < classes && i0 + k < padded_rows)
-                    put_operand<TERMS>(gt, c0 + a, i0 + k, padded_rows / HEAD_K, raw, f);
+                    put_gradients<TERMS>(gt, c0 + a, i0 + k, padded_rows / HEAD_K, terms, H.dtype, f);
             } else if (i0 + a < kept && c0 + k < padded_classes) {
-                put_operand<TERMS>(gn, i0 + a, c0 + k, padded_classes / HEAD_K, raw, f);
+                put_gradients<TERMS>(gn, i0 + a, c0 + k, padded_classes / HEAD_K, terms, H.dtype, f);
             }
         }
         if (sums != nullptr && threadIdx.x < 64 && c0 + threadIdx.x < classes) {
@@ -591,9 +615,9 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* loss, const float* logq, long long first,
                                                           int classes, unsigned short* gn, int padded_classes,
-                                                          unsigned short* gt, long long padded_rows, long long* taken)
+                                                          unsigned short* gt, long long padded_rows, int terms, long long* taken)
 {
-    const int lane = threadIdx.x & 63, terms = TERMS ? 3 : 1;
+    const int lane = threadIdx.x & 63;
     const long long kept = *H.count;
     for (long long i = blockIdx.x * 4ll + (threadIdx.x >> 6); i < kept; i += gridDim.x * 4ll) {
         const long long r = H.rows_of[i];
@@ -621,9 +645,12 @@ __global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* l
                 v[2] = round_to_16(r1 - low_half(v[1]), 1);
             } else {
                 v[0] = round_to_16(g, H.dtype == CAPSCAPS_FP16 ? 2 : 1);
+                v[1] = round_to_16(g - (H.dtype == CAPSCAPS_FP16 ? Element<CAPSCAPS_FP16>::get(v[0]) : Element<CAPSCAPS_BF16>::get(v[0])),
+                                   H.dtype == CAPSCAPS_FP16 ? 2 : 1);
             }
 #pragma unroll
-            for (int p = 0; p < (TERMS ? 3 : 1); ++p) {
+            for (int p = 0; p < (TERMS ? 3 : 2); ++p) {
+                if (p >= terms) break;
                 gn[head_block_at(i, c, terms * (padded_classes / HEAD_K)) + p * (padded_classes / HEAD_K) * 512ll] = v[p];
                 gt[head_block_at(c, i, terms * (padded_rows / HEAD_K)) + p * (padded_rows / HEAD_K) * 512] = v[p];
             }
@@ -701,11 +728,12 @@ struct Pick {
 };
 Pick pick_tile(long long m, long long n, long long k, int terms, bool may_split, double part_us)
 {
-    const long long stages = std::max<long long>(1, (k + HEAD_K - 1) / HEAD_K) * (terms > 1 ? HEAD_PRODUCTS : 1);
+    const long long stages = std::max<long long>(1, (k + HEAD_K - 1) / HEAD_K) * head_products(terms);
     Pick best{HEAD_TILE_128, 1};
     double least = 1e300;
     for (const int tile : {HEAD_TILE_256, HEAD_TILE_128, HEAD_TILE_FEW_ROWS}) {
         const HeadTileShape s = head_tile_shape(tile);
+        if (terms == 2 && tile == HEAD_TILE_256) continue;  // (not built)
         const double tiles = (double)((m + s.m - 1) / s.m) * (double)((n + s.n - 1) / s.n);
         const double slots = 256.0 * s.per_cu;
         // time of a stage of as many tiles as a CU holds, and stages' time to begin and end
@@ -750,6 +778,7 @@ struct Layout {
 
 struct Plan {
     int terms, padded;  // terms of an operand's value, contracted width
+    int grad_terms;     // ... of a gradient
     bool in_parts;      // logits in parts: few enough to lie in memory
     long long piece;    // classes of a piece
     int pieces, stat_parts;
@@ -777,11 +806,12 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     Plan P{};
     P.distill = distill, P.backward = backward;
     P.terms = A.dtype == CAPSCAPS_FP32 ? 3 : 1;
+    P.grad_terms = P.terms == 3 ? 3 : A.rows <= FEW_ROWS ? 2 : 1;
     P.padded = (int)round_up(A.width, HEAD_K);
     P.padded_rows = round_up(std::max<long long>(A.rows, 1), HEAD_K);
     const long long rows = std::max<long long>(A.rows, 1);
     // a piece's weights as operands, and its gradients
-    const long long per_class = 2ll * P.terms * std::max<long long>(P.padded, backward ? rows : 0);
+    const long long per_class = 2ll * std::max<long long>(P.terms * P.padded, backward ? P.grad_terms * rows : 0);
     P.piece = std::max<long long>(256, std::min(MOST_PIECE, PIECE_BYTES / per_class / 256 * 256));
     P.piece = std::min(P.piece, MOST_TILES / ((rows + 255) / 256) * 256);  // (a launch of tiles of 256 x 256)
     P.piece = std::min<long long>(round_up(A.classes, HEAD_K), P.piece);
@@ -812,14 +842,14 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
         return P;
     }
     W.coef = L.take<float>(A.rows);
-    P.dx = pick_tile(rows, A.width, P.piece, P.terms, P.pieces == 1, 0.0);  // (several: added up piece after piece)
-    P.dw = pick_tile(most, A.width, rows, P.terms, true, 3.0);
+    P.dx = pick_tile(rows, A.width, P.piece, P.grad_terms, P.pieces == 1, 0.0);  // (several: added up piece after piece)
+    P.dw = pick_tile(most, A.width, rows, P.grad_terms, true, 3.0);
     const long long ld = round_up(A.width, 4);
     const long long row_stages = P.terms * P.padded_rows / HEAD_K, class_stages = P.terms * round_up(P.piece, HEAD_K) / HEAD_K;
     P.xt = L.take<unsigned short>(head_block_values(A.width, row_stages));
     P.wt = L.take<unsigned short>(head_block_values(A.width, class_stages));
-    P.gn = L.take<unsigned short>(head_block_values(rows, class_stages));
-    P.gt = L.take<unsigned short>(head_block_values(most, row_stages));
+    P.gn = L.take<unsigned short>(head_block_values(rows, class_stages / P.terms * P.grad_terms));
+    P.gt = L.take<unsigned short>(head_block_values(most, row_stages / P.terms * P.grad_terms));
     P.dx_sums = L.take<float>(rows * ld * P.dx.splits);
     P.dw_sums = P.dw.splits > 1 ? L.take<float>(most * ld * P.dw.splits) : nullptr;
     P.bias_sums = L.take<float>((rows + 63) / 64 * P.piece);
@@ -901,6 +931,7 @@ int logits_of(const Head& H, const Plan& P, long long first, long long classes, 
                                      g.b == P.w ? P.w : nullptr, st));
     g.m_rows = H.rows, g.n_rows = classes, g.m_count = H.count, g.k = H.width;
     g.plane_a = g.plane_b = stages;
+    g.terms = P.terms;
     g.dtype = H.dtype, g.splits = P.z.splits;
     if (P.in_parts) {
         g.out = P.logits, g.ldo = P.piece, g.out_split = H.rows * P.piece, g.out_dtype = CAPSCAPS_FP32;
@@ -965,14 +996,15 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
             CAPSCAPS_TRY(launch_head_gemm(z, P.z.tile, HEAD_OUT, st));
             const long long tiles = (P.padded_rows + 63) / 64 * ((padded + 63) / 64);
             CAPSCAPS_TRY(run(gradient_kernel<TERMS>, blocks_for(tiles, 1), THREADS, st, H, G.lse, (const float*)P.logits, P.piece,
-                             P.z.splits, H.rows * P.piece, first, (int)classes, P.gn, padded, P.gt, P.padded_rows, sums));
+                             P.z.splits, H.rows * P.piece, first, (int)classes, P.gn, padded, P.gt, P.padded_rows, P.grad_terms, sums));
         } else {
             z.coef = H.coef, z.lse = G.lse, z.rows_of = H.rows_of;
             z.gn = P.gn, z.gt = P.gt, z.planes_n = padded / HEAD_K, z.planes_t = (int)(P.padded_rows / HEAD_K), z.sums = sums;
+            z.grad_terms = P.grad_terms;
             CAPSCAPS_TRY(launch_head_gemm(z, P.z.tile, HEAD_GRADIENT, st));
         }
         CAPSCAPS_TRY(run(entries_kernel<TERMS>, blocks_for(H.rows, 4), THREADS, st, H, G.loss, G.logq, first, (int)classes, P.gn,
-                         padded, P.gt, P.padded_rows, G.dbias != nullptr ? P.taken : nullptr));
+                         padded, P.gt, P.padded_rows, P.grad_terms, G.dbias != nullptr ? P.taken : nullptr));
         if (G.dbias != nullptr)
             CAPSCAPS_TRY(run(bias_kernel, (unsigned)((classes + THREADS - 1) / THREADS), THREADS, st, H, (const float*)P.bias_sums, padded,
                              P.in_parts ? 64 : head_tile_shape(P.z.tile).sum_rows,
@@ -980,8 +1012,8 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
         if (G.dx != nullptr) {
             HeadGemm g{};
             g.a = P.gn, g.b = P.wt;
-            g.plane_a = g.plane_b = padded / HEAD_K;
-            g.stages_a = g.stages_b = P.terms * g.plane_a;
+            g.plane_a = g.plane_b = padded / HEAD_K, g.terms = P.grad_terms;
+            g.stages_a = (long long)P.grad_terms * g.plane_a, g.stages_b = (long long)P.terms * g.plane_b;
             g.m_rows = H.rows, g.n_rows = H.width, g.m_count = H.count, g.k = classes;
             g.dtype = H.dtype, g.out = P.dx_sums, g.ldo = ld, g.out_split = H.rows * ld, g.out_dtype = CAPSCAPS_FP32;
             g.splits = P.dx.splits, g.accumulate = piece > 0;
@@ -991,8 +1023,8 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
             char* out = static_cast<char*>(G.dweight) + first * H.width * size;
             HeadGemm g{};
             g.a = P.gt, g.b = P.xt;
-            g.plane_a = g.plane_b = (int)(P.padded_rows / HEAD_K);
-            g.stages_a = g.stages_b = P.terms * g.plane_a;
+            g.plane_a = g.plane_b = (int)(P.padded_rows / HEAD_K), g.terms = P.grad_terms;
+            g.stages_a = (long long)P.grad_terms * g.plane_a, g.stages_b = (long long)P.terms * g.plane_b;
             g.m_rows = classes, g.n_rows = H.width, g.k = H.rows, g.k_count = H.count;
             g.dtype = H.dtype, g.splits = P.dw.splits;
             const bool direct = P.dw.splits == 1;

@@ -90,10 +90,12 @@ class Head:
         whole = 2.0 ** -37 * coef.abs().max()
         dbias, edbias = g.sum(0), (eg + 80 * U * (coef * q).abs() + whole).sum(0) + 2 * U * g.sum(0).abs()
         low = 2.0 ** -38 * coef.abs().max() if self.dtype == torch.float16 else 0.0  # (fp16's smallest step, scaled)
-        eg = eg + HALF[self.dtype] * (g.abs() + eg) + torch.where(self.row[:, None], low, 0.0)
+        # up to 256 rows of 16 bits: a rounding and that of what it leaves over, and sums of twice as many products
+        terms = 2 if len(q) <= 256 and self.dtype in (torch.bfloat16, torch.float16) else 1
+        eg = eg + HALF[self.dtype] ** terms * (g.abs() + eg) + torch.where(self.row[:, None], low, 0.0)
         dx, dw = g @ self.w, g.T @ self.x
-        edx = eg @ self.w.abs() + gamma(q.shape[1], self.dtype) * (g.abs() @ self.w.abs())
-        edw = eg.T @ self.x.abs() + gamma(len(q), self.dtype) * (g.abs().T @ self.x.abs())
+        edx = eg @ self.w.abs() + gamma(terms * q.shape[1], self.dtype) * (g.abs() @ self.w.abs())
+        edw = eg.T @ self.x.abs() + gamma(terms * len(q), self.dtype) * (g.abs().T @ self.x.abs())
 
         def stored(v, e):
             return e + HALF[self.dtype] * (v.abs() + e) + TINY[self.dtype]
