@@ -446,7 +446,6 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
             const long long m = m0 + wm * WM + b * 32 + lr;
             const bool row = m < m_end;
             const float lse = row ? G.lse[G.rows_of[m]] : 0.0f, coef = row ? G.coef[m] : 0.0f;
-            const float inv_log2 = G.inv_tau * 1.44269504f, lse_log2 = lse * -1.44269504f;
             // row m at the wave's first class, without its chunk; stage of these 32 rows in gt
             unsigned short* const gn = G.gn + ((m >> 4) * sn + ((n0 + wn * WN) >> 5)) * 512 + (m & 15) * 32;
             const long long stage_t = (m0 + wm * WM + b * 32) >> 5;
@@ -455,9 +454,8 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
                 float v[16];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    // (16 bits: the logarithm's base taken into both factors, an error of 2^-24 |lse| and |z|)
-                    v[r] = coef * (TERMS == 3 ? expf(__builtin_fmaf(acc[a][b][r], G.inv_tau, -lse))
-                                         : __builtin_amdgcn_exp2f(__builtin_fmaf(acc[a][b][r], inv_log2, lse_log2)));
+                    const float l = __builtin_fmaf(acc[a][b][r], G.inv_tau, -lse);
+                    v[r] = coef * (TERMS == 3 ? expf(l) : __expf(l));
                     if (G.sums != nullptr) sums[a * 16 + r] += row ? v[r] : 0.0f;
                     if constexpr (TERMS == 3) v[r] *= SPLIT_SCALE;
                 }

@@ -8,10 +8,11 @@
 //
 // z is T x V values, far more than x and W for many classes; it is computed by pieces of the classes, once in each
 // direction, and never kept whole.  A piece of g is rounded to the operands' 16 bits (fp32: three bf16 terms) for the
-// two products that read it, which takes a relative error of half a step to each term of sums over classes or rows, as the storage type of a
-// gradient anywhere else does.  Where rows are few (up to 256) a row of dx or dweight hangs on one or two values of g and their error
-// would be that row's: g is two terms there, the rounding and that of what it leaves over.  It is scaled by the power of two that brings the largest row's dloss to 2^13, so that fp16, whose
-// smallest step is 2^-24, holds shares down to 1e-11 of it.
+// two products that read it, which takes a relative error of half a step to each term of sums over classes or rows, as
+// the storage type of a gradient anywhere else does.  Where rows or classes are few (up to 256) a row of dweight or dx
+// hangs on few values of g, whose error would be that row's: g is two terms there, the rounding and that of what it
+// leaves over.  It is scaled so that the largest row's dloss is 2^13 to 2^14: fp16, whose smallest step is 2^-24, then
+// holds shares down to 1e-11 of it.
 //
 // Rows that are left out (no class for a target, no entry) take no part at all: the rows that are kept are counted and gathered on
 // the device first, and the products run over these.  So what stands in the others does not matter, and they cost nothing.
@@ -29,7 +30,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MOST_TOP = 1024;
-constexpr int FEW_ROWS = 256;  // whose gradients are two terms of 16 bits
+constexpr int FEW = 256;  // rows or classes whose gradients are two terms of 16 bits
 // (256 rows of an operand are within a signed 32-bit offset: rows of up to 2^20 values of three terms)
 constexpr long long MOST_ROWS = 1 << 20, MOST_PIECE = 1 << 20;
 constexpr long long MOST_TILES = 1 << 23;  // of a launch
@@ -115,8 +116,8 @@ __global__ void __launch_bounds__(THREADS) teacher_kernel(Head H)
     }
 }
 
-// The rows that are kept, in their order: rows_of[i], pos[row] (-1: left out), count[0]; coef[i] = dloss tau 2^e, count[1] the
-// bits of 2^-e.  One workgroup.
+// The rows that are kept, in their order: rows_of[i], pos[row] (-1: left out), count[0]; coef[i] = dloss tau times a scale,
+// count[1] the bits of one over it.  One workgroup.
 __global__ void __launch_bounds__(1024) rows_kernel(Head H, const float* dloss, long long dloss_stride)
 {
     __shared__ int sums[16];
@@ -140,13 +141,19 @@ __global__ void __launch_bounds__(1024) rows_kernel(Head H, const float* dloss, 
         __syncthreads();
         top = 0.0f;
         for (int k = 0; k < 16; ++k) top = __builtin_fmaxf(top, tops[k]);
-        int e = 0;
-        if (top > 0.0f && top <= 3.4e38f) {
-            e = 127 + 13 - (int)(__builtin_bit_cast(unsigned, top) >> 23);
+        float back = 1.0f;
+        if (top >= 1e-33f && top <= 3.4e38f && H.dtype != CAPSCAPS_FP32) {
+            // just below 2^14: the values that weigh most, those of the largest dloss at an entry of a row that has not been
+            // learnt, then have the longest mantissas, whose rounding is half that of the shortest
+            scale = 16352.0f / top;
+            back = top * (1.0f / 16352.0f);
+        } else if (top > 0.0f && top <= 3.4e38f) {
+            int e = 127 + 13 - (int)(__builtin_bit_cast(unsigned, top) >> 23);
             e = e > 126 ? 126 : e;
+            scale = __builtin_bit_cast(float, (unsigned)(127 + e) << 23);
+            back = __builtin_bit_cast(float, (unsigned)(127 - e) << 23);
         }
-        scale = __builtin_bit_cast(float, (unsigned)(127 + e) << 23);
-        if (threadIdx.x == 0) H.count[1] = (127 - e) << 23;
+        if (threadIdx.x == 0) H.count[1] = __builtin_bit_cast(int, back);
     }
     int before = 0;
     for (long long at = 0; at < H.rows; at += 1024) {
@@ -580,7 +587,7 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
                 for (int j = 0; j < 4; ++j) {
                     if (H.bias != nullptr && c + j < classes) v[j] += H.bias[first + c + j];
                     const float l = __builtin_fmaf(v[j], inv, -all);
-                    g[j] = c + j < classes ? coef * (TERMS ? expf(l) : __expf(l)) : 0.0f;
+                    g[j] = c + j < classes ? coef * expf(l) : 0.0f;
                 }
             }
 #pragma unroll
@@ -680,7 +687,7 @@ __global__ void __launch_bounds__(THREADS) bias_kernel(Head H, const float* sums
     dbias[first + c] = (float)(s * __builtin_bit_cast(float, H.count[1]));
 }
 
-// out[r][c] = 2^-e sum of `splits` parts of sums[pos[r]][c] (pos NULL: r), 0 where a row is left out
+// out[r][c] = one over the scale times the sum of `splits` parts of sums[pos[r]][c] (pos NULL: r), 0 where a row is left out
 __global__ void __launch_bounds__(THREADS) finish_kernel(const int* count, const int* pos, const float* sums, long long ld, int splits,
                                                          long long split, long long rows, int columns, void* out, int dtype)
 {
@@ -806,7 +813,7 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     Plan P{};
     P.distill = distill, P.backward = backward;
     P.terms = A.dtype == CAPSCAPS_FP32 ? 3 : 1;
-    P.grad_terms = P.terms == 3 ? 3 : A.rows <= FEW_ROWS ? 2 : 1;
+    P.grad_terms = P.terms == 3 ? 3 : A.rows <= FEW || A.classes <= FEW ? 2 : 1;
     P.padded = (int)round_up(A.width, HEAD_K);
     P.padded_rows = round_up(std::max<long long>(A.rows, 1), HEAD_K);
     const long long rows = std::max<long long>(A.rows, 1);

@@ -90,8 +90,8 @@ class Head:
         whole = 2.0 ** -37 * coef.abs().max()
         dbias, edbias = g.sum(0), (eg + 80 * U * (coef * q).abs() + whole).sum(0) + 2 * U * g.sum(0).abs()
         low = 2.0 ** -38 * coef.abs().max() if self.dtype == torch.float16 else 0.0  # (fp16's smallest step, scaled)
-        # up to 256 rows of 16 bits: a rounding and that of what it leaves over, and sums of twice as many products
-        terms = 2 if len(q) <= 256 and self.dtype in (torch.bfloat16, torch.float16) else 1
+        # up to 256 rows or classes in 16 bits: a rounding and that of what it leaves over, and sums of twice as many products
+        terms = 2 if min(q.shape) <= 256 and self.dtype in (torch.bfloat16, torch.float16) else 1
         eg = eg + HALF[self.dtype] ** terms * (g.abs() + eg) + torch.where(self.row[:, None], low, 0.0)
         dx, dw = g @ self.w, g.T @ self.x
         edx = eg @ self.w.abs() + gamma(terms * q.shape[1], self.dtype) * (g.abs() @ self.w.abs())
