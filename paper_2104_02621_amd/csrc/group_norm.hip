@@ -803,7 +803,11 @@ GroupPlan group_plan(const capscaps_group_norm& G)
         while (threads > 64 && threads / 2 >= vecs && ceil_div(G.positions, threads / 2 / vecs) <= aim) threads /= 2;
         const int rows = threads / (int)vecs;
         const int items = resident_items<FORWARD>(v, widest, ceil_div(G.positions, rows));
-        if (items > 0) {
+        // Where vectors straddle groups, a slab that takes a CU's registers for itself waits for its sums by columns alone: 64
+        // images of 1024 positions of 32 groups of 30 columns take 144 us in fp32 and 92 in bf16, in two passes 120 and 73;
+        // with half the positions, two slabs a CU, 71 and 42, in two passes 65 and 46.
+        const bool alone = FORWARD && !few && columns % v != 0 && threads * items > RESIDENT * 8;
+        if (items > 0 && !alone) {
             P.v = v, P.items = items, P.threads = threads, P.rows = rows, P.vecs = (int)vecs, P.slab = (int)wide;
             P.whole = k, P.parts = 1, P.slabs = G.groups / k, P.fold = columns % v == 0 ? v : 1;
             // (backward: a workgroup takes one image after the other, and as many lanes as the registers of a CU hold are at work)
