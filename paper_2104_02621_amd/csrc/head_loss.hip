@@ -402,66 +402,71 @@ __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, 
     }
 }
 
-// picked[row][k] = z of the rows' entries (0 where they do not count), from the operands in fp32.  A wave for four entries of a
-// row at a time: what it waits for is the weights' rows, which lie anywhere.  Where there are few, the four waves of a workgroup (WIDE).
+// z of entries k0 to k0 + 3 of row r (0 where they do not count), from the operands in fp32: to picked[r][k].  By a wave, or where there are
+// few by a workgroup (LANES); what it waits for is the weights' rows, which lie anywhere.
+template <int LANES>
+__device__ __forceinline__ void pick_entries(const Head& H, long long r, int k0, float* picked, bool vectors, float (*parts)[4])
+{
+    const int lane = threadIdx.x & (LANES - 1);
+    long long cls[4];
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) cls[j] = k0 + j < H.top ? index_of(H, r, k0 + j) : -1;
+    const long long xa = r * H.x_stride;
+    if (vectors && H.dtype != CAPSCAPS_FP32) {
+        const unsigned short *x = static_cast<const unsigned short*>(H.x) + xa, *w = static_cast<const unsigned short*>(H.weight);
+#pragma unroll 2
+        for (int c = lane * 8; c < H.width; c += LANES * 8) {
+            const chunk_t a = *reinterpret_cast<const chunk_t*>(x + c);
+            chunk_t b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (cls[j] >= 0) b[j] = *reinterpret_cast<const chunk_t*>(w + cls[j] * H.weight_stride + c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (cls[j] >= 0)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (H.dtype == CAPSCAPS_BF16) {
+                            s[j] = __builtin_fmaf(low_half(a[q]), low_half(b[j][q]), s[j]);
+                            s[j] = __builtin_fmaf(high_half(a[q]), high_half(b[j][q]), s[j]);
+                        } else {
+                            const half2v u = __builtin_bit_cast(half2v, (unsigned)a[q]), v = __builtin_bit_cast(half2v, (unsigned)b[j][q]);
+                            s[j] = __builtin_fmaf((float)u[0], (float)v[0], s[j]);
+                            s[j] = __builtin_fmaf((float)u[1], (float)v[1], s[j]);
+                        }
+                    }
+        }
+    } else {
+        for (int c = lane; c < H.width; c += LANES) {
+            const float a = load_element(H.x, xa + c, H.dtype);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (cls[j] >= 0) s[j] = __builtin_fmaf(a, load_element(H.weight, cls[j] * H.weight_stride + c, H.dtype), s[j]);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        s[j] = lanes_sum(s[j], 64);
+        if constexpr (LANES > 64) {
+            if ((lane & 63) == 0) parts[lane >> 6][j] = s[j];
+            __syncthreads();
+            s[j] = (parts[0][j] + parts[1][j]) + (parts[2][j] + parts[3][j]);
+        }
+        if (cls[j] >= 0 && H.bias != nullptr) s[j] += H.bias[cls[j]];
+        if (lane == 0 && k0 + j < H.top) picked[r * H.top + k0 + j] = s[j];
+    }
+}
+
+// ... of all rows that are kept
 template <bool WIDE>
 __global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bool vectors)
 {
     constexpr int LANES = WIDE ? THREADS : 64, PER = THREADS / LANES;
     __shared__ float parts[4][4];
-    const int lane = threadIdx.x & (LANES - 1);
     const long long kept = *H.count, quads = (H.top + 3) / 4;
     for (long long t = blockIdx.x * (long long)PER + threadIdx.x / LANES; t < kept * quads; t += gridDim.x * (long long)PER) {
-        const long long r = H.rows_of[t / quads];
-        const int k0 = (int)(t % quads) * 4;
-        long long cls[4];
-        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) cls[j] = k0 + j < H.top ? index_of(H, r, k0 + j) : -1;
-        const long long xa = r * H.x_stride;
-        if (vectors && H.dtype != CAPSCAPS_FP32) {
-            const unsigned short *x = static_cast<const unsigned short*>(H.x) + xa, *w = static_cast<const unsigned short*>(H.weight);
-#pragma unroll 2
-            for (int c = lane * 8; c < H.width; c += LANES * 8) {
-                const chunk_t a = *reinterpret_cast<const chunk_t*>(x + c);
-                chunk_t b[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (cls[j] >= 0) b[j] = *reinterpret_cast<const chunk_t*>(w + cls[j] * H.weight_stride + c);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (cls[j] >= 0)
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            if (H.dtype == CAPSCAPS_BF16) {
-                                s[j] = __builtin_fmaf(low_half(a[q]), low_half(b[j][q]), s[j]);
-                                s[j] = __builtin_fmaf(high_half(a[q]), high_half(b[j][q]), s[j]);
-                            } else {
-                                const half2v u = __builtin_bit_cast(half2v, (unsigned)a[q]), v = __builtin_bit_cast(half2v, (unsigned)b[j][q]);
-                                s[j] = __builtin_fmaf((float)u[0], (float)v[0], s[j]);
-                                s[j] = __builtin_fmaf((float)u[1], (float)v[1], s[j]);
-                            }
-                        }
-            }
-        } else {
-            for (int c = lane; c < H.width; c += LANES) {
-                const float a = load_element(H.x, xa + c, H.dtype);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (cls[j] >= 0) s[j] = __builtin_fmaf(a, load_element(H.weight, cls[j] * H.weight_stride + c, H.dtype), s[j]);
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            s[j] = lanes_sum(s[j], 64);
-            if constexpr (WIDE) {
-                if ((lane & 63) == 0) parts[lane >> 6][j] = s[j];
-                __syncthreads();
-                s[j] = (parts[0][j] + parts[1][j]) + (parts[2][j] + parts[3][j]);
-            }
-            if (cls[j] >= 0 && H.bias != nullptr) s[j] += H.bias[cls[j]];
-            if (lane == 0 && k0 + j < H.top) picked[r * H.top + k0 + j] = s[j];
-        }
+        pick_entries<LANES>(H, H.rows_of[t / quads], (int)(t % quads) * 4, picked, vectors, parts);
         if constexpr (WIDE) __syncthreads();
     }
 }
@@ -500,15 +505,17 @@ __global__ void __launch_bounds__(THREADS) fold_kernel(Head H, Stat* stats, int 
     }
 }
 
-// loss, lse, logq of all rows, from stats[part][i] and the entries' z (which logq takes the place of, where it is wanted).
+// loss, lse, logq of all rows, from stats[part][i] and the entries' z (which logq takes the place of, where it is wanted; PICK: and
+// are computed here, of rows with four entries at most, which spares a launch).
 // A workgroup for ROWS of the rows that are kept, and for the zeros of as many that are not (eight: whole 64-byte pieces of a
 // part's statistics; one where rows are few).
-template <int ROWS>
-__global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int parts, const float* picked, float* loss,
+template <int ROWS, bool PICK>
+__global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int parts, float* picked, bool vectors, float* loss,
                                                        float* lse, float* logq)
 {
+    static_assert(ROWS == 1 || !PICK);
     __shared__ Stat joined[4][ROWS];
-    __shared__ float lses[ROWS], sums[4][ROWS];
+    __shared__ float lses[ROWS], sums[4][ROWS], products[4][4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float inv = 1.0f / H.tau;
     const int kept = *H.count;
@@ -522,6 +529,7 @@ __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats
         }
         if (i0 >= kept) continue;
         const int rows = kept - i0 < ROWS ? (int)(kept - i0) : ROWS;
+        if constexpr (PICK) pick_entries<THREADS>(H, H.rows_of[i0], 0, picked, vectors, products);
         const Stat s = join_parts<ROWS>(stats, H.rows, parts, i0, rows, joined);
         if (threadIdx.x < ROWS) {
             lses[lane] = s.top + logf(s.sum);
@@ -973,9 +981,11 @@ int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, 
     // (the entries' z: where logq goes, or in the workspace)
     float* const picked = logq != nullptr ? logq : P.picked;
     const long long quads = H.rows * ((H.top + 3) / 4);
-    CAPSCAPS_TRY(run(quads < 1024 ? pick_kernel<true> : pick_kernel<false>, blocks_for(quads, quads < 1024 ? 1 : 4), THREADS, st, H, picked, vectors));
-    CAPSCAPS_TRY(run(few ? loss_kernel<1> : loss_kernel<8>, blocks_for(H.rows, few ? 1 : 8), THREADS, st, H, (const Stat*)P.stats,
-                     P.pieces > 1 ? 1 : P.stat_parts, (const float*)picked, loss, lse, logq));
+    const bool pick = few && H.top <= 4;
+    if (!pick)
+        CAPSCAPS_TRY(run(quads < 1024 ? pick_kernel<true> : pick_kernel<false>, blocks_for(quads, quads < 1024 ? 1 : 4), THREADS, st, H, picked, vectors));
+    CAPSCAPS_TRY(run(pick ? loss_kernel<1, true> : few ? loss_kernel<1, false> : loss_kernel<8, false>, blocks_for(H.rows, few ? 1 : 8), THREADS,
+                     st, H, (const Stat*)P.stats, P.pieces > 1 ? 1 : P.stat_parts, picked, vectors, loss, lse, logq));
     return CAPSCAPS_OK;
 }
 
