@@ -87,5 +87,14 @@ inline hipError_t launch_head_gemm(const HeadGemm& g, int tile, HeadEnd end, hip
            : tile == HEAD_TILE_128 ? launch_head_gemm_128(g, end, st)
                                    : launch_head_gemm_few_rows(g, end, st);
 }
+// Two products on the same tiles (not those of 256 x 256) in one launch, for HEAD_OUT
+hipError_t launch_head_gemm_pair_128(const HeadGemm& a, const HeadGemm& b, hipStream_t st);
+hipError_t launch_head_gemm_pair_few_rows(const HeadGemm& a, const HeadGemm& b, hipStream_t st);
+inline hipError_t launch_head_gemm_pair(const HeadGemm& a, const HeadGemm& b, int tile, hipStream_t st)
+{
+    return tile == HEAD_TILE_128        ? launch_head_gemm_pair_128(a, b, st)
+           : tile == HEAD_TILE_FEW_ROWS ? launch_head_gemm_pair_few_rows(a, b, st)
+                                        : hipErrorInvalidValue;
+}
 
 }  // namespace capscaps

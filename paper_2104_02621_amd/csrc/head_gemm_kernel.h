@@ -63,7 +63,7 @@ __device__ __forceinline__ void turn(unsigned& lo, unsigned& hi, int lane)
 
 // NB: stages of the ring
 template <typename Tag, int BM, int BN, int NWM, int NB, int TERMS, bool ROWS, int END>
-__global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kernel(const HeadGemm G, int tiles_n)
+__device__ __forceinline__ void head_gemm(const HeadGemm& G, int tiles_n, int block)
 {
     constexpr int NWN = 4 / NWM, WM = BM / NWM, WN = BN / NWN, TM = WM / 32, TN = WN / 32;
     constexpr int A_BYTES = BM * 64, STAGE = (BM + BN) * 64;
@@ -83,9 +83,9 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
     }
     // (of the rows that count: the others' workgroups end here, and leave no XCD without work)
     const int tiles_m = (int)((m_end + BM - 1) / BM), tiles = tiles_m * tiles_n, all = tiles * G.splits;
-    if ((int)blockIdx.x >= all) return;
+    if (block >= all) return;
     const int span = all & ~7;
-    const int id = (int)blockIdx.x < span ? ((int)blockIdx.x & 7) * (span >> 3) + ((int)blockIdx.x >> 3) : blockIdx.x;
+    const int id = block < span ? (block & 7) * (span >> 3) + (block >> 3) : block;
     const int part = id / tiles, L = id - part * tiles;
     const int band = L / (8 * tiles_n), in_band = L - band * 8 * tiles_n;
     const int high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
@@ -519,19 +519,75 @@ __global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kerne
 }
 
 template <typename Tag, int BM, int BN, int NWM, int NB, int TERMS, bool ROWS, int END>
-hipError_t launch(HeadGemm g, hipStream_t st)
+__global__ __launch_bounds__(256, BM * BN == 65536 ? 1 : 2) void head_gemm_kernel(const HeadGemm G, int tiles_n)
+{
+    head_gemm<Tag, BM, BN, NWM, NB, TERMS, ROWS, END>(G, tiles_n, blockIdx.x);
+}
+
+// Two products that do not need each other in one launch: neither of few tiles leaves CUs without work, or its first copies
+// waited for alone
+struct HeadPair {
+    HeadGemm g[2];
+    int tiles_n[2], blocks;  // workgroups of the first
+};
+template <typename Tag, int BM, int BN, int NWM, int NB, int TERMS>
+__global__ __launch_bounds__(256, 2) void head_gemm_pair_kernel(const HeadPair P)
+{
+    const int second = (int)blockIdx.x >= P.blocks ? 1 : 0;
+    head_gemm<Tag, BM, BN, NWM, NB, TERMS, false, HEAD_OUT>(P.g[second], P.tiles_n[second],
+                                                             (int)blockIdx.x - (second ? P.blocks : 0));
+}
+
+// Workgroups of a product, 0 where no launch holds them (the plan keeps within it)
+template <int BM, int BN>
+int workgroups_of(HeadGemm& g, int& tiles_n)
 {
     const int size = g.out_dtype == CAPSCAPS_FP32 ? 4 : 2;
     g.whole_vectors = (reinterpret_cast<uintptr_t>(g.out) & 15) == 0 && g.ldo * size % 16 == 0 && g.out_split * size % 16 == 0 &&
                       g.ldo * size * BM < 0x7fffffffll;
     const long long tm = (g.m_rows + BM - 1) / BM, tn = (g.n_rows + BN - 1) / BN;
-    if (tm * tn * g.splits > (1 << 23) || tm < 1 || tn < 1) return hipErrorInvalidValue;  // (the plan keeps within it)
+    if (tm * tn * g.splits > (1 << 23) || tm < 1 || tn < 1) return 0;
+    tiles_n = (int)tn;
+    return (int)(tm * tn * g.splits);
+}
+
+template <typename Tag, int BM, int BN, int NWM, int NB, int TERMS>
+hipError_t launch_two(const HeadGemm& a, const HeadGemm& b, hipStream_t st)
+{
+    HeadPair p{{a, b}, {0, 0}, 0};
+    p.blocks = workgroups_of<BM, BN>(p.g[0], p.tiles_n[0]);
+    const int more = workgroups_of<BM, BN>(p.g[1], p.tiles_n[1]);
+    if (p.blocks == 0 || more == 0) return hipErrorInvalidValue;
+    const auto kernel = head_gemm_pair_kernel<Tag, BM, BN, NWM, NB, TERMS>;
+    constexpr int lds = (BM + BN) * 64 * NB;
+    static std::atomic<unsigned long long> done{0};
+    const hipError_t err = set_dynamic_lds_once(reinterpret_cast<const void*>(kernel), lds, done);
+    if (err != hipSuccess) return err;
+    kernel<<<dim3((unsigned)p.blocks + (unsigned)more), dim3(256), lds, st>>>(p);
+    return hipGetLastError();
+}
+template <int BM, int BN, int NWM, int NB>
+hipError_t launch_pair(const HeadGemm& a, const HeadGemm& b, hipStream_t st)
+{
+    if (a.terms != b.terms || a.dtype != b.dtype || a.stages_b == 0 || b.stages_b == 0) return hipErrorInvalidValue;
+    if (a.terms == 3) return launch_two<bf16_tag, BM, BN, NWM, NB, 3>(a, b, st);
+    const bool bf16 = a.dtype == CAPSCAPS_BF16;
+    if (a.terms == 2) return bf16 ? launch_two<bf16_tag, BM, BN, NWM, NB, 2>(a, b, st) : launch_two<f16_tag, BM, BN, NWM, NB, 2>(a, b, st);
+    return bf16 ? launch_two<bf16_tag, BM, BN, NWM, NB, 1>(a, b, st) : launch_two<f16_tag, BM, BN, NWM, NB, 1>(a, b, st);
+}
+
+template <typename Tag, int BM, int BN, int NWM, int NB, int TERMS, bool ROWS, int END>
+hipError_t launch(HeadGemm g, hipStream_t st)
+{
+    int tn = 0;
+    const int blocks = workgroups_of<BM, BN>(g, tn);
+    if (blocks == 0) return hipErrorInvalidValue;
     const auto kernel = head_gemm_kernel<Tag, BM, BN, NWM, NB, TERMS, ROWS, END>;
     constexpr int lds = (BM + BN) * 64 * NB;
     static std::atomic<unsigned long long> done{0};
     const hipError_t err = set_dynamic_lds_once(reinterpret_cast<const void*>(kernel), lds, done);
     if (err != hipSuccess) return err;
-    kernel<<<dim3((unsigned)(tm * tn * g.splits)), dim3(256), lds, st>>>(g, (int)tn);
+    kernel<<<dim3((unsigned)blocks), dim3(256), lds, st>>>(g, tn);
     return hipGetLastError();
 }
 

@@ -683,52 +683,77 @@ __global__ void __launch_bounds__(THREADS) clear_kernel(long long* p, long long 
 }
 
 // dbias of a piece
-__global__ void __launch_bounds__(THREADS) bias_kernel(Head H, const float* sums, int padded_classes, int tile_rows,
-                                                       const long long* taken, long long first, int classes, float* dbias)
+struct Bias {
+    const float* sums;
+    const long long* taken;
+    float* dbias;
+    long long first;
+    int padded_classes, tile_rows, classes;
+    unsigned blocks;
+};
+__device__ __forceinline__ void bias_of(const Bias& B, const int* count, unsigned block)
 {
-    const int c = blockIdx.x * THREADS + threadIdx.x;
-    if (c >= classes) return;
-    const long long tiles = (*H.count + tile_rows - 1) / tile_rows;
+    const int c = block * THREADS + threadIdx.x;
+    if (c >= B.classes) return;
+    const long long tiles = (*count + B.tile_rows - 1) / B.tile_rows;
     double s = 0.0;
-    for (long long t = 0; t < tiles; ++t) s += sums[t * padded_classes + c];
-    s -= (double)taken[first + c] * 0x1p-24;
-    dbias[first + c] = (float)(s * __builtin_bit_cast(float, H.count[1]));
+    for (long long t = 0; t < tiles; ++t) s += B.sums[t * B.padded_classes + c];
+    s -= (double)B.taken[B.first + c] * 0x1p-24;
+    B.dbias[B.first + c] = (float)(s * __builtin_bit_cast(float, count[1]));
 }
 
 // out[r][c] = one over the scale times the sum of `splits` parts of sums[pos[r]][c] (pos NULL: r), 0 where a row is left out
-__global__ void __launch_bounds__(THREADS) finish_kernel(const int* count, const int* pos, const float* sums, long long ld, int splits,
-                                                         long long split, long long rows, int columns, void* out, int dtype)
+struct Finish {
+    const int* pos;
+    const float* sums;
+    long long ld, split, rows;
+    int splits, columns;
+    void* out;
+    unsigned blocks;
+};
+__device__ __forceinline__ void finish(const Finish& F, const int* count, int dtype, unsigned block)
 {
     const float scale = __builtin_bit_cast(float, count[1]);
-    const int vecs = (columns + 3) / 4;
-    const long long all = rows * vecs;
+    const int vecs = (F.columns + 3) / 4;
+    const long long all = F.rows * vecs;
     const bool none = *count == 0;  // (nothing was added up then)
-    for (long long t = blockIdx.x * (long long)THREADS + threadIdx.x; t < all; t += (long long)gridDim.x * THREADS) {
+    for (long long t = block * (long long)THREADS + threadIdx.x; t < all; t += (long long)F.blocks * THREADS) {
         const long long r = t / vecs;
         const int c = (int)(t - r * vecs) * 4;
-        const long long i = pos != nullptr ? pos[r] : r;
+        const long long i = F.pos != nullptr ? F.pos[r] : r;
         float4v v = {0, 0, 0, 0};
         if (i >= 0 && !none) {
-            for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const float4v*>(sums + p * split + i * ld + c);
+            for (int p = 0; p < F.splits; ++p) v += *reinterpret_cast<const float4v*>(F.sums + p * F.split + i * F.ld + c);
             v *= scale;
         }
-        const long long at = r * columns + c;
-        if ((columns & 3) == 0 && dtype == CAPSCAPS_FP32) {
+        const long long at = r * F.columns + c;
+        if ((F.columns & 3) == 0 && dtype == CAPSCAPS_FP32) {
             typedef float at4 __attribute__((ext_vector_type(4), aligned(4)));
-            *reinterpret_cast<at4*>(static_cast<float*>(out) + at) = v;
-        } else if ((columns & 3) == 0) {
+            *reinterpret_cast<at4*>(static_cast<float*>(F.out) + at) = v;
+        } else if ((F.columns & 3) == 0) {
             typedef unsigned u2 __attribute__((ext_vector_type(2)));
             typedef u2 at2 __attribute__((aligned(2)));
             const int kind = dtype == CAPSCAPS_FP16 ? 2 : 1;
             const u2 w = {round_to_16(v[0], kind) | (unsigned)round_to_16(v[1], kind) << 16,
                           round_to_16(v[2], kind) | (unsigned)round_to_16(v[3], kind) << 16};
-            *reinterpret_cast<at2*>(static_cast<unsigned short*>(out) + at) = w;
+            *reinterpret_cast<at2*>(static_cast<unsigned short*>(F.out) + at) = w;
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (c + j < columns) store_element(out, at + j, v[j], dtype);
+                if (c + j < F.columns) store_element(F.out, at + j, v[j], dtype);
         }
     }
+}
+
+// Gradients from their sums: of up to two tensors and the bias, each by workgroups of its own (0: none)
+__global__ void __launch_bounds__(THREADS) finish_kernel(const int* count, Finish a, Finish b, Bias c, int dtype)
+{
+    if (blockIdx.x < a.blocks)
+        finish(a, count, dtype, blockIdx.x);
+    else if (blockIdx.x < a.blocks + b.blocks)
+        finish(b, count, dtype, blockIdx.x - a.blocks);
+    else
+        bias_of(c, count, blockIdx.x - a.blocks - b.blocks);
 }
 
 // ---------------------------------------------------------------------------------------- host
@@ -741,29 +766,70 @@ unsigned blocks_for(long long work, long long per) { return (unsigned)std::max<l
 struct Pick {
     int tile, splits;
 };
-Pick pick_tile(long long m, long long n, long long k, int terms, bool may_split, double part_us)
+struct Product {
+    long long m, n, k;
+    int terms;
+    bool may_split;
+    double part_us;  // what parts cost besides their bytes
+    long long stages() const { return std::max<long long>(1, (k + HEAD_K - 1) / HEAD_K) * head_products(terms); }
+};
+// A product on these tiles in `parts`: rounds' worth of workgroups, units that one takes, and that joining the parts takes
+struct Estimate {
+    bool can;
+    double load, tile, join;
+};
+Estimate estimate(const Product& P, int tile, int parts)
 {
-    const long long stages = std::max<long long>(1, (k + HEAD_K - 1) / HEAD_K) * head_products(terms);
+    const HeadTileShape s = head_tile_shape(tile);
+    const double tiles = (double)((P.m + s.m - 1) / s.m) * (double)((P.n + s.n - 1) / s.n);
+    // time of a stage of as many tiles as a CU holds, and stages' time to begin and end
+    const double cost = tile == HEAD_TILE_256 ? 1.0 : tile == HEAD_TILE_128 ? 0.75 : 0.5;
+    const double ends = tile == HEAD_TILE_256 ? 24 : 8;
+    Estimate E{};
+    E.can = tiles * parts <= MOST_TILES && (parts == 1 || (P.may_split && P.stages() / parts >= 8)) &&
+            (P.terms != 2 || tile != HEAD_TILE_256);  // (not built)
+    E.load = tiles * parts / (256.0 * s.per_cu);
+    E.tile = ((double)((P.stages() + parts - 1) / parts) + ends) * cost;
+    E.join = parts > 1 ? ((double)P.m * P.n * 8 * parts / 4e6 + P.part_us) / 0.7 : 0.0;
+    return E;
+}
+double rounds_of(double load) { return load <= 4 ? std::max(1.0, (double)(long long)(load + 0.999)) : load; }
+int more_parts(int parts) { return parts < 4 ? parts + 1 : parts * 2; }
+
+Pick pick_tile(const Product& P, double* units = nullptr)
+{
     Pick best{HEAD_TILE_128, 1};
     double least = 1e300;
-    for (const int tile : {HEAD_TILE_256, HEAD_TILE_128, HEAD_TILE_FEW_ROWS}) {
-        const HeadTileShape s = head_tile_shape(tile);
-        if (terms == 2 && tile == HEAD_TILE_256) continue;  // (not built)
-        const double tiles = (double)((m + s.m - 1) / s.m) * (double)((n + s.n - 1) / s.n);
-        const double slots = 256.0 * s.per_cu;
-        // time of a stage of as many tiles as a CU holds, and stages' time to begin and end
-        const double cost = tile == HEAD_TILE_256 ? 1.0 : tile == HEAD_TILE_128 ? 0.75 : 0.5;
-        const double ends = tile == HEAD_TILE_256 ? 24 : 8;
-        for (int parts = 1; parts <= 64; parts = parts < 4 ? parts + 1 : parts * 2) {
-            if (parts > 1 && (!may_split || stages / parts < 8)) break;
-            if (tiles * parts > MOST_TILES) continue;
-            const double load = tiles * parts / slots;
-            const double rounds = load <= 4 ? std::max(1.0, (double)(long long)(load + 0.999)) : load;
-            double t = rounds * ((double)((stages + parts - 1) / parts) + ends) * cost;
-            if (parts > 1) t += ((double)m * n * 8 * parts / 4e6 + part_us) / 0.7;
+    for (const int tile : {HEAD_TILE_256, HEAD_TILE_128, HEAD_TILE_FEW_ROWS})
+        for (int parts = 1; parts <= 64; parts = more_parts(parts)) {
+            const Estimate E = estimate(P, tile, parts);
+            if (!E.can) continue;
+            const double t = rounds_of(E.load) * E.tile + E.join;
             if (t < least) least = t, best = {tile, parts};
         }
-    }
+    if (units != nullptr) *units += least;
+    return best;
+}
+
+// ... of two products in one launch, whose workgroups share the CUs
+struct Two {
+    Pick a, b;
+};
+Two pick_two(const Product& A, const Product& B, double* units)
+{
+    Two best{{HEAD_TILE_128, 1}, {HEAD_TILE_128, 1}};
+    double least = 1e300;
+    for (const int tile : {HEAD_TILE_128, HEAD_TILE_FEW_ROWS})
+        for (int pa = 1; pa <= 16; pa = more_parts(pa))
+            for (int pb = 1; pb <= 16; pb = more_parts(pb)) {
+                const Estimate a = estimate(A, tile, pa), b = estimate(B, tile, pb);
+                if (!a.can || !b.can) continue;
+                const double load = a.load + b.load;
+                const double t = rounds_of(load) * (a.load * a.tile + b.load * b.tile) / load;
+                const double all = std::max(t, std::max(a.tile, b.tile)) + a.join + b.join;
+                if (all < least) least = all, best = {{tile, pa}, {tile, pb}};
+            }
+    *units = least;
     return best;
 }
 
@@ -799,6 +865,7 @@ struct Plan {
     int pieces, stat_parts;
     long long padded_rows;
     Pick z, dx, dw;
+    bool pair;  // dx and dweight in one launch
     bool distill, backward;
     size_t bytes;
     // the workspace
@@ -834,7 +901,7 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     if (!backward) P.piece = std::min(P.piece, std::max<long long>(256, PIECE_BYTES / 8 / rows * 32 / 256 * 256));
     P.pieces = (int)((A.classes + P.piece - 1) / P.piece);
     const long long most = std::min<long long>(P.piece, A.classes);
-    P.z = pick_tile(rows, most, A.width, P.terms, P.pieces == 1 && A.classes <= MOST_IN_PARTS && rows * P.piece * 64 * 4 <= PIECE_BYTES, 6.0);
+    P.z = pick_tile({rows, most, A.width, P.terms, P.pieces == 1 && A.classes <= MOST_IN_PARTS && rows * P.piece * 64 * 4 <= PIECE_BYTES, 6.0});
     P.in_parts = P.z.splits > 1;
     P.stat_parts = P.in_parts ? 1 : ceil_div(most, head_tile_shape(P.z.tile).stat_columns);  // of a piece
     Layout L{static_cast<char*>(base)};
@@ -857,8 +924,14 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
         return P;
     }
     W.coef = L.take<float>(A.rows);
-    P.dx = pick_tile(rows, A.width, P.piece, P.grad_terms, P.pieces == 1, 0.0);  // (several: added up piece after piece)
-    P.dw = pick_tile(most, A.width, rows, P.grad_terms, true, 3.0);
+    const Product dx{rows, A.width, P.piece, P.grad_terms, P.pieces == 1, 0.0};  // (several: added up piece after piece)
+    const Product dw{most, A.width, rows, P.grad_terms, true, 3.0};
+    double apart = 0.0, together = 0.0;
+    P.dx = pick_tile(dx, &apart), P.dw = pick_tile(dw, &apart);
+    if (P.pieces == 1) {
+        const Two two = pick_two(dx, dw, &together);
+        if (together < apart) P.pair = true, P.dx = two.a, P.dw = two.b;
+    }
     const long long ld = round_up(A.width, 4);
     const long long row_stages = P.terms * P.padded_rows / HEAD_K, class_stages = P.terms * round_up(P.piece, HEAD_K) / HEAD_K;
     P.xt = L.take<unsigned short>(head_block_values(A.width, row_stages));
@@ -1022,41 +1095,46 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
         }
         CAPSCAPS_TRY(run(entries_kernel<TERMS>, blocks_for(H.rows, 4), THREADS, st, H, G.loss, G.logq, first, (int)classes, P.gn,
                          padded, P.gt, P.padded_rows, P.grad_terms, G.dbias != nullptr ? P.taken : nullptr));
+        Bias bias{};
         if (G.dbias != nullptr)
-            CAPSCAPS_TRY(run(bias_kernel, (unsigned)((classes + THREADS - 1) / THREADS), THREADS, st, H, (const float*)P.bias_sums, padded,
-                             P.in_parts ? 64 : head_tile_shape(P.z.tile).sum_rows,
-                             (const long long*)P.taken, first, (int)classes, G.dbias));
+            bias = {P.bias_sums, P.taken, G.dbias, first, padded, P.in_parts ? 64 : head_tile_shape(P.z.tile).sum_rows, (int)classes,
+                    blocks_for(classes, THREADS)};
+        HeadGemm x{}, w{};
+        Finish dx{}, dw{};
         if (G.dx != nullptr) {
-            HeadGemm g{};
-            g.a = P.gn, g.b = P.wt;
-            g.plane_a = g.plane_b = padded / HEAD_K, g.terms = P.grad_terms;
-            g.stages_a = (long long)P.grad_terms * g.plane_a, g.stages_b = (long long)P.terms * g.plane_b;
-            g.m_rows = H.rows, g.n_rows = H.width, g.m_count = H.count, g.k = classes;
-            g.dtype = H.dtype, g.out = P.dx_sums, g.ldo = ld, g.out_split = H.rows * ld, g.out_dtype = CAPSCAPS_FP32;
-            g.splits = P.dx.splits, g.accumulate = piece > 0;
-            CAPSCAPS_TRY(launch_head_gemm(g, P.dx.tile, HEAD_OUT, st));
+            x.a = P.gn, x.b = P.wt;
+            x.plane_a = x.plane_b = padded / HEAD_K, x.terms = P.grad_terms;
+            x.stages_a = (long long)P.grad_terms * x.plane_a, x.stages_b = (long long)P.terms * x.plane_b;
+            x.m_rows = H.rows, x.n_rows = H.width, x.m_count = H.count, x.k = classes;
+            x.dtype = H.dtype, x.out = P.dx_sums, x.ldo = ld, x.out_split = H.rows * ld, x.out_dtype = CAPSCAPS_FP32;
+            x.splits = P.dx.splits, x.accumulate = piece > 0;
+            if (piece == P.pieces - 1)
+                dx = {H.pos, P.dx_sums, ld, H.rows * ld, H.rows, P.dx.splits, H.width, G.dx, blocks_for(H.rows * (ld / 4), THREADS)};
         }
         if (G.dweight != nullptr) {
             char* out = static_cast<char*>(G.dweight) + first * H.width * size;
-            HeadGemm g{};
-            g.a = P.gt, g.b = P.xt;
-            g.plane_a = g.plane_b = (int)(P.padded_rows / HEAD_K), g.terms = P.grad_terms;
-            g.stages_a = (long long)P.grad_terms * g.plane_a, g.stages_b = (long long)P.terms * g.plane_b;
-            g.m_rows = classes, g.n_rows = H.width, g.k = H.rows, g.k_count = H.count;
-            g.dtype = H.dtype, g.splits = P.dw.splits;
+            w.a = P.gt, w.b = P.xt;
+            w.plane_a = w.plane_b = (int)(P.padded_rows / HEAD_K), w.terms = P.grad_terms;
+            w.stages_a = (long long)P.grad_terms * w.plane_a, w.stages_b = (long long)P.terms * w.plane_b;
+            w.m_rows = classes, w.n_rows = H.width, w.k = H.rows, w.k_count = H.count;
+            w.dtype = H.dtype, w.splits = P.dw.splits;
             const bool direct = P.dw.splits == 1;
-            g.out = direct ? out : (void*)P.dw_sums;
-            g.ldo = direct ? H.width : ld, g.out_split = classes * ld, g.out_dtype = direct ? H.dtype : CAPSCAPS_FP32;
-            if (direct) g.scale = scale;
-            CAPSCAPS_TRY(launch_head_gemm(g, P.dw.tile, HEAD_OUT, st));
-            if (!direct)
-                CAPSCAPS_TRY(run(finish_kernel, blocks_for(classes * (ld / 4), THREADS), THREADS, st, (const int*)H.count, (const int*)nullptr,
-                                 (const float*)P.dw_sums, ld, P.dw.splits, classes * ld, classes, H.width, (void*)out, H.dtype));
+            w.out = direct ? out : (void*)P.dw_sums;
+            w.ldo = direct ? H.width : ld, w.out_split = classes * ld, w.out_dtype = direct ? H.dtype : CAPSCAPS_FP32;
+            if (direct)
+                w.scale = scale;
+            else
+                dw = {nullptr, P.dw_sums, ld, classes * ld, classes, P.dw.splits, H.width, out, blocks_for(classes * (ld / 4), THREADS)};
         }
+        if (P.pair && G.dx != nullptr && G.dweight != nullptr) {
+            CAPSCAPS_TRY(launch_head_gemm_pair(x, w, P.dx.tile, st));
+        } else {
+            if (G.dx != nullptr) CAPSCAPS_TRY(launch_head_gemm(x, P.dx.tile, HEAD_OUT, st));
+            if (G.dweight != nullptr) CAPSCAPS_TRY(launch_head_gemm(w, P.dw.tile, HEAD_OUT, st));
+        }
+        const unsigned blocks = dx.blocks + dw.blocks + bias.blocks;
+        if (blocks > 0) CAPSCAPS_TRY(run(finish_kernel, blocks, THREADS, st, (const int*)H.count, dx, dw, bias, H.dtype));
     }
-    if (G.dx != nullptr)
-        CAPSCAPS_TRY(run(finish_kernel, blocks_for(H.rows * (ld / 4), THREADS), THREADS, st, (const int*)H.count, (const int*)H.pos,
-                         (const float*)P.dx_sums, ld, P.dx.splits, H.rows * ld, H.rows, H.width, G.dx, H.dtype));
     return CAPSCAPS_OK;
 }
 
