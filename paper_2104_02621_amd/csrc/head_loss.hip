@@ -276,31 +276,38 @@ __global__ void __launch_bounds__(THREADS) pack_kernel(const void* from, long lo
 
 // Columns of `from` as an operand that contracts its rows (rows_of[i], those that count); zeros past them.  And, where
 // `straight` is not NULL, what pack_kernel makes of it.  Tiles of 64 x 64.
+struct Across {
+    const void* from;
+    long long stride, rows, stages, straight_stages;
+    const int *rows_of, *count;
+    unsigned short *to, *straight;
+    int columns;
+    unsigned blocks;
+    bool vectors;
+};
 template <bool TERMS>
-__global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* from, long long stride, int columns,
-                                                                  long long rows, const int* rows_of, const int* count,
-                                                                  unsigned short* to, long long stages,
-                                                                  unsigned short* straight, long long straight_stages, bool vectors)
+using AcrossTile = std::conditional_t<TERMS, float, unsigned short>[64][TERMS ? 65 : 66];
+template <bool TERMS>
+__device__ __forceinline__ void pack_across(const Across& A, unsigned block0, AcrossTile<TERMS>& tile)
 {
     typedef std::conditional_t<TERMS, float, unsigned short> E;
-    __shared__ E tile[64][TERMS ? 65 : 66];
-    long long kept = rows;
-    if (count != nullptr && *count < kept) kept = *count;
+    long long kept = A.rows;
+    if (A.count != nullptr && *A.count < kept) kept = *A.count;
     const long long used = (kept + HEAD_K - 1) / HEAD_K;  // stages that are read
-    const int across = (columns + 63) / 64;
+    const int across = (A.columns + 63) / 64;
     const long long tiles = (used + 1) / 2 * across;
-    for (long long b = blockIdx.x; b < tiles; b += gridDim.x) {
+    for (long long b = block0; b < tiles; b += A.blocks) {
         const long long i0 = b / across * 64;
         const int c0 = (int)(b % across) * 64;
         constexpr int PER = 16 / sizeof(E), ROW = 64 / PER;  // values of a vector, vectors of a tile's row
-        if (vectors && c0 + 64 <= columns) {
+        if (A.vectors && c0 + 64 <= A.columns) {
 #pragma unroll
             for (int u = 0; u < 64 * ROW / THREADS; ++u) {
                 const int t = u * THREADS + threadIdx.x, i = t / ROW, c = t % ROW * PER;
                 chunk_t v = {0, 0, 0, 0};
                 if (i0 + i < kept) {
-                    const long long row = rows_of != nullptr ? rows_of[i0 + i] : i0 + i;
-                    v = *reinterpret_cast<const chunk_t*>(static_cast<const E*>(from) + row * stride + c0 + c);
+                    const long long row = A.rows_of != nullptr ? A.rows_of[i0 + i] : i0 + i;
+                    v = *reinterpret_cast<const chunk_t*>(static_cast<const E*>(A.from) + row * A.stride + c0 + c);
                 }
                 E e[PER];
                 __builtin_memcpy(e, &v, 16);
@@ -312,9 +319,9 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* fr
             for (int u = 0; u < 16; ++u) {
                 const int t = u * THREADS + threadIdx.x, i = t >> 6, c = t & 63;
                 E v = 0;
-                if (i0 + i < kept && c0 + c < columns) {
-                    const long long row = rows_of != nullptr ? rows_of[i0 + i] : i0 + i;
-                    v = static_cast<const E*>(from)[row * stride + c0 + c];
+                if (i0 + i < kept && c0 + c < A.columns) {
+                    const long long row = A.rows_of != nullptr ? A.rows_of[i0 + i] : i0 + i;
+                    v = static_cast<const E*>(A.from)[row * A.stride + c0 + c];
                 }
                 tile[i][c] = v;
             }
@@ -324,7 +331,7 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* fr
             // (a wave: a block)
             const int block = t >> 6, c = (block >> 1) * 16 + ((t & 63) >> 2);
             const int i = (block & 1) * HEAD_K + ((t & 3) ^ ((t & 63) >> 4)) * 8;
-            if (c0 + c < (columns + 15) / 16 * 16 && i0 + i < used * HEAD_K) {
+            if (c0 + c < (A.columns + 15) / 16 * 16 && i0 + i < used * HEAD_K) {
                 unsigned short raw[8];
                 float f[8];
 #pragma unroll
@@ -334,14 +341,14 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* fr
                     else
                         raw[j] = tile[i + j][c];
                 }
-                put_operand<TERMS>(to, c0 + c, i0 + i, stages, raw, f);
+                put_operand<TERMS>(A.to, c0 + c, i0 + i, A.stages, raw, f);
             }
         }
-        if (straight != nullptr)
+        if (A.straight != nullptr)
             for (int t = threadIdx.x; t < 64 * 8; t += THREADS) {
                 const int block = t >> 6, i = (block >> 1) * 16 + ((t & 63) >> 2);
                 const int c = (block & 1) * HEAD_K + ((t & 3) ^ ((t & 63) >> 4)) * 8;
-                if (i0 + i < (kept + 15) / 16 * 16 && c0 + c < straight_stages * HEAD_K) {
+                if (i0 + i < (kept + 15) / 16 * 16 && c0 + c < A.straight_stages * HEAD_K) {
                     unsigned short raw[8];
                     float f[8];
 #pragma unroll
@@ -351,11 +358,26 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(const void* fr
                         else
                             raw[j] = tile[i][c + j];
                     }
-                    put_operand<TERMS>(straight, i0 + i, c0 + c, straight_stages, raw, f);
+                    put_operand<TERMS>(A.straight, i0 + i, c0 + c, A.straight_stages, raw, f);
                 }
             }
         __syncthreads();
     }
+}
+
+// Of up to two tensors, each by workgroups of its own (0: none), and zeros to `clear`
+template <bool TERMS>
+__global__ void __launch_bounds__(THREADS) pack_transposed_kernel(Across a, Across b, long long* clear, long long n)
+{
+    __shared__ AcrossTile<TERMS> tile;
+    const unsigned both = a.blocks + b.blocks;
+    if (blockIdx.x < a.blocks)
+        pack_across<TERMS>(a, blockIdx.x, tile);
+    else if (blockIdx.x < both)
+        pack_across<TERMS>(b, blockIdx.x - a.blocks, tile);
+    else
+        for (long long t = (blockIdx.x - both) * (long long)THREADS + threadIdx.x; t < n; t += (gridDim.x - both) * (long long)THREADS)
+            clear[t] = 0;
 }
 
 // ---------------------------------------------------------------------------------------- forward
@@ -677,11 +699,6 @@ __global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* l
     }
 }
 
-__global__ void __launch_bounds__(THREADS) clear_kernel(long long* p, long long n)
-{
-    for (long long t = blockIdx.x * (long long)THREADS + threadIdx.x; t < n; t += (long long)gridDim.x * THREADS) p[t] = 0;
-}
-
 // dbias of a piece
 struct Bias {
     const float* sums;
@@ -969,17 +986,17 @@ hipError_t pack(const Plan& P, const void* from, long long stride, int columns, 
     return P.terms == 3 ? run(pack_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors)
                         : run(pack_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors);
 }
-hipError_t pack_transposed(const Plan& P, const void* from, long long stride, int columns, long long rows, const Head* kept,
-                           unsigned short* to, long long padded, unsigned short* straight, hipStream_t st)
+Across across_of(const Plan& P, const void* from, long long stride, int columns, long long rows, const Head* kept, unsigned short* to,
+                 long long padded, unsigned short* straight)
 {
-    const int* rows_of = kept != nullptr ? kept->rows_of : nullptr;
-    const int* count = kept != nullptr ? kept->count : nullptr;
-    const long long stages = padded / HEAD_K;
-    const unsigned blocks = blocks_for((padded + 63) / 64 * ((columns + 63) / 64), 1);
-    const bool vectors = vectors_of(from, stride, P.terms == 3 ? CAPSCAPS_FP32 : CAPSCAPS_BF16);
-    const long long across = P.padded / HEAD_K;
-    return P.terms == 3 ? run(pack_transposed_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, straight, across, vectors)
-                        : run(pack_transposed_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, straight, across, vectors);
+    Across A{};
+    A.from = from, A.stride = stride, A.columns = columns, A.rows = rows;
+    if (kept != nullptr) A.rows_of = kept->rows_of, A.count = kept->count;
+    A.to = to, A.stages = padded / HEAD_K;
+    A.straight = straight, A.straight_stages = P.padded / HEAD_K;
+    A.vectors = vectors_of(from, stride, P.terms == 3 ? CAPSCAPS_FP32 : CAPSCAPS_BF16);
+    A.blocks = blocks_for((padded + 63) / 64 * ((columns + 63) / 64), 1);
+    return A;
 }
 
 const void* weight_at(const Head& H, long long cls)
@@ -987,19 +1004,17 @@ const void* weight_at(const Head& H, long long cls)
     return static_cast<const char*>(H.weight) + cls * H.weight_stride * (long long)element_bytes(H.dtype);
 }
 
-// The rows that count, and x of these as an operand (and one that contracts rows)
-int begin(const Head& H, const Plan& P, const float* dloss, long long dloss_stride, bool both, hipStream_t st)
+// The rows that count
+int begin(const Head& H, const Plan& P, const float* dloss, long long dloss_stride, hipStream_t st)
 {
     if (P.distill) CAPSCAPS_TRY(run(teacher_kernel, blocks_for(H.rows, 4), THREADS, st, H));
     CAPSCAPS_TRY(run(rows_kernel, 1, 1024, st, H, dloss, dloss_stride));
-    CAPSCAPS_TRY(both ? pack_transposed(P, H.x, H.x_stride, H.width, H.rows, &H, P.xt, P.padded_rows, P.x, st)
-                      : pack(P, H.x, H.x_stride, H.width, H.rows, &H, H.dtype, P.x, st));
     return CAPSCAPS_OK;
 }
 
-// The product of x and a piece's weights, for launch_head_gemm with an end of the caller's; with `both`, the weights as an
-// operand that contracts classes too
-int logits_of(const Head& H, const Plan& P, long long first, long long classes, bool both, HeadGemm& g, hipStream_t st)
+// The product of x and a piece's weights, for launch_head_gemm with an end of the caller's; `across`: NULL, or what the caller packs
+// before it, the weights as an operand that contracts classes
+int logits_of(const Head& H, const Plan& P, long long first, long long classes, Across* across, HeadGemm& g, hipStream_t st)
 {
     g = HeadGemm{};
     const int stages = P.padded / HEAD_K;
@@ -1011,12 +1026,12 @@ int logits_of(const Head& H, const Plan& P, long long first, long long classes, 
         H.weight_stride <= (1 << 21)) {
         g.b = weight_at(H, first), g.ldb = H.weight_stride * 2;
     } else {
-        if (!both) CAPSCAPS_TRY(pack(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, H.dtype, P.w, st));
+        if (across == nullptr) CAPSCAPS_TRY(pack(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, H.dtype, P.w, st));
         g.b = P.w, g.stages_b = g.stages_a;
     }
-    if (both)
-        CAPSCAPS_TRY(pack_transposed(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, P.wt, round_up(classes, HEAD_K),
-                                     g.b == P.w ? P.w : nullptr, st));
+    if (across != nullptr)
+        *across = across_of(P, weight_at(H, first), H.weight_stride, H.width, classes, nullptr, P.wt, round_up(classes, HEAD_K),
+                            g.b == P.w ? P.w : nullptr);
     g.m_rows = H.rows, g.n_rows = classes, g.m_count = H.count, g.k = H.width;
     g.plane_a = g.plane_b = stages;
     g.terms = P.terms;
@@ -1034,12 +1049,13 @@ int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, 
 {
     if (H.rows == 0) return CAPSCAPS_OK;
     const bool few = H.rows < 512;
-    int rc = begin(H, P, nullptr, 0, false, st);
+    int rc = begin(H, P, nullptr, 0, st);
     if (rc != CAPSCAPS_OK) return rc;
+    CAPSCAPS_TRY(pack(P, H.x, H.x_stride, H.width, H.rows, &H, H.dtype, P.x, st));
     for (int piece = 0; piece < P.pieces; ++piece) {
         const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
         HeadGemm g;
-        rc = logits_of(H, P, first, classes, false, g, st);
+        rc = logits_of(H, P, first, classes, nullptr, g, st);
         if (rc != CAPSCAPS_OK) return rc;
         g.stats = P.pieces > 1 ? P.stats + H.rows : P.stats;
         CAPSCAPS_TRY(launch_head_gemm(g, P.z.tile, P.in_parts ? HEAD_OUT : HEAD_STATS, st));
@@ -1075,11 +1091,23 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
     const long long ld = round_up(H.width, 4);
     const float* scale = reinterpret_cast<const float*>(H.count + 1);
     const int size = (int)element_bytes(H.dtype);
+    // (with the first piece's weights: x both ways, and zeros for what entries take of the bias' gradient)
+    Across x_across{};
+    if (G.dweight != nullptr)
+        x_across = across_of(P, H.x, H.x_stride, H.width, H.rows, &H, P.xt, P.padded_rows, P.x);
+    else
+        CAPSCAPS_TRY(pack(P, H.x, H.x_stride, H.width, H.rows, &H, H.dtype, P.x, st));
+    unsigned clear = G.dbias != nullptr ? blocks_for(H.classes, THREADS) : 0;
     for (int piece = 0; piece < P.pieces; ++piece) {
         const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
         HeadGemm z;
-        const int rc = logits_of(H, P, first, classes, G.dx != nullptr, z, st);
+        Across w_across{};
+        const int rc = logits_of(H, P, first, classes, G.dx != nullptr ? &w_across : nullptr, z, st);
         if (rc != CAPSCAPS_OK) return rc;
+        if (x_across.blocks + w_across.blocks + clear > 0)
+            CAPSCAPS_TRY(run(pack_transposed_kernel<TERMS>, x_across.blocks + w_across.blocks + clear, THREADS, st, x_across, w_across, P.taken,
+                             H.classes));
+        x_across.blocks = clear = 0;
         const int padded = (int)round_up(classes, HEAD_K);
         float* const sums = G.dbias != nullptr ? P.bias_sums : nullptr;
         if (P.in_parts) {
@@ -1153,9 +1181,8 @@ int backward(const Head& H, const Plan& P, const Gradients& G, hipStream_t st)
             CAPSCAPS_TRY(run(zero_kernel, blocks_for(H.classes * 2, THREADS), THREADS, st, reinterpret_cast<unsigned short*>(G.dbias), H.classes * 2));
         return CAPSCAPS_OK;
     }
-    const int rc = begin(H, P, G.dloss, G.dloss_stride, G.dweight != nullptr, st);
+    const int rc = begin(H, P, G.dloss, G.dloss_stride, st);
     if (rc != CAPSCAPS_OK) return rc;
-    if (G.dbias != nullptr) CAPSCAPS_TRY(run(clear_kernel, blocks_for(H.classes, THREADS), THREADS, st, P.taken, H.classes));
     return P.terms == 3 ? backward_pieces<true>(H, P, G, st) : backward_pieces<false>(H, P, G, st);
 }
 
