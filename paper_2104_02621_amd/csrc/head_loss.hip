@@ -178,6 +178,10 @@ __global__ void __launch_bounds__(1024) rows_kernel(Head H, const float* dloss, 
 }
 
 // ---------------------------------------------------------------------------------------- operands
+// 16 bytes at an element's address
+typedef Words<4, 2>::at Vector2;
+typedef float4v Vector4 __attribute__((aligned(4)));
+
 // Eight values of a row as a product's operand: one 16-byte vector, or one in each of three terms (`stages` of a term)
 template <bool TERMS>
 __device__ __forceinline__ void put_operand(unsigned short* to, long long row, long long k, long long stages,
@@ -239,7 +243,7 @@ __device__ __forceinline__ void put_gradients(unsigned short* to, long long row,
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) pack_kernel(const void* from, long long stride, int columns, long long rows,
                                                        const int* rows_of, const int* count, unsigned short* to,
-                                                       long long stages, bool vectors)
+                                                       long long stages)
 {
     const long long kept = count != nullptr ? *count : rows, blocks = (kept + 15) / 16 * stages;
     const int lane = threadIdx.x & 63;
@@ -250,13 +254,14 @@ __global__ void __launch_bounds__(THREADS) pack_kernel(const void* from, long lo
         float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (i < kept) {
             const long long at = (rows_of != nullptr ? rows_of[i] : i) * stride + c;
-            if (vectors && c + 8 <= columns) {
+            if (c + 8 <= columns) {
                 if constexpr (TERMS) {
-                    const float4v *p = reinterpret_cast<const float4v*>(static_cast<const float*>(from) + at), u = p[0], v = p[1];
+                    const Vector4 *p = reinterpret_cast<const Vector4*>(static_cast<const float*>(from) + at);
+                    const float4v u = p[0], v = p[1];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) f[j] = u[j], f[4 + j] = v[j];
                 } else {
-                    const chunk_t u = *reinterpret_cast<const chunk_t*>(static_cast<const unsigned short*>(from) + at);
+                    const chunk_t u = *reinterpret_cast<const Vector2*>(static_cast<const unsigned short*>(from) + at);
                     __builtin_memcpy(raw, &u, 16);
                 }
             } else {
@@ -283,7 +288,6 @@ struct Across {
     unsigned short *to, *straight;
     int columns;
     unsigned blocks;
-    bool vectors;
 };
 template <bool TERMS>
 using AcrossTile = std::conditional_t<TERMS, float, unsigned short>[64][TERMS ? 65 : 66];
@@ -300,14 +304,14 @@ __device__ __forceinline__ void pack_across(const Across& A, unsigned block0, Ac
         const long long i0 = b / across * 64;
         const int c0 = (int)(b % across) * 64;
         constexpr int PER = 16 / sizeof(E), ROW = 64 / PER;  // values of a vector, vectors of a tile's row
-        if (A.vectors && c0 + 64 <= A.columns) {
+        if (c0 + 64 <= A.columns) {
 #pragma unroll
             for (int u = 0; u < 64 * ROW / THREADS; ++u) {
                 const int t = u * THREADS + threadIdx.x, i = t / ROW, c = t % ROW * PER;
                 chunk_t v = {0, 0, 0, 0};
                 if (i0 + i < kept) {
                     const long long row = A.rows_of != nullptr ? A.rows_of[i0 + i] : i0 + i;
-                    v = *reinterpret_cast<const chunk_t*>(static_cast<const E*>(A.from) + row * A.stride + c0 + c);
+                    v = *reinterpret_cast<const typename Words<4, sizeof(E)>::at*>(static_cast<const E*>(A.from) + row * A.stride + c0 + c);
                 }
                 E e[PER];
                 __builtin_memcpy(e, &v, 16);
@@ -396,6 +400,24 @@ __device__ __forceinline__ Stat wave_join(Stat s)
     return s;
 }
 
+// The sum of what lies at `from` in each of `splits` parts, four on their way at a time
+template <typename V>
+__device__ __forceinline__ V sum_of_parts(const float* from, long long split, int splits)
+{
+    V sum = {};
+    int p = 0;
+    for (; p + 4 <= splits; p += 4) {
+        V v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = *reinterpret_cast<const V*>(from + (p + q) * split);
+        __builtin_amdgcn_sched_barrier(0);  // (the compiler would wait for each before it asks for the next)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum += v[q];
+    }
+    for (; p < splits; ++p) sum += *reinterpret_cast<const V*>(from + p * split);
+    return sum;
+}
+
 // stats[i] of logits that lie in parts.  A workgroup for a row.
 __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, long long ldz, int splits, long long split,
                                                         Stat* stats)
@@ -407,8 +429,7 @@ __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, 
     for (long long i = blockIdx.x; i < kept; i += gridDim.x) {
         Stat s = {-__builtin_inff(), 0.0f};
         for (long long c = threadIdx.x; c < H.classes; c += THREADS) {
-            float v = 0.0f;
-            for (int p = 0; p < splits; ++p) v += z[p * split + i * ldz + c];
+            float v = sum_of_parts<float>(z + i * ldz + c, split, splits);
             if (H.bias != nullptr) v += H.bias[c];
             v *= inv;
             if (v != v)
@@ -427,7 +448,7 @@ __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, 
 // z of entries k0 to k0 + 3 of row r (0 where they do not count), from the operands in fp32: to picked[r][k].  By a wave, or where there are
 // few by a workgroup (LANES); what it waits for is the weights' rows, which lie anywhere.
 template <int LANES>
-__device__ __forceinline__ void pick_entries(const Head& H, long long r, int k0, float* picked, bool vectors, float (*parts)[4])
+__device__ __forceinline__ void pick_entries(const Head& H, long long r, int k0, float* picked, float (*parts)[4])
 {
     const int lane = threadIdx.x & (LANES - 1);
     long long cls[4];
@@ -435,15 +456,15 @@ __device__ __forceinline__ void pick_entries(const Head& H, long long r, int k0,
 #pragma unroll
     for (int j = 0; j < 4; ++j) cls[j] = k0 + j < H.top ? index_of(H, r, k0 + j) : -1;
     const long long xa = r * H.x_stride;
-    if (vectors && H.dtype != CAPSCAPS_FP32) {
+    if (H.dtype != CAPSCAPS_FP32) {
         const unsigned short *x = static_cast<const unsigned short*>(H.x) + xa, *w = static_cast<const unsigned short*>(H.weight);
 #pragma unroll 2
-        for (int c = lane * 8; c < H.width; c += LANES * 8) {
-            const chunk_t a = *reinterpret_cast<const chunk_t*>(x + c);
+        for (int c = lane * 8; c + 8 <= H.width; c += LANES * 8) {
+            const chunk_t a = *reinterpret_cast<const Vector2*>(x + c);
             chunk_t b[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (cls[j] >= 0) b[j] = *reinterpret_cast<const chunk_t*>(w + cls[j] * H.weight_stride + c);
+                if (cls[j] >= 0) b[j] = *reinterpret_cast<const Vector2*>(w + cls[j] * H.weight_stride + c);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (cls[j] >= 0)
@@ -459,13 +480,12 @@ __device__ __forceinline__ void pick_entries(const Head& H, long long r, int k0,
                         }
                     }
         }
-    } else {
-        for (int c = lane; c < H.width; c += LANES) {
-            const float a = load_element(H.x, xa + c, H.dtype);
+    }
+    for (int c = (H.dtype != CAPSCAPS_FP32 ? H.width & ~7 : 0) + lane; c < H.width; c += LANES) {  // (16 bits: the rest)
+        const float a = load_element(H.x, xa + c, H.dtype);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (cls[j] >= 0) s[j] = __builtin_fmaf(a, load_element(H.weight, cls[j] * H.weight_stride + c, H.dtype), s[j]);
-        }
+        for (int j = 0; j < 4; ++j)
+            if (cls[j] >= 0) s[j] = __builtin_fmaf(a, load_element(H.weight, cls[j] * H.weight_stride + c, H.dtype), s[j]);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -482,13 +502,13 @@ __device__ __forceinline__ void pick_entries(const Head& H, long long r, int k0,
 
 // ... of all rows that are kept
 template <bool WIDE>
-__global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked, bool vectors)
+__global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked)
 {
     constexpr int LANES = WIDE ? THREADS : 64, PER = THREADS / LANES;
     __shared__ float parts[4][4];
     const long long kept = *H.count, quads = (H.top + 3) / 4;
     for (long long t = blockIdx.x * (long long)PER + threadIdx.x / LANES; t < kept * quads; t += gridDim.x * (long long)PER) {
-        pick_entries<LANES>(H, H.rows_of[t / quads], (int)(t % quads) * 4, picked, vectors, parts);
+        pick_entries<LANES>(H, H.rows_of[t / quads], (int)(t % quads) * 4, picked, parts);
         if constexpr (WIDE) __syncthreads();
     }
 }
@@ -527,15 +547,21 @@ __global__ void __launch_bounds__(THREADS) fold_kernel(Head H, Stat* stats, int 
     }
 }
 
-// loss, lse, logq of all rows, from stats[part][i] and the entries' z (which logq takes the place of, where it is wanted; PICK: and
-// are computed here, of rows with four entries at most, which spares a launch).
+// loss, lse, logq of all rows, from stats[part][i] and the entries' z: picked[r][k], which logq takes the place of where it is wanted;
+// computed here, of rows with four entries at most, which spares a launch; or of logits that lie in parts.
 // A workgroup for ROWS of the rows that are kept, and for the zeros of as many that are not (eight: whole 64-byte pieces of a
 // part's statistics; one where rows are few).
-template <int ROWS, bool PICK>
-__global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int parts, float* picked, bool vectors, float* loss,
+enum Entries { PICKED, PICK, PARTS };
+struct Parts {
+    const float* z;
+    long long ld, split;
+    int splits;
+};
+template <int ROWS, int ENTRIES>
+__global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats, int parts, float* picked, Parts logits, float* loss,
                                                        float* lse, float* logq)
 {
-    static_assert(ROWS == 1 || !PICK);
+    static_assert(ROWS == 1 || ENTRIES != PICK);
     __shared__ Stat joined[4][ROWS];
     __shared__ float lses[ROWS], sums[4][ROWS], products[4][4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -551,7 +577,7 @@ __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats
         }
         if (i0 >= kept) continue;
         const int rows = kept - i0 < ROWS ? (int)(kept - i0) : ROWS;
-        if constexpr (PICK) pick_entries<THREADS>(H, H.rows_of[i0], 0, picked, vectors, products);
+        if constexpr (ENTRIES == PICK) pick_entries<THREADS>(H, H.rows_of[i0], 0, picked, products);
         const Stat s = join_parts<ROWS>(stats, H.rows, parts, i0, rows, joined);
         if (threadIdx.x < ROWS) {
             lses[lane] = s.top + logf(s.sum);
@@ -563,8 +589,16 @@ __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats
             const long long r = H.rows_of[i0 + (lane & (ROWS - 1))];
             for (int k = threadIdx.x / ROWS; k < H.top; k += THREADS / ROWS) {
                 float l = 0.0f;
-                if (index_of(H, r, k) >= 0) {
-                    l = picked[r * H.top + k] * inv - lses[lane & (ROWS - 1)];
+                const long long cls = index_of(H, r, k);
+                if (cls >= 0) {
+                    float z = 0.0f;
+                    if constexpr (ENTRIES == PARTS) {
+                        z = sum_of_parts<float>(logits.z + (i0 + (lane & (ROWS - 1))) * logits.ld + cls, logits.split, logits.splits);
+                        if (H.bias != nullptr) z += H.bias[cls];
+                    } else {
+                        z = picked[r * H.top + k];
+                    }
+                    l = z * inv - lses[lane & (ROWS - 1)];
                     const float t = share_of(H, r, k);
                     if (t != 0.0f) cross += t * l;
                 }
@@ -594,7 +628,7 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
                                                            int padded_classes, unsigned short* gt, long long padded_rows,
                                                            int terms, float* sums)
 {
-    __shared__ float tile[64][65];
+    __shared__ float tile[64][65], part[4][64];
     const float inv = 1.0f / H.tau;
     const long long kept = *H.count;
     const int across = (padded_classes + 63) / 64;
@@ -603,25 +637,44 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
         const long long i0 = b / across * 64;
         const int c0 = (int)(b % across) * 64;
         if (i0 >= (kept + HEAD_K - 1) / HEAD_K * HEAD_K) continue;
+        // (four columns a thread, of four rows, a part of all at a time: what it waits for is their loads)
+        const int c = c0 + (threadIdx.x & 15) * 4;
+        float4v v[4];
+        float all[4], coef[4];
+        bool mine[4];
+        const float* from[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {  // (four columns a thread, of four rows)
-            const int i = u * 16 + (threadIdx.x >> 4), c = c0 + (threadIdx.x & 15) * 4;
-            float4v g = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (i0 + i < kept && c < classes) {
-                float4v v = g;
-                const float* from = z + (i0 + i) * ldz + c;  // (rows are a multiple of 32 long)
-#pragma unroll 4
-                for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const float4v*>(from + p * split);
-                const float all = lse[H.rows_of[i0 + i]], coef = H.coef[i0 + i];
+        for (int u = 0; u < 4; ++u) {
+            const long long i = i0 + u * 16 + (threadIdx.x >> 4);
+            mine[u] = i < kept && c < classes;
+            v[u] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            from[u] = z + (mine[u] ? i : i0) * ldz + (mine[u] ? c : 0);  // (rows are a multiple of 32 long)
+            all[u] = lse[H.rows_of[mine[u] ? i : 0]], coef[u] = H.coef[mine[u] ? i : 0];
+        }
+        auto add = [&](int p, auto COUNT) {
+            constexpr int N = decltype(COUNT)::value;
+            float4v more[N][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (H.bias != nullptr && c + j < classes) v[j] += H.bias[first + c + j];
-                    const float l = __builtin_fmaf(v[j], inv, -all);
-                    g[j] = c + j < classes ? coef * expf(l) : 0.0f;
-                }
-            }
+            for (int q = 0; q < N; ++q)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) tile[i][(threadIdx.x & 15) * 4 + j] = g[j];
+                for (int u = 0; u < 4; ++u) more[q][u] = *reinterpret_cast<const float4v*>(from[u] + (p + q) * split);
+            __builtin_amdgcn_sched_barrier(0);  // (all on their way before the first is waited for)
+#pragma unroll
+            for (int q = 0; q < N; ++q)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) v[u] += more[q][u];
+        };
+        int p = 0;
+        for (; p + 4 <= splits; p += 4) add(p, std::integral_constant<int, 4>());
+        for (; p < splits; ++p) add(p, std::integral_constant<int, 1>());
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool in = c + j < classes;
+            const float b = H.bias != nullptr && in ? H.bias[first + c + j] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                tile[u * 16 + (threadIdx.x >> 4)][(threadIdx.x & 15) * 4 + j] =
+                    mine[u] && in ? coef[u] * expf(__builtin_fmaf(v[u][j] + b, inv, -all[u])) : 0.0f;
         }
         __syncthreads();
         for (int t = threadIdx.x; t < 2 * 64 * 8; t += THREADS) {
@@ -637,10 +690,15 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
                 put_gradients<TERMS>(gn, i0 + a, c0 + k, padded_classes / HEAD_K, terms, H.dtype, f);
             }
         }
-        if (sums != nullptr && threadIdx.x < 64 && c0 + threadIdx.x < classes) {
+        if (sums != nullptr) {  // (a wave for sixteen rows)
+            const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
             float s = 0.0f;
-            for (int i = 0; i < 64; ++i) s += tile[i][threadIdx.x];
-            sums[b / across * padded_classes + c0 + threadIdx.x] = s;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s += tile[wave * 16 + i][lane];
+            part[wave][lane] = s;
+            __syncthreads();
+            if (wave == 0 && c0 + lane < classes)
+                sums[b / across * padded_classes + c0 + lane] = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
         }
         __syncthreads();
     }
@@ -714,7 +772,16 @@ __device__ __forceinline__ void bias_of(const Bias& B, const int* count, unsigne
     if (c >= B.classes) return;
     const long long tiles = (*count + B.tile_rows - 1) / B.tile_rows;
     double s = 0.0;
-    for (long long t = 0; t < tiles; ++t) s += B.sums[t * B.padded_classes + c];
+    long long t = 0;
+    for (; t + 8 <= tiles; t += 8) {
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = B.sums[(t + q) * B.padded_classes + c];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s += v[q];
+    }
+    for (; t < tiles; ++t) s += B.sums[t * B.padded_classes + c];
     s -= (double)B.taken[B.first + c] * 0x1p-24;
     B.dbias[B.first + c] = (float)(s * __builtin_bit_cast(float, count[1]));
 }
@@ -740,7 +807,7 @@ __device__ __forceinline__ void finish(const Finish& F, const int* count, int dt
         const long long i = F.pos != nullptr ? F.pos[r] : r;
         float4v v = {0, 0, 0, 0};
         if (i >= 0 && !none) {
-            for (int p = 0; p < F.splits; ++p) v += *reinterpret_cast<const float4v*>(F.sums + p * F.split + i * F.ld + c);
+            v = sum_of_parts<float4v>(F.sums + i * F.ld + c, F.split, F.splits);
             v *= scale;
         }
         const long long at = r * F.columns + c;
@@ -982,9 +1049,8 @@ hipError_t pack(const Plan& P, const void* from, long long stride, int columns, 
     const int* count = kept != nullptr ? kept->count : nullptr;
     const long long stages = P.padded / HEAD_K;
     const unsigned blocks = blocks_for((rows + 15) / 16 * stages, 4);
-    const bool vectors = vectors_of(from, stride, dtype);
-    return P.terms == 3 ? run(pack_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors)
-                        : run(pack_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages, vectors);
+    return P.terms == 3 ? run(pack_kernel<true>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages)
+                        : run(pack_kernel<false>, blocks, THREADS, st, from, stride, columns, rows, rows_of, count, to, stages);
 }
 Across across_of(const Plan& P, const void* from, long long stride, int columns, long long rows, const Head* kept, unsigned short* to,
                  long long padded, unsigned short* straight)
@@ -994,7 +1060,6 @@ Across across_of(const Plan& P, const void* from, long long stride, int columns,
     if (kept != nullptr) A.rows_of = kept->rows_of, A.count = kept->count;
     A.to = to, A.stages = padded / HEAD_K;
     A.straight = straight, A.straight_stages = P.padded / HEAD_K;
-    A.vectors = vectors_of(from, stride, P.terms == 3 ? CAPSCAPS_FP32 : CAPSCAPS_BF16);
     A.blocks = blocks_for((padded + 63) / 64 * ((columns + 63) / 64), 1);
     return A;
 }
@@ -1066,15 +1131,18 @@ int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, 
             CAPSCAPS_TRY(run(few ? fold_kernel<1> : fold_kernel<8>, blocks_for(H.rows, few ? 1 : 8), THREADS, st, H, P.stats,
                              ceil_div(classes, head_tile_shape(P.z.tile).stat_columns), piece > 0));
     }
-    const bool vectors = vectors_of(H.x, H.x_stride, H.dtype) && vectors_of(H.weight, H.weight_stride, H.dtype) && H.width % 8 == 0;
     // (the entries' z: where logq goes, or in the workspace)
     float* const picked = logq != nullptr ? logq : P.picked;
     const long long quads = H.rows * ((H.top + 3) / 4);
-    const bool pick = few && H.top <= 4;
-    if (!pick)
-        CAPSCAPS_TRY(run(quads < 1024 ? pick_kernel<true> : pick_kernel<false>, blocks_for(quads, quads < 1024 ? 1 : 4), THREADS, st, H, picked, vectors));
-    CAPSCAPS_TRY(run(pick ? loss_kernel<1, true> : few ? loss_kernel<1, false> : loss_kernel<8, false>, blocks_for(H.rows, few ? 1 : 8), THREADS,
-                     st, H, (const Stat*)P.stats, P.pieces > 1 ? 1 : P.stat_parts, picked, vectors, loss, lse, logq));
+    const bool pick = !P.in_parts && few && H.top <= 4;
+    if (!P.in_parts && !pick)
+        CAPSCAPS_TRY(run(quads < 1024 ? pick_kernel<true> : pick_kernel<false>, blocks_for(quads, quads < 1024 ? 1 : 4), THREADS, st, H, picked));
+    const auto kernel = P.in_parts ? (few ? loss_kernel<1, PARTS> : loss_kernel<8, PARTS>)
+                        : pick     ? loss_kernel<1, PICK>
+                                   : (few ? loss_kernel<1, PICKED> : loss_kernel<8, PICKED>);
+    const Parts logits{P.logits, P.piece, H.rows * P.piece, P.z.splits};
+    CAPSCAPS_TRY(run(kernel, blocks_for(H.rows, few ? 1 : 8), THREADS, st, H, (const Stat*)P.stats, P.pieces > 1 ? 1 : P.stat_parts, picked,
+                     logits, loss, lse, logq));
     return CAPSCAPS_OK;
 }
 
