@@ -14,6 +14,11 @@
 // chunk of 16 rows touch 16 different 16-byte columns of the banks.  Operands in blocks lie so in memory; of one that is
 // rows, four neighbouring lanes of a copy bring a row's 64 bytes.  The n side is the matrix instruction's row operand, so that a lane ends up with runs of four
 // neighbouring n of one m.
+//
+// Bound on large products: the matrix pipes, at the clock that the power limit leaves.  6144 x 131072 x 4096 in bf16 with the
+// statistics as its end takes 4.9 ms (1340 TFLOP/s; a library's product of 8192 x 16384 x 4096 runs at 1310 on the same card), and
+// 8192 x 65536 x 2048 with the gradients, whose 2 GB of 16-bit values nothing overlaps, 2.2 ms (1000 TFLOP/s).  One row against 50000 of
+// 4096 values, on tiles of 64 x 128, takes 84 us, 4.9 TB/s of weights.
 #pragma once
 #include "head_gemm.h"
 

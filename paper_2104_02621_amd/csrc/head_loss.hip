@@ -500,7 +500,7 @@ __device__ __forceinline__ void pick_entries(const Head& H, long long r, int k0,
     }
 }
 
-// ... of all rows that are kept
+// ... of all rows that are kept (3686 rows of 64 entries, 2048 bf16 values wide: 138 us, 7 TB/s of rows of the weights out of the caches)
 template <bool WIDE>
 __global__ void __launch_bounds__(THREADS) pick_kernel(Head H, float* picked)
 {
@@ -706,7 +706,7 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
 
 // ... with them: g = coef (exp(logq) - share) at the rows' entries in the piece.  An index that comes twice is one
 // entry with both shares, written by the first.  `taken`: sums of coef share over rows for each class, as whole numbers of
-// 2^-24 (their order does not matter then).  A wave for a row.
+// 2^-24 (their order does not matter then).  A wave for a row; 4 us for few rows (a launch's time), 35 to 39 for 3686 rows of 64 entries.
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* loss, const float* logq, long long first,
                                                           int classes, unsigned short* gn, int padded_classes,
