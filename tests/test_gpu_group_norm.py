@@ -97,6 +97,13 @@ def test_shapes(shape, types):
 
 
 @pytest.mark.parametrize("types", TYPES, ids=IDS)
+@pytest.mark.parametrize("positions", [240, 560])
+def test_many_images_of_odd_groups(positions, types):
+    """Vectors that straddle groups: slabs that share a CU, and that would fill it alone."""
+    Case(520, positions, 120, 4, types).check()
+
+
+@pytest.mark.parametrize("types", TYPES, ids=IDS)
 @pytest.mark.parametrize("kind", ACTS)
 @pytest.mark.parametrize("affine", [True, False])
 def test_activations(kind, affine, types):

@@ -119,6 +119,14 @@ def test_distillation(shape, top, tau, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
+@pytest.mark.parametrize("shape", [(60, 2000, 444), (269, 1100, 397), (600, 72, 17), (1500, 130, 700)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("top", [None, 17])
+def test_small_products(shape, top, dtype):
+    """Gradients of rows and weights in one launch, contracted lengths in parts, entries' logits from these."""
+    Case(*shape, dtype, top=top, bias=True, left=0.2).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES.get)
 @pytest.mark.parametrize("gap,shift", [(8, 0), (5, 0), (0, 3), (1, 1), (64, 8)])
 def test_strides_and_addresses(gap, shift, dtype):
     Case(70, 64, 300, dtype, gap=gap, shift=shift, left=0.1).check()
