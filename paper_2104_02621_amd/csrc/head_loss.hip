@@ -30,6 +30,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int MOST_TOP = 1024;
+constexpr int STATS_CHUNK = 16384;  // classes of a row whose statistics a workgroup joins
 constexpr int FEW = 256;  // rows or classes whose gradients are two terms of 16 bits
 // (256 rows of an operand are within a signed 32-bit offset: rows of up to 2^20 values of three terms)
 constexpr long long MOST_ROWS = 1 << 20, MOST_PIECE = 1 << 20;
@@ -384,6 +385,136 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(Across a, Acro
             clear[t] = 0;
 }
 
+// ---------------------------------------------------------------------------------------- few rows of fp32
+// Up to 64 rows of fp32 are multiplied by the fp32 matrix instructions with the weights read once, as they lie: written out as
+// three terms and read by six products they would move five times the bytes, and the weights are all that counts here.
+constexpr int FEW_FP32 = 64;
+
+__device__ __forceinline__ float4v load_four(const float* p, long long left)
+{
+    if (left >= 4) return *reinterpret_cast<const Vector4*>(p);
+    float4v v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < left) v[k] = p[k];
+    return v;
+}
+
+// z[part][row][class] of T tiles of 16 rows.  A wave: 32 classes, which are the instruction's rows; a lane holds four values of the
+// contracted width of its class and of its row in each tile, taken up one by one (their order does not matter).
+template <int T>
+__global__ void __launch_bounds__(THREADS) few_logits_kernel(Head H, float* z, long long ldz, int splits, long long split)
+{
+    const int lane = threadIdx.x & 63, at = lane & 15, kq = (lane >> 4) * 4;
+    const int kept = *H.count, part = blockIdx.x % splits;
+    const long long n0 = (long long)(blockIdx.x / splits) * 128 + (threadIdx.x >> 6) * 32;
+    const int steps = (H.width + 15) / 16, per = (steps + splits - 1) / splits;
+    const int begin = part * per, end = begin + per < steps ? begin + per : steps;
+    const float *w[2], *x[T];
+    bool has_w[2], has_x[T];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        const long long n = n0 + a * 16 + at;
+        has_w[a] = n < H.classes;
+        w[a] = static_cast<const float*>(H.weight) + (has_w[a] ? n : 0) * H.weight_stride + kq;
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        has_x[t] = t * 16 + at < kept;
+        x[t] = static_cast<const float*>(H.x) + (has_x[t] ? (long long)H.rows_of[t * 16 + at] : 0) * H.x_stride + kq;
+    }
+    float4v acc[2][T];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int t = 0; t < T; ++t) acc[a][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    const float4v none = {0.0f, 0.0f, 0.0f, 0.0f};
+    float4v wv[2], xv[T];
+    auto load = [&](int step) {
+        const int k = step * 16, left = step < end ? H.width - k - kq : 0;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) wv[a] = has_w[a] ? load_four(w[a] + k, left) : none;
+#pragma unroll
+        for (int t = 0; t < T; ++t) xv[t] = has_x[t] ? load_four(x[t] + k, left) : none;
+    };
+    load(begin);
+    for (int step = begin; step < end; ++step) {
+        float4v wn[2], xn[T];
+#pragma unroll
+        for (int a = 0; a < 2; ++a) wn[a] = wv[a];
+#pragma unroll
+        for (int t = 0; t < T; ++t) xn[t] = xv[t];
+        load(step + 1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int a = 0; a < 2; ++a)
+#pragma unroll
+                for (int t = 0; t < T; ++t) acc[a][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(wn[a][j], xn[t][j], acc[a][t], 0, 0, 0);
+    }
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        const long long n = n0 + a * 16 + kq;
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+            if (n < H.classes && t * 16 + at < kept) *reinterpret_cast<float4v*>(z + part * split + (t * 16 + at) * ldz + n) = acc[a][t];
+    }
+}
+
+// dx[part][row][column] = sum over a part's classes of g[row][class] W[class][column].  A wave: 64 columns, of which a lane loads four
+// neighbouring ones of a class at a time; columns 4 i + c are the rows of one instruction.
+template <int T>
+__global__ void __launch_bounds__(THREADS) few_rows_kernel(Head H, const float* g, long long ldg, float* dx, long long ld, int splits,
+                                                           long long split)
+{
+    const int lane = threadIdx.x & 63, at = lane & 15, kq = (lane >> 4) * 4;
+    const int kept = *H.count, part = blockIdx.x % splits;
+    const int h0 = (blockIdx.x / splits) * 256 + (threadIdx.x >> 6) * 64, left = H.width - h0 - at * 4;
+    const int steps = (int)((H.classes + 15) / 16), per = (steps + splits - 1) / splits;
+    const int begin = part * per, end = begin + per < steps ? begin + per : steps;
+    float4v acc[4][T];
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int t = 0; t < T; ++t) acc[c][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    const float4v none = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float* const w = static_cast<const float*>(H.weight) + h0 + at * 4;
+    float4v wv[4], gv[T];
+    auto load = [&](int step) {
+        const long long n = step * 16ll + kq;
+        const bool some = step < end;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) wv[q] = some && n + q < H.classes && left > 0 ? load_four(w + (n + q) * H.weight_stride, left) : none;
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+            gv[t] = some && t * 16 + at < kept ? load_four(g + (t * 16 + at) * ldg + n, H.classes - n) : none;
+    };
+    load(begin);
+    for (int step = begin; step < end; ++step) {
+        float4v wn[4], gn[T];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) wn[q] = wv[q];
+#pragma unroll
+        for (int t = 0; t < T; ++t) gn[t] = gv[t];
+        load(step + 1);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int t = 0; t < T; ++t) acc[c][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(wn[q][c], gn[t][q], acc[c][t], 0, 0, 0);
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int h = h0 + (kq + r) * 4;
+            if (t * 16 + at < kept && h < H.width)  // (rows of dx are whole vectors)
+                *reinterpret_cast<float4v*>(dx + part * split + (t * 16 + at) * ld + h) =
+                    float4v{acc[0][t][r], acc[1][t][r], acc[2][t][r], acc[3][t][r]};
+        }
+}
+
 // ---------------------------------------------------------------------------------------- forward
 typedef HeadStat Stat;
 __device__ __forceinline__ Stat join(const Stat& a, const Stat& b)
@@ -418,7 +549,7 @@ __device__ __forceinline__ V sum_of_parts(const float* from, long long split, in
     return sum;
 }
 
-// stats[i] of logits that lie in parts.  A workgroup for a row.
+// stats[chunk][i] of logits that lie in parts.  A workgroup for STATS_CHUNK classes of a row.
 __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, long long ldz, int splits, long long split,
                                                         Stat* stats)
 {
@@ -426,9 +557,12 @@ __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float inv = 1.0f / H.tau;
     const long long kept = *H.count;
-    for (long long i = blockIdx.x; i < kept; i += gridDim.x) {
+    const int chunks = (int)((H.classes + STATS_CHUNK - 1) / STATS_CHUNK);
+    for (long long t = blockIdx.x; t < kept * chunks; t += gridDim.x) {
+        const long long i = t / chunks, first = t % chunks * STATS_CHUNK;
+        const long long end = first + STATS_CHUNK < H.classes ? first + STATS_CHUNK : H.classes;
         Stat s = {-__builtin_inff(), 0.0f};
-        for (long long c = threadIdx.x; c < H.classes; c += THREADS) {
+        for (long long c = first + threadIdx.x; c < end; c += THREADS) {
             float v = sum_of_parts<float>(z + i * ldz + c, split, splits);
             if (H.bias != nullptr) v += H.bias[c];
             v *= inv;
@@ -440,7 +574,7 @@ __global__ void __launch_bounds__(THREADS) stats_kernel(Head H, const float* z, 
         s = wave_join(s);
         if (lane == 0) joined[wave] = s;
         __syncthreads();
-        if (threadIdx.x == 0) stats[i] = join(join(joined[0], joined[1]), join(joined[2], joined[3]));
+        if (threadIdx.x == 0) stats[t % chunks * H.rows + i] = join(join(joined[0], joined[1]), join(joined[2], joined[3]));
         __syncthreads();
     }
 }
@@ -626,7 +760,7 @@ template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* lse, const float* z, long long ldz, int splits,
                                                            long long split, long long first, int classes, unsigned short* gn,
                                                            int padded_classes, unsigned short* gt, long long padded_rows,
-                                                           int terms, float* sums)
+                                                           int terms, float* sums, float* raw)
 {
     __shared__ float tile[64][65], part[4][64];
     const float inv = 1.0f / H.tau;
@@ -676,6 +810,13 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
                 tile[u * 16 + (threadIdx.x >> 4)][(threadIdx.x & 15) * 4 + j] =
                     mine[u] && in ? coef[u] * expf(__builtin_fmaf(v[u][j] + b, inv, -all[u])) : 0.0f;
         }
+        if (raw != nullptr)  // (where the first part's logits were, which only this thread reads)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (mine[u]) {
+                    const float* const g = tile[u * 16 + (threadIdx.x >> 4)] + (threadIdx.x & 15) * 4;
+                    *reinterpret_cast<float4v*>(raw + (from[u] - z)) = float4v{g[0], g[1], g[2], g[3]};
+                }
         __syncthreads();
         for (int t = threadIdx.x; t < 2 * 64 * 8; t += THREADS) {
             const bool across_rows = t >= 64 * 8;
@@ -710,7 +851,7 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* loss, const float* logq, long long first,
                                                           int classes, unsigned short* gn, int padded_classes,
-                                                          unsigned short* gt, long long padded_rows, int terms, long long* taken)
+                                                          unsigned short* gt, long long padded_rows, int terms, long long* taken, float* raw, long long ldr)
 {
     const int lane = threadIdx.x & 63;
     const long long kept = *H.count;
@@ -731,6 +872,7 @@ __global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* l
             if (again) continue;
             const float q = expf(logq != nullptr ? logq[r * H.top + k] : -loss[r]);
             const float g = H.coef[i] * (q - t);
+            if (raw != nullptr) raw[i * ldr + c] = g;
             unsigned short v[3];
             if constexpr (TERMS) {
                 const float xs = g * SPLIT_SCALE;
@@ -945,6 +1087,7 @@ struct Plan {
     int terms, padded;  // terms of an operand's value, contracted width
     int grad_terms;     // ... of a gradient
     bool in_parts;      // logits in parts: few enough to lie in memory
+    bool few;           // few rows of fp32
     long long piece;    // classes of a piece
     int pieces, stat_parts;
     long long padded_rows;
@@ -983,11 +1126,15 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     P.piece = std::min<long long>(round_up(A.classes, HEAD_K), P.piece);
     // (a piece's statistics: 8 bytes for as few as 32 classes of a row)
     if (!backward) P.piece = std::min(P.piece, std::max<long long>(256, PIECE_BYTES / 8 / rows * 32 / 256 * 256));
+    P.few = P.terms == 3 && rows <= FEW_FP32 && A.classes <= MOST_PIECE && A.classes <= (1ll << 38) / A.width;
+    if (P.few) P.piece = round_up(A.classes, HEAD_K);
     P.pieces = (int)((A.classes + P.piece - 1) / P.piece);
     const long long most = std::min<long long>(P.piece, A.classes);
     P.z = pick_tile({rows, most, A.width, P.terms, P.pieces == 1 && A.classes <= MOST_IN_PARTS && rows * P.piece * 64 * 4 <= PIECE_BYTES, 6.0});
-    P.in_parts = P.z.splits > 1;
-    P.stat_parts = P.in_parts ? 1 : ceil_div(most, head_tile_shape(P.z.tile).stat_columns);  // of a piece
+    // (of few rows: about four workgroups on a CU, parts of at least 256 values)
+    if (P.few) P.z.splits = (int)std::min<long long>(std::max(1, A.width / 256), std::max<long long>(1, 1024 / ceil_div(A.classes, 128)));
+    P.in_parts = P.few || P.z.splits > 1;
+    P.stat_parts = P.in_parts ? ceil_div(most, STATS_CHUNK) : ceil_div(most, head_tile_shape(P.z.tile).stat_columns);  // of a piece
     Layout L{static_cast<char*>(base)};
     Head unused;
     Head& W = H != nullptr ? *H : unused;
@@ -999,7 +1146,7 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     W.entropy = distill ? L.take<float>(A.rows) : nullptr;
     const long long stages = (long long)P.terms * P.padded / HEAD_K;
     P.x = L.take<unsigned short>(head_block_values(rows, stages));
-    P.w = L.take<unsigned short>(head_block_values(most, stages));
+    P.w = L.take<unsigned short>(P.few ? 0 : head_block_values(most, stages));
     P.logits = P.in_parts ? L.take<float>(rows * P.piece * P.z.splits) : nullptr;
     if (!backward) {
         P.stats = L.take<Stat>(rows * (P.stat_parts + (P.pieces > 1)));
@@ -1012,14 +1159,16 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     const Product dw{most, A.width, rows, P.grad_terms, true, 3.0};
     double apart = 0.0, together = 0.0;
     P.dx = pick_tile(dx, &apart), P.dw = pick_tile(dw, &apart);
-    if (P.pieces == 1) {
+    if (P.few) {
+        P.dx.splits = (int)std::min<long long>(std::max<long long>(1, A.classes / 256), std::max(1, 1024 / ceil_div(A.width, 256)));
+    } else if (P.pieces == 1) {
         const Two two = pick_two(dx, dw, &together);
         if (together < apart) P.pair = true, P.dx = two.a, P.dw = two.b;
     }
     const long long ld = round_up(A.width, 4);
     const long long row_stages = P.terms * P.padded_rows / HEAD_K, class_stages = P.terms * round_up(P.piece, HEAD_K) / HEAD_K;
     P.xt = L.take<unsigned short>(head_block_values(A.width, row_stages));
-    P.wt = L.take<unsigned short>(head_block_values(A.width, class_stages));
+    P.wt = L.take<unsigned short>(P.few ? 0 : head_block_values(A.width, class_stages));
     P.gn = L.take<unsigned short>(head_block_values(rows, class_stages / P.terms * P.grad_terms));
     P.gt = L.take<unsigned short>(head_block_values(most, row_stages / P.terms * P.grad_terms));
     P.dx_sums = L.take<float>(rows * ld * P.dx.splits);
@@ -1069,6 +1218,24 @@ const void* weight_at(const Head& H, long long cls)
     return static_cast<const char*>(H.weight) + cls * H.weight_stride * (long long)element_bytes(H.dtype);
 }
 
+hipError_t few_logits(const Head& H, const Plan& P, hipStream_t st)
+{
+    const auto kernel = H.rows <= 16   ? few_logits_kernel<1>
+                        : H.rows <= 32 ? few_logits_kernel<2>
+                        : H.rows <= 48 ? few_logits_kernel<3>
+                                       : few_logits_kernel<4>;
+    return run(kernel, (unsigned)(ceil_div(H.classes, 128) * P.z.splits), THREADS, st, H, P.logits, P.piece, P.z.splits, H.rows * P.piece);
+}
+hipError_t few_rows(const Head& H, const Plan& P, long long ld, hipStream_t st)
+{
+    const auto kernel = H.rows <= 16   ? few_rows_kernel<1>
+                        : H.rows <= 32 ? few_rows_kernel<2>
+                        : H.rows <= 48 ? few_rows_kernel<3>
+                                       : few_rows_kernel<4>;
+    return run(kernel, (unsigned)(ceil_div(H.width, 256) * P.dx.splits), THREADS, st, H, (const float*)P.logits, P.piece, P.dx_sums, ld,
+               P.dx.splits, H.rows * ld);
+}
+
 // The rows that count
 int begin(const Head& H, const Plan& P, const float* dloss, long long dloss_stride, hipStream_t st)
 {
@@ -1116,16 +1283,20 @@ int forward(const Head& H, const Plan& P, float* loss, float* lse, float* logq, 
     const bool few = H.rows < 512;
     int rc = begin(H, P, nullptr, 0, st);
     if (rc != CAPSCAPS_OK) return rc;
-    CAPSCAPS_TRY(pack(P, H.x, H.x_stride, H.width, H.rows, &H, H.dtype, P.x, st));
+    if (!P.few) CAPSCAPS_TRY(pack(P, H.x, H.x_stride, H.width, H.rows, &H, H.dtype, P.x, st));
     for (int piece = 0; piece < P.pieces; ++piece) {
         const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
         HeadGemm g;
-        rc = logits_of(H, P, first, classes, nullptr, g, st);
-        if (rc != CAPSCAPS_OK) return rc;
-        g.stats = P.pieces > 1 ? P.stats + H.rows : P.stats;
-        CAPSCAPS_TRY(launch_head_gemm(g, P.z.tile, P.in_parts ? HEAD_OUT : HEAD_STATS, st));
+        if (P.few) {
+            CAPSCAPS_TRY(few_logits(H, P, st));
+        } else {
+            rc = logits_of(H, P, first, classes, nullptr, g, st);
+            if (rc != CAPSCAPS_OK) return rc;
+            g.stats = P.pieces > 1 ? P.stats + H.rows : P.stats;
+            CAPSCAPS_TRY(launch_head_gemm(g, P.z.tile, P.in_parts ? HEAD_OUT : HEAD_STATS, st));
+        }
         if (P.in_parts)
-            CAPSCAPS_TRY(run(stats_kernel, blocks_for(H.rows, 1), THREADS, st, H, (const float*)P.logits, P.piece, P.z.splits,
+            CAPSCAPS_TRY(run(stats_kernel, blocks_for(H.rows * P.stat_parts, 1), THREADS, st, H, (const float*)P.logits, P.piece, P.z.splits,
                              H.rows * P.piece, P.stats));
         if (P.pieces > 1)
             CAPSCAPS_TRY(run(few ? fold_kernel<1> : fold_kernel<8>, blocks_for(H.rows, few ? 1 : 8), THREADS, st, H, P.stats,
@@ -1163,15 +1334,17 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
     Across x_across{};
     if (G.dweight != nullptr)
         x_across = across_of(P, H.x, H.x_stride, H.width, H.rows, &H, P.xt, P.padded_rows, P.x);
-    else
+    else if (!P.few)
         CAPSCAPS_TRY(pack(P, H.x, H.x_stride, H.width, H.rows, &H, H.dtype, P.x, st));
     unsigned clear = G.dbias != nullptr ? blocks_for(H.classes, THREADS) : 0;
     for (int piece = 0; piece < P.pieces; ++piece) {
         const long long first = piece * P.piece, classes = std::min<long long>(P.piece, H.classes - first);
         HeadGemm z;
         Across w_across{};
-        const int rc = logits_of(H, P, first, classes, G.dx != nullptr ? &w_across : nullptr, z, st);
-        if (rc != CAPSCAPS_OK) return rc;
+        if (!P.few) {
+            const int rc = logits_of(H, P, first, classes, G.dx != nullptr ? &w_across : nullptr, z, st);
+            if (rc != CAPSCAPS_OK) return rc;
+        }
         if (x_across.blocks + w_across.blocks + clear > 0)
             CAPSCAPS_TRY(run(pack_transposed_kernel<TERMS>, x_across.blocks + w_across.blocks + clear, THREADS, st, x_across, w_across, P.taken,
                              H.classes));
@@ -1179,10 +1352,10 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
         const int padded = (int)round_up(classes, HEAD_K);
         float* const sums = G.dbias != nullptr ? P.bias_sums : nullptr;
         if (P.in_parts) {
-            CAPSCAPS_TRY(launch_head_gemm(z, P.z.tile, HEAD_OUT, st));
+            CAPSCAPS_TRY(P.few ? few_logits(H, P, st) : launch_head_gemm(z, P.z.tile, HEAD_OUT, st));
             const long long tiles = (P.padded_rows + 63) / 64 * ((padded + 63) / 64);
             CAPSCAPS_TRY(run(gradient_kernel<TERMS>, blocks_for(tiles, 1), THREADS, st, H, G.lse, (const float*)P.logits, P.piece,
-                             P.z.splits, H.rows * P.piece, first, (int)classes, P.gn, padded, P.gt, P.padded_rows, P.grad_terms, sums));
+                             P.z.splits, H.rows * P.piece, first, (int)classes, P.gn, padded, P.gt, P.padded_rows, P.grad_terms, sums, P.few ? P.logits : nullptr));
         } else {
             z.coef = H.coef, z.lse = G.lse, z.rows_of = H.rows_of;
             z.gn = P.gn, z.gt = P.gt, z.planes_n = padded / HEAD_K, z.planes_t = (int)(P.padded_rows / HEAD_K), z.sums = sums;
@@ -1190,7 +1363,7 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
             CAPSCAPS_TRY(launch_head_gemm(z, P.z.tile, HEAD_GRADIENT, st));
         }
         CAPSCAPS_TRY(run(entries_kernel<TERMS>, blocks_for(H.rows, 4), THREADS, st, H, G.loss, G.logq, first, (int)classes, P.gn,
-                         padded, P.gt, P.padded_rows, P.grad_terms, G.dbias != nullptr ? P.taken : nullptr));
+                         padded, P.gt, P.padded_rows, P.grad_terms, G.dbias != nullptr ? P.taken : nullptr, P.few ? P.logits : nullptr, P.piece));
         Bias bias{};
         if (G.dbias != nullptr)
             bias = {P.bias_sums, P.taken, G.dbias, first, padded, P.in_parts ? 64 : head_tile_shape(P.z.tile).sum_rows, (int)classes,
@@ -1225,7 +1398,7 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
         if (P.pair && G.dx != nullptr && G.dweight != nullptr) {
             CAPSCAPS_TRY(launch_head_gemm_pair(x, w, P.dx.tile, st));
         } else {
-            if (G.dx != nullptr) CAPSCAPS_TRY(launch_head_gemm(x, P.dx.tile, HEAD_OUT, st));
+            if (G.dx != nullptr) CAPSCAPS_TRY(P.few ? few_rows(H, P, ld, st) : launch_head_gemm(x, P.dx.tile, HEAD_OUT, st));
             if (G.dweight != nullptr) CAPSCAPS_TRY(launch_head_gemm(w, P.dw.tile, HEAD_OUT, st));
         }
         const unsigned blocks = dx.blocks + dw.blocks + bias.blocks;
