@@ -434,7 +434,7 @@ int capscaps_group_norm_bwd(const capscaps_group_norm* norm, const capscaps_grou
  * Sums are held in fp32.  dtype is that of x, weight, dx and dweight.  The gradient of z is rounded to it once, piece by piece (where rows
  * or classes are 256 or fewer: to two terms of it, the rounding and that of what it leaves over; fp32: not rounded; fp32 values of 2^104 and more in magnitude count as infinite, and infinities there make their sums NaN).  Pointers are device pointers, aligned to their
  * elements (16 bits with whole 16-byte vectors, rows of a multiple of 32 values: read in place, else copied to the workspace); strides, in
- * elements, are those from row to row and >= 0.  Nothing overlaps.  Runs repeat bit for bit.  Stream and error rules as for the calls above.
+ * elements, are those from row to row and >= 0 (an input's rows may overlap, or be one row).  Outputs overlap nothing.  Runs repeat bit for bit.  Stream and error rules as for the calls above.
  */
 typedef struct capscaps_head {
     long long rows;     /* 0 .. 2^20 */

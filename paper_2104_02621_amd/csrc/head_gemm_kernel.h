@@ -122,7 +122,8 @@ __device__ __forceinline__ void head_gemm(const HeadGemm& G, int tiles_n, int bl
     const rsrc_t rs_a = blocks_of(G.a, G.stages_a, m0, m_end);
     rsrc_t rs_b;
     if constexpr (ROWS) {
-        const long long bytes = (G.n_rows - n0) * G.ldb;
+        // (up to the last row's last value: rows may lie closer than they are long, or all in one place)
+        const long long bytes = (G.n_rows - n0 - 1) * G.ldb + G.k * 2;
         rs_b = make_rsrc(static_cast<const char*>(G.b) + n0 * G.ldb, (unsigned)(bytes < 0x7fffffffll ? bytes : 0x7fffffffll));
     } else {
         rs_b = blocks_of(G.b, G.stages_b, n0, G.n_rows);
