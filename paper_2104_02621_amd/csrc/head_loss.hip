@@ -129,26 +129,25 @@ __global__ void __launch_bounds__(1024) rows_kernel(Head H, const float* dloss, 
     };
     float scale = 1.0f;
     if (dloss != nullptr) {
+        // (the largest that is finite: a row whose dloss is not says nothing about how the others are rounded)
         float top = 0.0f;
-        bool bad = false;
         for (long long r = threadIdx.x; r < H.rows; r += 1024)
             if (kept(r)) {
                 const float d = __builtin_fabsf(dloss[r * dloss_stride] * H.tau);
-                bad |= !(d <= 3.4e38f);
-                top = __builtin_fmaxf(top, d);
+                if (d < __builtin_inff()) top = __builtin_fmaxf(top, d);
             }
-        top = wave_max(bad ? __builtin_inff() : top);
+        top = wave_max(top);
         if (lane == 0) tops[wave] = top;
         __syncthreads();
         top = 0.0f;
         for (int k = 0; k < 16; ++k) top = __builtin_fmaxf(top, tops[k]);
         float back = 1.0f;
-        if (top >= 1e-33f && top <= 3.4e38f && H.dtype != CAPSCAPS_FP32) {
+        if (top >= 1e-33f && H.dtype != CAPSCAPS_FP32) {
             // just below 2^14: the values that weigh most, those of the largest dloss at an entry of a row that has not been
             // learnt, then have the longest mantissas, whose rounding is half that of the shortest
             scale = 16352.0f / top;
             back = top * (1.0f / 16352.0f);
-        } else if (top > 0.0f && top <= 3.4e38f) {
+        } else if (top > 0.0f) {
             int e = 127 + 13 - (int)(__builtin_bit_cast(unsigned, top) >> 23);
             e = e > 126 ? 126 : e;
             scale = __builtin_bit_cast(float, (unsigned)(127 + e) << 23);
