@@ -429,7 +429,7 @@ int capscaps_group_norm_bwd(const capscaps_group_norm* norm, const capscaps_grou
  * counts, or whose entries' teacher logits are all -infinity, is left out: its loss, lse and logq are 0, it has no gradient, and nothing of it
  * is computed; what stands in it does not matter.  An entry with t = 0 adds 0 to the loss.  An index that comes twice in a row is two entries.
  * Infinities and NaN of a row that counts make its loss NaN or infinite by the formulas (a row whose every class is ruled out: NaN), and those
- * of a row's gradient reach dweight.
+ * of a row's gradient reach dweight and dbias.
  *
  * Sums are held in fp32.  dtype is that of x, weight, dx and dweight.  The gradient of z is rounded to it once, piece by piece (where rows
  * or classes are 256 or fewer: to two terms of it, the rounding and that of what it leaves over; fp32: not rounded; fp32 values of 2^104 and more in magnitude count as infinite, and infinities there make their sums NaN).  Pointers are device pointers, aligned to their

@@ -452,6 +452,7 @@ __device__ __forceinline__ void head_gemm(const HeadGemm& G, int tiles_n, int bl
             const long long m = m0 + wm * WM + b * 32 + lr;
             const bool row = m < m_end;
             const float lse = row ? G.lse[G.rows_of[m]] : 0.0f, coef = row ? G.coef[m] : 0.0f;
+            const bool adds = row && __builtin_fabsf(coef) < __builtin_inff();  // (others: where the sums are added up)
             // row m at the wave's first class, without its chunk; stage of these 32 rows in gt
             unsigned short* const gn = G.gn + ((m >> 4) * sn + ((n0 + wn * WN) >> 5)) * 512 + (m & 15) * 32;
             const long long stage_t = (m0 + wm * WM + b * 32) >> 5;
@@ -462,7 +463,7 @@ __device__ __forceinline__ void head_gemm(const HeadGemm& G, int tiles_n, int bl
                 for (int r = 0; r < 16; ++r) {
                     const float l = __builtin_fmaf(acc[a][b][r], G.inv_tau, -lse);
                     v[r] = coef * (TERMS == 3 ? expf(l) : __expf(l));
-                    if (G.sums != nullptr) sums[a * 16 + r] += row ? v[r] : 0.0f;
+                    if (G.sums != nullptr) sums[a * 16 + r] += adds ? v[r] : 0.0f;
                     if constexpr (TERMS == 3) v[r] *= SPLIT_SCALE;
                 }
 #pragma unroll

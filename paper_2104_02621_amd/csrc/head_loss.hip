@@ -54,7 +54,7 @@ struct Head {
     long long teacher_stride;
     int teacher_dtype;
     // in the workspace
-    int *keep, *rows_of, *pos, *count;  // count: also the two scales, see rows_kernel
+    int *keep, *rows_of, *pos, *count, *boundless;  // see rows_kernel
     float *share, *entropy, *coef;
 };
 
@@ -68,6 +68,7 @@ __device__ __forceinline__ float share_of(const Head& H, long long row, int k)
 {
     return H.teacher != nullptr ? H.share[row * H.top + k] : 1.0f;
 }
+__device__ __forceinline__ bool finite(float v) { return __builtin_fabsf(v) < __builtin_inff(); }
 __device__ __forceinline__ float wave_max(float v)
 {
 #pragma unroll
@@ -118,12 +119,14 @@ __global__ void __launch_bounds__(THREADS) teacher_kernel(Head H)
 }
 
 // The rows that are kept, in their order: rows_of[i], pos[row] (-1: left out), count[0]; coef[i] = dloss tau times a scale,
-// count[1] the bits of one over it.  One workgroup.
+// count[1] the bits of one over it; boundless: the i whose coef is infinite or NaN, in any order, count[2] of them.  One workgroup.
 __global__ void __launch_bounds__(1024) rows_kernel(Head H, const float* dloss, long long dloss_stride)
 {
     __shared__ int sums[16];
     __shared__ float tops[16];
+    __shared__ int found;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (threadIdx.x == 0) found = 0;
     auto kept = [&](long long r) {
         return r < H.rows && (H.teacher != nullptr ? H.keep[r] != 0 : index_of(H, r, 0) >= 0);
     };
@@ -134,7 +137,7 @@ __global__ void __launch_bounds__(1024) rows_kernel(Head H, const float* dloss, 
         for (long long r = threadIdx.x; r < H.rows; r += 1024)
             if (kept(r)) {
                 const float d = __builtin_fabsf(dloss[r * dloss_stride] * H.tau);
-                if (d < __builtin_inff()) top = __builtin_fmaxf(top, d);
+                if (finite(d)) top = __builtin_fmaxf(top, d);
             }
         top = wave_max(top);
         if (lane == 0) tops[wave] = top;
@@ -171,10 +174,18 @@ __global__ void __launch_bounds__(1024) rows_kernel(Head H, const float* dloss, 
         if (r < H.rows) H.pos[r] = mine ? i : -1;
         if (mine) {
             H.rows_of[i] = (int)r;
-            if (dloss != nullptr) H.coef[i] = dloss[r * dloss_stride] * H.tau * scale;
+            if (dloss != nullptr) {
+                const float coef = dloss[r * dloss_stride] * H.tau * scale;
+                H.coef[i] = coef;
+                if (!finite(coef)) H.boundless[atomicAdd(&found, 1)] = i;
+            }
         }
     }
-    if (threadIdx.x == 0) H.count[0] = before;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        H.count[0] = before;
+        if (dloss != nullptr) H.count[2] = found;
+    }
 }
 
 // ---------------------------------------------------------------------------------------- operands
@@ -755,7 +766,7 @@ __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats
 
 // ---------------------------------------------------------------------------------------- backward
 // A piece's gradients without the entries' shares: g = coef exp(z - lse), as operands, rows innermost (gt) and classes
-// innermost (gn), and their sums over 64 rows (sums[row tile][class], for the bias).  Tiles of 64 x 64.
+// innermost (gn), and their sums over 64 rows but the boundless ones (sums[row tile][class], for the bias).  Tiles of 64 x 64.
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* lse, const float* z, long long ldz, int splits,
                                                            long long split, long long first, int classes, unsigned short* gn,
@@ -765,6 +776,7 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
     __shared__ float tile[64][65], part[4][64];
     const float inv = 1.0f / H.tau;
     const long long kept = *H.count;
+    const bool boundless = H.count[2] > 0;
     const int across = (padded_classes + 63) / 64;
     const long long tiles = (padded_rows + 63) / 64 * across;
     for (long long b = blockIdx.x; b < tiles; b += gridDim.x) {
@@ -835,7 +847,10 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
             const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
             float s = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s += tile[wave * 16 + i][lane];
+            for (int i = 0; i < 16; ++i) {
+                const long long row = i0 + wave * 16 + i;
+                if (!boundless || row >= kept || finite(H.coef[row])) s += tile[wave * 16 + i][lane];
+            }
             part[wave][lane] = s;
             __syncthreads();
             if (wave == 0 && c0 + lane < classes)
@@ -847,11 +862,13 @@ __global__ void __launch_bounds__(THREADS) gradient_kernel(Head H, const float* 
 
 // ... with them: g = coef (exp(logq) - share) at the rows' entries in the piece.  An index that comes twice is one
 // entry with both shares, written by the first.  `taken`: sums of coef share over rows for each class, as whole numbers of
-// 2^-24 (their order does not matter then).  A wave for a row; 4 us for few rows (a launch's time), 35 to 39 for 3686 rows of 64 entries.
+// 2^-24 (their order does not matter then), those of boundless rows left out; where a share is NaN the class's sum over the first rows
+// is made NaN instead.  A wave for a row; 4 us for few rows (a launch's time), 35 to 39 for 3686 rows of 64 entries.
 template <bool TERMS>
 __global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* loss, const float* logq, long long first,
                                                           int classes, unsigned short* gn, int padded_classes,
-                                                          unsigned short* gt, long long padded_rows, int terms, long long* taken, float* raw, long long ldr)
+                                                          unsigned short* gt, long long padded_rows, int terms, long long* taken,
+                                                          float* sums, float* raw, long long ldr)
 {
     const int lane = threadIdx.x & 63;
     const long long kept = *H.count;
@@ -891,24 +908,32 @@ __global__ void __launch_bounds__(THREADS) entries_kernel(Head H, const float* l
                 gn[head_block_at(i, c, terms * (padded_classes / HEAD_K)) + p * (padded_classes / HEAD_K) * 512ll] = v[p];
                 gt[head_block_at(c, i, terms * (padded_rows / HEAD_K)) + p * (padded_rows / HEAD_K) * 512] = v[p];
             }
-            if (taken != nullptr) {
-                const long long whole = (long long)__builtin_rintf(H.coef[i] * t * 0x1p24f);
-                atomicAdd(reinterpret_cast<unsigned long long*>(taken + cls), (unsigned long long)whole);
+            if (taken != nullptr && finite(H.coef[i])) {
+                if (t != t) {
+                    sums[c] = t;
+                } else {
+                    const long long whole = (long long)__builtin_rintf(H.coef[i] * t * 0x1p24f);
+                    atomicAdd(reinterpret_cast<unsigned long long*>(taken + cls), (unsigned long long)whole);
+                }
             }
         }
     }
 }
 
-// dbias of a piece
+// dbias of a piece: the sums over rows less the shares, and the boundless rows' gradients (infinite or NaN all of them) from the
+// operand that contracts rows, where they are whole
 struct Bias {
     const float* sums;
     const long long* taken;
+    const int* boundless;
+    const unsigned short* gt;
+    long long stages;  // of gt, all terms
     float* dbias;
     long long first;
     int padded_classes, tile_rows, classes;
     unsigned blocks;
 };
-__device__ __forceinline__ void bias_of(const Bias& B, const int* count, unsigned block)
+__device__ __forceinline__ void bias_of(const Bias& B, const int* count, int dtype, unsigned block)
 {
     const int c = block * THREADS + threadIdx.x;
     if (c >= B.classes) return;
@@ -925,6 +950,10 @@ __device__ __forceinline__ void bias_of(const Bias& B, const int* count, unsigne
     }
     for (; t < tiles; ++t) s += B.sums[t * B.padded_classes + c];
     s -= (double)B.taken[B.first + c] * 0x1p-24;
+    for (int k = 0; k < count[2]; ++k) {
+        const unsigned short g = B.gt[head_block_at(c, B.boundless[k], B.stages)];
+        s += dtype == CAPSCAPS_FP16 ? Element<CAPSCAPS_FP16>::get(g) : Element<CAPSCAPS_BF16>::get(g);
+    }
     B.dbias[B.first + c] = (float)(s * __builtin_bit_cast(float, count[1]));
 }
 
@@ -979,7 +1008,7 @@ __global__ void __launch_bounds__(THREADS) finish_kernel(const int* count, Finis
     else if (blockIdx.x < a.blocks + b.blocks)
         finish(b, count, dtype, blockIdx.x - a.blocks);
     else
-        bias_of(c, count, blockIdx.x - a.blocks - b.blocks);
+        bias_of(c, count, dtype, blockIdx.x - a.blocks - b.blocks);
 }
 
 // ---------------------------------------------------------------------------------------- host
@@ -1138,7 +1167,7 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     Layout L{static_cast<char*>(base)};
     Head unused;
     Head& W = H != nullptr ? *H : unused;
-    W.count = L.take<int>(2);
+    W.count = L.take<int>(3);
     W.rows_of = L.take<int>(A.rows);
     W.pos = L.take<int>(A.rows);
     W.keep = distill ? L.take<int>(A.rows) : nullptr;
@@ -1155,6 +1184,7 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
         return P;
     }
     W.coef = L.take<float>(A.rows);
+    W.boundless = L.take<int>(A.rows);
     const Product dx{rows, A.width, P.piece, P.grad_terms, P.pieces == 1, 0.0};  // (several: added up piece after piece)
     const Product dw{most, A.width, rows, P.grad_terms, true, 3.0};
     double apart = 0.0, together = 0.0;
@@ -1363,11 +1393,12 @@ int backward_pieces(const Head& H, const Plan& P, const Gradients& G, hipStream_
             CAPSCAPS_TRY(launch_head_gemm(z, P.z.tile, HEAD_GRADIENT, st));
         }
         CAPSCAPS_TRY(run(entries_kernel<TERMS>, blocks_for(H.rows, 4), THREADS, st, H, G.loss, G.logq, first, (int)classes, P.gn,
-                         padded, P.gt, P.padded_rows, P.grad_terms, G.dbias != nullptr ? P.taken : nullptr, P.few ? P.logits : nullptr, P.piece));
+                         padded, P.gt, P.padded_rows, P.grad_terms, G.dbias != nullptr ? P.taken : nullptr, sums, P.few ? P.logits : nullptr,
+                         P.piece));
         Bias bias{};
         if (G.dbias != nullptr)
-            bias = {P.bias_sums, P.taken, G.dbias, first, padded, P.in_parts ? 64 : head_tile_shape(P.z.tile).sum_rows, (int)classes,
-                    blocks_for(classes, THREADS)};
+            bias = {P.bias_sums, P.taken, H.boundless, P.gt, P.grad_terms * (P.padded_rows / HEAD_K), G.dbias, first, padded,
+                    P.in_parts ? 64 : head_tile_shape(P.z.tile).sum_rows, (int)classes, blocks_for(classes, THREADS)};
         HeadGemm x{}, w{};
         Finish dx{}, dw{};
         if (G.dx != nullptr) {
