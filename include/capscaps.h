@@ -419,7 +419,7 @@ int capscaps_group_norm_bwd(const capscaps_group_norm* norm, const capscaps_grou
  * x [rows][width], weight [classes][width], bias [classes] (fp32; NULL = zeros; -infinity rules a class out), z = x weight^T + bias
  * and tau the temperature,
  *
- *     lse  = log(sum over classes of exp(z / tau))             log q = z / tau - lse
+ *     lse  = log(sum over classes of exp(z / tau))             log q = z / tau - lse   (never above 0)
  *     loss = tau^2 * sum_k t_k (log t_k - log q[index_k])      t = softmax over the row's entries k of teacher_k / tau
  *
  * The class loss has one entry, the row's target, with t = 1 and tau = 1: loss = lse - z[target].  The logits, rows * classes

@@ -743,7 +743,10 @@ __global__ void __launch_bounds__(THREADS) loss_kernel(Head H, const Stat* stats
                     } else {
                         z = picked[r * H.top + k];
                     }
+                    // (no class is more likely than certain; z and lse come from sums of their own, and the difference of their roundings
+                    // may say so of a class that the row has learnt)
                     l = z * inv - lses[lane & (ROWS - 1)];
+                    l = l > 0.0f ? 0.0f : l;
                     const float t = share_of(H, r, k);
                     if (t != 0.0f) cross += t * l;
                 }
