@@ -811,11 +811,12 @@ GroupPlan group_plan(const capscaps_group_norm& G)
         // images of 1024 positions of 32 groups of 30 columns take 144 us in fp32 and 92 in bf16, in two passes 120 and 73;
         // with half the positions, two slabs a CU, 71 and 42, in two passes 65 and 46.
         const bool alone = FORWARD && !few && columns % v != 0 && threads * items > RESIDENT * 8;
-        if (items > 0 && !alone) {
+        const long long room = ((1ll << 32) - 1) / threads;  // workgroups: a launch has less than 2^32 threads
+        if (items > 0 && !alone && G.groups / k <= room) {
             P.v = v, P.items = items, P.threads = threads, P.rows = rows, P.vecs = (int)vecs, P.slab = (int)wide;
             P.whole = k, P.parts = 1, P.slabs = G.groups / k, P.fold = columns % v == 0 ? v : 1;
             // (backward: a workgroup takes one image after the other, and as many lanes as the registers of a CU hold are at work)
-            const int blocks = FORWARD ? MOST_BLOCKS : CUS * (RESIDENT_BACK / threads) * (items == 8 ? 1 : 2);
+            const long long blocks = FORWARD ? std::min<long long>(MOST_BLOCKS, room) : CUS * (RESIDENT_BACK / threads) * (items == 8 ? 1 : 2);
             P.shares = std::max<long long>(1, std::min<long long>(G.images, blocks / P.slabs));
             P.blocks = P.shares * P.slabs;
             return P;
@@ -944,6 +945,18 @@ hipError_t run_resident(const GroupCall& C, hipStream_t st)
 using namespace capscaps;
 
 extern "C" {
+
+// (for tests) the plan of one direction: workgroups and threads of the launch that takes most of them, and 1 where values stay in
+// registers, 0 where they are read twice; 0: an invalid norm
+int capscaps_testing_group_norm_launch(const capscaps_group_norm* norm, int forward, long long* blocks_threads_resident)
+{
+    if (check_group(norm) != CAPSCAPS_OK) return 0;
+    const GroupPlan P = forward ? group_plan<true>(*norm) : group_plan<false>(*norm);
+    blocks_threads_resident[0] = P.items > 0 ? P.blocks : grid_of(P.blocks);
+    blocks_threads_resident[1] = P.threads;
+    blocks_threads_resident[2] = P.items > 0;
+    return 1;
+}
 
 size_t capscaps_group_norm_fwd_workspace_bytes(const capscaps_group_norm* norm)
 {
