@@ -347,14 +347,15 @@ __global__ void __launch_bounds__(RESIDENT_BACK) group_bwd_resident_kernel(Group
 #pragma unroll
             for (int k = 0; k < V; ++k) s1[k] = s2[k] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < I; ++i)  // (vectors past the last position: dy = 0, which adds nothing)
+            for (int i = 0; i < I; ++i)
+                if (i < mine)  // (past the last position mean * rstd alone, which may be out of range, would make a NaN)
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const float off = v[i].value(k) - mean[k];
-                    da[i][k] = d[i].value(k) * act_slope(C.G.act, __builtin_fmaf(off, wr[k], bias[k]));
-                    s1[k] = __builtin_fmaf(da[i][k], off, s1[k]);
-                    s2[k] += da[i][k];
-                }
+                    for (int k = 0; k < V; ++k) {
+                        const float off = v[i].value(k) - mean[k];
+                        da[i][k] = d[i].value(k) * act_slope(C.G.act, __builtin_fmaf(off, wr[k], bias[k]));
+                        s1[k] = __builtin_fmaf(da[i][k], off, s1[k]);
+                        s2[k] += da[i][k];
+                    }
 #pragma unroll
             for (int k = 0; k < V; ++k) s1[k] *= rstd[k];
             if (q < P.rows) {

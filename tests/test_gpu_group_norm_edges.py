@@ -1,9 +1,11 @@
-"""The group norm at the edges of its range: more images than a launch has workgroups.  Needs an MI355X."""
+"""The group norm at the edges of its range: more images than a launch has workgroups, groups whose values are far larger than they
+differ.  Needs an MI355X."""
 import pytest
 import torch
 
 from paper_2104_02621_amd import capscaps as cc
-from tests.test_gpu_group_norm import BF16
+from tests import group_norm_ref as ref
+from tests.test_gpu_group_norm import BF16, FP16, FP32, NAMES, Case, close, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -18,3 +20,22 @@ def test_more_images_than_one_launch_has_workgroups_for(images):
     for part in r.y.split(1 << 20):
         assert bool((part == want.y).all())
     assert bool((r.mean == want.mean).all()) and bool((r.rstd == want.rstd).all())
+
+
+@pytest.mark.parametrize("layer", [FP32, BF16, FP16], ids=NAMES.get)
+@pytest.mark.parametrize("value", [2e36, -2e36])
+@pytest.mark.parametrize("shape", [(2, 5, 24, 3), (1, 3, 27, 1), (2, 7, 64, 4), (1, 1, 32, 1)])
+def test_gradients_of_large_equal_values(shape, value, layer):
+    """mean * rstd passes fp32's range, x - mean is 0: gradients are those of a group without variance."""
+    c = Case(*shape, (FP32, layer))
+    c.x.fill_(value)
+    r = c.forward()
+    assert bool(((r.mean - value).abs() <= 1e-6 * abs(value)).all())
+    mean = torch.full_like(r.mean, value)  # (the sum's rounding, 1e29 of 2e36, is no small distance)
+    rstd = torch.full_like(r.rstd, 1e-5 ** -0.5)
+    g = c.backward(cc.GroupNorm(r.y, mean, rstd))
+    dx, dw, db, edx, edw, edb = ref.backward(f64(c.x), c.groups, f64(mean), f64(rstd), f64(c.dy), f64(c.w), f64(c.b), "silu",
+                                             NAMES[layer])
+    close(g.dx, dx, edx, "dx")
+    close(g.dweight, dw, edw, "dweight")
+    close(g.dbias, db, edb, "dbias")
