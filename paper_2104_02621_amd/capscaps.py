@@ -77,7 +77,7 @@ class HeadArgs(ctypes.Structure):
     """capscaps_head"""
     _fields_ = ([("rows", ctypes.c_longlong)]
                 + _fields("width classes dtype index_bits top teacher_dtype", ctypes.c_int)
-                + [("temperature", ctypes.c_float)])
+                + [("temperature", ctypes.c_float), ("gradient_terms", ctypes.c_int)])
 
 
 _HEAD_TENSORS = (_fields("x weight bias index teacher", ctypes.c_void_p)
@@ -849,7 +849,7 @@ HeadGrads = namedtuple("HeadGrads", "dx dweight dbias")
 MOST_ROWS, MOST_WIDTH, MOST_CLASSES, MOST_TOP = 1 << 20, 1 << 20, 1 << 26, 1024
 
 
-def _head(x, weight, bias, index, teacher, temperature):
+def _head(x, weight, bias, index, teacher, temperature, gradient_terms=0):
     """(HeadArgs, what the tensors are as HeadFwdArgs and HeadBwdArgs have them): what both losses and directions check."""
     import torch
     gpu, device = _gpu_of(x), x.device
@@ -874,8 +874,10 @@ def _head(x, weight, bias, index, teacher, temperature):
         ts = _row_stride(teacher, (*shape, top), top, 1, "teacher_logits", gpu)
     if not 1e-6 <= temperature <= 1e6:
         raise ValueError("temperature is 1e-6 to 1e6")
+    if gradient_terms not in (0, 1, 2):
+        raise ValueError("gradient_terms is 1 or 2, or 0 for the rule")
     head = HeadArgs(rows, width, classes, _code(x.dtype), 64 if index.dtype == torch.int64 else 32, top, teacher_dtype,
-                    temperature)
+                    temperature, gradient_terms)
     return head, (x.data_ptr(), weight.data_ptr(), _vector(bias, classes, device, "bias"), index.data_ptr(), teacher_ptr,
                   _row_stride(x, x.shape, width, 1, "x", gpu), _row_stride(weight, weight.shape, width, 1, "weight", gpu),
                   ins, ts)
@@ -931,11 +933,15 @@ def class_loss_fwd(x, weight, targets, *, bias=None):
     return ClassLoss(loss, lse)
 
 
-def class_loss_bwd(x, weight, targets, loss, lse, dloss, *, bias=None, want_dx=True, want_dweight=True):
+def class_loss_bwd(x, weight, targets, loss, lse, dloss, *, bias=None, want_dx=True, want_dweight=True, gradient_terms=0):
     """The gradients of class_loss_fwd, from its arguments, what it returned and the gradient of the loss: float32, one for each row
     or one for all (a mean's: 1 / rows that have a target).  Returns HeadGrads(dx, dweight, dbias): dx and dweight in x's dtype
-    (None where not wanted), dbias float32, None without a bias."""
-    head, tensors = _head(x, weight, bias, targets, None, 1.0)
+    (None where not wanted), dbias float32, None without a bias.
+
+    In 16 bits the gradient of z, which the products for dx and dweight read, is rounded to x's dtype once (`gradient_terms` 1: about as
+    large an error again as that of storing dx and dweight), or held in two terms of it (2: no more than that one rounding, for
+    products of twice the length).  0 takes 2 where rows or classes are 256 or fewer, else 1."""
+    head, tensors = _head(x, weight, bias, targets, None, 1.0, gradient_terms)
     return _head_bwd(capscaps_class_loss_bwd, capscaps_class_loss_workspace_bytes(head, 1), x, weight, bias, head, tensors,
                      loss, lse, None, dloss, want_dx, want_dweight)
 
@@ -955,9 +961,9 @@ def distill_loss_fwd(x, weight, teacher_index, teacher_logits, *, bias=None, tem
 
 
 def distill_loss_bwd(x, weight, teacher_index, teacher_logits, lse, logq, dloss, *, bias=None, temperature=1.0, want_dx=True,
-                     want_dweight=True):
+                     want_dweight=True, gradient_terms=0):
     """The gradients of distill_loss_fwd, as class_loss_bwd's, from the lse and logq that it returned."""
-    head, tensors = _head(x, weight, bias, teacher_index, teacher_logits, temperature)
+    head, tensors = _head(x, weight, bias, teacher_index, teacher_logits, temperature, gradient_terms)
     return _head_bwd(capscaps_distill_loss_bwd, capscaps_distill_loss_workspace_bytes(head, 1), x, weight, bias, head, tensors,
                      None, lse, logq, dloss, want_dx, want_dweight)
 

@@ -603,7 +603,7 @@ hipError_t launch_type(const HeadGemm& g, hipStream_t st)
 {
     if (g.terms == 3) return launch<bf16_tag, BM, BN, NWM, NB, 3, false, END>(g, st);
     const bool bf16 = g.dtype == CAPSCAPS_BF16;
-    if constexpr (END == HEAD_OUT && BM < 256) {  // (few rows: the plan takes small tiles)
+    if constexpr (END == HEAD_OUT) {
         if (g.terms == 2)
             return bf16 ? launch<bf16_tag, BM, BN, NWM, NB, 2, false, END>(g, st) : launch<f16_tag, BM, BN, NWM, NB, 2, false, END>(g, st);
     }
