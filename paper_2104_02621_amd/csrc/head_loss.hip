@@ -399,8 +399,9 @@ __global__ void __launch_bounds__(THREADS) pack_transposed_kernel(Across a, Acro
 
 // ---------------------------------------------------------------------------------------- few rows of fp32
 // Up to 64 rows of fp32 are multiplied by the fp32 matrix instructions with the weights read once, as they lie: written out as
-// three terms and read by six products they would move five times the bytes, and the weights are all that counts here.
+// three terms and read by six products they would move five times the bytes, and large weights are all that counts here.
 // 50000 classes of 4096 values: 1 row 255 us forward and 622 back, by terms 958 and 2948; 40 rows 402 and 951, by terms 996 and 3254.
+// (Which heads take these kernels: few_of_fp32.)
 constexpr int FEW_FP32 = 64;
 
 __device__ __forceinline__ float4v load_four(const float* p, long long left)
@@ -1104,6 +1105,22 @@ int check_head(const capscaps_head* h, bool distill)
     return CAPSCAPS_OK;
 }
 
+// Whether up to 64 rows of fp32 are multiplied as they lie (few_logits_kernel, few_rows_kernel).  Backward that pays from 16 MB of weights
+// on for each of up to three tiles of 16 rows.  Times by terms and so, us: 1 row, 6.1 MB (12000 classes of 128 values) 53 and 51, 16.1 (6000 of
+// 672) 75 and 69, 32.3 (12000 of 672) 101 and 78; 40 rows, 4.8 MB (444 of 2680) 55 and 99, 32.3 MB 110 and 112, 53.8 MB (20000 of 672) 154 and 131; 64
+// rows, 1.2 MB (444 of 672) 44 and 110, 32.3 MB 116 and 123, 53.8 MB 156 and 147.  Forward the logits' own way to memory and back counts,
+// where the other path keeps them in registers (past 16384 classes) or the rows are short: 1 row, 20000 classes of 64 values 29 and 41, of 672 (53.8 MB)
+// 63 and 69, 40000 of 400 (64 MB) 76 and 56; 16000 of 128 values 31 and 40, of 256 61 and 47; 40 rows 33 and 47, 63 and 55, 40000 of
+// 400 77 and 78; 1216 classes of 64 values 29 and 26, of 4096 52 and 36.
+bool few_of_fp32(const capscaps_head& A, bool backward)
+{
+    if (A.dtype != CAPSCAPS_FP32 || A.rows > FEW_FP32 || A.classes > MOST_PIECE || A.classes > (1ll << 38) / A.width) return false;
+    const long long bytes = 4ll * A.classes * A.width;
+    if (backward) return bytes >= 16000000ll * std::min(3, std::max(1, ceil_div(A.rows, 16)));
+    if (A.classes <= MOST_IN_PARTS) return A.classes <= 4096 || A.width >= 256;
+    return bytes >= 60000000;
+}
+
 // The workspace, piece by piece
 struct Layout {
     char* base;
@@ -1160,7 +1177,7 @@ Plan make_plan(const capscaps_head& A, bool distill, bool backward, void* base, 
     P.piece = std::min<long long>(round_up(A.classes, HEAD_K), P.piece);
     // (a piece's statistics: 8 bytes for as few as 32 classes of a row)
     if (!backward) P.piece = std::min(P.piece, std::max<long long>(256, PIECE_BYTES / 8 / rows * 32 / 256 * 256));
-    P.few = P.terms == 3 && rows <= FEW_FP32 && A.classes <= MOST_PIECE && A.classes <= (1ll << 38) / A.width;
+    P.few = few_of_fp32(A, backward);
     if (P.few) P.piece = round_up(A.classes, HEAD_K);
     P.pieces = (int)((A.classes + P.piece - 1) / P.piece);
     const long long most = std::min<long long>(P.piece, A.classes);

@@ -9,8 +9,8 @@ pytestmark = pytest.mark.gpu
 
 INF, NAN = float("inf"), float("nan")
 TYPES = [FP32, BF16, FP16]
-# logits in parts; more classes than are kept in parts, in few rows and in many; several pieces of the classes
-SHAPES = [(20, 64, 130), (90, 64, 130), (300, 64, 513), (70, 64, 20011), (600, 64, 20011)]
+# logits in parts; more classes than are kept in parts, in few rows and in many; few rows of large weights
+SHAPES = [(20, 64, 130), (90, 64, 130), (300, 64, 513), (70, 64, 20011), (600, 64, 20011), (20, 800, 15013)]
 SHAPE_IDS = ["x".join(map(str, s)) for s in SHAPES]
 
 

@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 @pytest.mark.parametrize("dtype", [FP32, BF16, FP16], ids=NAMES.get)
 @pytest.mark.parametrize("top", [None, 3])
-@pytest.mark.parametrize("rows,classes", [(5, 300), (300, 300), (700, 20011)])
+@pytest.mark.parametrize("rows,classes", [(5, 300), (300, 300), (700, 20011), (5, 70001)])
 @pytest.mark.parametrize("stride", [0, 8, 24, 56])
 def test_rows_closer_than_their_width(stride, rows, classes, top, dtype):
     c = Case(rows, 64, classes, dtype, top=top, bias=True, left=0.2)
