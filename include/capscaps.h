@@ -431,11 +431,14 @@ int capscaps_group_norm_bwd(const capscaps_group_norm* norm, const capscaps_grou
  * Infinities and NaN of a row that counts make its loss NaN or infinite by the formulas (a row whose every class is ruled out: NaN), and those
  * of a row's gradient reach dweight and dbias.
  *
- * Sums are held in fp32.  dtype is that of x, weight, dx and dweight.  The gradient of z is rounded to it once, piece by piece, as a gradient
- * that is stored; or to two terms of it, the rounding and that of what it leaves over, 16 bits that sums in fp32 and one rounding of dx and dweight cannot be told
- * from: `gradient_terms`.  (fp32: not rounded; fp32 values of 2^104 and more in magnitude count as infinite, and infinities there make their sums NaN.)  Pointers are device pointers, aligned to their
- * elements (16 bits with whole 16-byte vectors, rows of a multiple of 32 values: read in place, else copied to the workspace); strides, in
- * elements, are those from row to row and >= 0 (an input's rows may overlap, or be one row).  Outputs overlap nothing.  Runs repeat bit for bit.  Stream and error rules as for the calls above.
+ * Sums are held in fp32.  dtype is that of x, weight, dx and dweight.  In 16 bits the gradient of z is rounded to dtype once, as a gradient
+ * that is stored, or held in two terms of it, the rounding and that of what it leaves over, which costs dx and dweight no more than their own
+ * rounding: `gradient_terms`.  In fp32 it is not rounded; values of 2^104 and more in magnitude may count as infinite, and infinities then
+ * make their sums NaN (few rows with large weights take them as they are).
+ *
+ * Pointers are device pointers, aligned to their elements (16 bits with whole 16-byte vectors, rows of a multiple of 32 values: read
+ * in place, else copied to the workspace); strides, in elements, are those from row to row and >= 0 (an input's rows may overlap, or be one
+ * row).  Outputs overlap nothing.  Runs repeat bit for bit.  Stream and error rules as for the calls above.
  */
 typedef struct capscaps_head {
     long long rows;     /* 0 .. 2^20 */
