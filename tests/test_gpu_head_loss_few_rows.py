@@ -15,7 +15,8 @@ SIZES = pytest.mark.parametrize("width,classes", [(530, 300), LARGE])
 
 
 @pytest.mark.parametrize("rows", ROWS)
-@pytest.mark.parametrize("width,classes", [(803, 1501), (66, 129), (1280, 515), (5, 2000), LARGE, (4100, 3001), (130, 95003)])
+@pytest.mark.parametrize("width,classes", [(803, 1501), (66, 129), (1280, 515), (5, 2000), LARGE, (4100, 3001), (130, 95003),
+                                           (801, 20011), (61, 17001)])  # (more classes than the products of terms keep logits of)
 def test_class_loss(rows, width, classes):
     Case(rows, width, classes, FP32, bias=rows % 2 == 1, left=0.2).check()
 
